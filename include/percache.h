@@ -377,6 +377,118 @@ PERCACHE_API int percache_qa_top1(int32_t device, void* stream, const float* ban
                      const float* queries, int32_t n_queries, float tau_query, int32_t* best_index,
                      float* best_score, uint8_t* hit, float* kernel_us);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators on the cache of a decoding batch.  The paper's decode stage (Section 2.1) produces one token at a time
+ * against the keys and values of everything before it; these are the steps a server adds to it: verifying drafted
+ * tokens several at a time, and keeping a prompt's context within a budget of slots.  They work on caller-owned device
+ * memory, without a handle; percache_decode_tree, percache_accept and percache_evict_context run them on a handle's
+ * own context.
+ *
+ * Rules of this group
+ *  - The calls only enqueue work on `stream` (a cudaStream_t or NULL) of `device` and return: they do not synchronise,
+ *    allocate or copy to the host, keep nothing between calls, leave the calling thread's current device as it was, and
+ *    may be captured into a CUDA graph.  All array arguments are device memory of `device`, and must stay valid until
+ *    the work has run.  Everything that differs from step to step (lengths, page tables, masks) is read on the device,
+ *    so a captured call may be replayed after those arrays were rewritten in place.
+ *  - Sizes the host has to know are given as upper bounds (max_len, max_nodes).  Device-side values beyond them, or
+ *    negative ones, are clamped; a page id or slot outside the pools reads as zeros and is never written.
+ *  - Refused calls (PERCACHE_E_INVAL, PERCACHE_E_CAPACITY) enqueue nothing.
+ *  - A prompt without rows, or a batch without prompts or rows, is allowed; outputs of rows at or behind
+ *    row_start[n_seqs], and of slots behind a prompt's last one, are left as they were.
+ *  - Bounded waits: where a kernel of this group gives up a wait (PERCACHE_E_DEVICE_TIMEOUT elsewhere), it says so in
+ *    the workspace's first word, which percache_ops_status() reads. */
+#define PERCACHE_BF16 0
+#define PERCACHE_F16  1
+#define PERCACHE_MAX_TREE_NODES 256
+#define PERCACHE_OPS_WORKSPACE_BYTES (24u << 20)
+
+/* K and V of a batch.  A slot of a prompt is a row of the pools: row page_table[b][slot / 16] * 16 + slot % 16 when
+ * page_table is given, else row ctx_start[b] + slot.  In a row the heads lie one behind the other (head_dim elements
+ * each).  K is as the attention uses it (after position encoding). */
+typedef struct {
+  void*   k;                       /* 16-byte aligned                                                             */
+  void*   v;                       /* likewise; unused (may be NULL) by percache_attention_weights                */
+  int64_t k_slot_stride;           /* elements from one row to the next, a multiple of 8, at least
+                                      n_kv_heads * head_dim                                                       */
+  int64_t v_slot_stride;
+  int64_t n_slots;                 /* rows of each pool, at most 2^31 - 1                                         */
+  const int32_t* page_table;       /* [n_seqs][page_table_stride] page ids, or NULL                               */
+  const int32_t* ctx_start;        /* [n_seqs], used when page_table is NULL                                      */
+  int32_t page_table_stride;       /* entries a prompt, at least ceil(max_len / 16)                               */
+  int32_t n_kv_heads;
+  int32_t head_dim;                /* 64 or 128                                                                   */
+  int32_t dtype;                   /* PERCACHE_BF16 or PERCACHE_F16: of k, v, q and out                           */
+} percache_kv_t;
+
+/* The rows (drafted tokens, "nodes") of a batch.  Prompt b has ctx_len[b] context slots and
+ * n = row_start[b + 1] - row_start[b] nodes; node i is row row_start[b] + i, and its K and V are in slot
+ * ctx_len[b] + i.  It sees every context slot and the nodes j < n whose bit (j % 64 of word j / 64) is set in its row
+ * of `mask`, itself included only if its own bit is set; without a mask it sees nodes 0 .. i. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_rows;                  /* rows of q, out, lse (and of mask and use)                                   */
+  int32_t max_nodes;               /* most nodes of a prompt, 1 .. PERCACHE_MAX_TREE_NODES                        */
+  int32_t max_len;                 /* most slots of a prompt, its nodes included; at most 2^26                    */
+  const int32_t*  ctx_len;         /* [n_seqs]                                                                    */
+  const int32_t*  row_start;       /* [n_seqs + 1], ascending                                                     */
+  const uint64_t* mask;            /* [n_rows][mask_words] or NULL                                                */
+  int32_t mask_words;              /* at least ceil(max_nodes / 64)                                               */
+  int32_t reserved0;
+} percache_rows_t;
+
+/* Attention of every node over the slots it sees: out[row][head] = softmax(scale * q . K) V in fp32, rounded once
+ * to the pools' type on the way out (the softmax weights are rounded to that type before they multiply V, their sum is
+ * not), and lse[row][head] = log of the sum of exp(scale * q . k) over those slots (fp32; may be NULL).  A row that
+ * sees nothing gets zeros and -inf.  q, out: [n_rows][n_q_heads][head_dim] with q_row_stride / out_row_stride elements
+ * from row to row (multiples of 8, 16-byte aligned); n_q_heads a multiple of n_kv_heads with at most 128 query heads
+ * per KV head.  scale > 0.  Slots a row does not see may hold anything, infinities and NaN included.
+ * workspace: PERCACHE_OPS_WORKSPACE_BYTES, 256-byte aligned, zeroed once before its first use; calls that may run at
+ * the same time need a workspace each. */
+PERCACHE_API int percache_tree_attention(int32_t device, void* stream, const percache_kv_t* kv,
+                                         const percache_rows_t* rows, const void* q, int64_t q_row_stride,
+                                         int32_t n_q_heads, float scale, void* out, int64_t out_row_stride, float* lse,
+                                         void* workspace, int64_t workspace_bytes);
+
+/* Running attention weights (what eviction by accumulated weight goes by): for every prompt b, KV head g and slot s
+ *   weights_out[b][g][s] = decay * weights_in[b][g][s] + sum of exp(scale * q[r][h] . k[s][g] - lse[r][h])
+ * over the rows r of the prompt with use[r] != 0 (use NULL: all) that see s and the query heads h of g.  lse as
+ * percache_tree_attention wrote it (fp32 [n_rows][n_q_heads]); a row whose lse is -inf counts nothing.  Sums are kept
+ * in fp32 and in a fixed order.  weights_in, weights_out: fp32 [n_seqs][n_kv_heads][weights_stride], weights_stride >=
+ * max_len; they may be the same array.  decay 1 accumulates, a smaller one (>= 0) forgets; with decay 0 weights_in is
+ * not read and may be NULL. */
+PERCACHE_API int percache_attention_weights(int32_t device, void* stream, const percache_kv_t* kv,
+                                            const percache_rows_t* rows, const void* q, int64_t q_row_stride,
+                                            int32_t n_q_heads, float scale, const float* lse, const uint8_t* use,
+                                            float decay, const float* weights_in, float* weights_out,
+                                            int64_t weights_stride, void* workspace, int64_t workspace_bytes);
+
+/* The slots to keep: of the length[b] slots of prompt b and every head, all when there are at most `budget`, else
+ * `budget` of them: the first `sink`, the last `recent` (sink + recent <= budget), and the heaviest of the rest, equal
+ * weights going to the lower slot (NaN counts as -infinity).  weights: fp32 [n_seqs][n_heads][weights_stride],
+ * weights_stride >= max_len.  keep: int32 [n_seqs][n_heads][budget], ascending, -1 behind the last one;
+ * count[b] = min(length[b], budget). */
+PERCACHE_API int percache_select_slots(int32_t device, void* stream, const float* weights, int64_t weights_stride,
+                                       const int32_t* length, int32_t n_seqs, int32_t n_heads, int32_t max_len,
+                                       int32_t budget, int32_t sink, int32_t recent, int32_t* keep, int32_t* count);
+
+/* Move kept slots together: for every prompt b, KV head g and j < count[b], slot first[b] + j of the destination gets
+ * the K and V of slot keep[b][g][j] (first NULL: 0), and weights_out[b][g][first[b] + j] = weights_in[b][g][keep[b][g][j]]
+ * (weights NULL: none).  keep: int32 [n_seqs][keep_heads][budget] with keep_heads = n_kv_heads, or 1 for a list that all
+ * heads share.  An index outside 0 .. max_len - 1, or a destination slot at or past max_len, moves nothing.
+ * dst_page_table / dst_start (as page_table / ctx_start of kv) NULL: in place; a list must then be strictly ascending
+ * with keep[j] >= first + j.  Else the destination's rows must not be rows that are read.  weights_in and weights_out
+ * may be the same array under the same rule as in place, with weights_stride >= max_len. */
+PERCACHE_API int percache_compact_slots(int32_t device, void* stream, const percache_kv_t* kv, int32_t n_seqs,
+                                        int32_t max_len, const int32_t* dst_page_table,
+                                        int32_t dst_page_table_stride, const int32_t* dst_start, const int32_t* first,
+                                        const int32_t* keep, int32_t keep_heads, int32_t budget, const int32_t* count,
+                                        const float* weights_in, float* weights_out, int64_t weights_stride);
+
+/* Waits for `stream` and reads the workspace's first word: PERCACHE_E_DEVICE_TIMEOUT if a wait of a call that used
+ * this workspace ran out since it was last zeroed (outputs of calls since then are invalid), PERCACHE_E_CUDA if the
+ * stream reports an error. */
+PERCACHE_API int percache_ops_status(int32_t device, void* stream, const void* workspace);
+
 PERCACHE_API const char* percache_strerror(int code);
 
 #ifdef __cplusplus

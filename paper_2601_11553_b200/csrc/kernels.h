@@ -194,6 +194,81 @@ int make_paged_attn_maps(AttnMaps* out, const __nv_bfloat16* qpool_layer, const 
 void launch_attention_merge(const AttnMerge* merges, int n_merges, const float* partial_o, const float* partial_ml,
                             __half* out, int n_q_heads, int n_kv_heads, cudaStream_t s);
 
+// ---- operators on the cache of a decoding batch (attn_tree.cu, slots.cu; entry points in ops_api.cu)
+struct KvView {                // percache_kv_t
+  const void *k, *v;
+  int64_t k_stride, v_stride;  // elements
+  int64_t n_slots;
+  const int32_t *page_table, *ctx_start;
+  int32_t pt_stride, n_kv_heads, head_dim, bf16;
+};
+struct TreeRows {              // percache_rows_t
+  int32_t n_seqs, n_rows, max_nodes, max_len;
+  const int32_t *ctx_len, *row_start;
+  const uint64_t* mask;
+  int32_t mask_words;
+};
+struct TreeAttention {
+  KvView kv;
+  TreeRows rows;
+  const void* q;
+  int64_t q_stride;
+  int32_t n_q_heads;
+  float scale;
+  void* out;
+  int64_t out_stride;
+  float* lse;
+  void* workspace;
+};
+struct AttentionWeights {
+  KvView kv;
+  TreeRows rows;
+  const void* q;
+  int64_t q_stride;
+  int32_t n_q_heads;
+  float scale;
+  const float* lse;
+  const uint8_t* use;
+  float decay;
+  const float* w_in;
+  float* w_out;
+  int64_t w_stride;
+  void* workspace;
+};
+struct CompactSlots {
+  KvView kv;
+  int32_t n_seqs, max_len;
+  const int32_t *dst_page_table, *dst_start, *first, *keep, *count;
+  int32_t dst_pt_stride, keep_heads, budget;
+  const float* w_in;
+  float* w_out;
+  int64_t w_stride;
+};
+// each returns 0, or -1 when a launch failed
+int launch_tree_attention(const TreeAttention& a, int n_sms, cudaStream_t s);
+int launch_attention_weights(const AttentionWeights& a, int n_sms, cudaStream_t s);
+int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
+                        int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s);
+int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s);
+
+// A prompt's part of a batch, from the device-side arrays, clamped to the bounds the host knows.
+struct SeqPart { int row0, n_nodes, ctx_len; };
+__device__ __forceinline__ SeqPart seq_part(const TreeRows& r, int b) {
+  SeqPart p;
+  p.row0 = min(max(__ldg(r.row_start + b), 0), r.n_rows);
+  const int end = min(max(__ldg(r.row_start + b + 1), p.row0), r.n_rows);
+  p.n_nodes = min(min(end - p.row0, r.max_nodes), r.max_len);
+  p.ctx_len = min(max(__ldg(r.ctx_len + b), 0), r.max_len - p.n_nodes);
+  return p;
+}
+// Pool row of a prompt's slot, or -1 when it lies outside the pool.
+__device__ __forceinline__ int64_t slot_row(const int32_t* page_table, int pt_stride, const int32_t* start, int64_t n_slots,
+                                            int b, int slot) {
+  const int64_t r = page_table ? static_cast<int64_t>(__ldg(page_table + static_cast<size_t>(b) * pt_stride + slot / PAGE_TOKENS)) * PAGE_TOKENS + slot % PAGE_TOKENS
+                               : static_cast<int64_t>(__ldg(start + b)) + slot;
+  return r >= 0 && r < n_slots ? r : -1;
+}
+
 int init_driver_api();   // resolves cuTensorMapEncodeTiled once; 0 on success
 
 // Kernel attributes (dynamic shared memory limit) and cluster occupancy belong to a device, not to the process:

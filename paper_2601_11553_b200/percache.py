@@ -34,7 +34,8 @@ PHASES = ("gather", "norm", "qkv", "attn", "oproj", "gateup", "down", "io")
 EXPORTS = ("percache_create", "percache_destroy", "percache_put_chunk_kv", "percache_prefill",
            "percache_has_chunk", "percache_drop_chunk", "percache_get_chunk_kv", "percache_get_chunk_q", "percache_put_chunk_synthetic",
            "percache_get_stats", "percache_set_flags", "percache_decode", "percache_set_decode_reserve", "percache_set_store_limit", "percache_chunk_info", "percache_debug_read_plan", "percache_debug_read_ctx", "percache_debug_attn_plan",
-           "percache_debug_gemm", "percache_debug_gemm_noalloc", "percache_debug_capture_layers", "percache_debug_wait_probe", "percache_path_key", "percache_qa_top1", "percache_strerror")
+           "percache_debug_gemm", "percache_debug_gemm_noalloc", "percache_debug_capture_layers", "percache_debug_wait_probe", "percache_path_key", "percache_qa_top1", "percache_tree_attention",
+           "percache_attention_weights", "percache_select_slots", "percache_compact_slots", "percache_ops_status", "percache_strerror")
 
 
 class PerCacheError(RuntimeError):
@@ -76,6 +77,18 @@ class StatsStruct(C.Structure):
                 ("gather_free", C.c_int32), ("reserved0", C.c_int32)]
 
 
+class KvStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_slot_stride", C.c_int64), ("v_slot_stride", C.c_int64),
+                ("n_slots", C.c_int64), ("page_table", C.c_void_p), ("ctx_start", C.c_void_p),
+                ("page_table_stride", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class RowsStruct(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_nodes", C.c_int32), ("max_len", C.c_int32),
+                ("ctx_len", C.c_void_p), ("row_start", C.c_void_p), ("mask", C.c_void_p), ("mask_words", C.c_int32),
+                ("reserved0", C.c_int32)]
+
+
 _lib = None
 
 
@@ -112,6 +125,12 @@ def load_library() -> C.CDLL:
     lib.percache_debug_capture_layers.argtypes = [vp, vp, i64]
     lib.percache_debug_wait_probe.argtypes = [i32, C.c_uint32, C.POINTER(i32), C.POINTER(u64)]
     lib.percache_qa_top1.argtypes = [i32, vp, vp, i32, i32, vp, i32, C.c_float, vp, vp, vp, C.POINTER(C.c_float)]
+    f32, kvp, rowsp = C.c_float, C.POINTER(KvStruct), C.POINTER(RowsStruct)
+    lib.percache_tree_attention.argtypes = [i32, vp, kvp, rowsp, vp, i64, i32, f32, vp, i64, vp, vp, i64]
+    lib.percache_attention_weights.argtypes = [i32, vp, kvp, rowsp, vp, i64, i32, f32, vp, vp, f32, vp, vp, i64, vp, i64]
+    lib.percache_select_slots.argtypes = [i32, vp, vp, i64, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.percache_compact_slots.argtypes = [i32, vp, kvp, i32, i32, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, i64]
+    lib.percache_ops_status.argtypes = [i32, vp, vp]
     lib.percache_path_key.argtypes = [C.POINTER(u64), i32]
     lib.percache_path_key.restype = u64
     lib.percache_strerror.argtypes = [C.c_int]
@@ -450,3 +469,148 @@ def qa_top1(bank: Any, queries: Any, tau_query: float, device: int = 0, stream: 
                                            C.c_float(tau_query), _ptr(idx), _ptr(score), _ptr(hit),
                                            C.byref(us) if timing else None), "percache_qa_top1")
     return (idx, score, hit, float(us.value)) if timing else (idx, score, hit)
+
+
+# ---------------------------------------------------------------------- operators on a decoding batch's cache
+OPS_WORKSPACE_BYTES = 24 << 20
+MAX_TREE_NODES = 256
+_KV_TYPES = {"torch.bfloat16": 0, "torch.float16": 1}
+
+
+def _arg(x: Any, name: str, dtype: Any, device: int, shape: Optional[Sequence[Optional[int]]] = None) -> int:
+    """Address of a contiguous device tensor of the given type(s) and shape (None: any extent); 0 for None."""
+    if x is None:
+        return 0
+    if not x.is_cuda or x.device.index != device:
+        raise ValueError(f"{name}: expected a tensor on cuda:{device}")
+    if str(x.dtype) != dtype and str(x.dtype) not in dtype.split("|"):
+        raise ValueError(f"{name}: expected {dtype}, got {x.dtype}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    if shape is not None and (len(x.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape))):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _row_stride(x: Any, name: str, heads: int, head_dim: int) -> int:
+    """Elements between the rows of a [rows, heads, head_dim] tensor whose heads and elements lie one behind the other."""
+    st = x.stride()
+    if len(st) != 3 or x.shape[1] != heads or x.shape[2] != head_dim or st[2] != 1 or (heads > 1 and st[1] != head_dim):
+        raise ValueError(f"{name}: expected [rows, {heads}, {head_dim}] with dense heads")
+    return st[0] if x.shape[0] > 1 else max(st[0], heads * head_dim)
+
+
+def _kv(k: Any, v: Any, page_table: Any, ctx_start: Any, n_seqs: int) -> KvStruct:
+    if len(k.shape) != 3 or not k.is_cuda:
+        raise ValueError("k: expected a [slots, kv_heads, head_dim] tensor on a CUDA device")
+    kind = _KV_TYPES.get(str(k.dtype))
+    if kind is None:
+        raise ValueError(f"k: expected bfloat16 or float16, got {k.dtype}")
+    slots, heads, dim = k.shape
+    dev = k.device.index
+    ks = _row_stride(k, "k", heads, dim)
+    vs, vp = 0, None
+    if v is not None:
+        if v.dtype != k.dtype or v.device != k.device or v.shape[0] != slots:
+            raise ValueError("v: expected k's type, device and number of slots")
+        vs, vp = _row_stride(v, "v", heads, dim), v.data_ptr()
+    if (page_table is None) == (ctx_start is None):
+        raise ValueError("give either page_table or ctx_start")
+    pt = _arg(page_table, "page_table", "torch.int32", dev, (n_seqs, None))
+    cs = _arg(ctx_start, "ctx_start", "torch.int32", dev, (n_seqs,))
+    return KvStruct(k.data_ptr(), vp, ks, vs, slots, pt or None, cs or None, page_table.shape[1] if pt else 0, heads, dim, kind)
+
+
+def _rows(q: Any, k: Any, ctx_len: Any, row_start: Any, mask: Any, max_nodes: int, max_len: int) -> RowsStruct:
+    dev = k.device.index
+    if q.dtype != k.dtype or q.device != k.device:
+        raise ValueError("q: expected k's type and device")
+    n_seqs, n_rows = ctx_len.shape[0], q.shape[0]
+    m = _arg(mask, "mask", "torch.int64|torch.uint64", dev, (n_rows, None))
+    return RowsStruct(n_seqs, n_rows, max_nodes, max_len, _arg(ctx_len, "ctx_len", "torch.int32", dev, (n_seqs,)) or None,
+                      _arg(row_start, "row_start", "torch.int32", dev, (n_seqs + 1,)) or None, m or None,
+                      mask.shape[1] if m else 0, 0)
+
+
+def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len: Any, row_start: Any, max_nodes: int,
+                   max_len: int, workspace: Any, mask: Any = None, page_table: Any = None, ctx_start: Any = None,
+                   scale: Optional[float] = None, stream: int = 0) -> Any:
+    """percache_tree_attention: attention of drafted tokens (a tree, a chain, one token a prompt) over the cache.
+
+    q, out: [rows, q_heads, head_dim]; k, v: [slots, kv_heads, head_dim] (pages: slots = 16 x pages); lse: fp32
+    [rows, q_heads] or None; mask: int64 words [rows, ceil(max_nodes / 64)] or None (node i sees nodes 0 .. i); workspace:
+    uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` and returns `out`."""
+    dev = k.device.index
+    kv = _kv(k, v, page_table, ctx_start, ctx_len.shape[0])
+    rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
+    hq, d = q.shape[1], kv.head_dim
+    if out.dtype != q.dtype or out.device != q.device or out.shape != q.shape:
+        raise ValueError("out: expected q's type, device and shape")
+    _check(load_library().percache_tree_attention(
+        dev, stream, kv, rows, q.data_ptr(), _row_stride(q, "q", hq, d), hq, d ** -0.5 if scale is None else scale,
+        out.data_ptr(), _row_stride(out, "out", hq, d), _arg(lse, "lse", "torch.float32", dev, (q.shape[0], hq)),
+        _arg(workspace, "workspace", "torch.uint8", dev), workspace.numel()), "percache_tree_attention")
+    return out
+
+
+def attention_weights(q: Any, k: Any, lse: Any, weights: Any, weights_out: Any = None, *, ctx_len: Any, row_start: Any,
+                      max_nodes: int, max_len: int, workspace: Any, mask: Any = None, use: Any = None,
+                      page_table: Any = None, ctx_start: Any = None, scale: Optional[float] = None, decay: float = 1.0,
+                      stream: int = 0) -> Any:
+    """percache_attention_weights: weights_out = decay * weights + the softmax weights of the rows with use != 0, summed
+    per slot over the rows and the query heads of a KV head.  weights: fp32 [seqs, kv_heads, slots]; weights_out None: in
+    place.  Enqueues on `stream` and returns weights_out."""
+    dev = k.device.index
+    n_seqs = ctx_len.shape[0]
+    kv = _kv(k, None, page_table, ctx_start, n_seqs)
+    rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
+    hq = q.shape[1]
+    weights_out = weights if weights_out is None else weights_out
+    shape = (n_seqs, kv.n_kv_heads, weights_out.shape[2])
+    _check(load_library().percache_attention_weights(
+        dev, stream, kv, rows, q.data_ptr(), _row_stride(q, "q", hq, kv.head_dim), hq,
+        kv.head_dim ** -0.5 if scale is None else scale, _arg(lse, "lse", "torch.float32", dev, (q.shape[0], hq)),
+        _arg(use, "use", "torch.uint8|torch.bool", dev, (q.shape[0],)), decay,
+        _arg(weights, "weights", "torch.float32", dev, shape), _arg(weights_out, "weights_out", "torch.float32", dev, shape),
+        shape[2], _arg(workspace, "workspace", "torch.uint8", dev), workspace.numel()), "percache_attention_weights")
+    return weights_out
+
+
+def select_slots(weights: Any, length: Any, keep: Any, count: Any, *, sink: int = 0, recent: int = 0,
+                 max_len: Optional[int] = None, stream: int = 0) -> Any:
+    """percache_select_slots: keep [seqs, heads, budget] (int32, ascending, -1 behind the last) and count [seqs] of the
+    slots that stay: the first `sink`, the last `recent`, and the heaviest of the rest."""
+    n_seqs, heads, width = weights.shape
+    dev = weights.device.index
+    _check(load_library().percache_select_slots(
+        dev, stream, _arg(weights, "weights", "torch.float32", dev), width, _arg(length, "length", "torch.int32", dev, (n_seqs,)),
+        n_seqs, heads, width if max_len is None else max_len, keep.shape[2], sink, recent,
+        _arg(keep, "keep", "torch.int32", dev, (n_seqs, heads, None)), _arg(count, "count", "torch.int32", dev, (n_seqs,))),
+        "percache_select_slots")
+    return keep, count
+
+
+def compact_slots(k: Any, v: Any, keep: Any, count: Any, *, max_len: int, weights: Any = None, weights_out: Any = None,
+                  first: Any = None, page_table: Any = None, ctx_start: Any = None, dst_page_table: Any = None,
+                  dst_start: Any = None, stream: int = 0) -> None:
+    """percache_compact_slots: slot first[b] + j of the destination takes the K, V and weight of slot keep[b][head][j].
+    Without dst_page_table / dst_start in place (keep strictly ascending, keep[j] >= first + j); weights_out None: the
+    weights in place."""
+    dev = k.device.index
+    n_seqs = count.shape[0]
+    kv = _kv(k, v, page_table, ctx_start, n_seqs)
+    weights_out = weights if weights_out is None else weights_out
+    width = 0 if weights is None else weights.shape[2]
+    shape = (n_seqs, kv.n_kv_heads, width)
+    _check(load_library().percache_compact_slots(
+        dev, stream, kv, n_seqs, max_len, _arg(dst_page_table, "dst_page_table", "torch.int32", dev, (n_seqs, None)),
+        0 if dst_page_table is None else dst_page_table.shape[1], _arg(dst_start, "dst_start", "torch.int32", dev, (n_seqs,)),
+        _arg(first, "first", "torch.int32", dev, (n_seqs,)), _arg(keep, "keep", "torch.int32", dev, (n_seqs, None, None)),
+        keep.shape[1], keep.shape[2], _arg(count, "count", "torch.int32", dev, (n_seqs,)),
+        _arg(weights, "weights", "torch.float32", dev, shape), _arg(weights_out, "weights_out", "torch.float32", dev, shape),
+        width), "percache_compact_slots")
+
+
+def ops_status(workspace: Any, stream: int = 0) -> None:
+    """percache_ops_status: waits for `stream`; raises PerCacheError if a call that used this workspace gave up a wait."""
+    _check(load_library().percache_ops_status(workspace.device.index, stream, workspace.data_ptr()), "percache_ops_status")
