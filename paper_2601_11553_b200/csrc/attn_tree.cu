@@ -1,4 +1,31 @@
-// Attention of drafted tokens over a cached context, and the running attention weights of its slots.
+// Attention of drafted tokens over a cached context, and the running attention weights of its slots, on tcgen05.
+//
+// Rows.  The nodes of a prompt and the query heads of one KV head are packed into the 128 rows of one MMA tile (row =
+// node * group + head): all of them read the same K and V, so a K or V byte that reaches shared memory serves every
+// row.  A unit of work is (prompt, tile of nodes, KV head); its context is cut into blocks of 128 slots.
+//
+// Bounds.  A block costs 64 KB of K and V (head size 128, 1.5 us of one SM's share of the HBM) and at most 8.4 MFLOP of
+// tensor work (0.75 us) and 16 K exponentials (0.55 us): with the tile at most 128 rows high the operator is bound by
+// reading K and V once, whatever the number of rows, and everything below serves to keep the copies running.
+//
+// Schedule.  Lengths live on the device, so the work is dealt there: every unit costs its blocks plus UNIT_COST, the
+// batch's total cost is cut into one contiguous span per CTA, and a unit that a span border cuts is finished in parts
+// whose unnormalised results a second kernel merges.  Every CTA forms the same prefix sums, so nothing is exchanged.
+//
+// One CTA per SM, 384 threads:
+//   warp 8       copies: Q tile, then K and V tiles in the order the MMAs take them (K0 K1 V0 K2 V1 ...) into one ring
+//   warp 9       MMA issuer: S = Q K^T of block j into the score buffer of j's parity, O += P V
+//   warps 0-3    softmax of the even blocks, warps 4-7 of the odd ones (thread = row), each parity with an O of its own:
+//                two blocks are always under way, so the chain S -> softmax -> PV of one hides behind the other's
+//   warps 10-11  clean the V tiles that hold drafted or no slots (see below)
+// TMEM (512 columns): O_0 [0,128) O_1 [128,256) S_0 [256,384) S_1 [384,512), P over the first half of its S.
+//
+// What a row does not see.  Scores are replaced (not added to) where a slot is invisible, so a K of NaN does no harm;
+// but 0 * V is NaN where V is infinite or NaN.  The only slots some rows see and others do not are the drafted ones: in
+// the V tiles that hold them warps 10-11 put zeros behind the prompt's last slot, and wherever a drafted V is not finite;
+// the latter raises a flag, and the rows that do see such a value get it added when they are written.
+#include <algorithm>
+
 #include "kernels.h"
 #include "ptx.cuh"
 
@@ -6,8 +33,701 @@ namespace pc {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int TREE_WARPS = 4;
+constexpr float LN2 = 0.6931471805599453f;
+constexpr int BLK = 128;                        // context slots per block, rows per tile
+constexpr int TREE_THREADS = 384;
+constexpr int RING_BYTES = 160 * 1024;
+constexpr int Q_BYTES = 32 * 1024;
+constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
+constexpr int MAX_STAGES = 10;
+constexpr uint32_t TMEM_S = 256;
+constexpr float RESCALE_THRESHOLD = 8.0f;       // the running reference is raised when a block exceeds it by 2^8
+constexpr int UNIT_COST = 2;                    // what a unit costs beside its blocks (Q, the row's end), in blocks
+constexpr int MIN_SPAN = 4;                     // least cost of a span: shorter ones cost more to merge than they save
+constexpr int FLAGS = 8;
 
+// Workspace: the error word, one merge record per CTA, partial results (two slots per CTA).
+constexpr int WS_MERGE = 256, WS_ML = 16384;
+constexpr int MAX_CTAS = 160;
+constexpr size_t WS_O = WS_ML + sizeof(float) * 2 * BLK * 2 * MAX_CTAS;
+static_assert(WS_MERGE + sizeof(int) * 8 * MAX_CTAS <= WS_ML, "");
+static_assert(WS_O + sizeof(float) * 2 * MAX_CTAS * BLK * HEAD_DIM <= (24u << 20), "PERCACHE_OPS_WORKSPACE_BYTES");
+
+struct MergeRecord {             // written by the CTA that has a cut unit's first part
+  int32_t n_parts;               // 0: none
+  int32_t row0, n_rows;          // first global row of the tile, valid tile rows
+  int32_t head0, cta;
+  int32_t pad[3];
+};
+
+struct TreeParams {
+  KvView kv;
+  TreeRows rows;
+  int32_t n_q_heads, group, tile_nodes;
+  float scale_log2;
+  void* out;
+  int64_t out_stride;
+  float* lse;
+  int* err_word;
+  MergeRecord* merges;
+  float *partial_ml, *partial_o;
+};
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Two values in the pools' type.  A finite value past fp16's range (an average of values at its limit, rounded up) becomes the
+// largest finite one; infinity stays infinity.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float a, float b) {
+  if constexpr (BF16) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&v);
+  } else {
+    if (isinf(a) || isinf(b)) {
+      const uint32_t lo = __half_as_ushort(isinf(a) ? __float2half_rn(a) : to_half_sat(a));
+      const uint32_t hi = __half_as_ushort(isinf(b) ? __float2half_rn(b) : to_half_sat(b));
+      return lo | (hi << 16);
+    }
+    return pack_half2(a, b);
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ float elem(uint32_t bits16) {
+  if constexpr (BF16) return __uint_as_float(bits16 << 16);
+  else return __half2float(__ushort_as_half(static_cast<unsigned short>(bits16)));
+}
+
+// ---------------------------------------------------------------------------------------------------- schedule
+struct Span { int64_t begin, end, total; int n_ctas, seq; int64_t seq_start; };
+struct Item {
+  int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes
+  int row0, node0, n_rows;       // the tile: first global row, first node, valid tile rows
+  int g, blk_begin, blk_end, n_blk;
+  int64_t unit_end;              // cost position behind the unit
+};
+
+__device__ __forceinline__ int64_t seq_cost(const TreeParams& a, const SeqPart& p) {
+  if (p.n_nodes == 0) return 0;
+  const int tiles = (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes;
+  return static_cast<int64_t>((p.ctx_len + p.n_nodes + BLK - 1) / BLK + UNIT_COST) * tiles * a.kv.n_kv_heads;
+}
+
+// The CTA's span and the prompt it starts in: block-wide, every thread takes a run of prompts.
+__device__ __forceinline__ void make_span(const TreeParams& a, Span* sp, int64_t* warp_sums) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (a.rows.n_seqs + TREE_THREADS - 1) / TREE_THREADS;
+  const int b0 = min(tid * per, a.rows.n_seqs), b1 = min(b0 + per, a.rows.n_seqs);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += seq_cost(a, seq_part(a.rows, b));
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) warp_sums[warp] = incl;
+  __syncthreads();
+  int64_t before = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < TREE_THREADS / 32; ++w) {
+    const int64_t x = warp_sums[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / MIN_SPAN, static_cast<int64_t>(1))));
+  const int c = blockIdx.x;
+  const int64_t begin = c < n ? total * c / n : total, end = c < n ? total * (c + 1) / n : total;
+  if (tid == 0) { sp->begin = begin; sp->end = end; sp->total = total; sp->n_ctas = n; sp->seq = a.rows.n_seqs; sp->seq_start = total; }
+  __syncthreads();
+  if (mine > 0 && begin >= before && begin < before + mine) {         // one thread at most
+    int b = b0;
+    int64_t at = before;
+    for (; b < b1; ++b) {
+      const int64_t cost = seq_cost(a, seq_part(a.rows, b));
+      if (begin < at + cost) break;
+      at += cost;
+    }
+    sp->seq = b;
+    sp->seq_start = at;
+  }
+  __syncthreads();
+}
+
+struct Cursor {
+  int64_t pos, end, seq_start;
+  int seq;
+  __device__ __forceinline__ explicit Cursor(const Span& s) : pos(s.begin), end(s.end), seq_start(s.seq_start), seq(s.seq) {}
+  __device__ __forceinline__ bool next(const TreeParams& a, Item* it) {
+    while (pos < end && seq < a.rows.n_seqs) {
+      const SeqPart p = seq_part(a.rows, seq);
+      const int64_t whole = seq_cost(a, p);
+      if (pos >= seq_start + whole) { seq_start += whole; ++seq; continue; }
+      const int tiles = (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes;
+      const int n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK, cost = n_blk + UNIT_COST;
+      const int64_t rel = pos - seq_start;
+      const int unit = static_cast<int>(rel / cost);
+      const int64_t unit_start = seq_start + static_cast<int64_t>(unit) * cost, unit_end = unit_start + cost;
+      const int64_t stop = min(end, unit_end);
+      // a unit's own cost lies ahead of its blocks: a border inside it leaves the whole unit to the later span
+      const int bb = max(static_cast<int>(pos - unit_start) - UNIT_COST, 0), be = max(static_cast<int>(stop - unit_start) - UNIT_COST, 0);
+      pos = stop;
+      if (be <= bb) continue;
+      const int tile = unit % tiles;                  // the tiles of one KV head follow each other: they share K and V in L2
+      it->seq = seq; it->ctx_len = p.ctx_len; it->n_nodes = p.n_nodes;
+      it->node0 = tile * a.tile_nodes;
+      it->row0 = p.row0 + it->node0;
+      it->n_rows = min(a.tile_nodes, p.n_nodes - it->node0) * a.group;
+      it->g = unit / tiles;
+      it->blk_begin = bb; it->blk_end = be; it->n_blk = n_blk; it->unit_end = unit_end;
+      return true;
+    }
+    return false;
+  }
+};
+
+// Bits of the nodes j0 .. j0 + 31 (j0 may be negative) that a node sees.
+__device__ __forceinline__ uint32_t node_bits(const TreeRows& r, int row, int node, int n_nodes, int j0) {
+  if (j0 <= -32 || j0 >= n_nodes) return 0u;
+  const int lo = max(j0, 0);
+  uint64_t w = 0;
+  if (r.mask != nullptr) {
+    const uint64_t* m = r.mask + static_cast<size_t>(row) * r.mask_words;
+    w = __ldg(m + (lo >> 6)) >> (lo & 63);
+    if ((lo & 63) != 0 && (lo >> 6) + 1 < r.mask_words) w |= __ldg(m + (lo >> 6) + 1) << (64 - (lo & 63));
+  } else if (node >= lo) {
+    w = node - lo >= 63 ? ~0ull : (1ull << (node - lo + 1)) - 1;
+  }
+  if (n_nodes - lo < 64) w &= (1ull << (n_nodes - lo)) - 1;
+  return static_cast<uint32_t>(w << (lo - j0));
+}
+// Bits of the 32 slots from slot0 on that a node sees.
+__device__ __forceinline__ uint32_t slot_bits(const TreeRows& r, const Item& it, int row, int node, int slot0) {
+  const int in_ctx = it.ctx_len - slot0;
+  if (in_ctx >= 32) return 0xffffffffu;
+  return (in_ctx > 0 ? (1u << in_ctx) - 1 : 0u) | node_bits(r, row, node, it.n_nodes, -in_ctx);
+}
+
+// ---------------------------------------------------------------------------------------------------- attention
+template <int D, bool BF16>
+__global__ void __launch_bounds__(TREE_THREADS, 1)
+tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                      const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TreeParams a) {
+  constexpr int HALVES = D / 64;                         // 64-column halves of a tile, 16 KB each
+  constexpr int HALF_BYTES = BLK * 128;
+  constexpr int TILE_BYTES = HALVES * HALF_BYTES;
+  constexpr int STAGES = RING_BYTES / TILE_BYTES;
+  static_assert(STAGES <= MAX_STAGES, "");
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t q_full, q_empty, full[MAX_STAGES], empty[MAX_STAGES], raw[MAX_STAGES], s_full[2], p_full[2], o_full, o_free, ml_full;
+  __shared__ float ml[2][2][BLK][2];                     // [item parity][block parity][row]: reference, sum
+  __shared__ int bad_v[FLAGS][2];
+  __shared__ Span span;
+  __shared__ int64_t warp_sums[TREE_THREADS / 32];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int cta_failed;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = q_smem + Q_BYTES;
+
+  if (threadIdx.x == 0) {
+    cta_failed = 0;
+    mbar_init(&q_full, 1); mbar_init(&q_empty, 1);
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 1); mbar_init(&raw[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
+    mbar_init(&o_full, 1); mbar_init(&o_free, 8); mbar_init(&ml_full, 8);
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc<512>(&tmem_slot);
+    tmem_relinquish();
+  }
+  if (warp == 8 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
+  pdl_launch_dependents();
+  pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
+  make_span(a, &span, warp_sums);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = tmem_slot;
+  // 384 threads start with 168 registers each (64 512); the softmax holds a whole row of scores and wants more, the other
+  // warpgroup needs few: 256 x 208 + 128 x 80 = 63 488
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    Cursor cur(span);
+    Item it{};
+   if (warp == 8) {
+    // ------------------------------------------------------------ copies
+    uint32_t n_item = 0, n_tile = 0, n_raw = 0;
+    MergeRecord rec{};
+    bool ok = true;
+    const int pg = lane & 7, hf = (lane >> 3) & 1;
+    auto load = [&](const CUtensorMap* tm, int blk, bool clean) {
+      const int st = n_tile % STAGES;
+      const uint32_t ph = (n_tile / STAGES) & 1u;
+      ++n_tile;
+      int page = 0;
+      if (a.kv.page_table) {           // pages behind the prompt's last slot repeat its last page: masked either way
+        const int last = (it.ctx_len + it.n_nodes - 1) / PAGE_TOKENS;
+        page = __ldg(a.kv.page_table + static_cast<size_t>(it.seq) * a.kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + pg, last));
+      } else if (lane == 0) {
+        page = __ldg(a.kv.ctx_start + it.seq);
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(&empty[st], ph ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+      if (!ok) return;
+      // a tile that warps 10-11 have to clean lands on a barrier of theirs; they then complete `full` in its place
+      uint64_t* bar = clean ? &raw[n_raw++ % STAGES] : &full[st];
+      if (lane == 0) mbar_arrive_expect_tx(bar, TILE_BYTES);
+      if (lane == 1 && !clean) mbar_arrive(bar);
+      __syncwarp();
+      uint8_t* dst = ring + st * TILE_BYTES;
+      if (a.kv.page_table) {
+        if (lane < 8 * HALVES)
+          tma_load_2d(dst + hf * HALF_BYTES + pg * (PAGE_TOKENS * 128), tm, bar, it.g * D + hf * 64, page * PAGE_TOKENS);
+      } else if (lane == 0) {
+        for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * HALF_BYTES, tm, bar, it.g * D + h * 64, page + blk * BLK);
+      }
+    };
+    while (ok && cur.next(a, &it)) {
+      if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
+        rec.n_parts = static_cast<int>((it.unit_end * span.n_ctas - 1) / span.total) - static_cast<int>(blockIdx.x) + 1;
+        rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group; rec.cta = blockIdx.x;
+      }
+      const int nb = it.blk_end - it.blk_begin;
+      ok = __all_sync(0xffffffffu, mbar_wait(&q_empty, (n_item & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+      if (!ok) break;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&q_full, HALVES * a.tile_nodes * a.group * 128);
+        for (int h = 0; h < HALVES; ++h) tma_load_3d(q_smem + h * HALF_BYTES, &tmQ, &q_full, h * 64, it.g * a.group, it.row0);
+      }
+      __syncwarp();
+      load(&tmK, it.blk_begin, false);
+      if (ok && nb > 1) load(&tmK, it.blk_begin + 1, false);
+      for (int j = 0; j < nb && ok; ++j) {
+        load(&tmV, it.blk_begin + j, (it.blk_begin + j + 1) * BLK > it.ctx_len);
+        if (ok && j + 2 < nb) load(&tmK, it.blk_begin + j + 2, false);
+      }
+      ++n_item;
+    }
+    if (!ok) cta_failed = 1;
+    if (lane == 0) a.merges[blockIdx.x] = rec;
+   } else if (warp == 9) {
+    // ------------------------------------------------------------ MMA issuer
+    if (lane == 0) {
+      constexpr uint32_t idesc_qk = make_idesc_f16(BLK, BLK, BF16 ? 1 : 0, 0, 0);
+      constexpr uint32_t idesc_pv = make_idesc_f16(BLK, D, BF16 ? 1 : 0, 0, 1);
+      uint32_t n_item = 0, n_tile = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok && !mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
+      };
+      const uint32_t qa = smem_u32(q_smem);
+      auto issue_s = [&](int i) {
+        const int st = n_tile % STAGES;
+        wait(&full[st], (n_tile / STAGES) & 1u);
+        ++n_tile;
+        if (!ok) return;
+        tc_fence_after_sync();
+        const uint32_t ka = smem_u32(ring + st * TILE_BYTES);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
+          umma_ss(tmem + TMEM_S + i * BLK, make_smem_desc_sw128(qa + off, 16, 1024), make_smem_desc_sw128(ka + off, 16, 1024), idesc_qk, kk != 0);
+        }
+        umma_commit(&s_full[i]);
+        umma_commit(&empty[st]);
+      };
+      while (ok && cur.next(a, &it)) {
+        const int nb = it.blk_end - it.blk_begin;
+        wait(&q_full, n_item & 1u);
+        issue_s(0);
+        if (nb > 1) issue_s(1);
+        if (nb <= 2 && ok) umma_commit(&q_empty);
+        for (int j = 0; j < nb && ok; ++j) {
+          const int i = j & 1;
+          const int st = n_tile % STAGES;
+          wait(&p_full[i], (p_phase >> i) & 1u);
+          p_phase ^= 1u << i;
+          if (j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
+          wait(&full[st], (n_tile / STAGES) & 1u);
+          ++n_tile;
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t va = smem_u32(ring + st * TILE_BYTES);
+#pragma unroll
+          for (int kk = 0; kk < BLK / 16; ++kk)
+            umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, make_smem_desc_sw128(va + kk * 2048, HALF_BYTES, 1024), idesc_pv,
+                    j > 1 || kk != 0);
+          umma_commit(&empty[st]);
+          if (j + 1 == nb) umma_commit(&o_full);
+          if (j + 2 < nb) {
+            issue_s(i);
+            if (j + 3 == nb && ok) umma_commit(&q_empty);
+          }
+        }
+        ++n_item;
+      }
+      if (!ok) cta_failed = 1;
+    }
+   } else {
+    // ------------------------------------------------------------ V tiles with drafted or no slots
+    const int tid = threadIdx.x - 320;
+    uint32_t n_item = 0, n_tile = 0, n_raw = 0;
+    bool ok = true;
+    while (ok && cur.next(a, &it)) {
+      const int nb = it.blk_end - it.blk_begin;
+      int* flag = &bad_v[n_item % FLAGS][warp - 10];       // read at the end of the item that set it, long before its next use
+      if (lane == 0) *flag = 0;
+      __syncwarp();
+      // the tiles' order in the ring: K0 [K1] V0 [K2] V1 ...
+      uint32_t tile = n_tile + (nb > 1 ? 2 : 1);
+      for (int j = 0; j < nb; ++j) {
+        const int blk = it.blk_begin + j;
+        if ((blk + 1) * BLK > it.ctx_len) {
+          const int st = tile % STAGES;
+          ok = __all_sync(0xffffffffu, mbar_wait(&raw[n_raw % STAGES], (n_raw / STAGES) & 1u, a.err_word, DEV_ERR_ATTN_CORR));
+          if (!ok) break;
+          ++n_raw;
+          uint8_t* v = ring + st * TILE_BYTES;
+          const int r0 = max(it.ctx_len - blk * BLK, 0), r_end = it.ctx_len + it.n_nodes - blk * BLK;
+          bool bad = false;
+          // thread t takes 16-byte vector t % 8 (as stored; the swizzle only permutes a row's vectors) of rows t / 8, t / 8 + 8 ...
+          for (int r = r0 + (tid >> 3); r < BLK; r += 8) {
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+              uint4* p = reinterpret_cast<uint4*>(v + h * HALF_BYTES + r * 128 + (tid & 7) * 16);
+              if (r >= r_end) {
+                *p = make_uint4(0, 0, 0, 0);
+              } else {
+                const uint4 x = *p;
+                uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                constexpr uint32_t E = BF16 ? 0x7f80u : 0x7c00u;             // all exponent bits set: infinity or NaN
+                bool any = false;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  if ((w[q] & E) == E) { w[q] &= 0xffff0000u; any = true; }
+                  if (((w[q] >> 16) & E) == E) { w[q] &= 0x0000ffffu; any = true; }
+                }
+                if (any) { *p = make_uint4(w[0], w[1], w[2], w[3]); bad = true; }
+              }
+            }
+          }
+          if (bad) *reinterpret_cast<volatile int*>(flag) = 1;
+          fence_proxy_async_smem();                        // the MMA reads the tile through the async proxy
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full[st]);
+        }
+        tile += j + 2 < nb ? 2 : 1;
+      }
+      n_tile += 2 * nb;
+      ++n_item;
+    }
+    if (!ok) cta_failed = 1;
+   }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    Cursor cur(span);
+    Item it{};
+    // ------------------------------------------------------------ softmax (warps 0-7)
+    const int i = warp >> 2, quarter = warp & 3;
+    const int r = quarter * 32 + lane;
+    const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t t_s = tmem + lane_base + TMEM_S + i * BLK, t_o = tmem + lane_base;
+    uint32_t n_item = 0, n_s = 0;
+    bool ok = true;
+    const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
+    while (ok && cur.next(a, &it)) {
+      const int nb = it.blk_end - it.blk_begin;
+      const bool live = quarter * 32 < it.n_rows;          // warps without rows only keep the barriers' count
+      const bool valid = r < it.n_rows;
+      const int node_in_tile = min(r, it.n_rows - 1) / a.group;
+      const int row = it.row0 + node_in_tile, node = it.node0 + node_in_tile;
+      float m = -INFINITY, l = 0.f;
+      for (int j = i; j < nb; j += 2) {
+        ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+        if (!ok) break;
+        ++n_s;
+        tc_fence_after_sync();
+        if (live) {
+          uint32_t s[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld_32x32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+          tmem_wait_ld();
+          const int slot0 = (it.blk_begin + j) * BLK;
+          if (slot0 + BLK > it.ctx_len) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t bits = slot_bits(a.rows, it, row, node, slot0 + c * 32);
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!((bits >> e) & 1u)) s[c * 32 + e] = 0xff800000u;       // -inf
+            }
+          }
+          float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < 128; c += 8) {
+            mx0 = fmax3(mx0, __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+            mx1 = fmax3(mx1, __uint_as_float(s[c + 2]), __uint_as_float(s[c + 3]));
+            mx2 = fmax3(mx2, __uint_as_float(s[c + 4]), __uint_as_float(s[c + 5]));
+            mx3 = fmax3(mx3, __uint_as_float(s[c + 6]), __uint_as_float(s[c + 7]));
+          }
+          const float m_blk = fmax3(fmaxf(mx0, mx1), mx2, mx3) * a.scale_log2;
+          if (j < 2) {
+            m = m_blk;
+          } else {
+            // also the first block that shows anything: the reference was -inf, the sum and O are zero
+            const bool need = m_blk > m + RESCALE_THRESHOLD;
+            if (__any_sync(0xffffffffu, need)) {           // s_full came behind this parity's last PV: O is complete
+              float alpha = 1.0f;
+              if (need) { alpha = fast_exp2(m - m_blk); m = m_blk; l *= alpha; }
+#pragma unroll 1
+              for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld_32x32(t_o + i * HEAD_DIM + c * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_st_32x32(t_o + i * HEAD_DIM + c * 32, o);
+              }
+              tmem_wait_st();
+            }
+          }
+          const float neg = m == -INFINITY ? 0.f : -m;      // nothing seen yet: every term is exp2(-inf)
+          const uint64_t neg2 = pack_f32x2(neg, neg);
+          uint64_t sum_a = pack_f32x2(0.f, 0.f), sum_b = sum_a;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {                     // 64 columns at a time: the packed words leave before the next are formed
+            uint32_t p[32];
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              float x0, x1;
+              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[h * 64 + 2 * c]), __uint_as_float(s[h * 64 + 2 * c + 1])), scale2, neg2), x0, x1);
+              const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+              if (c & 1) sum_b = add_f32x2(sum_b, pack_f32x2(p0, p1));
+              else sum_a = add_f32x2(sum_a, pack_f32x2(p0, p1));
+              if constexpr (BF16) {           // an MMA's operands have one type: P takes V's; the row sum stays unrounded
+                __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+                p[c] = *reinterpret_cast<uint32_t*>(&v);
+              } else {
+                __half2 v = __floats2half2_rn(p0, p1);
+                p[c] = *reinterpret_cast<uint32_t*>(&v);
+              }
+            }
+            tmem_st_32x32(t_s + h * 32, p);
+          }
+          float s0, s1;
+          unpack_f32x2(add_f32x2(sum_a, sum_b), s0, s1);
+          l += s0 + s1;
+          tmem_wait_st();
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[i]);
+      }
+      if (!ok) break;
+      // ---- the row's end: both parities' (reference, sum) are exchanged, each warp then writes half of the columns
+      const int par = n_item & 1;
+      ml[par][i][r][0] = m;
+      ml[par][i][r][1] = l;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ml_full);
+      ok = __all_sync(0xffffffffu, mbar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR)) ;
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full, par, a.err_word, DEV_ERR_ATTN_CORR));
+      if (!ok) break;
+      tc_fence_after_sync();
+      if (live) {
+        const float m0 = ml[par][0][r][0], m1 = ml[par][1][r][0];
+        const float M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
+        const float a0 = fast_exp2(m0 - ref), a1 = fast_exp2(m1 - ref);
+        const float L = a0 * ml[par][0][r][1] + a1 * ml[par][1][r][1];
+        const bool whole = it.blk_begin == 0 && it.blk_end == it.n_blk;
+        // a row that sees no slot at all (not: one whose scores are all -inf)
+        bool any = it.ctx_len > 0;
+        for (int w = 0; w < it.n_nodes && !any; w += 32) any = node_bits(a.rows, row, node, it.n_nodes, w) != 0;
+        const float inv = whole ? 1.0f / L : 1.0f;
+        const int head = it.g * a.group + min(r, it.n_rows - 1) % a.group;
+        const size_t part = static_cast<size_t>(2 * blockIdx.x + (it.blk_begin == 0 ? 1 : 0)) * BLK + r;
+        const bool bad = (*reinterpret_cast<volatile int*>(&bad_v[n_item % FLAGS][0]) | *reinterpret_cast<volatile int*>(&bad_v[n_item % FLAGS][1])) != 0;
+        char* dst = static_cast<char*>(a.out) + (static_cast<int64_t>(row) * a.out_stride + head * D) * 2;
+#pragma unroll 1
+        for (int c = i * (D / 64); c < (i + 1) * (D / 64); ++c) {
+          uint32_t o0[32], o1[32];
+          tmem_ld_32x32(t_o + c * 32, o0);
+          if (nb > 1) tmem_ld_32x32(t_o + HEAD_DIM + c * 32, o1);
+          tmem_wait_ld();
+          float o[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            o[e] = __uint_as_float(o0[e]) * a0;
+            if (nb > 1) o[e] = fmaf(__uint_as_float(o1[e]), a1, o[e]);
+          }
+          if (bad) {
+            // a drafted V that is not finite was taken out of the product: the rows that see it get it here
+#pragma unroll 1
+            for (int s = max(it.ctx_len, it.blk_begin * BLK); s < min(it.ctx_len + it.n_nodes, it.blk_end * BLK); ++s) {
+              if (!(node_bits(a.rows, row, node, it.n_nodes, s - it.ctx_len) & 1u)) continue;
+              const int64_t vr = slot_row(a.kv.page_table, a.kv.pt_stride, a.kv.ctx_start, a.kv.n_slots, it.seq, s);
+              if (vr < 0) continue;
+              const unsigned short* vp = static_cast<const unsigned short*>(a.kv.v) + vr * a.kv.v_stride + it.g * D + c * 32;
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const float x = elem<BF16>(vp[e]);
+                if (!isfinite(x)) o[e] += x;
+              }
+            }
+          }
+          if (valid && whole) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t pk[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) pk[q] = any ? pack_out<BF16>(o[8 * e + 2 * q] * inv, o[8 * e + 2 * q + 1] * inv) : 0u;
+              *reinterpret_cast<uint4*>(dst + c * 64 + e * 16) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            }
+          } else if (valid) {
+            float4* po = reinterpret_cast<float4*>(a.partial_o + part * HEAD_DIM + c * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) po[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          }
+        }
+        if (valid && i == 0) {
+          if (!whole) *reinterpret_cast<float2*>(a.partial_ml + part * 2) = make_float2(M, any ? L : -1.f);
+          else if (a.lse) a.lse[static_cast<size_t>(row) * a.n_q_heads + head] = any ? (M + log2f(L)) * LN2 : -INFINITY;
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free);
+      ++n_item;
+    }
+    if (!ok) cta_failed = 1;
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  if (cta_failed) {             // let this CTA's bulk copies land before its shared memory is released
+    if (threadIdx.x == 0) {
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < DRAIN_LIMIT_NS) { }
+    }
+    __syncthreads();
+  }
+  if (warp == 9) {
+    tc_fence_after_sync();
+    tmem_dealloc<512>(tmem);
+  }
+}
+
+// The parts of a cut unit: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, one warp per row.
+constexpr int MERGE_WARPS = 8;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(TreeParams a) {
+  constexpr int E = D / 32;                             // columns per lane
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int r = blockIdx.y * MERGE_WARPS + (threadIdx.x >> 5);
+  const MergeRecord* mr = a.merges + blockIdx.x;
+  const int n_parts = *reinterpret_cast<const volatile int*>(&mr->n_parts);
+  const int n_rows = *reinterpret_cast<const volatile int*>(&mr->n_rows);
+  if (n_parts <= 1 || r >= n_rows) return;
+  const int row = *reinterpret_cast<const volatile int*>(&mr->row0) + r / a.group;
+  const int head = *reinterpret_cast<const volatile int*>(&mr->head0) + r % a.group;
+  // part 0 is the record's CTA's last item, part s > 0 the first item of the s-th CTA behind it
+  auto slot = [&](int s) { return static_cast<size_t>(2 * (blockIdx.x + s) + (s == 0 ? 1 : 0)) * BLK + r; };
+  float M = -INFINITY;
+  bool any = true;
+  for (int s = lane; s < n_parts; s += 32) {
+    const float2 v = ld_dep_f32x2(a.partial_ml + slot(s) * 2);
+    M = fmaxf(M, v.x);
+    if (v.y < 0.f) any = false;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  any = __all_sync(0xffffffffu, any);
+  const float ref = M == -INFINITY ? 0.f : M;
+  float acc[E], L = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  for (int s0 = 0; s0 < n_parts; s0 += 4) {
+    float2 v[4];
+    float o[4][E];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const size_t at = slot(min(s0 + u, n_parts - 1));
+      v[u] = ld_dep_f32x2(a.partial_ml + at * 2);
+      if constexpr (E == 4) *reinterpret_cast<float4*>(o[u]) = ld_dep_f32x4(a.partial_o + at * HEAD_DIM + lane * 4);
+      else *reinterpret_cast<float2*>(o[u]) = ld_dep_f32x2(a.partial_o + at * HEAD_DIM + lane * 2);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (s0 + u >= n_parts) break;
+      const float w = fast_exp2(v[u].x - ref);
+      L = fmaf(w, v[u].y, L);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(w, o[u][e], acc[e]);
+    }
+  }
+  const float inv = 1.0f / L;
+  uint32_t pk[E / 2];
+#pragma unroll
+  for (int e = 0; e < E; e += 2) pk[e / 2] = any ? pack_out<BF16>(acc[e] * inv, acc[e + 1] * inv) : 0u;
+  char* dst = static_cast<char*>(a.out) + (static_cast<int64_t>(row) * a.out_stride + head * D + lane * E) * 2;
+  if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pk[0], pk[1]);
+  else *reinterpret_cast<uint32_t*>(dst) = pk[0];
+  if (lane == 0 && a.lse) a.lse[static_cast<size_t>(row) * a.n_q_heads + head] = any ? (M + log2f(L)) * LN2 : -INFINITY;
+}
+
+template <int D, bool BF16>
+int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TreeParams& p, int n_ctas, cudaStream_t s) {
+  static bool set[MAX_DEVICES] = {};
+  const int dev = current_device_slot();
+  if (!set[dev]) {
+    if (cudaFuncSetAttribute(tree_attention_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, TREE_SMEM) != cudaSuccess) return -1;
+    set[dev] = true;
+  }
+  if (launch_pdl(tree_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), TREE_SMEM, s, q, k, v, p) != cudaSuccess) return -1;
+  const int rows = std::min(p.tile_nodes, p.rows.max_nodes) * p.group;
+  return launch_pdl(tree_merge_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
+}
+
+// K or V rows as a 2-D map of 64-column boxes: a page's 16 rows or a block's 128
+int pool_map(CUtensorMap* out, const void* base, const KvView& kv, int64_t stride) {
+  const uint64_t dims[2] = {static_cast<uint64_t>(kv.n_kv_heads) * kv.head_dim, static_cast<uint64_t>(kv.n_slots)};
+  const uint64_t str[1] = {static_cast<uint64_t>(stride) * 2};
+  const uint32_t box[2] = {64u, static_cast<uint32_t>(kv.page_table ? PAGE_TOKENS : BLK)};
+  return encode_f16_map(out, base, 2, dims, str, box);
+}
+
+constexpr int TREE_WARPS = 4;
 template <bool BF16>
 __device__ __forceinline__ float2 load2(const void* p, int64_t i) {
   if constexpr (BF16) {
@@ -16,90 +736,9 @@ __device__ __forceinline__ float2 load2(const void* p, int64_t i) {
     return __half22float2(*reinterpret_cast<const __half2*>(static_cast<const __half*>(p) + i));
   }
 }
-// A finite value past the type's range (a rounded-up average of values at its limit) becomes the largest finite one; infinity stays.
-template <bool BF16>
-__device__ __forceinline__ void store1(void* p, int64_t i, float x) {
-  if constexpr (BF16) {
-    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
-  } else {
-    static_cast<__half*>(p)[i] = isinf(x) ? __float2half_rn(x) : to_half_sat(x);
-  }
-}
-
 __device__ __forceinline__ bool node_sees(const TreeRows& r, int row, int i, int j) {
   if (r.mask == nullptr) return j <= i;
   return (r.mask[static_cast<size_t>(row) * r.mask_words + (j >> 6)] >> (j & 63)) & 1;
-}
-
-// The prompt a row belongs to, or -1 (rows behind the last prompt, and rows past a prompt's bound).
-__device__ __forceinline__ int seq_of_row(const TreeRows& r, int row) {
-  for (int b = 0; b < r.n_seqs; ++b) {
-    const SeqPart p = seq_part(r, b);
-    if (row >= p.row0 && row < p.row0 + p.n_nodes) return b;
-  }
-  return -1;
-}
-
-template <int D, bool BF16>
-__global__ void __launch_bounds__(TREE_WARPS * 32) tree_attention_kernel(TreeAttention a) {
-  __shared__ float sm_o[TREE_WARPS][D], sm_m[TREE_WARPS], sm_l[TREE_WARPS];
-  const int row = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int b = seq_of_row(a.rows, row);
-  if (b < 0) return;
-  const SeqPart p = seq_part(a.rows, b);
-  const int i = row - p.row0;
-  const int g = head / (a.n_q_heads / a.kv.n_kv_heads);
-  const float scale_log2 = a.scale * LOG2E;
-  float q[D / 32], o[D / 32];
-#pragma unroll
-  for (int e = 0; e < D / 32; e += 2) {
-    const float2 f = load2<BF16>(a.q, static_cast<int64_t>(row) * a.q_stride + head * D + e * 32 + lane * 2);
-    q[e] = f.x; q[e + 1] = f.y; o[e] = o[e + 1] = 0.f;
-  }
-  float m = -INFINITY, l = 0.f;
-  bool any = false;
-  for (int s = warp; s < p.ctx_len + p.n_nodes; s += TREE_WARPS) {
-    if (s >= p.ctx_len && !node_sees(a.rows, row, i, s - p.ctx_len)) continue;
-    any = true;
-    const int64_t r = slot_row(a.kv.page_table, a.kv.pt_stride, a.kv.ctx_start, a.kv.n_slots, b, s);
-    float x = 0.f, v[D / 32];
-#pragma unroll
-    for (int e = 0; e < D / 32; e += 2) {
-      float2 kf = make_float2(0.f, 0.f), vf = kf;
-      if (r >= 0) {
-        kf = load2<BF16>(a.kv.k, r * a.kv.k_stride + g * D + e * 32 + lane * 2);
-        vf = load2<BF16>(a.kv.v, r * a.kv.v_stride + g * D + e * 32 + lane * 2);
-      }
-      x = fmaf(q[e], kf.x, fmaf(q[e + 1], kf.y, x));
-      v[e] = vf.x; v[e + 1] = vf.y;
-    }
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
-    x *= scale_log2;
-    const float m_new = fmaxf(m, x), ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2f(m - ref), pr = exp2f(x - ref);
-    l = l * alpha + pr;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] = o[e] * alpha + pr * v[e];
-    m = m_new;
-  }
-  if (lane == 0) { sm_m[warp] = m; sm_l[warp] = any ? l : -1.f; }
-#pragma unroll
-  for (int e = 0; e < D / 32; e += 2) { sm_o[warp][e * 32 + lane * 2] = o[e]; sm_o[warp][e * 32 + lane * 2 + 1] = o[e + 1]; }
-  __syncthreads();
-  float M = -INFINITY, L = 0.f, acc = 0.f;
-  bool seen = false;
-  for (int w = 0; w < TREE_WARPS; ++w) if (sm_l[w] >= 0.f || isnan(sm_l[w])) { M = fmaxf(M, sm_m[w]); seen = true; }
-  const float ref = M == -INFINITY ? 0.f : M;
-  const int d = threadIdx.x;
-  for (int w = 0; w < TREE_WARPS; ++w) {
-    if (!(sm_l[w] >= 0.f || isnan(sm_l[w]))) continue;
-    const float f = exp2f(sm_m[w] - ref);
-    L += f * sm_l[w];
-    if (d < D) acc += f * sm_o[w][d];
-  }
-  if (d < D) store1<BF16>(a.out, static_cast<int64_t>(row) * a.out_stride + head * D + d, seen ? acc / L : 0.f);
-  if (d == 0 && a.lse) a.lse[static_cast<size_t>(row) * a.n_q_heads + head] = seen ? (M + log2f(L)) / LOG2E : -INFINITY;
 }
 
 template <int D, bool BF16>
@@ -143,16 +782,30 @@ __global__ void __launch_bounds__(TREE_WARPS * 32) attention_weights_kernel(Atte
 
 }  // namespace
 
-int launch_tree_attention(const TreeAttention& a, int, cudaStream_t s) {
-  const dim3 grid(a.rows.n_rows, a.n_q_heads);
-  if (a.kv.head_dim == 128) {
-    if (a.kv.bf16) tree_attention_kernel<128, true><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-    else tree_attention_kernel<128, false><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-  } else {
-    if (a.kv.bf16) tree_attention_kernel<64, true><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-    else tree_attention_kernel<64, false><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-  }
-  return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
+int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
+  TreeParams p{};
+  p.kv = t.kv; p.rows = t.rows;
+  p.n_q_heads = t.n_q_heads;
+  p.group = t.n_q_heads / t.kv.n_kv_heads;
+  p.tile_nodes = std::min(BLK / p.group, t.rows.max_nodes);
+  p.scale_log2 = t.scale * LOG2E;
+  p.out = t.out; p.out_stride = t.out_stride; p.lse = t.lse;
+  char* ws = static_cast<char*>(t.workspace);
+  p.err_word = reinterpret_cast<int*>(ws);
+  p.merges = reinterpret_cast<MergeRecord*>(ws + WS_MERGE);
+  p.partial_ml = reinterpret_cast<float*>(ws + WS_ML);
+  p.partial_o = reinterpret_cast<float*>(ws + WS_O);
+  CUtensorMap q, k, v;
+  const uint64_t qd[3] = {static_cast<uint64_t>(t.kv.head_dim), static_cast<uint64_t>(t.n_q_heads), static_cast<uint64_t>(t.rows.n_rows)};
+  const uint64_t qs[2] = {static_cast<uint64_t>(t.kv.head_dim) * 2, static_cast<uint64_t>(t.q_stride) * 2};
+  const uint32_t box[3] = {64u, static_cast<uint32_t>(p.group), static_cast<uint32_t>(p.tile_nodes)};
+  if (encode_f16_map(&q, t.q, 3, qd, qs, box) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
+      pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
+    return -1;
+  const int n_ctas = std::min(n_sms, MAX_CTAS);
+  if (t.kv.head_dim == 128)
+    return t.kv.bf16 ? launch_tree<128, true>(q, k, v, p, n_ctas, s) : launch_tree<128, false>(q, k, v, p, n_ctas, s);
+  return t.kv.bf16 ? launch_tree<64, true>(q, k, v, p, n_ctas, s) : launch_tree<64, false>(q, k, v, p, n_ctas, s);
 }
 
 int launch_attention_weights(const AttentionWeights& a, int, cudaStream_t s) {
