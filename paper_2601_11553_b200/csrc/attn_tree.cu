@@ -26,32 +26,20 @@
 // the latter raises a flag, and the rows that do see such a value get it added when they are written.
 #include <algorithm>
 
-#include "kernels.h"
-#include "ptx.cuh"
+#include "tree_common.cuh"
 
 namespace pc {
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr int BLK = 128;                        // context slots per block, rows per tile
-constexpr int TREE_THREADS = 384;
 constexpr int RING_BYTES = 160 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
 constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
 constexpr int MAX_STAGES = 10;
 constexpr uint32_t TMEM_S = 256;
 constexpr float RESCALE_THRESHOLD = 8.0f;       // the running reference is raised when a block exceeds it by 2^8
-constexpr int UNIT_COST = 2;                    // what a unit costs beside its blocks (Q, the row's end), in blocks
-constexpr int MIN_SPAN = 4;                     // least cost of a span: shorter ones cost more to merge than they save
 constexpr int FLAGS = 8;
-
-// Workspace: the error word, one merge record per CTA, partial results (two slots per CTA).
-constexpr int WS_MERGE = 256, WS_ML = 16384;
-constexpr int MAX_CTAS = 160;
-constexpr size_t WS_O = WS_ML + sizeof(float) * 2 * BLK * 2 * MAX_CTAS;
-static_assert(WS_MERGE + sizeof(int) * 8 * MAX_CTAS <= WS_ML, "");
-static_assert(WS_O + sizeof(float) * 2 * MAX_CTAS * BLK * HEAD_DIM <= (24u << 20), "PERCACHE_OPS_WORKSPACE_BYTES");
+constexpr int MIN_SPAN = 4;                     // least cost of a span: shorter ones cost more to merge than they save
 
 struct MergeRecord {             // written by the CTA that has a cut unit's first part
   int32_t n_parts;               // 0: none
@@ -73,33 +61,34 @@ struct TreeParams {
   float *partial_ml, *partial_o;
 };
 
-__device__ __forceinline__ float fast_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+__device__ __forceinline__ Shape tree_shape(const TreeParams& a, const SeqPart& p) {
+  if (p.n_nodes == 0) return Shape{0, 0, 1};
+  return Shape{(p.n_nodes + a.tile_nodes - 1) / a.tile_nodes * a.kv.n_kv_heads, (p.ctx_len + p.n_nodes + BLK - 1) / BLK, 1};
 }
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float y;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
+struct Item {
+  int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes
+  int row0, node0, n_rows;       // the tile: first global row, first node, valid tile rows
+  int g, blk_begin, blk_end, n_blk;
+  int64_t unit_end;
+};
+__device__ __forceinline__ bool next_item(Cursor& cur, const TreeParams& a, Item* it) {
+  Piece pc;
+  if (!cur.next(a.rows, [&](const SeqPart& p) { return tree_shape(a, p); }, &pc)) return false;
+  // the tiles of one KV head follow each other: they share K and V in L2
+  const int tiles = (pc.part.n_nodes + a.tile_nodes - 1) / a.tile_nodes, tile = pc.unit % tiles;
+  it->seq = pc.seq; it->ctx_len = pc.part.ctx_len; it->n_nodes = pc.part.n_nodes;
+  it->node0 = tile * a.tile_nodes;
+  it->row0 = pc.part.row0 + it->node0;
+  it->n_rows = min(a.tile_nodes, pc.part.n_nodes - it->node0) * a.group;
+  it->g = pc.unit / tiles;
+  it->blk_begin = pc.blk_begin; it->blk_end = pc.blk_end; it->n_blk = pc.n_blk; it->unit_end = pc.unit_end;
+  return true;
 }
-__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
+// Bits of the 32 slots from slot0 on that a node sees.
+__device__ __forceinline__ uint32_t slot_bits(const TreeRows& r, const Item& it, int row, int node, int slot0) {
+  const int in_ctx = it.ctx_len - slot0;
+  if (in_ctx >= 32) return 0xffffffffu;
+  return (in_ctx > 0 ? (1u << in_ctx) - 1 : 0u) | node_bits(r, row, node, it.n_nodes, -in_ctx);
 }
 
 // Two values in the pools' type.  A finite value past fp16's range (an average of values at its limit, rounded up) becomes the
@@ -122,116 +111,6 @@ template <bool BF16>
 __device__ __forceinline__ float elem(uint32_t bits16) {
   if constexpr (BF16) return __uint_as_float(bits16 << 16);
   else return __half2float(__ushort_as_half(static_cast<unsigned short>(bits16)));
-}
-
-// ---------------------------------------------------------------------------------------------------- schedule
-struct Span { int64_t begin, end, total; int n_ctas, seq; int64_t seq_start; };
-struct Item {
-  int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes
-  int row0, node0, n_rows;       // the tile: first global row, first node, valid tile rows
-  int g, blk_begin, blk_end, n_blk;
-  int64_t unit_end;              // cost position behind the unit
-};
-
-__device__ __forceinline__ int64_t seq_cost(const TreeParams& a, const SeqPart& p) {
-  if (p.n_nodes == 0) return 0;
-  const int tiles = (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes;
-  return static_cast<int64_t>((p.ctx_len + p.n_nodes + BLK - 1) / BLK + UNIT_COST) * tiles * a.kv.n_kv_heads;
-}
-
-// The CTA's span and the prompt it starts in: block-wide, every thread takes a run of prompts.
-__device__ __forceinline__ void make_span(const TreeParams& a, Span* sp, int64_t* warp_sums) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (a.rows.n_seqs + TREE_THREADS - 1) / TREE_THREADS;
-  const int b0 = min(tid * per, a.rows.n_seqs), b1 = min(b0 + per, a.rows.n_seqs);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += seq_cost(a, seq_part(a.rows, b));
-  int64_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += x;
-  }
-  if (lane == 31) warp_sums[warp] = incl;
-  __syncthreads();
-  int64_t before = incl - mine, total = 0;
-#pragma unroll
-  for (int w = 0; w < TREE_THREADS / 32; ++w) {
-    const int64_t x = warp_sums[w];
-    if (w < warp) before += x;
-    total += x;
-  }
-  const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / MIN_SPAN, static_cast<int64_t>(1))));
-  const int c = blockIdx.x;
-  const int64_t begin = c < n ? total * c / n : total, end = c < n ? total * (c + 1) / n : total;
-  if (tid == 0) { sp->begin = begin; sp->end = end; sp->total = total; sp->n_ctas = n; sp->seq = a.rows.n_seqs; sp->seq_start = total; }
-  __syncthreads();
-  if (mine > 0 && begin >= before && begin < before + mine) {         // one thread at most
-    int b = b0;
-    int64_t at = before;
-    for (; b < b1; ++b) {
-      const int64_t cost = seq_cost(a, seq_part(a.rows, b));
-      if (begin < at + cost) break;
-      at += cost;
-    }
-    sp->seq = b;
-    sp->seq_start = at;
-  }
-  __syncthreads();
-}
-
-struct Cursor {
-  int64_t pos, end, seq_start;
-  int seq;
-  __device__ __forceinline__ explicit Cursor(const Span& s) : pos(s.begin), end(s.end), seq_start(s.seq_start), seq(s.seq) {}
-  __device__ __forceinline__ bool next(const TreeParams& a, Item* it) {
-    while (pos < end && seq < a.rows.n_seqs) {
-      const SeqPart p = seq_part(a.rows, seq);
-      const int64_t whole = seq_cost(a, p);
-      if (pos >= seq_start + whole) { seq_start += whole; ++seq; continue; }
-      const int tiles = (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes;
-      const int n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK, cost = n_blk + UNIT_COST;
-      const int64_t rel = pos - seq_start;
-      const int unit = static_cast<int>(rel / cost);
-      const int64_t unit_start = seq_start + static_cast<int64_t>(unit) * cost, unit_end = unit_start + cost;
-      const int64_t stop = min(end, unit_end);
-      // a unit's own cost lies ahead of its blocks: a border inside it leaves the whole unit to the later span
-      const int bb = max(static_cast<int>(pos - unit_start) - UNIT_COST, 0), be = max(static_cast<int>(stop - unit_start) - UNIT_COST, 0);
-      pos = stop;
-      if (be <= bb) continue;
-      const int tile = unit % tiles;                  // the tiles of one KV head follow each other: they share K and V in L2
-      it->seq = seq; it->ctx_len = p.ctx_len; it->n_nodes = p.n_nodes;
-      it->node0 = tile * a.tile_nodes;
-      it->row0 = p.row0 + it->node0;
-      it->n_rows = min(a.tile_nodes, p.n_nodes - it->node0) * a.group;
-      it->g = unit / tiles;
-      it->blk_begin = bb; it->blk_end = be; it->n_blk = n_blk; it->unit_end = unit_end;
-      return true;
-    }
-    return false;
-  }
-};
-
-// Bits of the nodes j0 .. j0 + 31 (j0 may be negative) that a node sees.
-__device__ __forceinline__ uint32_t node_bits(const TreeRows& r, int row, int node, int n_nodes, int j0) {
-  if (j0 <= -32 || j0 >= n_nodes) return 0u;
-  const int lo = max(j0, 0);
-  uint64_t w = 0;
-  if (r.mask != nullptr) {
-    const uint64_t* m = r.mask + static_cast<size_t>(row) * r.mask_words;
-    w = __ldg(m + (lo >> 6)) >> (lo & 63);
-    if ((lo & 63) != 0 && (lo >> 6) + 1 < r.mask_words) w |= __ldg(m + (lo >> 6) + 1) << (64 - (lo & 63));
-  } else if (node >= lo) {
-    w = node - lo >= 63 ? ~0ull : (1ull << (node - lo + 1)) - 1;
-  }
-  if (n_nodes - lo < 64) w &= (1ull << (n_nodes - lo)) - 1;
-  return static_cast<uint32_t>(w << (lo - j0));
-}
-// Bits of the 32 slots from slot0 on that a node sees.
-__device__ __forceinline__ uint32_t slot_bits(const TreeRows& r, const Item& it, int row, int node, int slot0) {
-  const int in_ctx = it.ctx_len - slot0;
-  if (in_ctx >= 32) return 0xffffffffu;
-  return (in_ctx > 0 ? (1u << in_ctx) - 1 : 0u) | node_bits(r, row, node, it.n_nodes, -in_ctx);
 }
 
 // ---------------------------------------------------------------------------------------------------- attention
@@ -272,7 +151,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   if (warp == 8 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
   pdl_launch_dependents();
   pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
-  make_span(a, &span, warp_sums);
+  make_span(a.rows, MIN_SPAN, &span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -288,18 +167,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     uint32_t n_item = 0, n_tile = 0, n_raw = 0;
     MergeRecord rec{};
     bool ok = true;
-    const int pg = lane & 7, hf = (lane >> 3) & 1;
     auto load = [&](const CUtensorMap* tm, int blk, bool clean) {
       const int st = n_tile % STAGES;
       const uint32_t ph = (n_tile / STAGES) & 1u;
       ++n_tile;
-      int page = 0;
-      if (a.kv.page_table) {           // pages behind the prompt's last slot repeat its last page: masked either way
-        const int last = (it.ctx_len + it.n_nodes - 1) / PAGE_TOKENS;
-        page = __ldg(a.kv.page_table + static_cast<size_t>(it.seq) * a.kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + pg, last));
-      } else if (lane == 0) {
-        page = __ldg(a.kv.ctx_start + it.seq);
-      }
+      const int where = tile_place(a.kv, SeqPart{it.row0, it.n_nodes, it.ctx_len}, it.seq, blk, lane);
       ok = __all_sync(0xffffffffu, mbar_wait(&empty[st], ph ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
       if (!ok) return;
       // a tile that warps 10-11 have to clean lands on a barrier of theirs; they then complete `full` in its place
@@ -307,15 +179,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       if (lane == 0) mbar_arrive_expect_tx(bar, TILE_BYTES);
       if (lane == 1 && !clean) mbar_arrive(bar);
       __syncwarp();
-      uint8_t* dst = ring + st * TILE_BYTES;
-      if (a.kv.page_table) {
-        if (lane < 8 * HALVES)
-          tma_load_2d(dst + hf * HALF_BYTES + pg * (PAGE_TOKENS * 128), tm, bar, it.g * D + hf * 64, page * PAGE_TOKENS);
-      } else if (lane == 0) {
-        for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * HALF_BYTES, tm, bar, it.g * D + h * 64, page + blk * BLK);
-      }
+      load_tile<HALVES>(ring + st * TILE_BYTES, tm, bar, a.kv.page_table != nullptr, where, it.g * D, blk, lane);
     };
-    while (ok && cur.next(a, &it)) {
+    while (ok && next_item(cur, a, &it)) {
       if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
         rec.n_parts = static_cast<int>((it.unit_end * span.n_ctas - 1) / span.total) - static_cast<int>(blockIdx.x) + 1;
         rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group; rec.cta = blockIdx.x;
@@ -364,7 +230,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         umma_commit(&s_full[i]);
         umma_commit(&empty[st]);
       };
-      while (ok && cur.next(a, &it)) {
+      while (ok && next_item(cur, a, &it)) {
         const int nb = it.blk_end - it.blk_begin;
         wait(&q_full, n_item & 1u);
         issue_s(0);
@@ -401,7 +267,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     const int tid = threadIdx.x - 320;
     uint32_t n_item = 0, n_tile = 0, n_raw = 0;
     bool ok = true;
-    while (ok && cur.next(a, &it)) {
+    while (ok && next_item(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin;
       int* flag = &bad_v[n_item % FLAGS][warp - 10];       // read at the end of the item that set it, long before its next use
       if (lane == 0) *flag = 0;
@@ -463,7 +329,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     uint32_t n_item = 0, n_s = 0;
     bool ok = true;
     const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
-    while (ok && cur.next(a, &it)) {
+    while (ok && next_item(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin;
       const bool live = quarter * 32 < it.n_rows;          // warps without rows only keep the barriers' count
       const bool valid = r < it.n_rows;
@@ -489,6 +355,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
               for (int e = 0; e < 32; ++e)
                 if (!((bits >> e) & 1u)) s[c * 32 + e] = 0xff800000u;       // -inf
             }
+            __syncwarp();
           }
           float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
@@ -571,6 +438,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         // a row that sees no slot at all (not: one whose scores are all -inf)
         bool any = it.ctx_len > 0;
         for (int w = 0; w < it.n_nodes && !any; w += 32) any = node_bits(a.rows, row, node, it.n_nodes, w) != 0;
+        __syncwarp();
         const float inv = whole ? 1.0f / L : 1.0f;
         const int head = it.g * a.group + min(r, it.n_rows - 1) % a.group;
         const size_t part = static_cast<size_t>(2 * blockIdx.x + (it.blk_begin == 0 ? 1 : 0)) * BLK + r;
@@ -602,6 +470,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 if (!isfinite(x)) o[e] += x;
               }
             }
+            __syncwarp();
           }
           if (valid && whole) {
 #pragma unroll
@@ -719,67 +588,6 @@ int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v
   return launch_pdl(tree_merge_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
 }
 
-// K or V rows as a 2-D map of 64-column boxes: a page's 16 rows or a block's 128
-int pool_map(CUtensorMap* out, const void* base, const KvView& kv, int64_t stride) {
-  const uint64_t dims[2] = {static_cast<uint64_t>(kv.n_kv_heads) * kv.head_dim, static_cast<uint64_t>(kv.n_slots)};
-  const uint64_t str[1] = {static_cast<uint64_t>(stride) * 2};
-  const uint32_t box[2] = {64u, static_cast<uint32_t>(kv.page_table ? PAGE_TOKENS : BLK)};
-  return encode_f16_map(out, base, 2, dims, str, box);
-}
-
-constexpr int TREE_WARPS = 4;
-template <bool BF16>
-__device__ __forceinline__ float2 load2(const void* p, int64_t i) {
-  if constexpr (BF16) {
-    return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(static_cast<const __nv_bfloat16*>(p) + i));
-  } else {
-    return __half22float2(*reinterpret_cast<const __half2*>(static_cast<const __half*>(p) + i));
-  }
-}
-__device__ __forceinline__ bool node_sees(const TreeRows& r, int row, int i, int j) {
-  if (r.mask == nullptr) return j <= i;
-  return (r.mask[static_cast<size_t>(row) * r.mask_words + (j >> 6)] >> (j & 63)) & 1;
-}
-
-template <int D, bool BF16>
-__global__ void __launch_bounds__(TREE_WARPS * 32) attention_weights_kernel(AttentionWeights a) {
-  const int b = blockIdx.z, g = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const SeqPart p = seq_part(a.rows, b);
-  const int group = a.n_q_heads / a.kv.n_kv_heads;
-  for (int s = blockIdx.x * TREE_WARPS + warp; s < p.ctx_len + p.n_nodes; s += gridDim.x * TREE_WARPS) {
-    const int64_t r = slot_row(a.kv.page_table, a.kv.pt_stride, a.kv.ctx_start, a.kv.n_slots, b, s);
-    float k[D / 32];
-#pragma unroll
-    for (int e = 0; e < D / 32; e += 2) {
-      float2 f = make_float2(0.f, 0.f);
-      if (r >= 0) f = load2<BF16>(a.kv.k, r * a.kv.k_stride + g * D + e * 32 + lane * 2);
-      k[e] = f.x; k[e + 1] = f.y;
-    }
-    float sum = 0.f;
-    for (int i = 0; i < p.n_nodes; ++i) {
-      const int row = p.row0 + i;
-      if ((a.use && !a.use[row]) || (s >= p.ctx_len && !node_sees(a.rows, row, i, s - p.ctx_len))) continue;
-      for (int h = g * group; h < (g + 1) * group; ++h) {
-        const float z = a.lse[static_cast<size_t>(row) * a.n_q_heads + h];
-        if (z == -INFINITY) continue;
-        float x = 0.f;
-#pragma unroll
-        for (int e = 0; e < D / 32; e += 2) {
-          const float2 f = load2<BF16>(a.q, static_cast<int64_t>(row) * a.q_stride + h * D + e * 32 + lane * 2);
-          x = fmaf(f.x, k[e], fmaf(f.y, k[e + 1], x));
-        }
-#pragma unroll
-        for (int w = 16; w > 0; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
-        sum += exp2f((x * a.scale - z) * LOG2E);
-      }
-    }
-    if (lane == 0) {
-      const size_t at = (static_cast<size_t>(b) * a.kv.n_kv_heads + g) * a.w_stride + s;
-      a.w_out[at] = a.w_in ? fmaf(a.decay, a.w_in[at], sum) : sum;
-    }
-  }
-}
-
 }  // namespace
 
 int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
@@ -796,28 +604,13 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   p.partial_ml = reinterpret_cast<float*>(ws + WS_ML);
   p.partial_o = reinterpret_cast<float*>(ws + WS_O);
   CUtensorMap q, k, v;
-  const uint64_t qd[3] = {static_cast<uint64_t>(t.kv.head_dim), static_cast<uint64_t>(t.n_q_heads), static_cast<uint64_t>(t.rows.n_rows)};
-  const uint64_t qs[2] = {static_cast<uint64_t>(t.kv.head_dim) * 2, static_cast<uint64_t>(t.q_stride) * 2};
-  const uint32_t box[3] = {64u, static_cast<uint32_t>(p.group), static_cast<uint32_t>(p.tile_nodes)};
-  if (encode_f16_map(&q, t.q, 3, qd, qs, box) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
+  if (q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_tree<128, true>(q, k, v, p, n_ctas, s) : launch_tree<128, false>(q, k, v, p, n_ctas, s);
   return t.kv.bf16 ? launch_tree<64, true>(q, k, v, p, n_ctas, s) : launch_tree<64, false>(q, k, v, p, n_ctas, s);
-}
-
-int launch_attention_weights(const AttentionWeights& a, int, cudaStream_t s) {
-  const dim3 grid((a.rows.max_len + 63) / 64, a.kv.n_kv_heads, a.rows.n_seqs);
-  if (a.kv.head_dim == 128) {
-    if (a.kv.bf16) attention_weights_kernel<128, true><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-    else attention_weights_kernel<128, false><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-  } else {
-    if (a.kv.bf16) attention_weights_kernel<64, true><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-    else attention_weights_kernel<64, false><<<grid, TREE_WARPS * 32, 0, s>>>(a);
-  }
-  return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
 }
 
 }  // namespace pc

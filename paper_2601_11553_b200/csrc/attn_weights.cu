@@ -1,0 +1,339 @@
+// Running attention weights of a cache's slots: w' = decay * w + the sum over rows and heads of exp(scale * q . k - lse), on tcgen05.
+//
+// The scores are formed transposed, S^T = K Q^T: a block of 128 slots is the MMA's M side and the rows (node, query head of
+// one KV head, packed as in the attention) its N side, so a slot is a TMEM lane, i.e. a thread, and the sum over the rows
+// is that thread's own: nothing is exchanged between threads, a slot's weight is written by exactly one, the order of its sum
+// never changes and no atomic is needed.  Only as many columns as there are rows (rounded up to 16) are computed.
+//
+// Bounds.  A block costs 32 KB of K (head size 128, 0.75 us of an SM's share of the HBM), at most 4.2 MFLOP (0.37 us) and
+// 16 K exponentials (0.55 us): bound by reading K once, so as in the attention the copies are what is kept running.
+//
+// Schedule as in the attention (spans of the batch's blocks), but a block belongs to one CTA: nothing is merged.
+// One CTA per SM, 384 threads: warp 8 copies (K ring, Q ring of two tiles), warp 9 issues the MMAs, warps 10-11 put the rows'
+// lse beside each Q tile, warps 0-3 sum the even blocks and warps 4-7 the odd ones, each from two TMEM buffers in turn.
+// One tile of rows stays in shared memory for the whole piece; of several, each is copied again for every block (L2).
+#include <algorithm>
+
+#include "tree_common.cuh"
+
+namespace pc {
+namespace {
+
+constexpr int K_RING = 128 * 1024;
+constexpr int Q_TILE = 32 * 1024;
+constexpr int WEIGHTS_SMEM = K_RING + 2 * Q_TILE + 1024;
+constexpr int MAX_STAGES = 8;
+constexpr int MASK_WORDS = 4;                    // 256 nodes
+constexpr int MIN_SPAN = 3;                      // unit cost and one block
+
+struct WeightParams {
+  KvView kv;
+  TreeRows rows;
+  int32_t n_q_heads, group, tile_nodes;
+  float scale, decay;
+  const float* lse;
+  const uint8_t* use;
+  const float* w_in;
+  float* w_out;
+  int64_t w_stride;
+  int* err_word;
+};
+
+__device__ __forceinline__ int n_tiles(const WeightParams& a, const SeqPart& p) { return (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes; }
+__device__ __forceinline__ Shape weight_shape(const WeightParams& a, const SeqPart& p) {
+  const int len = p.ctx_len + p.n_nodes;
+  if (len == 0) return Shape{0, 0, 1};
+  return Shape{a.kv.n_kv_heads, (len + BLK - 1) / BLK, max(n_tiles(a, p), 1)};
+}
+__device__ __forceinline__ bool next_piece(Cursor& cur, const WeightParams& a, Piece* pc) {
+  return cur.next(a.rows, [&](const SeqPart& p) { return weight_shape(a, p); }, pc);
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(TREE_THREADS, 1)
+attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                         const __grid_constant__ WeightParams a) {
+  constexpr int HALVES = D / 64;
+  constexpr int HALF_BYTES = BLK * 128;
+  constexpr int TILE_BYTES = HALVES * HALF_BYTES;
+  constexpr int STAGES = K_RING / TILE_BYTES;
+  static_assert(STAGES <= MAX_STAGES, "");
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], s_full[2][2], s_empty[2][2];
+  __shared__ __align__(16) float row_lse[2][BLK];          // per Q tile: the rows' lse (0 where a row does not count)
+  __shared__ uint32_t row_ok[2][4];                        // which rows count
+  __shared__ uint64_t node_mask[2][BLK][MASK_WORDS];       // and, where a piece has drafted slots, what the tile's nodes see of them
+  __shared__ Span span;
+  __shared__ int64_t warp_sums[TREE_THREADS / 32];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int cta_failed;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = q_smem + 2 * Q_TILE;
+
+  if (threadIdx.x == 0) {
+    cta_failed = 0;
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 3);          // the copy and the two warps that fill row_lse
+      mbar_init(&q_empty[i], 9);         // the MMAs and the eight summing warps
+      for (int j = 0; j < 2; ++j) { mbar_init(&s_full[i][j], 1); mbar_init(&s_empty[i][j], 4); }
+    }
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc<512>(&tmem_slot);
+    tmem_relinquish();
+  }
+  if (warp == 8 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); }
+  pdl_launch_dependents();
+  pdl_wait();
+  make_span(a.rows, MIN_SPAN, &span, warp_sums, [&](const SeqPart& p) { return weight_shape(a, p); });
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = tmem_slot;
+  Cursor cur(span);
+  Piece pc{};
+  bool ok = true;
+  uint32_t n_q = 0;                      // Q tiles so far: tile n is in slot n & 1
+
+  if (warp == 8) {
+    // ------------------------------------------------------------ copies
+    uint32_t n_tile = 0;
+    while (ok && next_piece(cur, a, &pc)) {
+      const int tiles = n_tiles(a, pc.part);
+      if (tiles == 0) continue;          // no rows: the weights only decay
+      auto load_q = [&](int t) {
+        const int qs = n_q & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+        if (!ok) return;
+        ++n_q;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&q_full[qs], HALVES * a.tile_nodes * a.group * 128);
+          for (int h = 0; h < HALVES; ++h)
+            tma_load_3d(q_smem + qs * Q_TILE + h * HALF_BYTES, &tmQ, &q_full[qs], h * 64, pc.unit * a.group, pc.part.row0 + t * a.tile_nodes);
+        }
+        __syncwarp();
+      };
+      if (tiles == 1) load_q(0);
+      for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
+        const int st = n_tile % STAGES;
+        const int where = tile_place(a.kv, pc.part, pc.seq, blk, lane);
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+        if (!ok) break;
+        ++n_tile;
+        if (lane == 0) mbar_arrive_expect_tx(&full[st], TILE_BYTES);
+        __syncwarp();
+        load_tile<HALVES>(ring + st * TILE_BYTES, &tmK, &full[st], a.kv.page_table != nullptr, where, pc.unit * D, blk, lane);
+        for (int t = 0; t < tiles && tiles > 1 && ok; ++t) load_q(t);
+      }
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ MMA issuer
+    if (lane == 0) {
+      uint32_t n_tile = 0, n_s[2] = {0, 0};
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok && !mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
+      };
+      while (ok && next_piece(cur, a, &pc)) {
+        const int tiles = n_tiles(a, pc.part);
+        if (tiles == 0) continue;
+        for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
+          const int i = (blk - pc.blk_begin) & 1;
+          const int st = n_tile % STAGES;
+          wait(&full[st], (n_tile / STAGES) & 1u);
+          ++n_tile;
+          const uint32_t ka = smem_u32(ring + st * TILE_BYTES);
+          for (int t = 0; t < tiles && ok; ++t) {
+            const int qs = n_q & 1;
+            wait(&q_full[qs], (n_q >> 1) & 1u);
+            const uint32_t n = i == 0 ? n_s[0] : n_s[1];
+            const int buf = n & 1;
+            wait(&s_empty[i][buf], ((n >> 1) & 1u) ^ 1u);
+            if (!ok) break;
+            if (i == 0) ++n_s[0]; else ++n_s[1];
+            tc_fence_after_sync();
+            const int cols = (min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group + 15) & ~15;
+            const uint32_t idesc = make_idesc_f16(BLK, cols, BF16 ? 1 : 0, 0, 0);
+            const uint32_t qa = smem_u32(q_smem + qs * Q_TILE);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
+              umma_ss(tmem + (i * 2 + buf) * BLK, make_smem_desc_sw128(ka + off, 16, 1024), make_smem_desc_sw128(qa + off, 16, 1024), idesc, kk != 0);
+            }
+            umma_commit(&s_full[i][buf]);
+            if (tiles > 1 || blk + 1 == pc.blk_end) { umma_commit(&q_empty[qs]); ++n_q; }
+          }
+          if (ok) umma_commit(&empty[st]);
+        }
+      }
+    }
+  } else if (warp >= 10) {
+    // ------------------------------------------------------------ the rows' lse
+    const int tid = threadIdx.x - 320;
+    while (ok && next_piece(cur, a, &pc)) {
+      const int tiles = n_tiles(a, pc.part);
+      const int loads = tiles == 1 ? 1 : tiles * (pc.blk_end - pc.blk_begin);
+      for (int x = 0; x < loads && ok; ++x) {
+        const int t = tiles == 1 ? 0 : x % tiles;
+        const int qs = n_q & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
+        if (!ok) break;
+        ++n_q;
+        const int n_rows = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int r = k * 64 + tid;
+          float z = -INFINITY;
+          if (r < n_rows) {
+            const int row = pc.part.row0 + t * a.tile_nodes + r / a.group;
+            if (!a.use || __ldg(a.use + row) != 0) z = ld_dep_f32(a.lse + static_cast<size_t>(row) * a.n_q_heads + pc.unit * a.group + r % a.group);
+          }
+          const uint32_t counts = __ballot_sync(0xffffffffu, z != -INFINITY);
+          row_lse[qs][r] = z != -INFINITY ? z : 0.f;
+          if (lane == 0) row_ok[qs][k * 2 + warp - 10] = counts;
+        }
+        if (pc.blk_end * BLK > pc.part.ctx_len) {
+          const int nodes = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes), words = (pc.part.n_nodes + 63) / 64;
+          for (int e = tid; e < nodes * words; e += 64) {
+            const int node = t * a.tile_nodes + e / words, w = e % words;
+            uint64_t bits;
+            if (a.rows.mask) bits = __ldg(a.rows.mask + static_cast<size_t>(pc.part.row0 + node) * a.rows.mask_words + w);
+            else bits = node < 64 * w ? 0ull : node - 64 * w >= 63 ? ~0ull : (1ull << (node - 64 * w + 1)) - 1;
+            node_mask[qs][e / words][w] = bits;
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[qs]);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ sums (warps 0-7): thread = slot of the block
+    const int i = warp >> 2, quarter = warp & 3;
+    const int r = quarter * 32 + lane;
+    const uint32_t t_s = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + i * 2 * BLK;
+    uint32_t n_s = 0;
+    while (ok && next_piece(cur, a, &pc)) {
+      const int tiles = n_tiles(a, pc.part), len = pc.part.ctx_len + pc.part.n_nodes;
+      float* w_row = a.w_out + (static_cast<size_t>(pc.seq) * a.kv.n_kv_heads + pc.unit) * a.w_stride;
+      const float* in_row = a.w_in ? a.w_in + (static_cast<size_t>(pc.seq) * a.kv.n_kv_heads + pc.unit) * a.w_stride : nullptr;
+      for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
+        const bool mine = ((blk - pc.blk_begin) & 1) == i;
+        const int slot = blk * BLK + r;
+        float before = 0.f, sum0 = 0.f, sum1 = 0.f;
+        if (mine && in_row && slot < len) before = ld_dep_f32(in_row + slot);
+        for (int t = 0; t < tiles; ++t) {
+          const int qs = n_q & 1;
+          if (tiles > 1 || blk == pc.blk_begin) {
+            ok = __all_sync(0xffffffffu, mbar_wait(&q_full[qs], (n_q >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+            if (!ok) break;
+          }
+          if (mine) {
+            const int buf = n_s & 1;
+            ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i][buf], (n_s >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+            if (!ok) break;
+            ++n_s;
+            tc_fence_after_sync();
+            const int n_rows = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group;
+#pragma unroll 1
+            for (int ch = 0; ch * 32 < n_rows; ++ch) {
+              uint32_t bits = row_ok[qs][ch];
+              if (bits == 0) continue;
+              uint32_t s[32];
+              tmem_ld_32x32(t_s + buf * BLK + ch * 32, s);
+              tmem_wait_ld();
+              if (slot >= pc.part.ctx_len) {           // a drafted slot: which of the rows see it
+                const int node = slot - pc.part.ctx_len;
+                uint32_t seen = 0;
+                if (slot < len) {
+                  const uint64_t* m = &node_mask[qs][0][node >> 6];
+#pragma unroll 4
+                  for (int c = 0; c < min(32, n_rows - ch * 32); ++c)
+                    seen |= static_cast<uint32_t>((m[(ch * 32 + c) / a.group * MASK_WORDS] >> (node & 63)) & 1u) << c;
+                }
+                seen &= bits;
+                bits = seen;
+              }
+              __syncwarp();
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) {
+                if (((row_ok[qs][ch] >> c) & 15u) == 0) continue;
+                const float4 z = *reinterpret_cast<const float4*>(&row_lse[qs][ch * 32 + c]);
+                // scale * s - lse in one rounding, then to base 2
+                const float e0 = fast_exp2(fmaf(__uint_as_float(s[c]), a.scale, -z.x) * LOG2E);
+                const float e1 = fast_exp2(fmaf(__uint_as_float(s[c + 1]), a.scale, -z.y) * LOG2E);
+                const float e2 = fast_exp2(fmaf(__uint_as_float(s[c + 2]), a.scale, -z.z) * LOG2E);
+                const float e3 = fast_exp2(fmaf(__uint_as_float(s[c + 3]), a.scale, -z.w) * LOG2E);
+                sum0 += (bits >> c) & 1u ? e0 : 0.f;
+                sum1 += (bits >> (c + 1)) & 1u ? e1 : 0.f;
+                sum0 += (bits >> (c + 2)) & 1u ? e2 : 0.f;
+                sum1 += (bits >> (c + 3)) & 1u ? e3 : 0.f;
+              }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s_empty[i][buf]);
+          }
+          if (tiles > 1 || blk + 1 == pc.blk_end) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_empty[qs]);
+            ++n_q;
+          }
+        }
+        if (ok && mine && slot < len) w_row[slot] = in_row ? fmaf(a.decay, before, sum0 + sum1) : sum0 + sum1;
+      }
+    }
+  }
+  if (!ok) cta_failed = 1;
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  if (cta_failed) {             // let this CTA's bulk copies land before its shared memory is released
+    if (threadIdx.x == 0) {
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < DRAIN_LIMIT_NS) { }
+    }
+    __syncthreads();
+  }
+  if (warp == 9) {
+    tc_fence_after_sync();
+    tmem_dealloc<512>(tmem);
+  }
+}
+
+template <int D, bool BF16>
+int launch_weights(const CUtensorMap& q, const CUtensorMap& k, const WeightParams& p, int n_ctas, cudaStream_t s) {
+  static bool set[MAX_DEVICES] = {};
+  const int dev = current_device_slot();
+  if (!set[dev]) {
+    if (cudaFuncSetAttribute(attention_weights_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, WEIGHTS_SMEM) != cudaSuccess) return -1;
+    set[dev] = true;
+  }
+  return launch_pdl(attention_weights_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), WEIGHTS_SMEM, s, q, k, p) == cudaSuccess ? 0 : -1;
+}
+
+}  // namespace
+
+int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t s) {
+  WeightParams p{};
+  p.kv = t.kv; p.rows = t.rows;
+  p.n_q_heads = t.n_q_heads;
+  p.group = t.n_q_heads / t.kv.n_kv_heads;
+  p.tile_nodes = std::min(BLK / p.group, t.rows.max_nodes);
+  p.scale = t.scale; p.decay = t.decay; p.lse = t.lse; p.use = t.use;
+  p.w_in = t.w_in; p.w_out = t.w_out; p.w_stride = t.w_stride;
+  p.err_word = static_cast<int*>(t.workspace);
+  CUtensorMap q{}, k;
+  if ((t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) ||
+      pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0)
+    return -1;
+  const int n_ctas = std::min(n_sms, MAX_CTAS);
+  if (t.kv.head_dim == 128)
+    return t.kv.bf16 ? launch_weights<128, true>(q, k, p, n_ctas, s) : launch_weights<128, false>(q, k, p, n_ctas, s);
+  return t.kv.bf16 ? launch_weights<64, true>(q, k, p, n_ctas, s) : launch_weights<64, false>(q, k, p, n_ctas, s);
+}
+
+}  // namespace pc

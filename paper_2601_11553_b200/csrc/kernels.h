@@ -194,7 +194,7 @@ int make_paged_attn_maps(AttnMaps* out, const __nv_bfloat16* qpool_layer, const 
 void launch_attention_merge(const AttnMerge* merges, int n_merges, const float* partial_o, const float* partial_ml,
                             __half* out, int n_q_heads, int n_kv_heads, cudaStream_t s);
 
-// ---- operators on the cache of a decoding batch (attn_tree.cu, slots.cu; entry points in ops_api.cu)
+// ---- operators on the cache of a decoding batch (attn_tree.cu, attn_weights.cu, slots.cu; entry points in ops_api.cu)
 struct KvView {                // percache_kv_t
   const void *k, *v;
   int64_t k_stride, v_stride;  // elements

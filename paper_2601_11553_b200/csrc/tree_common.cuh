@@ -1,0 +1,186 @@
+// What the kernels on a decoding batch's cache share: the device-side schedule, masks, workspace layout, small arithmetic.
+#pragma once
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace pc {
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int BLK = 128;                        // context slots per block, rows per tile
+constexpr int TREE_THREADS = 384;
+constexpr int UNIT_COST = 2;                    // what a unit costs beside its blocks (Q, the row's end), in blocks
+
+// Workspace: the error word, one merge record per CTA, partial results (two slots per CTA).
+constexpr int WS_MERGE = 256, WS_ML = 16384;
+constexpr int MAX_CTAS = 160;
+constexpr size_t WS_O = WS_ML + sizeof(float) * 2 * BLK * 2 * MAX_CTAS;
+static_assert(WS_MERGE + sizeof(int) * 8 * MAX_CTAS <= WS_ML, "");
+static_assert(WS_O + sizeof(float) * 2 * MAX_CTAS * BLK * HEAD_DIM <= (24u << 20), "PERCACHE_OPS_WORKSPACE_BYTES");
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// ---------------------------------------------------------------------------------------------------- schedule
+// What a prompt's work looks like to the schedule: units of n_blk blocks, each block costing blk_cost, each unit UNIT_COST more.
+struct Shape { int units, n_blk, blk_cost; };
+struct Span { int64_t begin, end, total; int n_ctas, seq; int64_t seq_start; };
+struct Piece {                   // blocks [blk_begin, blk_end) of one unit
+  int seq, unit, blk_begin, blk_end, n_blk;
+  SeqPart part;
+  int64_t unit_end;              // cost position behind the unit
+};
+
+__device__ __forceinline__ int64_t shape_cost(const Shape& s) {
+  return static_cast<int64_t>(s.n_blk * s.blk_cost + UNIT_COST) * s.units;
+}
+
+// The CTA's span and the prompt it starts in: block-wide, every thread takes a run of prompts.  shape(part): a prompt's Shape.
+template <typename ShapeFn>
+__device__ __forceinline__ void make_span(const TreeRows& rows, int min_span, Span* sp, int64_t* warp_sums, ShapeFn shape) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (rows.n_seqs + TREE_THREADS - 1) / TREE_THREADS;
+  const int b0 = min(tid * per, rows.n_seqs), b1 = min(b0 + per, rows.n_seqs);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += shape_cost(shape(seq_part(rows, b)));
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) warp_sums[warp] = incl;
+  __syncthreads();
+  int64_t before = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < TREE_THREADS / 32; ++w) {
+    const int64_t x = warp_sums[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / min_span, static_cast<int64_t>(1))));
+  const int c = blockIdx.x;
+  const int64_t begin = c < n ? total * c / n : total, end = c < n ? total * (c + 1) / n : total;
+  if (tid == 0) { sp->begin = begin; sp->end = end; sp->total = total; sp->n_ctas = n; sp->seq = rows.n_seqs; sp->seq_start = total; }
+  __syncthreads();
+  if (mine > 0 && begin >= before && begin < before + mine) {         // one thread at most
+    int b = b0;
+    int64_t at = before;
+    for (; b < b1; ++b) {
+      const int64_t cost = shape_cost(shape(seq_part(rows, b)));
+      if (begin < at + cost) break;
+      at += cost;
+    }
+    sp->seq = b;
+    sp->seq_start = at;
+  }
+  __syncthreads();
+}
+
+struct Cursor {
+  int64_t pos, end, seq_start;
+  int seq;
+  __device__ __forceinline__ explicit Cursor(const Span& s) : pos(s.begin), end(s.end), seq_start(s.seq_start), seq(s.seq) {}
+  template <typename ShapeFn>
+  __device__ __forceinline__ bool next(const TreeRows& rows, ShapeFn shape, Piece* pc) {
+    while (pos < end && seq < rows.n_seqs) {
+      const SeqPart p = seq_part(rows, seq);
+      const Shape sh = shape(p);
+      const int64_t whole = shape_cost(sh);
+      if (pos >= seq_start + whole) { seq_start += whole; ++seq; continue; }
+      const int cost = sh.n_blk * sh.blk_cost + UNIT_COST;
+      const int unit = static_cast<int>((pos - seq_start) / cost);
+      const int64_t unit_start = seq_start + static_cast<int64_t>(unit) * cost, unit_end = unit_start + cost;
+      const int64_t stop = min(end, unit_end);
+      // a unit's own cost lies ahead of its blocks: a border inside it leaves the whole unit to the later span; a border
+      // inside a block leaves the block to the later span
+      const int bb = max(static_cast<int>(pos - unit_start) - UNIT_COST, 0) / sh.blk_cost;
+      const int be = max(static_cast<int>(stop - unit_start) - UNIT_COST, 0) / sh.blk_cost;
+      pos = stop;
+      if (be <= bb) continue;
+      pc->seq = seq; pc->unit = unit; pc->part = p;
+      pc->blk_begin = bb; pc->blk_end = be; pc->n_blk = sh.n_blk; pc->unit_end = unit_end;
+      return true;
+    }
+    return false;
+  }
+};
+
+// Bits of the nodes j0 .. j0 + 31 (j0 may be negative) that a node sees.
+__device__ __forceinline__ uint32_t node_bits(const TreeRows& r, int row, int node, int n_nodes, int j0) {
+  if (j0 <= -32 || j0 >= n_nodes) return 0u;
+  const int lo = max(j0, 0);
+  uint64_t w = 0;
+  if (r.mask != nullptr) {
+    const uint64_t* m = r.mask + static_cast<size_t>(row) * r.mask_words;
+    w = __ldg(m + (lo >> 6)) >> (lo & 63);
+    if ((lo & 63) != 0 && (lo >> 6) + 1 < r.mask_words) w |= __ldg(m + (lo >> 6) + 1) << (64 - (lo & 63));
+  } else if (node >= lo) {
+    w = node - lo >= 63 ? ~0ull : (1ull << (node - lo + 1)) - 1;
+  }
+  if (n_nodes - lo < 64) w &= (1ull << (n_nodes - lo)) - 1;
+  return static_cast<uint32_t>(w << (lo - j0));
+}
+// A 128-slot tile of K or V rows through a map of pool_map(): called by a whole warp.  With pages eight lanes per 64-column
+// half copy one page each; `where` then is the lane's page id, else the pool row of the prompt's slot 0 (lane 0).
+template <int HALVES>
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, bool paged, int where, int col, int blk,
+                                          int lane) {
+  if (paged) {
+    if (lane < 8 * HALVES)
+      tma_load_2d(dst + (lane >> 3) * (BLK * 128) + (lane & 7) * (PAGE_TOKENS * 128), tm, bar, col + (lane >> 3) * 64, where * PAGE_TOKENS);
+  } else if (lane == 0) {
+    for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * (BLK * 128), tm, bar, col + h * 64, where + blk * BLK);
+  }
+}
+// `where` of load_tile: pages behind the prompt's last slot repeat its last page (masked either way).
+__device__ __forceinline__ int tile_place(const KvView& kv, const SeqPart& p, int seq, int blk, int lane) {
+  if (!kv.page_table) return lane == 0 ? __ldg(kv.ctx_start + seq) : 0;
+  const int last = (p.ctx_len + max(p.n_nodes, 1) - 1) / PAGE_TOKENS;
+  return __ldg(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
+}
+
+// K or V rows as a 2-D map of 64-column boxes: a page's 16 rows or a block's 128
+inline int pool_map(CUtensorMap* out, const void* base, const KvView& kv, int64_t stride) {
+  const uint64_t dims[2] = {static_cast<uint64_t>(kv.n_kv_heads) * kv.head_dim, static_cast<uint64_t>(kv.n_slots)};
+  const uint64_t str[1] = {static_cast<uint64_t>(stride) * 2};
+  const uint32_t box[2] = {64u, static_cast<uint32_t>(kv.page_table ? PAGE_TOKENS : BLK)};
+  return encode_f16_map(out, base, 2, dims, str, box);
+}
+
+// Rows of q as a 3-D map: one box is the query heads of a KV head for a tile of nodes.
+inline int q_map(CUtensorMap* out, const void* q, const KvView& kv, int64_t stride, int n_q_heads, int n_rows, int tile_nodes) {
+  const uint64_t dims[3] = {static_cast<uint64_t>(kv.head_dim), static_cast<uint64_t>(n_q_heads), static_cast<uint64_t>(n_rows)};
+  const uint64_t str[2] = {static_cast<uint64_t>(kv.head_dim) * 2, static_cast<uint64_t>(stride) * 2};
+  const uint32_t box[3] = {64u, static_cast<uint32_t>(n_q_heads / kv.n_kv_heads), static_cast<uint32_t>(tile_nodes)};
+  return encode_f16_map(out, q, 3, dims, str, box);
+}
+
+}  // namespace
+}  // namespace pc
