@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct as _struct
 from dataclasses import dataclass
 from typing import Any, Dict, List, Optional, Sequence
 
@@ -474,62 +475,87 @@ def qa_top1(bank: Any, queries: Any, tau_query: float, device: int = 0, stream: 
 # ---------------------------------------------------------------------- operators on a decoding batch's cache
 OPS_WORKSPACE_BYTES = 24 << 20
 MAX_TREE_NODES = 256
-_KV_TYPES = {"torch.bfloat16": 0, "torch.float16": 1}
 
 
-def _arg(x: Any, name: str, dtype: Any, device: int, shape: Optional[Sequence[Optional[int]]] = None) -> int:
-    """Address of a contiguous device tensor of the given type(s) and shape (None: any extent); 0 for None."""
-    if x is None:
-        return 0
-    if not x.is_cuda or x.device.index != device:
-        raise ValueError(f"{name}: expected a tensor on cuda:{device}")
-    if str(x.dtype) != dtype and str(x.dtype) not in dtype.split("|"):
-        raise ValueError(f"{name}: expected {dtype}, got {x.dtype}")
-    if not x.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor")
-    if shape is not None and (len(x.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, x.shape))):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
-    return x.data_ptr()
+class _Types:
+    """torch's types, looked up once (this module does not need torch for anything else)."""
+
+    def __init__(self):
+        import torch
+        self.i32, self.f32, self.u8 = (torch.int32,), (torch.float32,), (torch.uint8,)
+        self.flag, self.word = (torch.uint8, torch.bool), (torch.int64, torch.uint64)
+        self.pool = {torch.bfloat16: 0, torch.float16: 1}
+
+
+_types: Optional[_Types] = None
+_pack_kv = _struct.Struct("@PPqqqPPiiii").pack
+_pack_rows = _struct.Struct("@iiiiPPPii").pack
+
+
+def _t() -> _Types:
+    global _types
+    if _types is None:
+        _types = _Types()
+    return _types
+
+
+def _arg(x: Any, name: str, dtypes: Any, device: int, shape: Any = None) -> int:
+    """Address of a contiguous tensor of one of the types on the device, with this shape (None: any)."""
+    if x.dtype in dtypes and x.get_device() == device and x.is_contiguous() and (shape is None or x.shape == shape):
+        return x.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous tensor of {' or '.join(map(str, dtypes))} on cuda:{device}"
+                     f"{'' if shape is None else f' of shape {tuple(shape)}'}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+
+
+def _table(x: Any, name: str, dtypes: Any, device: int, n: int) -> int:
+    """The same for an [n, any] tensor."""
+    if len(x.shape) != 2 or x.shape[0] != n:
+        raise ValueError(f"{name}: expected shape ({n}, any), got {tuple(x.shape)}")
+    return _arg(x, name, dtypes, device)
 
 
 def _row_stride(x: Any, name: str, heads: int, head_dim: int) -> int:
     """Elements between the rows of a [rows, heads, head_dim] tensor whose heads and elements lie one behind the other."""
-    st = x.stride()
-    if len(st) != 3 or x.shape[1] != heads or x.shape[2] != head_dim or st[2] != 1 or (heads > 1 and st[1] != head_dim):
+    shape, st = x.shape, x.stride()
+    if len(st) != 3 or shape[1] != heads or shape[2] != head_dim or st[2] != 1 or (heads > 1 and st[1] != head_dim):
         raise ValueError(f"{name}: expected [rows, {heads}, {head_dim}] with dense heads")
-    return st[0] if x.shape[0] > 1 else max(st[0], heads * head_dim)
+    return st[0] if shape[0] > 1 else max(st[0], heads * head_dim)
 
 
 def _kv(k: Any, v: Any, page_table: Any, ctx_start: Any, n_seqs: int) -> KvStruct:
-    if len(k.shape) != 3 or not k.is_cuda:
+    dev = k.get_device()
+    if len(k.shape) != 3 or dev < 0:
         raise ValueError("k: expected a [slots, kv_heads, head_dim] tensor on a CUDA device")
-    kind = _KV_TYPES.get(str(k.dtype))
+    ty = _t()
+    kind = ty.pool.get(k.dtype)
     if kind is None:
         raise ValueError(f"k: expected bfloat16 or float16, got {k.dtype}")
     slots, heads, dim = k.shape
-    dev = k.device.index
-    ks = _row_stride(k, "k", heads, dim)
-    vs, vp = 0, None
+    ks, vs, vp = _row_stride(k, "k", heads, dim), 0, 0
     if v is not None:
-        if v.dtype != k.dtype or v.device != k.device or v.shape[0] != slots:
+        if v.dtype != k.dtype or v.get_device() != dev or v.shape[0] != slots:
             raise ValueError("v: expected k's type, device and number of slots")
         vs, vp = _row_stride(v, "v", heads, dim), v.data_ptr()
     if (page_table is None) == (ctx_start is None):
         raise ValueError("give either page_table or ctx_start")
-    pt = _arg(page_table, "page_table", "torch.int32", dev, (n_seqs, None))
-    cs = _arg(ctx_start, "ctx_start", "torch.int32", dev, (n_seqs,))
-    return KvStruct(k.data_ptr(), vp, ks, vs, slots, pt or None, cs or None, page_table.shape[1] if pt else 0, heads, dim, kind)
+    if page_table is not None:
+        pt, width, cs = _table(page_table, "page_table", ty.i32, dev, n_seqs), page_table.shape[1], 0
+    else:
+        pt, width, cs = 0, 0, _arg(ctx_start, "ctx_start", ty.i32, dev, (n_seqs,))
+    return KvStruct.from_buffer_copy(_pack_kv(k.data_ptr(), vp, ks, vs, slots, pt, cs, width, heads, dim, kind))
 
 
 def _rows(q: Any, k: Any, ctx_len: Any, row_start: Any, mask: Any, max_nodes: int, max_len: int) -> RowsStruct:
-    dev = k.device.index
-    if q.dtype != k.dtype or q.device != k.device:
-        raise ValueError("q: expected k's type and device")
-    n_seqs, n_rows = ctx_len.shape[0], q.shape[0]
-    m = _arg(mask, "mask", "torch.int64|torch.uint64", dev, (n_rows, None))
-    return RowsStruct(n_seqs, n_rows, max_nodes, max_len, _arg(ctx_len, "ctx_len", "torch.int32", dev, (n_seqs,)) or None,
-                      _arg(row_start, "row_start", "torch.int32", dev, (n_seqs + 1,)) or None, m or None,
-                      mask.shape[1] if m else 0, 0)
+    dev = k.get_device()
+    if q.dtype != k.dtype or q.get_device() != dev or len(q.shape) != 3:
+        raise ValueError("q: expected [rows, q_heads, head_dim] of k's type on k's device")
+    n_seqs, n_rows, ty = ctx_len.shape[0], q.shape[0], _t()
+    m, words = 0, 0
+    if mask is not None:
+        m, words = _table(mask, "mask", ty.word, dev, n_rows), mask.shape[1]
+    return RowsStruct.from_buffer_copy(_pack_rows(
+        n_seqs, n_rows, max_nodes, max_len, _arg(ctx_len, "ctx_len", ty.i32, dev, (n_seqs,)),
+        _arg(row_start, "row_start", ty.i32, dev, (n_seqs + 1,)), m, words, 0))
 
 
 def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len: Any, row_start: Any, max_nodes: int,
@@ -540,16 +566,17 @@ def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len
     q, out: [rows, q_heads, head_dim]; k, v: [slots, kv_heads, head_dim] (pages: slots = 16 x pages); lse: fp32
     [rows, q_heads] or None; mask: int64 words [rows, ceil(max_nodes / 64)] or None (node i sees nodes 0 .. i); workspace:
     uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` and returns `out`."""
-    dev = k.device.index
     kv = _kv(k, v, page_table, ctx_start, ctx_len.shape[0])
     rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
-    hq, d = q.shape[1], kv.head_dim
-    if out.dtype != q.dtype or out.device != q.device or out.shape != q.shape:
+    dev, ty = k.get_device(), _t()
+    n_rows, hq, d = q.shape
+    if out.dtype != q.dtype or out.get_device() != dev or out.shape[0] != n_rows:
         raise ValueError("out: expected q's type, device and shape")
-    _check(load_library().percache_tree_attention(
-        dev, stream, kv, rows, q.data_ptr(), _row_stride(q, "q", hq, d), hq, d ** -0.5 if scale is None else scale,
-        out.data_ptr(), _row_stride(out, "out", hq, d), _arg(lse, "lse", "torch.float32", dev, (q.shape[0], hq)),
-        _arg(workspace, "workspace", "torch.uint8", dev), workspace.numel()), "percache_tree_attention")
+    qs, os_ = _row_stride(q, "q", hq, k.shape[2]), _row_stride(out, "out", hq, k.shape[2])
+    rc = load_library().percache_tree_attention(
+        dev, stream, kv, rows, q.data_ptr(), qs, hq, d ** -0.5 if scale is None else scale, out.data_ptr(), os_,
+        0 if lse is None else _arg(lse, "lse", ty.f32, dev, (n_rows, hq)), _arg(workspace, "workspace", ty.u8, dev), workspace.numel())
+    _check(rc, "percache_tree_attention")
     return out
 
 
@@ -560,19 +587,20 @@ def attention_weights(q: Any, k: Any, lse: Any, weights: Any, weights_out: Any =
     """percache_attention_weights: weights_out = decay * weights + the softmax weights of the rows with use != 0, summed
     per slot over the rows and the query heads of a KV head.  weights: fp32 [seqs, kv_heads, slots]; weights_out None: in
     place.  Enqueues on `stream` and returns weights_out."""
-    dev = k.device.index
     n_seqs = ctx_len.shape[0]
     kv = _kv(k, None, page_table, ctx_start, n_seqs)
     rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
-    hq = q.shape[1]
+    dev, ty = k.get_device(), _t()
+    n_rows, hq, d = q.shape
     weights_out = weights if weights_out is None else weights_out
-    shape = (n_seqs, kv.n_kv_heads, weights_out.shape[2])
-    _check(load_library().percache_attention_weights(
-        dev, stream, kv, rows, q.data_ptr(), _row_stride(q, "q", hq, kv.head_dim), hq,
-        kv.head_dim ** -0.5 if scale is None else scale, _arg(lse, "lse", "torch.float32", dev, (q.shape[0], hq)),
-        _arg(use, "use", "torch.uint8|torch.bool", dev, (q.shape[0],)), decay,
-        _arg(weights, "weights", "torch.float32", dev, shape), _arg(weights_out, "weights_out", "torch.float32", dev, shape),
-        shape[2], _arg(workspace, "workspace", "torch.uint8", dev), workspace.numel()), "percache_attention_weights")
+    heads, width = k.shape[1], weights_out.shape[2]
+    rc = load_library().percache_attention_weights(
+        dev, stream, kv, rows, q.data_ptr(), _row_stride(q, "q", hq, k.shape[2]), hq, d ** -0.5 if scale is None else scale,
+        _arg(lse, "lse", ty.f32, dev, (n_rows, hq)), 0 if use is None else _arg(use, "use", ty.flag, dev, (n_rows,)), decay,
+        0 if weights is None else _arg(weights, "weights", ty.f32, dev, (n_seqs, heads, width)),
+        _arg(weights_out, "weights_out", ty.f32, dev, (n_seqs, heads, width)), width,
+        _arg(workspace, "workspace", ty.u8, dev), workspace.numel())
+    _check(rc, "percache_attention_weights")
     return weights_out
 
 
@@ -581,12 +609,12 @@ def select_slots(weights: Any, length: Any, keep: Any, count: Any, *, sink: int 
     """percache_select_slots: keep [seqs, heads, budget] (int32, ascending, -1 behind the last) and count [seqs] of the
     slots that stay: the first `sink`, the last `recent`, and the heaviest of the rest."""
     n_seqs, heads, width = weights.shape
-    dev = weights.device.index
-    _check(load_library().percache_select_slots(
-        dev, stream, _arg(weights, "weights", "torch.float32", dev), width, _arg(length, "length", "torch.int32", dev, (n_seqs,)),
+    dev, ty = weights.get_device(), _t()
+    rc = load_library().percache_select_slots(
+        dev, stream, _arg(weights, "weights", ty.f32, dev), width, _arg(length, "length", ty.i32, dev, (n_seqs,)),
         n_seqs, heads, width if max_len is None else max_len, keep.shape[2], sink, recent,
-        _arg(keep, "keep", "torch.int32", dev, (n_seqs, heads, None)), _arg(count, "count", "torch.int32", dev, (n_seqs,))),
-        "percache_select_slots")
+        _arg(keep, "keep", ty.i32, dev, (n_seqs, heads, keep.shape[2])), _arg(count, "count", ty.i32, dev, (n_seqs,)))
+    _check(rc, "percache_select_slots")
     return keep, count
 
 
@@ -596,21 +624,25 @@ def compact_slots(k: Any, v: Any, keep: Any, count: Any, *, max_len: int, weight
     """percache_compact_slots: slot first[b] + j of the destination takes the K, V and weight of slot keep[b][head][j].
     Without dst_page_table / dst_start in place (keep strictly ascending, keep[j] >= first + j); weights_out None: the
     weights in place."""
-    dev = k.device.index
     n_seqs = count.shape[0]
     kv = _kv(k, v, page_table, ctx_start, n_seqs)
+    dev, ty = k.get_device(), _t()
     weights_out = weights if weights_out is None else weights_out
-    width = 0 if weights is None else weights.shape[2]
-    shape = (n_seqs, kv.n_kv_heads, width)
-    _check(load_library().percache_compact_slots(
-        dev, stream, kv, n_seqs, max_len, _arg(dst_page_table, "dst_page_table", "torch.int32", dev, (n_seqs, None)),
-        0 if dst_page_table is None else dst_page_table.shape[1], _arg(dst_start, "dst_start", "torch.int32", dev, (n_seqs,)),
-        _arg(first, "first", "torch.int32", dev, (n_seqs,)), _arg(keep, "keep", "torch.int32", dev, (n_seqs, None, None)),
-        keep.shape[1], keep.shape[2], _arg(count, "count", "torch.int32", dev, (n_seqs,)),
-        _arg(weights, "weights", "torch.float32", dev, shape), _arg(weights_out, "weights_out", "torch.float32", dev, shape),
-        width), "percache_compact_slots")
+    heads, width = k.shape[1], 0 if weights is None else weights.shape[2]
+    shape, keep_heads, budget = (n_seqs, heads, width), keep.shape[1], keep.shape[2]
+    rc = load_library().percache_compact_slots(
+        dev, stream, kv, n_seqs, max_len,
+        0 if dst_page_table is None else _table(dst_page_table, "dst_page_table", ty.i32, dev, n_seqs),
+        0 if dst_page_table is None else dst_page_table.shape[1],
+        0 if dst_start is None else _arg(dst_start, "dst_start", ty.i32, dev, (n_seqs,)),
+        0 if first is None else _arg(first, "first", ty.i32, dev, (n_seqs,)),
+        _arg(keep, "keep", ty.i32, dev, (n_seqs, keep_heads, budget)), keep_heads, budget,
+        _arg(count, "count", ty.i32, dev, (n_seqs,)),
+        0 if weights is None else _arg(weights, "weights", ty.f32, dev, shape),
+        0 if weights is None else _arg(weights_out, "weights_out", ty.f32, dev, shape), width)
+    _check(rc, "percache_compact_slots")
 
 
 def ops_status(workspace: Any, stream: int = 0) -> None:
     """percache_ops_status: waits for `stream`; raises PerCacheError if a call that used this workspace gave up a wait."""
-    _check(load_library().percache_ops_status(workspace.device.index, stream, workspace.data_ptr()), "percache_ops_status")
+    _check(load_library().percache_ops_status(workspace.get_device(), stream, workspace.data_ptr()), "percache_ops_status")
