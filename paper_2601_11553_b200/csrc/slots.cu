@@ -1,4 +1,6 @@
 // Which slots of a context to keep, and moving the kept ones together.
+#include <algorithm>
+
 #include "kernels.h"
 #include "ptx.cuh"
 
@@ -6,8 +8,13 @@ namespace pc {
 namespace {
 
 // ---------------------------------------------------------------------------------------------------- choice
-constexpr int SEL_THREADS = 1024;
-constexpr int SEL_WARPS = SEL_THREADS / 32;
+// One block per (prompt, head).  The budget-th largest key is found by radix selection (11, 11 and 10 bits from the top: a
+// histogram of the keys that share the prefix found so far, and the bin in which the budget runs out); then every warp
+// counts and writes its own stretch of slots: those above the key, and of the equal ones as many as are left, lowest
+// slot first, so the list comes out ascending.  The weights are read five times, but only the first time from beyond L1 for
+// contexts that fit there; the kernel is bound by the latency of its dependent passes, not by its bytes.
+constexpr int SEL_BITS = 11, SEL_BINS = 1 << SEL_BITS;
+constexpr int SEL_UNROLL = 8;
 
 // Order-preserving map of a weight to 32 bits (NaN as -infinity, -0 as 0); slots that are always kept come first.
 __device__ __forceinline__ uint32_t weight_key(float w, int slot, int len, int sink, int recent) {
@@ -17,136 +24,256 @@ __device__ __forceinline__ uint32_t weight_key(float w, int slot, int len, int s
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// One block per (prompt, head): the budget-th largest key by radix selection, eight bits at a time from the top, then
-// one ordered pass that writes the slots above it and as many of the equal ones as are left, lowest slot first.
-__global__ void __launch_bounds__(SEL_THREADS)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 select_slots_kernel(const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ length, int n_heads,
                     int max_len, int budget, int sink, int recent, int32_t* __restrict__ keep, int32_t* __restrict__ count) {
-  __shared__ int hist[256];
-  __shared__ uint32_t sh_prefix;
-  __shared__ int sh_need;
-  __shared__ int warp_gt[SEL_WARPS], warp_eq[SEL_WARPS];
+  constexpr int WARPS = THREADS / 32;
+  constexpr int BINS_EACH = SEL_BINS / THREADS;
+  static_assert(SEL_BINS % THREADS == 0, "");
+  __shared__ int hist[SEL_BINS];
+  __shared__ int warp_sum[WARPS], warp_gt[WARPS], warp_eq[WARPS];
+  __shared__ int sh_bin, sh_need;
   const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int len = min(max(__ldg(length + b), 0), max_len);
   const float* w = weights + (static_cast<size_t>(b) * n_heads + h) * w_stride;
   int32_t* out = keep + (static_cast<size_t>(b) * n_heads + h) * budget;
   if (h == 0 && tid == 0) count[b] = min(len, budget);
-  for (int j = min(len, budget) + tid; j < budget; j += SEL_THREADS) out[j] = -1;
   if (len <= budget) {
-    for (int j = tid; j < len; j += SEL_THREADS) out[j] = j;
+    for (int j = tid; j < budget; j += THREADS) out[j] = j < len ? j : -1;
     return;
   }
-  uint32_t prefix = 0;
+  uint32_t prefix = 0;                     // the key's bits found so far, and which bits those are
+  uint32_t known = 0;
   int need = budget;                       // how many of the keys that share the prefix are kept
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += SEL_THREADS) hist[i] = 0;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t digit = pass == 2 ? 1023u : 2047u;
+    for (int i = tid; i < SEL_BINS; i += THREADS) hist[i] = 0;
     __syncthreads();
-    for (int s = tid; s < len; s += SEL_THREADS) {
-      const uint32_t k = weight_key(w[s], s, len, sink, recent);
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+    for (int s0 = tid; s0 < len; s0 += THREADS * SEL_UNROLL) {
+      float x[SEL_UNROLL];
+#pragma unroll
+      for (int u = 0; u < SEL_UNROLL; ++u) x[u] = s0 + u * THREADS < len ? __ldg(w + s0 + u * THREADS) : 0.f;
+#pragma unroll
+      for (int u = 0; u < SEL_UNROLL; ++u) {
+        const int s = s0 + u * THREADS;
+        const uint32_t k = weight_key(x[u], s, len, sink, recent);
+        if (s < len && (k & known) == prefix) atomicAdd(&hist[(k >> shift) & digit], 1);
+      }
     }
     __syncthreads();
-    if (tid == 0) {
-      int left = need, d = 255;
-      while (hist[d] < left) left -= hist[d--];
-      sh_prefix = prefix | (static_cast<uint32_t>(d) << shift);
-      sh_need = left;
+    // thread t has the bins from the top: BINS - 1 - t * BINS_EACH downwards; the one where the running count reaches `need`
+    int c[BINS_EACH], mine = 0;
+#pragma unroll
+    for (int i = 0; i < BINS_EACH; ++i) { c[i] = hist[SEL_BINS - 1 - tid * BINS_EACH - i]; mine += c[i]; }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int before = incl - mine;
+    for (int i = 0; i < warp; ++i) before += warp_sum[i];
+    if (before < need && before + mine >= need) {
+#pragma unroll
+      for (int i = 0; i < BINS_EACH; ++i) {
+        if (before < need && before + c[i] >= need) { sh_bin = SEL_BINS - 1 - tid * BINS_EACH - i; sh_need = need - before; }
+        before += c[i];
+      }
     }
     __syncthreads();
-    prefix = sh_prefix;
+    prefix |= static_cast<uint32_t>(sh_bin) << shift;
+    known |= digit << shift;
     need = sh_need;
   }
-  int base = 0, eq_base = 0;               // slots written so far; equal ones seen so far
-  for (int s0 = 0; s0 < len; s0 += SEL_THREADS) {
-    const int s = s0 + tid;
-    const uint32_t k = s < len ? weight_key(w[s], s, len, sink, recent) : 0u;
-    const bool gt = s < len && k > prefix, eq = s < len && k == prefix;
-    const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
-    if (lane == 0) { warp_gt[warp] = __popc(bg); warp_eq[warp] = __popc(be); }
-    __syncthreads();
-    int g0 = 0, e0 = 0, g_all = 0, e_all = 0;
-    for (int i = 0; i < SEL_WARPS; ++i) {
-      if (i < warp) { g0 += warp_gt[i]; e0 += warp_eq[i]; }
-      g_all += warp_gt[i]; e_all += warp_eq[i];
+  // every warp its own stretch
+  const int each = (len + WARPS - 1) / WARPS;
+  const int lo = min(warp * each, len), hi = min(lo + each, len);
+  int gt = 0, eq = 0;
+  for (int s0 = lo + lane; s0 < hi; s0 += 32 * SEL_UNROLL) {
+#pragma unroll
+    for (int u = 0; u < SEL_UNROLL; ++u) {
+      const int s = s0 + u * 32;
+      if (s < hi) {
+        const uint32_t k = weight_key(__ldg(w + s), s, len, sink, recent);
+        gt += k > prefix;
+        eq += k == prefix;
+      }
     }
-    const int eq_before = eq_base + e0 + __popc(be & ((1u << lane) - 1));
-    const int gt_before = g0 + __popc(bg & ((1u << lane) - 1));
-    if (gt || (eq && eq_before < need)) out[base + gt_before + min(eq_before, need) - min(eq_base, need)] = s;
-    base += g_all + min(eq_base + e_all, need) - min(eq_base, need);
-    eq_base += e_all;
-    __syncthreads();
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    gt += __shfl_xor_sync(0xffffffffu, gt, o);
+    eq += __shfl_xor_sync(0xffffffffu, eq, o);
+  }
+  if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
+  __syncthreads();
+  int gt_before = 0, eq_before = 0;
+  for (int i = 0; i < warp; ++i) { gt_before += warp_gt[i]; eq_before += warp_eq[i]; }
+  const uint32_t below = (1u << lane) - 1;
+  for (int s0 = lo; s0 < hi; s0 += 32 * SEL_UNROLL) {
+    float x[SEL_UNROLL];
+#pragma unroll
+    for (int u = 0; u < SEL_UNROLL; ++u) x[u] = s0 + u * 32 + lane < hi ? __ldg(w + s0 + u * 32 + lane) : 0.f;
+#pragma unroll
+    for (int u = 0; u < SEL_UNROLL; ++u) {
+      const int s = s0 + u * 32 + lane;
+      const uint32_t k = weight_key(x[u], s, len, sink, recent);
+      const bool is_gt = s < hi && k > prefix, is_eq = s < hi && k == prefix;
+      const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
+      const int e = eq_before + __popc(be & below);
+      if (is_gt || (is_eq && e < need)) out[gt_before + __popc(bg & below) + min(e, need)] = s;
+      gt_before += __popc(bg);
+      eq_before += __popc(be);
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------------- moving
-constexpr int MOVE_THREADS = 512;
-constexpr int MOVE_UNROLL = 4;
+constexpr int MOVE_THREADS = 256;
 
-// A block moves one slice of (prompt, KV head): all vectors of K, all of V, or the weights.  In place the list's chunks
-// go in order, each read whole before it is written: its sources lie at or behind the chunk's own start, because
-// keep[j] >= first + j and the list ascends, so no later chunk reads what an earlier one has written.
-__global__ void __launch_bounds__(MOVE_THREADS) compact_slots_kernel(CompactSlots a) {
-  const int b = blockIdx.z, g = blockIdx.y, slice = blockIdx.x;
+struct Move { int64_t src, dst; };       // pool rows, or dst = -1: nothing moves
+__device__ __forceinline__ Move move_of(const CompactSlots& a, int b, int j, int n, int first, const int32_t* keep) {
+  Move m{0, -1};
+  if (j >= n) return m;
+  const int s = __ldg(keep + j), t = first + j;
+  if (s < 0 || s >= a.max_len || t < 0 || t >= a.max_len) return m;
+  const int32_t* pt = a.dst_page_table ? a.dst_page_table : a.kv.page_table;
+  const int stride = a.dst_page_table ? a.dst_pt_stride : a.kv.pt_stride;
+  if (pt && t / PAGE_TOKENS >= stride) return m;
+  const int64_t src = slot_row(a.kv.page_table, a.kv.pt_stride, a.kv.ctx_start, a.kv.n_slots, b, s);
+  const int64_t dst = slot_row(pt, stride, a.dst_start ? a.dst_start : a.kv.ctx_start, a.kv.n_slots, b, t);
+  if (src < 0 || dst < 0) return m;
+  m.src = src;
+  m.dst = dst;
+  return m;
+}
+
+// To another place: nothing that is read is written, so every (prompt, KV head, stretch of the list) is a block of its own.
+// 16 lanes (8 for head size 64) take a row of K and of V; a thread has MOVE_ROWS rows of both in flight.  Bound by HBM:
+// 2 x 4 D bytes a kept slot and head.
+constexpr int MOVE_ROWS = 4;
+template <int D>
+__global__ void __launch_bounds__(MOVE_THREADS) copy_slots_kernel(CompactSlots a) {
+  constexpr int VECS = D / 8, ROWS = MOVE_THREADS / VECS;
+  const int b = blockIdx.z, g = blockIdx.y;
+  const int n = min(min(max(__ldg(a.count + b), 0), a.budget), a.max_len);
+  const int j0 = blockIdx.x * ROWS * MOVE_ROWS + threadIdx.x / VECS;
+  if (static_cast<int>(blockIdx.x) * ROWS * MOVE_ROWS >= n) return;
+  const int c = threadIdx.x % VECS;
+  const int first = a.first ? __ldg(a.first + b) : 0;
+  const int32_t* keep = a.keep + (static_cast<size_t>(b) * a.keep_heads + (a.keep_heads == 1 ? 0 : g)) * a.budget;
+  const uint4* k = static_cast<const uint4*>(a.kv.k) + g * VECS + c;
+  const uint4* v = static_cast<const uint4*>(a.kv.v) + g * VECS + c;
+  const int64_t ks = a.kv.k_stride / 8, vs = a.kv.v_stride / 8;
+  Move m[MOVE_ROWS];
+  uint4 rk[MOVE_ROWS], rv[MOVE_ROWS];
+#pragma unroll
+  for (int u = 0; u < MOVE_ROWS; ++u) m[u] = move_of(a, b, j0 + u * ROWS, n, first, keep);
+#pragma unroll
+  for (int u = 0; u < MOVE_ROWS; ++u) {
+    if (m[u].dst < 0) continue;
+    rk[u] = k[m[u].src * ks];
+    rv[u] = v[m[u].src * vs];
+  }
+#pragma unroll
+  for (int u = 0; u < MOVE_ROWS; ++u) {
+    if (m[u].dst < 0) continue;
+    const_cast<uint4*>(k)[m[u].dst * ks] = rk[u];
+    const_cast<uint4*>(v)[m[u].dst * vs] = rv[u];
+  }
+  if (a.w_in && a.w_in != a.w_out && c == 0) {
+    const size_t row = (static_cast<size_t>(b) * a.kv.n_kv_heads + g) * a.w_stride;
+#pragma unroll
+    for (int u = 0; u < MOVE_ROWS; ++u) {
+      const int j = j0 + u * ROWS, s = j < n ? __ldg(keep + j) : -1;
+      if (s >= 0 && s < a.max_len && first + j >= 0 && first + j < a.max_len) a.w_out[row + first + j] = __ldg(a.w_in + row + s);
+    }
+  }
+}
+
+// In place.  A block owns a slice (some 16-byte vectors of K or of V, or the weights) of one (prompt, KV head) and takes the
+// list's chunks in order, each read whole before any of it is written: its sources lie at or behind the chunk's own first
+// slot, because keep[j] >= first + j and the list ascends, so no chunk reads what an earlier one has written.  Slices, not
+// chunks, are what runs in parallel; the host makes them as narrow as it takes to fill the SMs.
+constexpr int SHIFT_UNROLL = 8;
+__global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots a, int slices, int vecs, int first_slice) {
+  const int b = blockIdx.z, g = blockIdx.y, slice = blockIdx.x + first_slice;
   const int n = min(min(max(__ldg(a.count + b), 0), a.budget), a.max_len);
   const int first = a.first ? __ldg(a.first + b) : 0;
   const int32_t* keep = a.keep + (static_cast<size_t>(b) * a.keep_heads + (a.keep_heads == 1 ? 0 : g)) * a.budget;
-  const int32_t* dpt = a.dst_page_table ? a.dst_page_table : a.kv.page_table;
-  const int dpt_stride = a.dst_page_table ? a.dst_pt_stride : a.kv.pt_stride;
-  const int32_t* dst0 = a.dst_start ? a.dst_start : a.kv.ctx_start;
-  if (first < 0) return;
-  if (slice == 2) {
-    if (!a.w_in) return;
+  if (slice == 2 * slices) {
     const size_t row = (static_cast<size_t>(b) * a.kv.n_kv_heads + g) * a.w_stride;
-    for (int j0 = 0; j0 < n; j0 += MOVE_THREADS) {
-      const int j = j0 + threadIdx.x;
-      const int s = j < n ? keep[j] : -1;
-      const bool ok = s >= 0 && s < a.max_len && first + j < a.max_len;
-      const float w = ok ? a.w_in[row + s] : 0.f;
+    for (int j0 = 0; j0 < n; j0 += MOVE_THREADS * SHIFT_UNROLL) {
+      float w[SHIFT_UNROLL];
+      bool ok[SHIFT_UNROLL];
+#pragma unroll
+      for (int u = 0; u < SHIFT_UNROLL; ++u) {
+        const int j = j0 + u * MOVE_THREADS + threadIdx.x;
+        const int s = j < n ? __ldg(keep + j) : -1;
+        ok[u] = s >= 0 && s < a.max_len && first + j >= 0 && first + j < a.max_len;
+        if (ok[u]) w[u] = a.w_in[row + s];
+      }
       __syncthreads();
-      if (ok) a.w_out[row + first + j] = w;
+#pragma unroll
+      for (int u = 0; u < SHIFT_UNROLL; ++u)
+        if (ok[u]) a.w_out[row + first + j0 + u * MOVE_THREADS + threadIdx.x] = w[u];
     }
     return;
   }
-  const int vecs = a.kv.head_dim / 8;                 // 16-byte vectors of a head's row
-  const int64_t stride = slice == 0 ? a.kv.k_stride : a.kv.v_stride;
-  uint4* pool = reinterpret_cast<uint4*>(const_cast<void*>(slice == 0 ? a.kv.k : a.kv.v));
-  const int total = n * vecs;
-  for (int e0 = 0; e0 < total; e0 += MOVE_THREADS * MOVE_UNROLL) {
-    uint4 r[MOVE_UNROLL];
-    int64_t to[MOVE_UNROLL];
+  const bool is_k = slice < slices;
+  const int64_t stride = (is_k ? a.kv.k_stride : a.kv.v_stride) / 8;
+  uint4* pool = static_cast<uint4*>(const_cast<void*>(is_k ? a.kv.k : a.kv.v)) + g * (a.kv.head_dim / 8) +
+                (is_k ? slice : slice - slices) * vecs + threadIdx.x % vecs;
+  const int rows = MOVE_THREADS / vecs;
+  for (int j0 = 0; j0 < n; j0 += rows * SHIFT_UNROLL) {
+    uint4 r[SHIFT_UNROLL];
+    int64_t to[SHIFT_UNROLL];
 #pragma unroll
-    for (int u = 0; u < MOVE_UNROLL; ++u) {
-      const int e = e0 + u * MOVE_THREADS + threadIdx.x;
-      to[u] = -1;
-      if (e >= total) continue;
-      const int j = e / vecs, c = e % vecs;
-      const int s = keep[j], t = first + j;
-      if (s < 0 || s >= a.max_len || t >= a.max_len) continue;
-      if (dpt && t / PAGE_TOKENS >= dpt_stride) continue;
-      const int64_t src = slot_row(a.kv.page_table, a.kv.pt_stride, a.kv.ctx_start, a.kv.n_slots, b, s);
-      const int64_t dst = slot_row(dpt, dpt_stride, dst0, a.kv.n_slots, b, t);
-      if (src < 0 || dst < 0) continue;
-      r[u] = pool[(src * stride + g * a.kv.head_dim) / 8 + c];
-      to[u] = (dst * stride + g * a.kv.head_dim) / 8 + c;
+    for (int u = 0; u < SHIFT_UNROLL; ++u) {
+      const Move m = move_of(a, b, j0 + u * rows + threadIdx.x / vecs, n, first, keep);
+      to[u] = m.dst == m.src ? -1 : m.dst;
+      if (to[u] >= 0) r[u] = pool[m.src * stride];
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < MOVE_UNROLL; ++u)
-      if (to[u] >= 0) pool[to[u]] = r[u];
+    for (int u = 0; u < SHIFT_UNROLL; ++u)
+      if (to[u] >= 0) pool[to[u] * stride] = r[u];
   }
 }
 
 }  // namespace
 
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
-                        int budget, int sink, int recent, int32_t* keep, int32_t* count, int, cudaStream_t s) {
-  select_slots_kernel<<<dim3(n_heads, n_seqs), SEL_THREADS, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget,
-                                                                    sink, recent, keep, count);
+                        int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s) {
+  const dim3 grid(n_heads, n_seqs);
+  // as many threads to a list as the batch leaves room for: with one list per SM or fewer the passes' latency is all there is
+  if (static_cast<int64_t>(n_seqs) * n_heads <= n_sms)
+    select_slots_kernel<1024><<<grid, 1024, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
+  else
+    select_slots_kernel<512><<<grid, 512, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
   return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
 }
 
-int launch_compact_slots(const CompactSlots& a, int, cudaStream_t s) {
-  compact_slots_kernel<<<dim3(3, a.kv.n_kv_heads, a.n_seqs), MOVE_THREADS, 0, s>>>(a);
+int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s) {
+  const int n = std::min(a.budget, a.max_len), vecs = a.kv.head_dim / 8;
+  const bool in_place = !a.dst_page_table && !a.dst_start;
+  const bool shift_weights = a.w_in && (in_place || a.w_in == a.w_out);
+  if (!in_place) {
+    const int rows = MOVE_THREADS / vecs * MOVE_ROWS;
+    const dim3 grid((n + rows - 1) / rows, a.kv.n_kv_heads, a.n_seqs);
+    if (a.kv.head_dim == 128) copy_slots_kernel<128><<<grid, MOVE_THREADS, 0, s>>>(a);
+    else copy_slots_kernel<64><<<grid, MOVE_THREADS, 0, s>>>(a);
+  }
+  if (in_place || shift_weights) {
+    int slices = 1;
+    while (slices < vecs / 2 && static_cast<int64_t>(a.n_seqs) * a.kv.n_kv_heads * 2 * slices < 4 * static_cast<int64_t>(n_sms)) slices *= 2;
+    const int first_slice = in_place ? 0 : 2 * slices, last = 2 * slices + (shift_weights ? 1 : 0);
+    shift_slots_kernel<<<dim3(last - first_slice, a.kv.n_kv_heads, a.n_seqs), MOVE_THREADS, 0, s>>>(a, slices, vecs / slices, first_slice);
+  }
   return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
 }
 
