@@ -26,92 +26,15 @@
 // the latter raises a flag, and the rows that do see such a value get it added when they are written.
 #include <algorithm>
 
-#include "tree_common.cuh"
+#include "tree_attn.cuh"
 
 namespace pc {
 namespace {
 
-constexpr float LN2 = 0.6931471805599453f;
 constexpr int RING_BYTES = 160 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
 constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
-constexpr int MAX_STAGES = 10;
 constexpr uint32_t TMEM_S = 256;
-constexpr float RESCALE_THRESHOLD = 8.0f;       // the running reference is raised when a block exceeds it by 2^8
-constexpr int FLAGS = 8;
-constexpr int MIN_SPAN = 4;                     // least cost of a span: shorter ones cost more to merge than they save
-
-struct MergeRecord {             // written by the CTA that has a cut unit's first part
-  int32_t n_parts;               // 0: none
-  int32_t row0, n_rows;          // first global row of the tile, valid tile rows
-  int32_t head0, cta;
-  int32_t pad[3];
-};
-
-struct TreeParams {
-  KvView kv;
-  TreeRows rows;
-  int32_t n_q_heads, group, tile_nodes;
-  float scale_log2;
-  void* out;
-  int64_t out_stride;
-  float* lse;
-  int* err_word;
-  MergeRecord* merges;
-  float *partial_ml, *partial_o;
-};
-
-__device__ __forceinline__ Shape tree_shape(const TreeParams& a, const SeqPart& p) {
-  if (p.n_nodes == 0) return Shape{0, 0, 1};
-  return Shape{(p.n_nodes + a.tile_nodes - 1) / a.tile_nodes * a.kv.n_kv_heads, (p.ctx_len + p.n_nodes + BLK - 1) / BLK, 1};
-}
-struct Item {
-  int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes
-  int row0, node0, n_rows;       // the tile: first global row, first node, valid tile rows
-  int g, blk_begin, blk_end, n_blk;
-  int64_t unit_end;
-};
-__device__ __forceinline__ bool next_item(Cursor& cur, const TreeParams& a, Item* it) {
-  Piece pc;
-  if (!cur.next(a.rows, [&](const SeqPart& p) { return tree_shape(a, p); }, &pc)) return false;
-  // the tiles of one KV head follow each other: they share K and V in L2
-  const int tiles = (pc.part.n_nodes + a.tile_nodes - 1) / a.tile_nodes, tile = pc.unit % tiles;
-  it->seq = pc.seq; it->ctx_len = pc.part.ctx_len; it->n_nodes = pc.part.n_nodes;
-  it->node0 = tile * a.tile_nodes;
-  it->row0 = pc.part.row0 + it->node0;
-  it->n_rows = min(a.tile_nodes, pc.part.n_nodes - it->node0) * a.group;
-  it->g = pc.unit / tiles;
-  it->blk_begin = pc.blk_begin; it->blk_end = pc.blk_end; it->n_blk = pc.n_blk; it->unit_end = pc.unit_end;
-  return true;
-}
-// Bits of the 32 slots from slot0 on that a node sees.
-__device__ __forceinline__ uint32_t slot_bits(const TreeRows& r, const Item& it, int row, int node, int slot0) {
-  const int in_ctx = it.ctx_len - slot0;
-  if (in_ctx >= 32) return 0xffffffffu;
-  return (in_ctx > 0 ? (1u << in_ctx) - 1 : 0u) | node_bits(r, row, node, it.n_nodes, -in_ctx);
-}
-
-// Two values in the pools' type.  A finite value past fp16's range (an average of values at its limit, rounded up) becomes the
-// largest finite one; infinity stays infinity.
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack_out(float a, float b) {
-  if constexpr (BF16) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t*>(&v);
-  } else {
-    if (isinf(a) || isinf(b)) {
-      const uint32_t lo = __half_as_ushort(isinf(a) ? __float2half_rn(a) : to_half_sat(a));
-      const uint32_t hi = __half_as_ushort(isinf(b) ? __float2half_rn(b) : to_half_sat(b));
-      return lo | (hi << 16);
-    }
-    return pack_half2(a, b);
-  }
-}
-template <bool BF16>
-__device__ __forceinline__ float elem(uint32_t bits16) {
-  if constexpr (BF16) return __uint_as_float(bits16 << 16);
-  else return __half2float(__ushort_as_half(static_cast<unsigned short>(bits16)));
-}
 
 // ---------------------------------------------------------------------------------------------------- attention
 template <int D, bool BF16>
@@ -156,6 +79,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = tmem_slot;
+  const Pipe pipe{q_smem, 0, HALF_BYTES, ring, &q_full, &q_empty, full, empty, raw, &bad_v[0][0], nullptr};
   // 384 threads start with 168 registers each (64 512); the softmax holds a whole row of scores and wants more, the other
   // warpgroup needs few: 256 x 208 + 128 x 80 = 63 488
   if (warp >= 8) {
@@ -163,47 +87,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     Cursor cur(span);
     Item it{};
    if (warp == 8) {
-    // ------------------------------------------------------------ copies
-    uint32_t n_item = 0, n_tile = 0, n_raw = 0;
-    MergeRecord rec{};
-    bool ok = true;
-    auto load = [&](const CUtensorMap* tm, int blk, bool clean) {
-      const int st = n_tile % STAGES;
-      const uint32_t ph = (n_tile / STAGES) & 1u;
-      ++n_tile;
-      const int where = tile_place(a.kv, SeqPart{it.row0, it.n_nodes, it.ctx_len}, it.seq, blk, lane);
-      ok = __all_sync(0xffffffffu, mbar_wait(&empty[st], ph ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
-      if (!ok) return;
-      // a tile that warps 10-11 have to clean lands on a barrier of theirs; they then complete `full` in its place
-      uint64_t* bar = clean ? &raw[n_raw++ % STAGES] : &full[st];
-      if (lane == 0) mbar_arrive_expect_tx(bar, TILE_BYTES);
-      if (lane == 1 && !clean) mbar_arrive(bar);
-      __syncwarp();
-      load_tile<HALVES>(ring + st * TILE_BYTES, tm, bar, a.kv.page_table != nullptr, where, it.g * D, blk, lane);
-    };
-    while (ok && next_item(cur, a, &it)) {
-      if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
-        rec.n_parts = static_cast<int>((it.unit_end * span.n_ctas - 1) / span.total) - static_cast<int>(blockIdx.x) + 1;
-        rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group; rec.cta = blockIdx.x;
-      }
-      const int nb = it.blk_end - it.blk_begin;
-      ok = __all_sync(0xffffffffu, mbar_wait(&q_empty, (n_item & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
-      if (!ok) break;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&q_full, HALVES * a.tile_nodes * a.group * 128);
-        for (int h = 0; h < HALVES; ++h) tma_load_3d(q_smem + h * HALF_BYTES, &tmQ, &q_full, h * 64, it.g * a.group, it.row0);
-      }
-      __syncwarp();
-      load(&tmK, it.blk_begin, false);
-      if (ok && nb > 1) load(&tmK, it.blk_begin + 1, false);
-      for (int j = 0; j < nb && ok; ++j) {
-        load(&tmV, it.blk_begin + j, (it.blk_begin + j + 1) * BLK > it.ctx_len);
-        if (ok && j + 2 < nb) load(&tmK, it.blk_begin + j + 2, false);
-      }
-      ++n_item;
-    }
-    if (!ok) cta_failed = 1;
-    if (lane == 0) a.merges[blockIdx.x] = rec;
+    copy_role<D, STAGES, 1, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
    } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
     if (lane == 0) {
@@ -214,48 +98,42 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (ok && !mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
       };
-      const uint32_t qa = smem_u32(q_smem);
-      auto issue_s = [&](int i) {
-        const int st = n_tile % STAGES;
-        wait(&full[st], (n_tile / STAGES) & 1u);
-        ++n_tile;
-        if (!ok) return;
-        tc_fence_after_sync();
-        const uint32_t ka = smem_u32(ring + st * TILE_BYTES);
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
-          umma_ss(tmem + TMEM_S + i * BLK, make_smem_desc_sw128(qa + off, 16, 1024), make_smem_desc_sw128(ka + off, 16, 1024), idesc_qk, kk != 0);
-        }
-        umma_commit(&s_full[i]);
-        umma_commit(&empty[st]);
-      };
+      const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
       while (ok && next_item(cur, a, &it)) {
         const int nb = it.blk_end - it.blk_begin;
         wait(&q_full, n_item & 1u);
-        issue_s(0);
-        if (nb > 1) issue_s(1);
-        if (nb <= 2 && ok) umma_commit(&q_empty);
-        for (int j = 0; j < nb && ok; ++j) {
-          const int i = j & 1;
-          const int st = n_tile % STAGES;
-          wait(&p_full[i], (p_phase >> i) & 1u);
-          p_phase ^= 1u << i;
-          if (j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
+#pragma unroll 1
+        for (int x = 0; x < 2 * nb; ++x) {
+          const Step sp = step_of(x, nb);
+          const int i = sp.j & 1, st = n_tile % STAGES;
+          if (!sp.is_k) {
+            wait(&p_full[i], (p_phase >> i) & 1u);
+            p_phase ^= 1u << i;
+            if (sp.j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
+          }
           wait(&full[st], (n_tile / STAGES) & 1u);
           ++n_tile;
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t va = smem_u32(ring + st * TILE_BYTES);
+          const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
+          if (sp.is_k) {
+            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, 1024);
 #pragma unroll
-          for (int kk = 0; kk < BLK / 16; ++kk)
-            umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, make_smem_desc_sw128(va + kk * 2048, HALF_BYTES, 1024), idesc_pv,
-                    j > 1 || kk != 0);
-          umma_commit(&empty[st]);
-          if (j + 1 == nb) umma_commit(&o_full);
-          if (j + 2 < nb) {
-            issue_s(i);
-            if (j + 3 == nb && ok) umma_commit(&q_empty);
+            for (int kk = 0; kk < D / 16; ++kk) {
+              constexpr int H = HALF_BYTES;
+              const uint32_t off = ((kk >> 2) * H + (kk & 3) * 32) >> 4;
+              umma_ss(tmem + TMEM_S + i * BLK, q_desc + off, k_desc + off, idesc_qk, kk != 0);
+            }
+            umma_commit(&s_full[i]);
+            umma_commit(&empty[st]);
+            if (sp.j + 1 == nb) umma_commit(&q_empty);
+          } else {
+            const uint64_t v_desc = make_smem_desc_sw128(tile, HALF_BYTES, 1024);
+#pragma unroll
+            for (int kk = 0; kk < BLK / 16; ++kk)
+              umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2048 >> 4), idesc_pv, sp.j > 1 || kk != 0);
+            umma_commit(&empty[st]);
+            if (sp.j + 1 == nb) umma_commit(&o_full);
           }
         }
         ++n_item;
@@ -263,59 +141,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       if (!ok) cta_failed = 1;
     }
    } else {
-    // ------------------------------------------------------------ V tiles with drafted or no slots
-    const int tid = threadIdx.x - 320;
-    uint32_t n_item = 0, n_tile = 0, n_raw = 0;
-    bool ok = true;
-    while (ok && next_item(cur, a, &it)) {
-      const int nb = it.blk_end - it.blk_begin;
-      int* flag = &bad_v[n_item % FLAGS][warp - 10];       // read at the end of the item that set it, long before its next use
-      if (lane == 0) *flag = 0;
-      __syncwarp();
-      // the tiles' order in the ring: K0 [K1] V0 [K2] V1 ...
-      uint32_t tile = n_tile + (nb > 1 ? 2 : 1);
-      for (int j = 0; j < nb; ++j) {
-        const int blk = it.blk_begin + j;
-        if ((blk + 1) * BLK > it.ctx_len) {
-          const int st = tile % STAGES;
-          ok = __all_sync(0xffffffffu, mbar_wait(&raw[n_raw % STAGES], (n_raw / STAGES) & 1u, a.err_word, DEV_ERR_ATTN_CORR));
-          if (!ok) break;
-          ++n_raw;
-          uint8_t* v = ring + st * TILE_BYTES;
-          const int r0 = max(it.ctx_len - blk * BLK, 0), r_end = it.ctx_len + it.n_nodes - blk * BLK;
-          bool bad = false;
-          // thread t takes 16-byte vector t % 8 (as stored; the swizzle only permutes a row's vectors) of rows t / 8, t / 8 + 8 ...
-          for (int r = r0 + (tid >> 3); r < BLK; r += 8) {
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-              uint4* p = reinterpret_cast<uint4*>(v + h * HALF_BYTES + r * 128 + (tid & 7) * 16);
-              if (r >= r_end) {
-                *p = make_uint4(0, 0, 0, 0);
-              } else {
-                const uint4 x = *p;
-                uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                constexpr uint32_t E = BF16 ? 0x7f80u : 0x7c00u;             // all exponent bits set: infinity or NaN
-                bool any = false;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                  if ((w[q] & E) == E) { w[q] &= 0xffff0000u; any = true; }
-                  if (((w[q] >> 16) & E) == E) { w[q] &= 0x0000ffffu; any = true; }
-                }
-                if (any) { *p = make_uint4(w[0], w[1], w[2], w[3]); bad = true; }
-              }
-            }
-          }
-          if (bad) *reinterpret_cast<volatile int*>(flag) = 1;
-          fence_proxy_async_smem();                        // the MMA reads the tile through the async proxy
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&full[st]);
-        }
-        tile += j + 2 < nb ? 2 : 1;
-      }
-      n_tile += 2 * nb;
-      ++n_item;
-    }
-    if (!ok) cta_failed = 1;
+    clean_role<D, STAGES, BF16, false, false>(a, pipe, cur, &cta_failed);
    }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -437,6 +263,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         const bool whole = it.blk_begin == 0 && it.blk_end == it.n_blk;
         // a row that sees no slot at all (not: one whose scores are all -inf)
         bool any = it.ctx_len > 0;
+#pragma unroll 1
         for (int w = 0; w < it.n_nodes && !any; w += 32) any = node_bits(a.rows, row, node, it.n_nodes, w) != 0;
         __syncwarp();
         const float inv = whole ? 1.0f / L : 1.0f;
@@ -583,7 +410,12 @@ int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v
     if (cudaFuncSetAttribute(tree_attention_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, TREE_SMEM) != cudaSuccess) return -1;
     set[dev] = true;
   }
-  if (launch_pdl(tree_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), TREE_SMEM, s, q, k, v, p) != cudaSuccess) return -1;
+  // Up to 32 rows a tile: the transposed form.
+  if (p.tile_nodes * p.group <= NARROW_ROWS) {
+    if (launch_narrow_attention(q, k, v, p, n_ctas, s) != 0) return -1;
+  } else if (launch_pdl(tree_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), TREE_SMEM, s, q, k, v, p) != cudaSuccess) {
+    return -1;
+  }
   const int rows = std::min(p.tile_nodes, p.rows.max_nodes) * p.group;
   return launch_pdl(tree_merge_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
 }
@@ -607,6 +439,7 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   if (q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
+  if (!units_fit(static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads, p.rows.max_len, 1)) return -2;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_tree<128, true>(q, k, v, p, n_ctas, s) : launch_tree<128, false>(q, k, v, p, n_ctas, s);

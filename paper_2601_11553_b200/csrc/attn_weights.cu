@@ -107,7 +107,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       if (tiles == 0) continue;          // no rows: the weights only decay
       auto load_q = [&](int t) {
         const int qs = n_q & 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+        ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
         if (!ok) return;
         ++n_q;
         if (lane == 0) {
@@ -121,7 +121,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
         const int st = n_tile % STAGES;
         const int where = tile_place(a.kv, pc.part, pc.seq, blk, lane);
-        ok = __all_sync(0xffffffffu, mbar_wait(&empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+        ok = __all_sync(0xffffffffu, bar_wait(&empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
         if (!ok) break;
         ++n_tile;
         if (lane == 0) mbar_arrive_expect_tx(&full[st], TILE_BYTES);
@@ -135,7 +135,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     if (lane == 0) {
       uint32_t n_tile = 0, n_s[2] = {0, 0};
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
+        if (ok && !bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
       };
       while (ok && next_piece(cur, a, &pc)) {
         const int tiles = n_tiles(a, pc.part);
@@ -179,7 +179,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
       for (int x = 0; x < loads && ok; ++x) {
         const int t = tiles == 1 ? 0 : x % tiles;
         const int qs = n_q & 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
+        ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
         if (!ok) break;
         ++n_q;
         const int n_rows = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group;
@@ -199,10 +199,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           const int nodes = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes), words = (pc.part.n_nodes + 63) / 64;
           for (int e = tid; e < nodes * words; e += 64) {
             const int node = t * a.tile_nodes + e / words, w = e % words;
-            uint64_t bits;
-            if (a.rows.mask) bits = __ldg(a.rows.mask + static_cast<size_t>(pc.part.row0 + node) * a.rows.mask_words + w);
-            else bits = node < 64 * w ? 0ull : node - 64 * w >= 63 ? ~0ull : (1ull << (node - 64 * w + 1)) - 1;
-            node_mask[qs][e / words][w] = bits;
+            node_mask[qs][e / words][w] = node_word(a.rows, pc.part.row0 + node, node, w);
           }
         }
         __syncwarp();
@@ -227,12 +224,12 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         for (int t = 0; t < tiles; ++t) {
           const int qs = n_q & 1;
           if (tiles > 1 || blk == pc.blk_begin) {
-            ok = __all_sync(0xffffffffu, mbar_wait(&q_full[qs], (n_q >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+            ok = __all_sync(0xffffffffu, bar_wait(&q_full[qs], (n_q >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
             if (!ok) break;
           }
           if (mine) {
             const int buf = n_s & 1;
-            ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i][buf], (n_s >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+            ok = __all_sync(0xffffffffu, bar_wait(&s_full[i][buf], (n_s >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
             if (!ok) break;
             ++n_s;
             tc_fence_after_sync();
@@ -330,6 +327,7 @@ int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t 
   if ((t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) ||
       pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0)
     return -1;
+  if (!units_fit(p.kv.n_kv_heads, p.rows.max_len, (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes)) return -2;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_weights<128, true>(q, k, p, n_ctas, s) : launch_weights<128, false>(q, k, p, n_ctas, s);

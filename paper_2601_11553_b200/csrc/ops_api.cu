@@ -92,6 +92,7 @@ TreeRows tree_rows(const percache_rows_t& r) {
 
 int launched(int rc) {
   if (rc == 0) return PERCACHE_OK;
+  if (rc == -2) return PERCACHE_E_CAPACITY;
   cudaGetLastError();
   return PERCACHE_E_CUDA;
 }

@@ -7,6 +7,7 @@ namespace pc {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
 constexpr int BLK = 128;                        // context slots per block, rows per tile
 constexpr int TREE_THREADS = 384;
 constexpr int UNIT_COST = 2;                    // what a unit costs beside its blocks (Q, the row's end), in blocks
@@ -47,6 +48,19 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   return r;
 }
 
+// Bounded wait for kernels with many wait sites.  A wait site in line is a dozen instructions; the timed loop of mbar_wait (with its
+// error word) is one function of the kernel, entered by waits that take long.  Instruction fetches are what a small call's time
+// goes into: with everything in line these kernels had 100 KB of code, most of it run once.
+__device__ __noinline__ bool bar_wait_slow(uint64_t* bar, uint32_t parity, int* err_word, int code) {
+  return mbar_wait(bar, parity, err_word, code);
+}
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, int* err_word, int code) {
+#pragma unroll 1
+  for (int i = 0; i < 4096; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  return bar_wait_slow(bar, parity, err_word, code);
+}
+
 // ---------------------------------------------------------------------------------------------------- schedule
 // What a prompt's work looks like to the schedule: units of n_blk blocks, each block costing blk_cost, each unit UNIT_COST more.
 struct Shape { int units, n_blk, blk_cost; };
@@ -57,8 +71,10 @@ struct Piece {                   // blocks [blk_begin, blk_end) of one unit
   int64_t unit_end;              // cost position behind the unit
 };
 
-__device__ __forceinline__ int64_t shape_cost(const Shape& s) {
-  return static_cast<int64_t>(s.n_blk * s.blk_cost + UNIT_COST) * s.units;
+// Fits 32 bits: the host refuses sizes for which it might not (units_fit).
+__device__ __forceinline__ int shape_cost(const Shape& s) { return (s.n_blk * s.blk_cost + UNIT_COST) * s.units; }
+inline bool units_fit(int64_t units, int64_t max_len, int64_t blk_cost) {
+  return ((max_len + BLK - 1) / BLK * blk_cost + UNIT_COST) * units <= INT32_MAX;
 }
 
 // The CTA's span and the prompt it starts in: block-wide, every thread takes a run of prompts.  shape(part): a prompt's Shape.
@@ -68,6 +84,7 @@ __device__ __forceinline__ void make_span(const TreeRows& rows, int min_span, Sp
   const int per = (rows.n_seqs + TREE_THREADS - 1) / TREE_THREADS;
   const int b0 = min(tid * per, rows.n_seqs), b1 = min(b0 + per, rows.n_seqs);
   int64_t mine = 0;
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) mine += shape_cost(shape(seq_part(rows, b)));
   int64_t incl = mine;
 #pragma unroll
@@ -78,22 +95,25 @@ __device__ __forceinline__ void make_span(const TreeRows& rows, int min_span, Sp
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
   int64_t before = incl - mine, total = 0;
-#pragma unroll
+#pragma unroll 1
   for (int w = 0; w < TREE_THREADS / 32; ++w) {
     const int64_t x = warp_sums[w];
     if (w < warp) before += x;
     total += x;
   }
-  const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / min_span, static_cast<int64_t>(1))));
-  const int c = blockIdx.x;
-  const int64_t begin = c < n ? total * c / n : total, end = c < n ? total * (c + 1) / n : total;
+  const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / static_cast<uint32_t>(min_span), static_cast<int64_t>(1))));
+  // lanes 0 and 1 form the two borders: one division instead of two in the code
+  const int c = min(static_cast<int>(blockIdx.x) + (lane & 1), n);
+  const int64_t border = static_cast<int64_t>(static_cast<uint64_t>(total) * c / static_cast<uint32_t>(n));
+  const int64_t begin = __shfl_sync(0xffffffffu, border, 0), end = __shfl_sync(0xffffffffu, border, 1);
   if (tid == 0) { sp->begin = begin; sp->end = end; sp->total = total; sp->n_ctas = n; sp->seq = rows.n_seqs; sp->seq_start = total; }
   __syncthreads();
   if (mine > 0 && begin >= before && begin < before + mine) {         // one thread at most
     int b = b0;
     int64_t at = before;
+#pragma unroll 1
     for (; b < b1; ++b) {
-      const int64_t cost = shape_cost(shape(seq_part(rows, b)));
+      const int cost = shape_cost(shape(seq_part(rows, b)));
       if (begin < at + cost) break;
       at += cost;
     }
@@ -109,13 +129,14 @@ struct Cursor {
   __device__ __forceinline__ explicit Cursor(const Span& s) : pos(s.begin), end(s.end), seq_start(s.seq_start), seq(s.seq) {}
   template <typename ShapeFn>
   __device__ __forceinline__ bool next(const TreeRows& rows, ShapeFn shape, Piece* pc) {
+#pragma unroll 1
     while (pos < end && seq < rows.n_seqs) {
       const SeqPart p = seq_part(rows, seq);
       const Shape sh = shape(p);
-      const int64_t whole = shape_cost(sh);
+      const int whole = shape_cost(sh);
       if (pos >= seq_start + whole) { seq_start += whole; ++seq; continue; }
       const int cost = sh.n_blk * sh.blk_cost + UNIT_COST;
-      const int unit = static_cast<int>((pos - seq_start) / cost);
+      const int unit = static_cast<int>(pos - seq_start) / cost;
       const int64_t unit_start = seq_start + static_cast<int64_t>(unit) * cost, unit_end = unit_start + cost;
       const int64_t stop = min(end, unit_end);
       // a unit's own cost lies ahead of its blocks: a border inside it leaves the whole unit to the later span; a border
@@ -180,6 +201,19 @@ inline int q_map(CUtensorMap* out, const void* q, const KvView& kv, int64_t stri
   const uint64_t str[2] = {static_cast<uint64_t>(kv.head_dim) * 2, static_cast<uint64_t>(stride) * 2};
   const uint32_t box[3] = {64u, static_cast<uint32_t>(n_q_heads / kv.n_kv_heads), static_cast<uint32_t>(tile_nodes)};
   return encode_f16_map(out, q, 3, dims, str, box);
+}
+
+// Does a node see any node at all.
+__device__ __noinline__ bool sees_a_node(const TreeRows& r, int row, int node, int n_nodes) {
+  bool any = false;
+#pragma unroll 1
+  for (int w = 0; w < n_nodes && !any; w += 32) any = node_bits(r, row, node, n_nodes, w) != 0;
+  return any;
+}
+// One 64-bit word of what a node sees (bits of nodes past the prompt's last are whatever the caller wrote).
+__device__ __forceinline__ uint64_t node_word(const TreeRows& r, int row, int node, int w) {
+  if (r.mask) return __ldg(r.mask + static_cast<size_t>(row) * r.mask_words + w);
+  return node < 64 * w ? 0ull : node - 64 * w >= 63 ? ~0ull : (1ull << (node - 64 * w + 1)) - 1;
 }
 
 }  // namespace
