@@ -97,7 +97,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   __shared__ float fin_m[2][2][NC];
   __shared__ uint64_t node_mask[2 * 32 * MASK_WORDS];
   __shared__ int bad_v[FLAGS][2];
-  __shared__ Span span;
+  __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
   __shared__ uint32_t tmem_slot;
   __shared__ int cta_failed;
@@ -125,11 +125,11 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   }
   if (warp == 8 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
   pdl_launch_dependents();
-  pdl_wait();
-  make_span(a.rows, MIN_SPAN, &span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
+  const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   const uint32_t tmem = tmem_slot;
   const Pipe pipe{q_smem, Q_SLOT, Q_HALF, ring, q_full, q_empty, full, empty, raw, &bad_v[0][0], node_mask};
   Cursor cur(span);

@@ -50,7 +50,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   __shared__ __align__(8) uint64_t q_full, q_empty, full[MAX_STAGES], empty[MAX_STAGES], raw[MAX_STAGES], s_full[2], p_full[2], o_full, o_free, ml_full;
   __shared__ float ml[2][2][BLK][2];                     // [item parity][block parity][row]: reference, sum
   __shared__ int bad_v[FLAGS][2];
-  __shared__ Span span;
+  __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
   __shared__ uint32_t tmem_slot;
   __shared__ int cta_failed;
@@ -73,11 +73,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   }
   if (warp == 8 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); prefetch_tmap(&tmV); }
   pdl_launch_dependents();
-  pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
-  make_span(a.rows, MIN_SPAN, &span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
+  const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   const uint32_t tmem = tmem_slot;
   const Pipe pipe{q_smem, 0, HALF_BYTES, ring, &q_full, &q_empty, full, empty, raw, &bad_v[0][0], nullptr};
   // 384 threads start with 168 registers each (64 512); the softmax holds a whole row of scores and wants more, the other
@@ -439,8 +439,9 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   if (q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
-  if (!units_fit(static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads, p.rows.max_len, 1)) return -2;
+  if (!units_fit(p.rows.n_seqs, static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads, p.rows.max_len, 1)) return -2;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
+  p.small = small_batch(p.rows.n_seqs, static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads, p.rows.max_len, 1) ? 1 : 0;
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_tree<128, true>(q, k, v, p, n_ctas, s) : launch_tree<128, false>(q, k, v, p, n_ctas, s);
   return t.kv.bf16 ? launch_tree<64, true>(q, k, v, p, n_ctas, s) : launch_tree<64, false>(q, k, v, p, n_ctas, s);

@@ -29,7 +29,7 @@ constexpr int MIN_SPAN = 3;                      // unit cost and one block
 struct WeightParams {
   KvView kv;
   TreeRows rows;
-  int32_t n_q_heads, group, tile_nodes;
+  int32_t n_q_heads, group, tile_nodes, small;
   float scale, decay;
   const float* lse;
   const uint8_t* use;
@@ -63,7 +63,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   __shared__ __align__(16) float row_lse[2][BLK];          // per Q tile: the rows' lse (0 where a row does not count)
   __shared__ uint32_t row_ok[2][4];                        // which rows count
   __shared__ uint64_t node_mask[2][BLK][MASK_WORDS];       // and, where a piece has drafted slots, what the tile's nodes see of them
-  __shared__ Span span;
+  __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
   __shared__ uint32_t tmem_slot;
   __shared__ int cta_failed;
@@ -88,11 +88,11 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   }
   if (warp == 8 && lane == 0) { prefetch_tmap(&tmQ); prefetch_tmap(&tmK); }
   pdl_launch_dependents();
-  pdl_wait();
-  make_span(a.rows, MIN_SPAN, &span, warp_sums, [&](const SeqPart& p) { return weight_shape(a, p); });
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
+  const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return weight_shape(a, p); });
   const uint32_t tmem = tmem_slot;
   Cursor cur(span);
   Piece pc{};
@@ -189,7 +189,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           float z = -INFINITY;
           if (r < n_rows) {
             const int row = pc.part.row0 + t * a.tile_nodes + r / a.group;
-            if (!a.use || __ldg(a.use + row) != 0) z = ld_dep_f32(a.lse + static_cast<size_t>(row) * a.n_q_heads + pc.unit * a.group + r % a.group);
+            if (!a.use || ld_dep_u8(a.use + row) != 0) z = ld_dep_f32(a.lse + static_cast<size_t>(row) * a.n_q_heads + pc.unit * a.group + r % a.group);
           }
           const uint32_t counts = __ballot_sync(0xffffffffu, z != -INFINITY);
           row_lse[qs][r] = z != -INFINITY ? z : 0.f;
@@ -327,7 +327,8 @@ int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t 
   if ((t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) ||
       pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0)
     return -1;
-  if (!units_fit(p.kv.n_kv_heads, p.rows.max_len, (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes)) return -2;
+  if (!units_fit(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes)) return -2;
+  p.small = small_batch(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) ? 1 : 0;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_weights<128, true>(q, k, p, n_ctas, s) : launch_weights<128, false>(q, k, p, n_ctas, s);

@@ -251,24 +251,6 @@ int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* l
                         int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s);
 int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s);
 
-// A prompt's part of a batch, from the device-side arrays, clamped to the bounds the host knows.
-struct SeqPart { int row0, n_nodes, ctx_len; };
-__device__ __forceinline__ SeqPart seq_part(const TreeRows& r, int b) {
-  SeqPart p;
-  p.row0 = min(max(__ldg(r.row_start + b), 0), r.n_rows);
-  const int end = min(max(__ldg(r.row_start + b + 1), p.row0), r.n_rows);
-  p.n_nodes = min(min(end - p.row0, r.max_nodes), r.max_len);
-  p.ctx_len = min(max(__ldg(r.ctx_len + b), 0), r.max_len - p.n_nodes);
-  return p;
-}
-// Pool row of a prompt's slot, or -1 when it lies outside the pool.
-__device__ __forceinline__ int64_t slot_row(const int32_t* page_table, int pt_stride, const int32_t* start, int64_t n_slots,
-                                            int b, int slot) {
-  const int64_t r = page_table ? static_cast<int64_t>(__ldg(page_table + static_cast<size_t>(b) * pt_stride + slot / PAGE_TOKENS)) * PAGE_TOKENS + slot % PAGE_TOKENS
-                               : static_cast<int64_t>(__ldg(start + b)) + slot;
-  return r >= 0 && r < n_slots ? r : -1;
-}
-
 int init_driver_api();   // resolves cuTensorMapEncodeTiled once; 0 on success
 
 // Kernel attributes (dynamic shared memory limit) and cluster occupancy belong to a device, not to the process:

@@ -1,8 +1,7 @@
 // Which slots of a context to keep, and moving the kept ones together.
 #include <algorithm>
 
-#include "kernels.h"
-#include "ptx.cuh"
+#include "slot_row.cuh"
 
 namespace pc {
 namespace {

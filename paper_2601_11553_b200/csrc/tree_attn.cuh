@@ -14,7 +14,7 @@ struct MergeRecord {             // written by the CTA that has a cut unit's fir
 struct TreeParams {
   KvView kv;
   TreeRows rows;
-  int32_t n_q_heads, group, tile_nodes;
+  int32_t n_q_heads, group, tile_nodes, small;
   float scale_log2;
   void* out;
   int64_t out_stride;
@@ -39,8 +39,12 @@ struct Item {
   int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes
   int row0, node0, n_rows;       // the tile: first global row, first node, valid tile rows
   int g, blk_begin, blk_end, n_blk;
-  int64_t unit_end;
+  int unit_end;
 };
+// The last CTA with a part of a unit: where its last cost position lies.
+__device__ __forceinline__ int last_cta(const Span& s, int unit_end) {
+  return static_cast<int>(static_cast<uint64_t>((s.begin + unit_end) * s.n_ctas - 1) / static_cast<uint64_t>(s.total));
+}
 __device__ __forceinline__ bool next_item(Cursor& cur, const TreeParams& a, Item* it) {
   Piece pc;
   if (!cur.next(a.rows, [&](const SeqPart& p) { return tree_shape(a, p); }, &pc)) return false;
@@ -127,10 +131,6 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
   bool ok = true;
   Item it{};
   while (ok && next_item(cur, a, &it)) {
-    if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
-      rec.n_parts = static_cast<int>((it.unit_end * span.n_ctas - 1) / span.total) - static_cast<int>(blockIdx.x) + 1;
-      rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group; rec.cta = blockIdx.x;
-    }
     const int nb = it.blk_end - it.blk_begin, qs = n_item % QSLOTS;
     ok = __all_sync(0xffffffffu, role_wait<CALLS>(&pipe.q_empty[qs], ((n_item / QSLOTS) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
     if (!ok) break;
@@ -155,6 +155,10 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
       if (lane == 1 && !clean) mbar_arrive(bar);
       __syncwarp();
       load_tile<HALVES>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g * D, blk, lane);
+    }
+    if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
+      rec.n_parts = last_cta(span, it.unit_end) - static_cast<int>(blockIdx.x) + 1;
+      rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group; rec.cta = blockIdx.x;
     }
     ++n_item;
   }

@@ -1,7 +1,6 @@
 // What the kernels on a decoding batch's cache share: the device-side schedule, masks, workspace layout, small arithmetic.
 #pragma once
-#include "kernels.h"
-#include "ptx.cuh"
+#include "slot_row.cuh"
 
 namespace pc {
 namespace {
@@ -64,23 +63,89 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, int* er
 // ---------------------------------------------------------------------------------------------------- schedule
 // What a prompt's work looks like to the schedule: units of n_blk blocks, each block costing blk_cost, each unit UNIT_COST more.
 struct Shape { int units, n_blk, blk_cost; };
-struct Span { int64_t begin, end, total; int n_ctas, seq; int64_t seq_start; };
+// A prompt's part of a batch, from the device-side arrays, clamped to the bounds the host knows.
+struct SeqPart { int row0, n_nodes, ctx_len; };
+__device__ __forceinline__ SeqPart seq_part(const TreeRows& r, int b) {
+  const int first = ld_dep_s32(r.row_start + b), last = ld_dep_s32(r.row_start + b + 1), ctx = ld_dep_s32(r.ctx_len + b);
+  SeqPart p;
+  p.row0 = min(max(first, 0), r.n_rows);
+  p.n_nodes = min(min(min(max(last, p.row0), r.n_rows) - p.row0, r.max_nodes), r.max_len);
+  p.ctx_len = min(max(ctx, 0), r.max_len - p.n_nodes);
+  return p;
+}
+// A CTA's stretch of the batch's cost, and the prompt it starts in.
+struct Span {
+  int64_t begin, end, total, seq_start;
+  int n_ctas, seq;
+  SeqPart part;
+};
 struct Piece {                   // blocks [blk_begin, blk_end) of one unit
   int seq, unit, blk_begin, blk_end, n_blk;
   SeqPart part;
-  int64_t unit_end;              // cost position behind the unit
+  int unit_end;                  // cost position behind the unit, from the span's begin on
 };
 
-// Fits 32 bits: the host refuses sizes for which it might not (units_fit).
+// Fits 32 bits, as does a CTA's share of the batch: the host refuses sizes for which it might not (units_fit).
 __device__ __forceinline__ int shape_cost(const Shape& s) { return (s.n_blk * s.blk_cost + UNIT_COST) * s.units; }
-inline bool units_fit(int64_t units, int64_t max_len, int64_t blk_cost) {
-  return ((max_len + BLK - 1) / BLK * blk_cost + UNIT_COST) * units <= INT32_MAX;
+inline bool units_fit(int64_t n_seqs, int64_t units, int64_t max_len, int64_t blk_cost) {
+  const int64_t cost = ((max_len + BLK - 1) / BLK * blk_cost + UNIT_COST) * units;
+  return cost <= INT32_MAX / 4 && cost * n_seqs <= INT64_C(1) << 35;       // over 148 CTAs: a span below 2^28 + a unit
 }
 
-// The CTA's span and the prompt it starts in: block-wide, every thread takes a run of prompts.  shape(part): a prompt's Shape.
+// Batches the whole of whose cost times the CTA count stays in 32 bits, and of few prompts, are dealt by every warp for itself.
+constexpr int SMALL_BATCH = 256;
+inline bool small_batch(int n_seqs, int64_t units, int64_t max_len, int64_t blk_cost) {
+  return n_seqs <= SMALL_BATCH && ((max_len + BLK - 1) / BLK * blk_cost + UNIT_COST) * units * n_seqs <= INT32_MAX / MAX_CTAS;
+}
+
+// shape(part): a prompt's Shape.  Small batches: every warp forms the prefix sums over the prompts for itself, 32 bits, no barrier
+// (these steps are ahead of everything a call does: one barrier and one 64-bit division less is 0.5 us of a small call).  Others:
+// block-wide, every thread takes a run of prompts; `shared` and `warp_sums` are the block's scratch.
 template <typename ShapeFn>
-__device__ __forceinline__ void make_span(const TreeRows& rows, int min_span, Span* sp, int64_t* warp_sums, ShapeFn shape) {
+__device__ __forceinline__ Span make_span(const TreeRows& rows, int min_span, bool small, Span* shared, int64_t* warp_sums, ShapeFn shape) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  Span sp;
+  if (small) {
+    const int per = (rows.n_seqs + 31) >> 5;
+    const int b0 = min(lane * per, rows.n_seqs), b1 = min(b0 + per, rows.n_seqs);
+    SeqPart p{0, 0, 0};
+    int mine = 0;
+#pragma unroll 1
+    for (int b = b0; b < b1; ++b) {
+      p = seq_part(rows, b);
+      mine += shape_cost(shape(p));
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    const uint32_t total = __shfl_sync(0xffffffffu, incl, 31);
+    const uint32_t n = min(gridDim.x, max(total / static_cast<uint32_t>(min_span), 1u));
+    const uint32_t border = total * min(blockIdx.x + (lane & 1), n) / n;
+    const int begin = __shfl_sync(0xffffffffu, border, 0), end = __shfl_sync(0xffffffffu, border, 1);
+    int at = incl - mine, seq = b0;
+    const uint32_t owner = __ballot_sync(0xffffffffu, begin >= at && begin < at + mine);
+    if (per > 1 && (owner >> lane & 1u)) {
+#pragma unroll 1
+      for (;; ++seq) {
+        p = seq_part(rows, seq);
+        const int cost = shape_cost(shape(p));
+        if (begin < at + cost) break;
+        at += cost;
+      }
+    }
+    __syncwarp();
+    const int from = owner ? __ffs(owner) - 1 : 0;
+    sp.begin = begin; sp.end = end; sp.total = total; sp.n_ctas = n;
+    sp.seq = owner ? __shfl_sync(0xffffffffu, seq, from) : rows.n_seqs;
+    sp.seq_start = __shfl_sync(0xffffffffu, at, from);
+    sp.part.row0 = __shfl_sync(0xffffffffu, p.row0, from);
+    sp.part.n_nodes = __shfl_sync(0xffffffffu, p.n_nodes, from);
+    sp.part.ctx_len = __shfl_sync(0xffffffffu, p.ctx_len, from);
+    return sp;
+  }
   const int per = (rows.n_seqs + TREE_THREADS - 1) / TREE_THREADS;
   const int b0 = min(tid * per, rows.n_seqs), b1 = min(b0 + per, rows.n_seqs);
   int64_t mine = 0;
@@ -94,58 +159,67 @@ __device__ __forceinline__ void make_span(const TreeRows& rows, int min_span, Sp
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  int64_t before = incl - mine, total = 0;
+  int64_t at = incl - mine, total = 0;
 #pragma unroll 1
   for (int w = 0; w < TREE_THREADS / 32; ++w) {
     const int64_t x = warp_sums[w];
-    if (w < warp) before += x;
+    if (w < warp) at += x;
     total += x;
   }
   const int n = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / static_cast<uint32_t>(min_span), static_cast<int64_t>(1))));
-  // lanes 0 and 1 form the two borders: one division instead of two in the code
   const int c = min(static_cast<int>(blockIdx.x) + (lane & 1), n);
   const int64_t border = static_cast<int64_t>(static_cast<uint64_t>(total) * c / static_cast<uint32_t>(n));
-  const int64_t begin = __shfl_sync(0xffffffffu, border, 0), end = __shfl_sync(0xffffffffu, border, 1);
-  if (tid == 0) { sp->begin = begin; sp->end = end; sp->total = total; sp->n_ctas = n; sp->seq = rows.n_seqs; sp->seq_start = total; }
+  sp.begin = __shfl_sync(0xffffffffu, border, 0);
+  sp.end = __shfl_sync(0xffffffffu, border, 1);
+  sp.total = sp.seq_start = total; sp.n_ctas = n; sp.seq = rows.n_seqs; sp.part = SeqPart{0, 0, 0};
+  if (tid == 0) *shared = sp;
   __syncthreads();
-  if (mine > 0 && begin >= before && begin < before + mine) {         // one thread at most
+  if (mine > 0 && sp.begin >= at && sp.begin < at + mine) {         // one thread at most
     int b = b0;
-    int64_t at = before;
 #pragma unroll 1
-    for (; b < b1; ++b) {
-      const int cost = shape_cost(shape(seq_part(rows, b)));
-      if (begin < at + cost) break;
+    for (;; ++b) {
+      sp.part = seq_part(rows, b);
+      const int cost = shape_cost(shape(sp.part));
+      if (sp.begin < at + cost) break;
       at += cost;
     }
-    sp->seq = b;
-    sp->seq_start = at;
+    sp.seq = b;
+    sp.seq_start = at;
+    *shared = sp;
   }
   __syncthreads();
+  return *shared;
 }
 
+// Walks a span.  Cost positions count from the span's begin: 32 bits (the host refuses batches whose span might not fit).
 struct Cursor {
-  int64_t pos, end, seq_start;
+  int pos, end, seq_start;
   int seq;
-  __device__ __forceinline__ explicit Cursor(const Span& s) : pos(s.begin), end(s.end), seq_start(s.seq_start), seq(s.seq) {}
+  SeqPart part;                  // of prompt `seq`
+  __device__ __forceinline__ explicit Cursor(const Span& s)
+      : pos(0), end(static_cast<int>(s.end - s.begin)), seq_start(static_cast<int>(s.seq_start - s.begin)), seq(s.seq), part(s.part) {}
   template <typename ShapeFn>
   __device__ __forceinline__ bool next(const TreeRows& rows, ShapeFn shape, Piece* pc) {
 #pragma unroll 1
     while (pos < end && seq < rows.n_seqs) {
-      const SeqPart p = seq_part(rows, seq);
-      const Shape sh = shape(p);
+      const Shape sh = shape(part);
       const int whole = shape_cost(sh);
-      if (pos >= seq_start + whole) { seq_start += whole; ++seq; continue; }
+      if (pos - seq_start >= whole) {
+        seq_start += whole;
+        if (++seq < rows.n_seqs) part = seq_part(rows, seq);
+        continue;
+      }
       const int cost = sh.n_blk * sh.blk_cost + UNIT_COST;
-      const int unit = static_cast<int>(pos - seq_start) / cost;
-      const int64_t unit_start = seq_start + static_cast<int64_t>(unit) * cost, unit_end = unit_start + cost;
-      const int64_t stop = min(end, unit_end);
+      const int unit = (pos - seq_start) / cost;
+      const int unit_start = seq_start + unit * cost, unit_end = unit_start + cost;
+      const int stop = min(end, unit_end);
       // a unit's own cost lies ahead of its blocks: a border inside it leaves the whole unit to the later span; a border
       // inside a block leaves the block to the later span
-      const int bb = max(static_cast<int>(pos - unit_start) - UNIT_COST, 0) / sh.blk_cost;
-      const int be = max(static_cast<int>(stop - unit_start) - UNIT_COST, 0) / sh.blk_cost;
+      int bb = max(pos - unit_start - UNIT_COST, 0), be = max(stop - unit_start - UNIT_COST, 0);
+      if (sh.blk_cost > 1) { bb /= sh.blk_cost; be /= sh.blk_cost; }
       pos = stop;
       if (be <= bb) continue;
-      pc->seq = seq; pc->unit = unit; pc->part = p;
+      pc->seq = seq; pc->unit = unit; pc->part = part;
       pc->blk_begin = bb; pc->blk_end = be; pc->n_blk = sh.n_blk; pc->unit_end = unit_end;
       return true;
     }
@@ -160,8 +234,8 @@ __device__ __forceinline__ uint32_t node_bits(const TreeRows& r, int row, int no
   uint64_t w = 0;
   if (r.mask != nullptr) {
     const uint64_t* m = r.mask + static_cast<size_t>(row) * r.mask_words;
-    w = __ldg(m + (lo >> 6)) >> (lo & 63);
-    if ((lo & 63) != 0 && (lo >> 6) + 1 < r.mask_words) w |= __ldg(m + (lo >> 6) + 1) << (64 - (lo & 63));
+    w = ld_dep_u64(m + (lo >> 6)) >> (lo & 63);
+    if ((lo & 63) != 0 && (lo >> 6) + 1 < r.mask_words) w |= ld_dep_u64(m + (lo >> 6) + 1) << (64 - (lo & 63));
   } else if (node >= lo) {
     w = node - lo >= 63 ? ~0ull : (1ull << (node - lo + 1)) - 1;
   }
@@ -182,9 +256,9 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, u
 }
 // `where` of load_tile: pages behind the prompt's last slot repeat its last page (masked either way).
 __device__ __forceinline__ int tile_place(const KvView& kv, const SeqPart& p, int seq, int blk, int lane) {
-  if (!kv.page_table) return lane == 0 ? __ldg(kv.ctx_start + seq) : 0;
+  if (!kv.page_table) return lane == 0 ? ld_dep_s32(kv.ctx_start + seq) : 0;
   const int last = (p.ctx_len + max(p.n_nodes, 1) - 1) / PAGE_TOKENS;
-  return __ldg(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
+  return ld_dep_s32(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
 }
 
 // K or V rows as a 2-D map of 64-column boxes: a page's 16 rows or a block's 128
@@ -212,7 +286,7 @@ __device__ __noinline__ bool sees_a_node(const TreeRows& r, int row, int node, i
 }
 // One 64-bit word of what a node sees (bits of nodes past the prompt's last are whatever the caller wrote).
 __device__ __forceinline__ uint64_t node_word(const TreeRows& r, int row, int node, int w) {
-  if (r.mask) return __ldg(r.mask + static_cast<size_t>(row) * r.mask_words + w);
+  if (r.mask) return ld_dep_u64(r.mask + static_cast<size_t>(row) * r.mask_words + w);
   return node < 64 * w ? 0ull : node - 64 * w >= 63 ? ~0ull : (1ull << (node - 64 * w + 1)) - 1;
 }
 
