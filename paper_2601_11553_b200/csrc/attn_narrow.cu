@@ -144,6 +144,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     if (lane == 0) {
       constexpr uint32_t idesc_s = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 0, 0);
       constexpr uint32_t idesc_o = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 1, 0);       // A = V^T: V's rows are the K index
+      const TileLayout<D> tl(a.kv.page_table != nullptr);
       uint32_t n_item = 0, n_tile = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -168,21 +169,21 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           tc_fence_after_sync();
           const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
           if (sp.is_k) {
-            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, 1024);
+            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, tl.group);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              umma_ss(tmem + i * NC, k_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4),
+              umma_ss(tmem + i * NC, k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
                       q_desc + (((kk >> 2) * Q_HALF + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
             umma_commit(&s_full[i]);
             umma_commit(&empty[st]);
             if (sp.j + 1 == nb) umma_commit(&q_empty[par]);
           } else {
             // head size 64 has one 64-element column block: the second 64 TMEM lanes repeat the first (distance 0) and are not read
-            const uint64_t v_desc = make_smem_desc_sw128(tile, HALVES == 2 ? HALF_BYTES : 0, 1024);
+            const uint64_t v_desc = make_smem_desc_sw128(tile, tl.mn_lbo, tl.group);
             const uint64_t p_desc = make_smem_desc_sw128(smem_u32(p_smem + i * P_BYTES), 16, 1024);
 #pragma unroll
             for (int kk = 0; kk < BLK / 16; ++kk)
-              umma_ss(tmem + TMEM_O + (par * 2 + i) * NC, v_desc + (kk * 2048 >> 4), p_desc + (((kk >> 2) * P_HALF + (kk & 3) * 32) >> 4), idesc_o,
+              umma_ss(tmem + TMEM_O + (par * 2 + i) * NC, v_desc + (kk * 2 * tl.group >> 4), p_desc + (((kk >> 2) * P_HALF + (kk & 3) * 32) >> 4), idesc_o,
                       sp.j > 1 || kk != 0);
             umma_commit(&empty[st]);
             if (sp.j + 1 == nb) umma_commit(&o_full[par]);

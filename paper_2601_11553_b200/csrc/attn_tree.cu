@@ -99,6 +99,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         if (ok && !mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
       };
       const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
+      const TileLayout<D> tl(a.kv.page_table != nullptr);
       while (ok && next_item(cur, a, &it)) {
         const int nb = it.blk_end - it.blk_begin;
         wait(&q_full, n_item & 1u);
@@ -117,21 +118,21 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
           tc_fence_after_sync();
           const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
           if (sp.is_k) {
-            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, 1024);
+            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, tl.group);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               constexpr int H = HALF_BYTES;
-              const uint32_t off = ((kk >> 2) * H + (kk & 3) * 32) >> 4;
-              umma_ss(tmem + TMEM_S + i * BLK, q_desc + off, k_desc + off, idesc_qk, kk != 0);
+              umma_ss(tmem + TMEM_S + i * BLK, q_desc + (((kk >> 2) * H + (kk & 3) * 32) >> 4), k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
+                      idesc_qk, kk != 0);
             }
             umma_commit(&s_full[i]);
             umma_commit(&empty[st]);
             if (sp.j + 1 == nb) umma_commit(&q_empty);
           } else {
-            const uint64_t v_desc = make_smem_desc_sw128(tile, HALF_BYTES, 1024);
+            const uint64_t v_desc = make_smem_desc_sw128(tile, tl.mn_lbo, tl.group);
 #pragma unroll
             for (int kk = 0; kk < BLK / 16; ++kk)
-              umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2048 >> 4), idesc_pv, sp.j > 1 || kk != 0);
+              umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2 * tl.group >> 4), idesc_pv, sp.j > 1 || kk != 0);
             umma_commit(&empty[st]);
             if (sp.j + 1 == nb) umma_commit(&o_full);
           }

@@ -126,13 +126,14 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ++n_tile;
         if (lane == 0) mbar_arrive_expect_tx(&full[st], TILE_BYTES);
         __syncwarp();
-        load_tile<HALVES>(ring + st * TILE_BYTES, &tmK, &full[st], a.kv.page_table != nullptr, where, pc.unit * D, blk, lane);
+        load_tile<D>(ring + st * TILE_BYTES, &tmK, &full[st], a.kv.page_table != nullptr, where, pc.unit, blk, lane);
         for (int t = 0; t < tiles && tiles > 1 && ok; ++t) load_q(t);
       }
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
     if (lane == 0) {
+      const TileLayout<D> tl(a.kv.page_table != nullptr);
       uint32_t n_tile = 0, n_s[2] = {0, 0};
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (ok && !bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
@@ -145,7 +146,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           const int st = n_tile % STAGES;
           wait(&full[st], (n_tile / STAGES) & 1u);
           ++n_tile;
-          const uint32_t ka = smem_u32(ring + st * TILE_BYTES);
+          const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
           for (int t = 0; t < tiles && ok; ++t) {
             const int qs = n_q & 1;
             wait(&q_full[qs], (n_q >> 1) & 1u);
@@ -157,11 +158,11 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             tc_fence_after_sync();
             const int cols = (min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group + 15) & ~15;
             const uint32_t idesc = make_idesc_f16(BLK, cols, BF16 ? 1 : 0, 0, 0);
-            const uint32_t qa = smem_u32(q_smem + qs * Q_TILE);
+            const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_TILE), 16, 1024);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-              const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
-              umma_ss(tmem + (i * 2 + buf) * BLK, make_smem_desc_sw128(ka + off, 16, 1024), make_smem_desc_sw128(qa + off, 16, 1024), idesc, kk != 0);
+              umma_ss(tmem + (i * 2 + buf) * BLK, k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
+                      q_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0);
             }
             umma_commit(&s_full[i][buf]);
             if (tiles > 1 || blk + 1 == pc.blk_end) { umma_commit(&q_empty[qs]); ++n_q; }

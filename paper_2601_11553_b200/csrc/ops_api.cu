@@ -45,10 +45,10 @@ bool kv_ok(const percache_kv_t* kv, int32_t max_len, bool need_v) {
       (kv->head_dim != 64 && kv->head_dim != 128) || (kv->dtype != PERCACHE_BF16 && kv->dtype != PERCACHE_F16))
     return false;
   const int64_t width = static_cast<int64_t>(kv->n_kv_heads) * kv->head_dim;
-  if (!aligned(kv->k, 16) || kv->k_slot_stride < width || kv->k_slot_stride % 8 != 0 || kv->k_slot_stride > (INT64_C(1) << 36))
+  if (!aligned(kv->k, 16) || kv->k_slot_stride < width || kv->k_slot_stride % 8 != 0 || kv->k_slot_stride > (INT64_C(1) << 35))
     return false;
   if (need_v && (!aligned(kv->v, 16) || kv->v_slot_stride < width || kv->v_slot_stride % 8 != 0 ||
-                 kv->v_slot_stride > (INT64_C(1) << 36)))
+                 kv->v_slot_stride > (INT64_C(1) << 35)))
     return false;
   if (kv->page_table) {
     // whole pages only: a page that hangs over the pool's end would be read in part
@@ -67,7 +67,7 @@ bool rows_ok(const percache_rows_t* r) {
 
 bool q_ok(const percache_kv_t* kv, const void* q, int64_t stride, int32_t n_q_heads, float scale) {
   return q && aligned(q, 16) && n_q_heads > 0 && n_q_heads % kv->n_kv_heads == 0 && n_q_heads / kv->n_kv_heads <= 128 &&
-         stride >= static_cast<int64_t>(n_q_heads) * kv->head_dim && stride % 8 == 0 && stride <= (INT64_C(1) << 36) &&
+         stride >= static_cast<int64_t>(n_q_heads) * kv->head_dim && stride % 8 == 0 && stride <= (INT64_C(1) << 35) &&
          scale > 0.f && std::isfinite(scale);
 }
 

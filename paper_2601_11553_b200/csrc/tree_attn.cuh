@@ -154,7 +154,7 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
       if (lane == 0) mbar_arrive_expect_tx(bar, TILE_BYTES);
       if (lane == 1 && !clean) mbar_arrive(bar);
       __syncwarp();
-      load_tile<HALVES>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g * D, blk, lane);
+      load_tile<D>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g, blk, lane);
     }
     if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
       rec.n_parts = last_cta(span, it.unit_end) - static_cast<int>(blockIdx.x) + 1;
@@ -170,7 +170,8 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
 // the flag raised).  MASKS: they also put the nodes' masks beside a Q tile whose piece has drafted slots, and then arrive on q_full.
 template <int D, int STAGES, bool BF16, bool MASKS, bool CALLS>
 __device__ __forceinline__ void clean_role(const TreeParams& a, const Pipe& pipe, Cursor& cur, int* cta_failed) {
-  constexpr int HALVES = D / 64, HALF_BYTES = BLK * 128, TILE_BYTES = HALVES * HALF_BYTES;
+  constexpr int HALVES = D / 64, TILE_BYTES = BLK * D * 2;
+  const TileLayout<D> tl(a.kv.page_table != nullptr);
   const int tid = threadIdx.x - 320, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t n_item = 0, n_tile = 0, n_raw = 0;
   bool ok = true;
@@ -211,7 +212,7 @@ __device__ __forceinline__ void clean_role(const TreeParams& a, const Pipe& pipe
         for (int r = r0 + (tid >> 3); r < BLK; r += 8) {
 #pragma unroll
           for (int h = 0; h < HALVES; ++h) {
-            uint4* p = reinterpret_cast<uint4*>(v + h * HALF_BYTES + r * 128 + (tid & 7) * 16);
+            uint4* p = reinterpret_cast<uint4*>(v + tl.row(r, h) + (tid & 7) * 16);
             if (r >= r_end) {
               *p = make_uint4(0, 0, 0, 0);
             } else {

@@ -242,16 +242,27 @@ __device__ __forceinline__ uint32_t node_bits(const TreeRows& r, int row, int no
   if (n_nodes - lo < 64) w &= (1ull << (n_nodes - lo)) - 1;
   return static_cast<uint32_t>(w << (lo - j0));
 }
-// A 128-slot tile of K or V rows through a map of pool_map(): called by a whole warp.  With pages eight lanes per 64-column
-// half copy one page each; `where` then is the lane's page id, else the pool row of the prompt's slot 0 (lane 0).
-template <int HALVES>
-__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, bool paged, int where, int col, int blk,
+// A 128-slot tile of K or V (D columns of one KV head) in shared memory, 128-byte swizzle.  From a contiguous context: 64-column
+// halves of 128 rows, one copy each.  From pages: one copy per page, of both halves; a box of (64 columns, 8 rows, halves, 2
+// row groups) lands as [row group][half][8 rows][128 bytes], so that row groups are one stride apart over all pages.  (With one copy
+// per page and half the copies' issue was the limit: 115 clocks each, 32 a block.)
+template <int D>
+struct TileLayout {
+  int half, group, mn_lbo;               // bytes: second 64 columns; next 8 rows; column-block distance of an MN-major operand
+  __device__ __forceinline__ explicit TileLayout(bool paged)
+      : half(paged ? 1024 : BLK * 128), group(paged ? D / 64 * 1024 : 1024), mn_lbo(D == 128 ? half : 0) {}
+  __device__ __forceinline__ int row(int r, int h) const { return (r >> 3) * group + h * half + (r & 7) * 128; }
+};
+// Called by a whole warp.  With pages lanes 0-7 copy one page each; `where` then is the lane's page id, else the pool row of the
+// prompt's slot 0 (lane 0).
+template <int D>
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, bool paged, int where, int head, int blk,
                                           int lane) {
   if (paged) {
-    if (lane < 8 * HALVES)
-      tma_load_2d(dst + (lane >> 3) * (BLK * 128) + (lane & 7) * (PAGE_TOKENS * 128), tm, bar, col + (lane >> 3) * 64, where * PAGE_TOKENS);
+    if (lane < 8) tma_load_4d(dst + lane * (PAGE_TOKENS * D * 2), tm, bar, 0, 0, head * (D / 64), where * 2);
   } else if (lane == 0) {
-    for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * (BLK * 128), tm, bar, col + h * 64, where + blk * BLK);
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) tma_load_2d(dst + h * (BLK * 128), tm, bar, head * D + h * 64, where + blk * BLK);
   }
 }
 // `where` of load_tile: pages behind the prompt's last slot repeat its last page (masked either way).
@@ -261,12 +272,18 @@ __device__ __forceinline__ int tile_place(const KvView& kv, const SeqPart& p, in
   return ld_dep_s32(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
 }
 
-// K or V rows as a 2-D map of 64-column boxes: a page's 16 rows or a block's 128
+// K or V for load_tile.
 inline int pool_map(CUtensorMap* out, const void* base, const KvView& kv, int64_t stride) {
-  const uint64_t dims[2] = {static_cast<uint64_t>(kv.n_kv_heads) * kv.head_dim, static_cast<uint64_t>(kv.n_slots)};
-  const uint64_t str[1] = {static_cast<uint64_t>(stride) * 2};
-  const uint32_t box[2] = {64u, static_cast<uint32_t>(kv.page_table ? PAGE_TOKENS : BLK)};
-  return encode_f16_map(out, base, 2, dims, str, box);
+  const uint64_t row = static_cast<uint64_t>(stride) * 2, cols = static_cast<uint64_t>(kv.n_kv_heads) * kv.head_dim;
+  if (kv.page_table) {
+    const uint64_t dims[4] = {64, 8, cols / 64, static_cast<uint64_t>(kv.n_slots) / 8};
+    const uint64_t str[3] = {row, 128, 8 * row};
+    const uint32_t box[4] = {64, 8, static_cast<uint32_t>(kv.head_dim / 64), 2};
+    return encode_f16_map(out, base, 4, dims, str, box);
+  }
+  const uint64_t dims[2] = {cols, static_cast<uint64_t>(kv.n_slots)};
+  const uint32_t box[2] = {64, static_cast<uint32_t>(BLK)};
+  return encode_f16_map(out, base, 2, dims, &row, box);
 }
 
 // Rows of q as a 3-D map: one box is the query heads of a KV head for a tile of nodes.
