@@ -141,14 +141,14 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     clean_role<D, STAGES, BF16, true, true>(a, pipe, cur, &cta_failed);
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
+    {     // the whole warp walks; one lane issues
       constexpr uint32_t idesc_s = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 0, 0);
       constexpr uint32_t idesc_o = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 1, 0);       // A = V^T: V's rows are the K index
       const TileLayout<D> tl(a.kv.page_table != nullptr);
       uint32_t n_item = 0, n_tile = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
       };
       while (ok && next_item(cur, a, &it)) {
         const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
@@ -168,6 +168,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
+          if (elect_one()) {
           if (sp.is_k) {
             const uint64_t k_desc = make_smem_desc_sw128(tile, 16, tl.group);
 #pragma unroll
@@ -188,6 +189,8 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
             umma_commit(&empty[st]);
             if (sp.j + 1 == nb) umma_commit(&o_full[par]);
           }
+          }
+          __syncwarp();
         }
         ++n_item;
       }

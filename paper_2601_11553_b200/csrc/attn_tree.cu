@@ -90,13 +90,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     copy_role<D, STAGES, 1, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
    } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
+    {     // the whole warp walks; one lane issues
       constexpr uint32_t idesc_qk = make_idesc_f16(BLK, BLK, BF16 ? 1 : 0, 0, 0);
       constexpr uint32_t idesc_pv = make_idesc_f16(BLK, D, BF16 ? 1 : 0, 0, 1);
       uint32_t n_item = 0, n_tile = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
       };
       const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
       const TileLayout<D> tl(a.kv.page_table != nullptr);
@@ -117,6 +117,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
+          if (elect_one()) {
           if (sp.is_k) {
             const uint64_t k_desc = make_smem_desc_sw128(tile, 16, tl.group);
 #pragma unroll
@@ -136,6 +137,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             umma_commit(&empty[st]);
             if (sp.j + 1 == nb) umma_commit(&o_full);
           }
+          }
+          __syncwarp();
         }
         ++n_item;
       }

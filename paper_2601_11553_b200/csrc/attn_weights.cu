@@ -132,11 +132,11 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
+    {     // the whole warp walks; one lane issues
       const TileLayout<D> tl(a.kv.page_table != nullptr);
       uint32_t n_tile = 0, n_s[2] = {0, 0};
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && !bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA)) ok = false;
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
       };
       while (ok && next_piece(cur, a, &pc)) {
         const int tiles = n_tiles(a, pc.part);
@@ -159,15 +159,19 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             const int cols = (min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group + 15) & ~15;
             const uint32_t idesc = make_idesc_f16(BLK, cols, BF16 ? 1 : 0, 0, 0);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_TILE), 16, 1024);
+            if (elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
               umma_ss(tmem + (i * 2 + buf) * BLK, k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
                       q_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0);
             }
             umma_commit(&s_full[i][buf]);
-            if (tiles > 1 || blk + 1 == pc.blk_end) { umma_commit(&q_empty[qs]); ++n_q; }
+            if (tiles > 1 || blk + 1 == pc.blk_end) umma_commit(&q_empty[qs]);
+            if (t + 1 == tiles) umma_commit(&empty[st]);
+            }
+            __syncwarp();
+            if (tiles > 1 || blk + 1 == pc.blk_end) ++n_q;
           }
-          if (ok) umma_commit(&empty[st]);
         }
       }
     }
