@@ -312,7 +312,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           fence_proxy_async_smem();                        // the MMA reads P through the async proxy
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&p_full[i]);
+          if (elect_one()) mbar_arrive(&p_full[i]);
         }
       }
       // ---- the piece's end: sums and references of both parities are exchanged; parity i writes rows i, i + 2, ...
@@ -324,7 +324,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         for (int c = 0; c < NC; ++c) mine = lane == c ? -neg[c] : mine;
         if (quarter == 0 && lane < NC) fin_m[par][i][lane] = ((unset >> lane) & 1u) || nb <= i ? -INFINITY : mine;
         __syncwarp();
-        if (lane == 0) { mbar_arrive(&ml_full); mbar_arrive(&q_empty[par]); }
+        if (elect_one()) { mbar_arrive(&ml_full); mbar_arrive(&q_empty[par]); }
         ok = __all_sync(0xffffffffu, bar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR));
       }
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&o_full[par], (n_item >> 1) & 1u, a.err_word, DEV_ERR_ATTN_CORR));
@@ -393,7 +393,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&o_free[par]);
+        if (elect_one()) mbar_arrive(&o_free[par]);
       }
       ++n_item;
     }

@@ -246,7 +246,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
         }
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[i]);
+        if (elect_one()) mbar_arrive(&p_full[i]);
       }
       if (!ok) break;
       // ---- the row's end: both parities' (reference, sum) are exchanged, each warp then writes half of the columns
@@ -254,7 +254,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       ml[par][i][r][0] = m;
       ml[par][i][r][1] = l;
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ml_full);
+      if (elect_one()) mbar_arrive(&ml_full);
       ok = __all_sync(0xffffffffu, mbar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR)) ;
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full, par, a.err_word, DEV_ERR_ATTN_CORR));
       if (!ok) break;
@@ -324,7 +324,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       }
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&o_free);
+      if (elect_one()) mbar_arrive(&o_free);
       ++n_item;
     }
     if (!ok) cta_failed = 1;

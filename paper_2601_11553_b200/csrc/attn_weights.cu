@@ -110,7 +110,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
         if (!ok) return;
         ++n_q;
-        if (lane == 0) {
+        if (elect_one()) {
           mbar_arrive_expect_tx(&q_full[qs], HALVES * a.tile_nodes * a.group * 128);
           for (int h = 0; h < HALVES; ++h)
             tma_load_3d(q_smem + qs * Q_TILE + h * HALF_BYTES, &tmQ, &q_full[qs], h * 64, pc.unit * a.group, pc.part.row0 + t * a.tile_nodes);
@@ -124,7 +124,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ok = __all_sync(0xffffffffu, bar_wait(&empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
         if (!ok) break;
         ++n_tile;
-        if (lane == 0) mbar_arrive_expect_tx(&full[st], TILE_BYTES);
+        if (elect_one()) mbar_arrive_expect_tx(&full[st], TILE_BYTES);
         __syncwarp();
         load_tile<D>(ring + st * TILE_BYTES, &tmK, &full[st], a.kv.page_table != nullptr, where, pc.unit, blk, lane);
         for (int t = 0; t < tiles && tiles > 1 && ok; ++t) load_q(t);
@@ -208,7 +208,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(&q_full[qs]);
+        if (elect_one()) mbar_arrive(&q_full[qs]);
       }
     }
   } else {
@@ -276,11 +276,11 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             }
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&s_empty[i][buf]);
+            if (elect_one()) mbar_arrive(&s_empty[i][buf]);
           }
           if (tiles > 1 || blk + 1 == pc.blk_end) {
             __syncwarp();
-            if (lane == 0) mbar_arrive(&q_empty[qs]);
+            if (elect_one()) mbar_arrive(&q_empty[qs]);
             ++n_q;
           }
         }

@@ -134,7 +134,7 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
     const int nb = it.blk_end - it.blk_begin, qs = n_item % QSLOTS;
     ok = __all_sync(0xffffffffu, role_wait<CALLS>(&pipe.q_empty[qs], ((n_item / QSLOTS) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
     if (!ok) break;
-    if (lane == 0) {
+    if (elect_one()) {
       mbar_arrive_expect_tx(&pipe.q_full[qs], HALVES * a.tile_nodes * a.group * 128);
       for (int h = 0; h < HALVES; ++h)
         tma_load_3d(pipe.q_smem + qs * pipe.q_slot_bytes + h * pipe.q_half_bytes, tmQ, &pipe.q_full[qs], h * 64, it.g * a.group, it.row0);
@@ -151,8 +151,10 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
       // a tile that has to be cleaned lands on a barrier of the cleaning warps; they then complete `full` in its place
       const bool clean = !sp.is_k && (blk + 1) * BLK > it.ctx_len;
       uint64_t* bar = clean ? &pipe.raw[n_raw++ % STAGES] : &pipe.full[st];
-      if (lane == 0) mbar_arrive_expect_tx(bar, TILE_BYTES);
-      if (lane == 1 && !clean) mbar_arrive(bar);
+      if (elect_one()) {
+        mbar_arrive_expect_tx(bar, TILE_BYTES);
+        if (!clean) mbar_arrive(bar);
+      }
       __syncwarp();
       load_tile<D>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g, blk, lane);
     }
@@ -192,7 +194,7 @@ __device__ __forceinline__ void clean_role(const TreeParams& a, const Pipe& pipe
           pipe.node_mask[(qs * 32 + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + e / words, it.node0 + e / words, e % words);
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&pipe.q_full[qs]);
+      if (elect_one()) mbar_arrive(&pipe.q_full[qs]);
     }
     // the tiles' order in the ring: K0 [K1] V0 [K2] V1 ...
     uint32_t tile = n_tile + (nb > 1 ? 2 : 1);
@@ -232,7 +234,7 @@ __device__ __forceinline__ void clean_role(const TreeParams& a, const Pipe& pipe
         if (bad) *reinterpret_cast<volatile int*>(flag) = 1;
         fence_proxy_async_smem();                        // the MMA reads the tile through the async proxy
         __syncwarp();
-        if (lane == 0) mbar_arrive(&pipe.full[st]);
+        if (elect_one()) mbar_arrive(&pipe.full[st]);
       }
       tile += j + 2 < nb ? 2 : 1;
     }

@@ -254,20 +254,20 @@ struct TileLayout {
   __device__ __forceinline__ int row(int r, int h) const { return (r >> 3) * group + h * half + (r & 7) * 128; }
 };
 // Called by a whole warp.  With pages lanes 0-7 copy one page each; `where` then is the lane's page id, else the pool row of the
-// prompt's slot 0 (lane 0).
+// prompt's slot 0.
 template <int D>
 __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, bool paged, int where, int head, int blk,
                                           int lane) {
   if (paged) {
     if (lane < 8) tma_load_4d(dst + lane * (PAGE_TOKENS * D * 2), tm, bar, 0, 0, head * (D / 64), where * 2);
-  } else if (lane == 0) {
+  } else if (elect_one()) {
 #pragma unroll
     for (int h = 0; h < D / 64; ++h) tma_load_2d(dst + h * (BLK * 128), tm, bar, head * D + h * 64, where + blk * BLK);
   }
 }
 // `where` of load_tile: pages behind the prompt's last slot repeat its last page (masked either way).
 __device__ __forceinline__ int tile_place(const KvView& kv, const SeqPart& p, int seq, int blk, int lane) {
-  if (!kv.page_table) return lane == 0 ? ld_dep_s32(kv.ctx_start + seq) : 0;
+  if (!kv.page_table) return ld_dep_s32(kv.ctx_start + seq);
   const int last = (p.ctx_len + max(p.n_nodes, 1) - 1) / PAGE_TOKENS;
   return ld_dep_s32(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
 }
