@@ -10,7 +10,7 @@
 //
 // Schedule as in the attention (spans of the batch's blocks), but a block belongs to one CTA: nothing is merged.
 // One CTA per SM, 384 threads: warp 8 copies (K ring, Q ring of two tiles), warp 9 issues the MMAs, warps 10-11 put the rows'
-// lse beside each Q tile, warps 0-3 sum the even blocks and warps 4-7 the odd ones, each from two TMEM buffers in turn.
+// lse beside each Q tile (and, where a mask says which rows count, fetch those rows alone: of a drafted tree few are accepted), warps 0-3 sum the even blocks and warps 4-7 the odd ones, each from two TMEM buffers in turn.
 // One tile of rows stays in shared memory for the whole piece; of several, each is copied again for every block (L2).
 #include <algorithm>
 
@@ -31,6 +31,8 @@ struct WeightParams {
   TreeRows rows;
   int32_t n_q_heads, group, tile_nodes, small;
   float scale, decay;
+  const void* q;
+  int64_t q_stride;
   const float* lse;
   const uint8_t* use;
   const float* w_in;
@@ -39,11 +41,21 @@ struct WeightParams {
   int* err_word;
 };
 
-__device__ __forceinline__ int n_tiles(const WeightParams& a, const SeqPart& p) { return (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes; }
+// Nodes of a prompt that count (a whole warp asks).
+__device__ __forceinline__ int used_nodes(const WeightParams& a, const SeqPart& p) {
+  if (!a.use) return p.n_nodes;
+  const int lane = threadIdx.x & 31;
+  int n = 0;
+#pragma unroll 1
+  for (int i = 0; i < p.n_nodes; i += 32)
+    n += __popc(__ballot_sync(0xffffffffu, i + lane < p.n_nodes && ld_dep_u8(a.use + p.row0 + i + lane) != 0));
+  return n;
+}
+__device__ __forceinline__ int n_tiles(const WeightParams& a, int nodes) { return (nodes + a.tile_nodes - 1) / a.tile_nodes; }
 __device__ __forceinline__ Shape weight_shape(const WeightParams& a, const SeqPart& p) {
   const int len = p.ctx_len + p.n_nodes;
   if (len == 0) return Shape{0, 0, 1};
-  return Shape{a.kv.n_kv_heads, (len + BLK - 1) / BLK, max(n_tiles(a, p), 1)};
+  return Shape{a.kv.n_kv_heads, (len + BLK - 1) / BLK, max(n_tiles(a, p.n_nodes), 1)};
 }
 __device__ __forceinline__ bool next_piece(Cursor& cur, const WeightParams& a, Piece* pc) {
   return cur.next(a.rows, [&](const SeqPart& p) { return weight_shape(a, p); }, pc);
@@ -62,6 +74,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], s_full[2][2], s_empty[2][2];
   __shared__ __align__(16) float row_lse[2][BLK];          // per Q tile: the rows' lse (0 where a row does not count)
   __shared__ uint32_t row_ok[2][4];                        // which rows count
+  __shared__ uint8_t node_list[2][BLK];                    // the tile's nodes
   __shared__ uint64_t node_mask[2][BLK][MASK_WORDS];       // and, where a piece has drafted slots, what the tile's nodes see of them
   __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
@@ -103,14 +116,16 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     // ------------------------------------------------------------ copies
     uint32_t n_tile = 0;
     while (ok && next_piece(cur, a, &pc)) {
-      const int tiles = n_tiles(a, pc.part);
+      const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes);
       if (tiles == 0) continue;          // no rows: the weights only decay
       auto load_q = [&](int t) {
         const int qs = n_q & 1;
         ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
         if (!ok) return;
         ++n_q;
-        if (elect_one()) {
+        if (a.use) {                     // the lse warps fetch the rows that count
+          if (elect_one()) mbar_arrive(&q_full[qs]);
+        } else if (elect_one()) {
           mbar_arrive_expect_tx(&q_full[qs], HALVES * a.tile_nodes * a.group * 128);
           for (int h = 0; h < HALVES; ++h)
             tma_load_3d(q_smem + qs * Q_TILE + h * HALF_BYTES, &tmQ, &q_full[qs], h * 64, pc.unit * a.group, pc.part.row0 + t * a.tile_nodes);
@@ -139,7 +154,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
       };
       while (ok && next_piece(cur, a, &pc)) {
-        const int tiles = n_tiles(a, pc.part);
+        const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes);
         if (tiles == 0) continue;
         for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
           const int i = (blk - pc.blk_begin) & 1;
@@ -156,7 +171,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             if (!ok) break;
             if (i == 0) ++n_s[0]; else ++n_s[1];
             tc_fence_after_sync();
-            const int cols = (min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group + 15) & ~15;
+            const int cols = (min(a.tile_nodes, nodes - t * a.tile_nodes) * a.group + 15) & ~15;
             const uint32_t idesc = make_idesc_f16(BLK, cols, BF16 ? 1 : 0, 0, 0);
             const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_TILE), 16, 1024);
             if (elect_one()) {
@@ -179,7 +194,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     // ------------------------------------------------------------ the rows' lse
     const int tid = threadIdx.x - 320;
     while (ok && next_piece(cur, a, &pc)) {
-      const int tiles = n_tiles(a, pc.part);
+      const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes);
       const int loads = tiles == 1 ? 1 : tiles * (pc.blk_end - pc.blk_begin);
       for (int x = 0; x < loads && ok; ++x) {
         const int t = tiles == 1 ? 0 : x % tiles;
@@ -187,24 +202,49 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
         if (!ok) break;
         ++n_q;
-        const int n_rows = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group;
+        const int tile_n = min(a.tile_nodes, nodes - t * a.tile_nodes), n_rows = tile_n * a.group;
+        // the tile's nodes: those that count, in order (both warps write the same)
+        if (a.use) {
+          int before = -t * a.tile_nodes;
+#pragma unroll 1
+          for (int n0 = 0; n0 < pc.part.n_nodes; n0 += 32) {
+            const bool u = n0 + lane < pc.part.n_nodes && ld_dep_u8(a.use + pc.part.row0 + n0 + lane) != 0;
+            const uint32_t all = __ballot_sync(0xffffffffu, u);
+            const int at = before + __popc(all & ((1u << lane) - 1));
+            if (u && at >= 0 && at < tile_n) node_list[qs][at] = static_cast<uint8_t>(n0 + lane);
+            before += __popc(all);
+          }
+        } else {
+#pragma unroll 1
+          for (int e = lane; e < tile_n; e += 32) node_list[qs][e] = static_cast<uint8_t>(t * a.tile_nodes + e);
+        }
+        __syncwarp();
+        if (a.use) {                                       // their rows, in the layout a copy would give them
+          constexpr int VECS = D / 8;
+          uint8_t* dst = q_smem + qs * Q_TILE;
+#pragma unroll 4
+          for (int e = tid; e < n_rows * VECS; e += 64) {
+            const int r = e / VECS, v = e % VECS;
+            const int64_t at = static_cast<int64_t>(pc.part.row0 + node_list[qs][r / a.group]) * a.q_stride + (pc.unit * a.group + r % a.group) * D + v * 8;
+            *reinterpret_cast<uint4*>(dst + (v >> 3) * HALF_BYTES + r * 128 + (((v & 7) ^ (r & 7)) << 4)) =
+                ld_dep_v4(static_cast<const unsigned short*>(a.q) + at);
+          }
+          fence_proxy_async_smem();
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int r = k * 64 + tid;
           float z = -INFINITY;
-          if (r < n_rows) {
-            const int row = pc.part.row0 + t * a.tile_nodes + r / a.group;
-            if (!a.use || ld_dep_u8(a.use + row) != 0) z = ld_dep_f32(a.lse + static_cast<size_t>(row) * a.n_q_heads + pc.unit * a.group + r % a.group);
-          }
+          if (r < n_rows) z = ld_dep_f32(a.lse + static_cast<size_t>(pc.part.row0 + node_list[qs][r / a.group]) * a.n_q_heads + pc.unit * a.group + r % a.group);
           const uint32_t counts = __ballot_sync(0xffffffffu, z != -INFINITY);
           row_lse[qs][r] = z != -INFINITY ? z : 0.f;
           if (lane == 0) row_ok[qs][k * 2 + warp - 10] = counts;
         }
         if (pc.blk_end * BLK > pc.part.ctx_len) {
-          const int nodes = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes), words = (pc.part.n_nodes + 63) / 64;
-          for (int e = tid; e < nodes * words; e += 64) {
-            const int node = t * a.tile_nodes + e / words, w = e % words;
-            node_mask[qs][e / words][w] = node_word(a.rows, pc.part.row0 + node, node, w);
+          const int words = (pc.part.n_nodes + 63) / 64;
+          for (int e = tid; e < tile_n * words; e += 64) {
+            const int node = node_list[qs][e / words];
+            node_mask[qs][e / words][e % words] = node_word(a.rows, pc.part.row0 + node, node, e % words);
           }
         }
         __syncwarp();
@@ -218,7 +258,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     const uint32_t t_s = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + i * 2 * BLK;
     uint32_t n_s = 0;
     while (ok && next_piece(cur, a, &pc)) {
-      const int tiles = n_tiles(a, pc.part), len = pc.part.ctx_len + pc.part.n_nodes;
+      const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes), len = pc.part.ctx_len + pc.part.n_nodes;
       float* w_row = a.w_out + (static_cast<size_t>(pc.seq) * a.kv.n_kv_heads + pc.unit) * a.w_stride;
       const float* in_row = a.w_in ? a.w_in + (static_cast<size_t>(pc.seq) * a.kv.n_kv_heads + pc.unit) * a.w_stride : nullptr;
       for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
@@ -238,41 +278,49 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
             if (!ok) break;
             ++n_s;
             tc_fence_after_sync();
-            const int n_rows = min(a.tile_nodes, pc.part.n_nodes - t * a.tile_nodes) * a.group;
-#pragma unroll 1
-            for (int ch = 0; ch * 32 < n_rows; ++ch) {
-              uint32_t bits = row_ok[qs][ch];
-              if (bits == 0) continue;
-              uint32_t s[32];
-              tmem_ld_32x32(t_s + buf * BLK + ch * 32, s);
-              tmem_wait_ld();
+            const int n_rows = min(a.tile_nodes, nodes - t * a.tile_nodes) * a.group;
+            const int n_ch = (n_rows + 15) / 16;
+            // 16 columns at a time without a branch among them (a branch per four columns ran at half the speed: every group then waits
+            // out its own latencies); the next 16 are on their way from TMEM meanwhile
+            auto add = [&](const uint32_t (&s)[16], int ch) {
+              uint32_t bits = row_ok[qs][ch >> 1] >> (ch & 1) * 16;
               if (slot >= pc.part.ctx_len) {           // a drafted slot: which of the rows see it
                 const int node = slot - pc.part.ctx_len;
                 uint32_t seen = 0;
                 if (slot < len) {
                   const uint64_t* m = &node_mask[qs][0][node >> 6];
 #pragma unroll 4
-                  for (int c = 0; c < min(32, n_rows - ch * 32); ++c)
-                    seen |= static_cast<uint32_t>((m[(ch * 32 + c) / a.group * MASK_WORDS] >> (node & 63)) & 1u) << c;
+                  for (int c = 0; c < min(16, n_rows - ch * 16); ++c)
+                    seen |= static_cast<uint32_t>((m[(ch * 16 + c) / a.group * MASK_WORDS] >> (node & 63)) & 1u) << c;
                 }
-                seen &= bits;
-                bits = seen;
+                bits &= seen;
               }
               __syncwarp();
 #pragma unroll
-              for (int c = 0; c < 32; c += 4) {
-                if (((row_ok[qs][ch] >> c) & 15u) == 0) continue;
-                const float4 z = *reinterpret_cast<const float4*>(&row_lse[qs][ch * 32 + c]);
+              for (int c = 0; c < 16; c += 4) {
+                const float4 z = *reinterpret_cast<const float4*>(&row_lse[qs][ch * 16 + c]);
                 // scale * s - lse in one rounding, then to base 2
                 const float e0 = fast_exp2(fmaf(__uint_as_float(s[c]), a.scale, -z.x) * LOG2E);
                 const float e1 = fast_exp2(fmaf(__uint_as_float(s[c + 1]), a.scale, -z.y) * LOG2E);
                 const float e2 = fast_exp2(fmaf(__uint_as_float(s[c + 2]), a.scale, -z.z) * LOG2E);
                 const float e3 = fast_exp2(fmaf(__uint_as_float(s[c + 3]), a.scale, -z.w) * LOG2E);
-                sum0 += (bits >> c) & 1u ? e0 : 0.f;
-                sum1 += (bits >> (c + 1)) & 1u ? e1 : 0.f;
-                sum0 += (bits >> (c + 2)) & 1u ? e2 : 0.f;
-                sum1 += (bits >> (c + 3)) & 1u ? e3 : 0.f;
+                sum0 += bits & (1u << c) ? e0 : 0.f;
+                sum1 += bits & (2u << c) ? e1 : 0.f;
+                sum0 += bits & (4u << c) ? e2 : 0.f;
+                sum1 += bits & (8u << c) ? e3 : 0.f;
               }
+            };
+            uint32_t sa[16], sb[16];
+            tmem_ld_32x16(t_s + buf * BLK, sa);
+#pragma unroll 1
+            for (int ch = 0; ch < n_ch; ch += 2) {
+              tmem_wait_ld();
+              if (ch + 1 < n_ch) tmem_ld_32x16(t_s + buf * BLK + ch * 16 + 16, sb);
+              add(sa, ch);
+              if (ch + 1 >= n_ch) break;
+              tmem_wait_ld();
+              if (ch + 2 < n_ch) tmem_ld_32x16(t_s + buf * BLK + ch * 16 + 32, sa);
+              add(sb, ch + 1);
             }
             tc_fence_before_sync();
             __syncwarp();
@@ -325,6 +373,7 @@ int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t 
   p.n_q_heads = t.n_q_heads;
   p.group = t.n_q_heads / t.kv.n_kv_heads;
   p.tile_nodes = std::min(BLK / p.group, t.rows.max_nodes);
+  p.q = t.q; p.q_stride = t.q_stride;
   p.scale = t.scale; p.decay = t.decay; p.lse = t.lse; p.use = t.use;
   p.w_in = t.w_in; p.w_out = t.w_out; p.w_stride = t.w_stride;
   p.err_word = static_cast<int*>(t.workspace);
