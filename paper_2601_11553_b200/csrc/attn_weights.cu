@@ -132,10 +132,12 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         }
         __syncwarp();
       };
+      int next = tile_place(a.kv, pc.part, pc.seq, pc.blk_begin, lane);          // page ids are asked for a tile ahead
       if (tiles == 1) load_q(0);
       for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
         const int st = n_tile % STAGES;
-        const int where = tile_place(a.kv, pc.part, pc.seq, blk, lane);
+        const int where = next;
+        if (a.kv.page_table && blk + 1 < pc.blk_end) next = tile_place(a.kv, pc.part, pc.seq, blk + 1, lane);
         ok = __all_sync(0xffffffffu, bar_wait(&empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
         if (!ok) break;
         ++n_tile;

@@ -140,11 +140,13 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
         tma_load_3d(pipe.q_smem + qs * pipe.q_slot_bytes + h * pipe.q_half_bytes, tmQ, &pipe.q_full[qs], h * 64, it.g * a.group, it.row0);
     }
     __syncwarp();
+    const SeqPart part{it.row0, it.n_nodes, it.ctx_len};
+    int next = tile_place(a.kv, part, it.seq, it.blk_begin, lane);          // page ids are asked for a tile ahead
 #pragma unroll 1
     for (int x = 0; x < 2 * nb; ++x) {
       const Step sp = step_of(x, nb);
-      const int blk = it.blk_begin + sp.j, st = n_tile % STAGES;
-      const int where = tile_place(a.kv, SeqPart{it.row0, it.n_nodes, it.ctx_len}, it.seq, blk, lane);
+      const int blk = it.blk_begin + sp.j, st = n_tile % STAGES, where = next;
+      if (a.kv.page_table && x + 1 < 2 * nb) next = tile_place(a.kv, part, it.seq, it.blk_begin + step_of(x + 1, nb).j, lane);
       ok = __all_sync(0xffffffffu, role_wait<CALLS>(&pipe.empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
       if (!ok) break;
       ++n_tile;
