@@ -7,134 +7,151 @@ namespace pc {
 namespace {
 
 // ---------------------------------------------------------------------------------------------------- choice
-// One block per (prompt, head).  The budget-th largest key is found by radix selection (11, 11 and 10 bits from the top: a
-// histogram of the keys that share the prefix found so far, and the bin in which the budget runs out); then every warp
-// counts and writes its own stretch of slots: those above the key, and of the equal ones as many as are left, lowest
-// slot first, so the list comes out ascending.  The weights are read five times, but only the first time from beyond L1 for
-// contexts that fit there; the kernel is bound by the latency of its dependent passes, not by its bytes.
+// One block per (prompt, head).  What is always kept (the first `sink`, the last `recent`) is written outright; of the slots
+// between, the heaviest `need` are found by radix selection: a histogram of the top 11 bits of their keys and the bin in which
+// `need` runs out, then of the next 11 bits of the keys in that bin, then of the last 10.  Every warp has a stretch of slots of
+// its own, so that it can count what it keeps and then write it, in slot order, without talking to the others: all above the key
+// found, and of the equal ones as many as are left, lowest slot first.
+// Bounds: the weights are a few bytes a thread; what counts is the number of instructions per weight and pass (11 bins of 43
+// were key arithmetic before the always-kept slots were taken out and NaN and -0 were folded into two operations) and the latency of
+// the dependent passes.  Weights stay in registers when a warp's stretch is at most 32 x SEL_UNROLL slots, else every pass reads them
+// again (L1 or L2).
 constexpr int SEL_BITS = 11, SEL_BINS = 1 << SEL_BITS;
 constexpr int SEL_UNROLL = 8;
 
-// Order-preserving map of a weight to 32 bits (NaN as -infinity, -0 as 0); slots that are always kept come first.
-__device__ __forceinline__ uint32_t weight_key(float w, int slot, int len, int sink, int recent) {
-  if (slot < sink || slot >= len - recent) return 0xffffffffu;
-  if (isnan(w)) w = -INFINITY;
-  const uint32_t u = __float_as_uint(w + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+// Order-preserving map of a weight to 32 bits: NaN as -infinity (maximum drops it), -0 as 0 (adding 0 does).
+__device__ __forceinline__ uint32_t weight_key(float w) {
+  const uint32_t u = __float_as_uint(fmaxf(w, -INFINITY) + 0.f);
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS)
-select_slots_kernel(const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ length, int n_heads,
-                    int max_len, int budget, int sink, int recent, int32_t* __restrict__ keep, int32_t* __restrict__ count) {
-  constexpr int WARPS = THREADS / 32;
+struct SelectShared {
+  int hist[SEL_BINS];
+  int warp_sum[THREADS / 32], warp_gt[THREADS / 32], warp_eq[THREADS / 32];
+  int bin, need;
+};
+
+// lo .. hi - 1: this warp's stretch; n: slots in the middle, counted from `first`; out: where the middle's list starts.
+template <int THREADS, bool IN_REGS>
+__device__ __forceinline__ void select_middle(SelectShared<THREADS>& sh, const float* w, int first, int lo, int hi, int need, int32_t* out) {
   constexpr int BINS_EACH = SEL_BINS / THREADS;
   static_assert(SEL_BINS % THREADS == 0, "");
-  __shared__ int hist[SEL_BINS];
-  __shared__ int warp_sum[WARPS], warp_gt[WARPS], warp_eq[WARPS];
-  __shared__ int sh_bin, sh_need;
-  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int len = min(max(__ldg(length + b), 0), max_len);
-  const float* w = weights + (static_cast<size_t>(b) * n_heads + h) * w_stride;
-  int32_t* out = keep + (static_cast<size_t>(b) * n_heads + h) * budget;
-  if (h == 0 && tid == 0) count[b] = min(len, budget);
-  if (len <= budget) {
-    for (int j = tid; j < budget; j += THREADS) out[j] = j < len ? j : -1;
-    return;
-  }
-  uint32_t prefix = 0;                     // the key's bits found so far, and which bits those are
-  uint32_t known = 0;
-  int need = budget;                       // how many of the keys that share the prefix are kept
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint32_t key[SEL_UNROLL];
+  auto fetch = [&](int s0) {
+    float x[SEL_UNROLL];
+#pragma unroll
+    for (int u = 0; u < SEL_UNROLL; ++u) x[u] = s0 + u * 32 < hi ? __ldg(w + s0 + u * 32) : 0.f;
+#pragma unroll
+    for (int u = 0; u < SEL_UNROLL; ++u) key[u] = weight_key(x[u]);
+  };
+  // fn(slot, key, inside) for every slot of the stretch, 32 consecutive ones a step
+  auto each = [&](auto fn) {
+    if constexpr (IN_REGS) {
+#pragma unroll
+      for (int u = 0; u < SEL_UNROLL; ++u) fn(lo + lane + u * 32, key[u], lo + lane + u * 32 < hi);
+    } else {
+#pragma unroll 1
+      for (int s0 = lo + lane; s0 - lane < hi; s0 += 32 * SEL_UNROLL) {
+        fetch(s0);
+#pragma unroll
+        for (int u = 0; u < SEL_UNROLL; ++u) fn(s0 + u * 32, key[u], s0 + u * 32 < hi);
+      }
+    }
+  };
+  if constexpr (IN_REGS) fetch(lo + lane);
+  uint32_t prefix = 0, known = 0;          // the key's bits found so far, and which bits those are
+#pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digit = pass == 2 ? 1023u : 2047u;
-    for (int i = tid; i < SEL_BINS; i += THREADS) hist[i] = 0;
+    for (int i = tid; i < SEL_BINS; i += THREADS) sh.hist[i] = 0;
     __syncthreads();
-    for (int s0 = tid; s0 < len; s0 += THREADS * SEL_UNROLL) {
-      float x[SEL_UNROLL];
-#pragma unroll
-      for (int u = 0; u < SEL_UNROLL; ++u) x[u] = s0 + u * THREADS < len ? __ldg(w + s0 + u * THREADS) : 0.f;
-#pragma unroll
-      for (int u = 0; u < SEL_UNROLL; ++u) {
-        const int s = s0 + u * THREADS;
-        const uint32_t k = weight_key(x[u], s, len, sink, recent);
-        if (s < len && (k & known) == prefix) atomicAdd(&hist[(k >> shift) & digit], 1);
-      }
-    }
+    each([&](int, uint32_t k, bool inside) {
+      if (inside && (k & known) == prefix) atomicAdd(&sh.hist[(k >> shift) & digit], 1);
+    });
     __syncthreads();
-    // thread t has the bins from the top: BINS - 1 - t * BINS_EACH downwards; the one where the running count reaches `need`
+    // thread t has the bins SEL_BINS - 1 - t * BINS_EACH downwards: which of them is it in which the running count reaches `need`
     int c[BINS_EACH], mine = 0;
 #pragma unroll
-    for (int i = 0; i < BINS_EACH; ++i) { c[i] = hist[SEL_BINS - 1 - tid * BINS_EACH - i]; mine += c[i]; }
+    for (int i = 0; i < BINS_EACH; ++i) { c[i] = sh.hist[SEL_BINS - 1 - tid * BINS_EACH - i]; mine += c[i]; }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += x;
     }
-    if (lane == 31) warp_sum[warp] = incl;
+    if (lane == 31) sh.warp_sum[warp] = incl;
     __syncthreads();
-    int before = incl - mine;
-    for (int i = 0; i < warp; ++i) before += warp_sum[i];
+    int others = lane < warp ? sh.warp_sum[lane] : 0;       // at most 32 warps
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
+    int before = others + incl - mine;
     if (before < need && before + mine >= need) {
 #pragma unroll
       for (int i = 0; i < BINS_EACH; ++i) {
-        if (before < need && before + c[i] >= need) { sh_bin = SEL_BINS - 1 - tid * BINS_EACH - i; sh_need = need - before; }
+        if (before < need && before + c[i] >= need) { sh.bin = SEL_BINS - 1 - tid * BINS_EACH - i; sh.need = need - before; }
         before += c[i];
       }
     }
     __syncthreads();
-    prefix |= static_cast<uint32_t>(sh_bin) << shift;
+    prefix |= static_cast<uint32_t>(sh.bin) << shift;
     known |= digit << shift;
-    need = sh_need;
+    need = sh.need;
   }
-  // every warp its own stretch
-  const int each = (len + WARPS - 1) / WARPS;
-  const int lo = min(warp * each, len), hi = min(lo + each, len);
   int gt = 0, eq = 0;
-  for (int s0 = lo + lane; s0 < hi; s0 += 32 * SEL_UNROLL) {
-#pragma unroll
-    for (int u = 0; u < SEL_UNROLL; ++u) {
-      const int s = s0 + u * 32;
-      if (s < hi) {
-        const uint32_t k = weight_key(__ldg(w + s), s, len, sink, recent);
-        gt += k > prefix;
-        eq += k == prefix;
-      }
-    }
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    gt += __shfl_xor_sync(0xffffffffu, gt, o);
-    eq += __shfl_xor_sync(0xffffffffu, eq, o);
-  }
-  if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
+  each([&](int, uint32_t k, bool inside) {
+    gt += inside && k > prefix;
+    eq += inside && k == prefix;
+  });
+  gt = __reduce_add_sync(0xffffffffu, gt);
+  eq = __reduce_add_sync(0xffffffffu, eq);
+  if (lane == 0) { sh.warp_gt[warp] = gt; sh.warp_eq[warp] = eq; }
   __syncthreads();
-  int gt_before = 0, eq_before = 0;
-  for (int i = 0; i < warp; ++i) { gt_before += warp_gt[i]; eq_before += warp_eq[i]; }
+  int gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_gt[lane] : 0);
+  int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_eq[lane] : 0);
   const uint32_t below = (1u << lane) - 1;
-  for (int s0 = lo; s0 < hi; s0 += 32 * SEL_UNROLL) {
-    float x[SEL_UNROLL];
-#pragma unroll
-    for (int u = 0; u < SEL_UNROLL; ++u) x[u] = s0 + u * 32 + lane < hi ? __ldg(w + s0 + u * 32 + lane) : 0.f;
-#pragma unroll
-    for (int u = 0; u < SEL_UNROLL; ++u) {
-      const int s = s0 + u * 32 + lane;
-      const uint32_t k = weight_key(x[u], s, len, sink, recent);
-      const bool is_gt = s < hi && k > prefix, is_eq = s < hi && k == prefix;
-      const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
-      const int e = eq_before + __popc(be & below);
-      if (is_gt || (is_eq && e < need)) out[gt_before + __popc(bg & below) + min(e, need)] = s;
-      gt_before += __popc(bg);
-      eq_before += __popc(be);
-    }
+  each([&](int s, uint32_t k, bool inside) {
+    const bool is_gt = inside && k > prefix, is_eq = inside && k == prefix;
+    const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
+    const int e = eq_before + __popc(be & below);
+    if (is_gt || (is_eq && e < need)) out[gt_before + __popc(bg & below) + min(e, need)] = first + s;
+    gt_before += __popc(bg);
+    eq_before += __popc(be);
+  });
+}
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
+select_slots_kernel(const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ length, int n_heads,
+                    int max_len, int budget, int sink, int recent, int32_t* __restrict__ keep, int32_t* __restrict__ count) {
+  __shared__ SelectShared<THREADS> sh;
+  const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, warp = tid >> 5;
+  const int len = min(max(__ldg(length + b), 0), max_len);
+  int32_t* out = keep + (static_cast<size_t>(b) * n_heads + h) * budget;
+  if (h == 0 && tid == 0) count[b] = min(len, budget);
+  if (len <= budget) {
+    for (int j = tid; j < budget; j += THREADS) out[j] = j < len ? j : -1;
+    return;
   }
+  for (int j = tid; j < sink + recent; j += THREADS) {
+    if (j < sink) out[j] = j;
+    else out[budget - recent + j - sink] = len - recent + j - sink;
+  }
+  const int need = budget - sink - recent, n = len - sink - recent;       // 0 <= need < n
+  if (need == 0) return;
+  const float* w = weights + (static_cast<size_t>(b) * n_heads + h) * w_stride + sink;
+  const int stretch = (n + THREADS - 1) / THREADS * 32;                    // whole steps of 32 for each warp
+  const int lo = min(warp * stretch, n), hi = min(lo + stretch, n);
+  if (stretch <= 32 * SEL_UNROLL) select_middle<THREADS, true>(sh, w, sink, lo, hi, need, out + sink);
+  else select_middle<THREADS, false>(sh, w, sink, lo, hi, need, out + sink);
 }
 
 // ---------------------------------------------------------------------------------------------------- moving
 constexpr int MOVE_THREADS = 256;
 
-struct Move { int64_t src, dst; };       // pool rows, or dst = -1: nothing moves
+struct Move { int32_t src, dst; };       // pool rows, or dst = -1: nothing moves
 __device__ __forceinline__ Move move_of(const CompactSlots& a, int b, int j, int n, int first, const int32_t* keep) {
   Move m{0, -1};
   if (j >= n) return m;
@@ -146,8 +163,8 @@ __device__ __forceinline__ Move move_of(const CompactSlots& a, int b, int j, int
   const int64_t src = slot_row(a.kv.page_table, a.kv.pt_stride, a.kv.ctx_start, a.kv.n_slots, b, s);
   const int64_t dst = slot_row(pt, stride, a.dst_start ? a.dst_start : a.kv.ctx_start, a.kv.n_slots, b, t);
   if (src < 0 || dst < 0) return m;
-  m.src = src;
-  m.dst = dst;
+  m.src = static_cast<int32_t>(src);        // pools have at most 2^31 - 1 rows
+  m.dst = static_cast<int32_t>(dst);
   return m;
 }
 
