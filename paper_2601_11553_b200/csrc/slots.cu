@@ -18,6 +18,7 @@ namespace {
 // again (L1 or L2).
 constexpr int SEL_BITS = 11, SEL_BINS = 1 << SEL_BITS;
 constexpr int SEL_UNROLL = 8;
+constexpr int LONG_LIST = 16384;
 
 // Order-preserving map of a weight to 32 bits: NaN as -infinity (maximum drops it), -0 as 0 (adding 0 does).
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -171,9 +172,9 @@ __device__ __forceinline__ Move move_of(const CompactSlots& a, int b, int j, int
 // To another place: nothing that is read is written, so every (prompt, KV head, stretch of the list) is a block of its own.
 // 16 lanes (8 for head size 64) take a row of K and of V; a thread has MOVE_ROWS rows of both in flight.  Bound by HBM:
 // 2 x 4 D bytes a kept slot and head.
-constexpr int MOVE_ROWS = 4;
+constexpr int MOVE_ROWS = 2;
 template <int D>
-__global__ void __launch_bounds__(MOVE_THREADS) copy_slots_kernel(CompactSlots a) {
+__global__ void __launch_bounds__(MOVE_THREADS, 6) copy_slots_kernel(CompactSlots a) {
   constexpr int VECS = D / 8, ROWS = MOVE_THREADS / VECS;
   const int b = blockIdx.z, g = blockIdx.y;
   const int n = min(min(max(__ldg(a.count + b), 0), a.budget), a.max_len);
@@ -266,8 +267,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots 
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
                         int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s) {
   const dim3 grid(n_heads, n_seqs);
-  // as many threads to a list as the batch leaves room for: with one list per SM or fewer the passes' latency is all there is
-  if (static_cast<int64_t>(n_seqs) * n_heads <= n_sms)
+  // 1024 threads to a list where there is one per SM or fewer, or where lists are long: the passes' latency is all there is
+  if (static_cast<int64_t>(n_seqs) * n_heads <= n_sms || max_len > LONG_LIST)
     select_slots_kernel<1024><<<grid, 1024, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
   else
     select_slots_kernel<512><<<grid, 512, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
