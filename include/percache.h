@@ -83,6 +83,8 @@ extern "C" {
 #define PERCACHE_FLAG_GATHER_FREE       128u  /* take the gather-free form of percache_prefill whenever it is possible
                                                 (see percache_prefill), not only when the cached part dominates   */
 #define PERCACHE_FLAG_ALWAYS_GATHER     256u  /* never take it: always assemble the contiguous context              */
+#define PERCACHE_FLAG_TRACK_WEIGHTS     512u  /* decode steps add their attention weights to running sums per layer, KV head
+                                                and context slot (see percache_evict_context)                     */
 #define PERCACHE_FLAG_PAPER_MODE         64u  /* creation only: the handle works exactly as the paper states the scheme
                                                 (see "Paper-faithful mode" below)                                 */
 
@@ -224,6 +226,41 @@ PERCACHE_API int percache_get_chunk_q(percache_t* h, uint64_t chunk_id, void* q_
  * Any later percache_prefill starts a new batch and discards the decoded tokens.  Synchronous. */
 PERCACHE_API int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_t hidden_on_device,
                     float* out_hidden, int32_t out_on_device);
+
+/* A decode step over drafted tokens: prompt b gets n_nodes[b] of them at once (0 .. PERCACHE_MAX_TREE_NODES, not all
+ * zero) as a tree.  parents [sum n_nodes], prompt after prompt: parents[i] < i is the index, inside its prompt, of the
+ * token that node i follows, -1 for one that follows the prompt's last token (so a chain is -1, 0, 1, ...).  hidden:
+ * bf16 [sum n_nodes][d_model]; out_hidden: fp32 [sum n_nodes][d_model].  Node i is at the position of its depth behind
+ * the prompt's tokens so far and attends to the prompt's context, its ancestors and itself, exactly as if the path to it
+ * had been decoded token by token.  The nodes' K and V lie behind the context, one slot each (the decode reserve has to
+ * hold them: PERCACHE_E_CAPACITY), until percache_accept keeps a path of them; any other decode or prefill call drops
+ * them.  Synchronous; same errors as percache_decode.  After a gather-free prefill the first such call assembles the
+ * context, whatever the flags. */
+PERCACHE_API int percache_decode_tree(percache_t* h, int32_t n_prompts, const int32_t* n_nodes, const int32_t* parents,
+                                      const void* hidden, int32_t hidden_on_device, float* out_hidden,
+                                      int32_t out_on_device);
+
+/* Keep a path of the last percache_decode_tree call's nodes: for prompt b n_accept[b] of them (0 .. n_nodes[b]),
+ * nodes [sum n_accept] prompt after prompt, each prompt's first with parent -1 and every other the child of the one
+ * before (PERCACHE_E_INVAL otherwise, and nothing changes).  Their K and V become the prompt's next context slots, the
+ * other nodes are dropped.  With PERCACHE_FLAG_TRACK_WEIGHTS set in that call, every prompt's running weights decay once and
+ * the accepted nodes' attention weights are added.  Synchronous. */
+PERCACHE_API int percache_accept(percache_t* h, int32_t n_prompts, const int32_t* n_accept, const int32_t* nodes);
+
+/* Cut every prompt's context to at most `budget` slots per layer and KV head: the first `sink`, the last `recent`
+ * (sink + recent <= budget) and the ones with the most running attention weight, equal weights going to the lower slot.
+ * The weights are those that percache_decode and percache_accept have added while PERCACHE_FLAG_TRACK_WEIGHTS was set,
+ * since the prefill (every step first multiplies the sums by the decay of percache_set_weight_decay, 1 at creation);
+ * without any such step PERCACHE_E_INVAL.  Positions are not touched: later tokens continue at theirs, and the freed
+ * slots are free for them (they count towards the decode reserve).  percache_debug_read_ctx and read_weights then see
+ * the slots that are left.  Synchronous. */
+PERCACHE_API int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t recent);
+PERCACHE_API int percache_set_weight_decay(percache_t* h, float decay);
+
+/* Running weights of one prompt and layer: fp32 [n_kv_heads][slots of the prompt's context], copied to a host buffer of
+ * capacity_floats floats (PERCACHE_E_CAPACITY if short).  Returns the number of slots, or a negative code. */
+PERCACHE_API int64_t percache_debug_read_weights(percache_t* h, int32_t prompt, int32_t layer, float* out,
+                                                 int64_t capacity_floats);
 
 /* Context slots kept free behind every prompt of later percache_prefill calls, so that percache_decode can
  * append tokens (default 0: no decode).  A batch needs sum(n_total) + n_prompts * tokens_per_prompt <=

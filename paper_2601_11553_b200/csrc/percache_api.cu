@@ -3,6 +3,7 @@
 // launches on the caller's stream, commit of missed chunks after success.
 #include <algorithm>
 #include <chrono>
+#include <cmath>
 #include <functional>
 #include <cstring>
 #include <new>
@@ -37,6 +38,12 @@ struct Plan {   // integer description of the last successful call (host)
   std::vector<int32_t> cu_ctx, cu_new, slot_chunk, slot_offset, slot_is_new, row_slot;
   std::vector<int32_t> ctx0;      // device context slot of every prompt's slot 0 (prompts are decode_reserve apart)
   std::vector<int32_t> dec_len;   // tokens appended to every prompt by percache_decode since the prefill
+  std::vector<int32_t> evicted;   // context slots percache_evict_context has taken out of every prompt (empty: none)
+  int32_t reserve = 0;            // decode_reserve as it was at the prefill: what lies between the prompts
+  std::vector<int32_t> tree_n, tree_parent;      // nodes of the last percache_decode_tree call, while they may be accepted
+  bool tree_tracked = false;      // that call kept its queries for percache_accept
+  bool weights_on = false;        // running attention weights of this batch exist
+  int32_t weights_stride = 0;
   bool ctx_assembled = true;      // false after a gather-free call: there is no contiguous context to read or extend
   // gather-free call with a decode reserve: the prompts' page tables (8-entry padded) and where each starts, kept so
   // that the first decode step can assemble the context after all
@@ -101,6 +108,15 @@ struct percache {
   float* capture_host = nullptr;   // debugging aid: layer inputs of the next calls are copied here (see header)
   int64_t capture_capacity = 0;    // floats
   int32_t decode_reserve = 0;     // context slots kept free behind every prompt for percache_decode
+  // steps over drafted tokens and tracked steps (allocated when the first one runs)
+  void* tree_ws = nullptr;         // workspace of the tree attention; its first word is an error word
+  int32_t* tree_ints = nullptr;    // lengths, row starts, masks ... of a step
+  float* weights = nullptr;        // running attention weights [L][prompts][n_kv_heads][stride]
+  __half* q_hist = nullptr;        // queries of a tracked tree step [L][rows][q_dim]
+  float* lse_hist = nullptr;       // their log-sum-exps [L][rows][n_q_heads]
+  int32_t* keep = nullptr;         // kept slots of one layer
+  size_t tree_ints_cap = 0, weights_cap = 0, q_hist_cap = 0, lse_hist_cap = 0, keep_cap = 0;
+  float weight_decay = 1.0f;
   percache_stats_t stats{};
   std::vector<cudaEvent_t> events;
   cudaEvent_t ev_begin = nullptr, ev_end = nullptr;
@@ -122,6 +138,21 @@ bool dev_alloc(percache* h, T** out, size_t count) {
   }
   h->dev_allocs.push_back(p);
   *out = static_cast<T*>(p);
+  return true;
+}
+
+// Makes *p hold at least `count` elements (contents are lost when it grows).
+template <typename T>
+bool dev_grow(percache* h, T** p, size_t* cap, size_t count) {
+  if (*cap >= count) return true;
+  if (*p) {
+    h->dev_allocs.erase(std::find(h->dev_allocs.begin(), h->dev_allocs.end(), static_cast<void*>(*p)));
+    cudaFree(*p);
+    *p = nullptr;
+    *cap = 0;
+  }
+  if (!dev_alloc(h, p, count)) return false;
+  *cap = count;
   return true;
 }
 
@@ -310,13 +341,25 @@ DevIndex dev_index(const percache* h) {
   return ix;
 }
 
+// A step whose attention is the tree attention (drafted tokens; tracked steps; steps after an eviction): the arguments that are the
+// same for every layer, and what the running weights need.
+struct TreeStep {
+  TreeAttention attn;              // k, v, q, out, lse are the layer's
+  float* lse = nullptr;            // [L][rows][n_q_heads], or NULL
+  __half* q_hist = nullptr;        // where the queries go for percache_accept, or NULL
+  float* weights = nullptr;        // add the rows' weights at once (plain tokens), or NULL
+  size_t weights_layer = 0;        // elements from layer to layer
+  int64_t weights_stride = 0;
+  float decay = 1.f;
+};
+
 // Every decoder block for the Mi rows in h->resid (prefill: the new rows of the batch; decode: one row per
 // prompt): RMSNorm, QKV projection (rotation, pages, context), attention over the assembled context, output
 // projection, RMSNorm, SwiGLU FFN.  Layer l's attention first waits for ev_gather[l] when the fetch runs beside.
 // n_decode_items > 0: the attention work is a decode step's list of DecodeAttnItem / DecodeAttnMerge records.
 bool run_layers(percache* h, int Mi, const DevIndex& ix, int n_attn_ctas, int n_merges, bool overlap_gather,
                 bool use_ref, PhaseTimer& timer, cudaStream_t s, int n_decode_items = 0,
-                const int32_t* gather_free_page_table = nullptr) {
+                const int32_t* gather_free_page_table = nullptr, const TreeStep* tree = nullptr) {
   const ModelDims& D = h->dims;
   const int d = D.d_model;
   const size_t pool_layer = static_cast<size_t>(h->cfg.pool_pages) * PAGE_TOKENS * D.kv_dim;
@@ -378,7 +421,26 @@ bool run_layers(percache* h, int Mi, const DevIndex& ix, int n_attn_ctas, int n_
 
     timer.begin(PERCACHE_PH_ATTN);
     if (overlap_gather) ok = ok && cudaStreamWaitEvent(s, h->ev_gather[l], 0) == cudaSuccess;
-    if (use_ref || (h->flags & PERCACHE_FLAG_REFERENCE_ATTENTION)) {
+    if (tree) {
+      TreeAttention a = tree->attn;
+      a.kv.k = qe.kctx; a.kv.v = qe.vctx;
+      a.q = h->qbuf; a.out = h->attn_out;
+      a.lse = tree->lse ? tree->lse + static_cast<size_t>(l) * Mi * D.n_q_heads : nullptr;
+      ok = ok && launch_tree_attention(a, h->n_sms, s) == 0;
+      if (tree->q_hist)
+        ok = ok && cudaMemcpyAsync(tree->q_hist + static_cast<size_t>(l) * Mi * D.q_dim, h->qbuf, static_cast<size_t>(Mi) * D.q_dim * 2,
+                                   cudaMemcpyDeviceToDevice, s) == cudaSuccess;
+      if (tree->weights) {
+        AttentionWeights w{};
+        w.kv = a.kv; w.rows = a.rows; w.q = a.q; w.q_stride = a.q_stride; w.n_q_heads = a.n_q_heads; w.scale = a.scale; w.lse = a.lse;
+        w.decay = tree->decay;
+        w.w_out = tree->weights + l * tree->weights_layer;
+        w.w_in = tree->decay != 0.f ? w.w_out : nullptr;
+        w.w_stride = tree->weights_stride;
+        w.workspace = a.workspace;
+        ok = ok && launch_attention_weights(w, h->n_sms, s) == 0;
+      }
+    } else if (use_ref || (h->flags & PERCACHE_FLAG_REFERENCE_ATTENTION)) {
       launch_ref_attention(h->qbuf, qe.kctx, qe.vctx, h->attn_out, d_row_pos, d_row_ctx0, Mi, D.n_q_heads, D.n_kv_heads, s);
     } else if (n_decode_items > 0) {
       ok = ok && launch_decode_attention(reinterpret_cast<const DecodeAttnItem*>(d_attn_items), n_decode_items,
@@ -463,6 +525,213 @@ bool run_layers(percache* h, int Mi, const DevIndex& ix, int n_attn_ctas, int n_
   return ok;
 }
 
+
+// First decode step after a gather-free prefill: every slot of every prompt still sits in a page (cached chunks in theirs, the
+// rows that prefill computed, and tokens decoded from the pages since, in the pages lent to them), so the fetch that prefill
+// skipped runs now, over all slots, and builds the contiguous context the decode kernels read and append to.  `items` is the
+// host side of the gather items.
+bool assemble_late(percache* h, GatherItem* items, PhaseTimer& timer, cudaStream_t s) {
+  const Plan& plan = h->plan;
+  int n_items = 0;
+  for (size_t b = 0; b + 1 < plan.cu_ctx.size(); ++b) {
+    const int32_t T = plan.cu_ctx[b + 1] - plan.cu_ctx[b] + plan.dec_len[b];
+    for (int32_t o = 0; o < T; o += PAGE_TOKENS) {
+      GatherItem& g = items[n_items++];
+      g.dst_slot = plan.ctx0[b] + o;
+      g.src_page = plan.page_table[static_cast<size_t>(plan.pt0[b] + o / PAGE_TOKENS)];
+      g.n_tok = std::min<int32_t>(PAGE_TOKENS, T - o);
+      g.pos = o;
+    }
+  }
+  const bool ok = cudaMemcpyAsync(reinterpret_cast<int32_t*>(const_cast<GatherItem*>(dev_index(h).items)), items,
+                                  static_cast<size_t>(n_items) * sizeof(GatherItem), cudaMemcpyHostToDevice, s) == cudaSuccess;
+  timer.begin(PERCACHE_PH_GATHER);
+  launch_gather_rerope(dev_index(h).items, n_items, h->dims.n_layers, h->kpool, h->vpool, h->cfg.pool_pages, h->kctx, h->vctx,
+                       h->ctx_cap, h->dims.kv_dim, h->rope, s);
+  timer.end();
+  return ok;
+}
+// The context exists now: the pages lent to the batch go back.
+void assembled(percache* h) {
+  h->plan.ctx_assembled = true;
+  h->plan.page_table.clear();
+  h->plan.pt0.clear();
+  release_pages(h, h->retained_scratch);
+  h->retained_scratch.clear();
+  refresh_page_stats(h);
+}
+
+int32_t evicted_of(const Plan& p, int b) { return p.evicted.empty() ? 0 : p.evicted[b]; }
+int32_t ctx_slots(const Plan& p, int b) { return p.cu_ctx[b + 1] - p.cu_ctx[b] + p.dec_len[b] - evicted_of(p, b); }
+
+KvView ctx_view(const percache* h, int layer, const int32_t* d_ctx_start) {
+  const size_t off = static_cast<size_t>(layer) * h->ctx_cap * h->dims.kv_dim;
+  KvView v{};
+  v.k = h->kctx + off; v.v = h->vctx + off;
+  v.k_stride = v.v_stride = h->dims.kv_dim;
+  v.n_slots = h->ctx_cap;
+  v.ctx_start = d_ctx_start;
+  v.n_kv_heads = h->dims.n_kv_heads; v.head_dim = HEAD_DIM; v.bf16 = 0;
+  return v;
+}
+
+// One decode step through the tree attention.  n_nodes NULL: one token a prompt, which joins the context at once.
+int decode_rows(percache* h, int32_t n_prompts, const int32_t* n_nodes, const int32_t* parents, const void* hidden,
+                int32_t hidden_on_device, float* out_hidden, int32_t out_on_device) try {
+  const auto t_host0 = std::chrono::steady_clock::now();
+  Plan& plan = h->plan;
+  const ModelDims& D = h->dims;
+  const int d = D.d_model, L = D.n_layers;
+  const bool track = (h->flags & PERCACHE_FLAG_TRACK_WEIGHTS) != 0;
+  // ---- sizes and checks
+  int64_t rows = 0;
+  int32_t max_n = 1, max_len = 1;
+  for (int b = 0; b < n_prompts; ++b) {
+    const int32_t n = n_nodes ? n_nodes[b] : 1;
+    if (n < 0 || n > PERCACHE_MAX_TREE_NODES) return PERCACHE_E_INVAL;
+    if (plan.dec_len[b] - evicted_of(plan, b) + n > plan.reserve) return PERCACHE_E_CAPACITY;
+    rows += n;
+    max_n = std::max(max_n, n);
+    max_len = std::max(max_len, ctx_slots(plan, b) + n);
+  }
+  if (rows == 0) return PERCACHE_E_INVAL;
+  if (rows > h->m_cap) return PERCACHE_E_CAPACITY;
+  const int M = static_cast<int>(rows), words = (max_n + 63) / 64;
+  std::vector<uint64_t> mask(static_cast<size_t>(M) * words, 0);
+  // lengths [n], row starts [n + 1], context starts [n], padding to 8 bytes, masks
+  const size_t head = (3 * static_cast<size_t>(n_prompts) + 2) & ~size_t(1);
+  std::vector<int32_t> ints(head + 2 * mask.size());
+  int32_t *row_slot = h->h_index, *row_pos = row_slot + h->m_cap, *row_pool = row_pos + h->m_cap, *row_ctx0 = row_pool + h->m_cap;
+  std::vector<int32_t> depth(max_n);
+  int64_t visible_pairs = 0;
+  int32_t r = 0;
+  for (int b = 0; b < n_prompts; ++b) {
+    const int32_t n = n_nodes ? n_nodes[b] : 1, T = plan.cu_ctx[b + 1] - plan.cu_ctx[b] + plan.dec_len[b], used = ctx_slots(plan, b);
+    ints[b] = used;
+    ints[n_prompts + b] = r;
+    ints[2 * n_prompts + 1 + b] = plan.ctx0[b];
+    for (int32_t i = 0; i < n; ++i) {
+      const int32_t p = n_nodes ? parents[r + i] : -1;
+      if (p < -1 || p >= i) return PERCACHE_E_INVAL;
+      depth[i] = p < 0 ? 0 : depth[p] + 1;
+      if (T + depth[i] + 1 > h->cfg.max_prompt_tokens) return PERCACHE_E_CAPACITY;
+      uint64_t* m = &mask[static_cast<size_t>(r + i) * words];
+      if (p >= 0) std::copy(m - static_cast<size_t>(i - p) * words, m - static_cast<size_t>(i - p) * words + words, m);
+      m[i >> 6] |= 1ull << (i & 63);
+      row_slot[r + i] = plan.ctx0[b] + used + i;
+      row_pos[r + i] = T + depth[i];
+      row_pool[r + i] = -1;
+      row_ctx0[r + i] = plan.ctx0[b];
+      visible_pairs += used + depth[i] + 1;
+    }
+    r += n;
+  }
+  ints[2 * static_cast<size_t>(n_prompts)] = r;
+  std::memcpy(ints.data() + head, mask.data(), mask.size() * sizeof(uint64_t));
+  // ---- memory
+  if (!h->tree_ws) {
+    char* ws = nullptr;
+    if (!dev_alloc(h, &ws, PERCACHE_OPS_WORKSPACE_BYTES)) return PERCACHE_E_NOMEM;
+    h->tree_ws = ws;
+  }
+  const size_t lse_n = static_cast<size_t>(L) * M * D.n_q_heads, q_n = static_cast<size_t>(L) * M * D.q_dim;
+  const int64_t stride = plan.weights_on ? plan.weights_stride : 0;
+  int64_t new_stride = 1;
+  for (int b = 0; b < n_prompts; ++b) new_stride = std::max<int64_t>(new_stride, plan.cu_ctx[b + 1] - plan.cu_ctx[b] + plan.reserve);
+  const size_t w_n = static_cast<size_t>(L) * n_prompts * D.n_kv_heads * new_stride;
+  if (!dev_grow(h, &h->tree_ints, &h->tree_ints_cap, ints.size()) ||
+      (track && (!dev_grow(h, &h->lse_hist, &h->lse_hist_cap, lse_n) || (n_nodes && !dev_grow(h, &h->q_hist, &h->q_hist_cap, q_n)) ||
+                 (!plan.weights_on && !dev_grow(h, &h->weights, &h->weights_cap, w_n)))))
+    return PERCACHE_E_NOMEM;
+  const bool use_ref = (h->flags & PERCACHE_FLAG_REFERENCE_KERNELS) != 0;
+  if (use_ref && !h->cref) {
+    const size_t wide = static_cast<size_t>(std::max(std::max(D.qkv_dim, 2 * D.d_ffn), d));
+    if (!dev_alloc(h, &h->cref, static_cast<size_t>(h->m_cap) * wide)) return PERCACHE_E_NOMEM;
+  }
+  const double plan_us = std::chrono::duration<double, std::micro>(std::chrono::steady_clock::now() - t_host0).count();
+  // ---- device work
+  plan.tree_n.clear();               // nodes of an earlier call end here
+  cudaStream_t s = h->stream;
+  percache_stats_t& st = h->stats;
+  std::memset(st.phase_us, 0, sizeof(st.phase_us));
+  std::memset(st.phase_launches, 0, sizeof(st.phase_launches));
+  PhaseTimer timer(h);
+  bool ok = true;
+  const bool assemble = !plan.ctx_assembled;
+  if (assemble) ok = ok && assemble_late(h, reinterpret_cast<GatherItem*>(row_ctx0 + h->m_cap), timer, s);
+  ok = ok && cudaMemcpyAsync(h->d_index, h->h_index, 4 * static_cast<size_t>(h->m_cap) * sizeof(int32_t), cudaMemcpyHostToDevice, s) == cudaSuccess;
+  ok = ok && cudaMemcpyAsync(h->tree_ints, ints.data(), ints.size() * sizeof(int32_t), cudaMemcpyHostToDevice, s) == cudaSuccess;
+  ok = ok && cudaMemsetAsync(h->d_err, 0, sizeof(int), s) == cudaSuccess && cudaMemsetAsync(h->tree_ws, 0, 256, s) == cudaSuccess;
+  if (track && !plan.weights_on) ok = ok && cudaMemsetAsync(h->weights, 0, w_n * sizeof(float), s) == cudaSuccess;
+  TreeStep step{};
+  step.attn.kv = ctx_view(h, 0, h->tree_ints + 2 * n_prompts + 1);
+  TreeRows& tr = step.attn.rows;
+  tr.n_seqs = n_prompts; tr.n_rows = M; tr.max_nodes = max_n; tr.max_len = max_len;
+  tr.ctx_len = h->tree_ints; tr.row_start = h->tree_ints + n_prompts;
+  tr.mask = reinterpret_cast<const uint64_t*>(h->tree_ints + head); tr.mask_words = words;
+  step.attn.q_stride = step.attn.out_stride = D.q_dim;
+  step.attn.n_q_heads = D.n_q_heads;
+  step.attn.scale = 0.08838834764831845f;          // 1 / sqrt(128)
+  step.attn.workspace = h->tree_ws;
+  if (track) {
+    step.lse = h->lse_hist;
+    step.weights_stride = plan.weights_on ? stride : new_stride;
+    step.weights_layer = static_cast<size_t>(n_prompts) * D.n_kv_heads * step.weights_stride;
+    step.decay = h->weight_decay;
+    if (n_nodes) step.q_hist = h->q_hist;
+    else step.weights = h->weights;
+  }
+  timer.begin(PERCACHE_PH_IO);
+  ok = ok && cudaMemcpyAsync(h->xin, hidden, static_cast<size_t>(M) * d * 2, hidden_on_device ? cudaMemcpyDeviceToDevice : cudaMemcpyHostToDevice, s) == cudaSuccess;
+  cudaEventRecord(h->ev_begin, s);
+  launch_bf16_to_f32(h->xin, h->resid, static_cast<int64_t>(M) * d, s);
+  timer.end();
+  ok = ok && run_layers(h, M, dev_index(h), 0, 0, false, use_ref, timer, s, 0, nullptr, &step);
+  cudaEventRecord(h->ev_end, s);
+  timer.begin(PERCACHE_PH_IO);
+  ok = ok && cudaMemcpyAsync(out_hidden, h->resid, static_cast<size_t>(M) * d * sizeof(float), out_on_device ? cudaMemcpyDeviceToDevice : cudaMemcpyDeviceToHost, s) == cudaSuccess;
+  int ws_err = 0;
+  ok = ok && cudaMemcpyAsync(h->h_err, h->d_err, sizeof(int), cudaMemcpyDeviceToHost, s) == cudaSuccess &&
+       cudaMemcpyAsync(&ws_err, h->tree_ws, sizeof(int), cudaMemcpyDeviceToHost, s) == cudaSuccess;
+  timer.end();
+  const cudaError_t sync_rc = cudaStreamSynchronize(s);
+  if (!ok || sync_rc != cudaSuccess || cudaGetLastError() != cudaSuccess) return PERCACHE_E_CUDA;
+  if (*h->h_err != 0 || ws_err != 0) return PERCACHE_E_DEVICE_TIMEOUT;
+  if (assemble) assembled(h);
+  if (track && !plan.weights_on) { plan.weights_on = true; plan.weights_stride = static_cast<int32_t>(new_stride); }
+  if (n_nodes) {
+    plan.tree_n.assign(n_nodes, n_nodes + n_prompts);
+    plan.tree_parent.assign(parents, parents + M);
+    plan.tree_tracked = track;
+  } else {
+    for (int b = 0; b < n_prompts; ++b) plan.dec_len[b] += 1;
+  }
+  st.n_prompts = n_prompts;
+  st.chunks_hit = st.chunks_missed = 0;
+  st.hit_tokens = 0;
+  st.new_rows = M;
+  st.ctx_tokens = 0;
+  for (int b = 0; b < n_prompts; ++b) st.ctx_tokens += ctx_slots(plan, b);
+  st.host_plan_us = plan_us;
+  st.attn_visible_pairs = visible_pairs;
+  st.evictions = 0;
+  st.gather_free = 0;
+  float ms = 0.f;
+  cudaEventElapsedTime(&ms, h->ev_begin, h->ev_end);
+  st.device_us = 1000.0 * ms;
+  timer.collect();
+  return PERCACHE_OK;
+} catch (const std::bad_alloc&) {          // host arrays of a step, before any device work
+  return PERCACHE_E_NOMEM;
+}
+
+// The batch a decode call continues: PERCACHE_OK, or why it cannot.
+int decode_batch(const percache* h, int32_t n_prompts) {
+  if (n_prompts <= 0 || h->paper_mode || static_cast<size_t>(n_prompts) + 1 != h->plan.cu_ctx.size()) return PERCACHE_E_INVAL;
+  // the last prefill ran gather-free: without a decode reserve nothing was kept to build the context from
+  if (!h->plan.ctx_assembled && h->plan.page_table.empty()) return PERCACHE_E_INVAL;
+  return PERCACHE_OK;
+}
 
 // ---------------------------------------------------------------------------------------------------------------
 // Paper-faithful mode (PERCACHE_FLAG_PAPER_MODE): the scheme as the paper states it.  The chunk list is matched as a
@@ -1384,6 +1653,7 @@ int percache_prefill(percache_t* h, const percache_prompt_t* prompts, int32_t n_
     const int32_t ctx0 = pbase + b * h->decode_reserve;                // slot in the device context
     const int32_t pt0 = pt_next;                                       // gather-free form: first entry of its page table
     plan.ctx0.push_back(ctx0);
+    plan.reserve = h->decode_reserve;
     plan.dec_len.push_back(0);
     int32_t t = 0;
     for (int i = 0; i <= P.n_chunks; ++i) {
@@ -1623,6 +1893,10 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
   if (!plan.ctx_assembled && plan.page_table.empty()) return PERCACHE_E_INVAL;
   if (n_prompts > h->m_cap) return PERCACHE_E_CAPACITY;
   if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
+  plan.tree_n.clear();               // nodes that were not accepted end here
+  // steps that leave their weights behind, and steps over a context whose slots are no longer its positions
+  if ((h->flags & PERCACHE_FLAG_TRACK_WEIGHTS) || !plan.evicted.empty())
+    return decode_rows(h, n_prompts, nullptr, nullptr, hidden, hidden_on_device, out_hidden, out_on_device);
   const auto t_host0 = std::chrono::steady_clock::now();
   const ModelDims& D = h->dims;
   const int d = D.d_model;
@@ -1724,26 +1998,7 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
     if (plan.page_table.size() > 4 * static_cast<size_t>(h->ctx_cap)) return PERCACHE_E_CAPACITY;
     std::memcpy(items, plan.page_table.data(), plan.page_table.size() * sizeof(int32_t));
   } else if (!plan.ctx_assembled) {
-    // First decode step after a gather-free prefill: every slot of every prompt still sits in a page (cached chunks
-    // in theirs, the rows that prefill computed in the pages lent to them), so the fetch that prefill skipped runs
-    // now, over all slots, and builds the contiguous context the decode kernels read and append to.
-    int n_items = 0;
-    for (int b = 0; b < n_prompts; ++b) {
-      const int32_t T = plan.cu_ctx[b + 1] - plan.cu_ctx[b];
-      for (int32_t o = 0; o < T; o += PAGE_TOKENS) {
-        GatherItem& g = items[n_items++];
-        g.dst_slot = plan.ctx0[b] + o;
-        g.src_page = plan.page_table[static_cast<size_t>(plan.pt0[b] + o / PAGE_TOKENS)];
-        g.n_tok = std::min<int32_t>(PAGE_TOKENS, T - o);
-        g.pos = o;
-      }
-    }
-    ok = ok && cudaMemcpyAsync(reinterpret_cast<int32_t*>(const_cast<GatherItem*>(dev_index(h).items)), items,
-                               static_cast<size_t>(n_items) * sizeof(GatherItem), cudaMemcpyHostToDevice, s) == cudaSuccess;
-    timer.begin(PERCACHE_PH_GATHER);
-    launch_gather_rerope(dev_index(h).items, n_items, D.n_layers, h->kpool, h->vpool, h->cfg.pool_pages, h->kctx, h->vctx,
-                         h->ctx_cap, D.kv_dim, h->rope, s);
-    timer.end();
+    ok = ok && assemble_late(h, items, timer, s);
     assembled_now = true;
   }
   const size_t used_ints = static_cast<size_t>(reinterpret_cast<int32_t*>(merges + n_merges) - h->h_index);
@@ -1766,14 +2021,7 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
   const cudaError_t sync_rc = cudaStreamSynchronize(s);
   if (!ok || sync_rc != cudaSuccess || cudaGetLastError() != cudaSuccess) return PERCACHE_E_CUDA;
   if (*h->h_err != 0) return PERCACHE_E_DEVICE_TIMEOUT;
-  if (assembled_now) {         // the context exists now: the lent pages go back
-    plan.ctx_assembled = true;
-    plan.page_table.clear();
-    plan.pt0.clear();
-    release_pages(h, h->retained_scratch);
-    h->retained_scratch.clear();
-    refresh_page_stats(h);
-  }
+  if (assembled_now) assembled(h);
   for (int b = 0; b < n_prompts; ++b) plan.dec_len[b] += 1;      // the token's K/V now is part of the context
   st.n_prompts = n_prompts;
   st.chunks_hit = st.chunks_missed = 0;
@@ -1790,6 +2038,178 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
   st.device_us = 1000.0 * ms;
   timer.collect();
   return PERCACHE_OK;
+}
+
+int percache_decode_tree(percache_t* h, int32_t n_prompts, const int32_t* n_nodes, const int32_t* parents, const void* hidden,
+                         int32_t hidden_on_device, float* out_hidden, int32_t out_on_device) {
+  if (!h || !n_nodes || !parents || !hidden || !out_hidden) return PERCACHE_E_INVAL;
+  if (const int rc = decode_batch(h, n_prompts)) return rc;
+  if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
+  return decode_rows(h, n_prompts, n_nodes, parents, hidden, hidden_on_device, out_hidden, out_on_device);
+}
+
+int percache_accept(percache_t* h, int32_t n_prompts, const int32_t* n_accept, const int32_t* nodes) {
+  if (!h || !n_accept || n_prompts <= 0 || static_cast<size_t>(n_prompts) != h->plan.tree_n.size()) return PERCACHE_E_INVAL;
+  Plan& plan = h->plan;
+  const ModelDims& D = h->dims;
+  try {
+    int32_t most = 0, M = 0;
+    int64_t total = 0, row0 = 0;
+    for (int b = 0; b < n_prompts; ++b) {
+      const int32_t a = n_accept[b];
+      if (a < 0 || a > plan.tree_n[b] || (a > 0 && !nodes)) return PERCACHE_E_INVAL;
+      for (int32_t k = 0; k < a; ++k) {
+        const int32_t i = nodes[total + k];
+        if (i < 0 || i >= plan.tree_n[b] || plan.tree_parent[row0 + i] != (k == 0 ? -1 : nodes[total + k - 1])) return PERCACHE_E_INVAL;
+      }
+      most = std::max(most, a);
+      total += a;
+      row0 += plan.tree_n[b];
+    }
+    M = static_cast<int32_t>(row0);
+    if (most == 0 && !plan.tree_tracked) { plan.tree_n.clear(); return PERCACHE_OK; }
+    most = std::max(most, 1);
+    if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
+    // the step's arrays (lengths, row starts, context starts, masks) are still on the device; these join them: accepted counts, new
+    // lengths, lengths with all nodes, kept slots [n][most], use flags (bytes)
+    int32_t max_n = 1, max_len = 1;
+    for (int b = 0; b < n_prompts; ++b) {
+      max_n = std::max(max_n, plan.tree_n[b]);
+      max_len = std::max(max_len, ctx_slots(plan, b) + plan.tree_n[b]);
+    }
+    const int words = (max_n + 63) / 64;
+    const size_t head = (3 * static_cast<size_t>(n_prompts) + 2) & ~size_t(1);
+    const size_t n = static_cast<size_t>(n_prompts), use_ints = (static_cast<size_t>(M) + 3) / 4;
+    std::vector<int32_t> ints(3 * n + n * most + use_ints, 0);
+    uint8_t* use = reinterpret_cast<uint8_t*>(ints.data() + 3 * n + n * most);
+    total = row0 = 0;
+    for (int b = 0; b < n_prompts; ++b) {
+      const int32_t used = ctx_slots(plan, b);
+      ints[b] = n_accept[b];
+      ints[n + b] = used + n_accept[b];
+      ints[2 * n + b] = used + plan.tree_n[b];
+      for (int32_t k = 0; k < n_accept[b]; ++k) {
+        ints[3 * n + static_cast<size_t>(b) * most + k] = used + nodes[total + k];
+        use[row0 + nodes[total + k]] = 1;
+      }
+      total += n_accept[b];
+      row0 += plan.tree_n[b];
+    }
+    cudaStream_t s = h->stream;
+    if (!dev_grow(h, &h->keep, &h->keep_cap, ints.size())) return PERCACHE_E_NOMEM;
+    bool ok = cudaMemcpyAsync(h->keep, ints.data(), ints.size() * sizeof(int32_t), cudaMemcpyHostToDevice, s) == cudaSuccess &&
+              cudaMemsetAsync(h->tree_ws, 0, 256, s) == cudaSuccess;
+    const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;
+    for (int l = 0; l < D.n_layers && ok; ++l) {
+      const KvView kv = ctx_view(h, l, h->tree_ints + 2 * n + 1);
+      if (plan.tree_tracked) {
+        AttentionWeights w{};
+        w.kv = kv;
+        w.rows.n_seqs = n_prompts; w.rows.n_rows = M; w.rows.max_nodes = max_n; w.rows.max_len = max_len;
+        w.rows.ctx_len = h->tree_ints; w.rows.row_start = h->tree_ints + n;
+        w.rows.mask = reinterpret_cast<const uint64_t*>(h->tree_ints + head); w.rows.mask_words = words;
+        w.q = h->q_hist + static_cast<size_t>(l) * M * D.q_dim; w.q_stride = D.q_dim; w.n_q_heads = D.n_q_heads;
+        w.scale = 0.08838834764831845f;
+        w.lse = h->lse_hist + static_cast<size_t>(l) * M * D.n_q_heads;
+        w.use = reinterpret_cast<const uint8_t*>(h->keep + 3 * n + n * most);
+        w.decay = h->weight_decay;
+        w.w_out = h->weights + l * w_layer; w.w_in = w.decay != 0.f ? w.w_out : nullptr; w.w_stride = plan.weights_stride;
+        w.workspace = h->tree_ws;
+        ok = ok && launch_attention_weights(w, h->n_sms, s) == 0;
+      }
+      CompactSlots c{};
+      c.kv = kv;
+      c.n_seqs = n_prompts; c.max_len = max_len;
+      c.first = h->tree_ints; c.keep = h->keep + 3 * n; c.count = h->keep; c.keep_heads = 1; c.budget = most;
+      if (plan.weights_on) { c.w_in = c.w_out = h->weights + l * w_layer; c.w_stride = plan.weights_stride; }
+      ok = ok && launch_compact_slots(c, h->n_sms, s) == 0;
+    }
+    if (plan.weights_on)
+      ok = ok && launch_clear_weights(h->weights, plan.weights_stride, D.n_layers * n_prompts, D.n_kv_heads, n_prompts, h->keep + n,
+                                      h->keep + 2 * n, s) == 0;
+    int ws_err = 0;
+    ok = ok && cudaMemcpyAsync(&ws_err, h->tree_ws, sizeof(int), cudaMemcpyDeviceToHost, s) == cudaSuccess;
+    const cudaError_t rc = cudaStreamSynchronize(s);
+    plan.tree_n.clear();
+    if (!ok || rc != cudaSuccess || cudaGetLastError() != cudaSuccess) return PERCACHE_E_CUDA;
+    if (ws_err != 0) return PERCACHE_E_DEVICE_TIMEOUT;
+    for (int b = 0; b < n_prompts; ++b) plan.dec_len[b] += n_accept[b];
+    return PERCACHE_OK;
+  } catch (const std::bad_alloc&) {
+    return PERCACHE_E_NOMEM;
+  }
+}
+
+int percache_set_weight_decay(percache_t* h, float decay) {
+  if (!h || !(decay >= 0.f) || !std::isfinite(decay)) return PERCACHE_E_INVAL;
+  h->weight_decay = decay;
+  return PERCACHE_OK;
+}
+
+int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t recent) {
+  if (!h || budget < 1 || sink < 0 || recent < 0 || static_cast<int64_t>(sink) + recent > budget || !h->plan.weights_on ||
+      !h->plan.tree_n.empty() || !h->plan.ctx_assembled)
+    return PERCACHE_E_INVAL;
+  if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
+  Plan& plan = h->plan;
+  const ModelDims& D = h->dims;
+  try {
+    const size_t n = plan.dec_len.size();
+    const int32_t np = static_cast<int32_t>(n);
+    // lengths, context starts, new lengths; then the kept counts and lists of one layer
+    std::vector<int32_t> ints(3 * n);
+    int32_t max_len = 1;
+    for (int b = 0; b < np; ++b) {
+      ints[b] = ctx_slots(plan, b);
+      ints[n + b] = plan.ctx0[b];
+      ints[2 * n + b] = std::min(ints[b], budget);
+      max_len = std::max(max_len, ints[b]);
+    }
+    if (max_len <= budget) return PERCACHE_OK;
+    cudaStream_t s = h->stream;
+    if (!dev_grow(h, &h->keep, &h->keep_cap, 4 * n + n * D.n_kv_heads * budget)) return PERCACHE_E_NOMEM;
+    int32_t *d_len = h->keep, *d_start = d_len + n, *d_new = d_start + n, *d_count = d_new + n, *d_keep = d_count + n;
+    bool ok = cudaMemcpyAsync(h->keep, ints.data(), ints.size() * sizeof(int32_t), cudaMemcpyHostToDevice, s) == cudaSuccess;
+    const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;
+    for (int l = 0; l < D.n_layers && ok; ++l) {
+      float* w = h->weights + l * w_layer;
+      ok = ok && launch_select_slots(w, plan.weights_stride, d_len, np, D.n_kv_heads, max_len, budget, sink, recent, d_keep, d_count, h->n_sms, s) == 0;
+      CompactSlots c{};
+      c.kv = ctx_view(h, l, d_start);
+      c.n_seqs = np; c.max_len = max_len;
+      c.keep = d_keep; c.count = d_count; c.keep_heads = D.n_kv_heads; c.budget = budget;
+      c.w_in = c.w_out = w; c.w_stride = plan.weights_stride;
+      ok = ok && launch_compact_slots(c, h->n_sms, s) == 0;
+    }
+    ok = ok && launch_clear_weights(h->weights, plan.weights_stride, D.n_layers * np, D.n_kv_heads, np, d_new, d_len, s) == 0;
+    const cudaError_t rc = cudaStreamSynchronize(s);
+    if (!ok || rc != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+      h->plan = Plan();              // some layers may be cut and others not: this batch cannot go on
+      return PERCACHE_E_CUDA;
+    }
+    if (plan.evicted.empty()) plan.evicted.assign(n, 0);
+    for (int b = 0; b < np; ++b) plan.evicted[b] += ints[b] - ints[2 * n + b];
+    return PERCACHE_OK;
+  } catch (const std::bad_alloc&) {
+    return PERCACHE_E_NOMEM;
+  }
+}
+
+int64_t percache_debug_read_weights(percache_t* h, int32_t prompt, int32_t layer, float* out, int64_t capacity_floats) {
+  if (!h || !out || layer < 0 || layer >= h->dims.n_layers || prompt < 0 || !h->plan.weights_on ||
+      prompt >= static_cast<int32_t>(h->plan.dec_len.size()))
+    return PERCACHE_E_INVAL;
+  if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
+  const Plan& plan = h->plan;
+  const int32_t slots = ctx_slots(plan, prompt), heads = h->dims.n_kv_heads;
+  if (capacity_floats < static_cast<int64_t>(slots) * heads) return PERCACHE_E_CAPACITY;
+  const float* w = h->weights + (static_cast<size_t>(layer) * plan.dec_len.size() + prompt) * heads * plan.weights_stride;
+  if (cudaMemcpy2D(out, static_cast<size_t>(slots) * sizeof(float), w, static_cast<size_t>(plan.weights_stride) * sizeof(float),
+                   static_cast<size_t>(slots) * sizeof(float), heads, cudaMemcpyDeviceToHost) != cudaSuccess) {
+    cudaGetLastError();
+    return PERCACHE_E_CUDA;
+  }
+  return slots;
 }
 
 int percache_get_stats(percache_t* h, percache_stats_t* out) {
@@ -1853,7 +2273,7 @@ int percache_debug_read_ctx(percache_t* h, int32_t prompt, int32_t layer, void* 
   if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
   const size_t ctx_layer = static_cast<size_t>(h->ctx_cap) * h->dims.kv_dim;
   const size_t off = layer * ctx_layer + static_cast<size_t>(h->plan.ctx0[prompt]) * h->dims.kv_dim;
-  const int64_t tokens = h->plan.cu_ctx[prompt + 1] - h->plan.cu_ctx[prompt] + h->plan.dec_len[prompt];
+  const int64_t tokens = ctx_slots(h->plan, prompt);
   if (capacity_tokens < tokens) return PERCACHE_E_CAPACITY;
   const size_t bytes = static_cast<size_t>(tokens) * h->dims.kv_dim * 2;
   if (cudaMemcpy(k_host, h->kctx + off, bytes, cudaMemcpyDeviceToHost) != cudaSuccess ||

@@ -262,7 +262,20 @@ __global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots 
   }
 }
 
+__global__ void __launch_bounds__(MOVE_THREADS) clear_weights_kernel(float* weights, int64_t w_stride, int n_prompts, const int32_t* __restrict__ from,
+                                                                     const int32_t* __restrict__ to) {
+  const int b = blockIdx.y % n_prompts;
+  float* w = weights + (static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * w_stride;
+  for (int s = __ldg(from + b) + threadIdx.x; s < __ldg(to + b); s += MOVE_THREADS) w[s] = 0.f;
+}
+
 }  // namespace
+
+int launch_clear_weights(float* weights, int64_t w_stride, int n_lists, int n_heads, int n_prompts, const int32_t* from, const int32_t* to,
+                         cudaStream_t s) {
+  clear_weights_kernel<<<dim3(n_heads, n_lists), MOVE_THREADS, 0, s>>>(weights, w_stride, n_prompts, from, to);
+  return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
+}
 
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
                         int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s) {

@@ -30,13 +30,15 @@ FLAG_SINGLE_CTA_GEMM = 16
 FLAG_NO_SMALL_ROW_KERNELS = 32
 FLAG_PAPER_MODE = 64
 FLAG_GATHER_FREE, FLAG_ALWAYS_GATHER = 128, 256
+FLAG_TRACK_WEIGHTS = 512
 PAGE_TOKENS = 16
 PHASES = ("gather", "norm", "qkv", "attn", "oproj", "gateup", "down", "io")
 EXPORTS = ("percache_create", "percache_destroy", "percache_put_chunk_kv", "percache_prefill",
            "percache_has_chunk", "percache_drop_chunk", "percache_get_chunk_kv", "percache_get_chunk_q", "percache_put_chunk_synthetic",
            "percache_get_stats", "percache_set_flags", "percache_decode", "percache_set_decode_reserve", "percache_set_store_limit", "percache_chunk_info", "percache_debug_read_plan", "percache_debug_read_ctx", "percache_debug_attn_plan",
            "percache_debug_gemm", "percache_debug_gemm_noalloc", "percache_debug_capture_layers", "percache_debug_wait_probe", "percache_path_key", "percache_qa_top1", "percache_tree_attention",
-           "percache_attention_weights", "percache_select_slots", "percache_compact_slots", "percache_ops_status", "percache_strerror")
+           "percache_decode_tree", "percache_accept", "percache_evict_context", "percache_set_weight_decay",
+           "percache_debug_read_weights", "percache_attention_weights", "percache_select_slots", "percache_compact_slots", "percache_ops_status", "percache_strerror")
 
 
 class PerCacheError(RuntimeError):
@@ -108,6 +110,12 @@ def load_library() -> C.CDLL:
     lib.percache_prefill.argtypes = [vp, C.POINTER(PromptStruct), i32, C.POINTER(ResultStruct)]
     lib.percache_decode.argtypes = [vp, i32, vp, i32, vp, i32]
     lib.percache_set_decode_reserve.argtypes = [vp, i32]
+    lib.percache_decode_tree.argtypes = [vp, i32, vp, vp, vp, i32, vp, i32]
+    lib.percache_accept.argtypes = [vp, i32, vp, vp]
+    lib.percache_evict_context.argtypes = [vp, i32, i32, i32]
+    lib.percache_set_weight_decay.argtypes = [vp, C.c_float]
+    lib.percache_debug_read_weights.argtypes = [vp, i32, i32, vp, i64]
+    lib.percache_debug_read_weights.restype = i64
     lib.percache_has_chunk.argtypes = [vp, u64, C.POINTER(i32)]
     lib.percache_drop_chunk.argtypes = [vp, u64]
     lib.percache_get_chunk_kv.argtypes = [vp, u64, vp, vp]
@@ -137,7 +145,7 @@ def load_library() -> C.CDLL:
     lib.percache_strerror.argtypes = [C.c_int]
     lib.percache_strerror.restype = C.c_char_p
     for name in EXPORTS:
-        if name not in ("percache_debug_read_plan", "percache_strerror", "percache_path_key"):
+        if name not in ("percache_debug_read_plan", "percache_debug_read_weights", "percache_strerror", "percache_path_key"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -355,6 +363,44 @@ class PerCache:
         _check(self._lib.percache_decode(self._h, n, _ptr(hidden), 1 if _is_device(hidden) else 0, _ptr(out),
                                          1 if _is_device(out) else 0), "percache_decode")
         return out
+
+    def decode_tree(self, parents: Sequence[Sequence[int]], hidden: Any, out: Optional[Any] = None):
+        """percache_decode_tree: drafted tokens of every prompt of the last prefill call at once.
+
+        parents: per prompt, the index of the node each node follows (-1: the prompt's last token), parents before
+        children.  hidden: bf16 [sum of nodes, d_model] (host uint16 or device tensor), prompt after prompt.  Returns fp32
+        [sum of nodes, d_model], or fills and returns `out`."""
+        n = np.array([len(p) for p in parents], dtype=np.int32)
+        par = np.array([int(x) for p in parents for x in p] or [0], dtype=np.int32)
+        rows = int(n.sum())
+        if int(hidden.shape[0]) != rows:
+            raise ValueError("one hidden row per node")
+        if out is None:
+            out = np.empty((rows, self.d_model), dtype=np.float32)
+        _check(self._lib.percache_decode_tree(self._h, len(parents), _ptr(n), _ptr(par), _ptr(hidden), 1 if _is_device(hidden) else 0,
+                                              _ptr(out), 1 if _is_device(out) else 0), "percache_decode_tree")
+        return out
+
+    def accept(self, paths: Sequence[Sequence[int]]) -> None:
+        """percache_accept: per prompt, the nodes of the last decode_tree call to keep, from a root down."""
+        n = np.array([len(p) for p in paths], dtype=np.int32)
+        nodes = np.array([int(x) for p in paths for x in p] or [0], dtype=np.int32)
+        _check(self._lib.percache_accept(self._h, len(paths), _ptr(n), _ptr(nodes)), "percache_accept")
+
+    def evict_context(self, budget: int, sink: int = 0, recent: int = 0) -> None:
+        """percache_evict_context: at most `budget` context slots per prompt, layer and KV head, by running attention weight."""
+        _check(self._lib.percache_evict_context(self._h, int(budget), int(sink), int(recent)), "percache_evict_context")
+
+    def set_weight_decay(self, decay: float) -> None:
+        _check(self._lib.percache_set_weight_decay(self._h, float(decay)), "percache_set_weight_decay")
+
+    def read_weights(self, prompt: int, layer: int, slots: int, n_kv_heads: int) -> np.ndarray:
+        """Running attention weights of one prompt and layer: float32 [n_kv_heads, slots of its context]."""
+        buf = np.empty(n_kv_heads * slots, dtype=np.float32)
+        got = int(self._lib.percache_debug_read_weights(self._h, prompt, layer, _ptr(buf), buf.size))
+        if got < 0:
+            raise PerCacheError(got, "percache_debug_read_weights")
+        return buf[:n_kv_heads * got].reshape(n_kv_heads, got)
 
     def stats(self) -> Dict[str, Any]:
         s = StatsStruct()
