@@ -8,7 +8,7 @@
 // tensor work (0.75 us) and 16 K exponentials (0.55 us): with the tile at most 128 rows high the operator is bound by
 // reading K and V once, whatever the number of rows, and everything below serves to keep the copies running.
 //
-// Schedule.  Lengths live on the device, so the work is dealt there: every unit costs its blocks plus UNIT_COST, the
+// Schedule.  Lengths live on the device, so the work is dealt there: every unit costs its blocks and a little more, the
 // batch's total cost is cut into one contiguous span per CTA, and a unit that a span border cuts is finished in parts
 // whose unnormalised results a second kernel merges.  Every CTA forms the same prefix sums, so nothing is exchanged.
 //
@@ -420,6 +420,7 @@ int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v
   } else if (launch_pdl(tree_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), TREE_SMEM, s, q, k, v, p) != cudaSuccess) {
     return -1;
   }
+  if (p.rows.max_len <= BLK) return 0;            // one block: nothing is ever cut
   const int rows = std::min(p.tile_nodes, p.rows.max_nodes) * p.group;
   return launch_pdl(tree_merge_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
 }
@@ -443,9 +444,13 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   if (q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
-  if (!units_fit(p.rows.n_seqs, static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads, p.rows.max_len, 1)) return -2;
+  // A unit's cost beside its blocks grows with its rows (the end of every row is written out while no block is worked on).  2 -> 4: 26-node
+  // trees on 2112 slots 18.6 -> 17.1 us, 7-token chains on 2 x 33024 slots 60 -> 57 us, but 64 x 2500 single tokens 108.4 -> 110.4 us.
+  p.over = p.tile_nodes * p.group <= 16 ? 2 : 4;
+  const int64_t units = static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads;
+  if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
-  p.small = small_batch(p.rows.n_seqs, static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads, p.rows.max_len, 1) ? 1 : 0;
+  p.small = small_batch(p.rows.n_seqs, units, p.rows.max_len, 1, p.over) ? 1 : 0;
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_tree<128, true>(q, k, v, p, n_ctas, s) : launch_tree<128, false>(q, k, v, p, n_ctas, s);
   return t.kv.bf16 ? launch_tree<64, true>(q, k, v, p, n_ctas, s) : launch_tree<64, false>(q, k, v, p, n_ctas, s);

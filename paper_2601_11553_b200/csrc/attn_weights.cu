@@ -24,7 +24,8 @@ constexpr int Q_TILE = 32 * 1024;
 constexpr int WEIGHTS_SMEM = K_RING + 2 * Q_TILE + 1024;
 constexpr int MAX_STAGES = 8;
 constexpr int MASK_WORDS = 4;                    // 256 nodes
-constexpr int MIN_SPAN = 3;                      // unit cost and one block
+constexpr int UNIT_COST = 2;                     // of a unit beside its blocks, in blocks
+constexpr int MIN_SPAN = UNIT_COST + 1;
 
 struct WeightParams {
   KvView kv;
@@ -54,8 +55,8 @@ __device__ __forceinline__ int used_nodes(const WeightParams& a, const SeqPart& 
 __device__ __forceinline__ int n_tiles(const WeightParams& a, int nodes) { return (nodes + a.tile_nodes - 1) / a.tile_nodes; }
 __device__ __forceinline__ Shape weight_shape(const WeightParams& a, const SeqPart& p) {
   const int len = p.ctx_len + p.n_nodes;
-  if (len == 0) return Shape{0, 0, 1};
-  return Shape{a.kv.n_kv_heads, (len + BLK - 1) / BLK, max(n_tiles(a, p.n_nodes), 1)};
+  if (len == 0) return Shape{0, 0, 1, 0};
+  return Shape{a.kv.n_kv_heads, (len + BLK - 1) / BLK, max(n_tiles(a, p.n_nodes), 1), UNIT_COST};
 }
 __device__ __forceinline__ bool next_piece(Cursor& cur, const WeightParams& a, Piece* pc) {
   return cur.next(a.rows, [&](const SeqPart& p) { return weight_shape(a, p); }, pc);
@@ -383,8 +384,9 @@ int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t 
   if ((t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) ||
       pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0)
     return -1;
-  if (!units_fit(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes)) return -2;
-  p.small = small_batch(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) ? 1 : 0;
+  const int tiles = (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes;
+  if (!units_fit(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, tiles, UNIT_COST)) return -2;
+  p.small = small_batch(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, tiles, UNIT_COST) ? 1 : 0;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_weights<128, true>(q, k, p, n_ctas, s) : launch_weights<128, false>(q, k, p, n_ctas, s);

@@ -14,7 +14,7 @@ struct MergeRecord {             // written by the CTA that has a cut unit's fir
 struct TreeParams {
   KvView kv;
   TreeRows rows;
-  int32_t n_q_heads, group, tile_nodes, small;
+  int32_t n_q_heads, group, tile_nodes, small, over;
   float scale_log2;
   void* out;
   int64_t out_stride;
@@ -32,8 +32,8 @@ constexpr int NARROW_ROWS = 32;
 namespace {
 
 __device__ __forceinline__ Shape tree_shape(const TreeParams& a, const SeqPart& p) {
-  if (p.n_nodes == 0) return Shape{0, 0, 1};
-  return Shape{(p.n_nodes + a.tile_nodes - 1) / a.tile_nodes * a.kv.n_kv_heads, (p.ctx_len + p.n_nodes + BLK - 1) / BLK, 1};
+  if (p.n_nodes == 0) return Shape{0, 0, 1, 0};
+  return Shape{(p.n_nodes + a.tile_nodes - 1) / a.tile_nodes * a.kv.n_kv_heads, (p.ctx_len + p.n_nodes + BLK - 1) / BLK, 1, a.over};
 }
 struct Item {
   int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes

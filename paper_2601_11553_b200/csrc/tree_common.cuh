@@ -9,7 +9,6 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr int BLK = 128;                        // context slots per block, rows per tile
 constexpr int TREE_THREADS = 384;
-constexpr int UNIT_COST = 2;                    // what a unit costs beside its blocks (Q, the row's end), in blocks
 
 // Workspace: the error word, one merge record per CTA, partial results (two slots per CTA).
 constexpr int WS_MERGE = 256, WS_ML = 16384;
@@ -61,8 +60,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity, int* er
 }
 
 // ---------------------------------------------------------------------------------------------------- schedule
-// What a prompt's work looks like to the schedule: units of n_blk blocks, each block costing blk_cost, each unit UNIT_COST more.
-struct Shape { int units, n_blk, blk_cost; };
+// What a prompt's work looks like to the schedule: units of n_blk blocks, each block costing blk_cost, each unit `over` more (its Q, the
+// rows' end).
+struct Shape { int units, n_blk, blk_cost, over; };
 // A prompt's part of a batch, from the device-side arrays, clamped to the bounds the host knows.
 struct SeqPart { int row0, n_nodes, ctx_len; };
 __device__ __forceinline__ SeqPart seq_part(const TreeRows& r, int b) {
@@ -86,16 +86,16 @@ struct Piece {                   // blocks [blk_begin, blk_end) of one unit
 };
 
 // Fits 32 bits, as does a CTA's share of the batch: the host refuses sizes for which it might not (units_fit).
-__device__ __forceinline__ int shape_cost(const Shape& s) { return (s.n_blk * s.blk_cost + UNIT_COST) * s.units; }
-inline bool units_fit(int64_t n_seqs, int64_t units, int64_t max_len, int64_t blk_cost) {
-  const int64_t cost = ((max_len + BLK - 1) / BLK * blk_cost + UNIT_COST) * units;
+__device__ __forceinline__ int shape_cost(const Shape& s) { return (s.n_blk * s.blk_cost + s.over) * s.units; }
+inline bool units_fit(int64_t n_seqs, int64_t units, int64_t max_len, int64_t blk_cost, int64_t over) {
+  const int64_t cost = ((max_len + BLK - 1) / BLK * blk_cost + over) * units;
   return cost <= INT32_MAX / 4 && cost * n_seqs <= INT64_C(1) << 35;       // over 148 CTAs: a span below 2^28 + a unit
 }
 
 // Batches the whole of whose cost times the CTA count stays in 32 bits, and of few prompts, are dealt by every warp for itself.
 constexpr int SMALL_BATCH = 256;
-inline bool small_batch(int n_seqs, int64_t units, int64_t max_len, int64_t blk_cost) {
-  return n_seqs <= SMALL_BATCH && ((max_len + BLK - 1) / BLK * blk_cost + UNIT_COST) * units * n_seqs <= INT32_MAX / MAX_CTAS;
+inline bool small_batch(int n_seqs, int64_t units, int64_t max_len, int64_t blk_cost, int64_t over) {
+  return n_seqs <= SMALL_BATCH && ((max_len + BLK - 1) / BLK * blk_cost + over) * units * n_seqs <= INT32_MAX / MAX_CTAS;
 }
 
 // shape(part): a prompt's Shape.  Small batches: every warp forms the prefix sums over the prompts for itself, 32 bits, no barrier
@@ -209,13 +209,13 @@ struct Cursor {
         if (++seq < rows.n_seqs) part = seq_part(rows, seq);
         continue;
       }
-      const int cost = sh.n_blk * sh.blk_cost + UNIT_COST;
+      const int cost = sh.n_blk * sh.blk_cost + sh.over;
       const int unit = (pos - seq_start) / cost;
       const int unit_start = seq_start + unit * cost, unit_end = unit_start + cost;
       const int stop = min(end, unit_end);
       // a unit's own cost lies ahead of its blocks: a border inside it leaves the whole unit to the later span; a border
       // inside a block leaves the block to the later span
-      int bb = max(pos - unit_start - UNIT_COST, 0), be = max(stop - unit_start - UNIT_COST, 0);
+      int bb = max(pos - unit_start - sh.over, 0), be = max(stop - unit_start - sh.over, 0);
       if (sh.blk_cost > 1) { bb /= sh.blk_cost; be /= sh.blk_cost; }
       pos = stop;
       if (be <= bb) continue;
