@@ -35,6 +35,7 @@ constexpr int RING_BYTES = 160 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
 constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
 constexpr uint32_t TMEM_S = 256;
+constexpr int WHOLE_BLOCKS = 6;
 
 // ---------------------------------------------------------------------------------------------------- attention
 template <int D, bool BF16>
@@ -420,7 +421,7 @@ int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v
   } else if (launch_pdl(tree_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), TREE_SMEM, s, q, k, v, p) != cudaSuccess) {
     return -1;
   }
-  if (p.rows.max_len <= BLK) return 0;            // one block: nothing is ever cut
+  if (p.whole) return 0;                          // nothing is ever cut
   const int rows = std::min(p.tile_nodes, p.rows.max_nodes) * p.group;
   return launch_pdl(tree_merge_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
 }
@@ -447,6 +448,8 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   // A unit's cost beside its blocks grows with its rows (the end of every row is written out while no block is worked on).  2 -> 4: 26-node
   // trees on 2112 slots 18.6 -> 17.1 us, 7-token chains on 2 x 33024 slots 60 -> 57 us, but 64 x 2500 single tokens 108.4 -> 110.4 us.
   p.over = p.tile_nodes * p.group <= 16 ? 2 : 4;
+  // Short contexts: a unit is not worth cutting, the second kernel costs more than the blocks it would spread.
+  p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;
   const int64_t units = static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads;
   if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
   const int n_ctas = std::min(n_sms, MAX_CTAS);

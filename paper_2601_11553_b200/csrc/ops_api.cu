@@ -15,8 +15,8 @@ struct DeviceGuard {
   int before = -1;
   bool ok = false;
   explicit DeviceGuard(int device) {
-    int n = 0;
-    if (cudaGetDeviceCount(&n) != cudaSuccess || device < 0 || device >= n || cudaGetDevice(&before) != cudaSuccess) {
+    static int n = 0;                          // of the machine: asked for until there is an answer
+    if ((n == 0 && cudaGetDeviceCount(&n) != cudaSuccess) || device < 0 || device >= n || cudaGetDevice(&before) != cudaSuccess) {
       cudaGetLastError();
       before = -1;
       return;

@@ -14,7 +14,7 @@ struct MergeRecord {             // written by the CTA that has a cut unit's fir
 struct TreeParams {
   KvView kv;
   TreeRows rows;
-  int32_t n_q_heads, group, tile_nodes, small, over;
+  int32_t n_q_heads, group, tile_nodes, small, over, whole;
   float scale_log2;
   void* out;
   int64_t out_stride;
@@ -33,7 +33,9 @@ namespace {
 
 __device__ __forceinline__ Shape tree_shape(const TreeParams& a, const SeqPart& p) {
   if (p.n_nodes == 0) return Shape{0, 0, 1, 0};
-  return Shape{(p.n_nodes + a.tile_nodes - 1) / a.tile_nodes * a.kv.n_kv_heads, (p.ctx_len + p.n_nodes + BLK - 1) / BLK, 1, a.over};
+  const int units = (p.n_nodes + a.tile_nodes - 1) / a.tile_nodes * a.kv.n_kv_heads, n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK;
+  // units that are not to be cut look like one block that costs as much
+  return a.whole ? Shape{units, 1, n_blk, a.over} : Shape{units, n_blk, 1, a.over};
 }
 struct Item {
   int seq, ctx_len, n_nodes;     // the prompt: its context slots and nodes
@@ -56,6 +58,7 @@ __device__ __forceinline__ bool next_item(Cursor& cur, const TreeParams& a, Item
   it->n_rows = min(a.tile_nodes, pc.part.n_nodes - it->node0) * a.group;
   it->g = pc.unit / tiles;
   it->blk_begin = pc.blk_begin; it->blk_end = pc.blk_end; it->n_blk = pc.n_blk; it->unit_end = pc.unit_end;
+  if (a.whole) it->blk_end = it->n_blk = (it->ctx_len + it->n_nodes + BLK - 1) / BLK;
   return true;
 }
 // Bits of the 32 slots from slot0 on that a node sees.
