@@ -14,8 +14,9 @@ namespace {
 // found, and of the equal ones as many as are left, lowest slot first.
 // Bounds: the weights are a few bytes a thread; what counts is the number of instructions per weight and pass (11 bins of 43
 // were key arithmetic before the always-kept slots were taken out and NaN and -0 were folded into two operations) and the latency of
-// the dependent passes.  Weights stay in registers when a warp's stretch is at most 32 x SEL_UNROLL slots, else every pass reads them
-// again (L1 or L2).
+// the dependent passes.  Weights stay in registers when a warp's stretch is at most 32 x SEL_UNROLL slots.  Longer lists are read
+// three times: for the first histogram, to put the keys of the bin found into a list in shared memory (the other passes work on
+// that), and to write; where the bin holds more than the list (many equal weights), every pass reads all again.
 constexpr int SEL_BITS = 11, SEL_BINS = 1 << SEL_BITS;
 constexpr int SEL_UNROLL = 8;
 constexpr int LONG_LIST = 16384;
@@ -26,16 +27,18 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 
+constexpr int SEL_LIST = 4096;
 template <int THREADS>
 struct SelectShared {
   int hist[SEL_BINS];
   int warp_sum[THREADS / 32], warp_gt[THREADS / 32], warp_eq[THREADS / 32];
-  int bin, need;
+  int bin, need, listed;
+  uint2 list[SEL_LIST];                    // key and slot of the first bin's weights
 };
 
-// lo .. hi - 1: this warp's stretch; n: slots in the middle, counted from `first`; out: where the middle's list starts.
+// lo .. hi - 1: this warp's stretch (of `stretch` slots) of the middle, whose first slot is `first`; out: where the middle's list starts.
 template <int THREADS, bool IN_REGS>
-__device__ __forceinline__ void select_middle(SelectShared<THREADS>& sh, const float* w, int first, int lo, int hi, int need, int32_t* out) {
+__device__ __forceinline__ void select_middle(SelectShared<THREADS>& sh, const float* w, int first, int stretch, int lo, int hi, int need, int32_t* out) {
   constexpr int BINS_EACH = SEL_BINS / THREADS;
   static_assert(SEL_BINS % THREADS == 0, "");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -53,25 +56,39 @@ __device__ __forceinline__ void select_middle(SelectShared<THREADS>& sh, const f
 #pragma unroll
       for (int u = 0; u < SEL_UNROLL; ++u) fn(lo + lane + u * 32, key[u], lo + lane + u * 32 < hi);
     } else {
+      int s0 = lo;
 #pragma unroll 1
-      for (int s0 = lo + lane; s0 - lane < hi; s0 += 32 * SEL_UNROLL) {
-        fetch(s0);
+      for (; s0 + 32 * SEL_UNROLL <= hi; s0 += 32 * SEL_UNROLL) {
+        float x[SEL_UNROLL];
 #pragma unroll
-        for (int u = 0; u < SEL_UNROLL; ++u) fn(s0 + u * 32, key[u], s0 + u * 32 < hi);
+        for (int u = 0; u < SEL_UNROLL; ++u) x[u] = __ldg(w + s0 + lane + u * 32);
+#pragma unroll
+        for (int u = 0; u < SEL_UNROLL; ++u) fn(s0 + lane + u * 32, weight_key(x[u]), true);
       }
+#pragma unroll 1
+      for (; s0 < hi; s0 += 32) fn(s0 + lane, weight_key(s0 + lane < hi ? __ldg(w + s0 + lane) : 0.f), s0 + lane < hi);
     }
   };
   if constexpr (IN_REGS) fetch(lo + lane);
   uint32_t prefix = 0, known = 0;          // the key's bits found so far, and which bits those are
+  bool listed = false;                     // the keys that share the prefix are all in sh.list
+  int gt = 0, eq = 0;
 #pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digit = pass == 2 ? 1023u : 2047u;
     for (int i = tid; i < SEL_BINS; i += THREADS) sh.hist[i] = 0;
     __syncthreads();
-    each([&](int, uint32_t k, bool inside) {
-      if (inside && (k & known) == prefix) atomicAdd(&sh.hist[(k >> shift) & digit], 1);
-    });
+    auto add = [&](uint32_t k) {
+      if ((k & known) == prefix) atomicAdd(&sh.hist[(k >> shift) & digit], 1);
+    };
+    if (listed) {
+      for (int i = tid; i < sh.listed; i += THREADS) add(sh.list[i].x);
+    } else {
+      each([&](int, uint32_t k, bool inside) {
+        if (inside) add(k);
+      });
+    }
     __syncthreads();
     // thread t has the bins SEL_BINS - 1 - t * BINS_EACH downwards: which of them is it in which the running count reaches `need`
     int c[BINS_EACH], mine = 0;
@@ -100,26 +117,63 @@ __device__ __forceinline__ void select_middle(SelectShared<THREADS>& sh, const f
     prefix |= static_cast<uint32_t>(sh.bin) << shift;
     known |= digit << shift;
     need = sh.need;
+    if constexpr (!IN_REGS) {
+      if (pass == 0) {
+        if (tid == 0) sh.listed = 0;
+        __syncthreads();
+        each([&](int s, uint32_t k, bool inside) {
+          const uint32_t top = k & known;
+          gt += inside && top > prefix;
+          const bool mine = inside && top == prefix;
+          const uint32_t all = __ballot_sync(0xffffffffu, mine);
+          if (all != 0) {
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&sh.listed, __popc(all));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(all & ((1u << lane) - 1));
+            if (mine && at < SEL_LIST) sh.list[at] = make_uint2(k, static_cast<uint32_t>(s));
+          }
+        });
+        __syncthreads();
+        listed = sh.listed <= SEL_LIST;
+      }
+    }
   }
-  int gt = 0, eq = 0;
-  each([&](int, uint32_t k, bool inside) {
-    gt += inside && k > prefix;
-    eq += inside && k == prefix;
-  });
-  gt = __reduce_add_sync(0xffffffffu, gt);
-  eq = __reduce_add_sync(0xffffffffu, eq);
-  if (lane == 0) { sh.warp_gt[warp] = gt; sh.warp_eq[warp] = eq; }
+  // what every warp keeps of its stretch
+  if (listed) {
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    if (lane == 0) { sh.warp_gt[warp] = gt; sh.warp_eq[warp] = 0; }
+    __syncthreads();
+    for (int i = tid; i < sh.listed; i += THREADS) {
+      const uint2 e = sh.list[i];
+      if (e.x >= prefix) atomicAdd(e.x > prefix ? &sh.warp_gt[e.y / stretch] : &sh.warp_eq[e.y / stretch], 1);
+    }
+  } else {
+    gt = 0;
+    each([&](int, uint32_t k, bool inside) {
+      gt += inside && k > prefix;
+      eq += inside && k == prefix;
+    });
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
+    if (lane == 0) { sh.warp_gt[warp] = gt; sh.warp_eq[warp] = eq; }
+  }
   __syncthreads();
+  const bool any_eq = sh.warp_eq[warp] != 0;
   int gt_before = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_gt[lane] : 0);
   int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_eq[lane] : 0);
   const uint32_t below = (1u << lane) - 1;
   each([&](int s, uint32_t k, bool inside) {
     const bool is_gt = inside && k > prefix, is_eq = inside && k == prefix;
-    const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
-    const int e = eq_before + __popc(be & below);
-    if (is_gt || (is_eq && e < need)) out[gt_before + __popc(bg & below) + min(e, need)] = first + s;
+    const uint32_t bg = __ballot_sync(0xffffffffu, is_gt);
+    if (!any_eq) {                                        // most stretches
+      if (is_gt) out[gt_before + __popc(bg & below) + min(eq_before, need)] = first + s;
+    } else {
+      const uint32_t be = __ballot_sync(0xffffffffu, is_eq);
+      const int e = eq_before + __popc(be & below);
+      if (is_gt || (is_eq && e < need)) out[gt_before + __popc(bg & below) + min(e, need)] = first + s;
+      eq_before += __popc(be);
+    }
     gt_before += __popc(bg);
-    eq_before += __popc(be);
   });
 }
 
@@ -145,8 +199,8 @@ select_slots_kernel(const float* __restrict__ weights, int64_t w_stride, const i
   const float* w = weights + (static_cast<size_t>(b) * n_heads + h) * w_stride + sink;
   const int stretch = (n + THREADS - 1) / THREADS * 32;                    // whole steps of 32 for each warp
   const int lo = min(warp * stretch, n), hi = min(lo + stretch, n);
-  if (stretch <= 32 * SEL_UNROLL) select_middle<THREADS, true>(sh, w, sink, lo, hi, need, out + sink);
-  else select_middle<THREADS, false>(sh, w, sink, lo, hi, need, out + sink);
+  if (stretch <= 32 * SEL_UNROLL) select_middle<THREADS, true>(sh, w, sink, stretch, lo, hi, need, out + sink);
+  else select_middle<THREADS, false>(sh, w, sink, stretch, lo, hi, need, out + sink);
 }
 
 // ---------------------------------------------------------------------------------------------------- moving
