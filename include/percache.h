@@ -427,6 +427,7 @@ PERCACHE_API int percache_qa_top1(int32_t device, void* stream, const float* ban
  *    may be captured into a CUDA graph.  All array arguments are device memory of `device`, and must stay valid until
  *    the work has run.  Everything that differs from step to step (lengths, page tables, masks) is read on the device,
  *    so a captured call may be replayed after those arrays were rewritten in place.
+ *  - NULL is the legacy default stream, which other streams do not wait for unless they were created to.
  *  - Sizes the host has to know are given as upper bounds (max_len, max_nodes).  Device-side values beyond them, or
  *    negative ones, are clamped; a page id or slot outside the pools reads as zeros and is never written.
  *  - Refused calls (PERCACHE_E_INVAL, PERCACHE_E_CAPACITY) enqueue nothing.
@@ -462,7 +463,7 @@ typedef struct {
  * ctx_len[b] + i.  It sees every context slot and the nodes j < n whose bit (j % 64 of word j / 64) is set in its row
  * of `mask`, itself included only if its own bit is set; without a mask it sees nodes 0 .. i. */
 typedef struct {
-  int32_t n_seqs;
+  int32_t n_seqs;                  /* at most 65535                                                               */
   int32_t n_rows;                  /* rows of q, out, lse (and of mask and use)                                   */
   int32_t max_nodes;               /* most nodes of a prompt, 1 .. PERCACHE_MAX_TREE_NODES                        */
   int32_t max_len;                 /* most slots of a prompt, its nodes included; at most 2^26                    */
@@ -513,7 +514,8 @@ PERCACHE_API int percache_select_slots(int32_t device, void* stream, const float
  * (weights NULL: none).  keep: int32 [n_seqs][keep_heads][budget] with keep_heads = n_kv_heads, or 1 for a list that all
  * heads share.  An index outside 0 .. max_len - 1, or a destination slot at or past max_len, moves nothing.
  * dst_page_table / dst_start (as page_table / ctx_start of kv) NULL: in place; a list must then be strictly ascending
- * with keep[j] >= first + j.  Else the destination's rows must not be rows that are read.  weights_in and weights_out
+ * with keep[j] >= first + j, and no two prompts may share rows.  Else the destination's rows must not be rows that are
+ * read, nor each other's.  weights_in and weights_out
  * may be the same array under the same rule as in place, with weights_stride >= max_len. */
 PERCACHE_API int percache_compact_slots(int32_t device, void* stream, const percache_kv_t* kv, int32_t n_seqs,
                                         int32_t max_len, const int32_t* dst_page_table,

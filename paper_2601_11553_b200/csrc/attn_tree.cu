@@ -256,7 +256,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       ml[par][i][r][1] = l;
       __syncwarp();
       if (elect_one()) mbar_arrive(&ml_full);
-      ok = __all_sync(0xffffffffu, mbar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR)) ;
+      ok = __all_sync(0xffffffffu, mbar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR));
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full, par, a.err_word, DEV_ERR_ATTN_CORR));
       if (!ok) break;
       tc_fence_after_sync();

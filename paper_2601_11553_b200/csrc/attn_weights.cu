@@ -10,7 +10,8 @@
 //
 // Schedule as in the attention (spans of the batch's blocks), but a block belongs to one CTA: nothing is merged.
 // One CTA per SM, 384 threads: warp 8 copies (K ring, Q ring of two tiles), warp 9 issues the MMAs, warps 10-11 put the rows'
-// lse beside each Q tile (and, where a mask says which rows count, fetch those rows alone: of a drafted tree few are accepted), warps 0-3 sum the even blocks and warps 4-7 the odd ones, each from two TMEM buffers in turn.
+// lse beside each Q tile (and, where a mask says which rows count, fetch those rows alone: of a drafted tree few are accepted),
+// warps 0-3 sum the even blocks and warps 4-7 the odd ones, each from two TMEM buffers in turn.
 // One tile of rows stays in shared memory for the whole piece; of several, each is copied again for every block (L2).
 #include <algorithm>
 
@@ -380,10 +381,10 @@ int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t 
   p.scale = t.scale; p.decay = t.decay; p.lse = t.lse; p.use = t.use;
   p.w_in = t.w_in; p.w_out = t.w_out; p.w_stride = t.w_stride;
   p.err_word = static_cast<int*>(t.workspace);
-  CUtensorMap q{}, k;
-  if ((t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) ||
-      pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0)
-    return -1;
+  CUtensorMap q, k;
+  if (pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0) return -1;
+  q = k;                       // a batch without rows copies none, but the kernel prefetches the map
+  if (t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) return -1;
   const int tiles = (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes;
   if (!units_fit(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, tiles, UNIT_COST)) return -2;
   p.small = small_batch(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, tiles, UNIT_COST) ? 1 : 0;

@@ -565,7 +565,7 @@ def _row_stride(x: Any, name: str, heads: int, head_dim: int) -> int:
     shape, st = x.shape, x.stride()
     if len(st) != 3 or shape[1] != heads or shape[2] != head_dim or st[2] != 1 or (heads > 1 and st[1] != head_dim):
         raise ValueError(f"{name}: expected [rows, {heads}, {head_dim}] with dense heads")
-    return st[0] if shape[0] > 1 else max(st[0], heads * head_dim)
+    return st[0] if shape[0] > 1 else heads * head_dim
 
 
 def _kv(k: Any, v: Any, page_table: Any, ctx_start: Any, n_seqs: int) -> KvStruct:
@@ -611,7 +611,8 @@ def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len
 
     q, out: [rows, q_heads, head_dim]; k, v: [slots, kv_heads, head_dim] (pages: slots = 16 x pages); lse: fp32
     [rows, q_heads] or None; mask: int64 words [rows, ceil(max_nodes / 64)] or None (node i sees nodes 0 .. i); workspace:
-    uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` and returns `out`."""
+    uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` (a cudaStream_t; 0 is the legacy default stream, not
+    torch's current one) and returns `out`."""
     kv = _kv(k, v, page_table, ctx_start, ctx_len.shape[0])
     rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
     dev, ty = k.get_device(), _t()

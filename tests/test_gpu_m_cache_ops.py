@@ -471,6 +471,109 @@ def test_compact_leaves_out_what_is_out_of_range():
     assert torch.equal(k.view(torch.int16), k0.view(torch.int16)) and torch.equal(v.view(torch.int16), v0.view(torch.int16))
 
 
+def test_pools_smaller_than_a_block_and_a_single_row():
+    b = Batch([(3, 1)], paged=False, hq=4, hkv=2, pad_rows=0)
+    assert b.k.shape[0] < 128
+    odd = torch.empty(2051, dtype=torch.bfloat16, device="cuda").as_strided((1, 4, 128), (2051, 128, 1))     # one row: its stride means nothing
+    odd.copy_(b.q)
+    b.q = odd
+    b.attend()
+    b.check()
+    w = torch.zeros((1, 2, b.max_len), device="cuda")
+    pcb.attention_weights(b.q, b.k, b.lse, w, **b.args())
+    check_weights(b, w, torch.zeros_like(w), None, 1.0)
+
+
+def test_a_batch_without_rows_only_decays_its_weights():
+    b = Batch([(300, 0), (5, 0)], pad_rows=0)
+    assert b.q.shape[0] == 0
+    b.attend()
+    w = torch.rand((2, b.hkv, b.max_len), device="cuda")
+    before = w.clone()
+    pcb.attention_weights(b.q, b.k, b.lse, w, decay=0.5, **b.args())
+    check_weights(b, w, before, None, 0.5)
+
+
+def test_two_calls_at_once_with_a_workspace_each():
+    parts = [Batch([(6000, 9)], mask="tree", seed=1), Batch([(7000, 1), (100, 3)], seed=2, dtype="f16", paged=False)]
+    streams = [torch.cuda.Stream() for _ in parts]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, s in zip(parts, streams):
+            pcb.tree_attention(b.q, b.k, b.v, b.out, b.lse, **b.args(), stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for b in parts:
+        pcb.ops_status(b.ws)
+        b.check()
+
+
+def test_one_workspace_for_all_calls_of_a_stream():
+    parts = [Batch([(6000, 9)], mask="tree", seed=1), Batch([(7000, 1), (100, 3)], seed=2, dtype="f16", paged=False),
+             Batch([(900, 40)], seed=3, mask="tree")]
+    ws = parts[0].ws
+    for b in parts:
+        b.ws = ws
+    for _ in range(10):
+        for b in parts:
+            pcb.tree_attention(b.q, b.k, b.v, b.out, b.lse, **b.args())
+    for b in parts:
+        b.check()
+
+
+def test_captured_selection_and_moves_follow_their_arrays():
+    n, h, budget = 700, 2, 64
+    k, v = _pools(n, h, 128, "f16")
+    k0, v0 = k.clone(), v.clone()
+    w = torch.zeros((1, h, n), device="cuda")
+    length = torch.tensor([n], dtype=torch.int32).cuda()
+    start = torch.zeros(1, dtype=torch.int32, device="cuda")
+    keep = torch.zeros((1, h, budget), dtype=torch.int32, device="cuda")
+    count = torch.zeros(1, dtype=torch.int32, device="cuda")
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            pcb.select_slots(w, length, keep, count, sink=1, recent=3, stream=side.cuda_stream)
+            pcb.compact_slots(k, v, keep, count, max_len=n, weights=w, ctx_start=start, stream=side.cuda_stream)
+    for m in (700, 65, 40):
+        fresh = torch.rand((1, h, n), device="cuda")
+        k.copy_(k0)
+        v.copy_(v0)
+        w.copy_(fresh)
+        length.fill_(m)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for g in range(h):
+            at = ops.select_slots(fresh[0, g].cpu().numpy(), m, budget, 1, 3)
+            assert count.item() == len(at) and keep[0, g, :len(at)].tolist() == at
+            assert torch.equal(k[:len(at), g].view(torch.int16), k0[at, g].view(torch.int16))
+            assert torch.equal(v[len(at):, g].view(torch.int16), v0[len(at):, g].view(torch.int16))
+            assert torch.equal(w[0, g, :len(at)], fresh[0, g, at])
+
+
+def test_moves_to_another_place_take_any_list():
+    k, v = _pools(128, 2, 64, "bf16")
+    k0 = k.clone()
+    keep = torch.tensor([[[9, 9, 3, 40, 0], [1, 63, 63, 2, 9]]], dtype=torch.int32).cuda()
+    start, dst = torch.tensor([0], dtype=torch.int32).cuda(), torch.tensor([64], dtype=torch.int32).cuda()
+    pcb.compact_slots(k, v, keep, torch.tensor([5], dtype=torch.int32).cuda(), max_len=64, ctx_start=start, dst_start=dst)
+    for g in range(2):
+        assert torch.equal(k[64:69, g].view(torch.int16), k0[keep[0, g].long(), g].view(torch.int16))
+    assert torch.equal(k[:64].view(torch.int16), k0[:64].view(torch.int16))
+
+
+@pytest.mark.parametrize("value", [0.0, 1.0, float("nan"), float("-inf")])
+@pytest.mark.parametrize("n", [300, 20000])
+def test_equal_weights_keep_the_lowest_slots(value, n):
+    w = torch.full((1, 1, n), value, device="cuda")
+    keep = torch.empty((1, 1, n // 2), dtype=torch.int32, device="cuda")
+    count = torch.empty(1, dtype=torch.int32, device="cuda")
+    pcb.select_slots(w, torch.tensor([n], dtype=torch.int32).cuda(), keep, count, sink=2, recent=5)
+    want = list(range(n // 2 - 5)) + list(range(n - 5, n))
+    assert keep[0, 0].tolist() == want and count.item() == n // 2
+
+
 def test_a_run_of_steps_draft_verify_accept_evict():
     """The operators together, as a server uses them: a tree is verified, one path of it accepted and moved behind the
     context, its weights added, and the context cut to a budget; the next step attends to what is left."""
