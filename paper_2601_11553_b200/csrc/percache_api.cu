@@ -628,7 +628,8 @@ int decode_rows(percache* h, int32_t n_prompts, const int32_t* n_nodes, const in
   }
   ints[2 * static_cast<size_t>(n_prompts)] = r;
   std::memcpy(ints.data() + head, mask.data(), mask.size() * sizeof(uint64_t));
-  // ---- memory
+  // ---- memory.  Growing it takes what percache_accept would read of an earlier call's nodes: they end here
+  plan.tree_n.clear();
   if (!h->tree_ws) {
     char* ws = nullptr;
     if (!dev_alloc(h, &ws, PERCACHE_OPS_WORKSPACE_BYTES)) return PERCACHE_E_NOMEM;
@@ -650,7 +651,6 @@ int decode_rows(percache* h, int32_t n_prompts, const int32_t* n_nodes, const in
   }
   const double plan_us = std::chrono::duration<double, std::micro>(std::chrono::steady_clock::now() - t_host0).count();
   // ---- device work
-  plan.tree_n.clear();               // nodes of an earlier call end here
   cudaStream_t s = h->stream;
   percache_stats_t& st = h->stats;
   std::memset(st.phase_us, 0, sizeof(st.phase_us));
@@ -1893,7 +1893,6 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
   if (!plan.ctx_assembled && plan.page_table.empty()) return PERCACHE_E_INVAL;
   if (n_prompts > h->m_cap) return PERCACHE_E_CAPACITY;
   if (cudaSetDevice(h->cfg.device) != cudaSuccess) return PERCACHE_E_CUDA;
-  plan.tree_n.clear();               // nodes that were not accepted end here
   // steps that leave their weights behind, and steps over a context whose slots are no longer its positions
   if ((h->flags & PERCACHE_FLAG_TRACK_WEIGHTS) || !plan.evicted.empty())
     return decode_rows(h, n_prompts, nullptr, nullptr, hidden, hidden_on_device, out_hidden, out_on_device);
@@ -1912,7 +1911,7 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
   int64_t visible_pairs = 0;
   for (int b = 0; b < n_prompts; ++b) {
     const int32_t T = plan.cu_ctx[b + 1] - plan.cu_ctx[b] + plan.dec_len[b];     // tokens so far = the new position
-    if (plan.dec_len[b] >= h->decode_reserve || T + 1 > h->cfg.max_prompt_tokens) return PERCACHE_E_CAPACITY;
+    if (plan.dec_len[b] >= plan.reserve || T + 1 > h->cfg.max_prompt_tokens) return PERCACHE_E_CAPACITY;
     row_slot[b] = plan.ctx0[b] + T;
     row_pos[b] = T;
     row_pool[b] = -1;                       // decoded tokens are not chunk content: nothing goes to the store
@@ -1922,6 +1921,7 @@ int percache_decode(percache_t* h, int32_t n_prompts, const void* hidden, int32_
     base_tiles.push_back(AttnBaseTile{b, 1, plan.ctx0[b], (T + 1 + 127) / 128});
     visible_pairs += T + 1;
   }
+  plan.tree_n.clear();               // nodes that were not accepted end here
   // One query row per prompt: the attention is a matter of reading every prompt's K and V once, which the
   // weight-streaming style kernel of attn_decode.cu does on the CUDA cores; (prompt, KV head) pairs are cut into
   // chunks of context slots so that a few hundred blocks per SM-full are in flight.

@@ -236,3 +236,29 @@ def test_refusals_change_nothing():
         c.accept(hidden, [[0], [0]], track=True)
         c.check_context()
         c.check_weights()
+
+
+def test_a_refused_step_leaves_the_nodes_to_be_accepted():
+    c = Case(77, [([64], 8, []), ([32], 4, [])], reserve=3, n_layers=1)
+    with c.h:
+        c.accept(c.tree([[-1, 0, 1], [-1]]), [[0, 1, 2], []])          # the first prompt's reserve is used up
+        hidden = c.tree([[], [-1, 0]])
+        with pytest.raises(pcb.PerCacheError) as e:
+            c.h.decode(np.ascontiguousarray(c.tokens(2)))
+        assert e.value.code == pcb.E_CAPACITY
+        c.accept(hidden, [[], [0, 1]])
+        c.check_context()
+
+
+@pytest.mark.parametrize("flags", [0, pcb.FLAG_TRACK_WEIGHTS])
+def test_a_reserve_set_after_the_prefill_holds_from_the_next_one(flags):
+    c = Case(78, [([64], 8, []), ([32], 4, [])], reserve=2, n_layers=1, flags=flags)
+    with c.h:
+        c.h.set_decode_reserve(50)
+        for _ in range(2):
+            c.decode(track=bool(flags))
+        for call, arg in ((c.h.decode, 2), (lambda x: c.h.decode_tree([[-1], []], x), 1)):
+            with pytest.raises(pcb.PerCacheError) as e:
+                call(np.ascontiguousarray(c.tokens(arg)))
+            assert e.value.code == pcb.E_CAPACITY
+        c.check_context()
