@@ -251,7 +251,7 @@ PERCACHE_API int percache_accept(percache_t* h, int32_t n_prompts, const int32_t
  * (sink + recent <= budget) and the ones with the most running attention weight, equal weights going to the lower slot.
  * The weights are those that percache_decode and percache_accept have added while PERCACHE_FLAG_TRACK_WEIGHTS was set,
  * since the prefill (every step first multiplies the sums by the decay of percache_set_weight_decay, 1 at creation);
- * without any such step PERCACHE_E_INVAL.  Positions are not touched: later tokens continue at theirs, and the freed
+ * without any such step, or while a tree's nodes wait for percache_accept, PERCACHE_E_INVAL.  Positions are not touched: later tokens continue at theirs, and the freed
  * slots are free for them (they count towards the decode reserve).  percache_debug_read_ctx and read_weights then see
  * the slots that are left.  Synchronous. */
 PERCACHE_API int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t recent);
@@ -504,7 +504,7 @@ PERCACHE_API int percache_attention_weights(int32_t device, void* stream, const 
  * `budget` of them: the first `sink`, the last `recent` (sink + recent <= budget), and the heaviest of the rest, equal
  * weights going to the lower slot (NaN counts as -infinity).  weights: fp32 [n_seqs][n_heads][weights_stride],
  * weights_stride >= max_len.  keep: int32 [n_seqs][n_heads][budget], ascending, -1 behind the last one;
- * count[b] = min(length[b], budget). */
+ * count[b] = min(length[b], budget).  budget: at most 2^26. */
 PERCACHE_API int percache_select_slots(int32_t device, void* stream, const float* weights, int64_t weights_stride,
                                        const int32_t* length, int32_t n_seqs, int32_t n_heads, int32_t max_len,
                                        int32_t budget, int32_t sink, int32_t recent, int32_t* keep, int32_t* count);

@@ -65,8 +65,12 @@ bool rows_ok(const percache_rows_t* r) {
          (r->n_seqs == 0 || (r->ctx_len && r->row_start)) && (!r->mask || r->mask_words >= (r->max_nodes + 63) / 64);
 }
 
+bool heads_ok(const percache_kv_t* kv, int32_t n_q_heads) {
+  return n_q_heads > 0 && n_q_heads % kv->n_kv_heads == 0 && n_q_heads / kv->n_kv_heads <= 128;
+}
+
 bool q_ok(const percache_kv_t* kv, const void* q, int64_t stride, int32_t n_q_heads, float scale) {
-  return q && aligned(q, 16) && n_q_heads > 0 && n_q_heads % kv->n_kv_heads == 0 && n_q_heads / kv->n_kv_heads <= 128 &&
+  return q && aligned(q, 16) && heads_ok(kv, n_q_heads) &&
          stride >= static_cast<int64_t>(n_q_heads) * kv->head_dim && stride % 8 == 0 && stride <= (INT64_C(1) << 35) &&
          scale > 0.f && std::isfinite(scale);
 }
@@ -130,7 +134,7 @@ int percache_attention_weights(int32_t device, void* stream, const percache_kv_t
   if (!rows_ok(rows)) return PERCACHE_E_INVAL;
   if (rows->n_seqs == 0) return PERCACHE_OK;
   if (!kv_ok(kv, rows->max_len, false) || (rows->n_rows > 0 && (!q_ok(kv, q, q_row_stride, n_q_heads, scale) || !lse)) ||
-      n_q_heads <= 0 || n_q_heads % kv->n_kv_heads != 0 || !weights_out || !(decay >= 0.f) || !std::isfinite(decay) || (decay != 0.f && !weights_in) ||
+      !heads_ok(kv, n_q_heads) || !weights_out || !(decay >= 0.f) || !std::isfinite(decay) || (decay != 0.f && !weights_in) ||
       weights_stride < rows->max_len)
     return PERCACHE_E_INVAL;
   if (!workspace_ok(workspace, workspace_bytes)) return workspace && aligned(workspace, 256) ? PERCACHE_E_CAPACITY : PERCACHE_E_INVAL;
@@ -150,7 +154,7 @@ int percache_select_slots(int32_t device, void* stream, const float* weights, in
                           int32_t sink, int32_t recent, int32_t* keep, int32_t* count) {
   if (n_seqs == 0) return PERCACHE_OK;
   if (!weights || !length || !keep || !count || n_seqs < 0 || n_seqs > 65535 || n_heads <= 0 || n_heads > 65535 || max_len < 1 ||
-      max_len > MAX_CONTEXT || weights_stride < max_len || budget < 1 || sink < 0 || recent < 0 ||
+      max_len > MAX_CONTEXT || weights_stride < max_len || budget < 1 || budget > MAX_CONTEXT || sink < 0 || recent < 0 ||
       static_cast<int64_t>(sink) + recent > budget)
     return PERCACHE_E_INVAL;
   const DeviceGuard dev(device);

@@ -269,7 +269,8 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, u
 __device__ __forceinline__ int tile_place(const KvView& kv, const SeqPart& p, int seq, int blk, int lane) {
   if (!kv.page_table) return ld_dep_s32(kv.ctx_start + seq);
   const int last = (p.ctx_len + max(p.n_nodes, 1) - 1) / PAGE_TOKENS;
-  return ld_dep_s32(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
+  const int page = ld_dep_s32(kv.page_table + static_cast<size_t>(seq) * kv.pt_stride + min(blk * (BLK / PAGE_TOKENS) + (lane & 7), last));
+  return static_cast<int>(min(static_cast<uint32_t>(page), 0x3fffffffu));       // twice that is outside any pool, and does not wrap
 }
 
 // K or V for load_tile.

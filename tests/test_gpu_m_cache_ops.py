@@ -312,6 +312,21 @@ def test_lengths_and_pages_outside_their_bounds_are_clamped_and_harmless():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("page", [-1, -2 ** 31 + 1, -2 ** 31, 2 ** 30 + 1, 2 ** 31 - 1])
+@pytest.mark.parametrize("n", [2, 40])
+def test_a_page_outside_the_pool_reads_as_zeros(page, n):
+    b = Batch([(200, n), (60, 2)], mask="tree", fill=0.0)
+    spare = next(p for p in range(b.k.shape[0] // 16) if not (b.page_table == p).any())       # a page of zeros
+    got = []
+    for p in (spare, page):
+        b.page_table[0, 3] = p
+        b.attend()
+        w = torch.zeros((2, b.hkv, b.max_len), device="cuda")
+        pcb.attention_weights(b.q, b.k, b.lse, w, **b.args())
+        got.append([x.clone() for x in (b.out, b.lse, w)])
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
 def check_weights(b, got, before, use, decay):
     q, lse, got, before = f64(b.q), b.lse.cpu().numpy(), f64(got), f64(before)
     for s, (c, n) in enumerate(b.seqs):

@@ -87,12 +87,14 @@ def test_bad_arguments_of_attention_weights(lib):
                 dict(stride=127), dict(ws=None), dict(hq=9)):
         assert weights(lib, **bad) == pcb.E_INVAL, bad
     assert weights(lib, nbytes=1024) == pcb.E_CAPACITY
+    assert weights(lib, rs=rows(n_rows=0), hq=8 * 129) == pcb.E_INVAL          # also where there is no row to look at
 
 
 def test_bad_arguments_of_select_and_compact(lib):
     for bad in (dict(w=None), dict(stride=100), dict(length=None), dict(n=-1), dict(heads=0), dict(max_len=0), dict(budget=0),
                 dict(sink=-1), dict(recent=-1), dict(sink=9), dict(keep=None), dict(count=None), dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1)):
         assert select(lib, **bad) == pcb.E_INVAL, bad
+    assert select(lib, budget=(1 << 26) + 1) == pcb.E_INVAL
     for bad in (dict(keep=None), dict(count=None), dict(heads=2), dict(budget=0), dict(dst=A), dict(dpt=A, dst=A), dict(dpt=A, dpt_stride=0),
                 dict(w_in=A), dict(w_out=A), dict(w_in=A, w_out=A, stride=127), dict(max_len=0), dict(n=-1),
                 dict(kvs=kv(page_table=None, ctx_start=A), dpt=A, dpt_stride=8)):
