@@ -1,4 +1,4 @@
-"""Builds libpercache.so (the C-ABI library) in-tree with nvcc for sm_100a.
+"""Builds libpercache.so (the C-ABI library) in-tree with nvcc for sm_100a, and the compiled part of the Python binding.
 
     python -m paper_2601_11553_b200.build [--force]
 
@@ -9,12 +9,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libpercache.so")
+BINDING_PATH = os.path.join(HERE, "_ops_binding" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["percache_api.cu", "kernels_mem.cu", "kernels_ref.cu", "gemm_umma.cu", "gemm_small.cu", "attn_umma.cu", "attn_decode.cu", "attn_plan.cu", "attn_tree.cu", "attn_narrow.cu", "attn_weights.cu", "slots.cu", "ops_api.cu", "gemm_noalloc.cu", "qa_bank.cu", "wait_probe.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
@@ -35,7 +37,7 @@ def _deps_mtime() -> float:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and os.path.exists(LIB_PATH) and os.path.getmtime(LIB_PATH) >= _deps_mtime():
+    if not force and all(os.path.exists(p) and os.path.getmtime(p) >= _deps_mtime() for p in (LIB_PATH, BINDING_PATH)):
         return LIB_PATH
     os.makedirs(OBJ_DIR, exist_ok=True)
     nvcc = _nvcc()
@@ -52,8 +54,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    def compile_binding() -> None:
+        tmp = BINDING_PATH + ".tmp"
+        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
+               "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "ops_binding.cpp"), "-o", tmp]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"{cmd[0]} failed for ops_binding.cpp:\n{r.stdout}\n{r.stderr}")
+        os.replace(tmp, BINDING_PATH)
+
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(compile_binding)
         objs = list(ex.map(compile_one, SOURCES))
+        binding.result()
     tmp = LIB_PATH + ".tmp"
     r = subprocess.run([nvcc, "-shared", "-o", tmp, *objs, "-cudart", "static"], capture_output=True, text=True)
     if r.returncode != 0:

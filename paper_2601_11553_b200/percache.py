@@ -13,7 +13,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct as _struct
 from dataclasses import dataclass
 from typing import Any, Dict, List, Optional, Sequence
 
@@ -523,85 +522,24 @@ OPS_WORKSPACE_BYTES = 24 << 20
 MAX_TREE_NODES = 256
 
 
-class _Types:
-    """torch's types, looked up once (this module does not need torch for anything else)."""
-
-    def __init__(self):
-        import torch
-        self.i32, self.f32, self.u8 = (torch.int32,), (torch.float32,), (torch.uint8,)
-        self.flag, self.word = (torch.uint8, torch.bool), (torch.int64, torch.uint64)
-        self.pool = {torch.bfloat16: 0, torch.float16: 1}
+_binding = None
 
 
-_types: Optional[_Types] = None
-_pack_kv = _struct.Struct("@PPqqqPPiiii").pack
-_pack_rows = _struct.Struct("@iiiiPPPii").pack
-
-
-def _t() -> _Types:
-    global _types
-    if _types is None:
-        _types = _Types()
-    return _types
-
-
-def _arg(x: Any, name: str, dtypes: Any, device: int, shape: Any = None) -> int:
-    """Address of a contiguous tensor of one of the types on the device, with this shape (None: any)."""
-    if x.dtype in dtypes and x.get_device() == device and x.is_contiguous() and (shape is None or x.shape == shape):
-        return x.data_ptr()
-    raise ValueError(f"{name}: expected a contiguous tensor of {' or '.join(map(str, dtypes))} on cuda:{device}"
-                     f"{'' if shape is None else f' of shape {tuple(shape)}'}, got {x.dtype} {tuple(x.shape)} on {x.device}")
-
-
-def _table(x: Any, name: str, dtypes: Any, device: int, n: int) -> int:
-    """The same for an [n, any] tensor."""
-    if len(x.shape) != 2 or x.shape[0] != n:
-        raise ValueError(f"{name}: expected shape ({n}, any), got {tuple(x.shape)}")
-    return _arg(x, name, dtypes, device)
-
-
-def _row_stride(x: Any, name: str, heads: int, head_dim: int) -> int:
-    """Elements between the rows of a [rows, heads, head_dim] tensor whose heads and elements lie one behind the other."""
-    shape, st = x.shape, x.stride()
-    if len(st) != 3 or shape[1] != heads or shape[2] != head_dim or st[2] != 1 or (heads > 1 and st[1] != head_dim):
-        raise ValueError(f"{name}: expected [rows, {heads}, {head_dim}] with dense heads")
-    return st[0] if shape[0] > 1 else heads * head_dim
-
-
-def _kv(k: Any, v: Any, page_table: Any, ctx_start: Any, n_seqs: int) -> KvStruct:
-    dev = k.get_device()
-    if len(k.shape) != 3 or dev < 0:
-        raise ValueError("k: expected a [slots, kv_heads, head_dim] tensor on a CUDA device")
-    ty = _t()
-    kind = ty.pool.get(k.dtype)
-    if kind is None:
-        raise ValueError(f"k: expected bfloat16 or float16, got {k.dtype}")
-    slots, heads, dim = k.shape
-    ks, vs, vp = _row_stride(k, "k", heads, dim), 0, 0
-    if v is not None:
-        if v.dtype != k.dtype or v.get_device() != dev or v.shape[0] != slots:
-            raise ValueError("v: expected k's type, device and number of slots")
-        vs, vp = _row_stride(v, "v", heads, dim), v.data_ptr()
-    if (page_table is None) == (ctx_start is None):
-        raise ValueError("give either page_table or ctx_start")
-    if page_table is not None:
-        pt, width, cs = _table(page_table, "page_table", ty.i32, dev, n_seqs), page_table.shape[1], 0
-    else:
-        pt, width, cs = 0, 0, _arg(ctx_start, "ctx_start", ty.i32, dev, (n_seqs,))
-    return KvStruct.from_buffer_copy(_pack_kv(k.data_ptr(), vp, ks, vs, slots, pt, cs, width, heads, dim, kind))
-
-
-def _rows(q: Any, k: Any, ctx_len: Any, row_start: Any, mask: Any, max_nodes: int, max_len: int) -> RowsStruct:
-    dev = k.get_device()
-    if q.dtype != k.dtype or q.get_device() != dev or len(q.shape) != 3:
-        raise ValueError("q: expected [rows, q_heads, head_dim] of k's type on k's device")
-    n_seqs, n_rows, ty = ctx_len.shape[0], q.shape[0], _t()
-    m, words = 0, 0
-    if mask is not None:
-        m, words = _table(mask, "mask", ty.word, dev, n_rows), mask.shape[1]
-    return RowsStruct.from_buffer_copy(_pack_rows(
-        n_seqs, n_rows, max_nodes, max_len, _arg(ctx_len, "ctx_len", ty.i32, dev, (n_seqs,)),
-        _arg(row_start, "row_start", ty.i32, dev, (n_seqs + 1,)), m, words, 0))
+def _ops() -> Any:
+    """The compiled checks and calls (csrc/ops_binding.cpp), bound to the loaded library."""
+    global _binding
+    if _binding is None:
+        import torch                 # this module does not need it for anything else
+        lib = load_library()
+        try:
+            from . import _ops_binding as m
+        except ImportError as e:
+            raise PerCacheError(E_CUDA, f"{e} (build it: python -m paper_2601_11553_b200.build)") from e
+        m.bind(tuple(C.cast(f, C.c_void_p).value for f in (lib.percache_tree_attention, lib.percache_attention_weights,
+                                                           lib.percache_select_slots, lib.percache_compact_slots)),
+               (torch.int32, torch.float32, torch.uint8, torch.bool, torch.int64, torch.uint64, torch.bfloat16, torch.float16))
+        _binding = m
+    return _binding
 
 
 def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len: Any, row_start: Any, max_nodes: int,
@@ -613,17 +551,8 @@ def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len
     [rows, q_heads] or None; mask: int64 words [rows, ceil(max_nodes / 64)] or None (node i sees nodes 0 .. i); workspace:
     uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` (a cudaStream_t; 0 is the legacy default stream, not
     torch's current one) and returns `out`."""
-    kv = _kv(k, v, page_table, ctx_start, ctx_len.shape[0])
-    rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
-    dev, ty = k.get_device(), _t()
-    n_rows, hq, d = q.shape
-    if out.dtype != q.dtype or out.get_device() != dev or out.shape[0] != n_rows:
-        raise ValueError("out: expected q's type, device and shape")
-    qs, os_ = _row_stride(q, "q", hq, k.shape[2]), _row_stride(out, "out", hq, k.shape[2])
-    rc = load_library().percache_tree_attention(
-        dev, stream, kv, rows, q.data_ptr(), qs, hq, d ** -0.5 if scale is None else scale, out.data_ptr(), os_,
-        0 if lse is None else _arg(lse, "lse", ty.f32, dev, (n_rows, hq)), _arg(workspace, "workspace", ty.u8, dev), workspace.numel())
-    _check(rc, "percache_tree_attention")
+    _check(_ops().tree_attention(q, k, v, out, lse, ctx_len, row_start, max_nodes, max_len, workspace, mask, page_table, ctx_start,
+                                 scale, stream), "percache_tree_attention")
     return out
 
 
@@ -634,20 +563,9 @@ def attention_weights(q: Any, k: Any, lse: Any, weights: Any, weights_out: Any =
     """percache_attention_weights: weights_out = decay * weights + the softmax weights of the rows with use != 0, summed
     per slot over the rows and the query heads of a KV head.  weights: fp32 [seqs, kv_heads, slots]; weights_out None: in
     place.  Enqueues on `stream` and returns weights_out."""
-    n_seqs = ctx_len.shape[0]
-    kv = _kv(k, None, page_table, ctx_start, n_seqs)
-    rows = _rows(q, k, ctx_len, row_start, mask, max_nodes, max_len)
-    dev, ty = k.get_device(), _t()
-    n_rows, hq, d = q.shape
     weights_out = weights if weights_out is None else weights_out
-    heads, width = k.shape[1], weights_out.shape[2]
-    rc = load_library().percache_attention_weights(
-        dev, stream, kv, rows, q.data_ptr(), _row_stride(q, "q", hq, k.shape[2]), hq, d ** -0.5 if scale is None else scale,
-        _arg(lse, "lse", ty.f32, dev, (n_rows, hq)), 0 if use is None else _arg(use, "use", ty.flag, dev, (n_rows,)), decay,
-        0 if weights is None else _arg(weights, "weights", ty.f32, dev, (n_seqs, heads, width)),
-        _arg(weights_out, "weights_out", ty.f32, dev, (n_seqs, heads, width)), width,
-        _arg(workspace, "workspace", ty.u8, dev), workspace.numel())
-    _check(rc, "percache_attention_weights")
+    _check(_ops().attention_weights(q, k, lse, weights, weights_out, ctx_len, row_start, max_nodes, max_len, workspace, mask, use,
+                                    page_table, ctx_start, scale, decay, stream), "percache_attention_weights")
     return weights_out
 
 
@@ -655,13 +573,7 @@ def select_slots(weights: Any, length: Any, keep: Any, count: Any, *, sink: int 
                  max_len: Optional[int] = None, stream: int = 0) -> Any:
     """percache_select_slots: keep [seqs, heads, budget] (int32, ascending, -1 behind the last) and count [seqs] of the
     slots that stay: the first `sink`, the last `recent`, and the heaviest of the rest."""
-    n_seqs, heads, width = weights.shape
-    dev, ty = weights.get_device(), _t()
-    rc = load_library().percache_select_slots(
-        dev, stream, _arg(weights, "weights", ty.f32, dev), width, _arg(length, "length", ty.i32, dev, (n_seqs,)),
-        n_seqs, heads, width if max_len is None else max_len, keep.shape[2], sink, recent,
-        _arg(keep, "keep", ty.i32, dev, (n_seqs, heads, keep.shape[2])), _arg(count, "count", ty.i32, dev, (n_seqs,)))
-    _check(rc, "percache_select_slots")
+    _check(_ops().select_slots(weights, length, keep, count, sink, recent, max_len, stream), "percache_select_slots")
     return keep, count
 
 
@@ -671,23 +583,9 @@ def compact_slots(k: Any, v: Any, keep: Any, count: Any, *, max_len: int, weight
     """percache_compact_slots: slot first[b] + j of the destination takes the K, V and weight of slot keep[b][head][j].
     Without dst_page_table / dst_start in place (keep strictly ascending, keep[j] >= first + j); weights_out None: the
     weights in place."""
-    n_seqs = count.shape[0]
-    kv = _kv(k, v, page_table, ctx_start, n_seqs)
-    dev, ty = k.get_device(), _t()
     weights_out = weights if weights_out is None else weights_out
-    heads, width = k.shape[1], 0 if weights is None else weights.shape[2]
-    shape, keep_heads, budget = (n_seqs, heads, width), keep.shape[1], keep.shape[2]
-    rc = load_library().percache_compact_slots(
-        dev, stream, kv, n_seqs, max_len,
-        0 if dst_page_table is None else _table(dst_page_table, "dst_page_table", ty.i32, dev, n_seqs),
-        0 if dst_page_table is None else dst_page_table.shape[1],
-        0 if dst_start is None else _arg(dst_start, "dst_start", ty.i32, dev, (n_seqs,)),
-        0 if first is None else _arg(first, "first", ty.i32, dev, (n_seqs,)),
-        _arg(keep, "keep", ty.i32, dev, (n_seqs, keep_heads, budget)), keep_heads, budget,
-        _arg(count, "count", ty.i32, dev, (n_seqs,)),
-        0 if weights is None else _arg(weights, "weights", ty.f32, dev, shape),
-        0 if weights is None else _arg(weights_out, "weights_out", ty.f32, dev, shape), width)
-    _check(rc, "percache_compact_slots")
+    _check(_ops().compact_slots(k, v, keep, count, max_len, weights, weights_out, first, page_table, ctx_start, dst_page_table,
+                                dst_start, stream), "percache_compact_slots")
 
 
 def ops_status(workspace: Any, stream: int = 0) -> None:

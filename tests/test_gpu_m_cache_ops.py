@@ -499,6 +499,53 @@ def test_pools_smaller_than_a_block_and_a_single_row():
     check_weights(b, w, torch.zeros_like(w), None, 1.0)
 
 
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    b = Batch([(300, 3), (5, 1)], mask="tree")
+    good = dict(b.args())
+
+    def refused(match, q=b.q, k=b.k, v=b.v, out=b.out, lse=b.lse, **kw):
+        with pytest.raises(ValueError, match=match):
+            pcb.tree_attention(q, k, v, out, lse, **{**good, **kw})
+
+    refused("lse", lse=b.lse.double())
+    refused("lse", lse=b.lse[:-1])
+    refused("lse", lse=b.lse.cpu())
+    refused("lse", lse=torch.zeros((b.hq, b.n_rows), device="cuda").t())
+    refused("out", out=b.out[:-1])
+    refused("out", out=b.out.float())
+    refused("q:", q=b.q.to(torch.float16))
+    refused("q:", q=b.q.transpose(0, 1))
+    refused("q:", q=torch.zeros((b.n_rows, b.hq, 64), dtype=torch.bfloat16, device="cuda"))
+    refused("k:", k=b.k.float())
+    refused("v:", v=b.v[:-16])
+    refused("v:", v=b.v.to(torch.float16))
+    refused("ctx_len", ctx_len=b.ctx_len.long())
+    refused("row_start", row_start=b.row_start_d[:-1])
+    refused("mask", mask=b.mask.int())
+    refused("mask", mask=b.mask[:-1])
+    refused("page_table", page_table=b.page_table[:1])
+    refused("page_table", page_table=None)
+    refused("page_table", ctx_start=b.ctx_len)
+    refused("workspace", workspace=b.ws.int())
+    w = torch.zeros((2, b.hkv, b.max_len), device="cuda")
+    keep, count = torch.zeros((2, b.hkv, 8), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for match, call in (("weights_out", lambda: pcb.attention_weights(b.q, b.k, b.lse, w, w[:, :1], **good)),
+                        ("use", lambda: pcb.attention_weights(b.q, b.k, b.lse, w, use=torch.zeros(1, dtype=torch.uint8, device="cuda"), **good)),
+                        ("keep", lambda: pcb.select_slots(w, count, keep[:, :1], count)),
+                        ("length", lambda: pcb.select_slots(w, count[:1], keep, count)),
+                        ("count", lambda: pcb.select_slots(w, count, keep, count.float())),
+                        ("keep", lambda: pcb.compact_slots(b.k, b.v, keep[:1], count, max_len=b.max_len, page_table=b.page_table)),
+                        ("first", lambda: pcb.compact_slots(b.k, b.v, keep, count, max_len=b.max_len, page_table=b.page_table, first=count[:1]))):
+        with pytest.raises(ValueError, match=match):
+            call()
+    with pytest.raises(TypeError):
+        pcb.select_slots(w, count, keep, count, sink="1")
+    with pytest.raises(ValueError):
+        pcb.select_slots(w, count, keep, count, sink=2 ** 40)
+    with pytest.raises(pcb.PerCacheError):
+        pcb.select_slots(w, count, keep, count, sink=5, recent=4)
+
+
 def test_a_batch_without_rows_only_decays_its_weights():
     b = Batch([(300, 0), (5, 0)], pad_rows=0)
     assert b.q.shape[0] == 0
