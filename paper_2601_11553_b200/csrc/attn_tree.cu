@@ -31,9 +31,9 @@
 namespace pc {
 namespace {
 
-constexpr int RING_BYTES = 160 * 1024;
+constexpr int RING_BYTES = 128 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
-constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
+constexpr int TREE_SMEM = RING_BYTES + 2 * Q_BYTES + 1024;
 constexpr uint32_t TMEM_S = 256;
 constexpr int WHOLE_BLOCKS = 6;
 
@@ -48,23 +48,23 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   constexpr int STAGES = RING_BYTES / TILE_BYTES;
   static_assert(STAGES <= MAX_STAGES, "");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t q_full, q_empty, full[MAX_STAGES], empty[MAX_STAGES], raw[MAX_STAGES], s_full[2], p_full[2], o_full, o_free, ml_full;
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], raw[MAX_STAGES], s_full[2], p_full[2], o_full, o_free, ml_full;
   __shared__ float ml[2][2][BLK][2];                     // [item parity][block parity][row]: reference, sum
   __shared__ int bad_v[FLAGS][2];
   __shared__ Span shared_span;
+  __shared__ Cursor walks[8];
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
   __shared__ uint32_t tmem_slot;
   __shared__ int cta_failed;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = q_smem + Q_BYTES;
+  uint8_t* ring = q_smem + 2 * Q_BYTES;
 
   if (threadIdx.x == 0) {
     cta_failed = 0;
-    mbar_init(&q_full, 1); mbar_init(&q_empty, 1);
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 1); mbar_init(&raw[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
     mbar_init(&o_full, 1); mbar_init(&o_free, 8); mbar_init(&ml_full, 8);
     fence_mbar_init();
   }
@@ -80,15 +80,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
   const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   const uint32_t tmem = tmem_slot;
-  const Pipe pipe{q_smem, 0, HALF_BYTES, ring, &q_full, &q_empty, full, empty, raw, &bad_v[0][0], nullptr};
+  const Pipe pipe{q_smem, Q_BYTES, HALF_BYTES, ring, q_full, q_empty, full, empty, raw, &bad_v[0][0], nullptr};
   // 384 threads start with 168 registers each (64 512); the softmax holds a whole row of scores and wants more, the other
-  // warpgroup needs few: 256 x 208 + 128 x 80 = 63 488
+  // warpgroup needs few: 256 x 216 + 128 x 72 = 64 512
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     Cursor cur(span);
     Item it{};
    if (warp == 8) {
-    copy_role<D, STAGES, 1, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
+    copy_role<D, STAGES, 2, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
    } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
     {     // the whole warp walks; one lane issues
@@ -99,11 +99,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
       };
-      const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
       const TileLayout<D> tl(a.kv.page_table != nullptr);
       while (ok && next_item(cur, a, &it)) {
-        const int nb = it.blk_end - it.blk_begin;
-        wait(&q_full, n_item & 1u);
+        const int nb = it.blk_end - it.blk_begin, qs = n_item & 1;
+        const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_BYTES), 16, 1024);
+        wait(&q_full[qs], (n_item >> 1) & 1u);
 #pragma unroll 1
         for (int x = 0; x < 2 * nb; ++x) {
           const Step sp = step_of(x, nb);
@@ -129,7 +129,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             }
             umma_commit(&s_full[i]);
             umma_commit(&empty[st]);
-            if (sp.j + 1 == nb) umma_commit(&q_empty);
+            if (sp.j + 1 == nb) umma_commit(&q_empty[qs]);
           } else {
             const uint64_t v_desc = make_smem_desc_sw128(tile, tl.mn_lbo, tl.group);
 #pragma unroll
@@ -149,8 +149,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     clean_role<D, STAGES, BF16, false, false>(a, pipe, cur, &cta_failed);
    }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    Cursor cur(span);
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    // where the walk stands waits in shared memory between pieces: the rows' scores want every register
+    if (lane == 0) walks[warp] = Cursor(span);
+    __syncwarp();
+    auto next = [&](Item* item) {
+      Cursor cur = walks[warp];
+      const bool more = next_item(cur, a, item);
+      __syncwarp();
+      if (lane == 0) walks[warp] = cur;
+      __syncwarp();
+      return more;
+    };
     Item it{};
     // ------------------------------------------------------------ softmax (warps 0-7)
     const int i = warp >> 2, quarter = warp & 3;
@@ -160,7 +170,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     uint32_t n_item = 0, n_s = 0;
     bool ok = true;
     const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2);
-    while (ok && next_item(cur, a, &it)) {
+    while (ok && next(&it)) {
       const int nb = it.blk_end - it.blk_begin;
       const bool live = quarter * 32 < it.n_rows;          // warps without rows only keep the barriers' count
       const bool valid = r < it.n_rows;
@@ -168,6 +178,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
       const int row = it.row0 + node_in_tile, node = it.node0 + node_in_tile;
       float m = -INFINITY, l = 0.f;
       for (int j = i; j < nb; j += 2) {
+        // what the row sees of a block with drafted slots is looked up before its scores take the registers
+        const int slot0 = (it.blk_begin + j) * BLK;
+        const bool tail = slot0 + BLK > it.ctx_len;
+        uint32_t bits[4] = {~0u, ~0u, ~0u, ~0u};
+        if (tail) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) bits[c] = slot_bits(a.rows, it, row, node, slot0 + c * 32);
+          __syncwarp();
+        }
         ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
         if (!ok) break;
         ++n_s;
@@ -177,16 +196,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld_32x32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
           tmem_wait_ld();
-          const int slot0 = (it.blk_begin + j) * BLK;
-          if (slot0 + BLK > it.ctx_len) {
+          if (tail) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const uint32_t bits = slot_bits(a.rows, it, row, node, slot0 + c * 32);
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (!((bits >> e) & 1u)) s[c * 32 + e] = 0xff800000u;       // -inf
+                if (!((bits[c] >> e) & 1u)) s[c * 32 + e] = 0xff800000u;       // -inf
             }
-            __syncwarp();
           }
           float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
@@ -206,13 +222,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
               float alpha = 1.0f;
               if (need) { alpha = fast_exp2(m - m_blk); m = m_blk; l *= alpha; }
 #pragma unroll 1
-              for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                tmem_ld_32x32(t_o + i * HEAD_DIM + c * 32, o);
+              for (int c = 0; c < D / 16; ++c) {
+                uint32_t o[16];
+                tmem_ld_32x16(t_o + i * HEAD_DIM + c * 16, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                tmem_st_32x32(t_o + i * HEAD_DIM + c * 32, o);
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_st_32x16(t_o + i * HEAD_DIM + c * 16, o);
               }
               tmem_wait_st();
             }
@@ -221,12 +237,12 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
           const uint64_t neg2 = pack_f32x2(neg, neg);
           uint64_t sum_a = pack_f32x2(0.f, 0.f), sum_b = sum_a;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {                     // 64 columns at a time: the packed words leave before the next are formed
-            uint32_t p[32];
+          for (int h = 0; h < 4; ++h) {                     // 32 columns at a time: the packed words leave before the next are formed
+            uint32_t p[16];
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
+            for (int c = 0; c < 16; ++c) {
               float x0, x1;
-              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[h * 64 + 2 * c]), __uint_as_float(s[h * 64 + 2 * c + 1])), scale2, neg2), x0, x1);
+              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[h * 32 + 2 * c]), __uint_as_float(s[h * 32 + 2 * c + 1])), scale2, neg2), x0, x1);
               const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
               if (c & 1) sum_b = add_f32x2(sum_b, pack_f32x2(p0, p1));
               else sum_a = add_f32x2(sum_a, pack_f32x2(p0, p1));
@@ -238,7 +254,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
                 p[c] = *reinterpret_cast<uint32_t*>(&v);
               }
             }
-            tmem_st_32x32(t_s + h * 32, p);
+            tmem_st_32x16(t_s + h * 16, p);
           }
           float s0, s1;
           unpack_f32x2(add_f32x2(sum_a, sum_b), s0, s1);

@@ -145,7 +145,7 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
         ++n_tile;
         if (elect_one()) mbar_arrive_expect_tx(&full[st], TILE_BYTES);
         __syncwarp();
-        load_tile<D>(ring + st * TILE_BYTES, &tmK, &full[st], a.kv.page_table != nullptr, where, pc.unit, blk, lane);
+        load_tile<D>(ring + st * TILE_BYTES, &tmK, &full[st], a.kv.page_table != nullptr, where, pc.unit, blk);
         for (int t = 0; t < tiles && tiles > 1 && ok; ++t) load_q(t);
       }
     }

@@ -161,7 +161,7 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
         if (!clean) mbar_arrive(bar);
       }
       __syncwarp();
-      load_tile<D>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g, blk, lane);
+      load_tile<D>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g, blk);
     }
     if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
       rec.n_parts = last_cta(span, it.unit_end) - static_cast<int>(blockIdx.x) + 1;

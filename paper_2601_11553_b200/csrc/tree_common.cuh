@@ -196,6 +196,7 @@ struct Cursor {
   int pos, end, seq_start;
   int seq;
   SeqPart part;                  // of prompt `seq`
+  Cursor() = default;
   __device__ __forceinline__ explicit Cursor(const Span& s)
       : pos(0), end(static_cast<int>(s.end - s.begin)), seq_start(static_cast<int>(s.seq_start - s.begin)), seq(s.seq), part(s.part) {}
   template <typename ShapeFn>
@@ -253,13 +254,19 @@ struct TileLayout {
       : half(paged ? 1024 : BLK * 128), group(paged ? D / 64 * 1024 : 1024), mn_lbo(D == 128 ? half : 0) {}
   __device__ __forceinline__ int row(int r, int h) const { return (r >> 3) * group + h * half + (r & 7) * 128; }
 };
-// Called by a whole warp.  With pages lanes 0-7 copy one page each; `where` then is the lane's page id, else the pool row of the
-// prompt's slot 0.
+// Called by a whole warp.  With pages, `where` of lanes 0-7 is a page id each, else the pool row of the prompt's slot 0.  One lane issues
+// all eight copies: a copy's operands are per-warp registers, so eight lanes with one each take turns anyway, and slower (48-node
+// trees on 64 x 2500 slots 157 -> 140 us, weights of 64 tokens 67.8 -> 62.6 us).
 template <int D>
-__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, bool paged, int where, int head, int blk,
-                                          int lane) {
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, bool paged, int where, int head, int blk) {
   if (paged) {
-    if (lane < 8) tma_load_4d(dst + lane * (PAGE_TOKENS * D * 2), tm, bar, 0, 0, head * (D / 64), where * 2);
+    int page[BLK / PAGE_TOKENS];
+#pragma unroll
+    for (int p = 0; p < BLK / PAGE_TOKENS; ++p) page[p] = __shfl_sync(0xffffffffu, where, p);
+    if (elect_one()) {
+#pragma unroll
+      for (int p = 0; p < BLK / PAGE_TOKENS; ++p) tma_load_4d(dst + p * (PAGE_TOKENS * D * 2), tm, bar, 0, 0, head * (D / 64), page[p] * 2);
+    }
   } else if (elect_one()) {
 #pragma unroll
     for (int h = 0; h < D / 64; ++h) tma_load_2d(dst + h * (BLK * 128), tm, bar, head * D + h * 64, where + blk * BLK);
