@@ -141,61 +141,67 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     clean_role<D, STAGES, BF16, true, true>(a, pipe, cur, &cta_failed);
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
-    {     // the whole warp walks; one lane issues
-      constexpr uint32_t idesc_s = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 0, 0);
-      constexpr uint32_t idesc_o = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 1, 0);       // A = V^T: V's rows are the K index
-      const TileLayout<D> tl(a.kv.page_table != nullptr);
-      uint32_t n_item = 0, n_tile = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
-      bool ok = true;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
-      };
-      while (ok && next_item(cur, a, &it)) {
-        const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
-        const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + par * Q_SLOT), 16, 1024);
-        wait(&q_full[par], (n_item >> 1) & 1u);
+    // the whole warp walks; one lane issues
+    constexpr uint32_t idesc_s = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 0, 0);
+    constexpr uint32_t idesc_o = make_idesc_f16(BLK, NC, BF16 ? 1 : 0, 1, 0);       // A = V^T: V's rows are the K index
+    const TileLayout<D> tl(a.kv.page_table != nullptr);
+    uint32_t n_item = 0, st = 0, st_phase = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
+    };
+    auto advance = [&] {
+      if (++st == STAGES) { st = 0; st_phase ^= 1u; }
+    };
+    while (ok && next_item(cur, a, &it)) {
+      const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
+      const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + par * Q_SLOT), 16, 1024);
+      wait(&q_full[par], (n_item >> 1) & 1u);
 #pragma unroll 1
-        for (int x = 0; x < 2 * nb; ++x) {
-          const Step sp = step_of(x, nb);
-          const int i = sp.j & 1, st = n_tile % STAGES;
-          if (!sp.is_k) {
-            wait(&p_full[i], (p_phase >> i) & 1u);
-            p_phase ^= 1u << i;
-            if (sp.j == 0) wait(&o_free[par], ((n_item >> 1) & 1u) ^ 1u);
-          }
-          wait(&full[st], (n_tile / STAGES) & 1u);
-          ++n_tile;
+      for (int j = -2; j < nb && ok; ++j) {                // K0 K1 V0 K2 V1 ...
+        const int i = j & 1;
+        if (j >= 0) {
+          wait(&p_full[i], (p_phase >> i) & 1u);
+          p_phase ^= 1u << i;
+          if (j == 0) wait(&o_free[par], ((n_item >> 1) & 1u) ^ 1u);
+          wait(&full[st], st_phase);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
           if (elect_one()) {
-          if (sp.is_k) {
-            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, tl.group);
+            // head size 64 has one 64-element column block: the second 64 TMEM lanes repeat the first (distance 0) and are not read
+            const uint64_t v_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), tl.mn_lbo, tl.group);
+            const uint64_t p_desc = make_smem_desc_sw128(smem_u32(p_smem + i * P_BYTES), 16, 1024);
+#pragma unroll
+            for (int kk = 0; kk < BLK / 16; ++kk)
+              umma_ss(tmem + TMEM_O + (par * 2 + i) * NC, v_desc + (kk * 2 * tl.group >> 4),
+                      p_desc + (((kk >> 2) * P_HALF + (kk & 3) * 32) >> 4), idesc_o, j > 1 || kk != 0);
+            umma_commit(&empty[st]);
+            if (j + 1 == nb) umma_commit(&o_full[par]);
+          }
+          __syncwarp();
+          advance();
+        }
+        if (j + 2 < nb) {
+          wait(&full[st], st_phase);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (elect_one()) {
+            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
               umma_ss(tmem + i * NC, k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
                       q_desc + (((kk >> 2) * Q_HALF + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
             umma_commit(&s_full[i]);
             umma_commit(&empty[st]);
-            if (sp.j + 1 == nb) umma_commit(&q_empty[par]);
-          } else {
-            // head size 64 has one 64-element column block: the second 64 TMEM lanes repeat the first (distance 0) and are not read
-            const uint64_t v_desc = make_smem_desc_sw128(tile, tl.mn_lbo, tl.group);
-            const uint64_t p_desc = make_smem_desc_sw128(smem_u32(p_smem + i * P_BYTES), 16, 1024);
-#pragma unroll
-            for (int kk = 0; kk < BLK / 16; ++kk)
-              umma_ss(tmem + TMEM_O + (par * 2 + i) * NC, v_desc + (kk * 2 * tl.group >> 4), p_desc + (((kk >> 2) * P_HALF + (kk & 3) * 32) >> 4), idesc_o,
-                      sp.j > 1 || kk != 0);
-            umma_commit(&empty[st]);
-            if (sp.j + 1 == nb) umma_commit(&o_full[par]);
-          }
+            if (j + 3 == nb) umma_commit(&q_empty[par]);
           }
           __syncwarp();
+          advance();
         }
-        ++n_item;
       }
-      if (!ok) cta_failed = 1;
+      ++n_item;
     }
+    if (!ok) cta_failed = 1;
   } else {
     // ------------------------------------------------------------ softmax (warps 0-7).  The four warps of a parity meet at a hardware
     // barrier in every block, so a warp whose wait ran out keeps walking the blocks, without waiting or computing, to the end.

@@ -33,7 +33,7 @@ namespace {
 
 constexpr int RING_BYTES = 128 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
-constexpr int TREE_SMEM = RING_BYTES + 2 * Q_BYTES + 1024;
+constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
 constexpr uint32_t TMEM_S = 256;
 constexpr int WHOLE_BLOCKS = 6;
 
@@ -48,7 +48,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   constexpr int STAGES = RING_BYTES / TILE_BYTES;
   static_assert(STAGES <= MAX_STAGES, "");
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], raw[MAX_STAGES], s_full[2], p_full[2], o_full, o_free, ml_full;
+  __shared__ __align__(8) uint64_t q_full, q_empty, full[MAX_STAGES], empty[MAX_STAGES], raw[MAX_STAGES], s_full[2], p_full[2], o_full, o_free, ml_full;
   __shared__ float ml[2][2][BLK][2];                     // [item parity][block parity][row]: reference, sum
   __shared__ int bad_v[FLAGS][2];
   __shared__ Span shared_span;
@@ -59,12 +59,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* q_smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = q_smem + 2 * Q_BYTES;
+  uint8_t* ring = q_smem + Q_BYTES;
 
   if (threadIdx.x == 0) {
     cta_failed = 0;
+    mbar_init(&q_full, 1); mbar_init(&q_empty, 1);
     for (int i = 0; i < STAGES; ++i) { mbar_init(&full[i], 2); mbar_init(&empty[i], 1); mbar_init(&raw[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4); }
     mbar_init(&o_full, 1); mbar_init(&o_free, 8); mbar_init(&ml_full, 8);
     fence_mbar_init();
   }
@@ -80,7 +81,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
   pdl_wait();                          // lengths, tables, Q, K and V may come from the kernel before
   const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return tree_shape(a, p); });
   const uint32_t tmem = tmem_slot;
-  const Pipe pipe{q_smem, Q_BYTES, HALF_BYTES, ring, q_full, q_empty, full, empty, raw, &bad_v[0][0], nullptr};
+  const Pipe pipe{q_smem, Q_BYTES, HALF_BYTES, ring, &q_full, &q_empty, full, empty, raw, &bad_v[0][0], nullptr};
   // 384 threads start with 168 registers each (64 512); the softmax holds a whole row of scores and wants more, the other
   // warpgroup needs few: 256 x 216 + 128 x 72 = 64 512
   if (warp >= 8) {
@@ -88,63 +89,67 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     Cursor cur(span);
     Item it{};
    if (warp == 8) {
-    copy_role<D, STAGES, 2, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
+    copy_role<D, STAGES, 1, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
    } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
-    {     // the whole warp walks; one lane issues
-      constexpr uint32_t idesc_qk = make_idesc_f16(BLK, BLK, BF16 ? 1 : 0, 0, 0);
-      constexpr uint32_t idesc_pv = make_idesc_f16(BLK, D, BF16 ? 1 : 0, 0, 1);
-      uint32_t n_item = 0, n_tile = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
-      bool ok = true;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
-      };
-      const TileLayout<D> tl(a.kv.page_table != nullptr);
-      while (ok && next_item(cur, a, &it)) {
-        const int nb = it.blk_end - it.blk_begin, qs = n_item & 1;
-        const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_BYTES), 16, 1024);
-        wait(&q_full[qs], (n_item >> 1) & 1u);
+    // the whole warp walks; one lane issues
+    constexpr uint32_t idesc_qk = make_idesc_f16(BLK, BLK, BF16 ? 1 : 0, 0, 0);
+    constexpr uint32_t idesc_pv = make_idesc_f16(BLK, D, BF16 ? 1 : 0, 0, 1);
+    uint32_t n_item = 0, st = 0, st_phase = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
+    };
+    auto advance = [&] {
+      if (++st == STAGES) { st = 0; st_phase ^= 1u; }
+    };
+    const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
+    const TileLayout<D> tl(a.kv.page_table != nullptr);
+    while (ok && next_item(cur, a, &it)) {
+      const int nb = it.blk_end - it.blk_begin;
+      wait(&q_full, n_item & 1u);
 #pragma unroll 1
-        for (int x = 0; x < 2 * nb; ++x) {
-          const Step sp = step_of(x, nb);
-          const int i = sp.j & 1, st = n_tile % STAGES;
-          if (!sp.is_k) {
-            wait(&p_full[i], (p_phase >> i) & 1u);
-            p_phase ^= 1u << i;
-            if (sp.j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
-          }
-          wait(&full[st], (n_tile / STAGES) & 1u);
-          ++n_tile;
+      for (int j = -2; j < nb && ok; ++j) {                // K0 K1 V0 K2 V1 ...
+        const int i = j & 1;
+        if (j >= 0) {
+          wait(&p_full[i], (p_phase >> i) & 1u);
+          p_phase ^= 1u << i;
+          if (j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
+          wait(&full[st], st_phase);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t tile = smem_u32(ring + st * TILE_BYTES);
           if (elect_one()) {
-          if (sp.is_k) {
-            const uint64_t k_desc = make_smem_desc_sw128(tile, 16, tl.group);
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              constexpr int H = HALF_BYTES;
-              umma_ss(tmem + TMEM_S + i * BLK, q_desc + (((kk >> 2) * H + (kk & 3) * 32) >> 4), k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
-                      idesc_qk, kk != 0);
-            }
-            umma_commit(&s_full[i]);
-            umma_commit(&empty[st]);
-            if (sp.j + 1 == nb) umma_commit(&q_empty[qs]);
-          } else {
-            const uint64_t v_desc = make_smem_desc_sw128(tile, tl.mn_lbo, tl.group);
+            const uint64_t v_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), tl.mn_lbo, tl.group);
 #pragma unroll
             for (int kk = 0; kk < BLK / 16; ++kk)
-              umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2 * tl.group >> 4), idesc_pv, sp.j > 1 || kk != 0);
+              umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2 * tl.group >> 4), idesc_pv, j > 1 || kk != 0);
             umma_commit(&empty[st]);
-            if (sp.j + 1 == nb) umma_commit(&o_full);
-          }
+            if (j + 1 == nb) umma_commit(&o_full);
           }
           __syncwarp();
+          advance();
         }
-        ++n_item;
+        if (j + 2 < nb) {
+          wait(&full[st], st_phase);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (elect_one()) {
+            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              umma_ss(tmem + TMEM_S + i * BLK, q_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4),
+                      k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4), idesc_qk, kk != 0);
+            umma_commit(&s_full[i]);
+            umma_commit(&empty[st]);
+            if (j + 3 == nb) umma_commit(&q_empty);
+          }
+          __syncwarp();
+          advance();
+        }
       }
-      if (!ok) cta_failed = 1;
+      ++n_item;
     }
+    if (!ok) cta_failed = 1;
    } else {
     clean_role<D, STAGES, BF16, false, false>(a, pipe, cur, &cta_failed);
    }
