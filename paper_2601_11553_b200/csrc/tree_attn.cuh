@@ -114,22 +114,13 @@ __device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, int* e
   else return mbar_wait(bar, parity, err_word, code);
 }
 
-// The order in which a piece of nb blocks takes its tiles, K0 K1 V0 K2 V1 K3 ... : x runs from 0 to 2 nb - 1.
-struct Step { bool is_k; int j; };
-__device__ __forceinline__ Step step_of(int x, int nb) {
-  const int y = x - min(nb, 2), pairs = 2 * max(nb - 2, 0);
-  if (y < 0) return Step{true, x};
-  if (y < pairs) return Step{(y & 1) != 0, (y & 1) ? y / 2 + 2 : y / 2};
-  return Step{false, pairs / 2 + y - pairs};
-}
-
-// Copies (one warp): Q tiles, and K and V tiles in the order the MMAs take them, K0 K1 V0 K2 V1 ...
+// Copies (one warp): Q tiles, and K and V tiles in the order the MMAs take them, K0 K1 V0 K2 V1 K3 ...
 template <int D, int STAGES, int QSLOTS, bool CALLS>
 __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe, Cursor& cur, const Span& span, const CUtensorMap* tmQ,
                                           const CUtensorMap* tmK, const CUtensorMap* tmV, int* cta_failed) {
   constexpr int HALVES = D / 64, TILE_BYTES = HALVES * BLK * 128;
   const int lane = threadIdx.x & 31;
-  uint32_t n_item = 0, n_tile = 0, n_raw = 0;
+  uint32_t n_item = 0, st = 0, st_phase = 0, n_raw = 0;
   MergeRecord rec{};
   bool ok = true;
   Item it{};
@@ -144,24 +135,30 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
     }
     __syncwarp();
     const SeqPart part{it.row0, it.n_nodes, it.ctx_len};
-    int next = tile_place(a.kv, part, it.seq, it.blk_begin, lane);          // page ids are asked for a tile ahead
-#pragma unroll 1
-    for (int x = 0; x < 2 * nb; ++x) {
-      const Step sp = step_of(x, nb);
-      const int blk = it.blk_begin + sp.j, st = n_tile % STAGES, where = next;
-      if (a.kv.page_table && x + 1 < 2 * nb) next = tile_place(a.kv, part, it.seq, it.blk_begin + step_of(x + 1, nb).j, lane);
-      ok = __all_sync(0xffffffffu, role_wait<CALLS>(&pipe.empty[st], ((n_tile / STAGES) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
-      if (!ok) break;
-      ++n_tile;
+    auto load = [&](bool is_k, int j, int where) {
+      ok = __all_sync(0xffffffffu, role_wait<CALLS>(&pipe.empty[st], st_phase ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+      if (!ok) return;
+      const int blk = it.blk_begin + j;
       // a tile that has to be cleaned lands on a barrier of the cleaning warps; they then complete `full` in its place
-      const bool clean = !sp.is_k && (blk + 1) * BLK > it.ctx_len;
+      const bool clean = !is_k && (blk + 1) * BLK > it.ctx_len;
       uint64_t* bar = clean ? &pipe.raw[n_raw++ % STAGES] : &pipe.full[st];
       if (elect_one()) {
         mbar_arrive_expect_tx(bar, TILE_BYTES);
         if (!clean) mbar_arrive(bar);
       }
       __syncwarp();
-      load_tile<D>(pipe.ring + st * TILE_BYTES, sp.is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g, blk);
+      load_tile<D>(pipe.ring + st * TILE_BYTES, is_k ? tmK : tmV, bar, a.kv.page_table != nullptr, where, it.g, blk);
+      if (++st == STAGES) { st = 0; st_phase ^= 1u; }
+    };
+    // where[n]: the places of block j + n.  Page ids are asked for a block ahead, once for K and V.
+    int where[4] = {0, 0, tile_place(a.kv, part, it.seq, it.blk_begin, lane), 0};
+#pragma unroll 1
+    for (int j = -2; j < nb && ok; ++j) {
+      where[3] = where[2];
+      if (a.kv.page_table && j + 3 < nb) where[3] = tile_place(a.kv, part, it.seq, it.blk_begin + j + 3, lane);
+      if (j >= 0) load(false, j, where[0]);
+      if (ok && j + 2 < nb) load(true, j + 2, where[2]);
+      where[0] = where[1]; where[1] = where[2]; where[2] = where[3];
     }
     if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
       rec.n_parts = last_cta(span, it.unit_end) - static_cast<int>(blockIdx.x) + 1;
