@@ -20,7 +20,7 @@
 namespace pc {
 namespace {
 
-constexpr int K_RING = 128 * 1024;
+constexpr int K_RING = 96 * 1024;              // 128 KB: 64 tokens x 2500 slots 62.9 -> 64.2 us, 33 nodes x 33024 31.2 -> 30.7; 64 KB: 71.8 and 35.4
 constexpr int Q_TILE = 32 * 1024;
 constexpr int WEIGHTS_SMEM = K_RING + 2 * Q_TILE + 1024;
 constexpr int MAX_STAGES = 8;
@@ -43,15 +43,28 @@ struct WeightParams {
   int* err_word;
 };
 
-// Nodes of a prompt that count (a whole warp asks).
-__device__ __forceinline__ int used_nodes(const WeightParams& a, const SeqPart& p) {
+// Which of 32 nodes of a prompt count (a whole warp asks).
+__device__ __forceinline__ uint32_t used_word(const WeightParams& a, const SeqPart& p, int n0) {
+  const int lane = threadIdx.x & 31;
+  return __ballot_sync(0xffffffffu, n0 + lane < p.n_nodes && ld_dep_u8(a.use + p.row0 + n0 + lane) != 0);
+}
+// How many nodes of a prompt count, and which of the first 64.  Those flags are asked for together: a call's first tile waits for
+// this, and every round trip is half a microsecond.
+__device__ __forceinline__ int used_nodes(const WeightParams& a, const SeqPart& p, uint32_t (&bits)[2]) {
   if (!a.use) return p.n_nodes;
   const int lane = threadIdx.x & 31;
-  int n = 0;
+  const uint8_t* flags = a.use + p.row0 + lane;
+  const uint32_t lo = lane < p.n_nodes ? ld_dep_u8(flags) : 0u, hi = lane + 32 < p.n_nodes ? ld_dep_u8(flags + 32) : 0u;
+  bits[0] = __ballot_sync(0xffffffffu, lo != 0);
+  bits[1] = __ballot_sync(0xffffffffu, hi != 0);
+  int n = __popc(bits[0]) + __popc(bits[1]);
 #pragma unroll 1
-  for (int i = 0; i < p.n_nodes; i += 32)
-    n += __popc(__ballot_sync(0xffffffffu, i + lane < p.n_nodes && ld_dep_u8(a.use + p.row0 + i + lane) != 0));
+  for (int n0 = 64; n0 < p.n_nodes; n0 += 32) n += __popc(used_word(a, p, n0));
   return n;
+}
+__device__ __forceinline__ int used_nodes(const WeightParams& a, const SeqPart& p) {
+  uint32_t bits[2];
+  return used_nodes(a, p, bits);
 }
 __device__ __forceinline__ int n_tiles(const WeightParams& a, int nodes) { return (nodes + a.tile_nodes - 1) / a.tile_nodes; }
 __device__ __forceinline__ Shape weight_shape(const WeightParams& a, const SeqPart& p) {
@@ -151,54 +164,53 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------ MMA issuer
-    {     // the whole warp walks; one lane issues
-      const TileLayout<D> tl(a.kv.page_table != nullptr);
-      uint32_t n_tile = 0, n_s[2] = {0, 0};
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
-      };
-      while (ok && next_piece(cur, a, &pc)) {
-        const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes);
-        if (tiles == 0) continue;
-        for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
-          const int i = (blk - pc.blk_begin) & 1;
-          const int st = n_tile % STAGES;
-          wait(&full[st], (n_tile / STAGES) & 1u);
-          ++n_tile;
-          const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
-          for (int t = 0; t < tiles && ok; ++t) {
-            const int qs = n_q & 1;
-            wait(&q_full[qs], (n_q >> 1) & 1u);
-            const uint32_t n = i == 0 ? n_s[0] : n_s[1];
-            const int buf = n & 1;
-            wait(&s_empty[i][buf], ((n >> 1) & 1u) ^ 1u);
-            if (!ok) break;
-            if (i == 0) ++n_s[0]; else ++n_s[1];
-            tc_fence_after_sync();
-            const int cols = (min(a.tile_nodes, nodes - t * a.tile_nodes) * a.group + 15) & ~15;
-            const uint32_t idesc = make_idesc_f16(BLK, cols, BF16 ? 1 : 0, 0, 0);
-            const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_TILE), 16, 1024);
-            if (elect_one()) {
+    // the whole warp walks; one lane issues
+    const TileLayout<D> tl(a.kv.page_table != nullptr);
+    uint32_t st = 0, st_phase = 0, n_s0 = 0, n_s1 = 0;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
+    };
+    while (ok && next_piece(cur, a, &pc)) {
+      const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes);
+      if (tiles == 0) continue;
+      if (tiles == 1) wait(&q_full[n_q & 1], (n_q >> 1) & 1u);
+      for (int blk = pc.blk_begin; blk < pc.blk_end && ok; ++blk) {
+        const int i = (blk - pc.blk_begin) & 1;
+        wait(&full[st], st_phase);
+        const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
+        for (int t = 0; t < tiles && ok; ++t) {
+          const int qs = n_q & 1;
+          if (tiles > 1) wait(&q_full[qs], (n_q >> 1) & 1u);
+          const uint32_t n = i == 0 ? n_s0++ : n_s1++;
+          const int buf = n & 1;
+          wait(&s_empty[i][buf], ((n >> 1) & 1u) ^ 1u);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const int cols = (min(a.tile_nodes, nodes - t * a.tile_nodes) * a.group + 15) & ~15;
+          const uint32_t idesc = make_idesc_f16(BLK, cols, BF16 ? 1 : 0, 0, 0);
+          const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem + qs * Q_TILE), 16, 1024);
+          const bool q_done = tiles > 1 || blk + 1 == pc.blk_end;
+          if (elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
+            for (int kk = 0; kk < D / 16; ++kk)
               umma_ss(tmem + (i * 2 + buf) * BLK, k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4),
                       q_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4), idesc, kk != 0);
-            }
             umma_commit(&s_full[i][buf]);
-            if (tiles > 1 || blk + 1 == pc.blk_end) umma_commit(&q_empty[qs]);
+            if (q_done) umma_commit(&q_empty[qs]);
             if (t + 1 == tiles) umma_commit(&empty[st]);
-            }
-            __syncwarp();
-            if (tiles > 1 || blk + 1 == pc.blk_end) ++n_q;
           }
+          __syncwarp();
+          if (q_done) ++n_q;
         }
+        if (++st == STAGES) { st = 0; st_phase ^= 1u; }
       }
     }
   } else if (warp >= 10) {
     // ------------------------------------------------------------ the rows' lse
     const int tid = threadIdx.x - 320;
     while (ok && next_piece(cur, a, &pc)) {
-      const int nodes = used_nodes(a, pc.part), tiles = n_tiles(a, nodes);
+      uint32_t used[2];
+      const int nodes = used_nodes(a, pc.part, used), tiles = n_tiles(a, nodes);
       const int loads = tiles == 1 ? 1 : tiles * (pc.blk_end - pc.blk_begin);
       for (int x = 0; x < loads && ok; ++x) {
         const int t = tiles == 1 ? 0 : x % tiles;
@@ -212,10 +224,9 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           int before = -t * a.tile_nodes;
 #pragma unroll 1
           for (int n0 = 0; n0 < pc.part.n_nodes; n0 += 32) {
-            const bool u = n0 + lane < pc.part.n_nodes && ld_dep_u8(a.use + pc.part.row0 + n0 + lane) != 0;
-            const uint32_t all = __ballot_sync(0xffffffffu, u);
+            const uint32_t all = n0 == 0 ? used[0] : n0 == 32 ? used[1] : used_word(a, pc.part, n0);
             const int at = before + __popc(all & ((1u << lane) - 1));
-            if (u && at >= 0 && at < tile_n) node_list[qs][at] = static_cast<uint8_t>(n0 + lane);
+            if ((all >> lane & 1u) && at >= 0 && at < tile_n) node_list[qs][at] = static_cast<uint8_t>(n0 + lane);
             before += __popc(all);
           }
         } else {
@@ -223,34 +234,50 @@ attention_weights_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_c
           for (int e = lane; e < tile_n; e += 32) node_list[qs][e] = static_cast<uint8_t>(t * a.tile_nodes + e);
         }
         __syncwarp();
-        if (a.use) {                                       // their rows, in the layout a copy would give them
-          constexpr int VECS = D / 8;
+        float z[2];                                        // on their way while the rows are fetched
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int r = k * 64 + tid;
+          z[k] = -INFINITY;
+          if (r < n_rows) z[k] = ld_dep_f32(a.lse + static_cast<size_t>(pc.part.row0 + node_list[qs][r / a.group]) * a.n_q_heads + pc.unit * a.group + r % a.group);
+        }
+        const int words = (pc.part.n_nodes + 63) / 64, n_mask = pc.blk_end * BLK > pc.part.ctx_len ? tile_n * words : 0;
+        auto mask_word = [&](int e) {
+          const int node = node_list[qs][e / words];
+          return node_word(a.rows, pc.part.row0 + node, node, e % words);
+        };
+        const uint64_t first_mask = tid < n_mask ? mask_word(tid) : 0;
+        if (a.use) {                                       // the rows, in the layout a copy would give them
+          constexpr int VECS = D / 8, BATCH = 8;
           uint8_t* dst = q_smem + qs * Q_TILE;
-#pragma unroll 4
-          for (int e = tid; e < n_rows * VECS; e += 64) {
-            const int r = e / VECS, v = e % VECS;
-            const int64_t at = static_cast<int64_t>(pc.part.row0 + node_list[qs][r / a.group]) * a.q_stride + (pc.unit * a.group + r % a.group) * D + v * 8;
-            *reinterpret_cast<uint4*>(dst + (v >> 3) * HALF_BYTES + r * 128 + (((v & 7) ^ (r & 7)) << 4)) =
-                ld_dep_v4(static_cast<const unsigned short*>(a.q) + at);
+          const int total = n_rows * VECS;
+#pragma unroll 1
+          for (int e0 = tid; e0 < total; e0 += 64 * BATCH) {
+            uint4 row[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+              const int e = e0 + u * 64, r = e / VECS;
+              if (e >= total) break;
+              const int64_t at = static_cast<int64_t>(pc.part.row0 + node_list[qs][r / a.group]) * a.q_stride + (pc.unit * a.group + r % a.group) * D + e % VECS * 8;
+              row[u] = ld_dep_v4(static_cast<const unsigned short*>(a.q) + at);
+            }
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+              const int e = e0 + u * 64, r = e / VECS, v = e % VECS;
+              if (e >= total) break;
+              *reinterpret_cast<uint4*>(dst + (v >> 3) * HALF_BYTES + r * 128 + (((v & 7) ^ (r & 7)) << 4)) = row[u];
+            }
           }
           fence_proxy_async_smem();
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int r = k * 64 + tid;
-          float z = -INFINITY;
-          if (r < n_rows) z = ld_dep_f32(a.lse + static_cast<size_t>(pc.part.row0 + node_list[qs][r / a.group]) * a.n_q_heads + pc.unit * a.group + r % a.group);
-          const uint32_t counts = __ballot_sync(0xffffffffu, z != -INFINITY);
-          row_lse[qs][r] = z != -INFINITY ? z : 0.f;
+          const uint32_t counts = __ballot_sync(0xffffffffu, z[k] != -INFINITY);
+          row_lse[qs][k * 64 + tid] = z[k] != -INFINITY ? z[k] : 0.f;
           if (lane == 0) row_ok[qs][k * 2 + warp - 10] = counts;
         }
-        if (pc.blk_end * BLK > pc.part.ctx_len) {
-          const int words = (pc.part.n_nodes + 63) / 64;
-          for (int e = tid; e < tile_n * words; e += 64) {
-            const int node = node_list[qs][e / words];
-            node_mask[qs][e / words][e % words] = node_word(a.rows, pc.part.row0 + node, node, e % words);
-          }
-        }
+        if (tid < n_mask) node_mask[qs][tid / words][tid % words] = first_mask;
+        for (int e = tid + 64; e < n_mask; e += 64) node_mask[qs][e / words][e % words] = mask_word(e);
         __syncwarp();
         if (elect_one()) mbar_arrive(&q_full[qs]);
       }
