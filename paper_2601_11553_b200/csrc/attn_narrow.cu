@@ -1,7 +1,7 @@
-// Tree attention of tiles with at most 32 rows (one token a prompt, short chains): both products formed transposed.
+// Tree attention of tiles with at most 16 rows (one token a prompt, short chains): both products formed transposed.
 //
 // With a handful of rows the 128-row tile of attn_tree.cu leaves its softmax to one warp per block, 128 scores a thread: a
-// chain of 1.5 us a block and 3 us at a piece's end, which the copies cannot always hide.  Here a block's slots are the
+// chain of 1.2 us a block and 2 us at a piece's end, which the copies cannot always hide.  Here a block's slots are the
 // MMA's M side: S^T = K Q^T has one TMEM lane, i.e. one thread, per slot and a column per row, so a thread forms as
 // many exponentials as there are rows; O^T = V^T P^T has a lane per element of the head and a column per row.  Three things
 // cross threads: whether a row's block maximum passes its reference (one barrier with an OR), its sum (only at the piece's end), and
@@ -17,11 +17,14 @@
 namespace pc {
 namespace {
 
-constexpr int RING_BYTES = 160 * 1024;
+constexpr int NC = NARROW_ROWS;                  // columns of the products
+// Four tiles of head size 128.  64 tokens on 2500 slots with 3 / 4 / 5 / 6 tiles: 111.6 / 107.4 / 107.2 / 113 us contiguous; in pages with
+// 4 / 5 / 6: 108.3 / 110.7 / 115.5.  (What is asked for too early comes in the way of what the other SMs wait for.)
+constexpr int RING_BYTES = 128 * 1024;
 
 // Per-column reduction over the warp's 32 lanes, transposing as it goes: every step exchanges half of the columns that are left
 // with the lane across and combines the other half, so NC columns cost about NC shuffles.  Lane l returns column l % NC.
-template <int NC, typename Op>
+template <typename Op>
 __device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
   const int lane = threadIdx.x & 31;
   float v[NC];
@@ -36,8 +39,7 @@ __device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
       v[e] = op(hi ? v[e + h] : v[e], other);
     }
   }
-  if constexpr (NC == 16) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
-  return v[0];
+  return op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
 }
 // What the drafted V elements that are not finite (slots s .. end - 1) add to an output element of a row: they were taken out
 // of the product.
@@ -63,20 +65,10 @@ __device__ __forceinline__ bool parity_any(int i, bool x) {
     asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
   return y != 0;
 }
-template <int NC>
-__device__ __forceinline__ void tmem_ld_cols(uint32_t addr, uint32_t (&r)[NC]) {
-  if constexpr (NC == 16) tmem_ld_32x16(addr, r);
-  else tmem_ld_32x32(addr, r);
-}
-template <int NC>
-__device__ __forceinline__ void tmem_st_cols(uint32_t addr, const uint32_t (&r)[NC]) {
-  if constexpr (NC == 16) tmem_st_32x16(addr, r);
-  else tmem_st_32x32(addr, r);
-}
-template <int D, int NC>
+template <int D>
 constexpr int narrow_smem() { return 1024 + RING_BYTES + 2 * NC * D * 2 + 2 * NC * BLK * 2; }
 
-template <int D, bool BF16, int NC>
+template <int D, bool BF16>
 __global__ void __launch_bounds__(TREE_THREADS, 1)
 narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TreeParams a) {
@@ -86,7 +78,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   constexpr int STAGES = RING_BYTES / TILE_BYTES;
   constexpr int Q_HALF = NC * 128, Q_SLOT = HALVES * Q_HALF;
   constexpr int P_HALF = NC * 128, P_BYTES = 2 * P_HALF;
-  constexpr int TMEM_COLS = NC == 16 ? 128 : 256;               // S_0 S_1, then O of (item parity, block parity): six times NC
+  constexpr int TMEM_COLS = 128;                               // S_0 S_1, then O of (item parity, block parity): six times NC
   constexpr uint32_t TMEM_O = 2 * NC;
   static_assert(STAGES <= MAX_STAGES, "");
   extern __shared__ uint8_t smem_raw[];
@@ -95,7 +87,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   __shared__ __align__(16) float block_max[2][2][NC][4];       // [block parity][use][row][warp]
   __shared__ __align__(16) float fin_l[2][2][NC][4];            // [item parity][block parity][row][warp]: a warp's share of the sum
   __shared__ float fin_m[2][2][NC];
-  __shared__ uint64_t node_mask[2 * 32 * MASK_WORDS];
+  __shared__ uint64_t node_mask[2 * NARROW_ROWS * MASK_WORDS];
   __shared__ int bad_v[FLAGS][2];
   __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
@@ -215,7 +207,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     while (next_item(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
       float neg[NC], l[NC];                                // -reference (the same in all threads); sum over this thread's slots only
-      uint32_t unset = it.n_rows == 32 ? ~0u : (1u << it.n_rows) - 1;       // rows that have seen nothing yet: reference 0, sum and O zero
+      uint32_t unset = (1u << it.n_rows) - 1;       // rows that have seen nothing yet: reference 0, sum and O zero
 #pragma unroll
       for (int c = 0; c < NC; ++c) { neg[c] = 0.f; l[c] = 0.f; }
       for (int j = i; j < nb; j += 2) {
@@ -225,7 +217,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         bool raise = j == i;                               // does any row's block maximum pass its reference by more than 2^8
         if (ok) {
           tc_fence_after_sync();
-          tmem_ld_cols<NC>(lanes + i * NC, s);
+          tmem_ld_32x16(lanes + i * NC, s);
           tmem_wait_ld();
           const int slot = (it.blk_begin + j) * BLK + r;
           if ((it.blk_begin + j + 1) * BLK > it.ctx_len) {
@@ -234,7 +226,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
               const int node = slot - it.ctx_len;
               uint32_t seen = 0;
               if (node < it.n_nodes) {
-                const uint64_t* w = node_mask + par * 32 * MASK_WORDS + (node >> 6);
+                const uint64_t* w = node_mask + par * NARROW_ROWS * MASK_WORDS + (node >> 6);
                 int at = 0, h = 0;
 #pragma unroll 1
                 for (int c = 0; c < it.n_rows; ++c) {
@@ -271,7 +263,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           float top[NC];
 #pragma unroll
           for (int c = 0; c < NC; ++c) top[c] = c < it.n_rows ? __uint_as_float(s[c]) : -INFINITY;
-          const float mine = column_reduce<NC>(top, [](float x, float y) { return fmaxf(x, y); });
+          const float mine = column_reduce(top, [](float x, float y) { return fmaxf(x, y); });
           if (lane < NC) maxima[lane][quarter] = mine;
           parity_any(i, false);
           const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
@@ -289,7 +281,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           if (j != i && ok) {                              // s_full came behind this parity's last product: O is complete
             const uint32_t t_o = lanes + TMEM_O + (par * 2 + i) * NC;
             uint32_t o[NC];
-            tmem_ld_cols<NC>(t_o, o);
+            tmem_ld_32x16(t_o, o);
             tmem_wait_ld();
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -297,7 +289,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
               l[c] *= f;
               o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
             }
-            tmem_st_cols<NC>(t_o, o);
+            tmem_st_32x16(t_o, o);
             tmem_wait_st();
           }
         }
@@ -323,7 +315,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
       }
       // ---- the piece's end: sums and references of both parities are exchanged; parity i writes rows i, i + 2, ...
       if (ok) {
-        const float sum = column_reduce<NC>(l, [](float x, float y) { return x + y; });
+        const float sum = column_reduce(l, [](float x, float y) { return x + y; });
         if (lane < NC) fin_l[par][i][lane][quarter] = sum;
         float mine = 0.f;
 #pragma unroll
@@ -422,28 +414,23 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
   }
 }
 
-template <int D, bool BF16, int NC>
+template <int D, bool BF16>
 int launch(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TreeParams& p, int n_ctas, cudaStream_t s) {
   static bool set[MAX_DEVICES] = {};
   const int dev = current_device_slot();
   if (!set[dev]) {
-    if (cudaFuncSetAttribute(narrow_attention_kernel<D, BF16, NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, narrow_smem<D, NC>()) != cudaSuccess)
-      return -1;
+    if (cudaFuncSetAttribute(narrow_attention_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, narrow_smem<D>()) != cudaSuccess) return -1;
     set[dev] = true;
   }
-  return launch_pdl(narrow_attention_kernel<D, BF16, NC>, dim3(n_ctas), dim3(TREE_THREADS), narrow_smem<D, NC>(), s, q, k, v, p) == cudaSuccess ? 0 : -1;
-}
-template <int D, bool BF16>
-int launch_cols(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TreeParams& p, int n_ctas, cudaStream_t s) {
-  return p.tile_nodes * p.group <= 16 ? launch<D, BF16, 16>(q, k, v, p, n_ctas, s) : launch<D, BF16, 32>(q, k, v, p, n_ctas, s);
+  return launch_pdl(narrow_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), narrow_smem<D>(), s, q, k, v, p) == cudaSuccess ? 0 : -1;
 }
 
 }  // namespace
 
 int launch_narrow_attention(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TreeParams& p, int n_ctas,
                             cudaStream_t s) {
-  if (p.kv.head_dim == 128) return p.kv.bf16 ? launch_cols<128, true>(q, k, v, p, n_ctas, s) : launch_cols<128, false>(q, k, v, p, n_ctas, s);
-  return p.kv.bf16 ? launch_cols<64, true>(q, k, v, p, n_ctas, s) : launch_cols<64, false>(q, k, v, p, n_ctas, s);
+  if (p.kv.head_dim == 128) return p.kv.bf16 ? launch<128, true>(q, k, v, p, n_ctas, s) : launch<128, false>(q, k, v, p, n_ctas, s);
+  return p.kv.bf16 ? launch<64, true>(q, k, v, p, n_ctas, s) : launch<64, false>(q, k, v, p, n_ctas, s);
 }
 
 }  // namespace pc

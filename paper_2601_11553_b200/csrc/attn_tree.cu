@@ -1,4 +1,6 @@
-// Attention of drafted tokens over a cached context, and the running attention weights of its slots, on tcgen05.
+// Attention of drafted tokens over a cached context, on tcgen05 (tiles of 17 to 128 rows; fewer rows: attn_narrow.cu).
+//
+//   out[r] = sum_s exp(scale q_r . k_s - lse_r) v_s,   lse_r = log sum_s exp(scale q_r . k_s),   s over the slots r sees
 //
 // Rows.  The nodes of a prompt and the query heads of one KV head are packed into the 128 rows of one MMA tile (row =
 // node * group + head): all of them read the same K and V, so a K or V byte that reaches shared memory serves every
@@ -6,11 +8,15 @@
 //
 // Bounds.  A block costs 64 KB of K and V (head size 128, 1.5 us of one SM's share of the HBM) and at most 8.4 MFLOP of
 // tensor work (0.75 us) and 16 K exponentials (0.55 us): with the tile at most 128 rows high the operator is bound by
-// reading K and V once, whatever the number of rows, and everything below serves to keep the copies running.
+// reading K and V once, whatever the number of rows, and everything below serves to keep the copies running.  Measured,
+// 96 rows: 1.50 us a block (6.5 TB/s over 148 SMs), 1.06 us when all K and V are in L2, and 13 - 17 us of a call for its start,
+// the ends of its pieces and the merge: 48-node trees on 64 x 2500 slots in pages 128 us (floor 105), 26-node trees on
+// one prompt of 2112 slots 15.7 us.
 //
 // Schedule.  Lengths live on the device, so the work is dealt there: every unit costs its blocks and a little more, the
 // batch's total cost is cut into one contiguous span per CTA, and a unit that a span border cuts is finished in parts
-// whose unnormalised results a second kernel merges.  Every CTA forms the same prefix sums, so nothing is exchanged.
+// whose unnormalised results a second kernel merges (in L2; some 5 us of the batch of trees.  Merging in the CTA that arrives last
+// took 4 us more).  Every CTA forms the same prefix sums, so nothing is exchanged.
 //
 // One CTA per SM, 384 threads:
 //   warp 8       copies: Q tile, then K and V tiles in the order the MMAs take them (K0 K1 V0 K2 V1 ...) into one ring
@@ -31,11 +37,13 @@
 namespace pc {
 namespace {
 
+// Four tiles of head size 128 and one Q tile: 48-node trees on 64 x 2500 slots 131 us; with five tiles or two Q tiles 134 - 142 us, 26-node
+// trees 15.9 -> 16.0 us.
 constexpr int RING_BYTES = 128 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
 constexpr int TREE_SMEM = RING_BYTES + Q_BYTES + 1024;
 constexpr uint32_t TMEM_S = 256;
-constexpr int WHOLE_BLOCKS = 6;
+constexpr int WHOLE_BLOCKS = 6;                 // contexts of up to so many blocks: a unit is one CTA's
 
 // ---------------------------------------------------------------------------------------------------- attention
 template <int D, bool BF16>
@@ -88,71 +96,71 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     Cursor cur(span);
     Item it{};
-   if (warp == 8) {
-    copy_role<D, STAGES, 1, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
-   } else if (warp == 9) {
-    // ------------------------------------------------------------ MMA issuer
-    // the whole warp walks; one lane issues
-    constexpr uint32_t idesc_qk = make_idesc_f16(BLK, BLK, BF16 ? 1 : 0, 0, 0);
-    constexpr uint32_t idesc_pv = make_idesc_f16(BLK, D, BF16 ? 1 : 0, 0, 1);
-    uint32_t n_item = 0, st = 0, st_phase = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
-    };
-    auto advance = [&] {
-      if (++st == STAGES) { st = 0; st_phase ^= 1u; }
-    };
-    const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
-    const TileLayout<D> tl(a.kv.page_table != nullptr);
-    while (ok && next_item(cur, a, &it)) {
-      const int nb = it.blk_end - it.blk_begin;
-      wait(&q_full, n_item & 1u);
+    if (warp == 8) {
+      copy_role<D, STAGES, 1, false>(a, pipe, cur, span, &tmQ, &tmK, &tmV, &cta_failed);
+    } else if (warp == 9) {
+      // ------------------------------------------------------------ MMA issuer
+      // the whole warp walks; one lane issues
+      constexpr uint32_t idesc_qk = make_idesc_f16(BLK, BLK, BF16 ? 1 : 0, 0, 0);
+      constexpr uint32_t idesc_pv = make_idesc_f16(BLK, D, BF16 ? 1 : 0, 0, 1);
+      uint32_t n_item = 0, st = 0, st_phase = 0, p_phase = 0;        // p_phase: bit i, the parity to wait for on p_full[i]
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
+      };
+      auto advance = [&] {
+        if (++st == STAGES) { st = 0; st_phase ^= 1u; }
+      };
+      const uint64_t q_desc = make_smem_desc_sw128(smem_u32(q_smem), 16, 1024);
+      const TileLayout<D> tl(a.kv.page_table != nullptr);
+      while (ok && next_item(cur, a, &it)) {
+        const int nb = it.blk_end - it.blk_begin;
+        wait(&q_full, n_item & 1u);
 #pragma unroll 1
-      for (int j = -2; j < nb && ok; ++j) {                // K0 K1 V0 K2 V1 ...
-        const int i = j & 1;
-        if (j >= 0) {
-          wait(&p_full[i], (p_phase >> i) & 1u);
-          p_phase ^= 1u << i;
-          if (j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
-          wait(&full[st], st_phase);
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (elect_one()) {
-            const uint64_t v_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), tl.mn_lbo, tl.group);
+        for (int j = -2; j < nb && ok; ++j) {                // K0 K1 V0 K2 V1 ...
+          const int i = j & 1;
+          if (j >= 0) {
+            wait(&p_full[i], (p_phase >> i) & 1u);
+            p_phase ^= 1u << i;
+            if (j == 0) wait(&o_free, (n_item & 1u) ^ 1u);
+            wait(&full[st], st_phase);
+            if (!ok) break;
+            tc_fence_after_sync();
+            if (elect_one()) {
+              const uint64_t v_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), tl.mn_lbo, tl.group);
 #pragma unroll
-            for (int kk = 0; kk < BLK / 16; ++kk)
-              umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2 * tl.group >> 4), idesc_pv, j > 1 || kk != 0);
-            umma_commit(&empty[st]);
-            if (j + 1 == nb) umma_commit(&o_full);
+              for (int kk = 0; kk < BLK / 16; ++kk)
+                umma_ts(tmem + i * HEAD_DIM, tmem + TMEM_S + i * BLK + kk * 8, v_desc + (kk * 2 * tl.group >> 4), idesc_pv, j > 1 || kk != 0);
+              umma_commit(&empty[st]);
+              if (j + 1 == nb) umma_commit(&o_full);
+            }
+            __syncwarp();
+            advance();
           }
-          __syncwarp();
-          advance();
-        }
-        if (j + 2 < nb) {
-          wait(&full[st], st_phase);
-          if (!ok) break;
-          tc_fence_after_sync();
-          if (elect_one()) {
-            const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
+          if (j + 2 < nb) {
+            wait(&full[st], st_phase);
+            if (!ok) break;
+            tc_fence_after_sync();
+            if (elect_one()) {
+              const uint64_t k_desc = make_smem_desc_sw128(smem_u32(ring + st * TILE_BYTES), 16, tl.group);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-              umma_ss(tmem + TMEM_S + i * BLK, q_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4),
-                      k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4), idesc_qk, kk != 0);
-            umma_commit(&s_full[i]);
-            umma_commit(&empty[st]);
-            if (j + 3 == nb) umma_commit(&q_empty);
+              for (int kk = 0; kk < D / 16; ++kk)
+                umma_ss(tmem + TMEM_S + i * BLK, q_desc + (((kk >> 2) * HALF_BYTES + (kk & 3) * 32) >> 4),
+                        k_desc + (((kk >> 2) * tl.half + (kk & 3) * 32) >> 4), idesc_qk, kk != 0);
+              umma_commit(&s_full[i]);
+              umma_commit(&empty[st]);
+              if (j + 3 == nb) umma_commit(&q_empty);
+            }
+            __syncwarp();
+            advance();
           }
-          __syncwarp();
-          advance();
         }
+        ++n_item;
       }
-      ++n_item;
+      if (!ok) cta_failed = 1;
+    } else {
+      clean_role<D, STAGES, BF16, false, false>(a, pipe, cur, &cta_failed);
     }
-    if (!ok) cta_failed = 1;
-   } else {
-    clean_role<D, STAGES, BF16, false, false>(a, pipe, cur, &cta_failed);
-   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // where the walk stands waits in shared memory between pieces: the rows' scores want every register
@@ -436,7 +444,8 @@ int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v
     if (cudaFuncSetAttribute(tree_attention_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, TREE_SMEM) != cudaSuccess) return -1;
     set[dev] = true;
   }
-  // Up to 32 rows a tile: the transposed form.
+  // Up to 16 rows a tile: the transposed form.  64 x 2500 slots, 2 rows: 107 us against 124 us for the 128-row form; 16 rows: 111 against
+  // 115; 32 rows (with twice the columns): 124 against 118; two prompts of 33024 slots, 32 rows: 57 against 55.
   if (p.tile_nodes * p.group <= NARROW_ROWS) {
     if (launch_narrow_attention(q, k, v, p, n_ctas, s) != 0) return -1;
   } else if (launch_pdl(tree_attention_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), TREE_SMEM, s, q, k, v, p) != cudaSuccess) {

@@ -1,4 +1,4 @@
-// What the two forms of the tree attention share (attn_tree.cu: up to 128 rows a tile; attn_narrow.cu: up to 32).
+// What the two forms of the tree attention share (attn_tree.cu: up to 128 rows a tile; attn_narrow.cu: up to 16).
 #pragma once
 #include "tree_common.cuh"
 
@@ -27,7 +27,7 @@ struct TreeParams {
 // Workspace places of a TreeParams; launches one of the two forms, then (attn_tree.cu) the merge.
 int launch_narrow_attention(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const TreeParams& p, int n_ctas,
                             cudaStream_t s);
-constexpr int NARROW_ROWS = 32;
+constexpr int NARROW_ROWS = 16;
 
 namespace {
 
@@ -93,7 +93,7 @@ __device__ __forceinline__ float elem(uint32_t bits16) {
 // ---------------------------------------------------------------------------------------------------- attention: shared roles
 constexpr float RESCALE_THRESHOLD = 8.0f;       // the running reference is raised when a block exceeds it by 2^8
 constexpr int MIN_SPAN = 4;                     // least cost of an attention span: shorter ones cost more to merge than they save
-constexpr int MAX_STAGES = 10;
+constexpr int MAX_STAGES = 8;
 constexpr int FLAGS = 8;                        // items a `bad V` flag lives for: more than the roles can be apart
 constexpr int MASK_WORDS = 4;                   // 256 nodes
 
@@ -193,7 +193,7 @@ __device__ __forceinline__ void clean_role(const TreeParams& a, const Pipe& pipe
         const int nodes = it.n_rows / a.group, words = (it.n_nodes + 63) / 64;
 #pragma unroll 1
         for (int e = tid; e < nodes * words; e += 64)
-          pipe.node_mask[(qs * 32 + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + e / words, it.node0 + e / words, e % words);
+          pipe.node_mask[(qs * NARROW_ROWS + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + e / words, it.node0 + e / words, e % words);
       }
       __syncwarp();
       if (elect_one()) mbar_arrive(&pipe.q_full[qs]);
