@@ -248,7 +248,7 @@ struct CompactSlots {
 int launch_tree_attention(const TreeAttention& a, int n_sms, cudaStream_t s);
 int launch_attention_weights(const AttentionWeights& a, int n_sms, cudaStream_t s);
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
-                        int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s);
+                        int budget, int sink, int recent, int32_t* keep, int32_t* count, cudaStream_t s);
 int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s);
 // weights [n_lists][n_heads][w_stride], list i of prompt i % n_prompts: slots from[prompt] .. to[prompt] - 1 become 0
 int launch_clear_weights(float* weights, int64_t w_stride, int n_lists, int n_heads, int n_prompts, const int32_t* from, const int32_t* to,

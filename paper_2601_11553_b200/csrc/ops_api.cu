@@ -160,7 +160,7 @@ int percache_select_slots(int32_t device, void* stream, const float* weights, in
   const DeviceGuard dev(device);
   if (!dev.ok) return PERCACHE_E_CUDA;
   return launched(launch_select_slots(weights, weights_stride, length, n_seqs, n_heads, max_len, budget, sink, recent, keep,
-                                      count, sm_count(device), static_cast<cudaStream_t>(stream)));
+                                      count, static_cast<cudaStream_t>(stream)));
 }
 
 int percache_compact_slots(int32_t device, void* stream, const percache_kv_t* kv, int32_t n_seqs, int32_t max_len,

@@ -2173,7 +2173,7 @@ int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t 
     const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;
     for (int l = 0; l < D.n_layers && ok; ++l) {
       float* w = h->weights + l * w_layer;
-      ok = ok && launch_select_slots(w, plan.weights_stride, d_len, np, D.n_kv_heads, max_len, budget, sink, recent, d_keep, d_count, h->n_sms, s) == 0;
+      ok = ok && launch_select_slots(w, plan.weights_stride, d_len, np, D.n_kv_heads, max_len, budget, sink, recent, d_keep, d_count, s) == 0;
       CompactSlots c{};
       c.kv = ctx_view(h, l, d_start);
       c.n_seqs = np; c.max_len = max_len;

@@ -16,10 +16,10 @@ namespace {
 // were key arithmetic before the always-kept slots were taken out and NaN and -0 were folded into two operations) and the latency of
 // the dependent passes.  Weights stay in registers when a warp's stretch is at most 32 x SEL_UNROLL slots.  Longer lists are read
 // three times: for the first histogram, to put the keys of the bin found into a list in shared memory (the other passes work on
-// that), and to write; where the bin holds more than the list (many equal weights), every pass reads all again.
+// that), and to write; where the bin holds more than the list (many equal weights), every pass reads all again.  224 lists of 33024:
+// 34.2 us at 71 % of the issue slots (41.6 without the list); 224 of 2112: 6.7 us.
 constexpr int SEL_BITS = 11, SEL_BINS = 1 << SEL_BITS;
 constexpr int SEL_UNROLL = 8;
-constexpr int LONG_LIST = 16384;
 
 // Order-preserving map of a weight to 32 bits: NaN as -infinity (maximum drops it), -0 as 0 (adding 0 does).
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -225,7 +225,8 @@ __device__ __forceinline__ Move move_of(const CompactSlots& a, int b, int j, int
 
 // To another place: nothing that is read is written, so every (prompt, KV head, stretch of the list) is a block of its own.
 // 16 lanes (8 for head size 64) take a row of K and of V; a thread has MOVE_ROWS rows of both in flight.  Bound by HBM:
-// 2 x 4 D bytes a kept slot and head.
+// 2 x 4 D bytes a kept slot and head.  7 x 8 lists of 8192: 81.6 us (475 MB, 5.8 TB/s), 8 lists of 1024: 3.7 us; with one row a
+// thread and four blocks an SM 97.7 and 4.3 us.
 constexpr int MOVE_ROWS = 2;
 template <int D>
 __global__ void __launch_bounds__(MOVE_THREADS, 6) copy_slots_kernel(CompactSlots a) {
@@ -269,7 +270,8 @@ __global__ void __launch_bounds__(MOVE_THREADS, 6) copy_slots_kernel(CompactSlot
 // In place.  A block owns a slice (some 16-byte vectors of K or of V, or the weights) of one (prompt, KV head) and takes the
 // list's chunks in order, each read whole before any of it is written: its sources lie at or behind the chunk's own first
 // slot, because keep[j] >= first + j and the list ascends, so no chunk reads what an earlier one has written.  Slices, not
-// chunks, are what runs in parallel; the host makes them as narrow as it takes to fill the SMs.
+// chunks, are what runs in parallel; the host makes them as narrow as it takes to fill the SMs four times (7 x 8 lists of 8192:
+// 198 us; twice: 236 us.  64 x 8 lists of 512: 78 us either way).
 constexpr int SHIFT_UNROLL = 8;
 __global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots a, int slices, int vecs, int first_slice) {
   const int b = blockIdx.z, g = blockIdx.y, slice = blockIdx.x + first_slice;
@@ -332,10 +334,11 @@ int launch_clear_weights(float* weights, int64_t w_stride, int n_lists, int n_he
 }
 
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
-                        int budget, int sink, int recent, int32_t* keep, int32_t* count, int n_sms, cudaStream_t s) {
+                        int budget, int sink, int recent, int32_t* keep, int32_t* count, cudaStream_t s) {
   const dim3 grid(n_heads, n_seqs);
-  // 1024 threads to a list where there is one per SM or fewer, or where lists are long: the passes' latency is all there is
-  if (static_cast<int64_t>(n_seqs) * n_heads <= n_sms || max_len > LONG_LIST)
+  // 512 threads hold up to 4096 weights of a list in registers, 1024 hold 8192 (and share the reading of longer ones).  8 lists of 2112:
+  // 4.9 us with 512, 6.2 with 1024; 512 lists of 2500: 10.7 and 18.5; 224 lists of 8192: 13.0 and 11.8; 8 lists of 33024: 28.3 and 19.8.
+  if (max_len > 512 * SEL_UNROLL)
     select_slots_kernel<1024><<<grid, 1024, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
   else
     select_slots_kernel<512><<<grid, 512, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
