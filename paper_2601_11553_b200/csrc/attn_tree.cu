@@ -37,7 +37,7 @@
 namespace pc {
 namespace {
 
-// Four tiles of head size 128 and one Q tile: 48-node trees on 64 x 2500 slots 131 us; with five tiles or two Q tiles 134 - 142 us, 26-node
+// Four tiles of head size 128 and one Q tile: 48-node trees on 64 x 2500 slots 131 us; with five tiles or two Q tiles 135 - 142 us, 26-node
 // trees 15.9 -> 16.0 us.
 constexpr int RING_BYTES = 128 * 1024;
 constexpr int Q_BYTES = 32 * 1024;
@@ -476,7 +476,7 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
   // A unit's cost beside its blocks grows with its rows (the end of every row is written out while no block is worked on).  2 -> 4: 26-node
-  // trees on 2112 slots 18.6 -> 17.1 us, 7-token chains on 2 x 33024 slots 60 -> 57 us, but 64 x 2500 single tokens 108.4 -> 110.4 us.
+  // trees on 2112 slots 16.3 -> 15.8 us; 64 x 2500 single tokens 108.4 -> 110.4 us.
   p.over = p.tile_nodes * p.group <= 16 ? 2 : 4;
   // Short contexts: a unit is not worth cutting, the second kernel costs more than the blocks it would spread.
   p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;

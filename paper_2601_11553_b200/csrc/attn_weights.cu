@@ -6,7 +6,9 @@
 // never changes and no atomic is needed.  Only as many columns as there are rows (rounded up to 16) are computed.
 //
 // Bounds.  A block costs 32 KB of K (head size 128, 0.75 us of an SM's share of the HBM), at most 4.2 MFLOP (0.37 us) and
-// 16 K exponentials (0.55 us): bound by reading K once, so as in the attention the copies are what is kept running.
+// 16 K exponentials (0.55 us): bound by reading K once, so as in the attention the copies are what is kept running.  Measured: one
+// token on each of 64 x 2500 slots in pages 62.8 us (floor 52.4), the accepted half of 33 nodes on 2 x 33024 slots 31.2 us (21.7: some
+// 9 us are the call's start and the blocks of the longest share), one token on 2112 slots 7.4 us.
 //
 // Schedule as in the attention (spans of the batch's blocks), but a block belongs to one CTA: nothing is merged.
 // One CTA per SM, 384 threads: warp 8 copies (K ring, Q ring of two tiles), warp 9 issues the MMAs, warps 10-11 put the rows'
