@@ -393,18 +393,9 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(TreeParams
   const int head = *reinterpret_cast<const volatile int*>(&mr->head0) + r % a.group;
   // part 0 is the record's CTA's last item, part s > 0 the first item of the s-th CTA behind it
   auto slot = [&](int s) { return static_cast<size_t>(2 * (blockIdx.x + s) + (s == 0 ? 1 : 0)) * BLK + r; };
-  float M = -INFINITY;
+  // four parts at a time, with a running reference: their sums and results are asked for together
   bool any = true;
-  for (int s = lane; s < n_parts; s += 32) {
-    const float2 v = ld_dep_f32x2(a.partial_ml + slot(s) * 2);
-    M = fmaxf(M, v.x);
-    if (v.y < 0.f) any = false;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  any = __all_sync(0xffffffffu, any);
-  const float ref = M == -INFINITY ? 0.f : M;
-  float acc[E], L = 0.f;
+  float acc[E], M = -INFINITY, L = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   for (int s0 = 0; s0 < n_parts; s0 += 4) {
@@ -412,14 +403,23 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(TreeParams
     float o[4][E];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const size_t at = slot(min(s0 + u, n_parts - 1));
+      v[u] = make_float2(-INFINITY, 0.f);
+      if (s0 + u >= n_parts) continue;
+      const size_t at = slot(s0 + u);
       v[u] = ld_dep_f32x2(a.partial_ml + at * 2);
       if constexpr (E == 4) *reinterpret_cast<float4*>(o[u]) = ld_dep_f32x4(a.partial_o + at * HEAD_DIM + lane * 4);
       else *reinterpret_cast<float2*>(o[u]) = ld_dep_f32x2(a.partial_o + at * HEAD_DIM + lane * 2);
     }
+    const float top = fmaxf(fmax3(v[0].x, v[1].x, v[2].x), v[3].x), now = fmaxf(M, top), ref = now == -INFINITY ? 0.f : now;
+    const float before = fast_exp2(M - ref);
+    M = now;
+    L *= before;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] *= before;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (s0 + u >= n_parts) break;
+      if (v[u].y < 0.f) any = false;
       const float w = fast_exp2(v[u].x - ref);
       L = fmaf(w, v[u].y, L);
 #pragma unroll
