@@ -9,9 +9,9 @@
 // Bounds.  A block costs 64 KB of K and V (head size 128, 1.5 us of one SM's share of the HBM) and at most 8.4 MFLOP of
 // tensor work (0.75 us) and 16 K exponentials (0.55 us): with the tile at most 128 rows high the operator is bound by
 // reading K and V once, whatever the number of rows, and everything below serves to keep the copies running.  Measured,
-// 96 rows: 1.50 us a block (6.5 TB/s over 148 SMs), 1.06 us when all K and V are in L2, and 13 - 17 us of a call for its start,
+// 96 rows: 1.50 us a block (6.5 TB/s over 148 SMs), 1.06 us when all K and V are in L2, and 10 - 15 us of a call for its start,
 // the ends of its pieces and the merge: 48-node trees on 64 x 2500 slots in pages 128 us (floor 105), 26-node trees on
-// one prompt of 2112 slots 15.7 us.
+// one prompt of 2112 slots 12.7 us.
 //
 // Schedule.  Lengths live on the device, so the work is dealt there: every unit costs its blocks and a little more, the
 // batch's total cost is cut into one contiguous span per CTA, and a unit that a span border cuts is finished in parts
@@ -478,7 +478,9 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   // A unit's cost beside its blocks grows with its rows (the end of every row is written out while no block is worked on).  2 -> 4: 26-node
   // trees on 2112 slots 16.3 -> 15.8 us; 64 x 2500 single tokens 108.4 -> 110.4 us.
   p.over = p.tile_nodes * p.group <= 16 ? 2 : 4;
-  // Short contexts: a unit is not worth cutting, the second kernel costs more than the blocks it would spread.
+  // Short contexts: a unit is one CTA's, and there is no second kernel.  64 prompts of 700 slots: 50.4 against 53.1 us for trees, 42.2 against
+  // 43.3 for single tokens; one prompt of 300 slots 8.8 against 9.2 us.  Of 512 slots 10.9 against 9.5 us, but a second launch is 2 us
+  // of the host's time, which such a call is bound by unless it was captured.
   p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;
   const int64_t units = static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads;
   if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
