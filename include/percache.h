@@ -476,7 +476,7 @@ typedef struct {
 
 /* Attention of every node over the slots it sees: out[row][head] = softmax(scale * q . K) V in fp32, rounded once
  * to the pools' type on the way out (the softmax weights are rounded to that type before they multiply V, their sum is
- * not), and lse[row][head] = log of the sum of exp(scale * q . k) over those slots (fp32; may be NULL).  A row that
+ * not; with fp16 a weight below 2^-21 of the largest is off by up to 2^-32 of that instead), and lse[row][head] = log of the sum of exp(scale * q . k) over those slots (fp32; may be NULL).  A row that
  * sees nothing gets zeros and -inf.  q, out: [n_rows][n_q_heads][head_dim] with q_row_stride / out_row_stride elements
  * from row to row (multiples of 8, 16-byte aligned); n_q_heads a multiple of n_kv_heads with at most 128 query heads
  * per KV head.  scale > 0.  Slots a row does not see may hold anything, infinities and NaN included.

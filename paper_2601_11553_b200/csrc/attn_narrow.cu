@@ -217,7 +217,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
         ++n_s;
         uint32_t s[NC];
-        bool raise = j == i;                               // does any row's block maximum pass its reference by more than 2^8
+        bool raise = j == i;                               // does any row's block maximum pass what its reference allows
         if (ok) {
           tc_fence_after_sync();
           tmem_ld_32x16(lanes + i * NC, s);
@@ -249,7 +249,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
 #pragma unroll
             for (int c = c0; c < c0 + 4; ++c) {
               if (c >= it.n_rows) s[c] = 0xff800000u;                // columns behind the last row hold anything
-              raise |= fmaf(__uint_as_float(s[c]), a.scale_log2, neg[c]) > RESCALE_THRESHOLD;
+              raise |= fmaf(__uint_as_float(s[c]), a.scale_log2, neg[c]) > P_HEADROOM<BF16> + RESCALE_THRESHOLD;
             }
           }
           if (unset != 0) {
@@ -270,7 +270,7 @@ narrow_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           if (lane < NC) maxima[lane][quarter] = mine;
           parity_any(i, false);
           const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
-          const float now = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) * a.scale_log2;
+          const float now = fmaf(fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)), a.scale_log2, -P_HEADROOM<BF16>);    // the block's own reference
           float old = 0.f;
 #pragma unroll
           for (int c = 0; c < NC; ++c) old = lane == c ? neg[c] : old;

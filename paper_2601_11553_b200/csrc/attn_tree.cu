@@ -225,7 +225,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_cons
             mx2 = fmax3(mx2, __uint_as_float(s[c + 4]), __uint_as_float(s[c + 5]));
             mx3 = fmax3(mx3, __uint_as_float(s[c + 6]), __uint_as_float(s[c + 7]));
           }
-          const float m_blk = fmax3(fmaxf(mx0, mx1), mx2, mx3) * a.scale_log2;
+          const float m_blk = fmaf(fmax3(fmaxf(mx0, mx1), mx2, mx3), a.scale_log2, -P_HEADROOM<BF16>);       // the block's own reference
           if (j < 2) {
             m = m_blk;
           } else {

@@ -91,7 +91,13 @@ __device__ __forceinline__ float elem(uint32_t bits16) {
 }
 
 // ---------------------------------------------------------------------------------------------------- attention: shared roles
-constexpr float RESCALE_THRESHOLD = 8.0f;       // the running reference is raised when a block exceeds it by 2^8
+// The running reference lies P_HEADROOM (base 2) below the largest score that set it and is raised when a block exceeds that score by
+// RESCALE_THRESHOLD: the largest weight P of a row is between 2^P_HEADROOM and 2^(P_HEADROOM + RESCALE_THRESHOLD).  A 16-bit P has to hold the
+// small weights of a long context, which together may be all of the result (a few heavy slots with values near 0): fp16 rounds what is
+// below 2^-14 to multiples of 2^-24, so with the largest at 2^7 or more a weight is off by at most 2^-32 of it (without the headroom 2^-25: of
+// 2500 slots under two of a score 17.5 higher nothing was left), and at 2^15 it still fits.  bf16 has fp32's exponents.
+constexpr float RESCALE_THRESHOLD = 8.0f;
+template <bool BF16> constexpr float P_HEADROOM = BF16 ? 0.f : 7.f;
 // Least cost of an attention span (in blocks; a unit's own cost counts).  4 -> 2: 26-node trees on one prompt of 2112 slots 14.4 -> 12.7 us,
 // one token on 1000 slots 10.9 -> 9.6; 1: 13.2 and 9.5.
 constexpr int MIN_SPAN = 2;

@@ -1,0 +1,45 @@
+"""Calls of the cache operators that once gave wrong results, wrong errors or none."""
+import numpy as np
+import pytest
+
+from paper_2601_11553_b200 import percache as pcb
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("n_seqs,ctx,hkv", [(1, 700, 1), (16, 2500, 8)])
+@pytest.mark.parametrize("nodes", [1, 20])
+def test_many_small_fp16_weights_are_not_lost(nodes, n_seqs, ctx, hkv):
+    """Two slots (one in a block of each parity) have a score of 17.5 and values of 0, all others a score of 0 and values of 1000,
+    so an output is 1000 n / (2 e^17.5 + n): each of the n weights is below 2^-25 of the largest, together they are the output.
+
+    Tolerance.  Scores are exact.  An exponential and a row sum are off by 2^-19 relative, rounding to fp16 by 2^-11 of a weight, plus
+    2^-32 of the largest where the weight is subnormal (multiples of 2^-24, the largest weight at 2^7 or more); the output is
+    rounded once more (2^-11 relative; 2^-25 where it is subnormal)."""
+    q_heads, d = 2 * hkv, 128
+    t = ctx + nodes
+    k = torch.zeros((n_seqs * t, hkv, d), dtype=torch.float16, device="cuda")
+    v = torch.full((n_seqs * t, hkv, d), 1000.0, dtype=torch.float16, device="cuda")
+    for b in range(n_seqs):
+        for s in (3, 130):
+            k[b * t + s, :, 0] = 17.5
+            v[b * t + s] = 0.0
+    q = torch.zeros((n_seqs * nodes, q_heads, d), dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 1.0
+    out = torch.full_like(q, 7.0)
+    lse = torch.zeros((n_seqs * nodes, q_heads), device="cuda")
+    ws = torch.zeros(pcb.OPS_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    pcb.tree_attention(q, k, v, out, lse, ctx_len=torch.full((n_seqs,), ctx, dtype=torch.int32, device="cuda"),
+                       row_start=torch.arange(0, n_seqs * nodes + 1, nodes, dtype=torch.int32, device="cuda"),
+                       ctx_start=torch.arange(0, n_seqs * t, t, dtype=torch.int32, device="cuda"), max_nodes=nodes, max_len=t,
+                       scale=1.0, workspace=ws)
+    pcb.ops_status(ws)
+    got = out.double().cpu().numpy().reshape(n_seqs, nodes, q_heads, d)
+    for i in range(nodes):                                  # node i sees ctx + i + 1 slots
+        n = ctx + i + 1 - 2
+        total = 2 * np.exp(17.5) + n
+        want = 1000.0 * n / total
+        tol = (2.0 ** -10 + 2.0 ** -18) * want + 1000.0 * n * 2.0 ** -32 + 2.0 ** -25
+        assert np.abs(got[:, i] - want).max() <= tol, (i, want, np.abs(got[:, i] - want).max(), tol)
+        assert np.abs(lse.view(n_seqs, nodes, q_heads)[:, i].double().cpu().numpy() - np.log(total)).max() <= 2.0 ** -19 * 18
