@@ -251,9 +251,12 @@ PERCACHE_API int percache_accept(percache_t* h, int32_t n_prompts, const int32_t
  * (sink + recent <= budget) and the ones with the most running attention weight, equal weights going to the lower slot.
  * The weights are those that percache_decode and percache_accept have added while PERCACHE_FLAG_TRACK_WEIGHTS was set,
  * since the prefill (every step first multiplies the sums by the decay of percache_set_weight_decay, 1 at creation);
- * without any such step, or while a tree's nodes wait for percache_accept, PERCACHE_E_INVAL.  Positions are not touched: later tokens continue at theirs, and the freed
- * slots are free for them (they count towards the decode reserve).  percache_debug_read_ctx and read_weights then see
- * the slots that are left.  Synchronous. */
+ * without any such step, or while a tree's nodes wait for percache_accept, PERCACHE_E_INVAL.  A tracked step or a
+ * percache_accept that returns PERCACHE_E_CUDA or PERCACHE_E_DEVICE_TIMEOUT ends the sums (some layers may have been added to
+ * and others not; the context stays as it was, nodes to be accepted are dropped): the next tracked step starts them
+ * from zero.  An eviction that returns PERCACHE_E_CUDA ends the batch.  Positions are not touched: later tokens continue at
+ * theirs, and the freed slots are free for them (they count towards the decode reserve).  percache_debug_read_ctx and
+ * read_weights then see the slots that are left.  Synchronous. */
 PERCACHE_API int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t recent);
 PERCACHE_API int percache_set_weight_decay(percache_t* h, float decay);
 
@@ -358,6 +361,11 @@ PERCACHE_API int percache_debug_attn_plan(const int32_t* n_blocks, int32_t n_til
  * prefill that needs more than the capacity fails with PERCACHE_E_CAPACITY before anything runs.  The copies
  * serialise the call's kernels: never leave this on while timing. */
 PERCACHE_API int percache_debug_capture_layers(percache_t* h, float* host_buf, int64_t capacity_floats);
+
+/* Test aid: the next decode step through the tree attention, percache_accept or percache_evict_context that gets to decoder
+ * block `layer` (-1: none, the default) treats the launch of its cache operators there as failed, on the host: it
+ * launches none of them from that block on and returns PERCACHE_E_CUDA. */
+PERCACHE_API int percache_debug_fail_layer(percache_t* h, int32_t layer);
 
 /* Assembled context of the last call: rotated K and V of one prompt and layer as fp16
  * [n_total + tokens decoded since][n_kv_heads][head_dim], copied to host buffers that hold capacity_tokens tokens

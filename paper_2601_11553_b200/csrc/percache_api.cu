@@ -107,6 +107,7 @@ struct percache {
   std::vector<int32_t> retained_scratch;   // pages of rows that are not stored, kept for that late assembly
   float* capture_host = nullptr;   // debugging aid: layer inputs of the next calls are copied here (see header)
   int64_t capture_capacity = 0;    // floats
+  int32_t fail_layer = -1;         // debugging aid: where the next step on the context reports a failed launch (see header)
   int32_t decode_reserve = 0;     // context slots kept free behind every prompt for percache_decode
   // steps over drafted tokens and tracked steps (allocated when the first one runs)
   void* tree_ws = nullptr;         // workspace of the tree attention; its first word is an error word
@@ -341,6 +342,13 @@ DevIndex dev_index(const percache* h) {
   return ix;
 }
 
+// Does percache_debug_fail_layer want the operators of block l to have failed?  Once.
+bool fails_at(percache* h, int l) {
+  if (h->fail_layer != l) return false;
+  h->fail_layer = -1;
+  return true;
+}
+
 // A step whose attention is the tree attention (drafted tokens; tracked steps; steps after an eviction): the arguments that are the
 // same for every layer, and what the running weights need.
 struct TreeStep {
@@ -422,6 +430,7 @@ bool run_layers(percache* h, int Mi, const DevIndex& ix, int n_attn_ctas, int n_
     timer.begin(PERCACHE_PH_ATTN);
     if (overlap_gather) ok = ok && cudaStreamWaitEvent(s, h->ev_gather[l], 0) == cudaSuccess;
     if (tree) {
+      if (fails_at(h, l)) ok = false;
       TreeAttention a = tree->attn;
       a.kv.k = qe.kctx; a.kv.v = qe.vctx;
       a.q = h->qbuf; a.out = h->attn_out;
@@ -695,8 +704,15 @@ int decode_rows(percache* h, int32_t n_prompts, const int32_t* n_nodes, const in
        cudaMemcpyAsync(&ws_err, h->tree_ws, sizeof(int), cudaMemcpyDeviceToHost, s) == cudaSuccess;
   timer.end();
   const cudaError_t sync_rc = cudaStreamSynchronize(s);
-  if (!ok || sync_rc != cudaSuccess || cudaGetLastError() != cudaSuccess) return PERCACHE_E_CUDA;
-  if (*h->h_err != 0 || ws_err != 0) return PERCACHE_E_DEVICE_TIMEOUT;
+  // A step that fails may have added its weights in some layers and not in others: the sums end.  (Its K and V lie in free slots.)
+  if (!ok || sync_rc != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+    if (step.weights) plan.weights_on = false;
+    return PERCACHE_E_CUDA;
+  }
+  if (*h->h_err != 0 || ws_err != 0) {
+    if (step.weights) plan.weights_on = false;
+    return PERCACHE_E_DEVICE_TIMEOUT;
+  }
   if (assemble) assembled(h);
   if (track && !plan.weights_on) { plan.weights_on = true; plan.weights_stride = static_cast<int32_t>(new_stride); }
   if (n_nodes) {
@@ -1878,6 +1894,12 @@ int percache_debug_capture_layers(percache_t* h, float* host_buf, int64_t capaci
   return PERCACHE_OK;
 }
 
+int percache_debug_fail_layer(percache_t* h, int32_t layer) {
+  if (!h || layer < -1 || layer >= h->dims.n_layers) return PERCACHE_E_INVAL;
+  h->fail_layer = layer;
+  return PERCACHE_OK;
+}
+
 int percache_set_decode_reserve(percache_t* h, int32_t tokens_per_prompt) {
   if (!h || tokens_per_prompt < 0) return PERCACHE_E_INVAL;
   h->decode_reserve = tokens_per_prompt;
@@ -2102,6 +2124,7 @@ int percache_accept(percache_t* h, int32_t n_prompts, const int32_t* n_accept, c
     const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;
     for (int l = 0; l < D.n_layers && ok; ++l) {
       const KvView kv = ctx_view(h, l, h->tree_ints + 2 * n + 1);
+      if (fails_at(h, l)) ok = false;
       if (plan.tree_tracked) {
         AttentionWeights w{};
         w.kv = kv;
@@ -2131,8 +2154,16 @@ int percache_accept(percache_t* h, int32_t n_prompts, const int32_t* n_accept, c
     ok = ok && cudaMemcpyAsync(&ws_err, h->tree_ws, sizeof(int), cudaMemcpyDeviceToHost, s) == cudaSuccess;
     const cudaError_t rc = cudaStreamSynchronize(s);
     plan.tree_n.clear();
-    if (!ok || rc != cudaSuccess || cudaGetLastError() != cudaSuccess) return PERCACHE_E_CUDA;
-    if (ws_err != 0) return PERCACHE_E_DEVICE_TIMEOUT;
+    // Failed: the nodes are dropped (what moved lies behind the context), and the sums, which some layers have added to, decayed or
+    // moved and others not, end.
+    if (!ok || rc != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+      plan.weights_on = false;
+      return PERCACHE_E_CUDA;
+    }
+    if (ws_err != 0) {
+      plan.weights_on = false;
+      return PERCACHE_E_DEVICE_TIMEOUT;
+    }
     for (int b = 0; b < n_prompts; ++b) plan.dec_len[b] += n_accept[b];
     return PERCACHE_OK;
   } catch (const std::bad_alloc&) {
@@ -2173,6 +2204,7 @@ int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t 
     const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;
     for (int l = 0; l < D.n_layers && ok; ++l) {
       float* w = h->weights + l * w_layer;
+      if (fails_at(h, l)) ok = false;
       ok = ok && launch_select_slots(w, plan.weights_stride, d_len, np, D.n_kv_heads, max_len, budget, sink, recent, d_keep, d_count, s) == 0;
       CompactSlots c{};
       c.kv = ctx_view(h, l, d_start);

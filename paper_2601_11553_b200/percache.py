@@ -35,7 +35,7 @@ PHASES = ("gather", "norm", "qkv", "attn", "oproj", "gateup", "down", "io")
 EXPORTS = ("percache_create", "percache_destroy", "percache_put_chunk_kv", "percache_prefill",
            "percache_has_chunk", "percache_drop_chunk", "percache_get_chunk_kv", "percache_get_chunk_q", "percache_put_chunk_synthetic",
            "percache_get_stats", "percache_set_flags", "percache_decode", "percache_set_decode_reserve", "percache_set_store_limit", "percache_chunk_info", "percache_debug_read_plan", "percache_debug_read_ctx", "percache_debug_attn_plan",
-           "percache_debug_gemm", "percache_debug_gemm_noalloc", "percache_debug_capture_layers", "percache_debug_wait_probe", "percache_path_key", "percache_qa_top1", "percache_tree_attention",
+           "percache_debug_gemm", "percache_debug_gemm_noalloc", "percache_debug_capture_layers", "percache_debug_fail_layer", "percache_debug_wait_probe", "percache_path_key", "percache_qa_top1", "percache_tree_attention",
            "percache_decode_tree", "percache_accept", "percache_evict_context", "percache_set_weight_decay",
            "percache_debug_read_weights", "percache_attention_weights", "percache_select_slots", "percache_compact_slots", "percache_ops_status", "percache_strerror")
 
@@ -131,6 +131,7 @@ def load_library() -> C.CDLL:
     lib.percache_debug_gemm.argtypes = [i32, i32, i32, i32, vp, vp, vp, i32]
     lib.percache_debug_gemm_noalloc.argtypes = [i32, i32, i32, i32, vp, vp, vp]
     lib.percache_debug_capture_layers.argtypes = [vp, vp, i64]
+    lib.percache_debug_fail_layer.argtypes = [vp, i32]
     lib.percache_debug_wait_probe.argtypes = [i32, C.c_uint32, C.POINTER(i32), C.POINTER(u64)]
     lib.percache_qa_top1.argtypes = [i32, vp, vp, i32, i32, vp, i32, C.c_float, vp, vp, vp, C.POINTER(C.c_float)]
     f32, kvp, rowsp = C.c_float, C.POINTER(KvStruct), C.POINTER(RowsStruct)
@@ -392,6 +393,10 @@ class PerCache:
 
     def set_weight_decay(self, decay: float) -> None:
         _check(self._lib.percache_set_weight_decay(self._h, float(decay)), "percache_set_weight_decay")
+
+    def fail_layer(self, layer: int) -> None:
+        """percache_debug_fail_layer: a test aid."""
+        _check(self._lib.percache_debug_fail_layer(self._h, int(layer)), "percache_debug_fail_layer")
 
     def read_weights(self, prompt: int, layer: int, slots: int, n_kv_heads: int) -> np.ndarray:
         """Running attention weights of one prompt and layer: float32 [n_kv_heads, slots of its context]."""
