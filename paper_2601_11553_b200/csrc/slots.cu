@@ -320,8 +320,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots 
 
 __global__ void __launch_bounds__(MOVE_THREADS) clear_weights_kernel(float* weights, int64_t w_stride, int n_prompts, const int32_t* __restrict__ from,
                                                                      const int32_t* __restrict__ to) {
-  const int b = blockIdx.y % n_prompts;
-  float* w = weights + (static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * w_stride;
+  const int b = blockIdx.x % n_prompts;                  // a list is a layer and a prompt: more than a grid's other dimensions hold
+  float* w = weights + (static_cast<size_t>(blockIdx.x) * gridDim.y + blockIdx.y) * w_stride;
   for (int s = __ldg(from + b) + threadIdx.x; s < __ldg(to + b); s += MOVE_THREADS) w[s] = 0.f;
 }
 
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) clear_weights_kernel(float* weig
 
 int launch_clear_weights(float* weights, int64_t w_stride, int n_lists, int n_heads, int n_prompts, const int32_t* from, const int32_t* to,
                          cudaStream_t s) {
-  clear_weights_kernel<<<dim3(n_heads, n_lists), MOVE_THREADS, 0, s>>>(weights, w_stride, n_prompts, from, to);
+  clear_weights_kernel<<<dim3(n_lists, n_heads), MOVE_THREADS, 0, s>>>(weights, w_stride, n_prompts, from, to);
   return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
 }
 

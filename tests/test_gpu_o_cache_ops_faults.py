@@ -43,3 +43,34 @@ def test_many_small_fp16_weights_are_not_lost(nodes, n_seqs, ctx, hkv):
         tol = (2.0 ** -10 + 2.0 ** -18) * want + 1000.0 * n * 2.0 ** -32 + 2.0 ** -25
         assert np.abs(got[:, i] - want).max() <= tol, (i, want, np.abs(got[:, i] - want).max(), tol)
         assert np.abs(lse.view(n_seqs, nodes, q_heads)[:, i].double().cpu().numpy() - np.log(total)).max() <= 2.0 ** -19 * 18
+
+
+def small_handle(n_prompts, n_layers, reserve, **kw):
+    """A handle after a prefill of n_prompts equal prompts of one token each."""
+    from paper_2601_11553_b200 import workloads as wl
+    shape = wl.ModelShape(n_layers=n_layers, d_model=256, n_q_heads=4, n_kv_heads=2, head_dim=128, d_ffn=512)
+    weights = wl.make_weights(shape, 5, random_gains=True)
+    h = pcb.PerCache(n_layers=n_layers, d_model=256, n_q_heads=4, n_kv_heads=2, head_dim=128, d_ffn=512, weights=weights, pool_pages=16,
+                     max_prompt_tokens=1 + reserve, max_batch_prompts=n_prompts, max_batch_ctx_tokens=n_prompts * (1 + reserve),
+                     max_batch_new_rows=n_prompts * 4, rope_theta=shape.rope_theta, rms_eps=shape.rms_eps, flags=pcb.FLAG_TRACK_WEIGHTS, **kw)
+    h.set_decode_reserve(reserve)
+    one = wl.make_hidden(5, (1,), 1, 256)
+    h.prefill([pcb.PromptSpec([], [], [], one, 1) for _ in range(n_prompts)])
+    return h, wl.make_hidden(5, (2,), 1, 256)
+
+
+def test_running_weights_of_more_layers_and_prompts_than_a_grid_has_rows():
+    n = 65535 // 28 + 1                                     # 28 layers: 65 548 lists of two heads
+    h, token = small_handle(n, 28, 3)
+    with h:
+        tokens = np.ascontiguousarray(np.repeat(token, n, axis=0))
+        h.decode_tree([[-1, -1]] * n, np.ascontiguousarray(np.repeat(token, 2 * n, axis=0)))
+        h.accept([[1]] * n)              # moves the second node's weight to the first one's slot, and clears its own
+        h.decode(tokens)                 # this token takes the slot that was cleared
+        for layer in (0, 27):
+            for b in (0, n - 1):
+                w = h.read_weights(b, layer, 3, 2)
+                # two rows, two heads a KV head.  A weight is off by its exponent's error: 2^-22 (|score| + |lse|), both far below 16
+                assert np.abs(w.sum(1) - 4.0).max() <= 4 * 2.0 ** -17, (layer, b, w)
+        h.evict_context(1)
+        assert h.read_weights(n - 1, 27, 1, 2).shape == (2, 1)
