@@ -511,7 +511,7 @@ PERCACHE_API int percache_attention_weights(int32_t device, void* stream, const 
 /* The slots to keep: of the length[b] slots of prompt b and every head, all when there are at most `budget`, else
  * `budget` of them: the first `sink`, the last `recent` (sink + recent <= budget), and the heaviest of the rest, equal
  * weights going to the lower slot (NaN counts as -infinity).  weights: fp32 [n_seqs][n_heads][weights_stride],
- * weights_stride >= max_len.  keep: int32 [n_seqs][n_heads][budget], ascending, -1 behind the last one;
+ * weights_stride >= max_len, at most 65535 heads.  keep: int32 [n_seqs][n_heads][budget], ascending, -1 behind the last one;
  * count[b] = min(length[b], budget).  budget: at most 2^26. */
 PERCACHE_API int percache_select_slots(int32_t device, void* stream, const float* weights, int64_t weights_stride,
                                        const int32_t* length, int32_t n_seqs, int32_t n_heads, int32_t max_len,
@@ -524,7 +524,7 @@ PERCACHE_API int percache_select_slots(int32_t device, void* stream, const float
  * dst_page_table / dst_start (as page_table / ctx_start of kv) NULL: in place; a list must then be strictly ascending
  * with keep[j] >= first + j, and no two prompts may share rows.  Else the destination's rows must not be rows that are
  * read, nor each other's.  weights_in and weights_out
- * may be the same array under the same rule as in place, with weights_stride >= max_len. */
+ * may be the same array under the same rule as in place, with weights_stride >= max_len.  At most 65535 KV heads. */
 PERCACHE_API int percache_compact_slots(int32_t device, void* stream, const percache_kv_t* kv, int32_t n_seqs,
                                         int32_t max_len, const int32_t* dst_page_table,
                                         int32_t dst_page_table_stride, const int32_t* dst_start, const int32_t* first,

@@ -169,7 +169,7 @@ int percache_compact_slots(int32_t device, void* stream, const percache_kv_t* kv
                            const int32_t* count, const float* weights_in, float* weights_out, int64_t weights_stride) {
   if (n_seqs == 0) return PERCACHE_OK;
   if (max_len < 1 || max_len > MAX_CONTEXT || !kv_ok(kv, max_len, true) || n_seqs < 0 || n_seqs > 65535 || !keep || !count ||
-      budget < 1 || (keep_heads != 1 && keep_heads != kv->n_kv_heads) || (dst_page_table && dst_start) ||
+      kv->n_kv_heads > 65535 || budget < 1 || (keep_heads != 1 && keep_heads != kv->n_kv_heads) || (dst_page_table && dst_start) ||
       (kv->page_table ? dst_start != nullptr : dst_page_table != nullptr) ||
       ((weights_in == nullptr) != (weights_out == nullptr)) || (weights_in && weights_stride < max_len) ||
       // destination slots are first + j <= max_len - 1, but a table only has to cover those that are written
