@@ -234,7 +234,8 @@ PERCACHE_API int percache_decode(percache_t* h, int32_t n_prompts, const void* h
  * the prompt's tokens so far and attends to the prompt's context, its ancestors and itself, exactly as if the path to it
  * had been decoded token by token.  The nodes' K and V lie behind the context, one slot each (the decode reserve has to
  * hold them: PERCACHE_E_CAPACITY), until percache_accept keeps a path of them; any other decode or prefill call drops
- * them.  Synchronous; same errors as percache_decode.  After a gather-free prefill the first such call assembles the
+ * them.  Synchronous; same errors as percache_decode; at most 65535 prompts (PERCACHE_E_CAPACITY), as for a
+ * percache_decode with PERCACHE_FLAG_TRACK_WEIGHTS.  After a gather-free prefill the first such call assembles the
  * context, whatever the flags. */
 PERCACHE_API int percache_decode_tree(percache_t* h, int32_t n_prompts, const int32_t* n_nodes, const int32_t* parents,
                                       const void* hidden, int32_t hidden_on_device, float* out_hidden,

@@ -593,6 +593,7 @@ int decode_rows(percache* h, int32_t n_prompts, const int32_t* n_nodes, const in
   const int d = D.d_model, L = D.n_layers;
   const bool track = (h->flags & PERCACHE_FLAG_TRACK_WEIGHTS) != 0;
   // ---- sizes and checks
+  if (n_prompts > 65535) return PERCACHE_E_CAPACITY;         // what selection and moves, which may follow, can take
   int64_t rows = 0;
   int32_t max_n = 1, max_len = 1;
   for (int b = 0; b < n_prompts; ++b) {

@@ -74,3 +74,15 @@ def test_running_weights_of_more_layers_and_prompts_than_a_grid_has_rows():
                 assert np.abs(w.sum(1) - 4.0).max() <= 4 * 2.0 ** -17, (layer, b, w)
         h.evict_context(1)
         assert h.read_weights(n - 1, 27, 1, 2).shape == (2, 1)
+
+
+def test_more_prompts_than_the_moves_can_take_are_refused_before_anything_runs():
+    h, token = small_handle(65536, 1, 2)
+    with h:
+        tokens = np.ascontiguousarray(np.repeat(token, 65536, axis=0))
+        for call in (lambda: h.decode_tree([[-1]] * 65536, tokens), lambda: h.decode(tokens)):
+            with pytest.raises(pcb.PerCacheError) as e:
+                call()
+            assert e.value.code == pcb.E_CAPACITY
+        h.set_flags(0)
+        h.decode(tokens)                                    # plain steps go on
