@@ -325,12 +325,21 @@ __global__ void __launch_bounds__(MOVE_THREADS) clear_weights_kernel(float* weig
   for (int s = __ldg(from + b) + threadIdx.x; s < __ldg(to + b); s += MOVE_THREADS) w[s] = 0.f;
 }
 
+// <<<>>> with the launch's own status: the thread's last error may be an earlier call's.
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int threads, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = s;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
 }  // namespace
 
 int launch_clear_weights(float* weights, int64_t w_stride, int n_lists, int n_heads, int n_prompts, const int32_t* from, const int32_t* to,
                          cudaStream_t s) {
-  clear_weights_kernel<<<dim3(n_lists, n_heads), MOVE_THREADS, 0, s>>>(weights, w_stride, n_prompts, from, to);
-  return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
+  return launch(clear_weights_kernel, dim3(n_lists, n_heads), MOVE_THREADS, s, weights, w_stride, n_prompts, from, to) == cudaSuccess ? 0 : -1;
 }
 
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,
@@ -338,11 +347,9 @@ int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* l
   const dim3 grid(n_heads, n_seqs);
   // 512 threads hold up to 4096 weights of a list in registers, 1024 hold 8192 (and share the reading of longer ones).  8 lists of 2112:
   // 4.9 us with 512, 6.2 with 1024; 512 lists of 2500: 10.7 and 18.5; 224 lists of 8192: 13.0 and 11.8; 8 lists of 33024: 28.3 and 19.8.
-  if (max_len > 512 * SEL_UNROLL)
-    select_slots_kernel<1024><<<grid, 1024, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
-  else
-    select_slots_kernel<512><<<grid, 512, 0, s>>>(weights, w_stride, length, n_heads, max_len, budget, sink, recent, keep, count);
-  return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
+  const bool large = max_len > 512 * SEL_UNROLL;
+  return launch(large ? select_slots_kernel<1024> : select_slots_kernel<512>, grid, large ? 1024 : 512, s, weights, w_stride, length, n_heads,
+                max_len, budget, sink, recent, keep, count) == cudaSuccess ? 0 : -1;
 }
 
 int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s) {
@@ -352,16 +359,16 @@ int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s) {
   if (!in_place) {
     const int rows = MOVE_THREADS / vecs * MOVE_ROWS;
     const dim3 grid((n + rows - 1) / rows, a.kv.n_kv_heads, a.n_seqs);
-    if (a.kv.head_dim == 128) copy_slots_kernel<128><<<grid, MOVE_THREADS, 0, s>>>(a);
-    else copy_slots_kernel<64><<<grid, MOVE_THREADS, 0, s>>>(a);
+    if (launch(a.kv.head_dim == 128 ? copy_slots_kernel<128> : copy_slots_kernel<64>, grid, MOVE_THREADS, s, a) != cudaSuccess) return -1;
   }
   if (in_place || shift_weights) {
     int slices = 1;
     while (slices < vecs / 2 && static_cast<int64_t>(a.n_seqs) * a.kv.n_kv_heads * 2 * slices < 4 * static_cast<int64_t>(n_sms)) slices *= 2;
     const int first_slice = in_place ? 0 : 2 * slices, last = 2 * slices + (shift_weights ? 1 : 0);
-    shift_slots_kernel<<<dim3(last - first_slice, a.kv.n_kv_heads, a.n_seqs), MOVE_THREADS, 0, s>>>(a, slices, vecs / slices, first_slice);
+    const dim3 grid(last - first_slice, a.kv.n_kv_heads, a.n_seqs);
+    if (launch(shift_slots_kernel, grid, MOVE_THREADS, s, a, slices, vecs / slices, first_slice) != cudaSuccess) return -1;
   }
-  return cudaPeekAtLastError() == cudaSuccess ? 0 : -1;
+  return 0;
 }
 
 }  // namespace pc

@@ -86,3 +86,46 @@ def test_more_prompts_than_the_moves_can_take_are_refused_before_anything_runs()
             assert e.value.code == pcb.E_CAPACITY
         h.set_flags(0)
         h.decode(tokens)                                    # plain steps go on
+
+
+def leave_an_error_behind(h, token):
+    """A decode step on a stream that is being captured is refused by the runtime (a host-side error; nothing runs)."""
+    import ctypes as C
+    cu = C.CDLL("libcuda.so.1")
+    side = C.c_void_p(h.test_stream.cuda_stream)
+    assert cu.cuStreamBeginCapture_v2(side, 2) == 0
+    try:
+        with pytest.raises(pcb.PerCacheError) as e:
+            h.decode(token)
+        assert e.value.code == pcb.E_CUDA
+    finally:
+        graph = C.c_void_p()
+        cu.cuStreamEndCapture(side, C.byref(graph))
+        if graph.value:
+            cu.cuGraphDestroy(graph)
+
+
+def handle_on_a_stream():
+    side = torch.cuda.Stream()
+    h, token = small_handle(1, 1, 12, stream=side.cuda_stream)
+    h.test_stream = side
+    h.decode(token)                                         # memory that the first step takes is there
+    return h, token
+
+
+def test_selection_and_moves_report_their_own_launch_only():
+    h, token = handle_on_a_stream()
+    with h:
+        w = torch.rand((1, 2, 100), device="cuda")
+        length = torch.tensor([100], dtype=torch.int32).cuda()
+        keep = torch.empty((1, 2, 10), dtype=torch.int32, device="cuda")
+        count = torch.empty(1, dtype=torch.int32, device="cuda")
+        k = torch.randn((100, 2, 128), device="cuda").half()
+        start = torch.zeros(1, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        leave_an_error_behind(h, token)
+        pcb.select_slots(w, length, keep, count)
+        leave_an_error_behind(h, token)
+        pcb.compact_slots(k, k.clone(), keep, count, max_len=100, ctx_start=start)
+        torch.cuda.synchronize()
+        assert sorted(keep[0, 0].tolist()) == sorted(torch.topk(w[0, 0], 10).indices.tolist())
