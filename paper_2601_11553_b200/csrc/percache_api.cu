@@ -661,6 +661,7 @@ int decode_rows(percache* h, int32_t n_prompts, const int32_t* n_nodes, const in
   }
   const double plan_us = std::chrono::duration<double, std::micro>(std::chrono::steady_clock::now() - t_host0).count();
   // ---- device work
+  cudaGetLastError();                // an earlier call's error is not this step's
   cudaStream_t s = h->stream;
   percache_stats_t& st = h->stats;
   std::memset(st.phase_us, 0, sizeof(st.phase_us));
@@ -2120,6 +2121,7 @@ int percache_accept(percache_t* h, int32_t n_prompts, const int32_t* n_accept, c
     }
     cudaStream_t s = h->stream;
     if (!dev_grow(h, &h->keep, &h->keep_cap, ints.size())) return PERCACHE_E_NOMEM;
+    cudaGetLastError();              // an earlier call's error is not this one's
     bool ok = cudaMemcpyAsync(h->keep, ints.data(), ints.size() * sizeof(int32_t), cudaMemcpyHostToDevice, s) == cudaSuccess &&
               cudaMemsetAsync(h->tree_ws, 0, 256, s) == cudaSuccess;
     const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;
@@ -2200,6 +2202,7 @@ int percache_evict_context(percache_t* h, int32_t budget, int32_t sink, int32_t 
     if (max_len <= budget) return PERCACHE_OK;
     cudaStream_t s = h->stream;
     if (!dev_grow(h, &h->keep, &h->keep_cap, 4 * n + n * D.n_kv_heads * budget)) return PERCACHE_E_NOMEM;
+    cudaGetLastError();              // an earlier call's error is not this one's (and must not end the batch)
     int32_t *d_len = h->keep, *d_start = d_len + n, *d_new = d_start + n, *d_count = d_new + n, *d_keep = d_count + n;
     bool ok = cudaMemcpyAsync(h->keep, ints.data(), ints.size() * sizeof(int32_t), cudaMemcpyHostToDevice, s) == cudaSuccess;
     const size_t w_layer = n * D.n_kv_heads * plan.weights_stride;

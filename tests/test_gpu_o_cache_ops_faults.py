@@ -129,3 +129,20 @@ def test_selection_and_moves_report_their_own_launch_only():
         pcb.compact_slots(k, k.clone(), keep, count, max_len=100, ctx_start=start)
         torch.cuda.synchronize()
         assert sorted(keep[0, 0].tolist()) == sorted(torch.topk(w[0, 0], 10).indices.tolist())
+
+
+def test_steps_on_a_handle_report_their_own_errors_only():
+    h, token = handle_on_a_stream()
+    with h:
+        leave_an_error_behind(h, token)
+        h.decode(token)
+        leave_an_error_behind(h, token)
+        h.decode_tree([[-1, 0]], np.ascontiguousarray(np.repeat(token, 2, axis=0)))
+        # (a step that fails drops the nodes, so the error before accept comes from another handle)
+        other, t = handle_on_a_stream()
+        with other:
+            leave_an_error_behind(other, t)
+            h.accept([[0, 1]])
+            leave_an_error_behind(other, t)
+            h.evict_context(2)
+        h.decode(token)
