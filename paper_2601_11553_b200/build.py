@@ -36,9 +36,11 @@ def _deps_mtime() -> float:
     return max(os.path.getmtime(p) for p in paths)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and all(os.path.exists(p) and os.path.getmtime(p) >= _deps_mtime() for p in (LIB_PATH, BINDING_PATH)):
-        return LIB_PATH
+def _current(path: str) -> bool:
+    return os.path.exists(path) and os.path.getmtime(path) >= _deps_mtime()
+
+
+def build_library(verbose: bool = False) -> None:
     os.makedirs(OBJ_DIR, exist_ok=True)
     nvcc = _nvcc()
 
@@ -54,24 +56,40 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    def compile_binding() -> None:
-        tmp = BINDING_PATH + ".tmp"
-        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
-               "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "ops_binding.cpp"), "-o", tmp]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"{cmd[0]} failed for ops_binding.cpp:\n{r.stdout}\n{r.stderr}")
-        os.replace(tmp, BINDING_PATH)
-
-    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        binding = ex.submit(compile_binding)
+    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
         objs = list(ex.map(compile_one, SOURCES))
-        binding.result()
     tmp = LIB_PATH + ".tmp"
     r = subprocess.run([nvcc, "-shared", "-o", tmp, *objs, "-cudart", "static"], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB_PATH)
+
+
+def build_binding() -> None:
+    tmp = BINDING_PATH + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "ops_binding.cpp"), "-o", tmp]
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        raise RuntimeError(f"{cmd[0]} failed for ops_binding.cpp: {e}") from e
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for ops_binding.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING_PATH)
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    """The library, and the binding where it can be compiled (it needs Python's headers and a host compiler, the library does not
+    need it): without it the cache operators' Python functions raise, and all else works."""
+    if force or not _current(LIB_PATH):
+        build_library(verbose)
+    if force or not _current(BINDING_PATH):
+        try:
+            build_binding()
+        except RuntimeError as e:
+            if os.path.exists(BINDING_PATH):
+                os.remove(BINDING_PATH)          # older than the library's interface
+            sys.stderr.write(f"warning: the Python binding of the cache operators was not built: {e}\n")
     return LIB_PATH
 
 
