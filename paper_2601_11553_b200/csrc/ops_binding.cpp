@@ -23,6 +23,7 @@ decltype(&percache_compact_slots) f_compact;
 enum Type { I32 = 1, F32 = 2, U8 = 4, BOOL = 8, I64 = 16, U64 = 32, BF16 = 64, F16 = 128 };
 constexpr int N_TYPES = 8;
 PyObject* types[N_TYPES];                       // torch's type objects, in the order of Type
+PyObject* current_stream;                       // device -> torch's current stream there
 PyObject *n_dtype, *n_shape, *n_get_device, *n_stride, *n_is_contiguous, *n_data_ptr;
 
 struct Ref {                                    // owns a reference
@@ -57,6 +58,15 @@ void* address(PyObject* x) {                    // of a number, e.g. a stream
   void* p = PyLong_AsVoidPtr(x);
   if (!p && PyErr_Occurred()) throw Error{};
   return p;
+}
+// The caller's stream, or torch's current one: that is what the tensors' other work is ordered on.
+void* stream_of(PyObject* x, int device) {
+  if (x != Py_None) return address(x);
+  const Ref d(PyLong_FromLong(device));
+  if (!d.p) throw Error{};
+  const Ref r(PyObject_CallOneArg(current_stream, d.p));
+  if (!r.p) throw Error{};
+  return address(r.p);
 }
 int64_t ask(PyObject* x, PyObject* method) {
   const Ref r(PyObject_CallMethodNoArgs(x, method));
@@ -237,7 +247,7 @@ PyObject* tree_attention(PyObject*, PyObject* const* x, Py_ssize_t n) {
     float* lse = x[4] == Py_None ? nullptr : static_cast<float*>(flat<2>(x[4], "lse", F32, k.device, {q.rows, q.heads}));
     const Space ws = workspace_of(x[9], k.device);
     const float scale = scale_of(x[13], q.dim);
-    void* stream = address(x[14]);
+    void* stream = stream_of(x[14], k.device);
     return released([&] {
       return f_tree(k.device, stream, &kv, &rows, q.p, q.stride, static_cast<int32_t>(q.heads), scale, out.p, out.stride, lse, ws.p, ws.bytes);
     });
@@ -258,7 +268,7 @@ PyObject* attention_weights(PyObject*, PyObject* const* x, Py_ssize_t n) {
     const float* w_in = x[3] == Py_None ? nullptr : static_cast<float*>(flat<3>(x[3], "weights", F32, k.device, {n_seqs, k.heads, width}));
     const Space ws = workspace_of(x[9], k.device);
     const float scale = scale_of(x[14], q.dim), decay = number(x[15]);
-    void* stream = address(x[16]);
+    void* stream = stream_of(x[16], k.device);
     return released([&] {
       return f_weights(k.device, stream, &kv, &rows, q.p, q.stride, static_cast<int32_t>(q.heads), scale, lse, use, decay, w_in, w_out, width,
                        ws.p, ws.bytes);
@@ -280,7 +290,7 @@ PyObject* select_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
     if (budget > INT32_MAX) refuse("keep", "a smaller budget");
     const int32_t sink = int32(x[4], "sink"), recent = int32(x[5], "recent");
     const int32_t max_len = x[6] == Py_None ? static_cast<int32_t>(s[2]) : int32(x[6], "max_len");
-    void* stream = address(x[7]);
+    void* stream = stream_of(x[7], device);
     return released([&] {
       return f_select(device, stream, w, s[2], length, static_cast<int32_t>(s[0]), static_cast<int32_t>(s[1]), max_len,
                       static_cast<int32_t>(budget), sink, recent, keep, count);
@@ -309,7 +319,7 @@ PyObject* compact_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
     const int32_t* table = x[10] == Py_None ? nullptr : static_cast<int32_t*>(flat<2>(x[10], "dst_page_table", I32, k.device, {n_seqs, -1}, &dst_width));
     if (dst_width > INT32_MAX) refuse("dst_page_table", "fewer entries a prompt");
     const int32_t* start = static_cast<int32_t*>(optional(x[11], "dst_start", I32, k.device, n_seqs));
-    void* stream = address(x[12]);
+    void* stream = stream_of(x[12], k.device);
     return released([&] {
       return f_compact(k.device, stream, &kv, static_cast<int32_t>(n_seqs), max_len, table, static_cast<int32_t>(dst_width), start, first, keep,
                        static_cast<int32_t>(s[1]), static_cast<int32_t>(s[2]), count, w_in, w_out, width);
@@ -317,15 +327,19 @@ PyObject* compact_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
   });
 }
 
-// bind((addresses of the four entry points), (torch's int32, float32, uint8, bool, int64, uint64, bfloat16, float16))
+// bind((addresses of the four entry points), (torch's int32, float32, uint8, bool, int64, uint64, bfloat16, float16), device -> stream)
 PyObject* bind(PyObject*, PyObject* args) {
   unsigned long long f[4];
-  PyObject* t[N_TYPES];
-  if (!PyArg_ParseTuple(args, "(KKKK)(OOOOOOOO)", &f[0], &f[1], &f[2], &f[3], &t[0], &t[1], &t[2], &t[3], &t[4], &t[5], &t[6], &t[7])) return nullptr;
+  PyObject *t[N_TYPES], *stream;
+  if (!PyArg_ParseTuple(args, "(KKKK)(OOOOOOOO)O", &f[0], &f[1], &f[2], &f[3], &t[0], &t[1], &t[2], &t[3], &t[4], &t[5], &t[6], &t[7],
+                        &stream))
+    return nullptr;
   for (int i = 0; i < N_TYPES; ++i) {
     Py_INCREF(t[i]);
     Py_XSETREF(types[i], t[i]);
   }
+  Py_INCREF(stream);
+  Py_XSETREF(current_stream, stream);
   f_tree = reinterpret_cast<decltype(f_tree)>(f[0]);
   f_weights = reinterpret_cast<decltype(f_weights)>(f[1]);
   f_select = reinterpret_cast<decltype(f_select)>(f[2]);

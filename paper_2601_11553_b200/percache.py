@@ -530,6 +530,11 @@ MAX_TREE_NODES = 256
 _binding = None
 
 
+def _current_stream(device: int) -> int:
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
 def _ops() -> Any:
     """The compiled checks and calls (csrc/ops_binding.cpp), bound to the loaded library."""
     global _binding
@@ -542,20 +547,22 @@ def _ops() -> Any:
             raise PerCacheError(E_CUDA, f"{e} (build it: python -m paper_2601_11553_b200.build)") from e
         m.bind(tuple(C.cast(f, C.c_void_p).value for f in (lib.percache_tree_attention, lib.percache_attention_weights,
                                                            lib.percache_select_slots, lib.percache_compact_slots)),
-               (torch.int32, torch.float32, torch.uint8, torch.bool, torch.int64, torch.uint64, torch.bfloat16, torch.float16))
+               (torch.int32, torch.float32, torch.uint8, torch.bool, torch.int64, torch.uint64, torch.bfloat16, torch.float16),
+               # without the Python objects of torch.cuda.current_stream, where torch has it (a small call's time is the host's)
+               getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream))
         _binding = m
     return _binding
 
 
 def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len: Any, row_start: Any, max_nodes: int,
                    max_len: int, workspace: Any, mask: Any = None, page_table: Any = None, ctx_start: Any = None,
-                   scale: Optional[float] = None, stream: int = 0) -> Any:
+                   scale: Optional[float] = None, stream: Optional[int] = None) -> Any:
     """percache_tree_attention: attention of drafted tokens (a tree, a chain, one token a prompt) over the cache.
 
     q, out: [rows, q_heads, head_dim]; k, v: [slots, kv_heads, head_dim] (pages: slots = 16 x pages); lse: fp32
     [rows, q_heads] or None; mask: int64 words [rows, ceil(max_nodes / 64)] or None (node i sees nodes 0 .. i); workspace:
-    uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` (a cudaStream_t; 0 is the legacy default stream, not
-    torch's current one) and returns `out`."""
+    uint8, OPS_WORKSPACE_BYTES, zeroed once.  Enqueues on `stream` (a cudaStream_t; None: torch's current
+    stream on the tensors' device; 0: the legacy default stream) and returns `out`."""
     _check(_ops().tree_attention(q, k, v, out, lse, ctx_len, row_start, max_nodes, max_len, workspace, mask, page_table, ctx_start,
                                  scale, stream), "percache_tree_attention")
     return out
@@ -564,7 +571,7 @@ def tree_attention(q: Any, k: Any, v: Any, out: Any, lse: Any = None, *, ctx_len
 def attention_weights(q: Any, k: Any, lse: Any, weights: Any, weights_out: Any = None, *, ctx_len: Any, row_start: Any,
                       max_nodes: int, max_len: int, workspace: Any, mask: Any = None, use: Any = None,
                       page_table: Any = None, ctx_start: Any = None, scale: Optional[float] = None, decay: float = 1.0,
-                      stream: int = 0) -> Any:
+                      stream: Optional[int] = None) -> Any:
     """percache_attention_weights: weights_out = decay * weights + the softmax weights of the rows with use != 0, summed
     per slot over the rows and the query heads of a KV head.  weights: fp32 [seqs, kv_heads, slots]; weights_out None: in
     place.  Enqueues on `stream` and returns weights_out."""
@@ -575,7 +582,7 @@ def attention_weights(q: Any, k: Any, lse: Any, weights: Any, weights_out: Any =
 
 
 def select_slots(weights: Any, length: Any, keep: Any, count: Any, *, sink: int = 0, recent: int = 0,
-                 max_len: Optional[int] = None, stream: int = 0) -> Any:
+                 max_len: Optional[int] = None, stream: Optional[int] = None) -> Any:
     """percache_select_slots: keep [seqs, heads, budget] (int32, ascending, -1 behind the last) and count [seqs] of the
     slots that stay: the first `sink`, the last `recent`, and the heaviest of the rest."""
     _check(_ops().select_slots(weights, length, keep, count, sink, recent, max_len, stream), "percache_select_slots")
@@ -584,7 +591,7 @@ def select_slots(weights: Any, length: Any, keep: Any, count: Any, *, sink: int 
 
 def compact_slots(k: Any, v: Any, keep: Any, count: Any, *, max_len: int, weights: Any = None, weights_out: Any = None,
                   first: Any = None, page_table: Any = None, ctx_start: Any = None, dst_page_table: Any = None,
-                  dst_start: Any = None, stream: int = 0) -> None:
+                  dst_start: Any = None, stream: Optional[int] = None) -> None:
     """percache_compact_slots: slot first[b] + j of the destination takes the K, V and weight of slot keep[b][head][j].
     Without dst_page_table / dst_start in place (keep strictly ascending, keep[j] >= first + j); weights_out None: the
     weights in place."""
@@ -593,6 +600,9 @@ def compact_slots(k: Any, v: Any, keep: Any, count: Any, *, max_len: int, weight
                                 dst_start, stream), "percache_compact_slots")
 
 
-def ops_status(workspace: Any, stream: int = 0) -> None:
-    """percache_ops_status: waits for `stream`; raises PerCacheError if a call that used this workspace gave up a wait."""
+def ops_status(workspace: Any, stream: Optional[int] = None) -> None:
+    """percache_ops_status: waits for `stream` (None: torch's current one); raises PerCacheError if a call that used this
+    workspace gave up a wait."""
+    if stream is None and workspace.get_device() >= 0:
+        stream = _current_stream(workspace.get_device())
     _check(load_library().percache_ops_status(workspace.get_device(), stream, workspace.data_ptr()), "percache_ops_status")

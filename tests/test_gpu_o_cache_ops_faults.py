@@ -146,3 +146,57 @@ def test_steps_on_a_handle_report_their_own_errors_only():
             leave_an_error_behind(other, t)
             h.evict_context(2)
         h.decode(token)
+
+
+def test_calls_without_a_stream_take_the_current_one():
+    n, h = 200, 2
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16)          # noqa: E731
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32).cuda()                               # noqa: E731
+    q, k, v = rnd(1, 4, 128), rnd(n, h, 128), rnd(n, h, 128)
+    ws = torch.zeros(pcb.OPS_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    kw = dict(ctx_len=ints(n - 1), row_start=ints(0, 1), ctx_start=ints(0), max_nodes=1, max_len=n, workspace=ws)
+    start = ints(0)
+
+    def steps(q, k, v, wait):
+        """Every operator on inputs that the current stream only has after `wait`."""
+        out, lse = torch.zeros_like(q), torch.zeros((1, 4), device="cuda")
+        w, w2 = torch.zeros((1, h, n), device="cuda"), torch.zeros((1, h, n), device="cuda")
+        keep, count = torch.full((1, h, 50), -1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        qq, kk, vv, length = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v), ints(0)
+        torch.cuda.synchronize()
+        wait()
+        qq.copy_(q), kk.copy_(k), vv.copy_(v), length.fill_(n)
+        pcb.tree_attention(qq, kk, vv, out, lse, **kw)
+        wait()
+        pcb.attention_weights(qq, kk, lse, w, w2, **kw)
+        wait()
+        pcb.select_slots(w2, length, keep, count, sink=1, recent=3)
+        wait()
+        pcb.compact_slots(kk, vv, keep, count, max_len=n, weights=w2, ctx_start=start)
+        torch.cuda.synchronize()
+        return out, lse, w2, keep, count, kk, vv
+
+    want = steps(q, k, v, lambda: None)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = steps(q, k, v, lambda: torch.cuda._sleep(20_000_000))
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
+def test_the_status_of_a_workspace_is_read_behind_the_current_stream():
+    ws = torch.zeros(pcb.OPS_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    pcb.ops_status(ws)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        ws[:4] = 1                                          # as a kernel does whose wait ran out
+        with pytest.raises(pcb.PerCacheError) as e:
+            pcb.ops_status(ws)
+    assert e.value.code == pcb.E_DEVICE_TIMEOUT
+    with pytest.raises(pcb.PerCacheError):
+        pcb.ops_status(ws)
+    ws[:4] = 0
+    pcb.ops_status(ws)
