@@ -301,6 +301,7 @@ PyObject* select_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
 // k v keep count max_len weights weights_out first page_table ctx_start dst_page_table dst_start stream
 PyObject* compact_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
   return guarded(n, 13, [&] {
+    if (x[5] == Py_None && x[6] != Py_None) refuse("weights_out", "weights beside it");
     const Strided k = strided(x[0], "k");
     const int64_t n_seqs = length_of(x[3], "count");
     const percache_kv_t kv = pools(k, x[1], x[8], x[9], n_seqs);
