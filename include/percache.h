@@ -439,7 +439,9 @@ PERCACHE_API int percache_qa_top1(int32_t device, void* stream, const float* ban
  *  - NULL is the legacy default stream, which other streams do not wait for unless they were created to.
  *  - Sizes the host has to know are given as upper bounds (max_len, max_nodes).  Device-side values beyond them, or
  *    negative ones, are clamped; a page id or slot outside the pools reads as zeros and is never written.
- *  - Refused calls (PERCACHE_E_INVAL, PERCACHE_E_CAPACITY) enqueue nothing.
+ *  - Refused calls (PERCACHE_E_INVAL, PERCACHE_E_CAPACITY) enqueue nothing.  PERCACHE_E_CAPACITY: a workspace that is too
+ *    small, or bounds that give tree_attention or attention_weights more work than they count: about
+ *    ceil(max_len / 128) x KV heads x tiles (128 / (query heads a KV head) nodes each) of 2^29 a prompt, or of 2^35 a batch.
  *  - A prompt without rows, or a batch without prompts or rows, is allowed; outputs of rows at or behind
  *    row_start[n_seqs], and of slots behind a prompt's last one, are left as they were.
  *  - Bounded waits: where a kernel of this group gives up a wait (PERCACHE_E_DEVICE_TIMEOUT elsewhere), it says so in

@@ -456,14 +456,30 @@ int launch_tree(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v
   return launch_pdl(tree_merge_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
 }
 
-}  // namespace
-
-int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
-  TreeParams p{};
+// What the host decides from a call's sizes; returns the most units a prompt can have.
+int64_t set_sizes(TreeParams& p, const TreeAttention& t) {
   p.kv = t.kv; p.rows = t.rows;
   p.n_q_heads = t.n_q_heads;
   p.group = t.n_q_heads / t.kv.n_kv_heads;
   p.tile_nodes = std::min(BLK / p.group, t.rows.max_nodes);
+  // A unit's cost beside its blocks grows with its rows (the end of every row is written out while no block is worked on).  2 -> 4: 26-node
+  // trees on 2112 slots 16.3 -> 15.8 us; 64 x 2500 single tokens 108.4 -> 110.4 us.
+  p.over = p.tile_nodes * p.group <= 16 ? 2 : 4;
+  return static_cast<int64_t>((t.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * t.kv.n_kv_heads;
+}
+
+}  // namespace
+
+bool tree_attention_fits(const TreeAttention& t) {
+  TreeParams p{};
+  const int64_t units = set_sizes(p, t);
+  return units_fit(t.rows.n_seqs, units, t.rows.max_len, 1, p.over);
+}
+
+int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
+  TreeParams p{};
+  const int64_t units = set_sizes(p, t);
+  if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
   p.scale_log2 = t.scale * LOG2E;
   p.out = t.out; p.out_stride = t.out_stride; p.lse = t.lse;
   char* ws = static_cast<char*>(t.workspace);
@@ -475,15 +491,10 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   if (q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
-  // A unit's cost beside its blocks grows with its rows (the end of every row is written out while no block is worked on).  2 -> 4: 26-node
-  // trees on 2112 slots 16.3 -> 15.8 us; 64 x 2500 single tokens 108.4 -> 110.4 us.
-  p.over = p.tile_nodes * p.group <= 16 ? 2 : 4;
   // Short contexts: a unit is one CTA's, and there is no second kernel.  64 prompts of 700 slots: 50.4 against 53.1 us for trees, 42.2 against
   // 43.3 for single tokens; one prompt of 300 slots 8.8 against 9.2 us.  Of 512 slots 10.9 against 9.5 us, but a second launch is 2 us
   // of the host's time, which such a call is bound by unless it was captured.
   p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;
-  const int64_t units = static_cast<int64_t>((p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes) * p.kv.n_kv_heads;
-  if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   p.small = small_batch(p.rows.n_seqs, units, p.rows.max_len, 1, p.over) ? 1 : 0;
   if (t.kv.head_dim == 128)

@@ -398,9 +398,17 @@ int launch_weights(const CUtensorMap& q, const CUtensorMap& k, const WeightParam
   return launch_pdl(attention_weights_kernel<D, BF16>, dim3(n_ctas), dim3(TREE_THREADS), WEIGHTS_SMEM, s, q, k, p) == cudaSuccess ? 0 : -1;
 }
 
+int most_tiles(const AttentionWeights& t) {
+  const int tile_nodes = std::min(BLK / (t.n_q_heads / t.kv.n_kv_heads), t.rows.max_nodes);
+  return (t.rows.max_nodes + tile_nodes - 1) / tile_nodes;
+}
+
 }  // namespace
 
+bool attention_weights_fit(const AttentionWeights& t) { return units_fit(t.rows.n_seqs, t.kv.n_kv_heads, t.rows.max_len, most_tiles(t), UNIT_COST); }
+
 int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t s) {
+  if (!attention_weights_fit(t)) return -2;
   WeightParams p{};
   p.kv = t.kv; p.rows = t.rows;
   p.n_q_heads = t.n_q_heads;
@@ -414,9 +422,7 @@ int launch_attention_weights(const AttentionWeights& t, int n_sms, cudaStream_t 
   if (pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0) return -1;
   q = k;                       // a batch without rows copies none, but the kernel prefetches the map
   if (t.rows.n_rows > 0 && q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0) return -1;
-  const int tiles = (p.rows.max_nodes + p.tile_nodes - 1) / p.tile_nodes;
-  if (!units_fit(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, tiles, UNIT_COST)) return -2;
-  p.small = small_batch(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, tiles, UNIT_COST) ? 1 : 0;
+  p.small = small_batch(p.rows.n_seqs, p.kv.n_kv_heads, p.rows.max_len, most_tiles(t), UNIT_COST) ? 1 : 0;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   if (t.kv.head_dim == 128)
     return t.kv.bf16 ? launch_weights<128, true>(q, k, p, n_ctas, s) : launch_weights<128, false>(q, k, p, n_ctas, s);

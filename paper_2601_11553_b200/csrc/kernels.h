@@ -244,7 +244,10 @@ struct CompactSlots {
   float* w_out;
   int64_t w_stride;
 };
-// each returns 0, -1 when a launch failed, -2 when a prompt's bounds give more units of work than the schedule can count
+// Do the call's bounds give no more units of work than the schedule can count?
+bool tree_attention_fits(const TreeAttention& a);
+bool attention_weights_fit(const AttentionWeights& a);
+// each returns 0, -1 when a launch failed, -2 when the work does not fit
 int launch_tree_attention(const TreeAttention& a, int n_sms, cudaStream_t s);
 int launch_attention_weights(const AttentionWeights& a, int n_sms, cudaStream_t s);
 int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* length, int n_seqs, int n_heads, int max_len,

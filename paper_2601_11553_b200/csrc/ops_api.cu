@@ -117,13 +117,14 @@ int percache_tree_attention(int32_t device, void* stream, const percache_kv_t* k
       !aligned(out, 16) || out_row_stride % 8 != 0 || out_row_stride < static_cast<int64_t>(n_q_heads) * kv->head_dim)
     return PERCACHE_E_INVAL;
   if (!workspace_ok(workspace, workspace_bytes)) return workspace && aligned(workspace, 256) ? PERCACHE_E_CAPACITY : PERCACHE_E_INVAL;
-  const DeviceGuard dev(device);
-  if (!dev.ok) return PERCACHE_E_CUDA;
   TreeAttention a{};
   a.kv = kv_view(*kv);
   a.rows = tree_rows(*rows);
   a.q = q; a.q_stride = q_row_stride; a.n_q_heads = n_q_heads; a.scale = scale;
   a.out = out; a.out_stride = out_row_stride; a.lse = lse; a.workspace = workspace;
+  if (!tree_attention_fits(a)) return PERCACHE_E_CAPACITY;
+  const DeviceGuard dev(device);
+  if (!dev.ok) return PERCACHE_E_CUDA;
   return launched(launch_tree_attention(a, sm_count(device), static_cast<cudaStream_t>(stream)));
 }
 
@@ -138,14 +139,15 @@ int percache_attention_weights(int32_t device, void* stream, const percache_kv_t
       weights_stride < rows->max_len)
     return PERCACHE_E_INVAL;
   if (!workspace_ok(workspace, workspace_bytes)) return workspace && aligned(workspace, 256) ? PERCACHE_E_CAPACITY : PERCACHE_E_INVAL;
-  const DeviceGuard dev(device);
-  if (!dev.ok) return PERCACHE_E_CUDA;
   AttentionWeights a{};
   a.kv = kv_view(*kv);
   a.rows = tree_rows(*rows);
   a.q = q; a.q_stride = q_row_stride; a.n_q_heads = n_q_heads; a.scale = scale; a.lse = lse; a.use = use;
   a.decay = decay; a.w_in = decay != 0.f ? weights_in : nullptr; a.w_out = weights_out; a.w_stride = weights_stride;
   a.workspace = workspace;
+  if (!attention_weights_fit(a)) return PERCACHE_E_CAPACITY;
+  const DeviceGuard dev(device);
+  if (!dev.ok) return PERCACHE_E_CUDA;
   return launched(launch_attention_weights(a, sm_count(device), static_cast<cudaStream_t>(stream)));
 }
 
