@@ -27,13 +27,15 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 
+// Block sizes: lists of up to 512 * SEL_UNROLL weights are always held in registers, so only the larger block has the list.
+constexpr int SEL_SHORT = 512, SEL_LONG = 1024;
 constexpr int SEL_LIST = 4096;
 template <int THREADS>
 struct SelectShared {
   int hist[SEL_BINS];
   int warp_sum[THREADS / 32], warp_gt[THREADS / 32], warp_eq[THREADS / 32];
   int bin, need, listed;
-  uint2 list[SEL_LIST];                    // key and slot of the first bin's weights
+  uint2 list[THREADS == SEL_LONG ? SEL_LIST : 1];       // key and slot of the first bin's weights
 };
 
 // lo .. hi - 1: this warp's stretch (of `stretch` slots) of the middle, whose first slot is `first`; out: where the middle's list starts.
@@ -199,8 +201,13 @@ select_slots_kernel(const float* __restrict__ weights, int64_t w_stride, const i
   const float* w = weights + (static_cast<size_t>(b) * n_heads + h) * w_stride + sink;
   const int stretch = (n + THREADS - 1) / THREADS * 32;                    // whole steps of 32 for each warp
   const int lo = min(warp * stretch, n), hi = min(lo + stretch, n);
-  if (stretch <= 32 * SEL_UNROLL) select_middle<THREADS, true>(sh, w, sink, stretch, lo, hi, need, out + sink);
-  else select_middle<THREADS, false>(sh, w, sink, stretch, lo, hi, need, out + sink);
+  if constexpr (THREADS == SEL_LONG) {
+    if (stretch > 32 * SEL_UNROLL) {
+      select_middle<THREADS, false>(sh, w, sink, stretch, lo, hi, need, out + sink);
+      return;
+    }
+  }
+  select_middle<THREADS, true>(sh, w, sink, stretch, lo, hi, need, out + sink);
 }
 
 // ---------------------------------------------------------------------------------------------------- moving
@@ -347,8 +354,8 @@ int launch_select_slots(const float* weights, int64_t w_stride, const int32_t* l
   const dim3 grid(n_heads, n_seqs);
   // 512 threads hold up to 4096 weights of a list in registers, 1024 hold 8192 (and share the reading of longer ones).  8 lists of 2112:
   // 4.9 us with 512, 6.2 with 1024; 512 lists of 2500: 10.7 and 18.5; 224 lists of 8192: 13.0 and 11.8; 8 lists of 33024: 28.3 and 19.8.
-  const bool large = max_len > 512 * SEL_UNROLL;
-  return launch(large ? select_slots_kernel<1024> : select_slots_kernel<512>, grid, large ? 1024 : 512, s, weights, w_stride, length, n_heads,
+  const bool large = max_len > SEL_SHORT * SEL_UNROLL;
+  return launch(large ? select_slots_kernel<SEL_LONG> : select_slots_kernel<SEL_SHORT>, grid, large ? SEL_LONG : SEL_SHORT, s, weights, w_stride, length, n_heads,
                 max_len, budget, sink, recent, keep, count) == cudaSuccess ? 0 : -1;
 }
 

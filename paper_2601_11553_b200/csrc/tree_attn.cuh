@@ -7,8 +7,8 @@ namespace pc {
 struct MergeRecord {             // written by the CTA that has a cut unit's first part
   int32_t n_parts;               // 0: none
   int32_t row0, n_rows;          // first global row of the tile, valid tile rows
-  int32_t head0, cta;
-  int32_t pad[3];
+  int32_t head0;
+  int32_t pad[4];
 };
 
 struct TreeParams {
@@ -170,7 +170,7 @@ __device__ __forceinline__ void copy_role(const TreeParams& a, const Pipe& pipe,
     }
     if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
       rec.n_parts = last_cta(span, it.unit_end) - static_cast<int>(blockIdx.x) + 1;
-      rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group; rec.cta = blockIdx.x;
+      rec.row0 = it.row0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group;
     }
     ++n_item;
   }
