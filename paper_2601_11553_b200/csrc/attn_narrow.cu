@@ -11,8 +11,8 @@
 // each keep a running reference, sum and O of their own, merged at the piece's end; O has two buffers per parity, so the next
 // piece's products do not wait for that.  Q has two slots for the same reason.
 //
-// Measured: one token on each of 64 ragged prompts around 2500 slots, two heads a KV head: 107 - 108 us (655 MB, 6.1 TB/s; a plain copy
-// reaches 6.45), 108 us in pages; the 128-row form takes 124 us.  One token on 512 slots: 10.3 us, one kernel.
+// Measured: one token on each of 64 ragged prompts around 2500 slots, two heads a KV head: 105 - 107 us (655 MB, 6.1 TB/s; a plain copy
+// reaches 6.45), 107 - 108 us in pages; the 128-row form takes 124 us.  One token on 512 slots: 10.6 us, one kernel.
 #include <algorithm>
 
 #include "tree_attn.cuh"

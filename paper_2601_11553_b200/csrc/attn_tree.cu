@@ -10,8 +10,9 @@
 // tensor work (0.75 us) and 16 K exponentials (0.55 us): with the tile at most 128 rows high the operator is bound by
 // reading K and V once, whatever the number of rows, and everything below serves to keep the copies running.  Measured,
 // 96 rows: 1.50 us a block (6.5 TB/s over 148 SMs), 1.06 us when all K and V are in L2, and 10 - 15 us of a call for its start,
-// the ends of its pieces and the merge: 48-node trees on 64 x 2500 slots in pages 128 us (floor 105), 26-node trees on
-// one prompt of 2112 slots 12.7 us.
+// the ends of its pieces and the merge: 48-node trees on 64 x 2500 slots in pages (floor 105 us) 120 - 123 us a call in a graph of
+// back-to-back calls, where one call's start hides behind the last one's end, and 136 - 143 us as one call among others;
+// 26-node trees on one prompt of 2112 slots 12.7 us.
 //
 // Schedule.  Lengths live on the device, so the work is dealt there: every unit costs its blocks and a little more, the
 // batch's total cost is cut into one contiguous span per CTA, and a unit that a span border cuts is finished in parts
@@ -491,9 +492,11 @@ int launch_tree_attention(const TreeAttention& t, int n_sms, cudaStream_t s) {
   if (q_map(&q, t.q, t.kv, t.q_stride, t.n_q_heads, t.rows.n_rows, p.tile_nodes) != 0 || pool_map(&k, t.kv.k, t.kv, t.kv.k_stride) != 0 ||
       pool_map(&v, t.kv.v, t.kv, t.kv.v_stride) != 0)
     return -1;
-  // Short contexts: a unit is one CTA's, and there is no second kernel.  64 prompts of 700 slots: 50.4 against 53.1 us for trees, 42.2 against
-  // 43.3 for single tokens; one prompt of 300 slots 8.8 against 9.2 us.  Of 512 slots 10.9 against 9.5 us, but a second launch is 2 us
-  // of the host's time, which such a call is bound by unless it was captured.
+  // Short contexts: a unit is one CTA's, and there is no second kernel.  On the device, whole against cut: 64 prompts of 700 slots 43 against
+  // 44 us for single tokens and 54 against 57 for trees of 26, ten such prompts 12.5 against 13.7 and 15.3 against 18.3, one prompt of
+  // 300 slots 8.7 against 9.0.  Few units of more slots lose by it: one prompt of 512 slots 10.6 against 9.5 us, of 700 11.1 against 9.3,
+  // with 26 nodes 13.7 against 11.0.  The rule leaves them whole for single calls, which the host bounds (a second launch is 2 us of its
+  // time); in a captured graph the cut form would be the faster one there.
   p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
   p.small = small_batch(p.rows.n_seqs, units, p.rows.max_len, 1, p.over) ? 1 : 0;

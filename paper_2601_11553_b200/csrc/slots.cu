@@ -17,7 +17,7 @@ namespace {
 // the dependent passes.  Weights stay in registers when a warp's stretch is at most 32 x SEL_UNROLL slots.  Longer lists are read
 // three times: for the first histogram, to put the keys of the bin found into a list in shared memory (the other passes work on
 // that), and to write; where the bin holds more than the list (many equal weights), every pass reads all again.  224 lists of 33024:
-// 34.2 us at 71 % of the issue slots (41.6 without the list); 224 of 2112: 6.7 us.
+// 34 us at 71 % of the issue slots (41.6 without the list); 224 of 2112: 6.8 us.
 constexpr int SEL_BITS = 11, SEL_BINS = 1 << SEL_BITS;
 constexpr int SEL_UNROLL = 8;
 
@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(MOVE_THREADS, 6) copy_slots_kernel(CompactSlot
 // list's chunks in order, each read whole before any of it is written: its sources lie at or behind the chunk's own first
 // slot, because keep[j] >= first + j and the list ascends, so no chunk reads what an earlier one has written.  Slices, not
 // chunks, are what runs in parallel; the host makes them as narrow as it takes to fill the SMs four times (7 x 8 lists of 8192:
-// 198 us; twice: 236 us.  64 x 8 lists of 512: 78 us either way).
+// 198 - 215 us from box to box, floor 74; twice: 236 us.  64 x 8 lists of 512: 78 - 81 us either way, floor 42).  What bounds it: a
+// chunk's loads, a barrier and its stores follow each other, and 32 bytes of a 256-byte row are a thin slice.
 constexpr int SHIFT_UNROLL = 8;
 __global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots a, int slices, int vecs, int first_slice) {
   const int b = blockIdx.z, g = blockIdx.y, slice = blockIdx.x + first_slice;
