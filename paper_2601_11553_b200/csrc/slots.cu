@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 6) copy_slots_kernel(CompactSlot
 // list's chunks in order, each read whole before any of it is written: its sources lie at or behind the chunk's own first
 // slot, because keep[j] >= first + j and the list ascends, so no chunk reads what an earlier one has written.  Slices, not
 // chunks, are what runs in parallel; the host makes them as narrow as it takes to fill the SMs four times (7 x 8 lists of 8192:
-// 198 - 215 us from box to box, floor 74; twice: 236 us.  64 x 8 lists of 512: 78 - 81 us either way, floor 42).  What bounds it: a
+// 198 - 215 us in several runs, floor 74; twice: 236 us.  64 x 8 lists of 512: 78 - 81 us either way, floor 42).  What bounds it: a
 // chunk's loads, a barrier and its stores follow each other, and 32 bytes of a 256-byte row are a thin slice.
 constexpr int SHIFT_UNROLL = 8;
 __global__ void __launch_bounds__(MOVE_THREADS) shift_slots_kernel(CompactSlots a, int slices, int vecs, int first_slice) {
