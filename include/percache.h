@@ -534,6 +534,114 @@ PERCACHE_API int percache_compact_slots(int32_t device, void* stream, const perc
                                         const int32_t* keep, int32_t keep_heads, int32_t budget, const int32_t* count,
                                         const float* weights_in, float* weights_out, int64_t weights_stride);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Writing, reading and sharing a decoding batch's pages.  The rules of the group above hold here too.
+ *
+ * 8-bit pages.  Slot s of prompt b is slot s % 16 of page page_table[b][s / 16].  A page holds, KV head by KV head, 16 keys and
+ * then 16 values of head_dim bytes each (4 exponent and 3 mantissa bits, bias 7, no infinities, largest 448, NaN 0x7f and
+ * 0xff), and has a scale per KV head for its keys and one for its values: what a byte stands for is multiplied by it.  K is
+ * as the attention uses it (after position encoding). */
+typedef struct {
+  void*   pages;                   /* [n_pages] of [n_kv_heads][2][16][head_dim] bytes; 16-byte aligned           */
+  float*  scales;                  /* [n_pages][n_kv_heads][2]; 8-byte aligned                                    */
+  int64_t page_stride;             /* bytes from page to page: a multiple of 32*head_dim, at least n_kv_heads as
+                                      many; n_pages x that multiple below 2^31 - 2^13                              */
+  int64_t n_pages;                 /* at most 2^26                                                                */
+  const int32_t* page_table;       /* [n_seqs][page_table_stride]                                                 */
+  int32_t page_table_stride;       /* entries a prompt, at least ceil(max_len / 16)                               */
+  int32_t n_kv_heads;              /* at most 4096                                                                */
+  int32_t head_dim;                /* 64 or 128                                                                   */
+  int32_t dtype;                   /* PERCACHE_BF16 or PERCACHE_F16: of q, k, v and out                           */
+} percache_kv8_t;
+
+/* New rows of a batch, on their way into the cache.  Prompt b has ctx_len[b] slots in use and n = row_start[b + 1] -
+ * row_start[b] new rows (any number); its row i is row row_start[b] + i of q, k and v, and belongs in slot ctx_len[b] + i. */
+typedef struct {
+  int32_t n_seqs;                  /* at most 65535                                                               */
+  int32_t n_rows;                  /* rows of q, k, v, q_out and position                                         */
+  int32_t max_len;                 /* most slots of a prompt, its new rows included; at most 2^26                 */
+  int32_t n_q_heads;               /* used when q is given; at most 4096                                          */
+  const int32_t* ctx_len;          /* [n_seqs]                                                                    */
+  const int32_t* row_start;        /* [n_seqs + 1], ascending                                                     */
+  const int32_t* position;         /* [n_rows] row of `rope` for each row, or NULL: its slot                      */
+  const void* q;                   /* [n_rows][n_q_heads][head_dim], or NULL: keys and values only                */
+  void*       q_out;               /* like q; may be q itself (with q's stride)                                   */
+  const void* k;                   /* [n_rows][n_kv_heads][head_dim]                                              */
+  const void* v;
+  int64_t q_row_stride, q_out_row_stride, k_row_stride, v_row_stride;   /* elements, multiples of 8               */
+  const float* q_gain;             /* [head_dim] fp32, 16-byte aligned, or NULL: queries are not normalised       */
+  const float* k_gain;             /* likewise for keys                                                           */
+  const float* rope;               /* [n_positions][head_dim / 2][2] fp32 (cos, sin), 16-byte aligned, or NULL    */
+  int32_t n_positions;             /* positions are clamped to 0 .. n_positions - 1                               */
+  float   eps;                     /* >= 0                                                                        */
+} percache_new_rows_t;
+
+/* q' = R(p) norm(q), k' = R(p) norm(k) head by head in fp32, rounded once (with fp16, finite values past its range become the
+ * largest): norm(x) = x / sqrt(mean(x^2) + eps) * gain, and R(p) turns
+ * the pair (x[i], x[i + head_dim / 2]) by the angle of position p.  q' goes to q_out, k' and v to the rows' slots of the
+ * pools (the 16-bit rules of percache_kv_t).  Rows whose slot is outside the pools write only q_out; two rows of a batch must not
+ * share a slot.  q, k and v may be parts of one array; none of them may overlap the pools.  At most 4096 KV heads. */
+PERCACHE_API int percache_append_rows(int32_t device, void* stream, const percache_kv_t* kv, const percache_new_rows_t* rows);
+
+/* The same into 8-bit pages.  A page that gets rows takes, for its keys and for its values of every KV head, the scale 2^e with the least
+ * e in -32 .. 32 for which the largest finite |value| of its new rows is at most 448 * 2^e.  Where slots below the first new one are in
+ * use and the page's scale (taken to lie within 2^-32 .. 2^32) is larger, that stays; where it is smaller, their bytes are rounded again to the new one (exact but
+ * for values below 2^-6 of it).  Values are rounded to nearest, ties to even; beyond 448 * 2^e (infinities, or e at 32) they
+ * become the largest; NaN stays NaN.  Slots behind the last new one are left as they were.  A page with new rows of a prompt must not be any
+ * other prompt's. */
+PERCACHE_API int percache_append_rows_8bit(int32_t device, void* stream, const percache_kv8_t* kv, const percache_new_rows_t* rows);
+
+/* percache_tree_attention over 8-bit pages: out = softmax(scale * q . K) V, lse, masks and rows that see nothing as there, with at
+ * most 128 query heads per KV head.  Products are formed on the 8-bit values themselves: q (exactly, but for elements below 2^-13 of
+ * the row's largest with bf16, 2^-17 with fp16, which are off by up to 2^-22 and 2^-26 of that) and the weights (rounded
+ * like bf16 or fp16 or finer) as sums of 8-bit numbers, accumulated in fp32.  Scales below 2^-32 (and NaN) count as 2^-32, above 2^32 as
+ * 2^32; pages outside the pool hold zeros.  A q that holds infinity or NaN gives NaN. */
+PERCACHE_API int percache_tree_attention_8bit(int32_t device, void* stream, const percache_kv8_t* kv, const percache_rows_t* rows,
+                                              const void* q, int64_t q_row_stride, int32_t n_q_heads, float scale, void* out,
+                                              int64_t out_row_stride, float* lse, void* workspace, int64_t workspace_bytes);
+
+/* Memory that pages lie in: page p of layer l is the page_bytes bytes from base + l * layer_stride + p * page_stride. */
+typedef struct {
+  void*   base;                    /* 4-byte aligned                                                              */
+  int64_t page_bytes;              /* a multiple of 4, as are the strides                                         */
+  int64_t page_stride;             /* bytes, at least page_bytes                                                  */
+  int64_t layer_stride;            /* bytes; layers and pages must not overlap                                    */
+  int32_t n_layers;                /* 1 .. 65535                                                                  */
+  int32_t reserved0;
+} percache_pool_t;
+#define PERCACHE_MAX_POOLS 8
+#define PERCACHE_MAX_FORK_SEQS 8192
+
+/* Sequences that go on as others (samples of one prompt, the beams of a search step): child i continues sequence parent[i].
+ * Sequence s holds the pages page_table[s][0 .. held[s] - 1], of which length[s] slots are in use; refs[p] counts the
+ * sequences (and whoever else) that hold page p, and free_list[0 .. free_count - 1] are the pages that nobody holds.
+ *  - A parent's full pages (the first length / 16) are shared by its children.  Its other pages, of which the first may be partly
+ *    filled, go to its first child; they must be held by that sequence only (whoever forks keeps it so).  The other children
+ *    get a copy of the partly filled page, in every layer of every pool.
+ *  - Every child gets pages for length + room slots, as far as its row of table_out (table_out_stride entries) goes.  What it lacks comes
+ *    from the end of the free list, children in order; what the list cannot give is counted in missing[0], and the
+ *    child's held_out and length_out end there.
+ *  - refs is brought up to date: a sequence without a child gives all its pages back, and pages that nobody holds any more are put
+ *    behind the free list's rest in ascending order.
+ *  - table_out[i]: the held_out[i] pages, then -1.  A parent outside 0 .. n_seqs - 1 makes an empty child.
+ * refs_out, free_list_out, free_count_out may be refs, free_list, free_count (each its own, all three or none); table_out must not be
+ * page_table, held_out not held, length_out not length.  Page ids outside 0 .. n_pages - 1 are passed on, and neither counted nor copied.
+ * A page taken from the free list must not be held.  refs, free_list: int32 [n_pages]; n_pages at most 2^26;
+ * n_seqs and n_children at most PERCACHE_MAX_FORK_SEQS; rows of at most 2^22 pages; room 0 .. 2^26.  n_children 0 gives everything back.
+ * workspace: as for percache_tree_attention (it need not be zeroed for this call). */
+typedef struct {
+  int32_t n_seqs, n_children;
+  int32_t page_table_stride, table_out_stride;
+  const int32_t *page_table, *held, *length, *parent;
+  int32_t *table_out, *held_out, *length_out;
+  int64_t n_pages;
+  const int32_t *refs, *free_list, *free_count;
+  int32_t *refs_out, *free_list_out, *free_count_out, *missing;
+  int32_t room, n_pools;
+  const percache_pool_t* pools;    /* host array [n_pools]; 0 .. PERCACHE_MAX_POOLS                               */
+} percache_fork_t;
+PERCACHE_API int percache_fork_pages(int32_t device, void* stream, const percache_fork_t* fork, void* workspace, int64_t workspace_bytes);
+
 /* Waits for `stream` and reads the workspace's first word: PERCACHE_E_DEVICE_TIMEOUT if a wait of a call that used
  * this workspace ran out since it was last zeroed (outputs of calls since then are invalid), PERCACHE_E_CUDA if the
  * stream reports an error. */

@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libpercache.so")
 BINDING_PATH = os.path.join(HERE, "_ops_binding" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["percache_api.cu", "kernels_mem.cu", "kernels_ref.cu", "gemm_umma.cu", "gemm_small.cu", "attn_umma.cu", "attn_decode.cu", "attn_plan.cu", "attn_tree.cu", "attn_narrow.cu", "attn_weights.cu", "slots.cu", "ops_api.cu", "gemm_noalloc.cu", "qa_bank.cu", "wait_probe.cu"]
+SOURCES = ["percache_api.cu", "kernels_mem.cu", "kernels_ref.cu", "gemm_umma.cu", "gemm_small.cu", "attn_umma.cu", "attn_decode.cu", "attn_plan.cu", "attn_tree.cu", "attn_narrow.cu", "attn_weights.cu", "slots.cu", "append.cu", "attn_8bit.cu", "pages.cu", "ops_api.cu", "gemm_noalloc.cu", "qa_bank.cu", "wait_probe.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 

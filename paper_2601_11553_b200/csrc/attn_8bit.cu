@@ -1,0 +1,824 @@
+// Tree attention over 8-bit pages: both products transposed, formed by the tensor cores on the 8-bit values as they are stored.
+//
+// With s_K, s_V a page's scales, x = scale * s_K (q . k8), and out = sum 2^x' s_V v8 / sum 2^x' (x' in base 2, less a reference).  A block's 128 slots are
+// the MMAs' M side: S^T = K Q^T has a TMEM lane, i.e. a thread, per slot and a column per row (query head of a node), so a page's
+// scales are a thread's own numbers; O^T = V^T P^T has a lane per element of the head.  An 8-bit MMA wants both operands in 8 bits, so q and
+// the weights P = 2^x' s_V are split into sums of e4m3 numbers, each some powers of two below the one before, which get columns of their own: a
+// product of 16 rows still is one of 32 to 64 columns, which costs less than reading K and V from shared memory as the A operand does.  Nothing
+// is unpacked: shared memory sees every byte of the cache twice (copy in, MMA), where forming 16-bit tiles would take seven times.
+//   q: 2 parts (bf16, exact: 8 bits of mantissa are 4 + 4) or 3 (fp16), 2^4 apart, of q * 2^-e with the row's largest in (224, 448].
+//   P: 2 parts 2^4 apart and one 2^18 below (bf16), 3 parts and one 2^22 below (fp16).  The largest weight of a row lies in 2^4 .. 2^8.  The last
+//   part only matters for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
+// The accumulation is fp32's (measured: off by at most 2^-21 of the sum of magnitudes).
+//
+// Bound by HBM: 2 D bytes a slot and KV head.  One copy per page fetches keys and values of a head: a box of [row group][K, V][8 rows][D
+// bytes], so that the row groups of K, and those of V, are one stride apart over all pages of a block.
+// Roles as in attn_narrow.cu: warps 0-7 softmax (even and odd blocks), 8 copies, 9 issues MMAs, 10-11 split Q, fetch masks and clean V.
+#include <algorithm>
+
+#include "tree_common.cuh"
+
+namespace pc {
+namespace {
+
+constexpr int RING_BYTES = 128 * 1024;
+constexpr int CLEAN_BARS = 8;                   // more than the tiles between a product with K and the one with V
+constexpr int FLAGS = 8;                        // items a `bad V` flag lives for: more than the roles can be apart
+constexpr int MASK_WORDS = 4;                   // 256 nodes
+constexpr float HEADROOM = 4.f, RESCALE_THRESHOLD = 4.f;       // the largest weight of a row: 2^4 .. 2^8, below 448
+constexpr int MIN_SPAN = 2;
+constexpr int WHOLE_BLOCKS = 6;
+constexpr int PAGES = BLK / PAGE_TOKENS;
+
+struct MergeRecord8 {            // written by the CTA that has a cut unit's first part
+  int32_t n_parts;               // 0: none
+  int32_t row0, flat0, n_rows;   // the prompt's first row; first of the tile's rows (node x head of the KV head), their number
+  int32_t head0;
+  int32_t pad[3];
+};
+static_assert(sizeof(MergeRecord8) == 32, "WS_MERGE");
+
+struct Tree8Params {
+  Kv8View kv;
+  TreeRows rows;
+  int32_t n_q_heads, group, small, over, whole, heads_a_page;
+  float scale_log2;
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  int64_t out_stride;
+  float* lse;
+  int* err_word;
+  MergeRecord8* merges;
+  float *partial_ml, *partial_o;
+};
+
+template <int NC, bool BF16> struct Parts {
+  static constexpr int Q = BF16 ? 2 : 3, P = BF16 ? 3 : 4;
+  static constexpr int NS = NC * Q, NO = NC * P;               // columns of S and O
+  // O of (item parity, block parity); one item's at a time where tensor memory does not hold two
+  static constexpr int O_ITEMS = 2 * NS + 4 * NO <= 512 ? 2 : 1;
+  static constexpr int USED = 2 * NS + 2 * O_ITEMS * NO;
+  static constexpr int TMEM = USED <= 256 ? 256 : 512;
+  static_assert(USED <= 512 && NS % 16 == 0 && NO % 16 == 0, "");
+  __device__ static constexpr int shift(int part) { return BF16 ? (part == 0 ? 0 : part == 1 ? 4 : 18) : (part < 3 ? 4 * part : 22); }
+};
+__device__ __forceinline__ constexpr float pow2(int e) { return e >= 0 ? static_cast<float>(1u << e) : 1.0f / static_cast<float>(1u << -e); }
+
+template <int NC>
+__device__ __forceinline__ Shape shape8(const Tree8Params& a, const SeqPart& p) {
+  if (p.n_nodes == 0) return Shape{0, 0, 1, 0};
+  const int units = (p.n_nodes * a.group + NC - 1) / NC * a.kv.n_kv_heads, n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK;
+  return a.whole ? Shape{units, 1, n_blk, a.over} : Shape{units, n_blk, 1, a.over};
+}
+struct Item {
+  int seq, ctx_len, n_nodes, row0;   // the prompt: its context slots, nodes, first row
+  int flat0, n_rows;                 // the tile: rows flat0 .. flat0 + n_rows - 1 of the KV head's node x head rows
+  int g, blk_begin, blk_end, n_blk;
+  int unit_end;
+};
+template <int NC>
+__device__ __forceinline__ bool next_item(Cursor& cur, const Tree8Params& a, Item* it) {
+  Piece pc;
+  if (!cur.next(a.rows, [&](const SeqPart& p) { return shape8<NC>(a, p); }, &pc)) return false;
+  // the tiles of one KV head follow each other: they share K and V in L2
+  const int flat = pc.part.n_nodes * a.group, tiles = (flat + NC - 1) / NC, tile = pc.unit % tiles;
+  it->seq = pc.seq; it->ctx_len = pc.part.ctx_len; it->n_nodes = pc.part.n_nodes; it->row0 = pc.part.row0;
+  it->flat0 = tile * NC;
+  it->n_rows = min(NC, flat - it->flat0);
+  it->g = pc.unit / tiles;
+  it->blk_begin = pc.blk_begin; it->blk_end = pc.blk_end; it->n_blk = pc.n_blk; it->unit_end = pc.unit_end;
+  if (a.whole) it->blk_end = it->n_blk = (it->ctx_len + it->n_nodes + BLK - 1) / BLK;
+  return true;
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float a, float b) {
+  if constexpr (BF16) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&v);
+  } else {
+    const uint32_t lo = __half_as_ushort(isinf(a) ? __float2half_rn(a) : to_half_sat(a));
+    const uint32_t hi = __half_as_ushort(isinf(b) ? __float2half_rn(b) : to_half_sat(b));
+    return lo | (hi << 16);
+  }
+}
+
+// Per-column reduction over the warp's 32 lanes, transposing as it goes: every step exchanges half of the columns that are left
+// with the lane across and combines the other half.  Lane l returns column l % NC.
+template <int NC, typename Op>
+__device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
+  const int lane = threadIdx.x & 31;
+  float v[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) v[c] = in[c];
+#pragma unroll
+  for (int h = NC / 2; h >= 1; h >>= 1) {
+    const bool hi = (lane & h) != 0;
+#pragma unroll
+    for (int e = 0; e < h; ++e) {
+      const float other = __shfl_xor_sync(0xffffffffu, hi ? v[e] : v[e + h], h);
+      v[e] = op(hi ? v[e + h] : v[e], other);
+    }
+  }
+  float x = v[0];
+#pragma unroll
+  for (int h = NC; h < 32; h <<= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, h));
+  return x;
+}
+// OR of a predicate over the 128 threads of a block parity.
+__device__ __forceinline__ bool parity_any(int i, bool x) {
+  uint32_t y;
+  if (i == 0)
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
+  else
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
+  return y != 0;
+}
+// NaN if a drafted V element (slots s .. end - 1) that a row sees is NaN: it was taken out of the product.
+template <int D>
+__device__ __noinline__ float bad_v(const Tree8Params& a, int seq, int ctx_len, int n_nodes, int s, int end, int row, int node, int g, int col) {
+#pragma unroll 1
+  for (; s < end; ++s) {
+    if (!(node_bits(a.rows, row, node, n_nodes, s - ctx_len) & 1u)) continue;
+    const int page = ld_dep_s32(a.kv.page_table + static_cast<size_t>(seq) * a.kv.pt_stride + s / PAGE_TOKENS);
+    if (page < 0 || page >= a.kv.n_pages) continue;
+    const uint8_t* v = static_cast<const uint8_t*>(a.kv.pages) + page * a.kv.page_stride + (static_cast<size_t>(g) * 2 + 1) * (PAGE_TOKENS * D);
+    if ((v[(s % PAGE_TOKENS) * D + col] & 0x7f) == 0x7f) return __uint_as_float(0x7fffffffu);
+  }
+  return 0.f;
+}
+
+// Byte b of row n of an operand with rows of W bytes (64 or 128) in the swizzle of that width.
+template <int W>
+__device__ __forceinline__ int swizzled(int n, int b) {
+  const int off = n * W + b;
+  return off ^ (W == 128 ? ((off >> 7) & 7) << 4 : ((off >> 7) & 3) << 4);
+}
+
+template <int D, int NC, bool BF16>
+constexpr int smem8() { return 1024 + RING_BYTES + 2 * Parts<NC, BF16>::NS * D + 2 * Parts<NC, BF16>::NO * BLK; }
+
+template <int D, int NC, bool BF16>
+__global__ void __launch_bounds__(TREE_THREADS, 1)
+attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Tree8Params a) {
+  using X = Parts<NC, BF16>;
+  constexpr int GROUP_BYTES = 8 * D;                           // eight rows of K or V
+  constexpr int SBO = 2 * GROUP_BYTES;                         // K and V take turns
+  constexpr int STAGE_BYTES = BLK * 2 * D;
+  constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+  constexpr int Q_BYTES = X::NS * D, P_BYTES = X::NO * BLK;
+  constexpr uint32_t TMEM_O = 2 * X::NS;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], landed[STAGES], empty[STAGES], dirty[CLEAN_BARS], cleaned[CLEAN_BARS], s_full[2], p_full[2], o_full[2], o_free[2], ml_full;
+  __shared__ __align__(16) float4 page_scale[STAGES][PAGES];   // s_K, log2 s_V, 1 / s_V
+  __shared__ __align__(16) float q_scale[2][NC];
+  __shared__ __align__(16) float block_max[2][2][NC][4];       // [block parity][use][row][warp]
+  __shared__ __align__(16) float fin_l[2][2][NC][4];           // [item parity][block parity][row][warp]: a warp's share of the sum
+  __shared__ float fin_m[2][2][NC];
+  __shared__ uint64_t node_mask[2 * NC * MASK_WORDS];
+  __shared__ int bad_flag[FLAGS][2];
+  __shared__ Span shared_span;
+  __shared__ int64_t warp_sums[TREE_THREADS / 32];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int cta_failed;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* q_smem = ring + RING_BYTES;
+  uint8_t* p_smem = q_smem + 2 * Q_BYTES;
+
+  if (threadIdx.x == 0) {
+    cta_failed = 0;
+    for (int i = 0; i < STAGES; ++i) { mbar_init(&landed[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < CLEAN_BARS; ++i) { mbar_init(&dirty[i], 1); mbar_init(&cleaned[i], 2); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 2);          // the two warps that split it
+      mbar_init(&q_empty[i], 9);         // the MMAs and the eight softmax warps
+      mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4);
+      mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 8);
+    }
+    mbar_init(&ml_full, 8);
+    fence_mbar_init();
+  }
+  if (warp == 9) {
+    tmem_alloc<X::TMEM>(&tmem_slot);
+    tmem_relinquish();
+  }
+  if (warp == 8 && lane == 0) prefetch_tmap(&tm);
+  pdl_launch_dependents();
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  pdl_wait();                          // lengths, tables, pages and q may come from the kernel before
+  const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return shape8<NC>(a, p); });
+  const uint32_t tmem = tmem_slot;
+  Cursor cur(span);
+  Item it{};
+
+  if (warp == 8) {
+    // ------------------------------------------------------------ copies
+    uint32_t st = 0, phase = 0;
+    MergeRecord8 rec{};
+    bool ok = true;
+    while (ok && next_item<NC>(cur, a, &it)) {
+      const int last_page = (it.ctx_len + it.n_nodes - 1) / PAGE_TOKENS;
+      const int32_t* table = a.kv.page_table + static_cast<size_t>(it.seq) * a.kv.pt_stride;
+      // Lanes 0-7: page ids (asked for two blocks ahead) and scales (one block ahead).  Pages behind the prompt's last slot repeat its last
+      // page (masked either way); ids outside the pool become one that copies zeros.
+      auto page_at = [&](int blk) {
+        const int page = ld_dep_s32(table + min(blk * PAGES + (lane & (PAGES - 1)), last_page));
+        return static_cast<int>(min(static_cast<uint32_t>(page), static_cast<uint32_t>(a.kv.n_pages)));
+      };
+      auto scale_at = [&](int page) {
+        return page < a.kv.n_pages ? ld_dep_f32x2(a.kv.scales + (static_cast<size_t>(page) * a.kv.n_kv_heads + it.g) * 2) : make_float2(1.f, 1.f);
+      };
+      int page0 = page_at(it.blk_begin), page1 = page_at(min(it.blk_begin + 1, it.blk_end - 1));
+      float2 sc0 = scale_at(page0);
+#pragma unroll 1
+      for (int blk = it.blk_begin; blk < it.blk_end; ++blk) {
+        const int page2 = page_at(min(blk + 2, it.blk_end - 1));
+        ok = __all_sync(0xffffffffu, bar_wait(&empty[st], phase ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+        if (!ok) break;
+        int page[PAGES];
+#pragma unroll
+        for (int p = 0; p < PAGES; ++p) page[p] = __shfl_sync(0xffffffffu, page0, p);
+        if (elect_one()) {
+#pragma unroll
+          for (int p = 0; p < PAGES; ++p)
+            tma_load_5d(ring + st * STAGE_BYTES + p * (PAGE_TOKENS * 2 * D), &tm, &landed[st], 0, 0, 0, 0, page[p] * a.heads_a_page + it.g);
+        }
+        __syncwarp();
+        const float2 sc1 = scale_at(page1);
+        if (lane < PAGES) {
+          const float v = fminf(fmaxf(sc0.y, 0x1p-32f), 0x1p32f);
+          page_scale[st][lane] = make_float4(fminf(fmaxf(sc0.x, 0x1p-32f), 0x1p32f), __log2f(v), 1.0f / v, 0.f);
+        }
+        __syncwarp();
+        if (elect_one()) mbar_arrive_expect_tx(&landed[st], STAGE_BYTES);       // the scales are out, too
+        __syncwarp();
+        sc0 = sc1; page0 = page1; page1 = page2;
+        if (++st == STAGES) { st = 0; phase ^= 1u; }
+      }
+      if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
+        rec.n_parts = static_cast<int>(static_cast<uint64_t>((span.begin + it.unit_end) * span.n_ctas - 1) / static_cast<uint64_t>(span.total)) -
+                      static_cast<int>(blockIdx.x) + 1;
+        rec.row0 = it.row0; rec.flat0 = it.flat0; rec.n_rows = it.n_rows; rec.head0 = it.g * a.group;
+      }
+    }
+    if (!ok) cta_failed = 1;
+    if (lane == 0) a.merges[blockIdx.x] = rec;
+  } else if (warp >= 10) {
+    // ------------------------------------------------------------ Q into parts, masks, V without what does not count
+    constexpr int LANES = D / 16;                                  // a thread has 16 elements of a row
+    const int tid = threadIdx.x - 320;
+    uint32_t n_item = 0, n_tile = 0, n_clean = 0;
+    bool ok = true;
+    while (ok && next_item<NC>(cur, a, &it)) {
+      const int nb = it.blk_end - it.blk_begin, qs = n_item & 1;
+      int* flag = &bad_flag[n_item % FLAGS][warp - 10];            // read at the end of the item that set it, long before its next use
+      if (lane == 0) *flag = 0;
+      ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_item >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
+      if (!ok) break;
+      const int node0 = it.flat0 / a.group;
+#pragma unroll 1
+      for (int c0 = 0; c0 < it.n_rows; c0 += 64 / LANES) {
+        const int c = c0 + tid / LANES, l = tid % LANES;
+        uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (c < it.n_rows) {
+          const int flat = it.flat0 + c, node = flat / a.group;
+          const unsigned short* src = static_cast<const unsigned short*>(a.q) + (it.row0 + node) * a.q_stride + (it.g * a.group + flat - node * a.group) * D + l * 16;
+          raw[0] = ld_dep_v4(src);
+          raw[1] = ld_dep_v4(src + 8);
+        }
+        float x[16], amax = 0.f;
+        const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const uint32_t bits = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+          if constexpr (BF16) x[e] = __uint_as_float(bits << 16);
+          else x[e] = __half2float(__ushort_as_half(static_cast<unsigned short>(bits)));
+          const float m = fabsf(x[e]);
+          if (m < INFINITY) amax = fmaxf(amax, m);
+          else x[e] = __uint_as_float(0x7fffffffu);                // infinity times anything ends as NaN
+        }
+#pragma unroll
+        for (int o = LANES / 2; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        const uint32_t b = __float_as_uint(amax);
+        const int ex = min(max(static_cast<int>(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+        if (c < it.n_rows) {
+          if (l == 0) q_scale[qs][c] = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) * a.scale_log2;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] *= down;
+#pragma unroll
+          for (int part = 0; part < X::Q; ++part) {
+            uint32_t out[4];
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const uint32_t lo = pack_e4m3x2(x[e], x[e + 1]), hi = pack_e4m3x2(x[e + 2], x[e + 3]);
+              out[e >> 2] = lo | hi << 16;
+              const float2 y = unpack_e4m3x2(lo), z = unpack_e4m3x2(hi);
+              x[e] = (x[e] - y.x) * 16.f; x[e + 1] = (x[e + 1] - y.y) * 16.f;
+              x[e + 2] = (x[e + 2] - z.x) * 16.f; x[e + 3] = (x[e + 3] - z.y) * 16.f;
+            }
+            *reinterpret_cast<uint4*>(q_smem + qs * Q_BYTES + swizzled<D>(part * NC + c, l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
+          }
+        }
+      }
+      if (it.blk_end * BLK > it.ctx_len) {
+        const int nodes = (it.flat0 + it.n_rows - 1) / a.group - node0 + 1, words = (it.n_nodes + 63) / 64;
+#pragma unroll 1
+        for (int e = tid; e < nodes * words; e += 64)
+          node_mask[(qs * NC + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + node0 + e / words, node0 + e / words, e % words);
+      }
+      fence_proxy_async_smem();                            // the MMA reads Q through the async proxy
+      __syncwarp();
+      if (elect_one()) mbar_arrive(&q_full[qs]);
+      // V: zeros behind the prompt's last slot, and where a drafted V is NaN (with the flag raised)
+#pragma unroll 1
+      for (int blk = max(it.blk_begin, it.ctx_len / BLK); blk < it.blk_end; ++blk) {
+        const uint32_t t = n_tile + blk - it.blk_begin;
+        // not on `landed`: these warps pass over most tiles, and a parity says nothing about a phase that is not the next one
+        ok = __all_sync(0xffffffffu, bar_wait(&dirty[n_clean % CLEAN_BARS], (n_clean / CLEAN_BARS) & 1u, a.err_word, DEV_ERR_ATTN_CORR));
+        if (!ok) break;
+        uint8_t* v = ring + (t % STAGES) * STAGE_BYTES + GROUP_BYTES;
+        const int r0 = max(it.ctx_len - blk * BLK, 0), r_end = it.ctx_len + it.n_nodes - blk * BLK;
+        bool bad = false;
+        // a thread takes a 16-byte vector (as stored; the swizzle only permutes vectors of the same rows' group) of rows 64 / LANES apart
+#pragma unroll 1
+        for (int r = r0 + tid / LANES; r < BLK; r += 64 / LANES) {
+          uint4* p = reinterpret_cast<uint4*>(v + (r >> 3) * SBO + swizzled<D>(r & 7, (tid % LANES) * 16));
+          if (r >= r_end) {
+            *p = make_uint4(0, 0, 0, 0);
+          } else {
+            const uint4 x = *p;
+            uint32_t w[4] = {x.x, x.y, x.z, x.w}, any = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t nan = ((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+              any |= nan;
+              w[e] &= ~((nan >> 7) * 0xffu);
+            }
+            if (any) { *p = make_uint4(w[0], w[1], w[2], w[3]); bad = true; }
+          }
+        }
+        if (bad) *reinterpret_cast<volatile int*>(flag) = 1;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&cleaned[n_clean % CLEAN_BARS]);
+        ++n_clean;
+      }
+      n_tile += nb;
+      ++n_item;
+    }
+    if (!ok) cta_failed = 1;
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ MMA issuer: the whole warp walks, one lane issues
+    constexpr uint32_t idesc_s = make_idesc_e4m3(BLK, X::NS, 0, 0);
+    constexpr uint32_t idesc_o = make_idesc_e4m3(BLK, X::NO, 1, 0);         // A = V^T: V's rows are the K index
+    auto desc = [](uint32_t addr, uint32_t sbo) { return D == 128 ? make_smem_desc_sw128(addr, 0, sbo) : make_smem_desc_sw64(addr, 0, sbo); };
+    uint32_t n_item = 0, n_tile = 0, n_dirty = 0, n_clean = 0, p_phase = 0;    // p_phase: bit i, the parity to wait for on p_full[i]
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
+    };
+    while (ok && next_item<NC>(cur, a, &it)) {
+      const int nb = it.blk_end - it.blk_begin, par = n_item & 1, ob = X::O_ITEMS == 2 ? par : 0;
+      const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
+      const uint64_t q_desc = desc(smem_u32(q_smem + par * Q_BYTES), GROUP_BYTES);
+      wait(&q_full[par], (n_item >> 1) & 1u);
+#pragma unroll 1
+      for (int j = -2; j < nb && ok; ++j) {                // S0 S1 O0 S2 O1 ...
+        const int i = j & 1;
+        if (j >= 0) {
+          const uint32_t t = n_tile + j;
+          wait(&p_full[i], (p_phase >> i) & 1u);
+          p_phase ^= 1u << i;
+          if (j == 0) wait(&o_free[ob], (o_uses & 1u) ^ 1u);
+          if ((it.blk_begin + j + 1) * BLK > it.ctx_len) {
+            wait(&cleaned[n_clean % CLEAN_BARS], (n_clean / CLEAN_BARS) & 1u);
+            ++n_clean;
+          }
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (elect_one()) {
+            // head size 64 has 64 elements of M in a row: the second 64 TMEM lanes repeat the first (distance 0) and are not read
+            const uint64_t v_desc = desc(smem_u32(ring + (t % STAGES) * STAGE_BYTES + GROUP_BYTES), SBO);
+            const uint64_t p_desc = make_smem_desc_sw128(smem_u32(p_smem + i * P_BYTES), 16, 1024);
+#pragma unroll
+            for (int kk = 0; kk < BLK / 32; ++kk)
+              umma_ss_8bit(tmem + TMEM_O + (ob * 2 + i) * X::NO, v_desc + (kk * 4 * SBO >> 4), p_desc + (kk * 32 >> 4), idesc_o, j > 1 || kk != 0);
+            umma_commit(&empty[t % STAGES]);
+            if (j + 1 == nb) umma_commit(&o_full[ob]);
+          }
+          __syncwarp();
+        }
+        if (j + 2 < nb) {
+          const uint32_t t = n_tile + j + 2;
+          wait(&landed[t % STAGES], (t / STAGES) & 1u);
+          if (!ok) break;
+          if ((it.blk_begin + j + 3) * BLK > it.ctx_len) {
+            if (elect_one()) mbar_arrive(&dirty[n_dirty % CLEAN_BARS]);
+            ++n_dirty;
+          }
+          tc_fence_after_sync();
+          if (elect_one()) {
+            const uint64_t k_desc = desc(smem_u32(ring + (t % STAGES) * STAGE_BYTES), SBO);
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+              umma_ss_8bit(tmem + i * X::NS, k_desc + (kk * 32 >> 4), q_desc + (kk * 32 >> 4), idesc_s, kk != 0);
+            umma_commit(&s_full[i]);
+            if (j + 3 == nb) umma_commit(&q_empty[par]);
+          }
+          __syncwarp();
+        }
+      }
+      n_tile += nb;
+      ++n_item;
+    }
+    if (!ok) cta_failed = 1;
+  } else {
+    // ------------------------------------------------------------ softmax (warps 0-7).  The four warps of a parity meet at a hardware
+    // barrier in every block, so a warp whose wait ran out keeps walking the blocks, without waiting or computing, to the end.
+    const int i = warp >> 2, quarter = warp & 3;
+    const int r = quarter * 32 + lane;                     // slot of the block; element of the head
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    uint8_t* p_row = p_smem + i * P_BYTES + (r & 15);
+    const int p_vec = r >> 4;
+    uint32_t n_item = 0, n_tile = 0, n_s = 0, n_raise = 0;
+    bool ok = true;
+    while (next_item<NC>(cur, a, &it)) {
+      const int nb = it.blk_end - it.blk_begin, par = n_item & 1, ob = X::O_ITEMS == 2 ? par : 0;
+      const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
+      float neg[NC], l[NC];                                // -reference (the same in all threads); sum over this thread's slots only
+      uint32_t unset = 0xffffffffu >> (32 - it.n_rows);    // rows that have seen nothing yet: reference 0, sum and O zero
+#pragma unroll
+      for (int c = 0; c < NC; ++c) { neg[c] = 0.f; l[c] = 0.f; }
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(&q_full[par], (n_item >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // scales, masks
+      for (int j = i; j < nb; j += 2) {
+        const uint32_t t = n_tile + j;
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&landed[t % STAGES], (t / STAGES) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
+        ++n_s;
+        float s[NC];                                       // scores in base 2, the page's log2 s_V added
+        float inv_v = 0.f;
+        bool raise = j == i;                               // does any row's block maximum pass what its reference allows
+        if (ok) {
+          const float4 sc = page_scale[t % STAGES][r / PAGE_TOKENS];
+          inv_v = sc.z;
+          uint32_t seen = 0xffffffffu;
+          const int slot = (it.blk_begin + j) * BLK + r;
+          if (slot >= it.ctx_len) {
+            const int node = slot - it.ctx_len;
+            seen = 0;
+            if (node < it.n_nodes) {
+              const uint64_t* w = node_mask + par * NC * MASK_WORDS + (node >> 6);
+              int at = 0, h = it.flat0 % a.group;
+#pragma unroll 1
+              for (int c = 0; c < it.n_rows; ++c) {
+                seen |= static_cast<uint32_t>((w[at] >> (node & 63)) & 1u) << c;
+                if (++h == a.group) { h = 0; at += MASK_WORDS; }
+              }
+            }
+          }
+          __syncwarp();
+          tc_fence_after_sync();
+#pragma unroll
+          for (int c0 = 0; c0 < NC; c0 += 4) {
+            if (c0 >= it.n_rows) {
+#pragma unroll
+              for (int c = c0; c < c0 + 4; ++c) s[c] = -INFINITY;
+              continue;
+            }
+            uint32_t x[X::Q][4];
+#pragma unroll
+            for (int part = 0; part < X::Q; ++part) tmem_ld_32x4(lanes + i * X::NS + part * NC + c0, x[part]);
+            tmem_wait_ld();
+            const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0]);
+            const float qf[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float y = __uint_as_float(x[X::Q - 1][e]);
+#pragma unroll
+              for (int part = X::Q - 2; part >= 0; --part) y = fmaf(y, 0.0625f, __uint_as_float(x[part][e]));
+              const int c = c0 + e;
+              // columns behind the last row hold anything
+              s[c] = c < it.n_rows && ((seen >> c) & 1u) ? fmaf(y, sc.x * qf[e], sc.y) : -INFINITY;
+              raise |= s[c] + neg[c] > HEADROOM + RESCALE_THRESHOLD;
+            }
+          }
+          if (unset != 0) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) raise |= ((unset >> c) & 1u) && s[c] > -INFINITY;
+          }
+        }
+        if (j != i) raise = parity_any(i, raise);
+        if (raise) {
+          // The rows' exact block maxima: a warp's by a transposing reduction, the block's from four words a row; lane c then works
+          // out row c's new reference and every thread fetches it by shuffles.  Two buffers: between two uses of one lies the
+          // other's barrier.
+          float(*maxima)[4] = block_max[i][n_raise++ & 1];
+          const float mine = column_reduce<NC>(s, [](float x, float y) { return fmaxf(x, y); });
+          if (lane < NC) maxima[lane][quarter] = mine;
+          parity_any(i, false);
+          const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
+          const float now = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) - HEADROOM;             // the block's own reference
+          float old = 0.f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) old = lane == c ? neg[c] : old;
+          const bool fresh = (unset >> lane) & 1u;
+          const bool up = lane < NC && now > -INFINITY && (fresh || now + old > RESCALE_THRESHOLD);
+          const float alpha = !up ? 1.f : fresh ? 0.f : fast_exp2(-old - now);
+          const float next = up ? -now : old;
+          unset &= ~(__ballot_sync(0xffffffffu, up));
+#pragma unroll
+          for (int c = 0; c < NC; ++c) neg[c] = __shfl_sync(0xffffffffu, next, c);
+          if (j != i && ok) {                              // s_full came behind this parity's last product: O is complete
+#pragma unroll 1
+            for (int c0 = 0; c0 < NC; c0 += 4) {
+              if (c0 >= it.n_rows) break;
+              float f[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) f[e] = __shfl_sync(0xffffffffu, alpha, c0 + e);
+#pragma unroll
+              for (int part = 0; part < X::P; ++part) {
+                const uint32_t t_o = lanes + TMEM_O + (ob * 2 + i) * X::NO + part * NC + c0;
+                uint32_t o[4];
+                tmem_ld_32x4(t_o, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[e]);
+                tmem_st_32x4(t_o, o);
+              }
+            }
+            tmem_wait_st();
+#pragma unroll
+            for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, alpha, c);
+          }
+        }
+        if (ok) {
+#pragma unroll
+          for (int c0 = 0; c0 < NC; c0 += 2) {
+            if (c0 >= it.n_rows) break;
+            float w0 = fast_exp2(s[c0] + neg[c0]), w1 = fast_exp2(s[c0 + 1] + neg[c0 + 1]);
+            l[c0] = fmaf(w0, inv_v, l[c0]);                // the row sum has the weights without s_V, and before they are split
+            l[c0 + 1] = fmaf(w1, inv_v, l[c0 + 1]);
+#pragma unroll
+            for (int part = 0; part < X::P; ++part) {
+              const float up = pow2(X::shift(part)), down = pow2(-X::shift(part));
+              const uint32_t two = pack_e4m3x2(w0 * up, w1 * up);
+              if (part + 1 < X::P) {
+                const float2 y = unpack_e4m3x2(two);
+                w0 = fmaf(y.x, -down, w0);
+                w1 = fmaf(y.y, -down, w1);
+              }
+              const int n = part * NC + c0;
+              p_row[n * 128 + ((p_vec ^ (n & 7)) << 4)] = static_cast<uint8_t>(two);
+              p_row[(n + 1) * 128 + ((p_vec ^ ((n + 1) & 7)) << 4)] = static_cast<uint8_t>(two >> 8);
+            }
+          }
+          fence_proxy_async_smem();                        // the MMA reads P through the async proxy
+          tc_fence_before_sync();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(&p_full[i]);
+        }
+      }
+      n_tile += nb;
+      // ---- the piece's end: sums and references of both parities are exchanged; parity i writes rows i * 4 .. i * 4 + 3, i * 4 + 8 ...
+      if (ok) {
+        const float sum = column_reduce<NC>(l, [](float x, float y) { return x + y; });
+        if (lane < NC) fin_l[par][i][lane][quarter] = sum;
+        float mine = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) mine = lane == c ? -neg[c] : mine;
+        if (quarter == 0 && lane < NC) fin_m[par][i][lane] = ((unset >> lane) & 1u) || nb <= i ? -INFINITY : mine;
+        __syncwarp();
+        if (elect_one()) { mbar_arrive(&ml_full); mbar_arrive(&q_empty[par]); }
+        ok = __all_sync(0xffffffffu, bar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR));
+      }
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(&o_full[ob], o_uses & 1u, a.err_word, DEV_ERR_ATTN_CORR));
+      if (ok) {
+        tc_fence_after_sync();
+        const bool whole = it.blk_begin == 0 && it.blk_end == it.n_blk;
+        const size_t part0 = static_cast<size_t>(2 * blockIdx.x + (it.blk_begin == 0 ? 1 : 0)) * BLK;
+        const bool bad = (*reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS][0]) | *reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS][1])) != 0;
+        // Lane c works out row c's two factors; the loop over rows then only scales and stores.
+        float f0 = 0.f, f1 = 0.f;
+        if (lane < it.n_rows) {
+          const float m0 = fin_m[par][0][lane], m1 = fin_m[par][1][lane];
+          const float4 l0 = *reinterpret_cast<const float4*>(fin_l[par][0][lane]), l1 = *reinterpret_cast<const float4*>(fin_l[par][1][lane]);
+          const float M = fmaxf(m0, m1), ref = M == -INFINITY ? 0.f : M;
+          f0 = fast_exp2(m0 - ref);
+          f1 = nb > 1 ? fast_exp2(m1 - ref) : 0.f;
+          float L = f0 * ((l0.x + l0.y) + (l0.z + l0.w));
+          if (nb > 1) L = fmaf(f1, (l1.x + l1.y) + (l1.z + l1.w), L);
+          const int flat = it.flat0 + lane, node = flat / a.group, row = it.row0 + node;
+          bool any = it.ctx_len > 0;                       // does the row see a slot at all (not: are its scores all -inf)
+          if (!any) any = sees_a_node(a.rows, row, node, it.n_nodes);
+          if (whole) {
+            const float inv = any ? 1.0f / L : 0.f;        // a row that sees nothing has an O of zeros
+            f0 *= inv;
+            f1 *= inv;
+            if (warp == 0 && a.lse)
+              a.lse[static_cast<size_t>(row) * a.n_q_heads + it.g * a.group + flat - node * a.group] = any ? (M + log2f(L)) * LN2 : -INFINITY;
+          } else if (warp == 0) {
+            *reinterpret_cast<float2*>(a.partial_ml + (part0 + lane) * 2) = make_float2(M, any ? L : -1.f);
+          }
+        }
+        __syncwarp();
+        int node = (it.flat0 + i * 4) / a.group, h = it.flat0 + i * 4 - node * a.group;
+#pragma unroll 1
+        for (int c0 = i * 4; c0 < it.n_rows; c0 += 8) {    // four rows at a time, the parities in turn
+          float o0[4] = {0.f, 0.f, 0.f, 0.f}, o1[4] = {0.f, 0.f, 0.f, 0.f};
+          uint32_t x0[X::P][4], x1[X::P][4];
+#pragma unroll
+          for (int part = 0; part < X::P; ++part) {
+            tmem_ld_32x4(lanes + TMEM_O + ob * 2 * X::NO + part * NC + c0, x0[part]);
+            tmem_ld_32x4(lanes + TMEM_O + (ob * 2 + 1) * X::NO + part * NC + c0, x1[part]);         // not used when there is one block
+          }
+          tmem_wait_ld();
+#pragma unroll
+          for (int part = X::P - 1; part >= 0; --part) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              o0[e] = fmaf(__uint_as_float(x0[part][e]), pow2(-X::shift(part)), o0[e]);
+              o1[e] = fmaf(__uint_as_float(x1[part][e]), pow2(-X::shift(part)), o1[e]);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int c = c0 + e;
+            float o = o0[e] * __shfl_sync(0xffffffffu, f0, c & 31);
+            const float w1 = __shfl_sync(0xffffffffu, f1, c & 31);
+            if (nb > 1) o = fmaf(o1[e], w1, o);
+            if (r < D && c < it.n_rows) {
+              const int row = it.row0 + node;
+              if (bad)
+                o += bad_v<D>(a, it.seq, it.ctx_len, it.n_nodes, max(it.ctx_len, it.blk_begin * BLK), min(it.ctx_len + it.n_nodes, it.blk_end * BLK), row,
+                              node, it.g, r);
+              if (whole) {
+                static_cast<unsigned short*>(a.out)[static_cast<int64_t>(row) * a.out_stride + (it.g * a.group + h) * D + r] =
+                    static_cast<unsigned short>(pack_out<BF16>(o, 0.f));
+              } else {
+                a.partial_o[(part0 + c) * HEAD_DIM + r] = o;
+              }
+            }
+            if (++h == a.group) { h = 0; ++node; }
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (h += 4; h >= a.group; ++node) h -= a.group; // the other parity's four rows
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&o_free[ob]);
+      }
+      ++n_item;
+    }
+    if (!ok) cta_failed = 1;
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before_sync();
+  __syncthreads();
+  if (cta_failed) {             // let this CTA's bulk copies land before its shared memory is released
+    if (threadIdx.x == 0) {
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < DRAIN_LIMIT_NS) { }
+    }
+    __syncthreads();
+  }
+  if (warp == 9) {
+    tc_fence_after_sync();
+    tmem_dealloc<X::TMEM>(tmem);
+  }
+}
+
+// The parts of a cut unit: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s, one warp per row.
+constexpr int MERGE_WARPS = 8;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) merge_8bit_kernel(Tree8Params a) {
+  constexpr int E = D / 32;                             // columns per lane
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int r = blockIdx.y * MERGE_WARPS + (threadIdx.x >> 5);
+  const volatile MergeRecord8* mr = a.merges + blockIdx.x;
+  const int n_parts = mr->n_parts, n_rows = mr->n_rows;
+  if (n_parts <= 1 || r >= n_rows) return;
+  const int flat = mr->flat0 + r, row = mr->row0 + flat / a.group, head = mr->head0 + flat % a.group;
+  // part 0 is the record's CTA's last item, part s > 0 the first item of the s-th CTA behind it
+  auto slot = [&](int s) { return static_cast<size_t>(2 * (blockIdx.x + s) + (s == 0 ? 1 : 0)) * BLK + r; };
+  // four parts at a time, with a running reference: their sums and results are asked for together
+  bool any = true;
+  float acc[E], M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  for (int s0 = 0; s0 < n_parts; s0 += 4) {
+    float2 v[4];
+    float o[4][E];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      v[u] = make_float2(-INFINITY, 0.f);
+      if (s0 + u >= n_parts) continue;
+      const size_t at = slot(s0 + u);
+      v[u] = ld_dep_f32x2(a.partial_ml + at * 2);
+      if constexpr (E == 4) *reinterpret_cast<float4*>(o[u]) = ld_dep_f32x4(a.partial_o + at * HEAD_DIM + lane * 4);
+      else *reinterpret_cast<float2*>(o[u]) = ld_dep_f32x2(a.partial_o + at * HEAD_DIM + lane * 2);
+    }
+    const float top = fmaxf(fmax3(v[0].x, v[1].x, v[2].x), v[3].x), now = fmaxf(M, top), ref = now == -INFINITY ? 0.f : now;
+    const float before = fast_exp2(M - ref);
+    M = now;
+    L *= before;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] *= before;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (s0 + u >= n_parts) break;
+      if (v[u].y < 0.f) any = false;
+      const float w = fast_exp2(v[u].x - ref);
+      L = fmaf(w, v[u].y, L);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(w, o[u][e], acc[e]);
+    }
+  }
+  const float inv = 1.0f / L;
+  uint32_t pk[E / 2];
+#pragma unroll
+  for (int e = 0; e < E; e += 2) pk[e / 2] = any ? pack_out<BF16>(acc[e] * inv, acc[e + 1] * inv) : 0u;
+  char* dst = static_cast<char*>(a.out) + (static_cast<int64_t>(row) * a.out_stride + head * D + lane * E) * 2;
+  if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pk[0], pk[1]);
+  else *reinterpret_cast<uint32_t*>(dst) = pk[0];
+  if (lane == 0 && a.lse) a.lse[static_cast<size_t>(row) * a.n_q_heads + head] = any ? (M + log2f(L)) * LN2 : -INFINITY;
+}
+
+template <int D, int NC, bool BF16>
+int launch(const CUtensorMap& tm, const Tree8Params& p, int n_ctas, cudaStream_t s) {
+  static bool set[MAX_DEVICES] = {};
+  const int dev = current_device_slot();
+  constexpr int smem = smem8<D, NC, BF16>();
+  if (!set[dev]) {
+    if (cudaFuncSetAttribute(attention_8bit_kernel<D, NC, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    set[dev] = true;
+  }
+  if (launch_pdl(attention_8bit_kernel<D, NC, BF16>, dim3(n_ctas), dim3(TREE_THREADS), smem, s, tm, p) != cudaSuccess) return -1;
+  if (p.whole) return 0;                          // nothing is ever cut
+  const int rows = std::min(NC, p.rows.max_nodes * p.group);
+  return launch_pdl(merge_8bit_kernel<D, BF16>, dim3(n_ctas, (rows + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, s, p) == cudaSuccess ? 0 : -1;
+}
+
+// What the host decides from a call's sizes; returns the most units a prompt can have.
+int64_t set_sizes(Tree8Params& p, const TreeAttention8& t, int* columns) {
+  p.kv = t.kv; p.rows = t.rows;
+  p.n_q_heads = t.n_q_heads;
+  p.group = t.n_q_heads / t.kv.n_kv_heads;
+  const int64_t rows = static_cast<int64_t>(t.rows.max_nodes) * p.group;
+  *columns = rows <= 16 ? 16 : 32;
+  p.over = 2;
+  return (rows + *columns - 1) / *columns * t.kv.n_kv_heads;
+}
+
+}  // namespace
+
+bool tree_attention_8bit_fits(const TreeAttention8& t) {
+  Tree8Params p{};
+  int columns;
+  const int64_t units = set_sizes(p, t, &columns);
+  return units_fit(t.rows.n_seqs, units, t.rows.max_len, 1, p.over);
+}
+
+int launch_tree_attention_8bit(const TreeAttention8& t, int n_sms, cudaStream_t s) {
+  Tree8Params p{};
+  int columns;
+  const int64_t units = set_sizes(p, t, &columns);
+  if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
+  p.scale_log2 = t.scale * LOG2E;
+  p.q = t.q; p.q_stride = t.q_stride;
+  p.out = t.out; p.out_stride = t.out_stride; p.lse = t.lse;
+  char* ws = static_cast<char*>(t.workspace);
+  p.err_word = reinterpret_cast<int*>(ws);
+  p.merges = reinterpret_cast<MergeRecord8*>(ws + WS_MERGE);
+  p.partial_ml = reinterpret_cast<float*>(ws + WS_ML);
+  p.partial_o = reinterpret_cast<float*>(ws + WS_O);
+  const uint64_t d = t.kv.head_dim, head_bytes = 2 * PAGE_TOKENS * d;
+  p.heads_a_page = static_cast<int32_t>(t.kv.page_stride / static_cast<int64_t>(head_bytes));
+  // a box: [row group][K, V][8 rows][D bytes] of one page and KV head
+  const uint64_t dims[5] = {d, 8, 2, 2, static_cast<uint64_t>(t.kv.n_pages - 1) * p.heads_a_page + t.kv.n_kv_heads};
+  const uint64_t strides[4] = {d, PAGE_TOKENS * d, 8 * d, head_bytes};
+  const uint32_t box[5] = {static_cast<uint32_t>(d), 8, 2, 2, 1};
+  CUtensorMap tm;
+  if (encode_u8_map(&tm, t.kv.pages, 5, dims, strides, box) != 0) return -1;
+  p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;
+  const int n_ctas = std::min(n_sms, MAX_CTAS);
+  p.small = small_batch(p.rows.n_seqs, units, p.rows.max_len, 1, p.over) ? 1 : 0;
+  auto run = [&](auto dim, auto nc) {
+    constexpr int D = decltype(dim)::value, NC = decltype(nc)::value;
+    return t.kv.bf16 ? launch<D, NC, true>(tm, p, n_ctas, s) : launch<D, NC, false>(tm, p, n_ctas, s);
+  };
+  using std::integral_constant;
+  if (d == 128) return columns == 16 ? run(integral_constant<int, 128>{}, integral_constant<int, 16>{}) : run(integral_constant<int, 128>{}, integral_constant<int, 32>{});
+  return columns == 16 ? run(integral_constant<int, 64>{}, integral_constant<int, 16>{}) : run(integral_constant<int, 64>{}, integral_constant<int, 32>{});
+}
+
+}  // namespace pc

@@ -171,6 +171,10 @@ int launch_small_gemm(GemmEpilogueKind kind, const void* epilogue, int M, int N,
 int encode_f16_map(CUtensorMap* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                    const uint32_t* box);
 
+// the same for bytes, with a swizzle as wide as the box's rows (64 or 128 bytes)
+int encode_u8_map(CUtensorMap* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                  const uint32_t* box);
+
 // ---- tcgen05 attention (attn_umma.cu)
 struct AttnMaps { CUtensorMap q, k, v; };
 int make_attn_maps(AttnMaps* out, const __half* q, int64_t m_cap, int q_dim, const __half* kctx_layer,
@@ -256,6 +260,56 @@ int launch_compact_slots(const CompactSlots& a, int n_sms, cudaStream_t s);
 // weights [n_lists][n_heads][w_stride], list i of prompt i % n_prompts: slots from[prompt] .. to[prompt] - 1 become 0
 int launch_clear_weights(float* weights, int64_t w_stride, int n_lists, int n_heads, int n_prompts, const int32_t* from, const int32_t* to,
                          cudaStream_t s);
+
+// ---- writing, reading and sharing a batch's pages (append.cu, attn_8bit.cu, pages.cu; entry points in ops_api.cu)
+struct Kv8View {               // percache_kv8_t
+  const void* pages;
+  const float* scales;
+  int64_t page_stride, n_pages;
+  const int32_t* page_table;
+  int32_t pt_stride, n_kv_heads, head_dim, bf16;
+};
+struct NewRows {               // percache_new_rows_t
+  int32_t n_seqs, n_rows, max_len, n_q_heads;
+  const int32_t *ctx_len, *row_start, *position;
+  const void* q;
+  void* q_out;
+  const void *k, *v;
+  int64_t q_stride, q_out_stride, k_stride, v_stride;
+  const float *q_gain, *k_gain, *rope;
+  int32_t n_positions;
+  float eps;
+};
+struct TreeAttention8 {
+  Kv8View kv;
+  TreeRows rows;
+  const void* q;
+  int64_t q_stride;
+  int32_t n_q_heads;
+  float scale;
+  void* out;
+  int64_t out_stride;
+  float* lse;
+  void* workspace;
+};
+int launch_append(const KvView& kv, const NewRows& r, int n_sms, cudaStream_t s);
+int launch_append_8bit(const Kv8View& kv, const NewRows& r, int n_sms, cudaStream_t s);
+bool tree_attention_8bit_fits(const TreeAttention8& a);
+int launch_tree_attention_8bit(const TreeAttention8& a, int n_sms, cudaStream_t s);
+
+constexpr int MAX_POOLS = 8, MAX_FORK_SEQS = 8192;
+struct Pool { char* base; int64_t page_bytes, page_stride, layer_stride; int32_t n_layers, vec; };      // vec: bytes of an access, 16 or 4
+struct Fork {                  // percache_fork_t
+  int32_t n_seqs, n_children, width, width_out, room, n_pools;
+  const int32_t *table, *held, *length, *parent;
+  int32_t *table_out, *held_out, *length_out;
+  int64_t n_pages;
+  const int32_t *refs, *free_list, *free_count;
+  int32_t *refs_out, *free_list_out, *free_count_out, *missing;
+  Pool pools[MAX_POOLS];
+  void* workspace;
+};
+int launch_fork(const Fork& f, int n_sms, cudaStream_t s);
 
 int init_driver_api();   // resolves cuTensorMapEncodeTiled once; 0 on success
 

@@ -20,11 +20,15 @@ decltype(&percache_tree_attention) f_tree;
 decltype(&percache_attention_weights) f_weights;
 decltype(&percache_select_slots) f_select;
 decltype(&percache_compact_slots) f_compact;
-enum Type { I32 = 1, F32 = 2, U8 = 4, BOOL = 8, I64 = 16, U64 = 32, BF16 = 64, F16 = 128 };
-constexpr int N_TYPES = 8;
+decltype(&percache_append_rows) f_append;
+decltype(&percache_append_rows_8bit) f_append8;
+decltype(&percache_tree_attention_8bit) f_tree8;
+decltype(&percache_fork_pages) f_fork;
+enum Type { I32 = 1, F32 = 2, U8 = 4, BOOL = 8, I64 = 16, U64 = 32, BF16 = 64, F16 = 128, F8 = 256 };
+constexpr int N_TYPES = 9;
 PyObject* types[N_TYPES];                       // torch's type objects, in the order of Type
 PyObject* current_stream;                       // device -> torch's current stream there
-PyObject *n_dtype, *n_shape, *n_get_device, *n_stride, *n_is_contiguous, *n_data_ptr;
+PyObject *n_dtype, *n_shape, *n_get_device, *n_stride, *n_is_contiguous, *n_data_ptr, *n_element_size;
 
 struct Ref {                                    // owns a reference
   PyObject* p;
@@ -85,16 +89,23 @@ int type_of(PyObject* x) {                      // 0: none of ours
     if (r.p == types[i]) return 1 << i;
   return 0;
 }
-// Up to three sizes or strides of a tensor; returns how many it has.
-int numbers(PyObject* tuple, int64_t (&out)[3]) {
+// The first N sizes or strides of a tensor; returns how many it has.
+template <int N>
+int numbers(PyObject* tuple, int64_t (&out)[N]) {
   if (!tuple) throw Error{};
   if (!PyTuple_Check(tuple)) refuse("argument", "a tensor");
   const Py_ssize_t n = PyTuple_GET_SIZE(tuple);
-  for (Py_ssize_t i = 0; i < n && i < 3; ++i) out[i] = integer(PyTuple_GET_ITEM(tuple, i));
+  for (Py_ssize_t i = 0; i < n && i < N; ++i) out[i] = integer(PyTuple_GET_ITEM(tuple, i));
   return static_cast<int>(n);
 }
-int shape_of(PyObject* x, int64_t (&out)[3]) {
+template <int N>
+int shape_of(PyObject* x, int64_t (&out)[N]) {
   const Ref r(PyObject_GetAttr(x, n_shape));
+  return numbers(r.p, out);
+}
+template <int N>
+int strides_of(PyObject* x, int64_t (&out)[N]) {
+  const Ref r(PyObject_CallMethodNoArgs(x, n_stride));
   return numbers(r.p, out);
 }
 bool contiguous(PyObject* x) {
@@ -328,12 +339,164 @@ PyObject* compact_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
   });
 }
 
-// bind((addresses of the four entry points), (torch's int32, float32, uint8, bool, int64, uint64, bfloat16, float16), device -> stream)
+// ---------------------------------------------------------------------------------------------------- pages
+// 8-bit pages [pages, kv_heads, 2, 16, head_dim] with dense inner sizes, and their scales [pages, kv_heads, 2].
+percache_kv8_t pages8(PyObject* pages, PyObject* scales, PyObject* page_table, int64_t n_seqs, int type, int device) {
+  percache_kv8_t kv = {};
+  int64_t s[5], st[5], width = 0;
+  if (!(type_of(pages) & (F8 | U8)) || ask(pages, n_get_device) != device) refuse("pages", "a float8_e4m3fn or uint8 tensor on the rows' device");
+  if (shape_of(pages, s) != 5 || s[2] != 2 || s[3] != 16 || s[1] > INT32_MAX || s[4] > INT32_MAX) refuse("pages", "[pages, kv_heads, 2, 16, head_dim]");
+  strides_of(pages, st);
+  if (st[4] != 1 || st[3] != s[4] || st[2] != 16 * s[4] || (s[1] > 1 && st[1] != 32 * s[4])) refuse("pages", "[pages, kv_heads, 2, 16, head_dim] with dense pages");
+  kv.scales = static_cast<float*>(flat<3>(scales, "scales", F32, device, {s[0], s[1], 2}));
+  kv.pages = data_of(pages);
+  kv.page_stride = s[0] > 1 ? st[0] : 32 * s[1] * s[4];
+  kv.n_pages = s[0]; kv.n_kv_heads = static_cast<int32_t>(s[1]); kv.head_dim = static_cast<int32_t>(s[4]);
+  kv.dtype = type == BF16 ? PERCACHE_BF16 : PERCACHE_F16;
+  kv.page_table = static_cast<int32_t*>(flat<2>(page_table, "page_table", I32, device, {n_seqs, -1}, &width));
+  if (width > INT32_MAX) refuse("page_table", "fewer entries a prompt");
+  kv.page_table_stride = static_cast<int32_t>(width);
+  return kv;
+}
+
+// q k v q_out ctx_len row_start max_len k_pool v_pool pages scales page_table ctx_start q_gain k_gain eps rope position stream
+PyObject* append_rows(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 19, [&] {
+    const Strided k = strided(x[1], "k"), v = strided(x[2], "v");
+    same_kind(v, k, "v", "k's type, device and shape");
+    if (v.rows != k.rows || v.heads != k.heads) refuse("v", "k's type, device and shape");
+    if (k.rows > INT32_MAX || k.heads > INT32_MAX || k.dim > INT32_MAX) refuse("k", "fewer rows or heads");
+    const int64_t n_seqs = length_of(x[4], "ctx_len");
+    percache_new_rows_t r = {};
+    r.n_seqs = static_cast<int32_t>(n_seqs); r.n_rows = static_cast<int32_t>(k.rows); r.max_len = int32(x[6], "max_len");
+    r.ctx_len = static_cast<int32_t*>(flat<1>(x[4], "ctx_len", I32, k.device, {n_seqs}));
+    r.row_start = static_cast<int32_t*>(flat<1>(x[5], "row_start", I32, k.device, {n_seqs + 1}));
+    r.k = k.p; r.v = v.p; r.k_row_stride = k.stride; r.v_row_stride = v.stride;
+    if ((x[0] == Py_None) != (x[3] == Py_None)) refuse("q_out", "q and q_out, or neither");
+    if (x[0] != Py_None) {
+      const Strided q = strided(x[0], "q"), o = strided(x[3], "q_out");
+      same_kind(q, k, "q", "[rows, q_heads, head_dim] of k's type on k's device");
+      same_kind(o, q, "q_out", "q's type, device and shape");
+      if (q.rows != k.rows || q.heads > INT32_MAX) refuse("q", "as many rows as k");
+      if (o.rows != q.rows || o.heads != q.heads) refuse("q_out", "q's type, device and shape");
+      r.q = q.p; r.q_out = o.p; r.q_row_stride = q.stride; r.q_out_row_stride = o.stride; r.n_q_heads = static_cast<int32_t>(q.heads);
+    }
+    if (x[13] != Py_None) r.q_gain = static_cast<float*>(flat<1>(x[13], "q_gain", F32, k.device, {k.dim}));
+    if (x[14] != Py_None) r.k_gain = static_cast<float*>(flat<1>(x[14], "k_gain", F32, k.device, {k.dim}));
+    r.eps = number(x[15]);
+    if (x[16] != Py_None) {
+      int64_t s[3] = {0, 0, 0};
+      shape_of(x[16], s);
+      if (s[0] > INT32_MAX) refuse("rope", "fewer positions");
+      r.rope = static_cast<float*>(flat<3>(x[16], "rope", F32, k.device, {-1, k.dim / 2, 2}));
+      r.n_positions = static_cast<int32_t>(s[0]);
+    }
+    r.position = static_cast<int32_t*>(optional(x[17], "position", I32, k.device, k.rows));
+    if ((x[7] == Py_None) == (x[9] == Py_None) || (x[7] == Py_None) != (x[8] == Py_None) || (x[9] == Py_None) != (x[10] == Py_None))
+      refuse("pools", "either k_pool and v_pool or pages and scales");
+    if (x[9] != Py_None) {
+      if (x[12] != Py_None) refuse("ctx_start", "a page_table with 8-bit pages");
+      const percache_kv8_t kv = pages8(x[9], x[10], x[11], n_seqs, k.type, k.device);
+      if (kv.n_kv_heads != k.heads || kv.head_dim != k.dim) refuse("pages", "k's heads");
+      void* stream = stream_of(x[18], k.device);
+      return released([&] { return f_append8(k.device, stream, &kv, &r); });
+    }
+    const Strided pool = strided(x[7], "k_pool");
+    same_kind(pool, k, "k_pool", "k's type, device and heads");
+    if (pool.heads != k.heads) refuse("k_pool", "k's type, device and heads");
+    const percache_kv_t kv = pools(pool, x[8], x[11], x[12], n_seqs);
+    void* stream = stream_of(x[18], k.device);
+    return released([&] { return f_append(k.device, stream, &kv, &r); });
+  });
+}
+
+// q pages scales out lse ctx_len row_start max_nodes max_len workspace mask page_table scale stream
+PyObject* tree_attention_8bit(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 14, [&] {
+    const Strided q = strided(x[0], "q"), out = strided(x[3], "out");
+    const int64_t n_seqs = length_of(x[5], "ctx_len");
+    const percache_kv8_t kv = pages8(x[1], x[2], x[11], n_seqs, q.type, q.device);
+    if (kv.head_dim != q.dim) refuse("q", "[rows, q_heads, head_dim] with the pages' head_dim");
+    const percache_rows_t rows = batch(q, q, x[5], x[6], x[10], x[7], x[8], n_seqs);
+    same_kind(out, q, "out", "q's type, device and shape");
+    if (out.rows != q.rows || out.heads != q.heads) refuse("out", "q's type, device and shape");
+    float* lse = x[4] == Py_None ? nullptr : static_cast<float*>(flat<2>(x[4], "lse", F32, q.device, {q.rows, q.heads}));
+    const Space ws = workspace_of(x[9], q.device);
+    const float scale = scale_of(x[12], q.dim);
+    void* stream = stream_of(x[13], q.device);
+    return released([&] {
+      return f_tree8(q.device, stream, &kv, &rows, q.p, q.stride, static_cast<int32_t>(q.heads), scale, out.p, out.stride, lse, ws.p, ws.bytes);
+    });
+  });
+}
+
+// A pool [layers, pages, ...] whose pages are dense.
+percache_pool_t pool_of(PyObject* x, int device, int64_t n_pages) {
+  constexpr int MOST = 8;
+  int64_t s[MOST], st[MOST];
+  percache_pool_t p = {};
+  if (ask(x, n_get_device) != device) refuse("pools", "tensors on the tables' device");
+  const int dims = shape_of(x, s);
+  if (dims < 2 || dims > MOST || s[1] != n_pages || s[0] < 1 || s[0] > INT32_MAX) refuse("pools", "[layers, pages, ...] with as many pages as refs");
+  strides_of(x, st);
+  const int64_t size = ask(x, n_element_size);
+  int64_t dense = 1;
+  for (int i = dims - 1; i >= 2; --i) {
+    if (s[i] != 1 && st[i] != dense) refuse("pools", "dense pages");
+    dense *= s[i];
+  }
+  if ((s[0] > 1 && st[0] <= 0) || (s[1] > 1 && st[1] < dense)) refuse("pools", "layers and pages that do not overlap");
+  p.base = data_of(x);
+  p.page_bytes = dense * size;
+  p.page_stride = s[1] > 1 ? st[1] * size : p.page_bytes;
+  p.layer_stride = s[0] > 1 ? st[0] * size : 0;
+  p.n_layers = static_cast<int32_t>(s[0]);
+  return p;
+}
+
+// page_table held length parent table_out held_out length_out refs free_list free_count missing pools room refs_out free_list_out
+// free_count_out workspace stream
+PyObject* fork_pages(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 18, [&] {
+    const int device = static_cast<int>(ask(x[0], n_get_device));
+    if (device < 0) refuse("page_table", "a tensor on a CUDA device");
+    percache_fork_t f = {};
+    const int64_t n_seqs = length_of(x[1], "held"), n_children = length_of(x[3], "parent");
+    int64_t width = 0, width_out = 0, n_pages = length_of(x[7], "refs");
+    auto ints = [&](int i, const char* name, int64_t size) { return static_cast<int32_t*>(flat<1>(x[i], name, I32, device, {size})); };
+    f.n_seqs = static_cast<int32_t>(n_seqs); f.n_children = static_cast<int32_t>(n_children);
+    f.page_table = static_cast<int32_t*>(flat<2>(x[0], "page_table", I32, device, {n_seqs, -1}, &width));
+    f.held = ints(1, "held", n_seqs); f.length = ints(2, "length", n_seqs); f.parent = ints(3, "parent", n_children);
+    f.table_out = static_cast<int32_t*>(flat<2>(x[4], "table_out", I32, device, {n_children, -1}, &width_out));
+    f.held_out = ints(5, "held_out", n_children); f.length_out = ints(6, "length_out", n_children);
+    if (width > INT32_MAX || width_out > INT32_MAX) refuse("page_table", "fewer entries a sequence");
+    f.page_table_stride = static_cast<int32_t>(width); f.table_out_stride = static_cast<int32_t>(width_out);
+    f.n_pages = n_pages;
+    f.refs = ints(7, "refs", n_pages); f.free_list = ints(8, "free_list", n_pages); f.free_count = ints(9, "free_count", 1);
+    f.missing = ints(10, "missing", 1);
+    f.refs_out = ints(13, "refs_out", n_pages); f.free_list_out = ints(14, "free_list_out", n_pages);
+    f.free_count_out = ints(15, "free_count_out", 1);
+    f.room = int32(x[12], "room");
+    const Ref list(PySequence_Fast(x[11], "pools: expected a sequence of tensors"));
+    if (!list.p) throw Error{};
+    const Py_ssize_t n_pools = PySequence_Fast_GET_SIZE(list.p);
+    if (n_pools > PERCACHE_MAX_POOLS) refuse("pools", "at most eight tensors");
+    percache_pool_t pool[PERCACHE_MAX_POOLS];
+    for (Py_ssize_t i = 0; i < n_pools; ++i) pool[i] = pool_of(PySequence_Fast_GET_ITEM(list.p, i), device, n_pages);
+    f.pools = pool; f.n_pools = static_cast<int32_t>(n_pools);
+    const Space ws = workspace_of(x[16], device);
+    void* stream = stream_of(x[17], device);
+    return released([&] { return f_fork(device, stream, &f, ws.p, ws.bytes); });
+  });
+}
+
+// bind((addresses of the eight entry points), (torch's int32, float32, uint8, bool, int64, uint64, bfloat16, float16,
+// float8_e4m3fn), device -> stream)
 PyObject* bind(PyObject*, PyObject* args) {
-  unsigned long long f[4];
+  unsigned long long f[8];
   PyObject *t[N_TYPES], *stream;
-  if (!PyArg_ParseTuple(args, "(KKKK)(OOOOOOOO)O", &f[0], &f[1], &f[2], &f[3], &t[0], &t[1], &t[2], &t[3], &t[4], &t[5], &t[6], &t[7],
-                        &stream))
+  if (!PyArg_ParseTuple(args, "(KKKKKKKK)(OOOOOOOOO)O", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &t[0], &t[1], &t[2], &t[3],
+                        &t[4], &t[5], &t[6], &t[7], &t[8], &stream))
     return nullptr;
   for (int i = 0; i < N_TYPES; ++i) {
     Py_INCREF(t[i]);
@@ -345,6 +508,10 @@ PyObject* bind(PyObject*, PyObject* args) {
   f_weights = reinterpret_cast<decltype(f_weights)>(f[1]);
   f_select = reinterpret_cast<decltype(f_select)>(f[2]);
   f_compact = reinterpret_cast<decltype(f_compact)>(f[3]);
+  f_append = reinterpret_cast<decltype(f_append)>(f[4]);
+  f_append8 = reinterpret_cast<decltype(f_append8)>(f[5]);
+  f_tree8 = reinterpret_cast<decltype(f_tree8)>(f[6]);
+  f_fork = reinterpret_cast<decltype(f_fork)>(f[7]);
   Py_RETURN_NONE;
 }
 
@@ -355,6 +522,9 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          {"attention_weights", fast(attention_weights), METH_FASTCALL, nullptr},
                          {"select_slots", fast(select_slots), METH_FASTCALL, nullptr},
                          {"compact_slots", fast(compact_slots), METH_FASTCALL, nullptr},
+                         {"append_rows", fast(append_rows), METH_FASTCALL, nullptr},
+                         {"tree_attention_8bit", fast(tree_attention_8bit), METH_FASTCALL, nullptr},
+                         {"fork_pages", fast(fork_pages), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_binding", "Checked calls of the cache operators.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -367,6 +537,7 @@ PyMODINIT_FUNC PyInit__ops_binding() {
   n_stride = PyUnicode_InternFromString("stride");
   n_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   n_data_ptr = PyUnicode_InternFromString("data_ptr");
-  if (!n_dtype || !n_shape || !n_get_device || !n_stride || !n_is_contiguous || !n_data_ptr) return nullptr;
+  n_element_size = PyUnicode_InternFromString("element_size");
+  if (!n_element_size || !n_dtype || !n_shape || !n_get_device || !n_stride || !n_is_contiguous || !n_data_ptr) return nullptr;
   return PyModule_Create(&module);
 }

@@ -1,0 +1,284 @@
+// Sequences that go on as others: page tables, counters, the free list, and copies of the pages that two of them would write.
+//
+// Three things depend on each other: how many pages every child takes (a prefix sum over the children), the counters (a page is free when the last
+// holder lets go), and the free list (freed pages in ascending order).  fork_plan_kernel: one block works the children out, while the
+// others clear the marks of freed pages and, where the outputs are arrays of their own, copy the counters and the list.  fork_kernel: tables,
+// counters and copies by all blocks; the block that is last with its tables and counters lists the freed pages, while the others copy on.
+// Bound by HBM where pages are copied (each read once, written once), else by the latency of two launches.
+#include <algorithm>
+
+#include "slot_row.cuh"
+
+namespace pc {
+namespace {
+
+struct Child { int32_t parent, have, got, full; int64_t start; };      // `have` pages of the parent's, `got` of the list's from place `start` on
+struct PlanHead { int32_t n_copies, count, taken, done; };
+// The workspace's first 256 bytes belong to the calls that report in them.
+constexpr size_t WS_HEAD = 256, WS_CHILD = 512, WS_COPY = WS_CHILD + sizeof(Child) * MAX_FORK_SEQS, WS_KIDS = WS_COPY + sizeof(int2) * MAX_FORK_SEQS,
+                 WS_MARKS = WS_KIDS + sizeof(int32_t) * MAX_FORK_SEQS;
+constexpr int64_t MAX_PAGES = INT64_C(1) << 26;
+static_assert(WS_MARKS + MAX_PAGES / 8 <= (24u << 20), "PERCACHE_OPS_WORKSPACE_BYTES");
+
+struct Plan {
+  PlanHead* head;
+  Child* child;
+  int2* copy;                    // page to page
+  int32_t* kids;                 // children of a sequence
+  uint32_t* marks;               // a bit per page: freed by this call
+};
+__host__ __device__ inline Plan plan_of(void* ws) {
+  char* w = static_cast<char*>(ws);
+  return Plan{reinterpret_cast<PlanHead*>(w + WS_HEAD), reinterpret_cast<Child*>(w + WS_CHILD), reinterpret_cast<int2*>(w + WS_COPY),
+              reinterpret_cast<int32_t*>(w + WS_KIDS), reinterpret_cast<uint32_t*>(w + WS_MARKS)};
+}
+
+struct Seq { int held, length; };
+__device__ __forceinline__ Seq seq_of(const Fork& f, int s) {
+  Seq q;
+  q.held = min(max(ld_dep_s32(f.held + s), 0), f.width);
+  q.length = min(max(ld_dep_s32(f.length + s), 0), q.held * PAGE_TOKENS);
+  return q;
+}
+
+// Inclusive sum over a block of 1024 threads; `total`: of all.
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* warp_sums, int64_t* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  int64_t all = 0;
+#pragma unroll 1
+  for (int w = 0; w < warps; ++w) {
+    const int64_t y = warp_sums[w];
+    if (w < warp) x += y;
+    all += y;
+  }
+  __syncthreads();
+  *total = all;
+  return x;
+}
+
+constexpr int PLAN_THREADS = 1024;
+__global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const __grid_constant__ Fork f) {
+  extern __shared__ int32_t by_seq[];             // [n_seqs] first child, [n_seqs] number of children
+  __shared__ int64_t warp_sums[PLAN_THREADS / 32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const Plan plan = plan_of(f.workspace);
+  const int tid = threadIdx.x;
+  if (blockIdx.x > 0) {
+    const int64_t step = static_cast<int64_t>(gridDim.x - 1) * PLAN_THREADS, at = static_cast<int64_t>(blockIdx.x - 1) * PLAN_THREADS + tid;
+    for (int64_t i = at; i < (f.n_pages + 31) / 32; i += step) plan.marks[i] = 0u;
+    if (f.refs_out != f.refs)
+      for (int64_t i = at; i < f.n_pages; i += step) {
+        const int a = ld_dep_s32(f.refs + i), b = ld_dep_s32(f.free_list + i);
+        f.refs_out[i] = a;
+        f.free_list_out[i] = b;
+      }
+    return;
+  }
+  int32_t *first = by_seq, *kids = by_seq + f.n_seqs;
+  for (int s = tid; s < f.n_seqs; s += PLAN_THREADS) { first[s] = INT32_MAX; kids[s] = 0; }
+  const int count = static_cast<int>(min(static_cast<int64_t>(max(ld_dep_s32(f.free_count), 0)), f.n_pages));
+  __syncthreads();
+  for (int i = tid; i < f.n_children; i += PLAN_THREADS) {
+    const int p = ld_dep_s32(f.parent + i);
+    if (p >= 0 && p < f.n_seqs) {
+      atomicMin(first + p, i);
+      atomicAdd(kids + p, 1);
+    }
+  }
+  __syncthreads();
+  for (int s = tid; s < f.n_seqs; s += PLAN_THREADS) plan.kids[s] = kids[s];
+  // pages taken in the upper bits, copies in the lower 16: one sum over the children in order
+  int64_t before = 0;
+  for (int i0 = 0; i0 < f.n_children; i0 += PLAN_THREADS) {
+    const int i = i0 + tid;
+    Child c{-1, 0, 0, 0, 0};
+    int fresh = 0;
+    bool part = false, heir = false;
+    Seq q{0, 0};
+    if (i < f.n_children) {
+      c.parent = ld_dep_s32(f.parent + i);
+      if (c.parent < 0 || c.parent >= f.n_seqs) c.parent = -1;
+      if (c.parent >= 0) {
+        q = seq_of(f, c.parent);
+        heir = first[c.parent] == i;
+        c.full = q.length / PAGE_TOKENS;
+        part = !heir && q.length % PAGE_TOKENS != 0 && c.full < f.width_out;
+        c.have = min(heir ? q.held : c.full, f.width_out);
+        const int want = static_cast<int>(min((static_cast<int64_t>(q.length) + f.room + PAGE_TOKENS - 1) / PAGE_TOKENS, static_cast<int64_t>(f.width_out)));
+        fresh = max(want - c.have, 0);
+      }
+    }
+    int64_t all;
+    const int64_t fresh_sum = before + block_sum(fresh, warp_sums, &all);
+    before += all;
+    c.start = fresh_sum - fresh;
+    c.got = static_cast<int>(min(max(static_cast<int64_t>(count) - c.start, static_cast<int64_t>(0)), static_cast<int64_t>(fresh)));
+    if (i < f.n_children) {
+      plan.child[i] = c;
+      f.held_out[i] = c.have + c.got;
+      f.length_out[i] = c.parent < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(q.length), static_cast<int64_t>(c.have + c.got) * PAGE_TOKENS));
+      // -1: nothing to copy (the place of a child's copy is its own, so that no order has to be found)
+      const bool copies = part && c.got > 0;
+      plan.copy[i] = copies ? make_int2(ld_dep_s32(f.table + static_cast<size_t>(c.parent) * f.width + c.full), ld_dep_s32(f.free_list + count - 1 - c.start))
+                            : make_int2(-1, -1);
+    }
+  }
+  if (tid == 0) {
+    const int64_t taken = min(before, static_cast<int64_t>(count));
+    f.missing[0] = static_cast<int>(min(before - taken, static_cast<int64_t>(INT32_MAX)));
+    *plan.head = PlanHead{0, count, static_cast<int>(taken), 0};
+  }
+}
+
+constexpr int FORK_THREADS = 256;
+constexpr int COPY_BYTES = 16384;                 // of a page that a block takes at a time
+
+__device__ __forceinline__ int volatile_s32(const int32_t* p) { return *reinterpret_cast<const volatile int32_t*>(p); }
+
+__global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constant__ Fork f, int chunks) {
+  __shared__ int64_t warp_sums[FORK_THREADS / 32];
+  __shared__ int last;
+  __shared__ int2 copies[FORK_THREADS];
+  pdl_launch_dependents();
+  pdl_wait();
+  const Plan plan = plan_of(f.workspace);
+  const int tid = threadIdx.x;
+  const int count = volatile_s32(&plan.head->count);
+
+  // ---- tables, and the counters of pages that were taken
+  for (int i = blockIdx.x; i < f.n_children; i += gridDim.x) {
+    const volatile Child* c = plan.child + i;
+    const int parent = c->parent, have = c->have, got = c->got;
+    const int64_t top = count - 1 - c->start;
+    for (int j = tid; j < f.width_out; j += FORK_THREADS) {
+      int page = -1;
+      if (j < have) page = ld_dep_s32(f.table + static_cast<size_t>(parent) * f.width + j);
+      else if (j < have + got) {
+        page = ld_dep_s32(f.free_list + top - (j - have));
+        if (page >= 0 && page < f.n_pages) f.refs_out[page] = 1;
+      }
+      f.table_out[static_cast<size_t>(i) * f.width_out + j] = page;
+    }
+  }
+  // ---- counters: from the other end of the grid
+  for (int s = gridDim.x - 1 - blockIdx.x; s < f.n_seqs; s += gridDim.x) {
+    const int kids = volatile_s32(plan.kids + s);
+    if (kids == 1) continue;
+    const Seq q = seq_of(f, s);
+    const int n = kids == 0 ? q.held : q.length / PAGE_TOKENS;
+    for (int j = tid; j < n; j += FORK_THREADS) {
+      const int page = ld_dep_s32(f.table + static_cast<size_t>(s) * f.width + j);
+      if (page < 0 || page >= f.n_pages) continue;
+      const int before = atomicAdd(f.refs_out + page, kids - 1);
+      if (kids == 0 && before == 1) atomicOr(plan.marks + (page >> 5), 1u << (page & 31));
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) last = atomicAdd(&plan.head->done, 1) == static_cast<int>(gridDim.x) - 1;
+  __syncthreads();
+  if (last) {
+    __threadfence();
+    // ---- the freed pages behind the list's rest, in ascending order
+    const int words = static_cast<int>((f.n_pages + 31) / 32);
+    int64_t at = count - volatile_s32(&plan.head->taken);
+    for (int w0 = 0; w0 < words; w0 += FORK_THREADS * 4) {
+      uint32_t m[4];
+      int n = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int w = w0 + tid * 4 + u;
+        m[u] = w < words ? *reinterpret_cast<const volatile uint32_t*>(plan.marks + w) : 0u;
+        n += __popc(m[u]);
+      }
+      int64_t all;
+      int64_t to = at + block_sum(n, warp_sums, &all) - n;
+      at += all;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        for (uint32_t x = m[u]; x; x &= x - 1, ++to)
+          if (to < f.n_pages) f.free_list_out[to] = (w0 + tid * 4 + u) * 32 + __ffs(x) - 1;
+    }
+    if (tid == 0) f.free_count_out[0] = static_cast<int>(min(at, f.n_pages));
+  }
+
+  // ---- copies
+  if (chunks == 0) return;
+  for (int i0 = 0; i0 < f.n_children; i0 += FORK_THREADS) {
+    // this window's copies, one behind the other
+    int2 c = make_int2(-1, -1);
+    if (i0 + tid < f.n_children) {
+      const volatile int2* p = plan.copy + i0 + tid;
+      c = make_int2(p->x, p->y);
+    }
+    const bool mine = c.x >= 0 && c.x < f.n_pages && c.y >= 0 && c.y < f.n_pages && c.x != c.y;
+    int64_t n;
+    const int64_t place = block_sum(mine ? 1 : 0, warp_sums, &n);
+    if (mine) copies[place - 1] = c;
+    __syncthreads();
+#pragma unroll 1
+    for (int64_t u = blockIdx.x; u < n * chunks; u += gridDim.x) {
+      const int2 pair = copies[u / chunks];
+      int chunk = static_cast<int>(u % chunks), k = 0;
+#pragma unroll 1
+      for (;; ++k) {                               // which pool, layer and stretch of the page
+        const int per = static_cast<int>((f.pools[k].page_bytes + COPY_BYTES - 1) / COPY_BYTES) * f.pools[k].n_layers;
+        if (chunk < per || k + 1 == f.n_pools) break;
+        chunk -= per;
+      }
+      const Pool& pool = f.pools[k];
+      const int pieces = static_cast<int>((pool.page_bytes + COPY_BYTES - 1) / COPY_BYTES);
+      const int64_t off = static_cast<int64_t>(chunk % pieces) * COPY_BYTES, len = min(pool.page_bytes - off, static_cast<int64_t>(COPY_BYTES));
+      char* base = pool.base + (chunk / pieces) * pool.layer_stride + off;
+      const char* src = base + pair.x * pool.page_stride;
+      char* dst = base + pair.y * pool.page_stride;
+      if (pool.vec == 16) {
+        uint4 v[COPY_BYTES / 16 / FORK_THREADS];
+#pragma unroll
+        for (int e = 0; e < COPY_BYTES / 16 / FORK_THREADS; ++e) {
+          const int at = (e * FORK_THREADS + tid) * 16;
+          if (at < len) v[e] = ld_dep_v4(src + at);
+        }
+#pragma unroll
+        for (int e = 0; e < COPY_BYTES / 16 / FORK_THREADS; ++e) {
+          const int at = (e * FORK_THREADS + tid) * 16;
+          if (at < len) *reinterpret_cast<uint4*>(dst + at) = v[e];
+        }
+      } else {
+        for (int at = tid * 4; at < len; at += FORK_THREADS * 4) *reinterpret_cast<int*>(dst + at) = ld_dep_s32(src + at);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+int launch_fork(const Fork& f, int n_sms, cudaStream_t s) {
+  static bool set[MAX_DEVICES] = {};
+  const int dev = current_device_slot();
+  if (!set[dev]) {
+    if (cudaFuncSetAttribute(fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_FORK_SEQS * 8) != cudaSuccess) return -1;
+    set[dev] = true;
+  }
+  int64_t chunks = 0;
+  for (int k = 0; k < f.n_pools; ++k) chunks += (f.pools[k].page_bytes + COPY_BYTES - 1) / COPY_BYTES * f.pools[k].n_layers;
+  if (chunks > INT32_MAX) return -2;
+  const int64_t lists = f.refs_out != f.refs ? f.n_pages : (f.n_pages + 31) / 32;
+  const int list_blocks = static_cast<int>(std::min<int64_t>((lists + PLAN_THREADS - 1) / PLAN_THREADS, n_sms));
+  if (launch_pdl(fork_plan_kernel, dim3(1 + std::max(list_blocks, 1)), dim3(PLAN_THREADS), static_cast<size_t>(f.n_seqs) * 8, s, f) != cudaSuccess) return -1;
+  // as many blocks as there is work at most: rows of tables and counters, and the copies if every child but one makes one
+  const int64_t work = std::max<int64_t>(std::max(f.n_seqs, f.n_children), chunks * std::max(f.n_children - 1, 0));
+  const int blocks = static_cast<int>(std::max<int64_t>(std::min<int64_t>(work, static_cast<int64_t>(n_sms) * 6), 1));
+  return launch_pdl(fork_kernel, dim3(blocks), dim3(FORK_THREADS), 0, s, f, static_cast<int>(chunks)) == cudaSuccess ? 0 : -1;
+}
+
+}  // namespace pc

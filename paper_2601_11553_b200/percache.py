@@ -91,6 +91,32 @@ class RowsStruct(C.Structure):
                 ("reserved0", C.c_int32)]
 
 
+class Kv8Struct(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("scales", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int64),
+                ("page_table", C.c_void_p), ("page_table_stride", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+class NewRowsStruct(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("n_seqs", "n_rows", "max_len", "n_q_heads")] +
+                [(n, C.c_void_p) for n in ("ctx_len", "row_start", "position", "q", "q_out", "k", "v")] +
+                [(n, C.c_int64) for n in ("q_row_stride", "q_out_row_stride", "k_row_stride", "v_row_stride")] +
+                [(n, C.c_void_p) for n in ("q_gain", "k_gain", "rope")] + [("n_positions", C.c_int32), ("eps", C.c_float)])
+
+
+class PoolStruct(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_bytes", C.c_int64), ("page_stride", C.c_int64), ("layer_stride", C.c_int64),
+                ("n_layers", C.c_int32), ("reserved0", C.c_int32)]
+
+
+class ForkStruct(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("n_seqs", "n_children", "page_table_stride", "table_out_stride")] +
+                [(n, C.c_void_p) for n in ("page_table", "held", "length", "parent", "table_out", "held_out", "length_out")] +
+                [("n_pages", C.c_int64)] +
+                [(n, C.c_void_p) for n in ("refs", "free_list", "free_count", "refs_out", "free_list_out", "free_count_out", "missing")] +
+                [("room", C.c_int32), ("n_pools", C.c_int32), ("pools", C.POINTER(PoolStruct))])
+
+
 _lib = None
 
 
@@ -139,6 +165,10 @@ def load_library() -> C.CDLL:
     lib.percache_attention_weights.argtypes = [i32, vp, kvp, rowsp, vp, i64, i32, f32, vp, vp, f32, vp, vp, i64, vp, i64]
     lib.percache_select_slots.argtypes = [i32, vp, vp, i64, vp, i32, i32, i32, i32, i32, i32, vp, vp]
     lib.percache_compact_slots.argtypes = [i32, vp, kvp, i32, i32, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, i64]
+    lib.percache_append_rows.argtypes = [i32, vp, kvp, C.POINTER(NewRowsStruct)]
+    lib.percache_append_rows_8bit.argtypes = [i32, vp, C.POINTER(Kv8Struct), C.POINTER(NewRowsStruct)]
+    lib.percache_tree_attention_8bit.argtypes = [i32, vp, C.POINTER(Kv8Struct), rowsp, vp, i64, i32, f32, vp, i64, vp, vp, i64]
+    lib.percache_fork_pages.argtypes = [i32, vp, C.POINTER(ForkStruct), vp, i64]
     lib.percache_ops_status.argtypes = [i32, vp, vp]
     lib.percache_path_key.argtypes = [C.POINTER(u64), i32]
     lib.percache_path_key.restype = u64
@@ -546,8 +576,11 @@ def _ops() -> Any:
         except ImportError as e:
             raise PerCacheError(E_CUDA, f"{e} (build it: python -m paper_2601_11553_b200.build)") from e
         m.bind(tuple(C.cast(f, C.c_void_p).value for f in (lib.percache_tree_attention, lib.percache_attention_weights,
-                                                           lib.percache_select_slots, lib.percache_compact_slots)),
-               (torch.int32, torch.float32, torch.uint8, torch.bool, torch.int64, torch.uint64, torch.bfloat16, torch.float16),
+                                                           lib.percache_select_slots, lib.percache_compact_slots,
+                                                           lib.percache_append_rows, lib.percache_append_rows_8bit,
+                                                           lib.percache_tree_attention_8bit, lib.percache_fork_pages)),
+               (torch.int32, torch.float32, torch.uint8, torch.bool, torch.int64, torch.uint64, torch.bfloat16, torch.float16,
+                torch.float8_e4m3fn),
                # without the Python objects of torch.cuda.current_stream, where torch has it (a small call's time is the host's)
                getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream))
         _binding = m
@@ -598,6 +631,44 @@ def compact_slots(k: Any, v: Any, keep: Any, count: Any, *, max_len: int, weight
     weights_out = weights if weights_out is None else weights_out
     _check(_ops().compact_slots(k, v, keep, count, max_len, weights, weights_out, first, page_table, ctx_start, dst_page_table,
                                 dst_start, stream), "percache_compact_slots")
+
+
+# ---------------------------------------------------------------------- writing, reading and sharing a batch's pages
+def append_rows(q: Any, k: Any, v: Any, q_out: Any = None, *, ctx_len: Any, row_start: Any, max_len: int, k_pool: Any = None,
+                v_pool: Any = None, pages: Any = None, scales: Any = None, page_table: Any = None, ctx_start: Any = None,
+                q_gain: Any = None, k_gain: Any = None, eps: float = 1e-6, rope: Any = None, position: Any = None,
+                stream: Optional[int] = None) -> Any:
+    """percache_append_rows (k_pool, v_pool) or percache_append_rows_8bit (pages, scales): new rows on their way into the cache.
+
+    q [rows, q_heads, head_dim] and k, v [rows, kv_heads, head_dim] may be parts of one projection's output.  Queries and keys are
+    normalised head by head (q_gain, k_gain: fp32 [head_dim]; None: not) and turned (rope: fp32 [positions, head_dim / 2, 2],
+    cosine and sine; position: int32 [rows], None: the slot).  Queries go to q_out (q itself: in place; q and q_out None: keys and
+    values only), row i of prompt b to slot ctx_len[b] + i - row_start[b] of k_pool, v_pool [slots, kv_heads, head_dim], or of
+    pages [pages, kv_heads, 2, 16, head_dim] (float8_e4m3fn) with scales fp32 [pages, kv_heads, 2].  Enqueues on `stream`; returns q_out."""
+    _check(_ops().append_rows(q, k, v, q_out, ctx_len, row_start, max_len, k_pool, v_pool, pages, scales, page_table, ctx_start, q_gain,
+                              k_gain, eps, rope, position, stream), "percache_append_rows")
+    return q_out
+
+
+def tree_attention_8bit(q: Any, pages: Any, scales: Any, out: Any, lse: Any = None, *, ctx_len: Any, row_start: Any, page_table: Any,
+                        max_nodes: int, max_len: int, workspace: Any, mask: Any = None, scale: Optional[float] = None,
+                        stream: Optional[int] = None) -> Any:
+    """percache_tree_attention_8bit: tree_attention over the 8-bit pages that append_rows writes.  Enqueues on `stream`, returns `out`."""
+    _check(_ops().tree_attention_8bit(q, pages, scales, out, lse, ctx_len, row_start, max_nodes, max_len, workspace, mask, page_table,
+                                      scale, stream), "percache_tree_attention_8bit")
+    return out
+
+
+def fork_pages(page_table: Any, held: Any, length: Any, parent: Any, table_out: Any, held_out: Any, length_out: Any, refs: Any,
+               free_list: Any, free_count: Any, missing: Any, *, workspace: Any, pools: Sequence[Any] = (), room: int = 0,
+               refs_out: Any = None, free_list_out: Any = None, free_count_out: Any = None, stream: Optional[int] = None) -> None:
+    """percache_fork_pages: child i goes on as sequence parent[i].  Full pages are shared (refs counts the holders), partly filled ones
+    copied in every pool [layers, pages, ...] for all children but the first, pages for `room` more slots taken from the end of the free
+    list, and what nobody holds any more given back.  refs_out, free_list_out, free_count_out None: in place.  missing[0]: pages that the
+    list could not give.  Enqueues on `stream`."""
+    _check(_ops().fork_pages(page_table, held, length, parent, table_out, held_out, length_out, refs, free_list, free_count, missing, pools,
+                             room, refs if refs_out is None else refs_out, free_list if free_list_out is None else free_list_out,
+                             free_count if free_count_out is None else free_count_out, workspace, stream), "percache_fork_pages")
 
 
 def ops_status(workspace: Any, stream: Optional[int] = None) -> None:
