@@ -1,19 +1,19 @@
 // Tree attention over 8-bit pages: both products transposed, formed by the tensor cores on the 8-bit values as they are stored.
 //
 // With s_K, s_V a page's scales, x = scale * s_K (q . k8), and out = sum 2^x' s_V v8 / sum 2^x' (x' in base 2, less a reference).  A block's 128 slots are
-// the MMAs' M side: S^T = K Q^T has a TMEM lane, i.e. a thread, per slot and a column per row (query head of a node), so a page's
+// the MMAs' M side: S^T = K Q^T has a TMEM lane, i.e. a thread, per slot and columns per row (query head of a node), so a page's
 // scales are a thread's own numbers; O^T = V^T P^T has a lane per element of the head.  An 8-bit MMA wants both operands in 8 bits, so q and
-// the weights P = 2^x' s_V are split into sums of e4m3 numbers, each some powers of two below the one before, which get columns of their own: a
-// product of 16 rows still is one of 32 to 64 columns, which costs less than reading K and V from shared memory as the A operand does.  Nothing
-// is unpacked: shared memory sees every byte of the cache twice (copy in, MMA), where forming 16-bit tiles would take seven times.
+// the weights P = 2^x' s_V are split into sums of e4m3 numbers, each some powers of two below the one before, with columns of their own.
+// Nothing is unpacked: shared memory sees every byte of the cache twice (copy in, MMA), where forming 16-bit tiles would take seven times.
 //   q: 2 parts (bf16, exact: 8 bits of mantissa are 4 + 4) or 3 (fp16), 2^4 apart, of q * 2^-e with the row's largest in (224, 448].
-//   P: 2 parts 2^4 apart and one 2^18 below (bf16), 3 parts and one 2^22 below (fp16).  The largest weight of a row lies in 2^4 .. 2^8.  The last
-//   part only matters for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
+//   P: 2 parts 2^4 apart and one 2^18 below (bf16), 3 parts and one 2^22 below (fp16), of the weight as a half: the largest of a row lies in
+//   2^11 .. 2^15.  The last part is for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
 // The accumulation is fp32's (measured: off by at most 2^-21 of the sum of magnitudes).
 //
 // Bound by HBM: 2 D bytes a slot and KV head.  One copy per page fetches keys and values of a head: a box of [row group][K, V][8 rows][D
 // bytes], so that the row groups of K, and those of V, are one stride apart over all pages of a block.
-// Roles as in attn_narrow.cu: warps 0-7 softmax (even and odd blocks), 8 copies, 9 issues MMAs, 10-11 split Q, fetch masks and clean V.
+// Warps 0-7: softmax (even and odd blocks), 8: copies, 9: S products, 10: O products, 11: splits Q, fetches masks, cleans V.  With one warp for
+// both products its waits and issues, one behind the other, took 1800 clocks a block (64 x 2500 slots 76 us); a block's bytes take 1490.
 #include <algorithm>
 
 #include "tree_common.cuh"
@@ -25,10 +25,13 @@ constexpr int RING_BYTES = 128 * 1024;
 constexpr int CLEAN_BARS = 8;                   // more than the tiles between a product with K and the one with V
 constexpr int FLAGS = 8;                        // items a `bad V` flag lives for: more than the roles can be apart
 constexpr int MASK_WORDS = 4;                   // 256 nodes
-constexpr float HEADROOM = 4.f, RESCALE_THRESHOLD = 4.f;       // the largest weight of a row: 2^4 .. 2^8, below 448
+// The running reference lies HEADROOM (base 2) below the largest score that set it and is raised when a score exceeds that by RESCALE_THRESHOLD.
+constexpr float HEADROOM = 11.f, RESCALE_THRESHOLD = 4.f;
+constexpr int P_UNIT = 7;                       // the first part of P counts 2^7: at most 2^8, below 448
 constexpr int MIN_SPAN = 2;
 constexpr int WHOLE_BLOCKS = 6;
 constexpr int PAGES = BLK / PAGE_TOKENS;
+constexpr int AHEAD = 32 / PAGES;               // blocks whose pages are asked for together
 
 struct MergeRecord8 {            // written by the CTA that has a cut unit's first part
   int32_t n_parts;               // 0: none
@@ -55,15 +58,52 @@ struct Tree8Params {
 
 template <int NC, bool BF16> struct Parts {
   static constexpr int Q = BF16 ? 2 : 3, P = BF16 ? 3 : 4;
-  static constexpr int NS = NC * Q, NO = NC * P;               // columns of S and O
+  // Columns: of S, row c's parts are c * Q + part; of O, rows c and c + 1 (c even) have c * P + 2 * part and the one behind it
+  static constexpr int NS = NC * Q, NO = NC * P;
+  static constexpr int P_ROW = NO <= 64 ? 64 : 128;            // bytes of a slot's row of P in shared memory
   // O of (item parity, block parity); one item's at a time where tensor memory does not hold two
   static constexpr int O_ITEMS = 2 * NS + 4 * NO <= 512 ? 2 : 1;
   static constexpr int USED = 2 * NS + 2 * O_ITEMS * NO;
   static constexpr int TMEM = USED <= 256 ? 256 : 512;
-  static_assert(USED <= 512 && NS % 16 == 0 && NO % 16 == 0, "");
-  __device__ static constexpr int shift(int part) { return BF16 ? (part == 0 ? 0 : part == 1 ? 4 : 18) : (part < 3 ? 4 * part : 22); }
+  static_assert(USED <= 512 && NS % 16 == 0 && NO % 16 == 0 && NO <= P_ROW, "");
+  __host__ __device__ static constexpr int shift(int part) { return BF16 ? (part == 0 ? 0 : part == 1 ? 4 : 18) : (part < 3 ? 4 * part : 22); }
 };
-__device__ __forceinline__ constexpr float pow2(int e) { return e >= 0 ? static_cast<float>(1u << e) : 1.0f / static_cast<float>(1u << -e); }
+__host__ __device__ constexpr float pow2(int e) { return e >= 0 ? static_cast<float>(1u << e) : 1.0f / static_cast<float>(1u << -e); }
+
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t e4m3x2_of(__half2 x) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&x)));
+  return r;
+}
+__device__ __forceinline__ __half2 half2_of(uint32_t e4m3x2) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(e4m3x2)));
+  return as_half2(h);
+}
+// The parts of two weights (at most 2^15), 16 bits each.  What is left after a part is exact in a half: a multiple of its last bit.
+template <typename X>
+__device__ __forceinline__ void split_weights(float w0, float w1, uint32_t (&out)[X::P]) {
+  __half2 r = __floats2half2_rn(w0, w1);
+#pragma unroll
+  for (int part = 0; part < X::P; ++part) {
+    const int e = X::shift(part) - P_UNIT;
+    out[part] = e4m3x2_of(__hmul2(r, __float2half2_rn(pow2(e))));
+    if (part + 1 < X::P) r = __hfma2(half2_of(out[part]), __float2half2_rn(-pow2(-e)), r);
+  }
+}
+
+// N consecutive columns of the warp's 32 lanes, N a multiple of 4.
+template <int N>
+__device__ __forceinline__ void tmem_columns(uint32_t at, uint32_t* x) {
+  if constexpr (N >= 16) {
+    tmem_ld_32x16(at, *reinterpret_cast<uint32_t(*)[16]>(x));
+    if constexpr (N > 16) tmem_columns<N - 16>(at + 16, x + 16);
+  } else {
+    tmem_ld_32x4(at, *reinterpret_cast<uint32_t(*)[4]>(x));
+    if constexpr (N > 4) tmem_columns<N - 4>(at + 4, x + 4);
+  }
+}
 
 template <int NC>
 __device__ __forceinline__ Shape shape8(const Tree8Params& a, const SeqPart& p) {
@@ -157,7 +197,7 @@ __device__ __forceinline__ int swizzled(int n, int b) {
 }
 
 template <int D, int NC, bool BF16>
-constexpr int smem8() { return 1024 + RING_BYTES + 2 * Parts<NC, BF16>::NS * D + 2 * Parts<NC, BF16>::NO * BLK; }
+constexpr int smem8() { return 1024 + RING_BYTES + 2 * Parts<NC, BF16>::NS * D + 2 * Parts<NC, BF16>::P_ROW * BLK; }
 
 template <int D, int NC, bool BF16>
 __global__ void __launch_bounds__(TREE_THREADS, 1)
@@ -167,17 +207,19 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
   constexpr int SBO = 2 * GROUP_BYTES;                         // K and V take turns
   constexpr int STAGE_BYTES = BLK * 2 * D;
   constexpr int STAGES = RING_BYTES / STAGE_BYTES;
-  constexpr int Q_BYTES = X::NS * D, P_BYTES = X::NO * BLK;
+  constexpr int Q_BYTES = X::NS * D, P_BYTES = X::P_ROW * BLK;
   constexpr uint32_t TMEM_O = 2 * X::NS;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], landed[STAGES], empty[STAGES], dirty[CLEAN_BARS], cleaned[CLEAN_BARS], s_full[2], p_full[2], o_full[2], o_free[2], ml_full;
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], landed[STAGES], empty[STAGES], dirty[CLEAN_BARS], cleaned[CLEAN_BARS], s_full[2], s_free[2], p_full[2], p_free[2],
+      o_full[2], o_free[2], ml_full;
   __shared__ __align__(16) float4 page_scale[STAGES][PAGES];   // s_K, log2 s_V, 1 / s_V
   __shared__ __align__(16) float q_scale[2][NC];
   __shared__ __align__(16) float block_max[2][2][NC][4];       // [block parity][use][row][warp]
   __shared__ __align__(16) float fin_l[2][2][NC][4];           // [item parity][block parity][row][warp]: a warp's share of the sum
   __shared__ float fin_m[2][2][NC];
+  __shared__ __align__(16) float neg_ref[8][NC];                // - reference, a copy per softmax warp
   __shared__ uint64_t node_mask[2 * NC * MASK_WORDS];
-  __shared__ int bad_flag[FLAGS][2];
+  __shared__ int bad_flag[FLAGS];
   __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
   __shared__ uint32_t tmem_slot;
@@ -191,11 +233,11 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
   if (threadIdx.x == 0) {
     cta_failed = 0;
     for (int i = 0; i < STAGES; ++i) { mbar_init(&landed[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < CLEAN_BARS; ++i) { mbar_init(&dirty[i], 1); mbar_init(&cleaned[i], 2); }
+    for (int i = 0; i < CLEAN_BARS; ++i) { mbar_init(&dirty[i], 1); mbar_init(&cleaned[i], 1); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 2);          // the two warps that split it
+      mbar_init(&q_full[i], 1);
       mbar_init(&q_empty[i], 9);         // the MMAs and the eight softmax warps
-      mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4);
+      mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 4); mbar_init(&p_full[i], 4); mbar_init(&p_free[i], 1);
       mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 8);
     }
     mbar_init(&ml_full, 8);
@@ -224,41 +266,47 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     while (ok && next_item<NC>(cur, a, &it)) {
       const int last_page = (it.ctx_len + it.n_nodes - 1) / PAGE_TOKENS;
       const int32_t* table = a.kv.page_table + static_cast<size_t>(it.seq) * a.kv.pt_stride;
-      // Lanes 0-7: page ids (asked for two blocks ahead) and scales (one block ahead).  Pages behind the prompt's last slot repeat its last
-      // page (masked either way); ids outside the pool become one that copies zeros.
+      // A lane has a page: its id and scales, of four blocks at a time, asked for four blocks ahead (what is moved from one register to the
+      // next has to have arrived: with a block at a time the warp spent its time on that, 64 x 2500 slots 79 us).
+      // Pages behind the prompt's last slot repeat its last page (masked either way); ids outside the pool become one that copies zeros.
       auto page_at = [&](int blk) {
-        const int page = ld_dep_s32(table + min(blk * PAGES + (lane & (PAGES - 1)), last_page));
+        const int page = ld_dep_s32(table + min(blk * PAGES + lane, last_page));
         return static_cast<int>(min(static_cast<uint32_t>(page), static_cast<uint32_t>(a.kv.n_pages)));
       };
       auto scale_at = [&](int page) {
         return page < a.kv.n_pages ? ld_dep_f32x2(a.kv.scales + (static_cast<size_t>(page) * a.kv.n_kv_heads + it.g) * 2) : make_float2(1.f, 1.f);
       };
-      int page0 = page_at(it.blk_begin), page1 = page_at(min(it.blk_begin + 1, it.blk_end - 1));
-      float2 sc0 = scale_at(page0);
+      int page = page_at(it.blk_begin);
+      float2 sc = scale_at(page);
 #pragma unroll 1
-      for (int blk = it.blk_begin; blk < it.blk_end; ++blk) {
-        const int page2 = page_at(min(blk + 2, it.blk_end - 1));
-        ok = __all_sync(0xffffffffu, bar_wait(&empty[st], phase ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
-        if (!ok) break;
-        int page[PAGES];
+      for (int blk0 = it.blk_begin; blk0 < it.blk_end && ok; blk0 += AHEAD) {
+        const int next_page = page_at(blk0 + AHEAD);
+        float2 next_sc = sc;
+        const int n = min(AHEAD, it.blk_end - blk0);
+#pragma unroll 1
+        for (int u = 0; u < n; ++u) {
+          ok = __all_sync(0xffffffffu, bar_wait(&empty[st], phase ^ 1u, a.err_word, DEV_ERR_ATTN_PRODUCER));
+          if (!ok) break;
+          int id[PAGES];
 #pragma unroll
-        for (int p = 0; p < PAGES; ++p) page[p] = __shfl_sync(0xffffffffu, page0, p);
-        if (elect_one()) {
+          for (int p = 0; p < PAGES; ++p) id[p] = __shfl_sync(0xffffffffu, page, u * PAGES + p);
+          if (elect_one()) {
 #pragma unroll
-          for (int p = 0; p < PAGES; ++p)
-            tma_load_5d(ring + st * STAGE_BYTES + p * (PAGE_TOKENS * 2 * D), &tm, &landed[st], 0, 0, 0, 0, page[p] * a.heads_a_page + it.g);
+            for (int p = 0; p < PAGES; ++p)
+              tma_load_5d(ring + st * STAGE_BYTES + p * (PAGE_TOKENS * 2 * D), &tm, &landed[st], 0, 0, 0, 0, id[p] * a.heads_a_page + it.g);
+          }
+          __syncwarp();
+          if (lane / PAGES == u) {
+            const float v = fminf(fmaxf(sc.y, 0x1p-32f), 0x1p32f);
+            page_scale[st][lane % PAGES] = make_float4(fminf(fmaxf(sc.x, 0x1p-32f), 0x1p32f), __log2f(v), 1.0f / v, 0.f);
+          }
+          __syncwarp();
+          if (elect_one()) mbar_arrive_expect_tx(&landed[st], STAGE_BYTES);     // the scales are out, too
+          __syncwarp();
+          if (u == 1) next_sc = scale_at(next_page);
+          if (++st == STAGES) { st = 0; phase ^= 1u; }
         }
-        __syncwarp();
-        const float2 sc1 = scale_at(page1);
-        if (lane < PAGES) {
-          const float v = fminf(fmaxf(sc0.y, 0x1p-32f), 0x1p32f);
-          page_scale[st][lane] = make_float4(fminf(fmaxf(sc0.x, 0x1p-32f), 0x1p32f), __log2f(v), 1.0f / v, 0.f);
-        }
-        __syncwarp();
-        if (elect_one()) mbar_arrive_expect_tx(&landed[st], STAGE_BYTES);       // the scales are out, too
-        __syncwarp();
-        sc0 = sc1; page0 = page1; page1 = page2;
-        if (++st == STAGES) { st = 0; phase ^= 1u; }
+        sc = next_sc; page = next_page;
       }
       if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
         rec.n_parts = static_cast<int>(static_cast<uint64_t>((span.begin + it.unit_end) * span.n_ctas - 1) / static_cast<uint64_t>(span.total)) -
@@ -268,22 +316,21 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     }
     if (!ok) cta_failed = 1;
     if (lane == 0) a.merges[blockIdx.x] = rec;
-  } else if (warp >= 10) {
+  } else if (warp == 11) {
     // ------------------------------------------------------------ Q into parts, masks, V without what does not count
     constexpr int LANES = D / 16;                                  // a thread has 16 elements of a row
-    const int tid = threadIdx.x - 320;
     uint32_t n_item = 0, n_tile = 0, n_clean = 0;
     bool ok = true;
     while (ok && next_item<NC>(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin, qs = n_item & 1;
-      int* flag = &bad_flag[n_item % FLAGS][warp - 10];            // read at the end of the item that set it, long before its next use
+      int* flag = &bad_flag[n_item % FLAGS];                       // read at the end of the item that set it, long before its next use
       if (lane == 0) *flag = 0;
       ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_item >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
       if (!ok) break;
       const int node0 = it.flat0 / a.group;
 #pragma unroll 1
-      for (int c0 = 0; c0 < it.n_rows; c0 += 64 / LANES) {
-        const int c = c0 + tid / LANES, l = tid % LANES;
+      for (int c0 = 0; c0 < it.n_rows; c0 += 32 / LANES) {
+        const int c = c0 + lane / LANES, l = lane % LANES;
         uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
         if (c < it.n_rows) {
           const int flat = it.flat0 + c, node = flat / a.group;
@@ -322,14 +369,14 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
               x[e] = (x[e] - y.x) * 16.f; x[e + 1] = (x[e + 1] - y.y) * 16.f;
               x[e + 2] = (x[e + 2] - z.x) * 16.f; x[e + 3] = (x[e + 3] - z.y) * 16.f;
             }
-            *reinterpret_cast<uint4*>(q_smem + qs * Q_BYTES + swizzled<D>(part * NC + c, l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
+            *reinterpret_cast<uint4*>(q_smem + qs * Q_BYTES + swizzled<D>(c * X::Q + part, l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
           }
         }
       }
       if (it.blk_end * BLK > it.ctx_len) {
         const int nodes = (it.flat0 + it.n_rows - 1) / a.group - node0 + 1, words = (it.n_nodes + 63) / 64;
 #pragma unroll 1
-        for (int e = tid; e < nodes * words; e += 64)
+        for (int e = lane; e < nodes * words; e += 32)
           node_mask[(qs * NC + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + node0 + e / words, node0 + e / words, e % words);
       }
       fence_proxy_async_smem();                            // the MMA reads Q through the async proxy
@@ -345,10 +392,10 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         uint8_t* v = ring + (t % STAGES) * STAGE_BYTES + GROUP_BYTES;
         const int r0 = max(it.ctx_len - blk * BLK, 0), r_end = it.ctx_len + it.n_nodes - blk * BLK;
         bool bad = false;
-        // a thread takes a 16-byte vector (as stored; the swizzle only permutes vectors of the same rows' group) of rows 64 / LANES apart
+        // a lane takes a 16-byte vector (as stored; the swizzle only permutes a row group's vectors) of rows 32 / LANES apart
 #pragma unroll 1
-        for (int r = r0 + tid / LANES; r < BLK; r += 64 / LANES) {
-          uint4* p = reinterpret_cast<uint4*>(v + (r >> 3) * SBO + swizzled<D>(r & 7, (tid % LANES) * 16));
+        for (int r = r0 + lane / LANES; r < BLK; r += 32 / LANES) {
+          uint4* p = reinterpret_cast<uint4*>(v + (r >> 3) * SBO + swizzled<D>(r & 7, (lane % LANES) * 16));
           if (r >= r_end) {
             *p = make_uint4(0, 0, 0, 0);
           } else {
@@ -373,63 +420,69 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       ++n_item;
     }
     if (!ok) cta_failed = 1;
-  } else if (warp == 9) {
-    // ------------------------------------------------------------ MMA issuer: the whole warp walks, one lane issues
-    constexpr uint32_t idesc_s = make_idesc_e4m3(BLK, X::NS, 0, 0);
-    constexpr uint32_t idesc_o = make_idesc_e4m3(BLK, X::NO, 1, 0);         // A = V^T: V's rows are the K index
+  } else if (warp == 9 || warp == 10) {
+    // ------------------------------------------------------------ MMAs: the whole warp walks, one lane issues
     auto desc = [](uint32_t addr, uint32_t sbo) { return D == 128 ? make_smem_desc_sw128(addr, 0, sbo) : make_smem_desc_sw64(addr, 0, sbo); };
-    uint32_t n_item = 0, n_tile = 0, n_dirty = 0, n_clean = 0, p_phase = 0;    // p_phase: bit i, the parity to wait for on p_full[i]
+    uint32_t n_item = 0, n_tile = 0, n_dirty = 0, phases = 0;     // phases: bit i, the parity to wait for on the barrier of block parity i
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, a.err_word, DEV_ERR_ATTN_MMA));
     };
     while (ok && next_item<NC>(cur, a, &it)) {
-      const int nb = it.blk_end - it.blk_begin, par = n_item & 1, ob = X::O_ITEMS == 2 ? par : 0;
-      const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
-      const uint64_t q_desc = desc(smem_u32(q_smem + par * Q_BYTES), GROUP_BYTES);
-      wait(&q_full[par], (n_item >> 1) & 1u);
+      const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
+      if (warp == 9) {
+        const uint32_t idesc = make_idesc_e4m3(BLK, (it.n_rows * X::Q + 15) & ~15, 0, 0);
+        const uint64_t q_desc = desc(smem_u32(q_smem + par * Q_BYTES), GROUP_BYTES);
+        wait(&q_full[par], (n_item >> 1) & 1u);
 #pragma unroll 1
-      for (int j = -2; j < nb && ok; ++j) {                // S0 S1 O0 S2 O1 ...
-        const int i = j & 1;
-        if (j >= 0) {
+        for (int j = 0; j < nb && ok; ++j) {
           const uint32_t t = n_tile + j;
-          wait(&p_full[i], (p_phase >> i) & 1u);
-          p_phase ^= 1u << i;
-          if (j == 0) wait(&o_free[ob], (o_uses & 1u) ^ 1u);
+          const int i = j & 1;
+          wait(&s_free[i], ((phases >> i) & 1u) ^ 1u);
+          phases ^= 1u << i;
+          wait(&landed[t % STAGES], (t / STAGES) & 1u);
+          if (!ok) break;
+          tc_fence_after_sync();
+          if (elect_one()) {
+            const uint64_t k_desc = desc(smem_u32(ring + (t % STAGES) * STAGE_BYTES), SBO);
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+              umma_ss_8bit(tmem + i * X::NS, k_desc + (kk * 32 >> 4), q_desc + (kk * 32 >> 4), idesc, kk != 0);
+            umma_commit(&s_full[i]);
+            if (j + 1 == nb) umma_commit(&q_empty[par]);
+            if ((it.blk_begin + j + 1) * BLK > it.ctx_len) mbar_arrive(&dirty[n_dirty % CLEAN_BARS]);
+          }
+          __syncwarp();
+          if ((it.blk_begin + j + 1) * BLK > it.ctx_len) ++n_dirty;
+        }
+      } else {
+        const int ob = X::O_ITEMS == 2 ? par : 0;
+        const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
+        const uint32_t idesc = make_idesc_e4m3(BLK, (((it.n_rows + 1) & ~1) * X::P + 15) & ~15, 1, 1);     // A = V^T, B = P^T: the K index is the slot
+        wait(&o_free[ob], (o_uses & 1u) ^ 1u);
+#pragma unroll 1
+        for (int j = 0; j < nb && ok; ++j) {
+          const uint32_t t = n_tile + j;
+          const int i = j & 1;
+          wait(&p_full[i], (phases >> i) & 1u);
+          phases ^= 1u << i;
           if ((it.blk_begin + j + 1) * BLK > it.ctx_len) {
-            wait(&cleaned[n_clean % CLEAN_BARS], (n_clean / CLEAN_BARS) & 1u);
-            ++n_clean;
+            wait(&cleaned[n_dirty % CLEAN_BARS], (n_dirty / CLEAN_BARS) & 1u);
+            ++n_dirty;
           }
           if (!ok) break;
           tc_fence_after_sync();
           if (elect_one()) {
             // head size 64 has 64 elements of M in a row: the second 64 TMEM lanes repeat the first (distance 0) and are not read
             const uint64_t v_desc = desc(smem_u32(ring + (t % STAGES) * STAGE_BYTES + GROUP_BYTES), SBO);
-            const uint64_t p_desc = make_smem_desc_sw128(smem_u32(p_smem + i * P_BYTES), 16, 1024);
+            const uint32_t p_at = smem_u32(p_smem + i * P_BYTES);
+            const uint64_t p_desc = X::P_ROW == 128 ? make_smem_desc_sw128(p_at, 0, 1024) : make_smem_desc_sw64(p_at, 0, 512);
 #pragma unroll
             for (int kk = 0; kk < BLK / 32; ++kk)
-              umma_ss_8bit(tmem + TMEM_O + (ob * 2 + i) * X::NO, v_desc + (kk * 4 * SBO >> 4), p_desc + (kk * 32 >> 4), idesc_o, j > 1 || kk != 0);
+              umma_ss_8bit(tmem + TMEM_O + (ob * 2 + i) * X::NO, v_desc + (kk * 4 * SBO >> 4), p_desc + (kk * 32 * X::P_ROW >> 4), idesc, j > 1 || kk != 0);
             umma_commit(&empty[t % STAGES]);
+            umma_commit(&p_free[i]);
             if (j + 1 == nb) umma_commit(&o_full[ob]);
-          }
-          __syncwarp();
-        }
-        if (j + 2 < nb) {
-          const uint32_t t = n_tile + j + 2;
-          wait(&landed[t % STAGES], (t / STAGES) & 1u);
-          if (!ok) break;
-          if ((it.blk_begin + j + 3) * BLK > it.ctx_len) {
-            if (elect_one()) mbar_arrive(&dirty[n_dirty % CLEAN_BARS]);
-            ++n_dirty;
-          }
-          tc_fence_after_sync();
-          if (elect_one()) {
-            const uint64_t k_desc = desc(smem_u32(ring + (t % STAGES) * STAGE_BYTES), SBO);
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-              umma_ss_8bit(tmem + i * X::NS, k_desc + (kk * 32 >> 4), q_desc + (kk * 32 >> 4), idesc_s, kk != 0);
-            umma_commit(&s_full[i]);
-            if (j + 3 == nb) umma_commit(&q_empty[par]);
           }
           __syncwarp();
         }
@@ -444,34 +497,65 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     const int i = warp >> 2, quarter = warp & 3;
     const int r = quarter * 32 + lane;                     // slot of the block; element of the head
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-    uint8_t* p_row = p_smem + i * P_BYTES + (r & 15);
-    const int p_vec = r >> 4;
+    uint8_t* p_row = p_smem + i * P_BYTES;
     uint32_t n_item = 0, n_tile = 0, n_s = 0, n_raise = 0;
     bool ok = true;
     while (next_item<NC>(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin, par = n_item & 1, ob = X::O_ITEMS == 2 ? par : 0;
       const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
-      float neg[NC], l[NC];                                // -reference (the same in all threads); sum over this thread's slots only
+      float l[NC];                                         // sum over this thread's slots only
+      float* neg = neg_ref[warp];                          // - reference: the same in all threads
       uint32_t unset = 0xffffffffu >> (32 - it.n_rows);    // rows that have seen nothing yet: reference 0, sum and O zero
 #pragma unroll
-      for (int c = 0; c < NC; ++c) { neg[c] = 0.f; l[c] = 0.f; }
+      for (int c = 0; c < NC; ++c) l[c] = 0.f;
+      if (lane < NC) neg[lane] = 0.f;
+      __syncwarp();
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&q_full[par], (n_item >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // scales, masks
       for (int j = i; j < nb; j += 2) {
         const uint32_t t = n_tile + j;
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&landed[t % STAGES], (t / STAGES) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
-        ++n_s;
         float s[NC];                                       // scores in base 2, the page's log2 s_V added
         float inv_v = 0.f;
         bool raise = j == i;                               // does any row's block maximum pass what its reference allows
         if (ok) {
+          tc_fence_after_sync();
           const float4 sc = page_scale[t % STAGES][r / PAGE_TOKENS];
           inv_v = sc.z;
-          uint32_t seen = 0xffffffffu;
+#pragma unroll
+          for (int c0 = 0; c0 < NC; c0 += 16) {            // 16 rows at a time, their columns asked for together
+            uint32_t x[16 * X::Q];
+#pragma unroll
+            for (int c = 0; c < 16; c += 4)
+              if (c0 + c < it.n_rows) tmem_columns<4 * X::Q>(lanes + i * X::NS + (c0 + c) * X::Q, x + c * X::Q);
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 16; c += 4) {
+              if (c0 + c < it.n_rows) {
+                const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0 + c]);
+                const float qf[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  float y = __uint_as_float(x[(c + e) * X::Q + X::Q - 1]);
+#pragma unroll
+                  for (int part = X::Q - 2; part >= 0; --part) y = fmaf(y, 0.0625f, __uint_as_float(x[(c + e) * X::Q + part]));
+                  // columns behind the last row hold anything
+                  s[c0 + c + e] = c0 + c + e < it.n_rows ? fmaf(y, sc.x * qf[e], sc.y) : -INFINITY;
+                }
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[c0 + c + e] = -INFINITY;
+              }
+            }
+          }
+          tc_fence_before_sync();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(&s_free[i]);
+          __syncwarp();
           const int slot = (it.blk_begin + j) * BLK + r;
           if (slot >= it.ctx_len) {
             const int node = slot - it.ctx_len;
-            seen = 0;
+            uint32_t seen = 0;
             if (node < it.n_nodes) {
               const uint64_t* w = node_mask + par * NC * MASK_WORDS + (node >> 6);
               int at = 0, h = it.flat0 % a.group;
@@ -481,36 +565,23 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
                 if (++h == a.group) { h = 0; at += MASK_WORDS; }
               }
             }
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+              if (!((seen >> c) & 1u)) s[c] = -INFINITY;
           }
           __syncwarp();
-          tc_fence_after_sync();
+          if (j != i) {                                    // (the first block always sets the references)
 #pragma unroll
-          for (int c0 = 0; c0 < NC; c0 += 4) {
-            if (c0 >= it.n_rows) {
-#pragma unroll
-              for (int c = c0; c < c0 + 4; ++c) s[c] = -INFINITY;
-              continue;
+            for (int c0 = 0; c0 < NC; c0 += 4) {
+              if (c0 >= it.n_rows) break;
+              const float4 n4 = *reinterpret_cast<const float4*>(neg + c0);
+              raise |= s[c0] + n4.x > HEADROOM + RESCALE_THRESHOLD || s[c0 + 1] + n4.y > HEADROOM + RESCALE_THRESHOLD ||
+                       s[c0 + 2] + n4.z > HEADROOM + RESCALE_THRESHOLD || s[c0 + 3] + n4.w > HEADROOM + RESCALE_THRESHOLD;
             }
-            uint32_t x[X::Q][4];
+            if (unset != 0) {
 #pragma unroll
-            for (int part = 0; part < X::Q; ++part) tmem_ld_32x4(lanes + i * X::NS + part * NC + c0, x[part]);
-            tmem_wait_ld();
-            const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0]);
-            const float qf[4] = {q4.x, q4.y, q4.z, q4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float y = __uint_as_float(x[X::Q - 1][e]);
-#pragma unroll
-              for (int part = X::Q - 2; part >= 0; --part) y = fmaf(y, 0.0625f, __uint_as_float(x[part][e]));
-              const int c = c0 + e;
-              // columns behind the last row hold anything
-              s[c] = c < it.n_rows && ((seen >> c) & 1u) ? fmaf(y, sc.x * qf[e], sc.y) : -INFINITY;
-              raise |= s[c] + neg[c] > HEADROOM + RESCALE_THRESHOLD;
+              for (int c = 0; c < NC; ++c) raise |= ((unset >> c) & 1u) && s[c] > -INFINITY;
             }
-          }
-          if (unset != 0) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) raise |= ((unset >> c) & 1u) && s[c] > -INFINITY;
           }
         }
         if (j != i) raise = parity_any(i, raise);
@@ -524,58 +595,68 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           parity_any(i, false);
           const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
           const float now = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) - HEADROOM;             // the block's own reference
-          float old = 0.f;
-#pragma unroll
-          for (int c = 0; c < NC; ++c) old = lane == c ? neg[c] : old;
+          const float old = lane < NC ? neg[lane] : 0.f;
           const bool fresh = (unset >> lane) & 1u;
           const bool up = lane < NC && now > -INFINITY && (fresh || now + old > RESCALE_THRESHOLD);
           const float alpha = !up ? 1.f : fresh ? 0.f : fast_exp2(-old - now);
-          const float next = up ? -now : old;
+          if (up) neg[lane] = -now;
           unset &= ~(__ballot_sync(0xffffffffu, up));
-#pragma unroll
-          for (int c = 0; c < NC; ++c) neg[c] = __shfl_sync(0xffffffffu, next, c);
-          if (j != i && ok) {                              // s_full came behind this parity's last product: O is complete
+          __syncwarp();
+          if (j != i) {
+            if (ok) ok = __all_sync(0xffffffffu, bar_wait(&p_free[i], (n_s & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));    // O is complete
+            if (ok) {
+              tc_fence_after_sync();
 #pragma unroll 1
-            for (int c0 = 0; c0 < NC; c0 += 4) {
-              if (c0 >= it.n_rows) break;
-              float f[4];
+              for (int c0 = 0; c0 < NC; c0 += 4) {
+                if (c0 >= it.n_rows) break;
+                const uint32_t t_o = lanes + TMEM_O + (ob * 2 + i) * X::NO + c0 * X::P;
+                float f[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) f[e] = __shfl_sync(0xffffffffu, alpha, c0 + e);
-#pragma unroll
-              for (int part = 0; part < X::P; ++part) {
-                const uint32_t t_o = lanes + TMEM_O + (ob * 2 + i) * X::NO + part * NC + c0;
-                uint32_t o[4];
-                tmem_ld_32x4(t_o, o);
+                for (int e = 0; e < 4; ++e) f[e] = __shfl_sync(0xffffffffu, alpha, c0 + e);
+                uint32_t o[4 * X::P];
+                tmem_columns<4 * X::P>(t_o, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[e]);
-                tmem_st_32x4(t_o, o);
-              }
-            }
-            tmem_wait_st();
+                for (int e = 0; e < 4 * X::P; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[e / (2 * X::P) * 2 + (e & 1)]);
 #pragma unroll
-            for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, alpha, c);
+                for (int e = 0; e < 4 * X::P; e += 4) tmem_st_32x4(t_o + e, *reinterpret_cast<uint32_t(*)[4]>(o + e));
+              }
+              tmem_wait_st();
+#pragma unroll
+              for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, alpha, c);
+            }
           }
         }
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&p_free[i], (n_s & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // the product before has read P
+        ++n_s;
         if (ok) {
 #pragma unroll
-          for (int c0 = 0; c0 < NC; c0 += 2) {
-            if (c0 >= it.n_rows) break;
-            float w0 = fast_exp2(s[c0] + neg[c0]), w1 = fast_exp2(s[c0 + 1] + neg[c0 + 1]);
-            l[c0] = fmaf(w0, inv_v, l[c0]);                // the row sum has the weights without s_V, and before they are split
-            l[c0 + 1] = fmaf(w1, inv_v, l[c0 + 1]);
+          for (int c16 = 0; c16 < NC; c16 += 16) {
+            if (c16 >= it.n_rows) break;
+            uint32_t w[4 * X::P];                          // the slot's row of P: two rows' parts a half word
 #pragma unroll
-            for (int part = 0; part < X::P; ++part) {
-              const float up = pow2(X::shift(part)), down = pow2(-X::shift(part));
-              const uint32_t two = pack_e4m3x2(w0 * up, w1 * up);
-              if (part + 1 < X::P) {
-                const float2 y = unpack_e4m3x2(two);
-                w0 = fmaf(y.x, -down, w0);
-                w1 = fmaf(y.y, -down, w1);
+            for (int c = 0; c < 16; c += 4) {
+              if (c16 + c >= it.n_rows) break;
+              const float4 n4 = *reinterpret_cast<const float4*>(neg + c16 + c);
+              uint32_t two[2][X::P];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const int c0 = c16 + c + 2 * u;
+                const float w0 = fast_exp2(s[c0] + (u ? n4.z : n4.x)), w1 = fast_exp2(s[c0 + 1] + (u ? n4.w : n4.y));
+                l[c0] = fmaf(w0, inv_v, l[c0]);            // the row sum has the weights without s_V, and before they are split
+                l[c0 + 1] = fmaf(w1, inv_v, l[c0 + 1]);
+                split_weights<X>(w0, w1, two[u]);
               }
-              const int n = part * NC + c0;
-              p_row[n * 128 + ((p_vec ^ (n & 7)) << 4)] = static_cast<uint8_t>(two);
-              p_row[(n + 1) * 128 + ((p_vec ^ ((n + 1) & 7)) << 4)] = static_cast<uint8_t>(two >> 8);
+#pragma unroll
+              for (int e = 0; e < X::P; ++e) {
+                const int lo = 2 * e, hi = 2 * e + 1;
+                w[c * X::P / 4 + e] = two[lo / X::P][lo % X::P] | two[hi / X::P][hi % X::P] << 16;
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < X::P; ++q) {
+              if (c16 * X::P + q * 16 < ((it.n_rows + 1) & ~1) * X::P)
+                *reinterpret_cast<uint4*>(p_row + swizzled<X::P_ROW>(r, c16 * X::P + q * 16)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
             }
           }
           fence_proxy_async_smem();                        // the MMA reads P through the async proxy
@@ -589,12 +670,11 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       if (ok) {
         const float sum = column_reduce<NC>(l, [](float x, float y) { return x + y; });
         if (lane < NC) fin_l[par][i][lane][quarter] = sum;
-        float mine = 0.f;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) mine = lane == c ? -neg[c] : mine;
+        const float mine = lane < NC ? -neg[lane] : 0.f;
         if (quarter == 0 && lane < NC) fin_m[par][i][lane] = ((unset >> lane) & 1u) || nb <= i ? -INFINITY : mine;
         __syncwarp();
         if (elect_one()) { mbar_arrive(&ml_full); mbar_arrive(&q_empty[par]); }
+        __syncwarp();
         ok = __all_sync(0xffffffffu, bar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR));
       }
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&o_full[ob], o_uses & 1u, a.err_word, DEV_ERR_ATTN_CORR));
@@ -602,7 +682,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         tc_fence_after_sync();
         const bool whole = it.blk_begin == 0 && it.blk_end == it.n_blk;
         const size_t part0 = static_cast<size_t>(2 * blockIdx.x + (it.blk_begin == 0 ? 1 : 0)) * BLK;
-        const bool bad = (*reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS][0]) | *reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS][1])) != 0;
+        const bool bad = *reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS]) != 0;
         // Lane c works out row c's two factors; the loop over rows then only scales and stores.
         float f0 = 0.f, f1 = 0.f;
         if (lane < it.n_rows) {
@@ -631,19 +711,17 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
 #pragma unroll 1
         for (int c0 = i * 4; c0 < it.n_rows; c0 += 8) {    // four rows at a time, the parities in turn
           float o0[4] = {0.f, 0.f, 0.f, 0.f}, o1[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t x0[X::P][4], x1[X::P][4];
-#pragma unroll
-          for (int part = 0; part < X::P; ++part) {
-            tmem_ld_32x4(lanes + TMEM_O + ob * 2 * X::NO + part * NC + c0, x0[part]);
-            tmem_ld_32x4(lanes + TMEM_O + (ob * 2 + 1) * X::NO + part * NC + c0, x1[part]);         // not used when there is one block
-          }
+          uint32_t x0[4 * X::P], x1[4 * X::P];
+          tmem_columns<4 * X::P>(lanes + TMEM_O + ob * 2 * X::NO + c0 * X::P, x0);
+          tmem_columns<4 * X::P>(lanes + TMEM_O + (ob * 2 + 1) * X::NO + c0 * X::P, x1);         // not used when there is one block
           tmem_wait_ld();
 #pragma unroll
           for (int part = X::P - 1; part >= 0; --part) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              o0[e] = fmaf(__uint_as_float(x0[part][e]), pow2(-X::shift(part)), o0[e]);
-              o1[e] = fmaf(__uint_as_float(x1[part][e]), pow2(-X::shift(part)), o1[e]);
+              const int at = (e >> 1) * 2 * X::P + part * 2 + (e & 1);
+              o0[e] = fmaf(__uint_as_float(x0[at]), pow2(P_UNIT - X::shift(part)), o0[e]);
+              o1[e] = fmaf(__uint_as_float(x1[at]), pow2(P_UNIT - X::shift(part)), o1[e]);
             }
           }
 #pragma unroll
