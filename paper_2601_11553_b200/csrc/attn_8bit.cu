@@ -15,13 +15,16 @@
 // Warps 0-7: softmax (even and odd blocks), 8: copies, 9: S products, 10: O products, 11: splits Q, fetches masks, cleans V.  With one warp for
 // both products its waits and issues, one behind the other, took 1800 clocks a block (64 x 2500 slots 76 us); a block's bytes take 1490.
 #include <algorithm>
+#include <type_traits>
 
 #include "tree_common.cuh"
 
 namespace pc {
 namespace {
 
-constexpr int RING_BYTES = 128 * 1024;
+// Six tiles of head size 128 (five beside the larger Q and P): an item's end, where nothing is taken from the ring for 7000 clocks, is as long as
+// five tiles take to come in.
+__host__ __device__ constexpr int ring_bytes(int nc) { return (nc == 16 ? 192 : 160) * 1024; }
 constexpr int CLEAN_BARS = 8;                   // more than the tiles between a product with K and the one with V
 constexpr int FLAGS = 8;                        // items a `bad V` flag lives for: more than the roles can be apart
 constexpr int MASK_WORDS = 4;                   // 256 nodes
@@ -56,6 +59,7 @@ struct Tree8Params {
   float *partial_ml, *partial_o;
 };
 
+template <int V> using Const = std::integral_constant<int, V>;
 template <int NC, bool BF16> struct Parts {
   static constexpr int Q = BF16 ? 2 : 3, P = BF16 ? 3 : 4;
   // Columns: of S, row c's parts are c * Q + part; of O, rows c and c + 1 (c even) have c * P + 2 * part and the one behind it
@@ -197,7 +201,7 @@ __device__ __forceinline__ int swizzled(int n, int b) {
 }
 
 template <int D, int NC, bool BF16>
-constexpr int smem8() { return 1024 + RING_BYTES + 2 * Parts<NC, BF16>::NS * D + 2 * Parts<NC, BF16>::P_ROW * BLK; }
+constexpr int smem8() { return 1024 + ring_bytes(NC) + 2 * Parts<NC, BF16>::NS * D + 2 * Parts<NC, BF16>::P_ROW * BLK; }
 
 template <int D, int NC, bool BF16>
 __global__ void __launch_bounds__(TREE_THREADS, 1)
@@ -206,7 +210,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
   constexpr int GROUP_BYTES = 8 * D;                           // eight rows of K or V
   constexpr int SBO = 2 * GROUP_BYTES;                         // K and V take turns
   constexpr int STAGE_BYTES = BLK * 2 * D;
-  constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+  constexpr int STAGES = ring_bytes(NC) / STAGE_BYTES;
   constexpr int Q_BYTES = X::NS * D, P_BYTES = X::P_ROW * BLK;
   constexpr uint32_t TMEM_O = 2 * X::NS;
   extern __shared__ uint8_t smem_raw[];
@@ -227,7 +231,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* q_smem = ring + RING_BYTES;
+  uint8_t* q_smem = ring + ring_bytes(NC);
   uint8_t* p_smem = q_smem + 2 * Q_BYTES;
 
   if (threadIdx.x == 0) {
@@ -266,22 +270,17 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     while (ok && next_item<NC>(cur, a, &it)) {
       const int last_page = (it.ctx_len + it.n_nodes - 1) / PAGE_TOKENS;
       const int32_t* table = a.kv.page_table + static_cast<size_t>(it.seq) * a.kv.pt_stride;
-      // A lane has a page: its id and scales, of four blocks at a time, asked for four blocks ahead (what is moved from one register to the
-      // next has to have arrived: with a block at a time the warp spent its time on that, 64 x 2500 slots 79 us).
+      // A lane has a page, of four blocks at a time: its id, asked for four blocks ahead, and scales.
       // Pages behind the prompt's last slot repeat its last page (masked either way); ids outside the pool become one that copies zeros.
       auto page_at = [&](int blk) {
         const int page = ld_dep_s32(table + min(blk * PAGES + lane, last_page));
         return static_cast<int>(min(static_cast<uint32_t>(page), static_cast<uint32_t>(a.kv.n_pages)));
       };
-      auto scale_at = [&](int page) {
-        return page < a.kv.n_pages ? ld_dep_f32x2(a.kv.scales + (static_cast<size_t>(page) * a.kv.n_kv_heads + it.g) * 2) : make_float2(1.f, 1.f);
-      };
       int page = page_at(it.blk_begin);
-      float2 sc = scale_at(page);
 #pragma unroll 1
       for (int blk0 = it.blk_begin; blk0 < it.blk_end && ok; blk0 += AHEAD) {
         const int next_page = page_at(blk0 + AHEAD);
-        float2 next_sc = sc;
+        float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
         const int n = min(AHEAD, it.blk_end - blk0);
 #pragma unroll 1
         for (int u = 0; u < n; ++u) {
@@ -296,17 +295,19 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
               tma_load_5d(ring + st * STAGE_BYTES + p * (PAGE_TOKENS * 2 * D), &tm, &landed[st], 0, 0, 0, 0, id[p] * a.heads_a_page + it.g);
           }
           __syncwarp();
-          if (lane / PAGES == u) {
-            const float v = fminf(fmaxf(sc.y, 0x1p-32f), 0x1p32f);
-            page_scale[st][lane % PAGES] = make_float4(fminf(fmaxf(sc.x, 0x1p-32f), 0x1p32f), __log2f(v), 1.0f / v, 0.f);
+          if (u == 0) {                                              // while the tile is on its way
+            float2 x = make_float2(1.f, 1.f);
+            if (page < a.kv.n_pages) x = ld_dep_f32x2(a.kv.scales + (static_cast<size_t>(page) * a.kv.n_kv_heads + it.g) * 2);
+            const float v = fminf(fmaxf(x.y, 0x1p-32f), 0x1p32f);
+            sc = make_float4(fminf(fmaxf(x.x, 0x1p-32f), 0x1p32f), __log2f(v), 1.0f / v, 0.f);
           }
+          if (lane / PAGES == u) page_scale[st][lane % PAGES] = sc;
           __syncwarp();
           if (elect_one()) mbar_arrive_expect_tx(&landed[st], STAGE_BYTES);     // the scales are out, too
           __syncwarp();
-          if (u == 1) next_sc = scale_at(next_page);
           if (++st == STAGES) { st = 0; phase ^= 1u; }
         }
-        sc = next_sc; page = next_page;
+        page = next_page;
       }
       if (it.blk_begin == 0 && it.blk_end < it.n_blk) {              // the rest of this unit is other CTAs' work
         rec.n_parts = static_cast<int>(static_cast<uint64_t>((span.begin + it.unit_end) * span.n_ctas - 1) / static_cast<uint64_t>(span.total)) -
@@ -318,18 +319,19 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     if (lane == 0) a.merges[blockIdx.x] = rec;
   } else if (warp == 11) {
     // ------------------------------------------------------------ Q into parts, masks, V without what does not count
-    constexpr int LANES = D / 16;                                  // a thread has 16 elements of a row
-    uint32_t n_item = 0, n_tile = 0, n_clean = 0;
+    constexpr int LANES = D / 16;                                  // a lane has 16 elements of a row
+    uint32_t n_q = 0, n_item = 0, n_tile = 0, n_clean = 0;
     bool ok = true;
-    while (ok && next_item<NC>(cur, a, &it)) {
-      const int nb = it.blk_end - it.blk_begin, qs = n_item & 1;
-      int* flag = &bad_flag[n_item % FLAGS];                       // read at the end of the item that set it, long before its next use
+    auto prepare_q = [&](const Item& it) {
+      const int qs = n_q & 1, node0 = it.flat0 / a.group;
+      int* flag = &bad_flag[n_q % FLAGS];                          // read at the end of its item, long before its next use
       if (lane == 0) *flag = 0;
-      ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_item >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
-      if (!ok) break;
-      const int node0 = it.flat0 / a.group;
-#pragma unroll 1
-      for (int c0 = 0; c0 < it.n_rows; c0 += 32 / LANES) {
+      ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
+      if (!ok) return;
+      // rows behind the last one, up to four or sixteen (what the softmax takes at a time), are zeros
+      const int last = it.n_rows & 15, n_zero = last == 0 ? it.n_rows : it.n_rows - last + (last <= 4 ? 4 : 16);
+#pragma unroll 2
+      for (int c0 = 0; c0 < n_zero; c0 += 32 / LANES) {
         const int c = c0 + lane / LANES, l = lane % LANES;
         uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
         if (c < it.n_rows) {
@@ -354,7 +356,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         const uint32_t b = __float_as_uint(amax);
         const int ex = min(max(static_cast<int>(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
         const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-        if (c < it.n_rows) {
+        if (c < n_zero) {
           if (l == 0) q_scale[qs][c] = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) * a.scale_log2;
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e] *= down;
@@ -382,42 +384,53 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       fence_proxy_async_smem();                            // the MMA reads Q through the async proxy
       __syncwarp();
       if (elect_one()) mbar_arrive(&q_full[qs]);
+      __syncwarp();
+      ++n_q;
+    };
+    // an item's Q is there before the item ahead of it ends (whose V is cleaned last)
+    bool more = next_item<NC>(cur, a, &it);
+    if (more) prepare_q(it);
+    while (ok && more) {
+      Item next{};
+      more = next_item<NC>(cur, a, &next);
+      if (more) prepare_q(next);
+      int* flag = &bad_flag[n_item % FLAGS];
       // V: zeros behind the prompt's last slot, and where a drafted V is NaN (with the flag raised)
 #pragma unroll 1
-      for (int blk = max(it.blk_begin, it.ctx_len / BLK); blk < it.blk_end; ++blk) {
+      for (int blk = max(it.blk_begin, it.ctx_len / BLK); ok && blk < it.blk_end; ++blk) {
         const uint32_t t = n_tile + blk - it.blk_begin;
-        // not on `landed`: these warps pass over most tiles, and a parity says nothing about a phase that is not the next one
+        // not on `landed`: this warp passes over most tiles, and a parity says nothing about a phase that is not the next one
         ok = __all_sync(0xffffffffu, bar_wait(&dirty[n_clean % CLEAN_BARS], (n_clean / CLEAN_BARS) & 1u, a.err_word, DEV_ERR_ATTN_CORR));
         if (!ok) break;
         uint8_t* v = ring + (t % STAGES) * STAGE_BYTES + GROUP_BYTES;
         const int r0 = max(it.ctx_len - blk * BLK, 0), r_end = it.ctx_len + it.n_nodes - blk * BLK;
         bool bad = false;
         // a lane takes a 16-byte vector (as stored; the swizzle only permutes a row group's vectors) of rows 32 / LANES apart
-#pragma unroll 1
-        for (int r = r0 + lane / LANES; r < BLK; r += 32 / LANES) {
-          uint4* p = reinterpret_cast<uint4*>(v + (r >> 3) * SBO + swizzled<D>(r & 7, (lane % LANES) * 16));
-          if (r >= r_end) {
-            *p = make_uint4(0, 0, 0, 0);
-          } else {
-            const uint4 x = *p;
-            uint32_t w[4] = {x.x, x.y, x.z, x.w}, any = 0;
+        auto vector = [&](int r) { return reinterpret_cast<uint4*>(v + (r >> 3) * SBO + swizzled<D>(r & 7, (lane % LANES) * 16)); };
+#pragma unroll 4
+        for (int r = max(r_end, 0) + lane / LANES; r < BLK; r += 32 / LANES) *vector(r) = make_uint4(0, 0, 0, 0);
+#pragma unroll 4
+        for (int r = r0 + lane / LANES; r < min(r_end, BLK); r += 32 / LANES) {
+          const uint4 x = *vector(r);
+          uint32_t w[4] = {x.x, x.y, x.z, x.w}, any = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t nan = ((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-              any |= nan;
-              w[e] &= ~((nan >> 7) * 0xffu);
-            }
-            if (any) { *p = make_uint4(w[0], w[1], w[2], w[3]); bad = true; }
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t nan = ((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            any |= nan;
+            w[e] &= ~((nan >> 7) * 0xffu);
           }
+          if (any) { *vector(r) = make_uint4(w[0], w[1], w[2], w[3]); bad = true; }
         }
         if (bad) *reinterpret_cast<volatile int*>(flag) = 1;
         fence_proxy_async_smem();
         __syncwarp();
         if (elect_one()) mbar_arrive(&cleaned[n_clean % CLEAN_BARS]);
+        __syncwarp();
         ++n_clean;
       }
-      n_tile += nb;
+      n_tile += it.blk_end - it.blk_begin;
       ++n_item;
+      it = next;
     }
     if (!ok) cta_failed = 1;
   } else if (warp == 9 || warp == 10) {
@@ -508,7 +521,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       uint32_t unset = 0xffffffffu >> (32 - it.n_rows);    // rows that have seen nothing yet: reference 0, sum and O zero
 #pragma unroll
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
-      if (lane < NC) neg[lane] = 0.f;
+      if (lane < NC) neg[lane] = lane < it.n_rows ? 0.f : -INFINITY;         // columns behind the last row get no weights
       __syncwarp();
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&q_full[par], (n_item >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // scales, masks
       for (int j = i; j < nb; j += 2) {
@@ -522,30 +535,33 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           tc_fence_after_sync();
           const float4 sc = page_scale[t % STAGES][r / PAGE_TOKENS];
           inv_v = sc.z;
-#pragma unroll
-          for (int c0 = 0; c0 < NC; c0 += 16) {            // 16 rows at a time, their columns asked for together
-            uint32_t x[16 * X::Q];
-#pragma unroll
-            for (int c = 0; c < 16; c += 4)
-              if (c0 + c < it.n_rows) tmem_columns<4 * X::Q>(lanes + i * X::NS + (c0 + c) * X::Q, x + c * X::Q);
+          // sixteen rows at a time, or four where there are no more: straight code, so that their latencies overlap
+          auto scores = [&](auto rows, int c0) {
+            constexpr int R = decltype(rows)::value;
+            uint32_t x[R * X::Q];
+            tmem_columns<R * X::Q>(lanes + i * X::NS + c0 * X::Q, x);
             tmem_wait_ld();
 #pragma unroll
-            for (int c = 0; c < 16; c += 4) {
-              if (c0 + c < it.n_rows) {
-                const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0 + c]);
-                const float qf[4] = {q4.x, q4.y, q4.z, q4.w};
+            for (int c = 0; c < R; c += 4) {
+              const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0 + c]);
+              const float qf[4] = {q4.x, q4.y, q4.z, q4.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  float y = __uint_as_float(x[(c + e) * X::Q + X::Q - 1]);
+              for (int e = 0; e < 4; ++e) {
+                float y = __uint_as_float(x[(c + e) * X::Q + X::Q - 1]);
 #pragma unroll
-                  for (int part = X::Q - 2; part >= 0; --part) y = fmaf(y, 0.0625f, __uint_as_float(x[(c + e) * X::Q + part]));
-                  // columns behind the last row hold anything
-                  s[c0 + c + e] = c0 + c + e < it.n_rows ? fmaf(y, sc.x * qf[e], sc.y) : -INFINITY;
-                }
-              } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[c0 + c + e] = -INFINITY;
+                for (int part = X::Q - 2; part >= 0; --part) y = fmaf(y, 0.0625f, __uint_as_float(x[(c + e) * X::Q + part]));
+                s[c0 + c + e] = fmaf(y, sc.x * qf[e], sc.y);
               }
+            }
+          };
+#pragma unroll
+          for (int c0 = 0; c0 < NC; c0 += 16) {
+            if (it.n_rows > c0 + 4) {
+              scores(Const<16>{}, c0);
+            } else {
+#pragma unroll
+              for (int c = c0; c < c0 + 16; ++c) s[c] = -INFINITY;
+              if (it.n_rows > c0) scores(Const<4>{}, c0);
             }
           }
           tc_fence_before_sync();
@@ -571,13 +587,22 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           }
           __syncwarp();
           if (j != i) {                                    // (the first block always sets the references)
+            float top = -INFINITY;
 #pragma unroll
-            for (int c0 = 0; c0 < NC; c0 += 4) {
-              if (c0 >= it.n_rows) break;
-              const float4 n4 = *reinterpret_cast<const float4*>(neg + c0);
-              raise |= s[c0] + n4.x > HEADROOM + RESCALE_THRESHOLD || s[c0 + 1] + n4.y > HEADROOM + RESCALE_THRESHOLD ||
-                       s[c0 + 2] + n4.z > HEADROOM + RESCALE_THRESHOLD || s[c0 + 3] + n4.w > HEADROOM + RESCALE_THRESHOLD;
+            for (int c0 = 0; c0 < NC; c0 += 16) {
+              auto most = [&](int c) {
+                const float4 n4 = *reinterpret_cast<const float4*>(neg + c);
+                top = fmax3(top, s[c] + n4.x, s[c + 1] + n4.y);
+                top = fmax3(top, s[c + 2] + n4.z, s[c + 3] + n4.w);
+              };
+              if (it.n_rows > c0) most(c0);
+              if (it.n_rows > c0 + 4) {
+                most(c0 + 4);
+                most(c0 + 8);
+                most(c0 + 12);
+              }
             }
+            raise = top > HEADROOM + RESCALE_THRESHOLD;
             if (unset != 0) {
 #pragma unroll
               for (int c = 0; c < NC; ++c) raise |= ((unset >> c) & 1u) && s[c] > -INFINITY;
@@ -597,7 +622,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           const float now = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) - HEADROOM;             // the block's own reference
           const float old = lane < NC ? neg[lane] : 0.f;
           const bool fresh = (unset >> lane) & 1u;
-          const bool up = lane < NC && now > -INFINITY && (fresh || now + old > RESCALE_THRESHOLD);
+          const bool up = lane < it.n_rows && now > -INFINITY && (fresh || now + old > RESCALE_THRESHOLD);
           const float alpha = !up ? 1.f : fresh ? 0.f : fast_exp2(-old - now);
           if (up) neg[lane] = -now;
           unset &= ~(__ballot_sync(0xffffffffu, up));
@@ -630,21 +655,21 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&p_free[i], (n_s & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // the product before has read P
         ++n_s;
         if (ok) {
+          auto weights = [&](auto rows, int c0) {          // of rows c0 ..: the slot's row of P, two rows' parts a half word
+            constexpr int R = decltype(rows)::value, WORDS = (R * X::P + 15) / 16 * 4;
+            uint32_t w[WORDS];
 #pragma unroll
-          for (int c16 = 0; c16 < NC; c16 += 16) {
-            if (c16 >= it.n_rows) break;
-            uint32_t w[4 * X::P];                          // the slot's row of P: two rows' parts a half word
+            for (int e = 0; e < WORDS; ++e) w[e] = 0u;
 #pragma unroll
-            for (int c = 0; c < 16; c += 4) {
-              if (c16 + c >= it.n_rows) break;
-              const float4 n4 = *reinterpret_cast<const float4*>(neg + c16 + c);
+            for (int c = 0; c < R; c += 4) {
+              const float4 n4 = *reinterpret_cast<const float4*>(neg + c0 + c);
               uint32_t two[2][X::P];
 #pragma unroll
               for (int u = 0; u < 2; ++u) {
-                const int c0 = c16 + c + 2 * u;
-                const float w0 = fast_exp2(s[c0] + (u ? n4.z : n4.x)), w1 = fast_exp2(s[c0 + 1] + (u ? n4.w : n4.y));
-                l[c0] = fmaf(w0, inv_v, l[c0]);            // the row sum has the weights without s_V, and before they are split
-                l[c0 + 1] = fmaf(w1, inv_v, l[c0 + 1]);
+                const int k = c0 + c + 2 * u;
+                const float w0 = fast_exp2(s[k] + (u ? n4.z : n4.x)), w1 = fast_exp2(s[k + 1] + (u ? n4.w : n4.y));
+                l[k] = fmaf(w0, inv_v, l[k]);              // the row sum has the weights without s_V, and before they are split
+                l[k + 1] = fmaf(w1, inv_v, l[k + 1]);
                 split_weights<X>(w0, w1, two[u]);
               }
 #pragma unroll
@@ -654,10 +679,13 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
               }
             }
 #pragma unroll
-            for (int q = 0; q < X::P; ++q) {
-              if (c16 * X::P + q * 16 < ((it.n_rows + 1) & ~1) * X::P)
-                *reinterpret_cast<uint4*>(p_row + swizzled<X::P_ROW>(r, c16 * X::P + q * 16)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
-            }
+            for (int q = 0; q < WORDS / 4; ++q)
+              *reinterpret_cast<uint4*>(p_row + swizzled<X::P_ROW>(r, c0 * X::P + q * 16)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+          };
+#pragma unroll
+          for (int c0 = 0; c0 < NC; c0 += 16) {
+            if (it.n_rows > c0 + 4) weights(Const<16>{}, c0);
+            else if (it.n_rows > c0) weights(Const<4>{}, c0);
           }
           fence_proxy_async_smem();                        // the MMA reads P through the async proxy
           tc_fence_before_sync();
@@ -894,9 +922,8 @@ int launch_tree_attention_8bit(const TreeAttention8& t, int n_sms, cudaStream_t 
     constexpr int D = decltype(dim)::value, NC = decltype(nc)::value;
     return t.kv.bf16 ? launch<D, NC, true>(tm, p, n_ctas, s) : launch<D, NC, false>(tm, p, n_ctas, s);
   };
-  using std::integral_constant;
-  if (d == 128) return columns == 16 ? run(integral_constant<int, 128>{}, integral_constant<int, 16>{}) : run(integral_constant<int, 128>{}, integral_constant<int, 32>{});
-  return columns == 16 ? run(integral_constant<int, 64>{}, integral_constant<int, 16>{}) : run(integral_constant<int, 64>{}, integral_constant<int, 32>{});
+  if (d == 128) return columns == 16 ? run(Const<128>{}, Const<16>{}) : run(Const<128>{}, Const<32>{});
+  return columns == 16 ? run(Const<64>{}, Const<16>{}) : run(Const<64>{}, Const<32>{});
 }
 
 }  // namespace pc
