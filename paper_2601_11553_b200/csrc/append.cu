@@ -16,6 +16,12 @@ namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
 // The prompt that owns a row: the last one whose row_start is not above it (-1 or n_seqs: none).  A whole warp asks for 128 entries at
 // a time, so that up to 127 prompts cost one round trip.
 __device__ __forceinline__ int owner_of(const int32_t* row_start, int n_seqs, int row) {
@@ -48,79 +54,124 @@ __device__ __forceinline__ RowPlace place_of(const NewRows& r, int seq) {
   return p;
 }
 
-template <bool BF16>
-__device__ __forceinline__ void unpack8(const uint4& w, float* x) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (BF16) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    } else {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-      x[2 * i] = f.x;
-      x[2 * i + 1] = f.y;
-    }
-  }
+// Two floats, for the packed instructions.
+struct Two { uint64_t v; };
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
 }
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  if constexpr (BF16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  } else {
-    // finite values past fp16's range become the largest, infinity and NaN stay
-    if (!(fabsf(a) <= 65504.f) && fabsf(a) < INFINITY) a = copysignf(65504.f, a);
-    if (!(fabsf(b) <= 65504.f) && fabsf(b) < INFINITY) b = copysignf(65504.f, b);
-    const __half2 v = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
+__device__ __forceinline__ float2 floats(Two x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+  return r;
 }
-template <bool BF16>
-__device__ __forceinline__ uint4 pack8(const float* x) {
-  return make_uint4(pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]), pack2<BF16>(x[6], x[7]));
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
 }
 
-// Eight consecutive floats.
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  *reinterpret_cast<float4*>(x) = ld_dep_f32x4(p);
-  *reinterpret_cast<float4*>(x + 4) = ld_dep_f32x4(p + 4);
+// A lane's part of a row of one head: eight elements from 8 l on, and the eight behind the half that they are turned with; l: lane within the
+// row's D / 16.
+struct Part { Two lo[4], hi[4]; };
+template <bool BF16>
+__device__ __forceinline__ Two unpack2(uint32_t w) {
+  if constexpr (BF16) return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return two(f.x, f.y);
 }
-// x[0..7]: elements 8 l .. of the lower half, x[8..15]: those of the upper half; l: lane within the row's D / 16.  Only that row's lanes meet.
+template <bool BF16>
+__device__ __forceinline__ Part unpack(const uint4& lo, const uint4& hi) {
+  return Part{{unpack2<BF16>(lo.x), unpack2<BF16>(lo.y), unpack2<BF16>(lo.z), unpack2<BF16>(lo.w)},
+              {unpack2<BF16>(hi.x), unpack2<BF16>(hi.y), unpack2<BF16>(hi.z), unpack2<BF16>(hi.w)}};
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(Two x) {
+  const float2 f = floats(x);
+  if constexpr (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const __half2 v = __floats2half2_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+// Halves that became infinite though the value was not: the largest finite one instead (infinity and NaN stay).
+__device__ __noinline__ uint32_t largest_half2(uint32_t h, float2 f) {
+  if ((h & 0x7fffu) == 0x7c00u && fabsf(f.x) < INFINITY) h -= 1u;
+  if ((h & 0x7fff0000u) == 0x7c000000u && fabsf(f.y) < INFINITY) h -= 0x10000u;
+  return h;
+}
+template <bool BF16>
+__device__ __forceinline__ uint4 pack4(const Two (&x)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = pack2<BF16>(x[e]);
+  if constexpr (!BF16) {
+    const __half2 a = __hmax2(__habs2(*reinterpret_cast<__half2*>(&w[0])), __habs2(*reinterpret_cast<__half2*>(&w[1])));
+    const __half2 b = __hmax2(__habs2(*reinterpret_cast<__half2*>(&w[2])), __habs2(*reinterpret_cast<__half2*>(&w[3])));
+    const __half2 m = __hmax2(a, b);
+    const uint32_t bits = *reinterpret_cast<const uint32_t*>(&m);
+    if ((bits & 0xffffu) == 0x7c00u || (bits >> 16) == 0x7c00u) {            // (the maximum passes NaN over)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = largest_half2(w[e], floats(x[e]));
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 1 / sqrt(mean x^2 + eps) of the row; the whole warp calls.
 template <int D>
-__device__ __forceinline__ void normalise(float (&x)[16], const float* gain, float eps, int l) {
-  constexpr int LANES = D / 16;
-  const uint32_t row = ((1u << LANES) - 1) << (threadIdx.x & 31 & ~(LANES - 1));
-  float sum = 0.f;
+__device__ __forceinline__ float norm_factor(const Part& x, float eps) {
+  Two a = x.lo[0] * x.lo[0], b = x.hi[0] * x.hi[0];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) sum = fmaf(x[e], x[e], sum);
+  for (int e = 1; e < 4; ++e) { a = fma2(x.lo[e], x.lo[e], a); b = fma2(x.hi[e], x.hi[e], b); }
+  const float2 fa = floats(a), fb = floats(b);
+  float sum = (fa.x + fa.y) + (fb.x + fb.y);
 #pragma unroll
-  for (int o = LANES / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(row, sum, o);
-  const float f = rsqrtf(fmaf(sum, 1.0f / D, eps));
-  float g[16];
-  load8(gain + l * 8, g);
-  load8(gain + D / 2 + l * 8, g + 8);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) x[e] = x[e] * f * g[e];
+  for (int o = D / 32; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return rsqrtf(fmaf(sum, 1.0f / D, eps));
 }
-struct Turn { float c[8], s[8]; };
+// x times f and the gain, of which load(q) gives the lane's q-th four.
+template <typename Load>
+__device__ __forceinline__ void scale_by(Part& x, float f, Load load) {
+  const Two ff = two(f, f);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float4 g = load(q);                     // elements 4 q .. of the lane's sixteen
+    Two* y = (q < 2 ? x.lo : x.hi) + (q & 1) * 2;
+    y[0] = y[0] * ff * two(g.x, g.y);
+    y[1] = y[1] * ff * two(g.z, g.w);
+  }
+}
+template <int D>
+__device__ __forceinline__ float4 gain_part(const float* gain, int l, int q) { return ld_dep_f32x4(gain + (q >> 1) * (D / 2) + l * 8 + (q & 1) * 4); }
+struct Turn { Two c[4], s[4]; };
 template <int D>
 __device__ __forceinline__ Turn turn_of(const float* rope, int position, int l) {
   Turn t;
   const float* p = rope + (static_cast<size_t>(position) * (D / 2) + l * 8) * 2;
 #pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    const float4 v = ld_dep_f32x4(p + e * 2);
-    t.c[e] = v.x; t.s[e] = v.y; t.c[e + 1] = v.z; t.s[e + 1] = v.w;
+  for (int e = 0; e < 4; ++e) {
+    const float4 v = ld_dep_f32x4(p + e * 4);
+    t.c[e] = two(v.x, v.z);
+    t.s[e] = two(v.y, v.w);
   }
   return t;
 }
-__device__ __forceinline__ void rotate(float (&x)[16], const Turn& t) {
+__device__ __forceinline__ void rotate(Part& x, const Turn& t) {
+  const Two minus = two(-1.f, -1.f);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float a = x[e], b = x[e + 8];
-    x[e] = a * t.c[e] - b * t.s[e];
-    x[e + 8] = fmaf(b, t.c[e], a * t.s[e]);
+  for (int e = 0; e < 4; ++e) {
+    const Two a = x.lo[e], b = x.hi[e];
+    x.lo[e] = fma2(b * t.s[e], minus, a * t.c[e]);
+    x.hi[e] = fma2(b, t.c[e], a * t.s[e]);
   }
 }
 __device__ __forceinline__ int position_of(const NewRows& r, int row, int slot) {
@@ -162,15 +213,15 @@ __device__ __forceinline__ void row_heads(const KvView& kv, const NewRows& r, in
     if (h0 + u * GROUPS >= h1) break;
     const int h = h0 + u * GROUPS + g;
     const bool is_q = !POOLS || h < hq, is_k = !is_q && h < hq + hkv;
-    const float* gain = is_q ? r.q_gain : is_k ? r.k_gain : nullptr;
+    // heads of different kinds may be side by side: all lanes work theirs out, values are then stored as they came
+    const float* gain = is_q ? r.q_gain : r.k_gain;
+    Part x = unpack<BF16>(lo[u], hi[u]);
+    const float f = norm_factor<D>(x, r.eps);
+    if (gain) scale_by(x, f, [&](int q) { return gain_part<D>(gain, l, q); });
+    if (r.rope) rotate(x, t);
     if (is_q || is_k) {
-      float x[16];
-      unpack8<BF16>(lo[u], x);
-      unpack8<BF16>(hi[u], x + 8);
-      if (gain) normalise<D>(x, gain, r.eps, l);
-      if (r.rope) rotate(x, t);
-      lo[u] = pack8<BF16>(x);
-      hi[u] = pack8<BF16>(x + 8);
+      lo[u] = pack4<BF16>(x.lo);
+      hi[u] = pack4<BF16>(x.hi);
     }
     E* dst;
     if (h >= h1) continue;
@@ -201,6 +252,87 @@ __device__ __forceinline__ int scale_exponent(float amax) {
   return min(max(e, -32), 32);
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+
+__device__ __forceinline__ float largest(const Part& x) {                      // finite magnitude
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 a = floats(x.lo[e]), b = floats(x.hi[e]);
+    m = fmax3(fmax3(m, fabsf(a.x), fabsf(a.y)), fabsf(b.x), fabsf(b.y));
+  }
+  if (m < INFINITY) return m;                     // (the maximum passes NaN over)
+  m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 a = floats(x.lo[e]), b = floats(x.hi[e]);
+    const float v[4] = {fabsf(a.x), fabsf(a.y), fabsf(b.x), fabsf(b.y)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (v[i] < INFINITY) m = fmaxf(m, v[i]);
+  }
+  return m;
+}
+// The scale of a page's keys or values (kind: head * 2, + 1 for values) with new values up to amax (a lane's; the whole warp calls), written.
+struct PageScale {
+  int kind;
+  float inv, again;              // 1 / the scale; what it was times that, or 1: bytes in use stay
+};
+__device__ __forceinline__ PageScale page_scale(const Kv8View& kv, int page, int kind, int lo, float amax) {
+  float* at = const_cast<float*>(kv.scales) + static_cast<size_t>(page) * kv.n_kv_heads * 2 + kind;
+  const float before = lo > 0 ? fminf(fmaxf(ld_dep_f32(at), 0x1p-32f), 0x1p32f) : 0.f;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+  const float want = power_of_two(scale_exponent(amax)), scale = fmaxf(before, want);
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) *at = scale;
+  const float inv = 1.0f / scale;
+  return PageScale{kind, inv, before >= want ? 1.f : before * inv};
+}
+// A row's values as bytes, from element 8 l of its lower half on.
+template <int D>
+__device__ __forceinline__ void store_row(uint8_t* to, const Part& x, float inv) {
+  const Two by = two(inv, inv);
+  auto bytes = [&](Two a, Two b) {
+    const float2 x = floats(a * by), y = floats(b * by);
+    return pack_e4m3x2(x.x, x.y) | pack_e4m3x2(y.x, y.y) << 16;
+  };
+  *reinterpret_cast<uint2*>(to) = make_uint2(bytes(x.lo[0], x.lo[1]), bytes(x.lo[2], x.lo[3]));
+  *reinterpret_cast<uint2*>(to + D / 2) = make_uint2(bytes(x.hi[0], x.hi[1]), bytes(x.hi[2], x.hi[3]));
+}
+template <int D>
+__device__ __forceinline__ void round_again(uint8_t* to, const PageScale& ps) {
+  if (ps.again == 1.f) return;
+  const uint2 a = *reinterpret_cast<uint2*>(to), b = *reinterpret_cast<uint2*>(to + D / 2);
+  uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 y = unpack_e4m3x2(w[e] & 0xffffu), z = unpack_e4m3x2(w[e] >> 16);
+    w[e] = pack_e4m3x2(y.x * ps.again, y.y * ps.again) | pack_e4m3x2(z.x * ps.again, z.y * ps.again) << 16;
+  }
+  *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+  *reinterpret_cast<uint2*>(to + D / 2) = make_uint2(w[2], w[3]);
+}
+
+// The units (UNIT slots of a prompt, aligned to that) whose first new row is among rows [begin, end): fn(prompt, unit of the prompt, first and behind
+// the last new slot in it).
+template <int UNIT, typename Fn>
+__device__ __forceinline__ void each_unit(const NewRows& r, int begin, int end, Fn fn) {
+  RowPlace p = place_of(r, owner_of(r.row_start, r.n_seqs, begin));
+  if (p.seq < 0) p = place_of(r, 0);               // rows ahead of the first prompt's
+  int row = begin;
+#pragma unroll 1
+  while (p.seq < r.n_seqs) {
+    row = max(row, p.first);
+    if (row >= end) break;
+    const int i = row - p.first, in_unit = (p.ctx + i) % UNIT;
+    if (i >= p.n) {
+      p = place_of(r, p.seq + 1);
+      continue;
+    }
+    if (i == 0 || in_unit == 0) fn(p, (p.ctx + i) / UNIT, in_unit, min(UNIT, in_unit + p.n - i));
+    row = p.first + min(i + UNIT - in_unit, p.n);       // the next unit's first new row, or the next prompt's
+  }
+}
 
 // Page j of a prompt: slots [lo, hi) are new.  The keys (even) and values (odd) of KV heads in turn, kinds [kind0, kind1) by one warp: the next kind's rows
 // are asked for before this one's are worked on.
@@ -236,65 +368,31 @@ __device__ __forceinline__ void fill_page(const Kv8View& kv, const NewRows& r, c
     }
   }
   if (static_cast<uint32_t>(page) >= static_cast<uint64_t>(kv.n_pages)) return;
-  uint8_t* dst0 = static_cast<uint8_t*>(const_cast<void*>(kv.pages)) + page * kv.page_stride;
-  float* scales = const_cast<float*>(kv.scales) + static_cast<size_t>(page) * kv.n_kv_heads * 2;
 #pragma unroll 1
   for (int kind = kind0; kind < kind1; ++kind) {
     const bool is_k = !(kind & 1);
-    const float before = lo > 0 ? fminf(fmaxf(ld_dep_f32(scales + kind), 0x1p-32f), 0x1p32f) : 0.f;
-    float x[PER][16];
+    Part x[PER];
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      unpack8<BF16>(raw[u][0], x[u]);
-      unpack8<BF16>(raw[u][1], x[u] + 8);
-    }
+    for (int u = 0; u < PER; ++u) x[u] = unpack<BF16>(raw[u][0], raw[u][1]);
     if (kind + 1 < kind1) fetch(kind + 1);
     float amax = 0.f;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
+      if (hi <= GROUPS * u || lo >= GROUPS * (u + 1)) continue;      // no lane's row is new
+      if (is_k && r.k_gain) scale_by(x[u], norm_factor<D>(x[u], r.eps), [&](int q) { return gain_part<D>(r.k_gain, l, q); });
+      if (is_k && r.rope) rotate(x[u], turn_of<D>(r.rope, position[u], l));
       const int s = g + GROUPS * u;
-      if (s >= lo && s < hi) {
-        if (is_k && r.k_gain) normalise<D>(x[u], r.k_gain, r.eps, l);
-        if (is_k && r.rope) rotate(x[u], turn_of<D>(r.rope, position[u], l));
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float a = fabsf(x[u][e]);
-          if (a < INFINITY) amax = fmaxf(amax, a);
-        }
-      }
+      amax = fmaxf(amax, s >= lo && s < hi ? largest(x[u]) : 0.f);
     }
     __syncwarp();
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    float scale = power_of_two(scale_exponent(amax));
-    const bool keep = before >= scale;
-    if (keep) scale = before;
-    const float inv = 1.0f / scale, again = before * inv;
-    uint8_t* dst = dst0 + static_cast<size_t>(kind) * (PAGE_TOKENS * D) + l * 8;
+    const PageScale ps = page_scale(kv, page, kind, lo, amax);
+    uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv.pages)) + page * kv.page_stride + static_cast<size_t>(kind) * (PAGE_TOKENS * D) + l * 8;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const int s = g + GROUPS * u;
-      uint2* to = reinterpret_cast<uint2*>(dst + s * D);
-      uint2* to_hi = reinterpret_cast<uint2*>(dst + s * D + D / 2);
-      if (s >= lo && s < hi) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_e4m3x2(x[u][4 * e] * inv, x[u][4 * e + 1] * inv) | pack_e4m3x2(x[u][4 * e + 2] * inv, x[u][4 * e + 3] * inv) << 16;
-        *to = make_uint2(w[0], w[1]);
-        *to_hi = make_uint2(w[2], w[3]);
-      } else if (s < lo && !keep) {
-        const uint2 a = *to, b = *to_hi;
-        uint32_t w[4] = {a.x, a.y, b.x, b.y};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 y = unpack_e4m3x2(w[e] & 0xffffu), z = unpack_e4m3x2(w[e] >> 16);
-          w[e] = pack_e4m3x2(y.x * again, y.y * again) | pack_e4m3x2(z.x * again, z.y * again) << 16;
-        }
-        *to = make_uint2(w[0], w[1]);
-        *to_hi = make_uint2(w[2], w[3]);
-      }
+      if (s >= lo && s < hi) store_row<D>(dst + s * D, x[u], ps.inv);
+      else if (s < lo) round_again<D>(dst + s * D, ps);
     }
-    if (lane == 0) scales[kind] = scale;
   }
 }
 
@@ -319,22 +417,167 @@ __global__ void __launch_bounds__(THREADS, 2) append_pages_kernel(const __grid_c
   const int kind0 = static_cast<int>(task % runs) * kinds, kind1 = min(kind0 + kinds, all);
   if (c * chunk >= r.n_rows) return;
   const int begin = static_cast<int>(c) * chunk, end = min(begin + chunk, r.n_rows);
-  RowPlace p = place_of(r, owner_of(r.row_start, r.n_seqs, begin));
-  if (p.seq < 0) p = place_of(r, 0);               // rows ahead of the first prompt's
-  int row = begin;
-#pragma unroll 1
-  while (p.seq < r.n_seqs) {
-    row = max(row, p.first);
-    if (row >= end) break;
-    const int i = row - p.first, in_page = (p.ctx + i) % PAGE_TOKENS;
-    if (i >= p.n) {
-      p = place_of(r, p.seq + 1);
-      continue;
+  each_unit<PAGE_TOKENS>(r, begin, end, [&](const RowPlace& p, int j, int lo, int hi) { fill_page<D, BF16>(kv, r, p, j, lo, hi, kind0, kind1); });
+}
+
+// ---------------------------------------------------------------------------------------------------- long prompts
+// 16 rows (those of 16 slots of a prompt, aligned to 16) of the queries', keys' and values' heads in turn, all by asynchronous copies into the warp's
+// own shared memory: a lane copies what it reads itself, so that nothing is waited for but its own copies, and the look-ups are shared by
+// 16 rows.  (With a row a warp and loads into registers, a warp's time went into look-ups: 33024 rows 113 us.)
+constexpr int DEPTH = 3;                          // heads on their way
+__device__ __forceinline__ void copy_async_16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+// Rows of a unit: a page's where that has one scale, else half as many, which leaves registers for half as many warps again.
+__host__ __device__ constexpr int unit_rows(bool eight) { return eight ? PAGE_TOKENS : PAGE_TOKENS / 2; }
+template <int D, bool BF16, bool EIGHT>
+__device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8, const NewRows& r, const RowPlace& p, int j, int lo, int hi, int first_kind, int kinds,
+                                           int step, uint4* mine, const float* gains) {
+  constexpr int LANES = D / 16, GROUPS = 32 / LANES, UNIT = unit_rows(EIGHT), PER = UNIT / GROUPS;
+  const int lane = threadIdx.x & 31, l = lane % LANES, g = lane / LANES;
+  using E = unsigned short;
+  const int hq = r.q ? r.n_q_heads : 0, hkv = EIGHT ? kv8.n_kv_heads : kv.n_kv_heads;
+  const int64_t row0 = p.first + j * UNIT - p.ctx;          // of the first slot
+  // kinds: queries' heads, keys' heads, values' heads
+  auto fetch = [&](int kind, int n) {
+    if (kind < kinds) {
+      const bool is_q = kind < hq, is_k = !is_q && kind < hq + hkv;
+      const E* src = is_q ? static_cast<const E*>(r.q) + kind * D : is_k ? static_cast<const E*>(r.k) + (kind - hq) * D : static_cast<const E*>(r.v) + (kind - hq - hkv) * D;
+      const int64_t stride = is_q ? r.q_stride : is_k ? r.k_stride : r.v_stride;
+      uint4* to = mine + (n % DEPTH) * (PER * 2 * 32) + lane;
+      const E* row = src + (row0 + g) * stride + l * 8;
+#pragma unroll
+      for (int u = 0; u < PER; ++u, row += GROUPS * stride) {
+        const int s = g + GROUPS * u;
+        if (s >= lo && s < hi) {
+          copy_async_16(to + (2 * u) * 32, row);
+          copy_async_16(to + (2 * u + 1) * 32, row + D / 2);
+        }
+      }
     }
-    if (i == 0 || in_page == 0)
-      fill_page<D, BF16>(kv, r, p, (p.ctx + i) / PAGE_TOKENS, in_page, min(PAGE_TOKENS, in_page + p.n - i), kind0, kind1);
-    row = p.first + min(i + PAGE_TOKENS - in_page, p.n);       // the next page's first new row, or the next prompt's
+    copies_commit();                                               // a group per step, empty ones too
+  };
+#pragma unroll
+  for (int n = 0; n < DEPTH - 1; ++n) fetch(first_kind + n * step, n);
+  // where they go
+  int64_t at[PER];                                                 // 16 bits: row of the pools, or -1
+  int page = 0;
+  bool there = true;
+  if constexpr (EIGHT) {
+    page = ld_dep_s32(kv8.page_table + static_cast<size_t>(p.seq) * kv8.pt_stride + j);
+    there = static_cast<uint32_t>(page) < static_cast<uint64_t>(kv8.n_pages);
+  } else {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int s = g + GROUPS * u;
+      at[u] = s >= lo && s < hi ? slot_row(kv.page_table, kv.pt_stride, kv.ctx_start, kv.n_slots, p.seq, j * UNIT + s) : -1;
+    }
   }
+  Turn turn[PER];                                                  // the rows' cosines and sines, for all kinds
+  if (r.rope) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int s = min(max(g + GROUPS * u, lo), hi - 1);
+      turn[u] = turn_of<D>(r.rope, position_of(r, static_cast<int>(row0) + s, j * UNIT + s), l);
+    }
+  }
+  int n = 0;
+#pragma unroll 1
+  for (int kind = first_kind; kind < kinds; kind += step, ++n) {
+    fetch(kind + (DEPTH - 1) * step, n + DEPTH - 1);
+    copies_wait<DEPTH - 1>();
+    const bool is_q = kind < hq, is_k = !is_q && kind < hq + hkv;
+    const float* gain = is_q ? (r.q_gain ? gains : nullptr) : is_k && r.k_gain ? gains + D : nullptr;
+    const uint4* from = mine + (n % DEPTH) * (PER * 2 * 32) + lane;
+    // A row's values, normalised and turned.  Rows that are not new are worked on too (whatever is there), so that lanes keep together;
+    // nothing of them is stored.
+    auto values = [&](int u) {
+      Part x = unpack<BF16>(from[(2 * u) * 32], from[(2 * u + 1) * 32]);
+      if (gain) scale_by(x, norm_factor<D>(x, r.eps), [&](int q) { return *reinterpret_cast<const float4*>(gain + (q * LANES + l) * 4); });
+      if (r.rope && (is_q || is_k)) rotate(x, turn[u]);
+      return x;
+    };
+    if (!EIGHT || is_q) {
+      const int64_t stride = is_q ? r.q_out_stride : 0;
+      E* q_row = is_q ? static_cast<E*>(r.q_out) + (row0 + g) * stride + kind * D + l * 8 : nullptr;
+#pragma unroll
+      for (int u = 0; u < PER; ++u, q_row += GROUPS * stride) {
+        const int s = g + GROUPS * u;
+        uint4 a, b;
+        if (is_q || is_k) {
+          const Part x = values(u);
+          a = pack4<BF16>(x.lo);
+          b = pack4<BF16>(x.hi);
+        } else {
+          a = from[(2 * u) * 32];
+          b = from[(2 * u + 1) * 32];
+        }
+        E* dst = q_row;
+        bool put = s >= lo && s < hi;
+        if constexpr (!EIGHT) {
+          if (!is_q) {
+            put = at[u] >= 0;
+            dst = (is_k ? static_cast<E*>(const_cast<void*>(kv.k)) + at[u] * kv.k_stride + (kind - hq) * D
+                        : static_cast<E*>(const_cast<void*>(kv.v)) + at[u] * kv.v_stride + (kind - hq - hkv) * D) + l * 8;
+          }
+        }
+        if (put) {
+          *reinterpret_cast<uint4*>(dst) = a;
+          *reinterpret_cast<uint4*>(dst + D / 2) = b;
+        }
+      }
+    } else if constexpr (EIGHT) {
+      // twice over the rows: for the page's largest value, then for the bytes (16 rows' values beside their cosines and sines are more
+      // than a thread's registers)
+      float amax = 0.f;
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const float m = largest(values(u));
+        const int s = g + GROUPS * u;
+        amax = fmaxf(amax, s >= lo && s < hi ? m : 0.f);
+      }
+      if (there) {
+        const PageScale ps = page_scale(kv8, page, (is_k ? kind - hq : kind - hq - hkv) * 2 + (is_k ? 0 : 1), lo, amax);
+        uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(ps.kind) * (PAGE_TOKENS * D) + l * 8;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const Part x = values(u);
+          const int s = g + GROUPS * u;
+          if (s >= lo && s < hi) store_row<D>(dst + s * D, x, ps.inv);
+          else if (s < lo) round_again<D>(dst + s * D, ps);
+        }
+      }
+    }
+    __syncwarp();
+  }
+  copies_wait<0>();
+}
+
+template <int D, bool BF16, bool EIGHT>
+__global__ void __launch_bounds__(THREADS, EIGHT ? 2 : 3) append_units_kernel(const __grid_constant__ KvView kv, const __grid_constant__ Kv8View kv8, const __grid_constant__ NewRows r, int kinds, int parts) {
+  constexpr int LANES = D / 16, GROUPS = 32 / LANES, UNIT = unit_rows(EIGHT), PER = UNIT / GROUPS;
+  extern __shared__ uint4 ring[];
+  __shared__ __align__(16) float gains[2 * D];
+  pdl_launch_dependents();
+  pdl_wait();
+  if (threadIdx.x < 2 * D) {
+    const float* gain = threadIdx.x < D ? r.q_gain : r.k_gain;
+    // a lane's sixteen in four parts, the lanes' parts one behind the other (no bank is asked twice)
+    const int e = threadIdx.x % D, half = e / (D / 2), in = e % (D / 2), part = half * 2 + (in % 8) / 4;
+    if (gain) gains[threadIdx.x / D * D + (part * LANES + in / 8) * 4 + in % 4] = ld_dep_f32(gain + e);
+  }
+  __syncthreads();
+  const int64_t task = static_cast<int64_t>(blockIdx.x) * WARPS + (threadIdx.x >> 5);
+  const int64_t c = task / parts;
+  if (c * UNIT >= r.n_rows) return;
+  const int part = static_cast<int>(task % parts), begin = static_cast<int>(c) * UNIT, end = min(begin + UNIT, r.n_rows);
+  each_unit<UNIT>(r, begin, end, [&](const RowPlace& p, int j, int lo, int hi) {
+    unit_kinds<D, BF16, EIGHT>(kv, kv8, r, p, j, lo, hi, part, kinds, parts, ring + (threadIdx.x >> 5) * (DEPTH * PER * 2 * 32), gains);
+  });
 }
 
 // Heads a warp takes: as many as it can hold at once when that leaves enough warps for every SM, else one a group.
@@ -344,8 +587,26 @@ int run_of(int64_t rows, int heads, int n_sms) {
   return rows * ((heads + 4 * GROUPS - 1) / (4 * GROUPS)) >= static_cast<int64_t>(n_sms) * WARPS * 2 ? 4 * GROUPS : GROUPS;
 }
 
+// Sixteen rows at a time where prompts have that many new rows on average.
+constexpr int LONG = 16;
+template <int D, bool BF16, bool EIGHT>
+int append_units(const KvView& kv, const Kv8View& kv8, const NewRows& r, cudaStream_t s) {
+  static bool set[MAX_DEVICES] = {};
+  const int dev = current_device_slot();
+  constexpr int UNIT = unit_rows(EIGHT), smem = WARPS * DEPTH * UNIT * D * 2;
+  if (!set[dev]) {
+    if (cudaFuncSetAttribute(append_units_kernel<D, BF16, EIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    set[dev] = true;
+  }
+  const int kinds = (r.q ? r.n_q_heads : 0) + 2 * (EIGHT ? kv8.n_kv_heads : kv.n_kv_heads), parts = std::min(kinds, WARPS);
+  const int64_t blocks = ((static_cast<int64_t>(r.n_rows) + UNIT - 1) / UNIT * parts + WARPS - 1) / WARPS;
+  if (blocks > INT32_MAX) return -2;
+  return launch_pdl(append_units_kernel<D, BF16, EIGHT>, dim3(static_cast<unsigned>(blocks)), dim3(THREADS), smem, s, kv, kv8, r, kinds, parts) == cudaSuccess ? 0 : -1;
+}
+
 template <int D, bool BF16>
 int append(const KvView& kv, const NewRows& r, int n_sms, cudaStream_t s) {
+  if (r.n_rows / r.n_seqs >= LONG) return append_units<D, BF16, false>(kv, Kv8View{}, r, s);
   const int heads = (r.q ? r.n_q_heads : 0) + 2 * kv.n_kv_heads, run = run_of<D>(r.n_rows, heads, n_sms);
   const int64_t blocks = (static_cast<int64_t>(r.n_rows) * ((heads + run - 1) / run) + WARPS - 1) / WARPS;
   if (blocks > INT32_MAX) return -2;
@@ -353,9 +614,10 @@ int append(const KvView& kv, const NewRows& r, int n_sms, cudaStream_t s) {
 }
 template <int D, bool BF16>
 int append8(const Kv8View& kv, const NewRows& r, int n_sms, cudaStream_t s) {
+  if (r.n_rows / r.n_seqs >= LONG) return append_units<D, BF16, true>(KvView{}, kv, r, s);
   // Rows of a warp: about as many as a prompt has, so that batches of single tokens spread over the warps and long prompts have a page each.
-  const int per = r.n_rows / std::max(r.n_seqs, 1);
-  const int chunk = per >= 16 ? 16 : per >= 8 ? 8 : per >= 4 ? 4 : per >= 2 ? 2 : 1;
+  const int per = r.n_rows / r.n_seqs;
+  const int chunk = per >= 8 ? 8 : per >= 4 ? 4 : per >= 2 ? 2 : 1;
   const int64_t chunks = (static_cast<int64_t>(r.n_rows) + chunk - 1) / chunk;
   // Keys and values of a warp, one behind the other: four where that leaves enough warps.
   const int all = 2 * kv.n_kv_heads, kinds = chunks * ((all + 3) / 4) >= static_cast<int64_t>(n_sms) * WARPS ? 4 : 1;
