@@ -272,21 +272,14 @@ __device__ __forceinline__ float largest(const Part& x) {                      /
   }
   return m;
 }
-// The scale of a page's keys or values (kind: head * 2, + 1 for values) with new values up to amax (a lane's; the whole warp calls), written.
+// The scale of a page's keys or values with new values up to amax; before: what it has, which counts if slots are in use.
 struct PageScale {
-  int kind;
-  float inv, again;              // 1 / the scale; what it was times that, or 1: bytes in use stay
+  float scale, inv, again;       // again: what it was over what it is, or 1: bytes in use stay
 };
-__device__ __forceinline__ PageScale page_scale(const Kv8View& kv, int page, int kind, int lo, float amax) {
-  float* at = const_cast<float*>(kv.scales) + static_cast<size_t>(page) * kv.n_kv_heads * 2 + kind;
-  const float before = lo > 0 ? fminf(fmaxf(ld_dep_f32(at), 0x1p-32f), 0x1p32f) : 0.f;
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-  const float want = power_of_two(scale_exponent(amax)), scale = fmaxf(before, want);
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) *at = scale;
+__device__ __forceinline__ PageScale page_scale(bool in_use, float before, float amax) {
+  const float want = power_of_two(scale_exponent(amax)), have = in_use ? fminf(fmaxf(before, 0x1p-32f), 0x1p32f) : 0.f, scale = fmaxf(have, want);
   const float inv = 1.0f / scale;
-  return PageScale{kind, inv, before >= want ? 1.f : before * inv};
+  return PageScale{scale, inv, have >= want ? 1.f : have * inv};
 }
 // A row's values as bytes, from element 8 l of its lower half on.
 template <int D>
@@ -385,7 +378,12 @@ __device__ __forceinline__ void fill_page(const Kv8View& kv, const NewRows& r, c
       amax = fmaxf(amax, s >= lo && s < hi ? largest(x[u]) : 0.f);
     }
     __syncwarp();
-    const PageScale ps = page_scale(kv, page, kind, lo, amax);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    float* scale_at = const_cast<float*>(kv.scales) + static_cast<size_t>(page) * kv.n_kv_heads * 2 + kind;
+    const PageScale ps = page_scale(lo > 0, lo > 0 ? ld_dep_f32(scale_at) : 0.f, amax);
+    __syncwarp();
+    if (lane == 0) *scale_at = ps.scale;
     uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv.pages)) + page * kv.page_stride + static_cast<size_t>(kind) * (PAGE_TOKENS * D) + l * 8;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
@@ -425,6 +423,8 @@ __global__ void __launch_bounds__(THREADS, 2) append_pages_kernel(const __grid_c
 // own shared memory: a lane copies what it reads itself, so that nothing is waited for but its own copies, and the look-ups are shared by
 // 16 rows.  (With a row a warp and loads into registers, a warp's time went into look-ups: 33024 rows 113 us.)
 constexpr int DEPTH = 3;                          // heads on their way
+// Four warps a block, five blocks an SM: 96 registers.  (With 80 a few were kept in memory, and to fetch one took as long as the copies ahead of it.)
+constexpr int UNIT_WARPS = 4, UNIT_BLOCKS = 5, PARTS = 4;
 __device__ __forceinline__ void copy_async_16(void* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
 }
@@ -432,16 +432,28 @@ template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
-// Rows of a unit: a page's where that has one scale, else half as many, which leaves registers for half as many warps again.
-__host__ __device__ constexpr int unit_rows(bool eight) { return eight ? PAGE_TOKENS : PAGE_TOKENS / 2; }
+// Eight rows a warp: with sixteen, their cosines and sines leave registers for two thirds of the warps (33024 rows 107 -> 98 us).  An 8-bit page's two
+// halves are two warps' that tell each other their largest values.
+constexpr int UNIT = PAGE_TOKENS / 2;
+struct Pair {                    // of warps
+  int half, barrier;             // which half of the page is this warp's; a hardware barrier of the two
+  float (*amax)[2];              // [turn & 1][half] in shared memory
+};
 template <int D, bool BF16, bool EIGHT>
 __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8, const NewRows& r, const RowPlace& p, int j, int lo, int hi, int first_kind, int kinds,
-                                           int step, uint4* mine, const float* gains) {
-  constexpr int LANES = D / 16, GROUPS = 32 / LANES, UNIT = unit_rows(EIGHT), PER = UNIT / GROUPS;
+                                           int step, uint4* mine, const float* gains, const Pair& pair) {
+  constexpr int LANES = D / 16, GROUPS = 32 / LANES, PER = UNIT / GROUPS;
   const int lane = threadIdx.x & 31, l = lane % LANES, g = lane / LANES;
   using E = unsigned short;
   const int hq = r.q ? r.n_q_heads : 0, hkv = EIGHT ? kv8.n_kv_heads : kv.n_kv_heads;
-  const int64_t row0 = p.first + j * UNIT - p.ctx;          // of the first slot
+  // this warp's slots: from slot0 on, [lo, hi) of them new (in a page, those below lo are in use)
+  const bool in_use = lo > 0;
+  const int slot0 = EIGHT ? j * PAGE_TOKENS + pair.half * UNIT : j * UNIT;
+  if constexpr (EIGHT) {
+    lo = min(max(lo - pair.half * UNIT, 0), UNIT);
+    hi = min(max(hi - pair.half * UNIT, 0), UNIT);
+  }
+  const int64_t row0 = p.first + slot0 - p.ctx;          // of the first slot
   // kinds: queries' heads, keys' heads, values' heads
   auto fetch = [&](int kind, int n) {
     if (kind < kinds) {
@@ -474,15 +486,15 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const int s = g + GROUPS * u;
-      at[u] = s >= lo && s < hi ? slot_row(kv.page_table, kv.pt_stride, kv.ctx_start, kv.n_slots, p.seq, j * UNIT + s) : -1;
+      at[u] = s >= lo && s < hi ? slot_row(kv.page_table, kv.pt_stride, kv.ctx_start, kv.n_slots, p.seq, slot0 + s) : -1;
     }
   }
-  Turn turn[PER];                                                  // the rows' cosines and sines, for all kinds
+  Turn turn[PER] = {};                                              // the rows' cosines and sines, for all kinds
   if (r.rope) {
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const int s = min(max(g + GROUPS * u, lo), hi - 1);
-      turn[u] = turn_of<D>(r.rope, position_of(r, static_cast<int>(row0) + s, j * UNIT + s), l);
+      const int s = g + GROUPS * u;
+      if (s >= lo && s < hi) turn[u] = turn_of<D>(r.rope, position_of(r, static_cast<int>(row0) + s, slot0 + s), l);
     }
   }
   int n = 0;
@@ -531,23 +543,29 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
         }
       }
     } else if constexpr (EIGHT) {
-      // twice over the rows: for the page's largest value, then for the bytes (16 rows' values beside their cosines and sines are more
-      // than a thread's registers)
+      const int page_kind = (is_k ? kind - hq : kind - hq - hkv) * 2 + (is_k ? 0 : 1);
+      float* scale_at = const_cast<float*>(kv8.scales) + static_cast<size_t>(there ? page : 0) * kv8.n_kv_heads * 2 + page_kind;
+      const float before = in_use && there ? ld_dep_f32(scale_at) : 0.f;
+      Part x[PER];
       float amax = 0.f;
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
-        const float m = largest(values(u));
+        x[u] = values(u);
         const int s = g + GROUPS * u;
-        amax = fmaxf(amax, s >= lo && s < hi ? m : 0.f);
+        amax = fmaxf(amax, s >= lo && s < hi ? largest(x[u]) : 0.f);
       }
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      if (lane == 0) pair.amax[n & 1][pair.half] = amax;
+      asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair.barrier) : "memory");
+      const PageScale ps = page_scale(in_use, before, fmaxf(amax, pair.amax[n & 1][pair.half ^ 1]));
       if (there) {
-        const PageScale ps = page_scale(kv8, page, (is_k ? kind - hq : kind - hq - hkv) * 2 + (is_k ? 0 : 1), lo, amax);
-        uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(ps.kind) * (PAGE_TOKENS * D) + l * 8;
+        if (lane == 0 && pair.half == 0) *scale_at = ps.scale;
+        uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(page_kind) * (PAGE_TOKENS * D) + pair.half * (UNIT * D) + l * 8;
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-          const Part x = values(u);
           const int s = g + GROUPS * u;
-          if (s >= lo && s < hi) store_row<D>(dst + s * D, x, ps.inv);
+          if (s >= lo && s < hi) store_row<D>(dst + s * D, x[u], ps.inv);
           else if (s < lo) round_again<D>(dst + s * D, ps);
         }
       }
@@ -558,25 +576,30 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
 }
 
 template <int D, bool BF16, bool EIGHT>
-__global__ void __launch_bounds__(THREADS, EIGHT ? 2 : 3) append_units_kernel(const __grid_constant__ KvView kv, const __grid_constant__ Kv8View kv8, const __grid_constant__ NewRows r, int kinds, int parts) {
-  constexpr int LANES = D / 16, GROUPS = 32 / LANES, UNIT = unit_rows(EIGHT), PER = UNIT / GROUPS;
+__global__ void __launch_bounds__(UNIT_WARPS * 32, UNIT_BLOCKS) append_units_kernel(const __grid_constant__ KvView kv, const __grid_constant__ Kv8View kv8, const __grid_constant__ NewRows r, int kinds, int parts) {
+  constexpr int LANES = D / 16, GROUPS = 32 / LANES, PER = UNIT / GROUPS, ROWS = EIGHT ? PAGE_TOKENS : UNIT, SHARE = EIGHT ? 2 : 1;
   extern __shared__ uint4 ring[];
   __shared__ __align__(16) float gains[2 * D];
+  __shared__ float amax[UNIT_WARPS / 2][2][2];
   pdl_launch_dependents();
   pdl_wait();
-  if (threadIdx.x < 2 * D) {
-    const float* gain = threadIdx.x < D ? r.q_gain : r.k_gain;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float* gain = which ? r.k_gain : r.q_gain;
+    const int e = threadIdx.x;
     // a lane's sixteen in four parts, the lanes' parts one behind the other (no bank is asked twice)
-    const int e = threadIdx.x % D, half = e / (D / 2), in = e % (D / 2), part = half * 2 + (in % 8) / 4;
-    if (gain) gains[threadIdx.x / D * D + (part * LANES + in / 8) * 4 + in % 4] = ld_dep_f32(gain + e);
+    const int half = e / (D / 2), in = e % (D / 2), part = half * 2 + (in % 8) / 4;
+    if (gain && e < D) gains[which * D + (part * LANES + in / 8) * 4 + in % 4] = ld_dep_f32(gain + e);
   }
   __syncthreads();
-  const int64_t task = static_cast<int64_t>(blockIdx.x) * WARPS + (threadIdx.x >> 5);
+  const int warp = threadIdx.x >> 5;
+  const int64_t task = static_cast<int64_t>(blockIdx.x) * (UNIT_WARPS / SHARE) + warp / SHARE;
   const int64_t c = task / parts;
-  if (c * UNIT >= r.n_rows) return;
-  const int part = static_cast<int>(task % parts), begin = static_cast<int>(c) * UNIT, end = min(begin + UNIT, r.n_rows);
-  each_unit<UNIT>(r, begin, end, [&](const RowPlace& p, int j, int lo, int hi) {
-    unit_kinds<D, BF16, EIGHT>(kv, kv8, r, p, j, lo, hi, part, kinds, parts, ring + (threadIdx.x >> 5) * (DEPTH * PER * 2 * 32), gains);
+  if (c * ROWS >= r.n_rows) return;
+  const int part = static_cast<int>(task % parts), begin = static_cast<int>(c) * ROWS, end = min(begin + ROWS, r.n_rows);
+  const Pair pair{warp & 1, 1 + warp / 2, amax[warp / 2]};
+  each_unit<ROWS>(r, begin, end, [&](const RowPlace& p, int j, int lo, int hi) {
+    unit_kinds<D, BF16, EIGHT>(kv, kv8, r, p, j, lo, hi, part, kinds, parts, ring + warp * (DEPTH * PER * 2 * 32), gains, pair);
   });
 }
 
@@ -593,15 +616,15 @@ template <int D, bool BF16, bool EIGHT>
 int append_units(const KvView& kv, const Kv8View& kv8, const NewRows& r, cudaStream_t s) {
   static bool set[MAX_DEVICES] = {};
   const int dev = current_device_slot();
-  constexpr int UNIT = unit_rows(EIGHT), smem = WARPS * DEPTH * UNIT * D * 2;
+  constexpr int ROWS = EIGHT ? PAGE_TOKENS : UNIT, AT_ONCE = EIGHT ? UNIT_WARPS / 2 : UNIT_WARPS, smem = UNIT_WARPS * DEPTH * UNIT * D * 2;
   if (!set[dev]) {
     if (cudaFuncSetAttribute(append_units_kernel<D, BF16, EIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
     set[dev] = true;
   }
-  const int kinds = (r.q ? r.n_q_heads : 0) + 2 * (EIGHT ? kv8.n_kv_heads : kv.n_kv_heads), parts = std::min(kinds, WARPS);
-  const int64_t blocks = ((static_cast<int64_t>(r.n_rows) + UNIT - 1) / UNIT * parts + WARPS - 1) / WARPS;
+  const int kinds = (r.q ? r.n_q_heads : 0) + 2 * (EIGHT ? kv8.n_kv_heads : kv.n_kv_heads), parts = std::min(kinds, PARTS);
+  const int64_t blocks = ((static_cast<int64_t>(r.n_rows) + ROWS - 1) / ROWS * parts + AT_ONCE - 1) / AT_ONCE;
   if (blocks > INT32_MAX) return -2;
-  return launch_pdl(append_units_kernel<D, BF16, EIGHT>, dim3(static_cast<unsigned>(blocks)), dim3(THREADS), smem, s, kv, kv8, r, kinds, parts) == cudaSuccess ? 0 : -1;
+  return launch_pdl(append_units_kernel<D, BF16, EIGHT>, dim3(static_cast<unsigned>(blocks)), dim3(UNIT_WARPS * 32), smem, s, kv, kv8, r, kinds, parts) == cudaSuccess ? 0 : -1;
 }
 
 template <int D, bool BF16>
