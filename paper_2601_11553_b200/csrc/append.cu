@@ -22,11 +22,47 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   return y;
 }
 
-// The prompt that owns a row: the last one whose row_start is not above it (-1 or n_seqs: none).  A whole warp asks for 128 entries at
-// a time, so that up to 127 prompts cost one round trip.
-__device__ __forceinline__ int owner_of(const int32_t* row_start, int n_seqs, int row) {
+struct RowPlace { int seq, first, n, ctx; };      // a prompt, its first row, its new rows, its slots in use
+__device__ __forceinline__ RowPlace place_from(const NewRows& r, int seq, int first, int last, int ctx) {
+  RowPlace p;
+  p.seq = seq;
+  p.first = min(max(first, 0), r.n_rows);
+  p.n = min(min(max(last, p.first), r.n_rows) - p.first, r.max_len);
+  p.ctx = min(max(ctx, 0), r.max_len - p.n);
+  return p;
+}
+__device__ __forceinline__ RowPlace place_of(const NewRows& r, int seq) {
+  if (seq < 0 || seq >= r.n_seqs) return RowPlace{seq, 0, 0, 0};
+  return place_from(r, seq, ld_dep_s32(r.row_start + seq), ld_dep_s32(r.row_start + seq + 1), ld_dep_s32(r.ctx_len + seq));
+}
+// The prompt that owns a row: the last one whose row_start is not above it (seq -1 or n_seqs: none).  A whole warp asks for 128 entries at
+// a time: up to 127 prompts cost one round trip, which brings their slots in use along.
+__device__ __forceinline__ RowPlace owner_of(const NewRows& r, int row) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, n = n_seqs + 1;                     // candidates [lo, lo + n)
+  if (r.n_seqs < 128) {
+    int start[4], ctx[4], below = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int at = u * 32 + lane;
+      start[u] = at <= r.n_seqs ? ld_dep_s32(r.row_start + at) : INT32_MAX;
+      ctx[u] = at < r.n_seqs ? ld_dep_s32(r.ctx_len + at) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) below += __popc(__ballot_sync(0xffffffffu, start[u] <= row));
+    auto pick = [&](const int (&x)[4], int i) {
+      int y = __shfl_sync(0xffffffffu, x[0], i & 31);
+#pragma unroll
+      for (int u = 1; u < 4; ++u) {
+        const int z = __shfl_sync(0xffffffffu, x[u], i & 31);
+        if (i >> 5 == u) y = z;
+      }
+      return y;
+    };
+    const int seq = below - 1;
+    if (seq < 0 || seq >= r.n_seqs) return RowPlace{seq, 0, 0, 0};
+    return place_from(r, seq, pick(start, seq), pick(start, seq + 1), pick(ctx, seq));
+  }
+  int lo = 0, n = r.n_seqs + 1;                   // candidates [lo, lo + n)
 #pragma unroll 1
   for (;;) {
     const int step = (n + 127) >> 7;
@@ -34,24 +70,14 @@ __device__ __forceinline__ int owner_of(const int32_t* row_start, int n_seqs, in
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int at = (u * 32 + lane) * step;
-      const bool in = at < n && ld_dep_s32(row_start + lo + at) <= row;
+      const bool in = at < n && ld_dep_s32(r.row_start + lo + at) <= row;
       below += __popc(__ballot_sync(0xffffffffu, in));
     }
-    if (below == 0) return lo - 1;                // only at the top
+    if (below == 0) return place_of(r, lo - 1);   // only at the top
     lo += (below - 1) * step;
     n = min(step, n - (below - 1) * step);
-    if (step == 1) return lo;
+    if (step == 1) return place_of(r, lo);
   }
-}
-struct RowPlace { int seq, first, n, ctx; };      // a prompt, its first row, its new rows, its slots in use
-__device__ __forceinline__ RowPlace place_of(const NewRows& r, int seq) {
-  RowPlace p{seq, 0, 0, 0};
-  if (seq < 0 || seq >= r.n_seqs) return p;
-  const int first = ld_dep_s32(r.row_start + seq), last = ld_dep_s32(r.row_start + seq + 1), ctx = ld_dep_s32(r.ctx_len + seq);
-  p.first = min(max(first, 0), r.n_rows);
-  p.n = min(min(max(last, p.first), r.n_rows) - p.first, r.max_len);
-  p.ctx = min(max(ctx, 0), r.max_len - p.n);
-  return p;
 }
 
 // Two floats, for the packed instructions.
@@ -126,18 +152,20 @@ __device__ __forceinline__ uint4 pack4(const Two (&x)[4]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// 1 / sqrt(mean x^2 + eps) of the row; the whole warp calls.
-template <int D>
-__device__ __forceinline__ float norm_factor(const Part& x, float eps) {
-  Two a = x.lo[0] * x.lo[0], b = x.hi[0] * x.hi[0];
+// 1 / sqrt(mean x^2 + eps) of the row, which LANES lanes have; the whole warp calls.
+template <int LANES, int D, int N>
+__device__ __forceinline__ float norm_factor(const Part (&x)[N], float eps) {
+  Two a = x[0].lo[0] * x[0].lo[0], b = x[0].hi[0] * x[0].hi[0];
 #pragma unroll
-  for (int e = 1; e < 4; ++e) { a = fma2(x.lo[e], x.lo[e], a); b = fma2(x.hi[e], x.hi[e], b); }
+  for (int e = 1; e < 4 * N; ++e) { a = fma2(x[e / 4].lo[e % 4], x[e / 4].lo[e % 4], a); b = fma2(x[e / 4].hi[e % 4], x[e / 4].hi[e % 4], b); }
   const float2 fa = floats(a), fb = floats(b);
   float sum = (fa.x + fa.y) + (fb.x + fb.y);
 #pragma unroll
-  for (int o = D / 32; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  for (int o = LANES / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   return rsqrtf(fmaf(sum, 1.0f / D, eps));
 }
+template <int D>
+__device__ __forceinline__ float norm_factor(const Part& x, float eps) { return norm_factor<D / 16, D, 1>(reinterpret_cast<const Part(&)[1]>(x), eps); }
 // x times f and the gain, of which load(q) gives the lane's q-th four.
 template <typename Load>
 __device__ __forceinline__ void scale_by(Part& x, float f, Load load) {
@@ -153,10 +181,8 @@ __device__ __forceinline__ void scale_by(Part& x, float f, Load load) {
 template <int D>
 __device__ __forceinline__ float4 gain_part(const float* gain, int l, int q) { return ld_dep_f32x4(gain + (q >> 1) * (D / 2) + l * 8 + (q & 1) * 4); }
 struct Turn { Two c[4], s[4]; };
-template <int D>
-__device__ __forceinline__ Turn turn_of(const float* rope, int position, int l) {
+__device__ __forceinline__ Turn turn_at(const float* p) {         // eight pairs
   Turn t;
-  const float* p = rope + (static_cast<size_t>(position) * (D / 2) + l * 8) * 2;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float4 v = ld_dep_f32x4(p + e * 4);
@@ -165,6 +191,8 @@ __device__ __forceinline__ Turn turn_of(const float* rope, int position, int l) 
   }
   return t;
 }
+template <int D>
+__device__ __forceinline__ Turn turn_of(const float* rope, int position, int l) { return turn_at(rope + (static_cast<size_t>(position) * (D / 2) + l * 8) * 2); }
 __device__ __forceinline__ void rotate(Part& x, const Turn& t) {
   const Two minus = two(-1.f, -1.f);
 #pragma unroll
@@ -201,7 +229,7 @@ __device__ __forceinline__ void row_heads(const KvView& kv, const NewRows& r, in
       hi[u] = ld_dep_v4(src + D / 2 + l * 8);
     }
   }
-  const RowPlace p = place_of(r, owner_of(r.row_start, r.n_seqs, row));
+  const RowPlace p = owner_of(r, row);
   if (row - p.first >= p.n) return;                // no prompt's row
   const int slot = p.ctx + row - p.first;
   Turn t;
@@ -235,7 +263,7 @@ __device__ __forceinline__ void row_heads(const KvView& kv, const NewRows& r, in
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(THREADS, 3) append_rows_kernel(const __grid_constant__ KvView kv, const __grid_constant__ NewRows r, int heads, int run) {
+__global__ void __launch_bounds__(THREADS, 2) append_rows_kernel(const __grid_constant__ KvView kv, const __grid_constant__ NewRows r, int heads, int run) {
   pdl_launch_dependents();
   pdl_wait();
   const int runs = (heads + run - 1) / run;
@@ -310,7 +338,7 @@ __device__ __forceinline__ void round_again(uint8_t* to, const PageScale& ps) {
 // the last new slot in it).
 template <int UNIT, typename Fn>
 __device__ __forceinline__ void each_unit(const NewRows& r, int begin, int end, Fn fn) {
-  RowPlace p = place_of(r, owner_of(r.row_start, r.n_seqs, begin));
+  RowPlace p = owner_of(r, begin);
   if (p.seq < 0) p = place_of(r, 0);               // rows ahead of the first prompt's
   int row = begin;
 #pragma unroll 1
@@ -423,8 +451,9 @@ __global__ void __launch_bounds__(THREADS, 2) append_pages_kernel(const __grid_c
 // own shared memory: a lane copies what it reads itself, so that nothing is waited for but its own copies, and the look-ups are shared by
 // 16 rows.  (With a row a warp and loads into registers, a warp's time went into look-ups: 33024 rows 113 us.)
 constexpr int DEPTH = 3;                          // heads on their way
-// Four warps a block, five blocks an SM: 96 registers.  (With 80 a few were kept in memory, and to fetch one took as long as the copies ahead of it.)
-constexpr int UNIT_WARPS = 4, UNIT_BLOCKS = 5, PARTS = 4;
+// Four warps a block, four blocks an SM, so that nothing is kept in memory for want of registers (to fetch it takes as long as the copies ahead
+// of it: 8 prompts into 8-bit pages with 4 / 5 / 6 blocks 44.8 / 47.2 / 57.0 us).
+constexpr int UNIT_WARPS = 4, UNIT_BLOCKS = 4, PARTS = 4;
 __device__ __forceinline__ void copy_async_16(void* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
 }
@@ -439,64 +468,50 @@ struct Pair {                    // of warps
   int half, barrier;             // which half of the page is this warp's; a hardware barrier of the two
   float (*amax)[2];              // [turn & 1][half] in shared memory
 };
+// Four lanes have a row: lane l the chunks of eight elements l, l + 4, .. of the lower half and of the upper one.
 template <int D, bool BF16, bool EIGHT>
 __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8, const NewRows& r, const RowPlace& p, int j, int lo, int hi, int first_kind, int kinds,
                                            int step, uint4* mine, const float* gains, const Pair& pair) {
-  constexpr int LANES = D / 16, GROUPS = 32 / LANES, PER = UNIT / GROUPS;
-  const int lane = threadIdx.x & 31, l = lane % LANES, g = lane / LANES;
+  constexpr int LANES = 32 / UNIT, CHUNKS = D / 16 / LANES;
+  const int lane = threadIdx.x & 31, l = lane % LANES, s = lane / LANES;     // s: the lane's slot of the unit
   using E = unsigned short;
   const int hq = r.q ? r.n_q_heads : 0, hkv = EIGHT ? kv8.n_kv_heads : kv.n_kv_heads;
   // this warp's slots: from slot0 on, [lo, hi) of them new (in a page, those below lo are in use)
   const bool in_use = lo > 0;
   const int slot0 = EIGHT ? j * PAGE_TOKENS + pair.half * UNIT : j * UNIT;
   if constexpr (EIGHT) {
-    lo = min(max(lo - pair.half * UNIT, 0), UNIT);
-    hi = min(max(hi - pair.half * UNIT, 0), UNIT);
+    lo -= pair.half * UNIT;
+    hi -= pair.half * UNIT;
   }
-  const int64_t row0 = p.first + slot0 - p.ctx;          // of the first slot
+  const bool is_new = s >= lo && s < hi;
+  const int64_t row = p.first + slot0 + s - p.ctx;
   // kinds: queries' heads, keys' heads, values' heads
   auto fetch = [&](int kind, int n) {
-    if (kind < kinds) {
+    if (kind < kinds && is_new) {
       const bool is_q = kind < hq, is_k = !is_q && kind < hq + hkv;
-      const E* src = is_q ? static_cast<const E*>(r.q) + kind * D : is_k ? static_cast<const E*>(r.k) + (kind - hq) * D : static_cast<const E*>(r.v) + (kind - hq - hkv) * D;
-      const int64_t stride = is_q ? r.q_stride : is_k ? r.k_stride : r.v_stride;
-      uint4* to = mine + (n % DEPTH) * (PER * 2 * 32) + lane;
-      const E* row = src + (row0 + g) * stride + l * 8;
+      const E* src = (is_q ? static_cast<const E*>(r.q) + row * r.q_stride + kind * D
+                      : is_k ? static_cast<const E*>(r.k) + row * r.k_stride + (kind - hq) * D
+                             : static_cast<const E*>(r.v) + row * r.v_stride + (kind - hq - hkv) * D) + l * 8;
+      uint4* to = mine + (n % DEPTH) * (CHUNKS * 2 * 32) + lane;
 #pragma unroll
-      for (int u = 0; u < PER; ++u, row += GROUPS * stride) {
-        const int s = g + GROUPS * u;
-        if (s >= lo && s < hi) {
-          copy_async_16(to + (2 * u) * 32, row);
-          copy_async_16(to + (2 * u + 1) * 32, row + D / 2);
-        }
-      }
+      for (int c = 0; c < 2 * CHUNKS; ++c) copy_async_16(to + c * 32, src + c * (LANES * 8));
     }
     copies_commit();                                               // a group per step, empty ones too
   };
 #pragma unroll
   for (int n = 0; n < DEPTH - 1; ++n) fetch(first_kind + n * step, n);
   // where they go
-  int64_t at[PER];                                                 // 16 bits: row of the pools, or -1
+  int64_t at = -1;                                                 // 16 bits: row of the pools
   int page = 0;
-  bool there = true;
-  if constexpr (EIGHT) {
-    page = ld_dep_s32(kv8.page_table + static_cast<size_t>(p.seq) * kv8.pt_stride + j);
-    there = static_cast<uint32_t>(page) < static_cast<uint64_t>(kv8.n_pages);
-  } else {
+  if constexpr (EIGHT) page = ld_dep_s32(kv8.page_table + static_cast<size_t>(p.seq) * kv8.pt_stride + j);
+  else if (is_new) at = slot_row(kv.page_table, kv.pt_stride, kv.ctx_start, kv.n_slots, p.seq, slot0 + s);
+  Turn turn[CHUNKS] = {};                                          // the row's cosines and sines, for all kinds
+  if (r.rope && is_new) {
+    const float* rope = r.rope + static_cast<size_t>(position_of(r, static_cast<int>(row), slot0 + s)) * D;
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int s = g + GROUPS * u;
-      at[u] = s >= lo && s < hi ? slot_row(kv.page_table, kv.pt_stride, kv.ctx_start, kv.n_slots, p.seq, slot0 + s) : -1;
-    }
+    for (int c = 0; c < CHUNKS; ++c) turn[c] = turn_at(rope + (l + c * LANES) * 16);
   }
-  Turn turn[PER] = {};                                              // the rows' cosines and sines, for all kinds
-  if (r.rope) {
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int s = g + GROUPS * u;
-      if (s >= lo && s < hi) turn[u] = turn_of<D>(r.rope, position_of(r, static_cast<int>(row0) + s, slot0 + s), l);
-    }
-  }
+  const bool there = static_cast<uint32_t>(page) < static_cast<uint64_t>(kv8.n_pages);
   int n = 0;
 #pragma unroll 1
   for (int kind = first_kind; kind < kinds; kind += step, ++n) {
@@ -504,56 +519,51 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
     copies_wait<DEPTH - 1>();
     const bool is_q = kind < hq, is_k = !is_q && kind < hq + hkv;
     const float* gain = is_q ? (r.q_gain ? gains : nullptr) : is_k && r.k_gain ? gains + D : nullptr;
-    const uint4* from = mine + (n % DEPTH) * (PER * 2 * 32) + lane;
-    // A row's values, normalised and turned.  Rows that are not new are worked on too (whatever is there), so that lanes keep together;
-    // nothing of them is stored.
-    auto values = [&](int u) {
-      Part x = unpack<BF16>(from[(2 * u) * 32], from[(2 * u + 1) * 32]);
-      if (gain) scale_by(x, norm_factor<D>(x, r.eps), [&](int q) { return *reinterpret_cast<const float4*>(gain + (q * LANES + l) * 4); });
-      if (r.rope && (is_q || is_k)) rotate(x, turn[u]);
-      return x;
-    };
-    if (!EIGHT || is_q) {
-      const int64_t stride = is_q ? r.q_out_stride : 0;
-      E* q_row = is_q ? static_cast<E*>(r.q_out) + (row0 + g) * stride + kind * D + l * 8 : nullptr;
+    const uint4* from = mine + (n % DEPTH) * (CHUNKS * 2 * 32) + lane;
+    uint4 raw[2 * CHUNKS];                                         // lower half's chunks, upper half's chunks
 #pragma unroll
-      for (int u = 0; u < PER; ++u, q_row += GROUPS * stride) {
-        const int s = g + GROUPS * u;
-        uint4 a, b;
-        if (is_q || is_k) {
-          const Part x = values(u);
-          a = pack4<BF16>(x.lo);
-          b = pack4<BF16>(x.hi);
-        } else {
-          a = from[(2 * u) * 32];
-          b = from[(2 * u + 1) * 32];
-        }
-        E* dst = q_row;
-        bool put = s >= lo && s < hi;
-        if constexpr (!EIGHT) {
-          if (!is_q) {
-            put = at[u] >= 0;
-            dst = (is_k ? static_cast<E*>(const_cast<void*>(kv.k)) + at[u] * kv.k_stride + (kind - hq) * D
-                        : static_cast<E*>(const_cast<void*>(kv.v)) + at[u] * kv.v_stride + (kind - hq - hkv) * D) + l * 8;
-          }
-        }
-        if (put) {
-          *reinterpret_cast<uint4*>(dst) = a;
-          *reinterpret_cast<uint4*>(dst + D / 2) = b;
-        }
+    for (int c = 0; c < 2 * CHUNKS; ++c) raw[c] = from[c * 32];
+    // Rows that are not new are worked on too (whatever is there), so that lanes keep together; nothing of them is stored.
+    Part x[CHUNKS];
+    if (EIGHT || is_q || is_k) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) x[c] = unpack<BF16>(raw[c], raw[CHUNKS + c]);
+      if (gain) {
+        const float f = norm_factor<LANES, D>(x, r.eps);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) scale_by(x[c], f, [&](int q) { return *reinterpret_cast<const float4*>(gain + ((c * 4 + q) * LANES + l) * 4); });
+      }
+      if (r.rope && (is_q || is_k)) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) rotate(x[c], turn[c]);
+      }
+    }
+    if (!EIGHT || is_q) {
+      if (is_q || is_k) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) { raw[c] = pack4<BF16>(x[c].lo); raw[CHUNKS + c] = pack4<BF16>(x[c].hi); }
+      }
+      bool put = is_new;
+      E* dst;
+      if (EIGHT || is_q) {
+        dst = static_cast<E*>(r.q_out) + row * r.q_out_stride + kind * D;
+      } else {
+        put = at >= 0;
+        dst = is_k ? static_cast<E*>(const_cast<void*>(kv.k)) + at * kv.k_stride + (kind - hq) * D
+                   : static_cast<E*>(const_cast<void*>(kv.v)) + at * kv.v_stride + (kind - hq - hkv) * D;
+      }
+      if (put) {
+#pragma unroll
+        for (int c = 0; c < 2 * CHUNKS; ++c) *reinterpret_cast<uint4*>(dst + l * 8 + c * (LANES * 8)) = raw[c];
       }
     } else if constexpr (EIGHT) {
       const int page_kind = (is_k ? kind - hq : kind - hq - hkv) * 2 + (is_k ? 0 : 1);
       float* scale_at = const_cast<float*>(kv8.scales) + static_cast<size_t>(there ? page : 0) * kv8.n_kv_heads * 2 + page_kind;
       const float before = in_use && there ? ld_dep_f32(scale_at) : 0.f;
-      Part x[PER];
       float amax = 0.f;
 #pragma unroll
-      for (int u = 0; u < PER; ++u) {
-        x[u] = values(u);
-        const int s = g + GROUPS * u;
-        amax = fmaxf(amax, s >= lo && s < hi ? largest(x[u]) : 0.f);
-      }
+      for (int c = 0; c < CHUNKS; ++c) amax = fmaxf(amax, largest(x[c]));
+      if (!is_new) amax = 0.f;
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
       if (lane == 0) pair.amax[n & 1][pair.half] = amax;
@@ -561,12 +571,11 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
       const PageScale ps = page_scale(in_use, before, fmaxf(amax, pair.amax[n & 1][pair.half ^ 1]));
       if (there) {
         if (lane == 0 && pair.half == 0) *scale_at = ps.scale;
-        uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(page_kind) * (PAGE_TOKENS * D) + pair.half * (UNIT * D) + l * 8;
+        uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(page_kind) * (PAGE_TOKENS * D) + (pair.half * UNIT + s) * D + l * 8;
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-          const int s = g + GROUPS * u;
-          if (s >= lo && s < hi) store_row<D>(dst + s * D, x[u], ps.inv);
-          else if (s < lo) round_again<D>(dst + s * D, ps);
+        for (int c = 0; c < CHUNKS; ++c) {
+          if (is_new) store_row<D>(dst + c * (LANES * 8), x[c], ps.inv);
+          else if (s < lo) round_again<D>(dst + c * (LANES * 8), ps);
         }
       }
     }
@@ -577,7 +586,7 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
 
 template <int D, bool BF16, bool EIGHT>
 __global__ void __launch_bounds__(UNIT_WARPS * 32, UNIT_BLOCKS) append_units_kernel(const __grid_constant__ KvView kv, const __grid_constant__ Kv8View kv8, const __grid_constant__ NewRows r, int kinds, int parts) {
-  constexpr int LANES = D / 16, GROUPS = 32 / LANES, PER = UNIT / GROUPS, ROWS = EIGHT ? PAGE_TOKENS : UNIT, SHARE = EIGHT ? 2 : 1;
+  constexpr int LANES = 32 / UNIT, CHUNKS = D / 16 / LANES, ROWS = EIGHT ? PAGE_TOKENS : UNIT, SHARE = EIGHT ? 2 : 1;
   extern __shared__ uint4 ring[];
   __shared__ __align__(16) float gains[2 * D];
   __shared__ float amax[UNIT_WARPS / 2][2][2];
@@ -587,9 +596,9 @@ __global__ void __launch_bounds__(UNIT_WARPS * 32, UNIT_BLOCKS) append_units_ker
   for (int which = 0; which < 2; ++which) {
     const float* gain = which ? r.k_gain : r.q_gain;
     const int e = threadIdx.x;
-    // a lane's sixteen in four parts, the lanes' parts one behind the other (no bank is asked twice)
-    const int half = e / (D / 2), in = e % (D / 2), part = half * 2 + (in % 8) / 4;
-    if (gain && e < D) gains[which * D + (part * LANES + in / 8) * 4 + in % 4] = ld_dep_f32(gain + e);
+    // a chunk's sixteen (eight of either half) in four parts, the lanes' parts one behind the other: no bank is asked twice
+    const int half = e / (D / 2), in = e % (D / 2), chunk = in / 8, part = half * 2 + (in % 8) / 4;
+    if (gain && e < D) gains[which * D + (((chunk / LANES) * 4 + part) * LANES + chunk % LANES) * 4 + in % 4] = ld_dep_f32(gain + e);
   }
   __syncthreads();
   const int warp = threadIdx.x >> 5;
@@ -599,7 +608,7 @@ __global__ void __launch_bounds__(UNIT_WARPS * 32, UNIT_BLOCKS) append_units_ker
   const int part = static_cast<int>(task % parts), begin = static_cast<int>(c) * ROWS, end = min(begin + ROWS, r.n_rows);
   const Pair pair{warp & 1, 1 + warp / 2, amax[warp / 2]};
   each_unit<ROWS>(r, begin, end, [&](const RowPlace& p, int j, int lo, int hi) {
-    unit_kinds<D, BF16, EIGHT>(kv, kv8, r, p, j, lo, hi, part, kinds, parts, ring + warp * (DEPTH * PER * 2 * 32), gains, pair);
+    unit_kinds<D, BF16, EIGHT>(kv, kv8, r, p, j, lo, hi, part, kinds, parts, ring + warp * (DEPTH * CHUNKS * 2 * 32), gains, pair);
   });
 }
 
