@@ -6,8 +6,8 @@
 // the weights P = 2^x' s_V are split into sums of e4m3 numbers, each some powers of two below the one before, with columns of their own.
 // Nothing is unpacked: shared memory sees every byte of the cache twice (copy in, MMA), where forming 16-bit tiles would take seven times.
 //   q: 2 parts (bf16, exact: 8 bits of mantissa are 4 + 4) or 3 (fp16), 2^4 apart, of q * 2^-e with the row's largest in (224, 448].
-//   P: 2 parts 2^4 apart and one 2^18 below (bf16), 3 parts and one 2^22 below (fp16), of the weight as a half: the largest of a row lies in
-//   2^11 .. 2^15.  The last part is for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
+//   P: 2 parts 2^4 apart (bf16) or 3 (fp16) and one 2^22 below the first, of the weight as a half: the largest of a row lies in
+//   2^7 .. 2^15.  The last part is for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
 // The accumulation is fp32's (measured: off by at most 2^-21 of the sum of magnitudes).
 //
 // Bound by HBM: 2 D bytes a slot and KV head.  One copy per page fetches keys and values of a head: a box of [row group][K, V][8 rows][D
@@ -29,7 +29,7 @@ constexpr int CLEAN_BARS = 8;                   // more than the tiles between a
 constexpr int FLAGS = 8;                        // items a `bad V` flag lives for: more than the roles can be apart
 constexpr int MASK_WORDS = 4;                   // 256 nodes
 // The running reference lies HEADROOM (base 2) below the largest score that set it and is raised when a score exceeds that by RESCALE_THRESHOLD.
-constexpr float HEADROOM = 11.f, RESCALE_THRESHOLD = 4.f;
+constexpr float HEADROOM = 7.f, RESCALE_THRESHOLD = 8.f;
 constexpr int P_UNIT = 7;                       // the first part of P counts 2^7: at most 2^8, below 448
 constexpr int MIN_SPAN = 2;
 constexpr int WHOLE_BLOCKS = 6;
@@ -48,6 +48,7 @@ struct Tree8Params {
   Kv8View kv;
   TreeRows rows;
   int32_t n_q_heads, group, small, over, whole, heads_a_page;
+  uint32_t group_inverse;        // 2^32 / group, rounded up; 0: group is 1
   float scale_log2;
   const void* q;
   int64_t q_stride;
@@ -70,7 +71,7 @@ template <int NC, bool BF16> struct Parts {
   static constexpr int USED = 2 * NS + 2 * O_ITEMS * NO;
   static constexpr int TMEM = USED <= 256 ? 256 : 512;
   static_assert(USED <= 512 && NS % 16 == 0 && NO % 16 == 0 && NO <= P_ROW, "");
-  __host__ __device__ static constexpr int shift(int part) { return BF16 ? (part == 0 ? 0 : part == 1 ? 4 : 18) : (part < 3 ? 4 * part : 22); }
+  __host__ __device__ static constexpr int shift(int part) { return BF16 ? (part == 0 ? 0 : part == 1 ? 4 : 22) : (part < 3 ? 4 * part : 22); }
 };
 __host__ __device__ constexpr float pow2(int e) { return e >= 0 ? static_cast<float>(1u << e) : 1.0f / static_cast<float>(1u << -e); }
 
@@ -115,6 +116,8 @@ __device__ __forceinline__ Shape shape8(const Tree8Params& a, const SeqPart& p) 
   const int units = (p.n_nodes * a.group + NC - 1) / NC * a.kv.n_kv_heads, n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK;
   return a.whole ? Shape{units, 1, n_blk, a.over} : Shape{units, n_blk, 1, a.over};
 }
+// Row / group: exact below 2^32 / group.
+__device__ __forceinline__ int node_of(const Tree8Params& a, int flat) { return a.group_inverse ? static_cast<int>(__umulhi(static_cast<uint32_t>(flat), a.group_inverse)) : flat; }
 struct Item {
   int seq, ctx_len, n_nodes, row0;   // the prompt: its context slots, nodes, first row
   int flat0, n_rows;                 // the tile: rows flat0 .. flat0 + n_rows - 1 of the KV head's node x head rows
@@ -200,6 +203,62 @@ __device__ __forceinline__ int swizzled(int n, int b) {
   return off ^ (W == 128 ? ((off >> 7) & 7) << 4 : ((off >> 7) & 3) << 4);
 }
 
+// Rows c0, c0 + step, .. (a warp takes 512 / D of them at a time) of a tile's q as sums of e4m3 numbers, and what those count.  A lane has 16 elements of
+// a row.  Rows behind the last one, up to four or sixteen (what the softmax takes at a time), become zeros.
+template <int D, int NC, bool BF16>
+__device__ __noinline__ void split_q(const Tree8Params& a, int row0, int flat0, int n_rows, int g, uint8_t* q_smem, float* q_scale, int c0, int step) {
+  using X = Parts<NC, BF16>;
+  constexpr int LANES = D / 16;
+  const int lane = threadIdx.x & 31, l = lane % LANES;
+  const int last = n_rows & 15, n_zero = last == 0 ? n_rows : n_rows - last + (last <= 4 ? 4 : 16);
+#pragma unroll 2
+  for (; c0 < n_zero; c0 += step) {
+    const int c = c0 + lane / LANES;
+    uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (c < n_rows) {
+      const int flat = flat0 + c, node = node_of(a, flat);
+      const unsigned short* src = static_cast<const unsigned short*>(a.q) + (row0 + node) * a.q_stride + (g * a.group + flat - node * a.group) * D + l * 16;
+      raw[0] = ld_dep_v4(src);
+      raw[1] = ld_dep_v4(src + 8);
+    }
+    float x[16], amax = 0.f;
+    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint32_t bits = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+      if constexpr (BF16) x[e] = __uint_as_float(bits << 16);
+      else x[e] = __half2float(__ushort_as_half(static_cast<unsigned short>(bits)));
+      const float m = fabsf(x[e]);
+      if (m < INFINITY) amax = fmaxf(amax, m);
+      else x[e] = __uint_as_float(0x7fffffffu);                // infinity times anything ends as NaN
+    }
+#pragma unroll
+    for (int o = LANES / 2; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const uint32_t b = __float_as_uint(amax);
+    const int ex = min(max(static_cast<int>(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+    if (c < n_zero) {
+      if (l == 0) q_scale[c] = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) * a.scale_log2;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] *= down;
+#pragma unroll
+      for (int part = 0; part < X::Q; ++part) {
+        uint32_t out[4];
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const uint32_t lo = pack_e4m3x2(x[e], x[e + 1]), hi = pack_e4m3x2(x[e + 2], x[e + 3]);
+          out[e >> 2] = lo | hi << 16;
+          const float2 y = unpack_e4m3x2(lo), z = unpack_e4m3x2(hi);
+          x[e] = (x[e] - y.x) * 16.f; x[e + 1] = (x[e + 1] - y.y) * 16.f;
+          x[e + 2] = (x[e + 2] - z.x) * 16.f; x[e + 3] = (x[e + 3] - z.y) * 16.f;
+        }
+        *reinterpret_cast<uint4*>(q_smem + swizzled<D>(c * X::Q + part, l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
+      }
+    }
+  }
+  fence_proxy_async_smem();                                    // the MMA reads Q through the async proxy
+}
+
 template <int D, int NC, bool BF16>
 constexpr int smem8() { return 1024 + ring_bytes(NC) + 2 * Parts<NC, BF16>::NS * D + 2 * Parts<NC, BF16>::P_ROW * BLK; }
 
@@ -215,7 +274,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
   constexpr uint32_t TMEM_O = 2 * X::NS;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t q_full[2], q_empty[2], landed[STAGES], empty[STAGES], dirty[CLEAN_BARS], cleaned[CLEAN_BARS], s_full[2], s_free[2], p_full[2], p_free[2],
-      o_full[2], o_free[2], ml_full;
+      o_full[2], o_free[2], ml_full, q_first;
   __shared__ __align__(16) float4 page_scale[STAGES][PAGES];   // s_K, log2 s_V, 1 / s_V
   __shared__ __align__(16) float q_scale[2][NC];
   __shared__ __align__(16) float block_max[2][2][NC][4];       // [block parity][use][row][warp]
@@ -241,10 +300,10 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 1);
       mbar_init(&q_empty[i], 9);         // the MMAs and the eight softmax warps
-      mbar_init(&s_full[i], 1); mbar_init(&s_free[i], 4); mbar_init(&p_full[i], 4); mbar_init(&p_free[i], 1);
+      mbar_init(&s_full[i], 2); mbar_init(&s_free[i], 4); mbar_init(&p_full[i], 4); mbar_init(&p_free[i], 1);
       mbar_init(&o_full[i], 1); mbar_init(&o_free[i], 8);
     }
-    mbar_init(&ml_full, 8);
+    mbar_init(&ml_full, 8); mbar_init(&q_first, 8);
     fence_mbar_init();
   }
   if (warp == 9) {
@@ -323,65 +382,21 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     uint32_t n_q = 0, n_item = 0, n_tile = 0, n_clean = 0;
     bool ok = true;
     auto prepare_q = [&](const Item& it) {
-      const int qs = n_q & 1, node0 = it.flat0 / a.group;
+      const int qs = n_q & 1, node0 = node_of(a, it.flat0);
       int* flag = &bad_flag[n_q % FLAGS];                          // read at the end of its item, long before its next use
       if (lane == 0) *flag = 0;
       ok = __all_sync(0xffffffffu, bar_wait(&q_empty[qs], ((n_q >> 1) & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_CORR));
       if (!ok) return;
-      // rows behind the last one, up to four or sixteen (what the softmax takes at a time), are zeros
-      const int last = it.n_rows & 15, n_zero = last == 0 ? it.n_rows : it.n_rows - last + (last <= 4 ? 4 : 16);
-#pragma unroll 2
-      for (int c0 = 0; c0 < n_zero; c0 += 32 / LANES) {
-        const int c = c0 + lane / LANES, l = lane % LANES;
-        uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-        if (c < it.n_rows) {
-          const int flat = it.flat0 + c, node = flat / a.group;
-          const unsigned short* src = static_cast<const unsigned short*>(a.q) + (it.row0 + node) * a.q_stride + (it.g * a.group + flat - node * a.group) * D + l * 16;
-          raw[0] = ld_dep_v4(src);
-          raw[1] = ld_dep_v4(src + 8);
-        }
-        float x[16], amax = 0.f;
-        const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const uint32_t bits = (w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-          if constexpr (BF16) x[e] = __uint_as_float(bits << 16);
-          else x[e] = __half2float(__ushort_as_half(static_cast<unsigned short>(bits)));
-          const float m = fabsf(x[e]);
-          if (m < INFINITY) amax = fmaxf(amax, m);
-          else x[e] = __uint_as_float(0x7fffffffu);                // infinity times anything ends as NaN
-        }
-#pragma unroll
-        for (int o = LANES / 2; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        const uint32_t b = __float_as_uint(amax);
-        const int ex = min(max(static_cast<int>(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-        if (c < n_zero) {
-          if (l == 0) q_scale[qs][c] = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) * a.scale_log2;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] *= down;
-#pragma unroll
-          for (int part = 0; part < X::Q; ++part) {
-            uint32_t out[4];
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const uint32_t lo = pack_e4m3x2(x[e], x[e + 1]), hi = pack_e4m3x2(x[e + 2], x[e + 3]);
-              out[e >> 2] = lo | hi << 16;
-              const float2 y = unpack_e4m3x2(lo), z = unpack_e4m3x2(hi);
-              x[e] = (x[e] - y.x) * 16.f; x[e + 1] = (x[e + 1] - y.y) * 16.f;
-              x[e + 2] = (x[e + 2] - z.x) * 16.f; x[e + 3] = (x[e + 3] - z.y) * 16.f;
-            }
-            *reinterpret_cast<uint4*>(q_smem + qs * Q_BYTES + swizzled<D>(c * X::Q + part, l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
-          }
-        }
-      }
+      if (n_q > 0) split_q<D, NC, BF16>(a, it.row0, it.flat0, it.n_rows, it.g, q_smem + qs * Q_BYTES, q_scale[qs], 0, 512 / D);
       if (it.blk_end * BLK > it.ctx_len) {
-        const int nodes = (it.flat0 + it.n_rows - 1) / a.group - node0 + 1, words = (it.n_nodes + 63) / 64;
+        const int nodes = node_of(a, it.flat0 + it.n_rows - 1) - node0 + 1, words = (it.n_nodes + 63) / 64;
 #pragma unroll 1
         for (int e = lane; e < nodes * words; e += 32)
           node_mask[(qs * NC + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + node0 + e / words, node0 + e / words, e % words);
       }
-      fence_proxy_async_smem();                            // the MMA reads Q through the async proxy
+      // the first item's Q is the softmax warps' work, who have nothing else to do yet (by one warp: 32 rows 20000 clocks)
+      if (n_q == 0) ok = __all_sync(0xffffffffu, bar_wait(&q_first, 0, a.err_word, DEV_ERR_ATTN_CORR));
+      if (!ok) return;
       __syncwarp();
       if (elect_one()) mbar_arrive(&q_full[qs]);
       __syncwarp();
@@ -462,6 +477,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
             for (int kk = 0; kk < D / 32; ++kk)
               umma_ss_8bit(tmem + i * X::NS, k_desc + (kk * 32 >> 4), q_desc + (kk * 32 >> 4), idesc, kk != 0);
             umma_commit(&s_full[i]);
+            mbar_arrive(&s_full[i]);           // and what this warp has seen to arrive: the pages' scales
             if (j + 1 == nb) umma_commit(&q_empty[par]);
             if ((it.blk_begin + j + 1) * BLK > it.ctx_len) mbar_arrive(&dirty[n_dirty % CLEAN_BARS]);
           }
@@ -523,10 +539,15 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
       if (lane < NC) neg[lane] = lane < it.n_rows ? 0.f : -INFINITY;         // columns behind the last row get no weights
       __syncwarp();
+      if (n_item == 0) {
+        split_q<D, NC, BF16>(a, it.row0, it.flat0, it.n_rows, it.g, q_smem, q_scale[0], warp * (512 / D), 8 * (512 / D));
+        __syncwarp();
+        if (elect_one()) mbar_arrive(&q_first);
+        __syncwarp();
+      }
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&q_full[par], (n_item >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // scales, masks
       for (int j = i; j < nb; j += 2) {
         const uint32_t t = n_tile + j;
-        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&landed[t % STAGES], (t / STAGES) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
         float s[NC];                                       // scores in base 2, the page's log2 s_V added
         float inv_v = 0.f;
@@ -574,7 +595,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
             uint32_t seen = 0;
             if (node < it.n_nodes) {
               const uint64_t* w = node_mask + par * NC * MASK_WORDS + (node >> 6);
-              int at = 0, h = it.flat0 % a.group;
+              int at = 0, h = it.flat0 - node_of(a, it.flat0) * a.group;
 #pragma unroll 1
               for (int c = 0; c < it.n_rows; ++c) {
                 seen |= static_cast<uint32_t>((w[at] >> (node & 63)) & 1u) << c;
@@ -721,7 +742,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           f1 = nb > 1 ? fast_exp2(m1 - ref) : 0.f;
           float L = f0 * ((l0.x + l0.y) + (l0.z + l0.w));
           if (nb > 1) L = fmaf(f1, (l1.x + l1.y) + (l1.z + l1.w), L);
-          const int flat = it.flat0 + lane, node = flat / a.group, row = it.row0 + node;
+          const int flat = it.flat0 + lane, node = node_of(a, flat), row = it.row0 + node;
           bool any = it.ctx_len > 0;                       // does the row see a slot at all (not: are its scores all -inf)
           if (!any) any = sees_a_node(a.rows, row, node, it.n_nodes);
           if (whole) {
@@ -735,7 +756,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           }
         }
         __syncwarp();
-        int node = (it.flat0 + i * 4) / a.group, h = it.flat0 + i * 4 - node * a.group;
+        int node = node_of(a, it.flat0 + i * 4), h = it.flat0 + i * 4 - node * a.group;
 #pragma unroll 1
         for (int c0 = i * 4; c0 < it.n_rows; c0 += 8) {    // four rows at a time, the parities in turn
           float o0[4] = {0.f, 0.f, 0.f, 0.f}, o1[4] = {0.f, 0.f, 0.f, 0.f};
@@ -813,7 +834,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) merge_8bit_kernel(Tree8Param
   const volatile MergeRecord8* mr = a.merges + blockIdx.x;
   const int n_parts = mr->n_parts, n_rows = mr->n_rows;
   if (n_parts <= 1 || r >= n_rows) return;
-  const int flat = mr->flat0 + r, row = mr->row0 + flat / a.group, head = mr->head0 + flat % a.group;
+  const int flat = mr->flat0 + r, node = node_of(a, flat), row = mr->row0 + node, head = mr->head0 + flat - node * a.group;
   // part 0 is the record's CTA's last item, part s > 0 the first item of the s-th CTA behind it
   auto slot = [&](int s) { return static_cast<size_t>(2 * (blockIdx.x + s) + (s == 0 ? 1 : 0)) * BLK + r; };
   // four parts at a time, with a running reference: their sums and results are asked for together
@@ -879,6 +900,7 @@ int64_t set_sizes(Tree8Params& p, const TreeAttention8& t, int* columns) {
   p.kv = t.kv; p.rows = t.rows;
   p.n_q_heads = t.n_q_heads;
   p.group = t.n_q_heads / t.kv.n_kv_heads;
+  p.group_inverse = p.group == 1 ? 0u : static_cast<uint32_t>((UINT64_C(1) << 32) / p.group + ((UINT64_C(1) << 32) % p.group != 0));
   const int64_t rows = static_cast<int64_t>(t.rows.max_nodes) * p.group;
   *columns = rows <= 16 ? 16 : 32;
   p.over = 2;
