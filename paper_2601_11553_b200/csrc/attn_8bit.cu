@@ -63,7 +63,7 @@ struct Tree8Params {
 template <int V> using Const = std::integral_constant<int, V>;
 template <int NC, bool BF16> struct Parts {
   static constexpr int Q = BF16 ? 2 : 3, P = BF16 ? 3 : 4;
-  // Columns: of S, row c's parts are c * Q + part; of O, rows c and c + 1 (c even) have c * P + 2 * part and the one behind it
+  // Columns: rows c and c + 1 (c even) have c * Q + 2 * part and the one behind it of S, c * P + 2 * part and the one behind it of O
   static constexpr int NS = NC * Q, NO = NC * P;
   static constexpr int P_ROW = NO <= 64 ? 64 : 128;            // bytes of a slot's row of P in shared memory
   // O of (item parity, block parity); one item's at a time where tensor memory does not hold two
@@ -252,7 +252,7 @@ __device__ __noinline__ void split_q(const Tree8Params& a, int row0, int flat0, 
           x[e] = (x[e] - y.x) * 16.f; x[e + 1] = (x[e + 1] - y.y) * 16.f;
           x[e + 2] = (x[e + 2] - z.x) * 16.f; x[e + 3] = (x[e + 3] - z.y) * 16.f;
         }
-        *reinterpret_cast<uint4*>(q_smem + swizzled<D>(c * X::Q + part, l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
+        *reinterpret_cast<uint4*>(q_smem + swizzled<D>((c & ~1) * X::Q + part * 2 + (c & 1), l * 16)) = make_uint4(out[0], out[1], out[2], out[3]);
       }
     }
   }
@@ -459,7 +459,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     while (ok && next_item<NC>(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
       if (warp == 9) {
-        const uint32_t idesc = make_idesc_e4m3(BLK, (it.n_rows * X::Q + 15) & ~15, 0, 0);
+        const uint32_t idesc = make_idesc_e4m3(BLK, (((it.n_rows + 1) & ~1) * X::Q + 15) & ~15, 0, 0);
         const uint64_t q_desc = desc(smem_u32(q_smem + par * Q_BYTES), GROUP_BYTES);
         wait(&q_full[par], (n_item >> 1) & 1u);
 #pragma unroll 1
@@ -532,11 +532,11 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     while (next_item<NC>(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin, par = n_item & 1, ob = X::O_ITEMS == 2 ? par : 0;
       const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
-      float l[NC];                                         // sum over this thread's slots only
+      uint64_t l[NC / 2];                                  // two rows' sums over this thread's slots only
       float* neg = neg_ref[warp];                          // - reference: the same in all threads
       uint32_t unset = 0xffffffffu >> (32 - it.n_rows);    // rows that have seen nothing yet: reference 0, sum and O zero
 #pragma unroll
-      for (int c = 0; c < NC; ++c) l[c] = 0.f;
+      for (int c = 0; c < NC / 2; ++c) l[c] = 0u;
       if (lane < NC) neg[lane] = lane < it.n_rows ? 0.f : -INFINITY;         // columns behind the last row get no weights
       __syncwarp();
       if (n_item == 0) {
@@ -547,15 +547,15 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       }
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&q_full[par], (n_item >> 1) & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // scales, masks
       for (int j = i; j < nb; j += 2) {
-        const uint32_t t = n_tile + j;
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s_full[i], n_s & 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));
-        float s[NC];                                       // scores in base 2, the page's log2 s_V added
+        float t[NC];                                       // scores in base 2, the page's log2 s_V added, less the reference
         float inv_v = 0.f;
         bool raise = j == i;                               // does any row's block maximum pass what its reference allows
         if (ok) {
           tc_fence_after_sync();
-          const float4 sc = page_scale[t % STAGES][r / PAGE_TOKENS];
+          const float4 sc = page_scale[(n_tile + j) % STAGES][r / PAGE_TOKENS];
           inv_v = sc.z;
+          const uint64_t sc_k = pack_f32x2(sc.x, sc.x), sc_v = pack_f32x2(sc.y, sc.y), sixteenth = pack_f32x2(0.0625f, 0.0625f);
           // sixteen rows at a time, or four where there are no more: straight code, so that their latencies overlap
           auto scores = [&](auto rows, int c0) {
             constexpr int R = decltype(rows)::value;
@@ -564,14 +564,19 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
             tmem_wait_ld();
 #pragma unroll
             for (int c = 0; c < R; c += 4) {
-              const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0 + c]);
-              const float qf[4] = {q4.x, q4.y, q4.z, q4.w};
+              const float4 q4 = *reinterpret_cast<const float4*>(&q_scale[par][c0 + c]), n4 = *reinterpret_cast<const float4*>(neg + c0 + c);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float y = __uint_as_float(x[(c + e) * X::Q + X::Q - 1]);
+              for (int u = 0; u < 2; ++u) {
+                auto column = [&](int part) {
+                  const int at = (c + 2 * u) * X::Q + part * 2;
+                  return pack_f32x2(__uint_as_float(x[at]), __uint_as_float(x[at + 1]));
+                };
+                uint64_t y = column(X::Q - 1);
 #pragma unroll
-                for (int part = X::Q - 2; part >= 0; --part) y = fmaf(y, 0.0625f, __uint_as_float(x[(c + e) * X::Q + part]));
-                s[c0 + c + e] = fmaf(y, sc.x * qf[e], sc.y);
+                for (int part = X::Q - 2; part >= 0; --part) y = fma_f32x2(y, sixteenth, column(part));
+                const uint64_t by = mul_f32x2(sc_k, u ? pack_f32x2(q4.z, q4.w) : pack_f32x2(q4.x, q4.y));
+                const uint64_t plus = add_f32x2(sc_v, u ? pack_f32x2(n4.z, n4.w) : pack_f32x2(n4.x, n4.y));
+                unpack_f32x2(fma_f32x2(y, by, plus), t[c0 + c + 2 * u], t[c0 + c + 2 * u + 1]);
               }
             }
           };
@@ -581,7 +586,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
               scores(Const<16>{}, c0);
             } else {
 #pragma unroll
-              for (int c = c0; c < c0 + 16; ++c) s[c] = -INFINITY;
+              for (int c = c0; c < c0 + 16; ++c) t[c] = -INFINITY;
               if (it.n_rows > c0) scores(Const<4>{}, c0);
             }
           }
@@ -604,29 +609,26 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-              if (!((seen >> c) & 1u)) s[c] = -INFINITY;
+              if (!((seen >> c) & 1u)) t[c] = -INFINITY;
           }
           __syncwarp();
           if (j != i) {                                    // (the first block always sets the references)
             float top = -INFINITY;
 #pragma unroll
             for (int c0 = 0; c0 < NC; c0 += 16) {
-              auto most = [&](int c) {
-                const float4 n4 = *reinterpret_cast<const float4*>(neg + c);
-                top = fmax3(top, s[c] + n4.x, s[c + 1] + n4.y);
-                top = fmax3(top, s[c + 2] + n4.z, s[c + 3] + n4.w);
-              };
-              if (it.n_rows > c0) most(c0);
+              if (it.n_rows > c0) {
+                top = fmax3(top, t[c0], t[c0 + 1]);
+                top = fmax3(top, t[c0 + 2], t[c0 + 3]);
+              }
               if (it.n_rows > c0 + 4) {
-                most(c0 + 4);
-                most(c0 + 8);
-                most(c0 + 12);
+#pragma unroll
+                for (int c = 4; c < 16; c += 2) top = fmax3(top, t[c0 + c], t[c0 + c + 1]);
               }
             }
             raise = top > HEADROOM + RESCALE_THRESHOLD;
             if (unset != 0) {
 #pragma unroll
-              for (int c = 0; c < NC; ++c) raise |= ((unset >> c) & 1u) && s[c] > -INFINITY;
+              for (int c = 0; c < NC; ++c) raise |= ((unset >> c) & 1u) && t[c] > -INFINITY;
             }
           }
         }
@@ -636,18 +638,22 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           // out row c's new reference and every thread fetches it by shuffles.  Two buffers: between two uses of one lies the
           // other's barrier.
           float(*maxima)[4] = block_max[i][n_raise++ & 1];
-          const float mine = column_reduce<NC>(s, [](float x, float y) { return fmaxf(x, y); });
+          const float mine = column_reduce<NC>(t, [](float x, float y) { return fmaxf(x, y); });
           if (lane < NC) maxima[lane][quarter] = mine;
           parity_any(i, false);
           const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
-          const float now = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) - HEADROOM;             // the block's own reference
           const float old = lane < NC ? neg[lane] : 0.f;
+          const float over = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) - HEADROOM;             // the block's own reference, less the present one
           const bool fresh = (unset >> lane) & 1u;
-          const bool up = lane < it.n_rows && now > -INFINITY && (fresh || now + old > RESCALE_THRESHOLD);
-          const float alpha = !up ? 1.f : fresh ? 0.f : fast_exp2(-old - now);
-          if (up) neg[lane] = -now;
+          const bool up = lane < it.n_rows && over > -INFINITY && (fresh || over > RESCALE_THRESHOLD);
+          const float alpha = !up ? 1.f : fresh ? 0.f : fast_exp2(-over);
+          const float less = up ? over : 0.f;
+          __syncwarp();
+          if (up) neg[lane] = old - over;
           unset &= ~(__ballot_sync(0xffffffffu, up));
           __syncwarp();
+#pragma unroll
+          for (int c = 0; c < NC; ++c) t[c] -= __shfl_sync(0xffffffffu, less, c);
           if (j != i) {
             if (ok) ok = __all_sync(0xffffffffu, bar_wait(&p_free[i], (n_s & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));    // O is complete
             if (ok) {
@@ -669,13 +675,14 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
               }
               tmem_wait_st();
 #pragma unroll
-              for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, alpha, c);
+              for (int c = 0; c < NC; c += 2) l[c / 2] = mul_f32x2(l[c / 2], pack_f32x2(__shfl_sync(0xffffffffu, alpha, c), __shfl_sync(0xffffffffu, alpha, c + 1)));
             }
           }
         }
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&p_free[i], (n_s & 1u) ^ 1u, a.err_word, DEV_ERR_ATTN_SOFTMAX));     // the product before has read P
         ++n_s;
         if (ok) {
+          const uint64_t inv_v2 = pack_f32x2(inv_v, inv_v);
           auto weights = [&](auto rows, int c0) {          // of rows c0 ..: the slot's row of P, two rows' parts a half word
             constexpr int R = decltype(rows)::value, WORDS = (R * X::P + 15) / 16 * 4;
             uint32_t w[WORDS];
@@ -683,14 +690,12 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
             for (int e = 0; e < WORDS; ++e) w[e] = 0u;
 #pragma unroll
             for (int c = 0; c < R; c += 4) {
-              const float4 n4 = *reinterpret_cast<const float4*>(neg + c0 + c);
               uint32_t two[2][X::P];
 #pragma unroll
               for (int u = 0; u < 2; ++u) {
                 const int k = c0 + c + 2 * u;
-                const float w0 = fast_exp2(s[k] + (u ? n4.z : n4.x)), w1 = fast_exp2(s[k + 1] + (u ? n4.w : n4.y));
-                l[k] = fmaf(w0, inv_v, l[k]);              // the row sum has the weights without s_V, and before they are split
-                l[k + 1] = fmaf(w1, inv_v, l[k + 1]);
+                const float w0 = fast_exp2(t[k]), w1 = fast_exp2(t[k + 1]);
+                l[k / 2] = fma_f32x2(pack_f32x2(w0, w1), inv_v2, l[k / 2]);   // the row sum has the weights without s_V, and before they are split
                 split_weights<X>(w0, w1, two[u]);
               }
 #pragma unroll
@@ -717,7 +722,10 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       n_tile += nb;
       // ---- the piece's end: sums and references of both parities are exchanged; parity i writes rows i * 4 .. i * 4 + 3, i * 4 + 8 ...
       if (ok) {
-        const float sum = column_reduce<NC>(l, [](float x, float y) { return x + y; });
+        float ll[NC];
+#pragma unroll
+        for (int c = 0; c < NC; c += 2) unpack_f32x2(l[c / 2], ll[c], ll[c + 1]);
+        const float sum = column_reduce<NC>(ll, [](float x, float y) { return x + y; });
         if (lane < NC) fin_l[par][i][lane][quarter] = sum;
         const float mine = lane < NC ? -neg[lane] : 0.f;
         if (quarter == 0 && lane < NC) fin_m[par][i][lane] = ((unset >> lane) & 1u) || nb <= i ? -INFINITY : mine;
