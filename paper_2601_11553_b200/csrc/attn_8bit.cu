@@ -173,6 +173,13 @@ __device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
   for (int h = NC; h < 32; h <<= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, h));
   return x;
 }
+// The same, where the first four columns may be all that counts.
+template <int NC, typename Op>
+__device__ __forceinline__ float column_reduce(const float (&in)[NC], int n_rows, Op op) {
+  if (n_rows > 4) return column_reduce<NC>(in, op);
+  const float few[4] = {in[0], in[1], in[2], in[3]};
+  return column_reduce<4>(few, op);
+}
 // OR of a predicate over the 128 threads of a block parity.
 __device__ __forceinline__ bool parity_any(int i, bool x) {
   uint32_t y;
@@ -638,7 +645,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           // out row c's new reference and every thread fetches it by shuffles.  Two buffers: between two uses of one lies the
           // other's barrier.
           float(*maxima)[4] = block_max[i][n_raise++ & 1];
-          const float mine = column_reduce<NC>(t, [](float x, float y) { return fmaxf(x, y); });
+          const float mine = column_reduce<NC>(t, it.n_rows, [](float x, float y) { return fmaxf(x, y); });
           if (lane < NC) maxima[lane][quarter] = mine;
           parity_any(i, false);
           const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
@@ -725,7 +732,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         float ll[NC];
 #pragma unroll
         for (int c = 0; c < NC; c += 2) unpack_f32x2(l[c / 2], ll[c], ll[c + 1]);
-        const float sum = column_reduce<NC>(ll, [](float x, float y) { return x + y; });
+        const float sum = column_reduce<NC>(ll, it.n_rows, [](float x, float y) { return x + y; });
         if (lane < NC) fin_l[par][i][lane][quarter] = sum;
         const float mine = lane < NC ? -neg[lane] : 0.f;
         if (quarter == 0 && lane < NC) fin_m[par][i][lane] = ((unset >> lane) & 1u) || nb <= i ? -INFINITY : mine;
@@ -734,14 +741,11 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         __syncwarp();
         ok = __all_sync(0xffffffffu, bar_wait(&ml_full, par, a.err_word, DEV_ERR_ATTN_CORR));
       }
-      if (ok) ok = __all_sync(0xffffffffu, bar_wait(&o_full[ob], o_uses & 1u, a.err_word, DEV_ERR_ATTN_CORR));
+      const bool whole = it.blk_begin == 0 && it.blk_end == it.n_blk;
+      const size_t part0 = static_cast<size_t>(2 * blockIdx.x + (it.blk_begin == 0 ? 1 : 0)) * BLK;
+      float f0 = 0.f, f1 = 0.f;
       if (ok) {
-        tc_fence_after_sync();
-        const bool whole = it.blk_begin == 0 && it.blk_end == it.n_blk;
-        const size_t part0 = static_cast<size_t>(2 * blockIdx.x + (it.blk_begin == 0 ? 1 : 0)) * BLK;
-        const bool bad = *reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS]) != 0;
         // Lane c works out row c's two factors; the loop over rows then only scales and stores.
-        float f0 = 0.f, f1 = 0.f;
         if (lane < it.n_rows) {
           const float m0 = fin_m[par][0][lane], m1 = fin_m[par][1][lane];
           const float4 l0 = *reinterpret_cast<const float4*>(fin_l[par][0][lane]), l1 = *reinterpret_cast<const float4*>(fin_l[par][1][lane]);
@@ -763,6 +767,11 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
             *reinterpret_cast<float2*>(a.partial_ml + (part0 + lane) * 2) = make_float2(M, any ? L : -1.f);
           }
         }
+      }
+      if (ok) ok = __all_sync(0xffffffffu, bar_wait(&o_full[ob], o_uses & 1u, a.err_word, DEV_ERR_ATTN_CORR));
+      if (ok) {
+        tc_fence_after_sync();
+        const bool bad = *reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS]) != 0;
         __syncwarp();
         int node = node_of(a, it.flat0 + i * 4), h = it.flat0 + i * 4 - node * a.group;
 #pragma unroll 1
@@ -911,7 +920,9 @@ int64_t set_sizes(Tree8Params& p, const TreeAttention8& t, int* columns) {
   p.group_inverse = p.group == 1 ? 0u : static_cast<uint32_t>((UINT64_C(1) << 32) / p.group + ((UINT64_C(1) << 32) % p.group != 0));
   const int64_t rows = static_cast<int64_t>(t.rows.max_nodes) * p.group;
   *columns = rows <= 16 ? 16 : 32;
-  p.over = 2;
+  // A unit's own cost in blocks (its Q, its rows' end).  64 x 2500 slots with 1 / 2 / 3 / 4 / 6: 62.6 / 62.5 / 62.3 / 62.5 / 64.5 us; trees of 26 with
+  // 2 / 4 / 8 / 11: 148 / 137 / 136 / 135, chains of 7 on 2 x 33024 slots 41.4 / 39.5 / 37.4 / 37.7.  (Tiles of a prompt made equally large: no change.)
+  p.over = *columns == 16 ? 3 : 8;
   return (rows + *columns - 1) / *columns * t.kv.n_kv_heads;
 }
 
