@@ -28,7 +28,8 @@ enum Type { I32 = 1, F32 = 2, U8 = 4, BOOL = 8, I64 = 16, U64 = 32, BF16 = 64, F
 constexpr int N_TYPES = 9;
 PyObject* types[N_TYPES];                       // torch's type objects, in the order of Type
 PyObject* current_stream;                       // device -> torch's current stream there
-PyObject *n_dtype, *n_shape, *n_get_device, *n_stride, *n_is_contiguous, *n_data_ptr, *n_element_size;
+PyObject* to_dlpack;                            // tensor -> its DLPack capsule, or NULL
+PyObject *n_dtype, *n_shape, *n_get_device, *n_stride, *n_data_ptr, *n_element_size;
 
 struct Ref {                                    // owns a reference
   PyObject* p;
@@ -108,18 +109,86 @@ int strides_of(PyObject* x, int64_t (&out)[N]) {
   const Ref r(PyObject_CallMethodNoArgs(x, n_stride));
   return numbers(r.p, out);
 }
-bool contiguous(PyObject* x) {
-  const Ref r(PyObject_CallMethodNoArgs(x, n_is_contiguous));
-  if (!r.p) throw Error{};
-  return r.p == Py_True;
+// What a tensor is.  DLPack's description (a public, stable layout: the parts of it used here are restated) comes in one call where the tensor can be
+// asked for it (not one that requires a gradient, say); its Python attributes take five: a fork of one prompt to four samples, 17 tensors, is the
+// host's 13 us that way.
+constexpr int MOST = 8;                         // sizes
+struct Info {
+  int type, device, dims;                       // type 0: none of ours; device -1: the host
+  int64_t item;                                 // bytes of an element
+  int64_t shape[MOST], stride[MOST];
+  void* p;
+};
+struct DlTensor {
+  void* data;
+  struct { int32_t type, id; } device;
+  int32_t ndim;
+  struct { uint8_t code, bits; uint16_t lanes; } dtype;
+  int64_t *shape, *strides;
+  uint64_t byte_offset;
+};
+int dl_type(const DlTensor& t) {
+  if (t.dtype.lanes != 1) return 0;
+  switch (t.dtype.code << 8 | t.dtype.bits) {
+    case 0 << 8 | 32: return I32;
+    case 0 << 8 | 64: return I64;
+    case 1 << 8 | 8: return U8;
+    case 1 << 8 | 64: return U64;
+    case 2 << 8 | 32: return F32;
+    case 2 << 8 | 16: return F16;
+    case 4 << 8 | 16: return BF16;
+    case 6 << 8 | 8: return BOOL;
+    case 10 << 8 | 8: return F8;               // 4 exponent bits, 3 mantissa bits, no infinities
+    default: return 0;
+  }
+}
+bool described(PyObject* x, Info& out) {
+  if (!to_dlpack) return false;
+  const Ref capsule(PyObject_CallOneArg(to_dlpack, x));
+  const DlTensor* t = capsule.p && PyCapsule_IsValid(capsule.p, "dltensor") ? static_cast<DlTensor*>(PyCapsule_GetPointer(capsule.p, "dltensor")) : nullptr;
+  if (!t) {
+    PyErr_Clear();
+    return false;
+  }
+  out.type = dl_type(*t);
+  // 1: host, 2: CUDA; the types that are told apart here only (others ask the attribute)
+  if (out.type == 0 || t->ndim > MOST || (t->device.type != 1 && t->device.type != 2) || (!t->strides && t->ndim > 0)) return false;
+  out.device = t->device.type == 2 ? t->device.id : -1;
+  out.dims = t->ndim;
+  out.item = t->dtype.bits / 8;
+  for (int i = 0; i < t->ndim; ++i) { out.shape[i] = t->shape[i]; out.stride[i] = t->strides[i]; }
+  out.p = static_cast<char*>(t->data) + t->byte_offset;
+  return true;
+}
+Info look(PyObject* x) {
+  Info t = {};
+  if (described(x, t)) return t;
+  t.type = type_of(x);
+  t.device = static_cast<int>(ask(x, n_get_device));
+  t.dims = shape_of(x, t.shape);
+  strides_of(x, t.stride);
+  t.item = ask(x, n_element_size);
+  t.p = data_of(x);
+  return t;
+}
+// Dense in the order of its sizes, from size `from` on.
+bool dense(const Info& t, int from = 0) {
+  int64_t n = 1;
+  for (int i = 0; i < t.dims && i < MOST; ++i)
+    if (t.shape[i] == 0) return true;
+  for (int i = (t.dims < MOST ? t.dims : MOST) - 1; i >= from; --i) {
+    if (t.shape[i] != 1 && t.stride[i] != n) return false;
+    n *= t.shape[i];
+  }
+  return t.dims <= MOST;
 }
 
 // Address of a contiguous tensor of one of the types on the device with these sizes (a size below 0: any).
 template <int DIMS>
 void* flat(PyObject* x, const char* name, int allowed, int device, const int64_t (&want)[DIMS], int64_t* last = nullptr) {
-  int64_t s[3] = {0, 0, 0};
-  bool ok = (type_of(x) & allowed) != 0 && ask(x, n_get_device) == device && shape_of(x, s) == DIMS && contiguous(x);
-  for (int i = 0; i < DIMS; ++i) ok = ok && (want[i] < 0 || s[i] == want[i]);
+  const Info t = look(x);
+  bool ok = (t.type & allowed) != 0 && t.device == device && t.dims == DIMS && dense(t);
+  for (int i = 0; i < DIMS; ++i) ok = ok && (want[i] < 0 || t.shape[i] == want[i]);
   if (!ok) {
     const Ref shape(PyObject_GetAttr(x, n_shape)), type(PyObject_GetAttr(x, n_dtype));
     if (!shape.p || !type.p) throw Error{};
@@ -132,8 +201,8 @@ void* flat(PyObject* x, const char* name, int allowed, int device, const int64_t
                  device, type.p, shape.p, static_cast<long long>(ask(x, n_get_device)));
     throw Error{};
   }
-  if (last) *last = s[DIMS - 1];
-  return data_of(x);
+  if (last) *last = t.shape[DIMS - 1];
+  return t.p;
 }
 void* optional(PyObject* x, const char* name, int allowed, int device, int64_t n) {
   return x == Py_None ? nullptr : flat<1>(x, name, allowed, device, {n});
@@ -146,18 +215,17 @@ struct Strided {
   void* p;
 };
 Strided strided(PyObject* x, const char* name) {
+  const Info f = look(x);
+  const int64_t *s = f.shape, *st = f.stride;
   Strided t;
-  int64_t s[3], st[3];
-  t.type = type_of(x);
-  t.device = static_cast<int>(ask(x, n_get_device));
+  t.type = f.type;
+  t.device = f.device;
   if (!(t.type & (BF16 | F16)) || t.device < 0) refuse(name, "a bfloat16 or float16 tensor on a CUDA device");
-  if (shape_of(x, s) != 3) refuse(name, "[rows, heads, head_dim]");
-  const Ref r(PyObject_CallMethodNoArgs(x, n_stride));
-  numbers(r.p, st);
-  if (st[2] != 1 || (s[1] > 1 && st[1] != s[2])) refuse(name, "[rows, heads, head_dim] with dense heads");
+  if (f.dims != 3) refuse(name, "[rows, heads, head_dim]");
+  if ((s[2] > 1 && st[2] != 1) || (s[1] > 1 && st[1] != s[2])) refuse(name, "[rows, heads, head_dim] with dense heads");
   t.rows = s[0]; t.heads = s[1]; t.dim = s[2];
   t.stride = s[0] > 1 ? st[0] : s[1] * s[2];
-  t.p = data_of(x);
+  t.p = f.p;
   return t;
 }
 void same_kind(const Strided& t, const Strided& k, const char* name, const char* what) {
@@ -343,13 +411,14 @@ PyObject* compact_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
 // 8-bit pages [pages, kv_heads, 2, 16, head_dim] with dense inner sizes, and their scales [pages, kv_heads, 2].
 percache_kv8_t pages8(PyObject* pages, PyObject* scales, PyObject* page_table, int64_t n_seqs, int type, int device) {
   percache_kv8_t kv = {};
-  int64_t s[5], st[5], width = 0;
-  if (!(type_of(pages) & (F8 | U8)) || ask(pages, n_get_device) != device) refuse("pages", "a float8_e4m3fn or uint8 tensor on the rows' device");
-  if (shape_of(pages, s) != 5 || s[2] != 2 || s[3] != 16 || s[1] > INT32_MAX || s[4] > INT32_MAX) refuse("pages", "[pages, kv_heads, 2, 16, head_dim]");
-  strides_of(pages, st);
+  const Info f = look(pages);
+  const int64_t *s = f.shape, *st = f.stride;
+  int64_t width = 0;
+  if (!(f.type & (F8 | U8)) || f.device != device) refuse("pages", "a float8_e4m3fn or uint8 tensor on the rows' device");
+  if (f.dims != 5 || s[2] != 2 || s[3] != 16 || s[1] > INT32_MAX || s[4] > INT32_MAX) refuse("pages", "[pages, kv_heads, 2, 16, head_dim]");
   if (st[4] != 1 || st[3] != s[4] || st[2] != 16 * s[4] || (s[1] > 1 && st[1] != 32 * s[4])) refuse("pages", "[pages, kv_heads, 2, 16, head_dim] with dense pages");
   kv.scales = static_cast<float*>(flat<3>(scales, "scales", F32, device, {s[0], s[1], 2}));
-  kv.pages = data_of(pages);
+  kv.pages = f.p;
   kv.page_stride = s[0] > 1 ? st[0] : 32 * s[1] * s[4];
   kv.n_pages = s[0]; kv.n_kv_heads = static_cast<int32_t>(s[1]); kv.head_dim = static_cast<int32_t>(s[4]);
   kv.dtype = type == BF16 ? PERCACHE_BF16 : PERCACHE_F16;
@@ -432,24 +501,19 @@ PyObject* tree_attention_8bit(PyObject*, PyObject* const* x, Py_ssize_t n) {
 
 // A pool [layers, pages, ...] whose pages are dense.
 percache_pool_t pool_of(PyObject* x, int device, int64_t n_pages) {
-  constexpr int MOST = 8;
-  int64_t s[MOST], st[MOST];
+  const Info f = look(x);
+  const int64_t *s = f.shape, *st = f.stride;
   percache_pool_t p = {};
-  if (ask(x, n_get_device) != device) refuse("pools", "tensors on the tables' device");
-  const int dims = shape_of(x, s);
-  if (dims < 2 || dims > MOST || s[1] != n_pages || s[0] < 1 || s[0] > INT32_MAX) refuse("pools", "[layers, pages, ...] with as many pages as refs");
-  strides_of(x, st);
-  const int64_t size = ask(x, n_element_size);
-  int64_t dense = 1;
-  for (int i = dims - 1; i >= 2; --i) {
-    if (s[i] != 1 && st[i] != dense) refuse("pools", "dense pages");
-    dense *= s[i];
-  }
-  if ((s[0] > 1 && st[0] <= 0) || (s[1] > 1 && st[1] < dense)) refuse("pools", "layers and pages that do not overlap");
-  p.base = data_of(x);
-  p.page_bytes = dense * size;
-  p.page_stride = s[1] > 1 ? st[1] * size : p.page_bytes;
-  p.layer_stride = s[0] > 1 ? st[0] * size : 0;
+  if (f.device != device) refuse("pools", "tensors on the tables' device");
+  if (f.dims < 2 || f.dims > MOST || s[1] != n_pages || s[0] < 1 || s[0] > INT32_MAX) refuse("pools", "[layers, pages, ...] with as many pages as refs");
+  if (!dense(f, 2)) refuse("pools", "dense pages");
+  int64_t page = 1;
+  for (int i = 2; i < f.dims; ++i) page *= s[i];
+  if ((s[0] > 1 && st[0] <= 0) || (s[1] > 1 && st[1] < page)) refuse("pools", "layers and pages that do not overlap");
+  p.base = f.p;
+  p.page_bytes = page * f.item;
+  p.page_stride = s[1] > 1 ? st[1] * f.item : p.page_bytes;
+  p.layer_stride = s[0] > 1 ? st[0] * f.item : 0;
   p.n_layers = static_cast<int32_t>(s[0]);
   return p;
 }
@@ -491,12 +555,12 @@ PyObject* fork_pages(PyObject*, PyObject* const* x, Py_ssize_t n) {
 }
 
 // bind((addresses of the eight entry points), (torch's int32, float32, uint8, bool, int64, uint64, bfloat16, float16,
-// float8_e4m3fn), device -> stream)
+// float8_e4m3fn), device -> stream, tensor -> DLPack capsule or None)
 PyObject* bind(PyObject*, PyObject* args) {
   unsigned long long f[8];
-  PyObject *t[N_TYPES], *stream;
-  if (!PyArg_ParseTuple(args, "(KKKKKKKK)(OOOOOOOOO)O", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &t[0], &t[1], &t[2], &t[3],
-                        &t[4], &t[5], &t[6], &t[7], &t[8], &stream))
+  PyObject *t[N_TYPES], *stream, *dlpack;
+  if (!PyArg_ParseTuple(args, "(KKKKKKKK)(OOOOOOOOO)OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &t[0], &t[1], &t[2], &t[3],
+                        &t[4], &t[5], &t[6], &t[7], &t[8], &stream, &dlpack))
     return nullptr;
   for (int i = 0; i < N_TYPES; ++i) {
     Py_INCREF(t[i]);
@@ -504,6 +568,8 @@ PyObject* bind(PyObject*, PyObject* args) {
   }
   Py_INCREF(stream);
   Py_XSETREF(current_stream, stream);
+  Py_XINCREF(dlpack == Py_None ? nullptr : dlpack);
+  Py_XSETREF(to_dlpack, dlpack == Py_None ? nullptr : dlpack);
   f_tree = reinterpret_cast<decltype(f_tree)>(f[0]);
   f_weights = reinterpret_cast<decltype(f_weights)>(f[1]);
   f_select = reinterpret_cast<decltype(f_select)>(f[2]);
@@ -535,9 +601,8 @@ PyMODINIT_FUNC PyInit__ops_binding() {
   n_shape = PyUnicode_InternFromString("shape");
   n_get_device = PyUnicode_InternFromString("get_device");
   n_stride = PyUnicode_InternFromString("stride");
-  n_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   n_data_ptr = PyUnicode_InternFromString("data_ptr");
   n_element_size = PyUnicode_InternFromString("element_size");
-  if (!n_element_size || !n_dtype || !n_shape || !n_get_device || !n_stride || !n_is_contiguous || !n_data_ptr) return nullptr;
+  if (!n_element_size || !n_dtype || !n_shape || !n_get_device || !n_stride || !n_data_ptr) return nullptr;
   return PyModule_Create(&module);
 }

@@ -1,10 +1,12 @@
 // Sequences that go on as others: page tables, counters, the free list, and copies of the pages that two of them would write.
 //
 // Three things depend on each other: how many pages every child takes (a prefix sum over the children), the counters (a page is free when the last
-// holder lets go), and the free list (freed pages in ascending order).  fork_plan_kernel: one block works the children out, while the
+// holder lets go), and the free list (freed pages in ascending order).  fork_small_kernel: up to 512 sequences and 8192 pages, outputs in arrays of their own; every block
+// works the children out for itself, the first one has the counters (in shared memory) and the list, the others tables and copies, and nobody
+// waits for anybody.  Else two kernels.  fork_plan_kernel: one block works the children out, while the
 // others clear the marks of freed pages and, where the outputs are arrays of their own, copy the counters and the list.  fork_kernel: tables,
 // counters and copies by all blocks; the block that is last with its tables and counters lists the freed pages, while the others copy on.
-// Bound by HBM where pages are copied (each read once, written once), else by the latency of two launches.
+// Bound by HBM where pages are copied (each read once, written once), else by latency: 1 prompt to 4 samples 10.3 us with two kernels.
 #include <algorithm>
 
 #include "slot_row.cuh"
@@ -13,7 +15,7 @@ namespace pc {
 namespace {
 
 struct Child { int32_t parent, have, got, full; int64_t start; };      // `have` pages of the parent's, `got` of the list's from place `start` on
-struct PlanHead { int32_t n_copies, count, taken, done; };
+struct PlanHead { int32_t count, taken, done, pad; };
 // The workspace's first 256 bytes belong to the calls that report in them.
 constexpr size_t WS_HEAD = 256, WS_CHILD = 512, WS_COPY = WS_CHILD + sizeof(Child) * MAX_FORK_SEQS, WS_KIDS = WS_COPY + sizeof(int2) * MAX_FORK_SEQS,
                  WS_MARKS = WS_KIDS + sizeof(int32_t) * MAX_FORK_SEQS;
@@ -63,6 +65,174 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* warp_sums, int6
   return x;
 }
 
+// Pages of a word of marks into the list, from place `to` on.
+__device__ __forceinline__ void return_freed(const Fork& f, uint32_t marks, int page0, int64_t to) {
+  for (uint32_t x = marks; x; x &= x - 1, ++to)
+    if (to < f.n_pages) f.free_list_out[to] = page0 + __ffs(x) - 1;
+}
+// What child i takes over (first: every sequence's first child), and how many pages it lacks.
+struct Wants {
+  Child c;
+  int fresh, length;
+  bool part;                     // a partly filled page to copy
+};
+__device__ __forceinline__ Wants wants_of(const Fork& f, int i, const int32_t* first) {
+  Wants w{Child{-1, 0, 0, 0, 0}, 0, 0, false};
+  if (i >= f.n_children) return w;
+  const int p = ld_dep_s32(f.parent + i);
+  if (p < 0 || p >= f.n_seqs) return w;
+  const Seq q = seq_of(f, p);
+  const bool heir = first[p] == i;
+  w.c.parent = p;
+  w.c.full = q.length / PAGE_TOKENS;
+  w.c.have = min(heir ? q.held : w.c.full, f.width_out);
+  w.length = q.length;
+  w.part = !heir && q.length % PAGE_TOKENS != 0 && w.c.full < f.width_out;
+  const int want = static_cast<int>(min((static_cast<int64_t>(q.length) + f.room + PAGE_TOKENS - 1) / PAGE_TOKENS, static_cast<int64_t>(f.width_out)));
+  w.fresh = max(want - w.c.have, 0);
+  return w;
+}
+// What the list has for it; start: how many pages the children before it lack.
+__device__ __forceinline__ void give(Wants& w, int64_t start, int count) {
+  w.c.start = start;
+  w.c.got = static_cast<int>(min(max(static_cast<int64_t>(count) - start, static_cast<int64_t>(0)), static_cast<int64_t>(w.fresh)));
+}
+// Page to page, or -1.
+__device__ __forceinline__ int2 copy_of(const Fork& f, const Wants& w, int count) {
+  if (!w.part || w.c.got == 0) return make_int2(-1, -1);
+  return make_int2(ld_dep_s32(f.table + static_cast<size_t>(w.c.parent) * f.width + w.c.full), ld_dep_s32(f.free_list + count - 1 - w.c.start));
+}
+__device__ __forceinline__ bool copies(const Fork& f, int2 c) { return c.x >= 0 && c.x < f.n_pages && c.y >= 0 && c.y < f.n_pages && c.x != c.y; }
+__device__ __forceinline__ int length_of(const Wants& w) {
+  return static_cast<int>(min(static_cast<int64_t>(w.length), static_cast<int64_t>(w.c.have + w.c.got) * PAGE_TOKENS));
+}
+__device__ __forceinline__ int count_of(const Fork& f) { return static_cast<int>(min(static_cast<int64_t>(max(ld_dep_s32(f.free_count), 0)), f.n_pages)); }
+// Entry j of a child's row of table_out.
+__device__ __forceinline__ int entry_of(const Fork& f, const Child& c, int count, int j) {
+  if (j < c.have) return ld_dep_s32(f.table + static_cast<size_t>(c.parent) * f.width + j);
+  return j < c.have + c.got ? ld_dep_s32(f.free_list + count - 1 - c.start - (j - c.have)) : -1;
+}
+
+constexpr int COPY_BYTES = 16384;                 // of a page that a block takes at a time
+// Stretch `chunk` of a page (over pools, their layers and the page's stretches) by the block.
+template <int THREADS>
+__device__ __forceinline__ void copy_chunk(const Fork& f, int2 pair, int chunk) {
+  int k = 0;
+#pragma unroll 1
+  for (;; ++k) {                                  // which pool
+    const int per = static_cast<int>((f.pools[k].page_bytes + COPY_BYTES - 1) / COPY_BYTES) * f.pools[k].n_layers;
+    if (chunk < per || k + 1 == f.n_pools) break;
+    chunk -= per;
+  }
+  const Pool& pool = f.pools[k];
+  const int pieces = static_cast<int>((pool.page_bytes + COPY_BYTES - 1) / COPY_BYTES);
+  const int64_t off = static_cast<int64_t>(chunk % pieces) * COPY_BYTES, len = min(pool.page_bytes - off, static_cast<int64_t>(COPY_BYTES));
+  char* base = pool.base + (chunk / pieces) * pool.layer_stride + off;
+  const char* src = base + pair.x * pool.page_stride;
+  char* dst = base + pair.y * pool.page_stride;
+  const int tid = threadIdx.x;
+  if (pool.vec == 16) {
+    uint4 v[COPY_BYTES / 16 / THREADS];
+#pragma unroll
+    for (int e = 0; e < COPY_BYTES / 16 / THREADS; ++e) {
+      const int at = (e * THREADS + tid) * 16;
+      if (at < len) v[e] = ld_dep_v4(src + at);
+    }
+#pragma unroll
+    for (int e = 0; e < COPY_BYTES / 16 / THREADS; ++e) {
+      const int at = (e * THREADS + tid) * 16;
+      if (at < len) *reinterpret_cast<uint4*>(dst + at) = v[e];
+    }
+  } else {
+    for (int at = tid * 4; at < len; at += THREADS * 4) *reinterpret_cast<int*>(dst + at) = ld_dep_s32(src + at);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- one kernel
+constexpr int SMALL_SEQS = 512, SMALL_PAGES = 8192, SMALL_ENTRIES = 65536, SMALL_THREADS = 512;
+struct SmallPlan {
+  int32_t first[SMALL_SEQS], kids[SMALL_SEQS];
+  Child child[SMALL_SEQS];
+  int2 copy[SMALL_SEQS];
+};
+__global__ void __launch_bounds__(SMALL_THREADS) fork_small_kernel(const __grid_constant__ Fork f, int chunks) {
+  __shared__ SmallPlan plan;
+  __shared__ int64_t warp_sums[SMALL_THREADS / 32];
+  __shared__ uint32_t marks[SMALL_PAGES / 32];
+  extern __shared__ int32_t refs[];               // [n_pages], the first block's
+  pdl_launch_dependents();
+  pdl_wait();
+  const int tid = threadIdx.x, n_pages = static_cast<int>(f.n_pages);
+  const bool counts = blockIdx.x == 0;
+  const int count = count_of(f);
+  if (counts) {
+    for (int i = tid; i < n_pages; i += SMALL_THREADS) refs[i] = ld_dep_s32(f.refs + i);
+    for (int i = tid; i < (n_pages + 31) / 32; i += SMALL_THREADS) marks[i] = 0u;
+    for (int i = tid; i < n_pages; i += SMALL_THREADS) f.free_list_out[i] = ld_dep_s32(f.free_list + i);
+  }
+  plan.first[tid] = INT32_MAX;
+  plan.kids[tid] = 0;
+  __syncthreads();
+  if (tid < f.n_children) {
+    const int p = ld_dep_s32(f.parent + tid);
+    if (p >= 0 && p < f.n_seqs) {
+      atomicMin(plan.first + p, tid);
+      atomicAdd(plan.kids + p, 1);
+    }
+  }
+  __syncthreads();
+  Wants w = wants_of(f, tid, plan.first);
+  int64_t lacking, n_copies;
+  give(w, block_sum(w.fresh, warp_sums, &lacking) - w.fresh, count);
+  const int2 c = copy_of(f, w, count);
+  const bool mine = copies(f, c);
+  const int64_t place = block_sum(mine ? 1 : 0, warp_sums, &n_copies);
+  if (mine) plan.copy[place - 1] = c;
+  plan.child[tid] = w.c;
+  const int taken = static_cast<int>(min(lacking, static_cast<int64_t>(count)));
+  __syncthreads();
+  if (counts) {
+    if (tid < f.n_children) {
+      f.held_out[tid] = w.c.have + w.c.got;
+      f.length_out[tid] = length_of(w);
+    }
+    if (tid == 0) f.missing[0] = static_cast<int>(min(lacking - taken, static_cast<int64_t>(INT32_MAX)));
+    // a warp a sequence: its full pages have its children for holders, without any all its pages one holder less
+    for (int s = tid >> 5; s < f.n_seqs; s += SMALL_THREADS / 32) {
+      const int kids = plan.kids[s];
+      if (kids == 1) continue;
+      const Seq q = seq_of(f, s);
+      const int n = kids == 0 ? q.held : q.length / PAGE_TOKENS;
+      for (int j = tid & 31; j < n; j += 32) {
+        const int page = ld_dep_s32(f.table + static_cast<size_t>(s) * f.width + j);
+        if (page < 0 || page >= n_pages) continue;
+        const int before = atomicAdd(refs + page, kids - 1);
+        if (kids == 0 && before == 1) atomicOr(marks + (page >> 5), 1u << (page & 31));
+      }
+    }
+    __syncthreads();
+    for (int k = tid; k < taken; k += SMALL_THREADS) {            // the list's last pages
+      const int page = ld_dep_s32(f.free_list + count - 1 - k);
+      if (page >= 0 && page < n_pages) refs[page] = 1;
+    }
+    __syncthreads();
+    for (int i = tid; i < n_pages; i += SMALL_THREADS) f.refs_out[i] = refs[i];
+    int64_t n_freed;
+    const uint32_t m = tid < (n_pages + 31) / 32 ? marks[tid] : 0u;
+    int64_t to = count - taken + block_sum(__popc(m), warp_sums, &n_freed) - __popc(m);
+    return_freed(f, m, tid * 32, to);
+    if (tid == 0) f.free_count_out[0] = static_cast<int>(min(count - taken + n_freed, f.n_pages));
+    return;
+  }
+  const int64_t others = gridDim.x - 1, me = blockIdx.x - 1;
+  for (int64_t i = me; i < f.n_children; i += others) {
+    const Child ch = plan.child[i];
+    for (int j = tid; j < f.width_out; j += SMALL_THREADS) f.table_out[static_cast<size_t>(i) * f.width_out + j] = entry_of(f, ch, count, j);
+  }
+  for (int64_t u = me; u < n_copies * chunks; u += others) copy_chunk<SMALL_THREADS>(f, plan.copy[u / chunks], static_cast<int>(u % chunks));
+}
+
+// ---------------------------------------------------------------------------------------------------- two kernels
 constexpr int PLAN_THREADS = 1024;
 __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const __grid_constant__ Fork f) {
   extern __shared__ int32_t by_seq[];             // [n_seqs] first child, [n_seqs] number of children
@@ -84,7 +254,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const __grid_co
   }
   int32_t *first = by_seq, *kids = by_seq + f.n_seqs;
   for (int s = tid; s < f.n_seqs; s += PLAN_THREADS) { first[s] = INT32_MAX; kids[s] = 0; }
-  const int count = static_cast<int>(min(static_cast<int64_t>(max(ld_dep_s32(f.free_count), 0)), f.n_pages));
+  const int count = count_of(f);
   __syncthreads();
   for (int i = tid; i < f.n_children; i += PLAN_THREADS) {
     const int p = ld_dep_s32(f.parent + i);
@@ -95,58 +265,35 @@ __global__ void __launch_bounds__(PLAN_THREADS) fork_plan_kernel(const __grid_co
   }
   __syncthreads();
   for (int s = tid; s < f.n_seqs; s += PLAN_THREADS) plan.kids[s] = kids[s];
-  // pages taken in the upper bits, copies in the lower 16: one sum over the children in order
   int64_t before = 0;
   for (int i0 = 0; i0 < f.n_children; i0 += PLAN_THREADS) {
     const int i = i0 + tid;
-    Child c{-1, 0, 0, 0, 0};
-    int fresh = 0;
-    bool part = false, heir = false;
-    Seq q{0, 0};
-    if (i < f.n_children) {
-      c.parent = ld_dep_s32(f.parent + i);
-      if (c.parent < 0 || c.parent >= f.n_seqs) c.parent = -1;
-      if (c.parent >= 0) {
-        q = seq_of(f, c.parent);
-        heir = first[c.parent] == i;
-        c.full = q.length / PAGE_TOKENS;
-        part = !heir && q.length % PAGE_TOKENS != 0 && c.full < f.width_out;
-        c.have = min(heir ? q.held : c.full, f.width_out);
-        const int want = static_cast<int>(min((static_cast<int64_t>(q.length) + f.room + PAGE_TOKENS - 1) / PAGE_TOKENS, static_cast<int64_t>(f.width_out)));
-        fresh = max(want - c.have, 0);
-      }
-    }
+    Wants w = wants_of(f, i, first);
     int64_t all;
-    const int64_t fresh_sum = before + block_sum(fresh, warp_sums, &all);
+    give(w, before + block_sum(w.fresh, warp_sums, &all) - w.fresh, count);
     before += all;
-    c.start = fresh_sum - fresh;
-    c.got = static_cast<int>(min(max(static_cast<int64_t>(count) - c.start, static_cast<int64_t>(0)), static_cast<int64_t>(fresh)));
     if (i < f.n_children) {
-      plan.child[i] = c;
-      f.held_out[i] = c.have + c.got;
-      f.length_out[i] = c.parent < 0 ? 0 : static_cast<int>(min(static_cast<int64_t>(q.length), static_cast<int64_t>(c.have + c.got) * PAGE_TOKENS));
-      // -1: nothing to copy (the place of a child's copy is its own, so that no order has to be found)
-      const bool copies = part && c.got > 0;
-      plan.copy[i] = copies ? make_int2(ld_dep_s32(f.table + static_cast<size_t>(c.parent) * f.width + c.full), ld_dep_s32(f.free_list + count - 1 - c.start))
-                            : make_int2(-1, -1);
+      plan.child[i] = w.c;
+      f.held_out[i] = w.c.have + w.c.got;
+      f.length_out[i] = length_of(w);
+      plan.copy[i] = copy_of(f, w, count);
     }
   }
   if (tid == 0) {
     const int64_t taken = min(before, static_cast<int64_t>(count));
     f.missing[0] = static_cast<int>(min(before - taken, static_cast<int64_t>(INT32_MAX)));
-    *plan.head = PlanHead{0, count, static_cast<int>(taken), 0};
+    *plan.head = PlanHead{count, static_cast<int>(taken), 0, 0};
   }
 }
 
 constexpr int FORK_THREADS = 256;
-constexpr int COPY_BYTES = 16384;                 // of a page that a block takes at a time
 
 __device__ __forceinline__ int volatile_s32(const int32_t* p) { return *reinterpret_cast<const volatile int32_t*>(p); }
 
 __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constant__ Fork f, int chunks) {
   __shared__ int64_t warp_sums[FORK_THREADS / 32];
   __shared__ int last;
-  __shared__ int2 copies[FORK_THREADS];
+  __shared__ int2 list[FORK_THREADS];
   pdl_launch_dependents();
   pdl_wait();
   const Plan plan = plan_of(f.workspace);
@@ -155,16 +302,11 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
 
   // ---- tables, and the counters of pages that were taken
   for (int i = blockIdx.x; i < f.n_children; i += gridDim.x) {
-    const volatile Child* c = plan.child + i;
-    const int parent = c->parent, have = c->have, got = c->got;
-    const int64_t top = count - 1 - c->start;
+    const volatile Child* at = plan.child + i;
+    const Child c{at->parent, at->have, at->got, at->full, at->start};
     for (int j = tid; j < f.width_out; j += FORK_THREADS) {
-      int page = -1;
-      if (j < have) page = ld_dep_s32(f.table + static_cast<size_t>(parent) * f.width + j);
-      else if (j < have + got) {
-        page = ld_dep_s32(f.free_list + top - (j - have));
-        if (page >= 0 && page < f.n_pages) f.refs_out[page] = 1;
-      }
+      const int page = entry_of(f, c, count, j);
+      if (j >= c.have && page >= 0 && page < f.n_pages) f.refs_out[page] = 1;
       f.table_out[static_cast<size_t>(i) * f.width_out + j] = page;
     }
   }
@@ -203,9 +345,10 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
       int64_t to = at + block_sum(n, warp_sums, &all) - n;
       at += all;
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        for (uint32_t x = m[u]; x; x &= x - 1, ++to)
-          if (to < f.n_pages) f.free_list_out[to] = (w0 + tid * 4 + u) * 32 + __ffs(x) - 1;
+      for (int u = 0; u < 4; ++u) {
+        return_freed(f, m[u], (w0 + tid * 4 + u) * 32, to);
+        to += __popc(m[u]);
+      }
     }
     if (tid == 0) f.free_count_out[0] = static_cast<int>(min(at, f.n_pages));
   }
@@ -219,42 +362,14 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
       const volatile int2* p = plan.copy + i0 + tid;
       c = make_int2(p->x, p->y);
     }
-    const bool mine = c.x >= 0 && c.x < f.n_pages && c.y >= 0 && c.y < f.n_pages && c.x != c.y;
+    const bool mine = copies(f, c);
     int64_t n;
     const int64_t place = block_sum(mine ? 1 : 0, warp_sums, &n);
-    if (mine) copies[place - 1] = c;
+    if (mine) list[place - 1] = c;
     __syncthreads();
 #pragma unroll 1
     for (int64_t u = blockIdx.x; u < n * chunks; u += gridDim.x) {
-      const int2 pair = copies[u / chunks];
-      int chunk = static_cast<int>(u % chunks), k = 0;
-#pragma unroll 1
-      for (;; ++k) {                               // which pool, layer and stretch of the page
-        const int per = static_cast<int>((f.pools[k].page_bytes + COPY_BYTES - 1) / COPY_BYTES) * f.pools[k].n_layers;
-        if (chunk < per || k + 1 == f.n_pools) break;
-        chunk -= per;
-      }
-      const Pool& pool = f.pools[k];
-      const int pieces = static_cast<int>((pool.page_bytes + COPY_BYTES - 1) / COPY_BYTES);
-      const int64_t off = static_cast<int64_t>(chunk % pieces) * COPY_BYTES, len = min(pool.page_bytes - off, static_cast<int64_t>(COPY_BYTES));
-      char* base = pool.base + (chunk / pieces) * pool.layer_stride + off;
-      const char* src = base + pair.x * pool.page_stride;
-      char* dst = base + pair.y * pool.page_stride;
-      if (pool.vec == 16) {
-        uint4 v[COPY_BYTES / 16 / FORK_THREADS];
-#pragma unroll
-        for (int e = 0; e < COPY_BYTES / 16 / FORK_THREADS; ++e) {
-          const int at = (e * FORK_THREADS + tid) * 16;
-          if (at < len) v[e] = ld_dep_v4(src + at);
-        }
-#pragma unroll
-        for (int e = 0; e < COPY_BYTES / 16 / FORK_THREADS; ++e) {
-          const int at = (e * FORK_THREADS + tid) * 16;
-          if (at < len) *reinterpret_cast<uint4*>(dst + at) = v[e];
-        }
-      } else {
-        for (int at = tid * 4; at < len; at += FORK_THREADS * 4) *reinterpret_cast<int*>(dst + at) = ld_dep_s32(src + at);
-      }
+      copy_chunk<FORK_THREADS>(f, list[u / chunks], static_cast<int>(u % chunks));
     }
     __syncthreads();
   }
@@ -266,18 +381,25 @@ int launch_fork(const Fork& f, int n_sms, cudaStream_t s) {
   static bool set[MAX_DEVICES] = {};
   const int dev = current_device_slot();
   if (!set[dev]) {
-    if (cudaFuncSetAttribute(fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_FORK_SEQS * 8) != cudaSuccess) return -1;
+    if (cudaFuncSetAttribute(fork_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_FORK_SEQS * 8) != cudaSuccess ||
+        cudaFuncSetAttribute(fork_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMALL_PAGES * 4) != cudaSuccess)
+      return -1;
     set[dev] = true;
   }
   int64_t chunks = 0;
   for (int k = 0; k < f.n_pools; ++k) chunks += (f.pools[k].page_bytes + COPY_BYTES - 1) / COPY_BYTES * f.pools[k].n_layers;
   if (chunks > INT32_MAX) return -2;
+  // as many blocks as there is work at most: rows of tables, and the copies if every child but one makes one
+  const int64_t work = std::max<int64_t>(f.n_children, chunks * std::max(f.n_children - 1, 0));
+  // (in place the first block would change what blocks that start later still have to read)
+  if (f.refs_out != f.refs && f.n_seqs <= SMALL_SEQS && f.n_children <= SMALL_SEQS && f.n_pages <= SMALL_PAGES && static_cast<int64_t>(f.n_seqs) * f.width <= SMALL_ENTRIES) {
+    const int others = static_cast<int>(std::max<int64_t>(std::min<int64_t>(work, static_cast<int64_t>(n_sms) * 4 - 1), 1));
+    return launch_pdl(fork_small_kernel, dim3(1 + others), dim3(SMALL_THREADS), static_cast<size_t>(f.n_pages) * 4, s, f, static_cast<int>(chunks)) == cudaSuccess ? 0 : -1;
+  }
   const int64_t lists = f.refs_out != f.refs ? f.n_pages : (f.n_pages + 31) / 32;
   const int list_blocks = static_cast<int>(std::min<int64_t>((lists + PLAN_THREADS - 1) / PLAN_THREADS, n_sms));
   if (launch_pdl(fork_plan_kernel, dim3(1 + std::max(list_blocks, 1)), dim3(PLAN_THREADS), static_cast<size_t>(f.n_seqs) * 8, s, f) != cudaSuccess) return -1;
-  // as many blocks as there is work at most: rows of tables and counters, and the copies if every child but one makes one
-  const int64_t work = std::max<int64_t>(std::max(f.n_seqs, f.n_children), chunks * std::max(f.n_children - 1, 0));
-  const int blocks = static_cast<int>(std::max<int64_t>(std::min<int64_t>(work, static_cast<int64_t>(n_sms) * 6), 1));
+  const int blocks = static_cast<int>(std::max<int64_t>(std::min<int64_t>(std::max<int64_t>(work, f.n_seqs), static_cast<int64_t>(n_sms) * 6), 1));
   return launch_pdl(fork_kernel, dim3(blocks), dim3(FORK_THREADS), 0, s, f, static_cast<int>(chunks)) == cudaSuccess ? 0 : -1;
 }
 

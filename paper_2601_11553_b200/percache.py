@@ -570,6 +570,7 @@ def _ops() -> Any:
     global _binding
     if _binding is None:
         import torch                 # this module does not need it for anything else
+        import torch.utils.dlpack
         lib = load_library()
         try:
             from . import _ops_binding as m
@@ -582,7 +583,7 @@ def _ops() -> Any:
                (torch.int32, torch.float32, torch.uint8, torch.bool, torch.int64, torch.uint64, torch.bfloat16, torch.float16,
                 torch.float8_e4m3fn),
                # without the Python objects of torch.cuda.current_stream, where torch has it (a small call's time is the host's)
-               getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream))
+               getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream), getattr(torch.utils.dlpack, "to_dlpack", None))
         _binding = m
     return _binding
 
