@@ -4,9 +4,14 @@
 // eight that they are turned with: the norm is a sum over those lanes, the rotation needs no exchange, and all accesses are 16 bytes.
 // Bound by HBM: every element is read once and written once.
 //
-// append_rows_kernel: a warp is one row's run of heads (queries, keys, values in turn), four or eight heads side by side; the row's
-// cosines and sines stay in registers over the run.  append_pages_kernel: a warp is the keys or the values of one KV head in one 8-bit page (the
-// scale is one number for all of the page's new rows), its 16 slots in registers between the maximum and the rounding.
+// Three kernels.  append_rows_kernel (16-bit pools, few rows): a warp is one row's run of heads, queries, keys and values in turn, four or eight
+// heads side by side; the row's cosines and sines stay in registers over the run.  append_pages_kernel (8-bit pages, few rows): a warp is
+// keys or values of one KV head in one page (the scale is one number for all of the page's new rows), its 16 slots in registers between
+// the maximum and the rounding; other blocks write the queries.  append_units_kernel (many rows of long prompts, either cache): a warp has eight
+// rows, and takes their heads one after the other through a ring of asynchronous copies.
+// Measured, 16 query and 8 KV heads of 128 elements: one row 2.6 us, 64 single rows into 8-bit pages 4.6 us (latency); 33024 rows into a 16-bit
+// context 90 us (6.0 TB/s), 11.6 thousand rows of 8 prompts into 8-bit pages 44.6 us (3.6 TB/s: instruction issue, 430 a warp for eight rows of a
+// head, of which 40 for the page's maximum).
 #include <algorithm>
 
 #include "slot_row.cuh"
@@ -209,7 +214,7 @@ __device__ __forceinline__ int position_of(const NewRows& r, int row, int slot) 
 
 // ---------------------------------------------------------------------------------------------------- 16 bits
 // One row's heads [h0, h1) by one warp: queries first, then (POOLS) keys and values.  At most four a group of lanes: they are asked for before the
-// row's place is looked up (three round trips: its prompt, the prompt's numbers, table entries).
+// row's place is looked up (two round trips: its prompt, then table entries and the rotation).
 template <int D, bool BF16, bool POOLS>
 __device__ __forceinline__ void row_heads(const KvView& kv, const NewRows& r, int row, int h0, int h1) {
   constexpr int LANES = D / 16, GROUPS = 32 / LANES, UNROLL = 4;
@@ -447,9 +452,9 @@ __global__ void __launch_bounds__(THREADS, 2) append_pages_kernel(const __grid_c
 }
 
 // ---------------------------------------------------------------------------------------------------- long prompts
-// 16 rows (those of 16 slots of a prompt, aligned to 16) of the queries', keys' and values' heads in turn, all by asynchronous copies into the warp's
-// own shared memory: a lane copies what it reads itself, so that nothing is waited for but its own copies, and the look-ups are shared by
-// 16 rows.  (With a row a warp and loads into registers, a warp's time went into look-ups: 33024 rows 113 us.)
+// Eight rows (those of eight slots of a prompt, aligned to eight), their queries', keys' and values' heads in turn, all by asynchronous copies into the
+// warp's own shared memory: a lane copies what it reads itself, so that nothing is waited for but its own copies, and the look-ups are shared by
+// eight rows and all heads.  (With a row a warp and loads into registers, a warp's time went into look-ups: 33024 rows 113 us.)
 constexpr int DEPTH = 3;                          // heads on their way
 // Four warps a block, four blocks an SM, so that nothing is kept in memory for want of registers (to fetch it takes as long as the copies ahead
 // of it: 8 prompts into 8-bit pages with 4 / 5 / 6 blocks 44.8 / 47.2 / 57.0 us).
@@ -619,8 +624,13 @@ int run_of(int64_t rows, int heads, int n_sms) {
   return rows * ((heads + 4 * GROUPS - 1) / (4 * GROUPS)) >= static_cast<int64_t>(n_sms) * WARPS * 2 ? 4 * GROUPS : GROUPS;
 }
 
-// Sixteen rows at a time where prompts have that many new rows on average.
-constexpr int LONG = 16;
+// Whether units of rows are the faster form: from enough heads of rows on that a warp's eight or so in turn do not leave the GPU half empty, and if
+// units are full on average.  With 16 + 2 x 8 heads, rows or pages against units: into 8-bit pages 2048 rows of one prompt 15.1 / 18.4 us, 4096 20.8 / 20.9,
+// 8192 38.5 / 28.3, of 64 prompts 36.2 / 36.1, 16000 of 500 prompts 64 / 69.5, 32000 122.7 / 111.6; into 16-bit pages 2048 10.9 / 14.6, 4096
+// 21.0 / 17.5, of 64 prompts 19.7 / 19.2, 8000 of 500 35.8 / 34.8.
+bool units_pay(const NewRows& r, int kinds, bool eight) {
+  return static_cast<int64_t>(r.n_rows) * kinds >= (eight ? 1 << 18 : 1 << 17) && r.n_rows / r.n_seqs >= (eight ? 64 : 16);
+}
 template <int D, bool BF16, bool EIGHT>
 int append_units(const KvView& kv, const Kv8View& kv8, const NewRows& r, cudaStream_t s) {
   static bool set[MAX_DEVICES] = {};
@@ -638,15 +648,16 @@ int append_units(const KvView& kv, const Kv8View& kv8, const NewRows& r, cudaStr
 
 template <int D, bool BF16>
 int append(const KvView& kv, const NewRows& r, int n_sms, cudaStream_t s) {
-  if (r.n_rows / r.n_seqs >= LONG) return append_units<D, BF16, false>(kv, Kv8View{}, r, s);
-  const int heads = (r.q ? r.n_q_heads : 0) + 2 * kv.n_kv_heads, run = run_of<D>(r.n_rows, heads, n_sms);
+  const int heads = (r.q ? r.n_q_heads : 0) + 2 * kv.n_kv_heads;
+  if (units_pay(r, heads, false)) return append_units<D, BF16, false>(kv, Kv8View{}, r, s);
+  const int run = run_of<D>(r.n_rows, heads, n_sms);
   const int64_t blocks = (static_cast<int64_t>(r.n_rows) * ((heads + run - 1) / run) + WARPS - 1) / WARPS;
   if (blocks > INT32_MAX) return -2;
   return launch_pdl(append_rows_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(THREADS), 0, s, kv, r, heads, run) == cudaSuccess ? 0 : -1;
 }
 template <int D, bool BF16>
 int append8(const Kv8View& kv, const NewRows& r, int n_sms, cudaStream_t s) {
-  if (r.n_rows / r.n_seqs >= LONG) return append_units<D, BF16, true>(KvView{}, kv, r, s);
+  if (units_pay(r, (r.q ? r.n_q_heads : 0) + 2 * kv.n_kv_heads, true)) return append_units<D, BF16, true>(KvView{}, kv, r, s);
   // Rows of a warp: about as many as a prompt has, so that batches of single tokens spread over the warps and long prompts have a page each.
   const int per = r.n_rows / r.n_seqs;
   const int chunk = per >= 8 ? 8 : per >= 4 ? 4 : per >= 2 ? 2 : 1;

@@ -56,12 +56,12 @@ def test_attention_with_values_beyond_the_bounds(hq):
 
 
 @pytest.mark.parametrize("cache", ["8bit", "pages", "slots"])
-@pytest.mark.parametrize("new", [3, 60])
-def test_append_with_values_beyond_the_bounds(cache, new):
+@pytest.mark.parametrize("new, hq, hkv", [(3, 4, 2), (60, 4, 2), (1500, 47, 24)])          # the last: enough for the kernel of long prompts
+def test_append_with_values_beyond_the_bounds(cache, new, hq, hkv):
     """Slots in use beyond max_len (the prompt's end), negative ones (none), rows past the last (all there are)."""
     got = []
     for ctx, first in (([40, 0], [0, new, 2 * new + 2]), ([10 ** 9, -5], [-3, new, 10 ** 6])):
-        r = Rows([(40, new), (30, new)], cache=cache, pad_rows=2)
+        r = Rows([(40, new), (30, new)], cache=cache, pad_rows=2, hq=hq, hkv=hkv)
         r.kw["max_len"] = 40 + new
         r.kw["ctx_len"].copy_(i32(ctx)), r.kw["row_start"].copy_(i32(first))
         if cache != "slots":
@@ -73,6 +73,52 @@ def test_append_with_values_beyond_the_bounds(cache, new):
         got.append([r.q_out.clone()] + [x.clone() for x in ([r.pages.view(torch.uint8), r.scales] if cache == "8bit" else r.pool)])
     assert all(torch.equal(x, y) for x, y in zip(*got))
     assert torch.isfinite(got[0][0].float()).all()
+
+
+# Batches that the kernel of many rows takes: units that begin and end inside a prompt's pages, prompts shorter than a unit, heads that do not divide
+# among the warps, rows ahead of and behind the prompts'.
+MANY = [
+    dict(seqs=[(5, 8300)], hq=16, hkv=8), dict(seqs=[(0, 3000), (117, 2500), (16, 2801)], hq=16, hkv=8, norm=False, rope=False),
+    dict(seqs=[(i % 37, 64 + i % 51) for i in range(61)], hq=30, hkv=10, position=True), dict(seqs=[(0, 1), (3, 4000), (7, 0), (21, 5), (8, 300)], hq=45, hkv=9),
+    dict(seqs=[(2, 5400)], hq=33, hkv=9, d=64, dtype="f16"), dict(seqs=[(31, 2200), (0, 3300)], hq=0, hkv=30, d=64, rope=False), dict(seqs=[(9, 90000)], hq=1, hkv=1, d=64),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MANY)))
+@pytest.mark.parametrize("cache, dtype", [("8bit", "bf16"), ("8bit", "f16"), ("pages", "bf16"), ("slots", "f16")])
+def test_append_of_many_rows_matches_the_oracle(case, cache, dtype):
+    kw = {"dtype": dtype, **MANY[case]}
+    no_q = kw["hq"] == 0
+    r = Rows(cache=cache, seed=case, **{**kw, "hq": kw["hq"] or 2})
+    r.run(q=not no_q)
+    r.check(q=not no_q)
+
+
+def test_many_rows_in_place_beside_other_prompts_rows():
+    r = Rows([(3, 4000), (50, 4500)], hq=16, hkv=8, packed=False)
+    q = r.q.clone()
+    pcb.append_rows(q, r.k, r.v, q, **r.kw)
+    r.q_out[:r.n] = q[:r.n]
+    assert torch.equal(q[r.n:], r.q[r.n:])
+    r.check()
+    first = raw(r.pages).copy(), r.scales.clone()
+    for _ in range(3):                                          # the same rows again, over pages whose scales are theirs already
+        r.run()
+        assert np.array_equal(raw(r.pages), first[0]) and torch.equal(r.scales, first[1])
+
+
+def test_large_and_odd_values_among_many_rows():
+    r = Rows([(3, 8300)], hq=16, hkv=8, norm=False, rope=False)
+    r.k[0, 0, 3], r.k[900, 7, 127], r.k[901, 1, 64], r.v[8299, 5, 0], r.v[40, 2, 9] = float("inf"), float("nan"), float("-inf"), 3e38, float("nan")
+    r.k[16 * 7 - 3:16 * 8 - 3] = 0.0
+    r.run()
+    r.check()
+    r = Rows([(3, 8300)], hq=16, hkv=8, dtype="f16", cache="slots")
+    r.k[500] = 60000.0
+    r.kw["k_gain"] = torch.full_like(r.gains[1], 3e5)
+    r.run()
+    k = f64(r.pool[0])[int(r.start[0]) + 503]
+    assert np.isfinite(k).all() and np.abs(k).max() == 65504
 
 
 def test_twenty_thousand_prompts():
