@@ -27,7 +27,7 @@ namespace {
 __host__ __device__ constexpr int ring_bytes(int nc) { return (nc == 16 ? 192 : 160) * 1024; }
 constexpr int CLEAN_BARS = 8;                   // more than the tiles between a product with K and the one with V
 constexpr int FLAGS = 8;                        // items a `bad V` flag lives for: more than the roles can be apart
-constexpr int MASK_WORDS = 4;                   // 256 nodes
+constexpr int MAX_NODES = 256;             // of a prompt, at most
 // The running reference lies HEADROOM (base 2) below the largest score that set it and is raised when a score exceeds that by RESCALE_THRESHOLD.
 constexpr float HEADROOM = 7.f, RESCALE_THRESHOLD = 8.f;
 constexpr int P_UNIT = 7;                       // the first part of P counts 2^7: at most 2^8, below 448
@@ -180,6 +180,12 @@ __device__ __forceinline__ float column_reduce(const float (&in)[NC], int n_rows
   const float few[4] = {in[0], in[1], in[2], in[3]};
   return column_reduce<4>(few, op);
 }
+// The warp's largest x (NaN passed over).
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 // OR of a predicate over the 128 threads of a block parity.
 __device__ __forceinline__ bool parity_any(int i, bool x) {
   uint32_t y;
@@ -287,8 +293,10 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
   __shared__ __align__(16) float block_max[2][2][NC][4];       // [block parity][use][row][warp]
   __shared__ __align__(16) float fin_l[2][2][NC][4];           // [item parity][block parity][row][warp]: a warp's share of the sum
   __shared__ float fin_m[2][2][NC];
-  __shared__ __align__(16) float neg_ref[8][NC];                // - reference, a copy per softmax warp
-  __shared__ uint64_t node_mask[2 * NC * MASK_WORDS];
+  __shared__ __align__(16) float neg_ref[8][NC];                // - reference, a copy per softmax warp; at a piece's end the rows' first factor
+  __shared__ __align__(16) float other_factor[8][NC];
+  using RowBits = std::conditional_t<NC == 16, uint16_t, uint32_t>;
+  __shared__ RowBits seen_by[2][MAX_NODES];               // the tile's rows that see a node
   __shared__ int bad_flag[FLAGS];
   __shared__ Span shared_span;
   __shared__ int64_t warp_sums[TREE_THREADS / 32];
@@ -396,10 +404,20 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       if (!ok) return;
       if (n_q > 0) split_q<D, NC, BF16>(a, it.row0, it.flat0, it.n_rows, it.g, q_smem + qs * Q_BYTES, q_scale[qs], 0, 512 / D);
       if (it.blk_end * BLK > it.ctx_len) {
-        const int nodes = node_of(a, it.flat0 + it.n_rows - 1) - node0 + 1, words = (it.n_nodes + 63) / 64;
 #pragma unroll 1
-        for (int e = lane; e < nodes * words; e += 32)
-          node_mask[(qs * NC + e / words) * MASK_WORDS + e % words] = node_word(a.rows, it.row0 + node0 + e / words, node0 + e / words, e % words);
+        for (int node = lane; node < it.n_nodes; node += 32) {
+          uint32_t seen = 0;
+          int h = it.flat0 - node0 * a.group, k = node0;           // the tile may begin and end inside a node's heads
+#pragma unroll 1
+          for (int c = 0; c < it.n_rows; ++k) {
+            const int n = min(a.group - h, it.n_rows - c);
+            if ((node_word(a.rows, it.row0 + k, k, node >> 6) >> (node & 63)) & 1u) seen |= (0xffffffffu >> (32 - n)) << c;
+            c += n;
+            h = 0;
+          }
+          seen_by[qs][node] = static_cast<RowBits>(seen);
+        }
+        __syncwarp();
       }
       // the first item's Q is the softmax warps' work, who have nothing else to do yet (by one warp: 32 rows 20000 clocks)
       if (n_q == 0) ok = __all_sync(0xffffffffu, bar_wait(&q_first, 0, a.err_word, DEV_ERR_ATTN_CORR));
@@ -604,16 +622,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           const int slot = (it.blk_begin + j) * BLK + r;
           if (slot >= it.ctx_len) {
             const int node = slot - it.ctx_len;
-            uint32_t seen = 0;
-            if (node < it.n_nodes) {
-              const uint64_t* w = node_mask + par * NC * MASK_WORDS + (node >> 6);
-              int at = 0, h = it.flat0 - node_of(a, it.flat0) * a.group;
-#pragma unroll 1
-              for (int c = 0; c < it.n_rows; ++c) {
-                seen |= static_cast<uint32_t>((w[at] >> (node & 63)) & 1u) << c;
-                if (++h == a.group) { h = 0; at += MASK_WORDS; }
-              }
-            }
+            const uint32_t seen = node < it.n_nodes ? seen_by[par][node] : 0u;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
               if (!((seen >> c) & 1u)) t[c] = -INFINITY;
@@ -645,7 +654,16 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           // out row c's new reference and every thread fetches it by shuffles.  Two buffers: between two uses of one lies the
           // other's barrier.
           float(*maxima)[4] = block_max[i][n_raise++ & 1];
-          const float mine = column_reduce<NC>(t, it.n_rows, [](float x, float y) { return fmaxf(x, y); });
+          float mine = -INFINITY;                          // lane c: row c's
+#pragma unroll
+          for (int c0 = 0; c0 < NC; c0 += 4) {
+            if (c0 >= it.n_rows) break;
+#pragma unroll
+            for (int c = c0; c < c0 + 4; ++c) {
+              const float m = warp_max(t[c]);
+              mine = lane == c ? m : mine;
+            }
+          }
           if (lane < NC) maxima[lane][quarter] = mine;
           parity_any(i, false);
           const float4 x = *reinterpret_cast<const float4*>(maxima[lane % NC]);
@@ -768,18 +786,26 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           }
         }
       }
+      __syncwarp();
+      if (lane < NC) { neg[lane] = f0; other_factor[warp][lane] = f1; }      // (the reference is done with)
+      __syncwarp();
       if (ok) ok = __all_sync(0xffffffffu, bar_wait(&o_full[ob], o_uses & 1u, a.err_word, DEV_ERR_ATTN_CORR));
       if (ok) {
         tc_fence_after_sync();
         const bool bad = *reinterpret_cast<volatile int*>(&bad_flag[n_item % FLAGS]) != 0;
         __syncwarp();
         int node = node_of(a, it.flat0 + i * 4), h = it.flat0 + i * 4 - node * a.group;
+        unsigned short* out = static_cast<unsigned short*>(a.out) + static_cast<int64_t>(it.row0 + node) * a.out_stride + (it.g * a.group + h) * D + r;
+        const int64_t next_node = a.out_stride - a.group * D;
+        float* partial = a.partial_o + (part0 + i * 4) * HEAD_DIM + r;
 #pragma unroll 1
         for (int c0 = i * 4; c0 < it.n_rows; c0 += 8) {    // four rows at a time, the parities in turn
           float o0[4] = {0.f, 0.f, 0.f, 0.f}, o1[4] = {0.f, 0.f, 0.f, 0.f};
           uint32_t x0[4 * X::P], x1[4 * X::P];
           tmem_columns<4 * X::P>(lanes + TMEM_O + ob * 2 * X::NO + c0 * X::P, x0);
           tmem_columns<4 * X::P>(lanes + TMEM_O + (ob * 2 + 1) * X::NO + c0 * X::P, x1);         // not used when there is one block
+          const float4 g0 = *reinterpret_cast<const float4*>(neg + c0), g1 = *reinterpret_cast<const float4*>(other_factor[warp] + c0);
+          const float f[4] = {g0.x, g0.y, g0.z, g0.w}, w1[4] = {g1.x, g1.y, g1.z, g1.w};
           tmem_wait_ld();
 #pragma unroll
           for (int part = X::P - 1; part >= 0; --part) {
@@ -792,27 +818,23 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int c = c0 + e;
-            float o = o0[e] * __shfl_sync(0xffffffffu, f0, c & 31);
-            const float w1 = __shfl_sync(0xffffffffu, f1, c & 31);
-            if (nb > 1) o = fmaf(o1[e], w1, o);
-            if (r < D && c < it.n_rows) {
-              const int row = it.row0 + node;
+            float o = o0[e] * f[e];
+            if (nb > 1) o = fmaf(o1[e], w1[e], o);
+            if (r < D && c0 + e < it.n_rows) {
               if (bad)
-                o += bad_v<D>(a, it.seq, it.ctx_len, it.n_nodes, max(it.ctx_len, it.blk_begin * BLK), min(it.ctx_len + it.n_nodes, it.blk_end * BLK), row,
-                              node, it.g, r);
-              if (whole) {
-                static_cast<unsigned short*>(a.out)[static_cast<int64_t>(row) * a.out_stride + (it.g * a.group + h) * D + r] =
-                    static_cast<unsigned short>(pack_out<BF16>(o, 0.f));
-              } else {
-                a.partial_o[(part0 + c) * HEAD_DIM + r] = o;
-              }
+                o += bad_v<D>(a, it.seq, it.ctx_len, it.n_nodes, max(it.ctx_len, it.blk_begin * BLK), min(it.ctx_len + it.n_nodes, it.blk_end * BLK),
+                              it.row0 + node, node, it.g, r);
+              if (whole) *out = static_cast<unsigned short>(pack_out<BF16>(o, 0.f));
+              else partial[e * HEAD_DIM] = o;
             }
-            if (++h == a.group) { h = 0; ++node; }
+            out += D;
+            if (++h == a.group) { h = 0; ++node; out += next_node; }
           }
-          __syncwarp();
+          // the other parity's four rows
+          partial += 8 * HEAD_DIM;
+          out += 4 * D;
 #pragma unroll 1
-          for (h += 4; h >= a.group; ++node) h -= a.group; // the other parity's four rows
+          for (h += 4; h >= a.group; ++node, out += next_node) h -= a.group;
         }
         tc_fence_before_sync();
         __syncwarp();
