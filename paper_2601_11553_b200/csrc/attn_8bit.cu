@@ -31,7 +31,7 @@ constexpr int MAX_NODES = 256;             // of a prompt, at most
 // The running reference lies HEADROOM (base 2) below the largest score that set it and is raised when a score exceeds that by RESCALE_THRESHOLD.
 constexpr float HEADROOM = 7.f, RESCALE_THRESHOLD = 8.f;
 constexpr int P_UNIT = 7;                       // the first part of P counts 2^7: at most 2^8, below 448
-constexpr int MIN_SPAN = 2;
+template <int NC> constexpr int MIN_SPAN = NC == 16 ? 2 : 24;      // a CTA's least share: two blocks, so that none that a unit reaches is without one
 constexpr int WHOLE_BLOCKS = 6;
 constexpr int PAGES = BLK / PAGE_TOKENS;
 constexpr int AHEAD = 32 / PAGES;               // blocks whose pages are asked for together
@@ -110,11 +110,15 @@ __device__ __forceinline__ void tmem_columns(uint32_t at, uint32_t* x) {
   }
 }
 
+// With 16 columns a block's time is its copy's, whatever its rows; with 32 it is the softmax's and goes with them (0.53 us with 4 rows,
+// 0.78 with 32, so 4 + rows / 4, of a prompt's tiles on average): trees of 26 on 64 x 2500 slots 123.7 us, every block alike 129.3; rows / 3 124.5.
+constexpr int max_blk_cost(int columns) { return columns == 16 ? 1 : 12; }
 template <int NC>
 __device__ __forceinline__ Shape shape8(const Tree8Params& a, const SeqPart& p) {
   if (p.n_nodes == 0) return Shape{0, 0, 1, 0};
-  const int units = (p.n_nodes * a.group + NC - 1) / NC * a.kv.n_kv_heads, n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK;
-  return a.whole ? Shape{units, 1, n_blk, a.over} : Shape{units, n_blk, 1, a.over};
+  const int rows = p.n_nodes * a.group, tiles = (rows + NC - 1) / NC, units = tiles * a.kv.n_kv_heads, n_blk = (p.ctx_len + p.n_nodes + BLK - 1) / BLK;
+  const int c = NC == 16 ? 1 : 4 + (tiles == 1 ? rows >> 2 : tiles == 2 ? rows >> 3 : 7);
+  return a.whole ? Shape{units, 1, n_blk * c, a.over} : Shape{units, n_blk, c, a.over};
 }
 // Row / group: exact below 2^32 / group.
 __device__ __forceinline__ int node_of(const Tree8Params& a, int flat) { return a.group_inverse ? static_cast<int>(__umulhi(static_cast<uint32_t>(flat), a.group_inverse)) : flat; }
@@ -331,7 +335,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
   __syncthreads();
   tc_fence_after_sync();
   pdl_wait();                          // lengths, tables, pages and q may come from the kernel before
-  const Span span = make_span(a.rows, MIN_SPAN, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return shape8<NC>(a, p); });
+  const Span span = make_span(a.rows, MIN_SPAN<NC>, a.small, &shared_span, warp_sums, [&](const SeqPart& p) { return shape8<NC>(a, p); });
   const uint32_t tmem = tmem_slot;
   Cursor cur(span);
   Item it{};
@@ -942,9 +946,10 @@ int64_t set_sizes(Tree8Params& p, const TreeAttention8& t, int* columns) {
   p.group_inverse = p.group == 1 ? 0u : static_cast<uint32_t>((UINT64_C(1) << 32) / p.group + ((UINT64_C(1) << 32) % p.group != 0));
   const int64_t rows = static_cast<int64_t>(t.rows.max_nodes) * p.group;
   *columns = rows <= 16 ? 16 : 32;
-  // A unit's own cost in blocks (its Q, its rows' end).  64 x 2500 slots with 1 / 2 / 3 / 4 / 6: 62.6 / 62.5 / 62.3 / 62.5 / 64.5 us; trees of 26 with
-  // 2 / 4 / 8 / 11: 148 / 137 / 136 / 135, chains of 7 on 2 x 33024 slots 41.4 / 39.5 / 37.4 / 37.7.  (Tiles of a prompt made equally large: no change.)
-  p.over = *columns == 16 ? 3 : 8;
+  // A unit's own cost (its Q, its rows' end), on the scale of its blocks'.  64 x 2500 slots with 1 / 2 / 3 / 4 / 6 blocks: 62.6 / 62.5 / 62.3 /
+  // 62.5 / 64.5 us; trees of 26 with about 2 / 4 / 8 / 11: 148 / 137 / 136 / 135 (of an earlier form), chains of 7 on 2 x 33024 slots 41.4 /
+  // 39.5 / 37.4 / 37.7.  (Tiles of a prompt made equally large: no change.)
+  p.over = *columns == 16 ? 3 : 90;
   return (rows + *columns - 1) / *columns * t.kv.n_kv_heads;
 }
 
@@ -954,14 +959,14 @@ bool tree_attention_8bit_fits(const TreeAttention8& t) {
   Tree8Params p{};
   int columns;
   const int64_t units = set_sizes(p, t, &columns);
-  return units_fit(t.rows.n_seqs, units, t.rows.max_len, 1, p.over);
+  return units_fit(t.rows.n_seqs, units, t.rows.max_len, max_blk_cost(columns), p.over);
 }
 
 int launch_tree_attention_8bit(const TreeAttention8& t, int n_sms, cudaStream_t s) {
   Tree8Params p{};
   int columns;
   const int64_t units = set_sizes(p, t, &columns);
-  if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, 1, p.over)) return -2;
+  if (!units_fit(p.rows.n_seqs, units, p.rows.max_len, max_blk_cost(columns), p.over)) return -2;
   p.scale_log2 = t.scale * LOG2E;
   p.q = t.q; p.q_stride = t.q_stride;
   p.out = t.out; p.out_stride = t.out_stride; p.lse = t.lse;
@@ -980,7 +985,7 @@ int launch_tree_attention_8bit(const TreeAttention8& t, int n_sms, cudaStream_t 
   if (encode_u8_map(&tm, t.kv.pages, 5, dims, strides, box) != 0) return -1;
   p.whole = p.rows.max_len <= WHOLE_BLOCKS * BLK ? 1 : 0;
   const int n_ctas = std::min(n_sms, MAX_CTAS);
-  p.small = small_batch(p.rows.n_seqs, units, p.rows.max_len, 1, p.over) ? 1 : 0;
+  p.small = small_batch(p.rows.n_seqs, units, p.rows.max_len, max_blk_cost(columns), p.over) ? 1 : 0;
   auto run = [&](auto dim, auto nc) {
     constexpr int D = decltype(dim)::value, NC = decltype(nc)::value;
     return t.kv.bf16 ? launch<D, NC, true>(tm, p, n_ctas, s) : launch<D, NC, false>(tm, p, n_ctas, s);
