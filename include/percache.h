@@ -593,7 +593,7 @@ PERCACHE_API int percache_append_rows_8bit(int32_t device, void* stream, const p
 
 /* percache_tree_attention over 8-bit pages: out = softmax(scale * q . K) V, lse, masks and rows that see nothing as there, with at
  * most 128 query heads per KV head.  Products are formed on the 8-bit values themselves: q (exactly, but for elements below 2^-13 of
- * the row's largest with bf16, 2^-17 with fp16, which are off by up to 2^-22 and 2^-26 of that) and the weights (rounded
+ * the row's largest with bf16, 2^-14 with fp16, which are off by up to 2^-21 and 2^-25 of that) and the weights (rounded
  * like bf16 or fp16 or finer) as sums of 8-bit numbers, accumulated in fp32.  Scales below 2^-32 (and NaN) count as 2^-32, above 2^32 as
  * 2^32; pages outside the pool hold zeros.  A q that holds infinity or NaN gives NaN. */
 PERCACHE_API int percache_tree_attention_8bit(int32_t device, void* stream, const percache_kv8_t* kv, const percache_rows_t* rows,

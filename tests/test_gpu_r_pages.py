@@ -4,8 +4,9 @@ Tolerances.  append_rows: the norm is a sum of D squares, a reciprocal root and 
 values no larger than the pair's length: off by at most (D + 12) * 2^-24 of that length (2^-16 of the head's largest |value| covers it, with the
 gain's spread), then half a step of the stored type.  Without norm and rotation the 8-bit bytes are the oracle's, bit for bit.
 tree_attention_8bit: a score is a sum of D products, exact in 8 bits, accumulated with an error of at most D * 2^-23 of the sum of magnitudes (measured
-2^-21), of q's parts, which leave at most 2^-22 of the row's largest |q| per element; weights are split to half a step of the 16-bit
-type or finer, with an absolute floor of 2^-32 of the row's largest (2^16 slots: 2^-16 of the largest |v|), the output is rounded once.
+2^-21), of q's parts: the row's largest counts 224 or more there, the last part's least step is 2^-9 and it counts 2^-4 (two parts: bf16) of
+that, so half a step, what they leave of an element, is 2^-10 * 2^-4 / 224 < 2^-21 of the row's largest |q| (fp16's third part: less); weights are split
+to half a step of the 16-bit type or finer, with an absolute floor of 2^-32 of the row's largest (2^16 slots: 2^-16 of the largest |v|), the output is rounded once.
 """
 import numpy as np
 import pytest
@@ -144,7 +145,7 @@ class Batch:
         kk = np.abs(np.repeat(np.nan_to_num(k), group, axis=1))
         with np.errstate(invalid="ignore", over="ignore"):
             x = np.einsum("nhd,thd->nht", np.abs(q), kk) * self.d * 2.0 ** -23
-            x += np.abs(q).max(-1)[:, :, None] * kk.sum(-1).T[None] * 2.0 ** -22
+            x += np.abs(q).max(-1)[:, :, None] * kk.sum(-1).T[None] * 2.0 ** -21
         x = np.where(np.isfinite(x) & seen[:, None, :], x * self.scale, 0)
         return x.max(axis=2, initial=0.0)
 
