@@ -471,12 +471,13 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 constexpr int UNIT = PAGE_TOKENS / 2;
 struct Pair {                    // of warps
   int half, barrier;             // which half of the page is this warp's; a hardware barrier of the two
-  float (*amax)[2];              // [turn & 1][half] in shared memory
+  float (*amax)[2];              // [turn & 1][half] in shared memory; turns count on from page to page
+  int turn;
 };
 // Four lanes have a row: lane l the chunks of eight elements l, l + 4, .. of the lower half and of the upper one.
 template <int D, bool BF16, bool EIGHT>
 __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8, const NewRows& r, const RowPlace& p, int j, int lo, int hi, int first_kind, int kinds,
-                                           int step, uint4* mine, const float* gains, const Pair& pair) {
+                                           int step, uint4* mine, const float* gains, Pair& pair) {
   constexpr int LANES = 32 / UNIT, CHUNKS = D / 16 / LANES;
   const int lane = threadIdx.x & 31, l = lane % LANES, s = lane / LANES;     // s: the lane's slot of the unit
   using E = unsigned short;
@@ -571,9 +572,10 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
       if (!is_new) amax = 0.f;
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      if (lane == 0) pair.amax[n & 1][pair.half] = amax;
+      if (lane == 0) pair.amax[pair.turn & 1][pair.half] = amax;
       asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair.barrier) : "memory");
-      const PageScale ps = page_scale(in_use, before, fmaxf(amax, pair.amax[n & 1][pair.half ^ 1]));
+      const PageScale ps = page_scale(in_use, before, fmaxf(amax, pair.amax[pair.turn & 1][pair.half ^ 1]));
+      ++pair.turn;
       if (there) {
         if (lane == 0 && pair.half == 0) *scale_at = ps.scale;
         uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(page_kind) * (PAGE_TOKENS * D) + (pair.half * UNIT + s) * D + l * 8;
@@ -611,7 +613,7 @@ __global__ void __launch_bounds__(UNIT_WARPS * 32, UNIT_BLOCKS) append_units_ker
   const int64_t c = task / parts;
   if (c * ROWS >= r.n_rows) return;
   const int part = static_cast<int>(task % parts), begin = static_cast<int>(c) * ROWS, end = min(begin + ROWS, r.n_rows);
-  const Pair pair{warp & 1, 1 + warp / 2, amax[warp / 2]};
+  Pair pair{warp & 1, 1 + warp / 2, amax[warp / 2], 0};
   each_unit<ROWS>(r, begin, end, [&](const RowPlace& p, int j, int lo, int hi) {
     unit_kinds<D, BF16, EIGHT>(kv, kv8, r, p, j, lo, hi, part, kinds, parts, ring + warp * (DEPTH * CHUNKS * 2 * 32), gains, pair);
   });

@@ -94,6 +94,14 @@ def test_append_of_many_rows_matches_the_oracle(case, cache, dtype):
     r.check(q=not no_q)
 
 
+@pytest.mark.parametrize("hkv, n, rows", [(2, 1000, 66), (6, 340, 67)])
+def test_pages_in_turn_with_an_odd_number_of_heads_a_warp(hkv, n, rows):
+    """The warps of a page's halves go from a page's last head to the next page's first: one and three heads each, values of very different sizes."""
+    r = Rows([(3 + 5 * i % 16, rows) for i in range(n)], hkv=hkv, d=64, norm=False, rope=False, spread=4.0)
+    r.run(q=False)
+    r.check(q=False)
+
+
 def test_many_rows_in_place_beside_other_prompts_rows():
     r = Rows([(3, 4000), (50, 4500)], hq=16, hkv=8, packed=False)
     q = r.q.clone()
