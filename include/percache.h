@@ -618,7 +618,8 @@ typedef struct {
  *  - A parent's full pages (the first length / 16) are shared by its children.  Its other pages, of which the first may be partly
  *    filled, go to its first child; they must be held by that sequence only (whoever forks keeps it so).  The other children
  *    get a copy of the partly filled page, in every layer of every pool.
- *  - Every child gets pages for length + room slots, as far as its row of table_out (table_out_stride entries) goes.  What it lacks comes
+ *  - Every child gets pages for length + room slots, as far as its row of table_out (table_out_stride entries) goes (pages of its
+ *    parent's that lie behind that stay counted: give children rows as long as their parents').  What it lacks comes
  *    from the end of the free list, children in order; what the list cannot give is counted in missing[0], and the
  *    child's held_out and length_out end there.
  *  - refs is brought up to date: a sequence without a child gives all its pages back, and pages that nobody holds any more are put
