@@ -185,7 +185,7 @@ bool dense(const Info& t, int from = 0) {
 
 // Address of a contiguous tensor of one of the types on the device with these sizes (a size below 0: any).
 template <int DIMS>
-void* flat(PyObject* x, const char* name, int allowed, int device, const int64_t (&want)[DIMS], int64_t* last = nullptr) {
+void* flat(PyObject* x, const char* name, int allowed, int device, const int64_t (&want)[DIMS], int64_t* last = nullptr, int64_t* first = nullptr) {
   const Info t = look(x);
   bool ok = (t.type & allowed) != 0 && t.device == device && t.dims == DIMS && dense(t);
   for (int i = 0; i < DIMS; ++i) ok = ok && (want[i] < 0 || t.shape[i] == want[i]);
@@ -202,6 +202,7 @@ void* flat(PyObject* x, const char* name, int allowed, int device, const int64_t
     throw Error{};
   }
   if (last) *last = t.shape[DIMS - 1];
+  if (first) *first = t.shape[0];
   return t.p;
 }
 void* optional(PyObject* x, const char* name, int allowed, int device, int64_t n) {
@@ -454,11 +455,10 @@ PyObject* append_rows(PyObject*, PyObject* const* x, Py_ssize_t n) {
     if (x[14] != Py_None) r.k_gain = static_cast<float*>(flat<1>(x[14], "k_gain", F32, k.device, {k.dim}));
     r.eps = number(x[15]);
     if (x[16] != Py_None) {
-      int64_t s[3] = {0, 0, 0};
-      shape_of(x[16], s);
-      if (s[0] > INT32_MAX) refuse("rope", "fewer positions");
-      r.rope = static_cast<float*>(flat<3>(x[16], "rope", F32, k.device, {-1, k.dim / 2, 2}));
-      r.n_positions = static_cast<int32_t>(s[0]);
+      int64_t positions = 0;
+      r.rope = static_cast<float*>(flat<3>(x[16], "rope", F32, k.device, {-1, k.dim / 2, 2}, nullptr, &positions));
+      if (positions > INT32_MAX) refuse("rope", "fewer positions");
+      r.n_positions = static_cast<int32_t>(positions);
     }
     r.position = static_cast<int32_t*>(optional(x[17], "position", I32, k.device, k.rows));
     if ((x[7] == Py_None) == (x[9] == Py_None) || (x[7] == Py_None) != (x[8] == Py_None) || (x[9] == Py_None) != (x[10] == Py_None))
