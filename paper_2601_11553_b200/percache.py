@@ -37,7 +37,8 @@ EXPORTS = ("percache_create", "percache_destroy", "percache_put_chunk_kv", "perc
            "percache_get_stats", "percache_set_flags", "percache_decode", "percache_set_decode_reserve", "percache_set_store_limit", "percache_chunk_info", "percache_debug_read_plan", "percache_debug_read_ctx", "percache_debug_attn_plan",
            "percache_debug_gemm", "percache_debug_gemm_noalloc", "percache_debug_capture_layers", "percache_debug_fail_layer", "percache_debug_wait_probe", "percache_path_key", "percache_qa_top1", "percache_tree_attention",
            "percache_decode_tree", "percache_accept", "percache_evict_context", "percache_set_weight_decay",
-           "percache_debug_read_weights", "percache_attention_weights", "percache_select_slots", "percache_compact_slots", "percache_ops_status", "percache_strerror")
+           "percache_debug_read_weights", "percache_attention_weights", "percache_select_slots", "percache_compact_slots", "percache_append_rows", "percache_append_rows_8bit",
+           "percache_tree_attention_8bit", "percache_fork_pages", "percache_ops_status", "percache_strerror")
 
 
 class PerCacheError(RuntimeError):
