@@ -10,7 +10,7 @@
 //   2^7 .. 2^15.  The last part is for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
 // The accumulation is fp32's (measured: off by at most 2^-21 of the sum of magnitudes).
 //
-// Bound by HBM: 2 D bytes a slot and KV head.  Measured (bf16, head size 128, 8 KV heads): one token on each of 64 prompts around 2500 slots 62.6 us (329 MB,
+// Bound by HBM: 2 D bytes a slot and KV head.  Measured (bf16, the chains fp16; head size 128, 8 KV heads): one token on each of 64 prompts around 2500 slots 62.6 us (329 MB,
 // 5.3 TB/s; the blocks run at the HBM's rate, the rest is the start, uneven ends and the merge), chains of 7 with four heads a KV head on 2 x 33024
 // slots 37.3 us (136 MB), trees of 26 with two heads a KV head 122 us (339 MB; every prompt has one or two tiles of up to 32 rows, whose softmax
 // takes 0.53 - 0.78 us a block), one token on 512 slots 7.6 us (latency).  One copy per page fetches keys and values of a head: a box of [row group][K, V][8 rows][D
