@@ -3,16 +3,19 @@
 // With s_K, s_V a page's scales, x = scale * s_K (q . k8), and out = sum 2^x' s_V v8 / sum 2^x' (x' in base 2, less a reference).  A block's 128 slots are
 // the MMAs' M side: S^T = K Q^T has a TMEM lane, i.e. a thread, per slot and columns per row (query head of a node), so a page's
 // scales are a thread's own numbers; O^T = V^T P^T has a lane per element of the head.  An 8-bit MMA wants both operands in 8 bits, so q and
-// the weights P = 2^x' s_V are split into sums of e4m3 numbers, each some powers of two below the one before, with columns of their own.
+// the weights P = 2^x' s_V are split into sums of 8-bit numbers, each some powers of two below the one before, with columns of their own.
 // Nothing is unpacked: shared memory sees every byte of the cache twice (copy in, MMA), where forming 16-bit tiles would take seven times.
 //   q: 2 parts (bf16, exact: 8 bits of mantissa are 4 + 4) or 3 (fp16), 2^4 apart, of q * 2^-e with the row's largest in (224, 448].
-//   P: 2 parts 2^4 apart (bf16) or 3 (fp16) and one 2^22 below the first, of the weight as a half: the largest of a row lies in
-//   2^7 .. 2^15.  The last part is for small weights: of a long context's many slots under one heavy one, each is kept to 2^-32 of the largest.
+//   P: 3 parts (bf16) or 4 (fp16), 2^4 apart, of 5 exponent bits and 2 mantissa bits (the MMA takes them beside V's e4m3): a rounding to 3 bits
+//   leaves 2^-4 of a power of two at most, so weights are kept to 2^-11 or 2^-15 of themselves.  A row's largest lies in 2^7 .. 2^15 and a
+//   part's last bit is worth 2^-16, so that holds down to 2^-21 of the largest, and below each is off by at most 2^-32 (bf16) or 2^-36 (fp16) of it.
+//   (e4m3 parts have 4 bits but 2^15 less range.  With two or three of them and one far below for small weights, those below 2^-13 or 2^-17 of the
+//   largest were off by up to 2^-4 of themselves: all that a long context under one heavy slot, or under a page of a larger scale, adds up to.)
 // The accumulation is fp32's (measured: off by at most 2^-21 of the sum of magnitudes).
 //
-// Bound by HBM: 2 D bytes a slot and KV head.  Measured (bf16, the chains fp16; head size 128, 8 KV heads): one token on each of 64 prompts around 2500 slots 62.6 us (329 MB,
+// Bound by HBM: 2 D bytes a slot and KV head.  Measured (bf16, the chains fp16; head size 128, 8 KV heads): one token on each of 64 prompts around 2500 slots 62 us (329 MB,
 // 5.3 TB/s; the blocks run at the HBM's rate, the rest is the start, uneven ends and the merge), chains of 7 with four heads a KV head on 2 x 33024
-// slots 37.3 us (136 MB), trees of 26 with two heads a KV head 122 us (339 MB; every prompt has one or two tiles of up to 32 rows, whose softmax
+// slots 38.2 us (136 MB; with fp16's weights off by 2^-12 37.2), trees of 26 with two heads a KV head 122 us (339 MB; every prompt has one or two tiles of up to 32 rows, whose softmax
 // takes 0.53 - 0.78 us a block), one token on 512 slots 7.6 us (latency).  One copy per page fetches keys and values of a head: a box of [row group][K, V][8 rows][D
 // bytes], so that the row groups of K, and those of V, are one stride apart over all pages of a block.
 // Warps 0-7: softmax (even and odd blocks), 8: copies, 9: S products, 10: O products, 11: splits Q, fetches masks, cleans V.  With one warp for
@@ -33,7 +36,6 @@ constexpr int FLAGS = 8;                        // items a `bad V` flag lives fo
 constexpr int MAX_NODES = 256;             // of a prompt, at most
 // The running reference lies HEADROOM (base 2) below the largest score that set it and is raised when a score exceeds that by RESCALE_THRESHOLD.
 constexpr float HEADROOM = 7.f, RESCALE_THRESHOLD = 8.f;
-constexpr int P_UNIT = 7;                       // the first part of P counts 2^7: at most 2^8, below 448
 template <int NC> constexpr int MIN_SPAN = NC == 16 ? 2 : 24;      // a CTA's least share: two blocks, so that none that a unit reaches is without one
 constexpr int WHOLE_BLOCKS = 6;
 constexpr int PAGES = BLK / PAGE_TOKENS;
@@ -83,30 +85,44 @@ template <int NC, bool BF16> struct Parts {
   static constexpr int USED = 2 * NS + 2 * O_ITEMS * NO;
   static constexpr int TMEM = USED <= 256 ? 256 : 512;
   static_assert(USED <= 512 && NS % 16 == 0 && NO % 16 == 0 && NO <= P_ROW, "");
-  __host__ __device__ static constexpr int shift(int part) { return BF16 ? (part == 0 ? 0 : part == 1 ? 4 : 22) : (part < 3 ? 4 * part : 22); }
+  __host__ __device__ static constexpr float worth(int part) { return 1.0f / static_cast<float>(1 << 4 * part); }    // of a part of P
 };
-__host__ __device__ constexpr float pow2(int e) { return e >= 0 ? static_cast<float>(1u << e) : 1.0f / static_cast<float>(1u << -e); }
 
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
-__device__ __forceinline__ uint32_t e4m3x2_of(__half2 x) {
+// To bytes of 5 exponent bits and 2 mantissa bits, to nearest even, and back: such a byte is a half's upper one.
+__device__ __forceinline__ uint32_t e5m2x2_of(__half2 x) {
   uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&x)));
+  asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&x)));
   return r;
 }
-__device__ __forceinline__ __half2 half2_of(uint32_t e4m3x2) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(e4m3x2)));
-  return as_half2(h);
+__device__ __forceinline__ uint32_t e5m2x2_of(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
 }
-// The parts of two weights (at most 2^15), 16 bits each.  What is left after a part is exact in a half: a multiple of its last bit.
-template <typename X>
+__device__ __forceinline__ __half2 half2_of(uint32_t e5m2x2) { return as_half2(__byte_perm(e5m2x2, 0u, 0x1404)); }
+// The parts of two weights (at most 2^15), 16 bits each.  What a part leaves is at most 2^11 and exact in a half, also as 16 times as much: a
+// multiple of the last bit.  bf16 takes the weight as a half, whose own rounding (2^-12 of the next power of two) is less than the parts'; fp16's four keep
+// more, so its first part is the weight's itself and the half is what that leaves.
+template <typename X, bool BF16>
 __device__ __forceinline__ void split_weights(float w0, float w1, uint32_t (&out)[X::P]) {
-  __half2 r = __floats2half2_rn(w0, w1);
+  const __half2 sixteen = __float2half2_rn(16.f);
+  __half2 r;
+  if constexpr (BF16) {
+    r = __floats2half2_rn(w0, w1);
+    out[0] = e5m2x2_of(r);
+    r = __hmul2(__hsub2(r, half2_of(out[0])), sixteen);
+  } else {
+    out[0] = e5m2x2_of(w0, w1);
+    const float2 f = __half22float2(half2_of(out[0]));
+    float r0, r1;
+    unpack_f32x2(fma_f32x2(pack_f32x2(f.x, f.y), pack_f32x2(-16.f, -16.f), mul_f32x2(pack_f32x2(w0, w1), pack_f32x2(16.f, 16.f))), r0, r1);
+    r = __floats2half2_rn(r0, r1);
+  }
 #pragma unroll
-  for (int part = 0; part < X::P; ++part) {
-    const int e = X::shift(part) - P_UNIT;
-    out[part] = e4m3x2_of(__hmul2(r, __float2half2_rn(pow2(e))));
-    if (part + 1 < X::P) r = __hfma2(half2_of(out[part]), __float2half2_rn(-pow2(-e)), r);
+  for (int part = 1; part < X::P; ++part) {
+    out[part] = e5m2x2_of(r);
+    if (part + 1 < X::P) r = __hmul2(__hsub2(r, half2_of(out[part])), sixteen);
   }
 }
 
@@ -500,7 +516,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
     while (ok && next_item<NC>(cur, a, &it)) {
       const int nb = it.blk_end - it.blk_begin, par = n_item & 1;
       if (warp == 9) {
-        const uint32_t idesc = make_idesc_e4m3(BLK, (((it.n_rows + 1) & ~1) * X::Q + 15) & ~15, 0, 0);
+        const uint32_t idesc = make_idesc_8bit(BLK, (((it.n_rows + 1) & ~1) * X::Q + 15) & ~15, E4M3, E4M3, 0, 0);
         const uint64_t q_desc = desc(smem_u32(q_smem + par * Q_BYTES), GROUP_BYTES);
         wait(&q_full[par], (n_item >> 1) & 1u);
 #pragma unroll 1
@@ -528,7 +544,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
       } else {
         const int ob = X::O_ITEMS == 2 ? par : 0;
         const uint32_t o_uses = X::O_ITEMS == 2 ? n_item >> 1 : n_item;
-        const uint32_t idesc = make_idesc_e4m3(BLK, (((it.n_rows + 1) & ~1) * X::P + 15) & ~15, 1, 1);     // A = V^T, B = P^T: the K index is the slot
+        const uint32_t idesc = make_idesc_8bit(BLK, (((it.n_rows + 1) & ~1) * X::P + 15) & ~15, E4M3, E5M2, 1, 1);     // A = V^T, B = P^T: the K index is the slot
         wait(&o_free[ob], (o_uses & 1u) ^ 1u);
 #pragma unroll 1
         for (int j = 0; j < nb && ok; ++j) {
@@ -666,9 +682,9 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
         }
         if (j != i) raise = parity_any(i, raise);
         if (raise) {
-          // The rows' exact block maxima: a warp's by a transposing reduction, the block's from four words a row; lane c then works
-          // out row c's new reference and every thread fetches it by shuffles.  Two buffers: between two uses of one lies the
-          // other's barrier.
+          // The rows' exact block maxima: a warp's by one instruction a row, the block's from four words a row; lane c then works
+          // out row c's new reference, every thread reads it from shared memory, and what the present scores lose comes by shuffles.  Two
+          // buffers: between two uses of one lies the other's barrier.
           float(*maxima)[4] = block_max[i][n_raise++ & 1];
           float mine = -INFINITY;                          // lane c: row c's
 #pragma unroll
@@ -737,7 +753,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
                 const int k = c0 + c + 2 * u;
                 const float w0 = fast_exp2(t[k]), w1 = fast_exp2(t[k + 1]);
                 l[k / 2] = fma_f32x2(pack_f32x2(w0, w1), inv_v2, l[k / 2]);   // the row sum has the weights without s_V, and before they are split
-                split_weights<X>(w0, w1, two[u]);
+                split_weights<X, BF16>(w0, w1, two[u]);
               }
 #pragma unroll
               for (int e = 0; e < X::P; ++e) {
@@ -828,8 +844,8 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int at = (e >> 1) * 2 * X::P + part * 2 + (e & 1);
-              o0[e] = fmaf(__uint_as_float(x0[at]), pow2(P_UNIT - X::shift(part)), o0[e]);
-              o1[e] = fmaf(__uint_as_float(x1[at]), pow2(P_UNIT - X::shift(part)), o1[e]);
+              o0[e] = fmaf(__uint_as_float(x0[at]), X::worth(part), o0[e]);
+              o1[e] = fmaf(__uint_as_float(x1[at]), X::worth(part), o1[e]);
             }
           }
 #pragma unroll

@@ -221,7 +221,7 @@ __device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint64_t adesc, uint64_
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// The same on 8-bit inputs (see make_idesc_e4m3).
+// The same on 8-bit inputs (see make_idesc_8bit).
 __device__ __forceinline__ void umma_ss_8bit(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
                                              uint32_t accumulate) {
   asm volatile(
@@ -380,10 +380,11 @@ __device__ __forceinline__ uint64_t make_smem_desc_sw128(uint32_t smem_addr, uin
 __device__ __forceinline__ uint64_t make_smem_desc_sw64(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
   return (make_smem_desc_sw128(smem_addr, lbo_bytes, sbo_bytes) & ~(7ull << 61)) | (4ull << 61);
 }
-// Instruction descriptor for kind::f8f6f4: fp32 accumulator, A and B both e4m3 (format 0), 32 elements of K.  The other fields are
+// Instruction descriptor for kind::f8f6f4: fp32 accumulator, A and B of a format each, 32 elements of K.  The other fields are
 // those of make_idesc_f16.  An MN-major operand's 128-byte rows hold 128 elements of M or N.
-__host__ __device__ constexpr uint32_t make_idesc_e4m3(int m, int n, int a_mn_major, int b_mn_major) {
-  return (1u << 4) | (static_cast<uint32_t>(a_mn_major) << 15) | (static_cast<uint32_t>(b_mn_major) << 16) |
+constexpr uint32_t E4M3 = 0, E5M2 = 1;
+__host__ __device__ constexpr uint32_t make_idesc_8bit(int m, int n, uint32_t a_format, uint32_t b_format, int a_mn_major, int b_mn_major) {
+  return (1u << 4) | (a_format << 7) | (b_format << 10) | (static_cast<uint32_t>(a_mn_major) << 15) | (static_cast<uint32_t>(b_mn_major) << 16) |
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 // Instruction descriptor for kind::f16: fp32 accumulator, A and B both fp16 (0) or both bf16 (1).
