@@ -586,7 +586,7 @@ PERCACHE_API int percache_append_rows(int32_t device, void* stream, const percac
 /* The same into 8-bit pages.  A page that gets rows takes, for its keys and for its values of every KV head, the scale 2^e with the least
  * e in -32 .. 32 for which the largest finite |value| of its new rows is at most 448 * 2^e.  Where slots below the first new one are in
  * use and the page's scale (taken to lie within 2^-32 .. 2^32) is larger, that stays; where it is smaller, their bytes are rounded again to the new one (exact but
- * for values below 2^-6 of it).  Values are rounded to nearest, ties to even; beyond 448 * 2^e (infinities, or e at 32) they
+ * for values below 2^-6 of it, if the old one is a power of two).  Values over the scale are rounded once, to nearest, ties to even; beyond 448 * 2^e (infinities, or e at 32) they
  * become the largest; NaN stays NaN.  Slots behind the last new one are left as they were.  A page with new rows of a prompt must not be any
  * other prompt's. */
 PERCACHE_API int percache_append_rows_8bit(int32_t device, void* stream, const percache_kv8_t* kv, const percache_new_rows_t* rows);

@@ -305,19 +305,39 @@ __device__ __forceinline__ float largest(const Part& x) {                      /
   }
   return m;
 }
-// The scale of a page's keys or values with new values up to amax; before: what it has, which counts if slots are in use.
+__device__ __forceinline__ bool is_power_of_two(float x) { return (__float_as_uint(x) & 0x7fffffu) == 0u; }       // of scales: normal numbers
+// The scale of a page's keys or values with new values up to amax; before: what it has, which counts if slots are in use.  It need not be a power of
+// two (somebody else may have written the page): quotients and products by one that is not are rounded, and a second rounding, to 8 bits, could
+// take a value for the border of two bytes that it only lies next to.  So the first one is towards zero with a last bit that says that it left something.
 struct PageScale {
-  float scale, inv, again;       // again: what it was over what it is, or 1: bytes in use stay
+  float scale, inv, again;       // inv: exact, or 0: divide; again: what it was over what it is, or 1: bytes in use stay
 };
+__device__ __forceinline__ float over_scale(float x, float scale) {
+  const float q = __fdiv_rz(x, scale);
+  return fabsf(q) < INFINITY && fmaf(-q, scale, x) != 0.f ? __uint_as_float(__float_as_uint(q) | 1u) : q;
+}
+__device__ __forceinline__ float times_again(float x, float again) {
+  const float y = __fmul_rz(x, again);
+  return fmaf(x, again, -y) != 0.f ? __uint_as_float(__float_as_uint(y) | 1u) : y;
+}
 __device__ __forceinline__ PageScale page_scale(bool in_use, float before, float amax) {
   const float want = power_of_two(scale_exponent(amax)), have = in_use ? fminf(fmaxf(before, 0x1p-32f), 0x1p32f) : 0.f, scale = fmaxf(have, want);
-  const float inv = 1.0f / scale;
-  return PageScale{scale, inv, have >= want ? 1.f : have * inv};
+  const float inv = is_power_of_two(scale) ? 1.0f / scale : 0.f;
+  return PageScale{scale, inv, have >= want ? 1.f : have * inv};          // (a scale that grows is a power of two)
 }
 // A row's values as bytes, from element 8 l of its lower half on.
 template <int D>
-__device__ __forceinline__ void store_row(uint8_t* to, const Part& x, float inv) {
-  const Two by = two(inv, inv);
+__device__ __forceinline__ void store_row(uint8_t* to, Part x, const PageScale& ps) {
+  Two by = two(ps.inv, ps.inv);
+  if (ps.inv == 0.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 a = floats(x.lo[e]), b = floats(x.hi[e]);
+      x.lo[e] = two(over_scale(a.x, ps.scale), over_scale(a.y, ps.scale));
+      x.hi[e] = two(over_scale(b.x, ps.scale), over_scale(b.y, ps.scale));
+    }
+    by = two(1.f, 1.f);
+  }
   auto bytes = [&](Two a, Two b) {
     const float2 x = floats(a * by), y = floats(b * by);
     return pack_e4m3x2(x.x, x.y) | pack_e4m3x2(y.x, y.y) << 16;
@@ -330,10 +350,12 @@ __device__ __forceinline__ void round_again(uint8_t* to, const PageScale& ps) {
   if (ps.again == 1.f) return;
   const uint2 a = *reinterpret_cast<uint2*>(to), b = *reinterpret_cast<uint2*>(to + D / 2);
   uint32_t w[4] = {a.x, a.y, b.x, b.y};
+  const bool exact = is_power_of_two(ps.again);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 y = unpack_e4m3x2(w[e] & 0xffffu), z = unpack_e4m3x2(w[e] >> 16);
-    w[e] = pack_e4m3x2(y.x * ps.again, y.y * ps.again) | pack_e4m3x2(z.x * ps.again, z.y * ps.again) << 16;
+    if (exact) w[e] = pack_e4m3x2(y.x * ps.again, y.y * ps.again) | pack_e4m3x2(z.x * ps.again, z.y * ps.again) << 16;
+    else w[e] = pack_e4m3x2(times_again(y.x, ps.again), times_again(y.y, ps.again)) | pack_e4m3x2(times_again(z.x, ps.again), times_again(z.y, ps.again)) << 16;
   }
   *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
   *reinterpret_cast<uint2*>(to + D / 2) = make_uint2(w[2], w[3]);
@@ -421,7 +443,7 @@ __device__ __forceinline__ void fill_page(const Kv8View& kv, const NewRows& r, c
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const int s = g + GROUPS * u;
-      if (s >= lo && s < hi) store_row<D>(dst + s * D, x[u], ps.inv);
+      if (s >= lo && s < hi) store_row<D>(dst + s * D, x[u], ps);
       else if (s < lo) round_again<D>(dst + s * D, ps);
     }
   }
@@ -581,7 +603,7 @@ __device__ __forceinline__ void unit_kinds(const KvView& kv, const Kv8View& kv8,
         uint8_t* dst = static_cast<uint8_t*>(const_cast<void*>(kv8.pages)) + page * kv8.page_stride + static_cast<size_t>(page_kind) * (PAGE_TOKENS * D) + (pair.half * UNIT + s) * D + l * 8;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-          if (is_new) store_row<D>(dst + c * (LANES * 8), x[c], ps.inv);
+          if (is_new) store_row<D>(dst + c * (LANES * 8), x[c], ps);
           else if (s < lo) round_again<D>(dst + c * (LANES * 8), ps);
         }
       }
