@@ -628,8 +628,8 @@ typedef struct {
  *  - refs is brought up to date: a sequence without a child gives all its pages back, and pages that nobody holds any more are put
  *    behind the free list's rest in ascending order.
  *  - table_out[i]: the held_out[i] pages, then -1.  A parent outside 0 .. n_seqs - 1 makes an empty child.
- * refs_out, free_list_out, free_count_out may be refs, free_list, free_count (each its own, all three or none); table_out must not be
- * page_table, held_out not held, length_out not length.  Page ids outside 0 .. n_pages - 1 are passed on, and neither counted nor copied.
+ * refs_out, free_list_out, free_count_out may be refs, free_list, free_count (each its own, all three or none); apart from that no array that
+ * is written, the workspace among them, may overlap another array of the call (PERCACHE_E_INVAL).  Page ids outside 0 .. n_pages - 1 are passed on, and neither counted nor copied.
  * A page taken from the free list must not be held.  refs, free_list: int32 [n_pages]; n_pages 1 .. 2^26;
  * n_seqs and n_children at most PERCACHE_MAX_FORK_SEQS; rows of at most 2^22 pages; room 0 .. 2^26.  n_children 0 gives everything back.
  * workspace: as for percache_tree_attention (it need not be zeroed for this call). */

@@ -141,6 +141,29 @@ NewRows new_rows(const percache_new_rows_t& r) {
   return n;
 }
 
+// Arrays of a fork: blocks write one while others read, or write, another.
+struct Array {
+  const void* p;
+  int64_t n;                                    // int32 numbers
+};
+bool apart(const Array& a, const Array& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.n == 0 || b.n == 0 || x + static_cast<uint64_t>(a.n) * 4 <= y || y + static_cast<uint64_t>(b.n) * 4 <= x;
+}
+bool fork_arrays_apart(const percache_fork_t& f, const void* workspace) {
+  const Array in[] = {{f.refs, f.n_pages}, {f.free_list, f.n_pages}, {f.free_count, 1}, {f.page_table, static_cast<int64_t>(f.n_seqs) * f.page_table_stride},
+                      {f.held, f.n_seqs}, {f.length, f.n_seqs}, {f.parent, f.n_children}};
+  const Array out[] = {{f.refs_out, f.n_pages}, {f.free_list_out, f.n_pages}, {f.free_count_out, 1}, {f.table_out, static_cast<int64_t>(f.n_children) * f.table_out_stride},
+                       {f.held_out, f.n_children}, {f.length_out, f.n_children}, {f.missing, 1}, {workspace, PERCACHE_OPS_WORKSPACE_BYTES / 4}};
+  for (int o = 0; o < 8; ++o) {
+    for (int i = 0; i < 7; ++i)
+      if (!apart(out[o], in[i]) && !(o == i && o < 3 && out[o].p == in[i].p)) return false;      // the first three: in place
+    for (int i = 0; i < o; ++i)
+      if (!apart(out[o], out[i])) return false;
+  }
+  return true;
+}
+
 bool pool_ok(const percache_pool_t& p) {
   return p.base && aligned(p.base, 4) && p.page_bytes > 0 && p.page_bytes % 4 == 0 && p.page_bytes <= (INT64_C(1) << 32) && p.page_stride % 4 == 0 &&
          p.page_stride >= p.page_bytes && p.page_stride <= (INT64_C(1) << 36) && p.layer_stride % 4 == 0 && p.layer_stride >= 0 &&
@@ -284,8 +307,7 @@ int percache_fork_pages(int32_t device, void* stream, const percache_fork_t* f, 
   if (!f || f->n_seqs < 0 || f->n_children < 0 || f->n_seqs > MAX_FORK_SEQS || f->n_children > MAX_FORK_SEQS) return PERCACHE_E_INVAL;
   const bool in_place = f->refs_out == f->refs;
   if ((f->n_seqs > 0 && (!f->page_table || !f->held || !f->length || f->page_table_stride < 1 || f->page_table_stride > (1 << 22))) ||
-      (f->n_children > 0 && (!f->parent || !f->table_out || !f->held_out || !f->length_out || f->table_out_stride < 1 || f->table_out_stride > (1 << 22) ||
-                             f->table_out == f->page_table || f->held_out == f->held || f->length_out == f->length)) ||
+      (f->n_children > 0 && (!f->parent || !f->table_out || !f->held_out || !f->length_out || f->table_out_stride < 1 || f->table_out_stride > (1 << 22))) ||
       f->n_pages <= 0 || f->n_pages > (INT64_C(1) << 26) || !f->refs || !f->free_list || !f->free_count || !f->refs_out || !f->free_list_out ||
       !f->free_count_out || !f->missing || (f->free_list_out == f->free_list) != in_place || (f->free_count_out == f->free_count) != in_place ||
       f->room < 0 || f->room > MAX_CONTEXT || f->n_pools < 0 || f->n_pools > PERCACHE_MAX_POOLS || (f->n_pools > 0 && !f->pools))
@@ -298,6 +320,7 @@ int percache_fork_pages(int32_t device, void* stream, const percache_fork_t* f, 
     k.pools[i] = Pool{static_cast<char*>(p.base), p.page_bytes, p.page_stride, p.layer_stride, p.n_layers, wide ? 16 : 4};
   }
   if (!workspace_ok(workspace, workspace_bytes)) return workspace && aligned(workspace, 256) ? PERCACHE_E_CAPACITY : PERCACHE_E_INVAL;
+  if (!fork_arrays_apart(*f, workspace)) return PERCACHE_E_INVAL;
   k.n_seqs = f->n_seqs; k.n_children = f->n_children; k.width = f->page_table_stride; k.width_out = f->table_out_stride;
   k.room = f->room; k.n_pools = f->n_pools; k.table = f->page_table; k.held = f->held; k.length = f->length; k.parent = f->parent;
   k.table_out = f->table_out; k.held_out = f->held_out; k.length_out = f->length_out; k.n_pages = f->n_pages;
