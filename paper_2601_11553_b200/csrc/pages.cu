@@ -1,10 +1,9 @@
 // Sequences that go on as others: page tables, counters, the free list, and copies of the pages that two of them would write.
 //
 // Three things depend on each other: how many pages every child takes (a prefix sum over the children), the counters (a page is free when the last
-// holder lets go), and the free list (freed pages in ascending order).  fork_small_kernel: up to 512 sequences and 8192 pages, outputs in arrays of their own; every block
+// holder lets go), and the free list (freed pages in ascending order).  fork_small_kernel: few sequences, table entries and pages, outputs in arrays of their own; every block
 // works the children out for itself, the first one has the counters (in shared memory) and the list, the others tables and copies, and nobody
-// waits for anybody.  Against two kernels (8-bit pages, one prompt to 4 samples / 16 / 64 / 128 / 500 beams): 7.7 / 8.7 / 10.9 / 13.5 / 15.2 and
-// 10.3 / 13.8 / 15.0 / 17.1 / 17.6 us.  Else those two.  fork_plan_kernel: one block works the children out, while the
+// waits for anybody (one prompt to 4 samples 7.5 us, two kernels 8.6).  Else two.  fork_plan_kernel: one block works the children out, while the
 // others clear the marks of freed pages and, where the outputs are arrays of their own, copy the counters and the list.  fork_kernel: tables,
 // counters and copies by all blocks; the block that is last with its tables and counters lists the freed pages, while the others copy on.
 // Bound by HBM where pages are copied (each read once, written once): 64 beams of a 28-layer cache, 143 MB, 23.5 us; else by latency.
@@ -44,7 +43,7 @@ __device__ __forceinline__ Seq seq_of(const Fork& f, int s) {
   return q;
 }
 
-// Inclusive sum over a block of 1024 threads; `total`: of all.
+// Inclusive sum over the block's threads (up to 1024); `total`: of all.
 __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* warp_sums, int64_t* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
@@ -150,11 +149,16 @@ __device__ __forceinline__ void copy_chunk(const Fork& f, int2 pair, int chunk) 
 }
 
 // ---------------------------------------------------------------------------------------------------- one kernel
-constexpr int SMALL_SEQS = 512, SMALL_PAGES = 8192, SMALL_ENTRIES = 65536, SMALL_THREADS = 512;
+// Where it is the faster one: the first block walks all counters, the list, and the pages of sequences that end or go on as several, which grows with the
+// pages and with the tables' entries; the two kernels' time hardly does.  Device us, one kernel / two, without copies (every sequence goes on, or a
+// quarter of them does): 4096 pages, one prompt of 127 pages to 4 samples 7.5 / 8.6, to 500 10.3 / 12.0; 16 beams of 127 pages 7.9 / 11.0 or 8.6 / 12.4, 64
+// beams of 127 10.4 / 11.6 or 12.4 / 14.7; past the limits 128 beams of 127 pages 12.9 / 12.2 or 17.1 / 15.6, 256 of 34 11.7 / 11.9 or 16.3 / 15.0, 500 of 65
+// 18.4 / 14.2 or 31.9 / 18.3, and on 8192 pages the sample 9.5 / 8.6, 64 beams of 127 12.5 / 11.5 or 14.5 / 15.0.
+constexpr int SMALL_SEQS = 128, SMALL_CHILDREN = 512, SMALL_PAGES = 4096, SMALL_ENTRIES = 10240, SMALL_THREADS = SMALL_CHILDREN;
 struct SmallPlan {
   int32_t first[SMALL_SEQS], kids[SMALL_SEQS];
-  Child child[SMALL_SEQS];
-  int2 copy[SMALL_SEQS];
+  Child child[SMALL_CHILDREN];
+  int2 copy[SMALL_CHILDREN];
 };
 __global__ void __launch_bounds__(SMALL_THREADS) fork_small_kernel(const __grid_constant__ Fork f, int chunks) {
   __shared__ SmallPlan plan;
@@ -171,8 +175,10 @@ __global__ void __launch_bounds__(SMALL_THREADS) fork_small_kernel(const __grid_
     for (int i = tid; i < (n_pages + 31) / 32; i += SMALL_THREADS) marks[i] = 0u;
     for (int i = tid; i < n_pages; i += SMALL_THREADS) f.free_list_out[i] = ld_dep_s32(f.free_list + i);
   }
-  plan.first[tid] = INT32_MAX;
-  plan.kids[tid] = 0;
+  if (tid < SMALL_SEQS) {
+    plan.first[tid] = INT32_MAX;
+    plan.kids[tid] = 0;
+  }
   __syncthreads();
   if (tid < f.n_children) {
     const int p = ld_dep_s32(f.parent + tid);
@@ -393,7 +399,7 @@ int launch_fork(const Fork& f, int n_sms, cudaStream_t s) {
   // as many blocks as there is work at most: rows of tables, and the copies if every child but one makes one
   const int64_t work = std::max<int64_t>(f.n_children, chunks * std::max(f.n_children - 1, 0));
   // (in place the first block would change what blocks that start later still have to read)
-  if (f.refs_out != f.refs && f.n_seqs <= SMALL_SEQS && f.n_children <= SMALL_SEQS && f.n_pages <= SMALL_PAGES && static_cast<int64_t>(f.n_seqs) * f.width <= SMALL_ENTRIES) {
+  if (f.refs_out != f.refs && f.n_seqs <= SMALL_SEQS && f.n_children <= SMALL_CHILDREN && f.n_pages <= SMALL_PAGES && static_cast<int64_t>(f.n_seqs) * f.width <= SMALL_ENTRIES) {
     const int others = static_cast<int>(std::max<int64_t>(std::min<int64_t>(work, static_cast<int64_t>(n_sms) * 4 - 1), 1));
     return launch_pdl(fork_small_kernel, dim3(1 + others), dim3(SMALL_THREADS), static_cast<size_t>(f.n_pages) * 4, s, f, static_cast<int>(chunks)) == cudaSuccess ? 0 : -1;
   }
