@@ -565,7 +565,7 @@ typedef struct {
   const int32_t* row_start;        /* [n_seqs + 1], ascending                                                     */
   const int32_t* position;         /* [n_rows] row of `rope` for each row, or NULL: its slot                      */
   const void* q;                   /* [n_rows][n_q_heads][head_dim], or NULL: keys and values only                */
-  void*       q_out;               /* like q; may be q itself (with q's stride)                                   */
+  void*       q_out;               /* like q; may be q itself (with q's stride), else no part of q, k or v        */
   const void* k;                   /* [n_rows][n_kv_heads][head_dim]                                              */
   const void* v;
   int64_t q_row_stride, q_out_row_stride, k_row_stride, v_row_stride;   /* elements, multiples of 8               */

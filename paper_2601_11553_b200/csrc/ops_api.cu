@@ -118,6 +118,15 @@ bool rows16_ok(const void* p, int64_t stride, int32_t heads, int32_t dim) {
   return p && aligned(p, 16) && stride % 8 == 0 && stride >= static_cast<int64_t>(heads) * dim && stride <= (INT64_C(1) << 35);
 }
 
+// Whether two sets of rows of 16-bit elements, of `a_dim` and `b_dim` elements each, share none.  Rows side by side have one stride.
+bool rows_apart(const void* a, int64_t a_stride, int64_t a_dim, const void* b, int64_t b_stride, int64_t b_dim, int64_t n) {
+  const int64_t x = reinterpret_cast<intptr_t>(a), y = reinterpret_cast<intptr_t>(b), as = a_stride * 2, bs = b_stride * 2, aw = a_dim * 2, bw = b_dim * 2;
+  if (x + (n - 1) * as + aw <= y || y + (n - 1) * bs + bw <= x) return true;
+  if (as != bs) return false;
+  const int64_t d = ((y - x) % as + as) % as;
+  return d >= aw && d + bw <= as;
+}
+
 // What does not depend on whether there are rows, then what does.
 bool new_rows_ok(const percache_new_rows_t* r) {
   return r && r->n_seqs >= 0 && r->n_seqs <= 65535 && r->n_rows >= 0 && r->max_len >= 1 && r->max_len <= MAX_CONTEXT;
@@ -126,7 +135,11 @@ bool new_rows_ok(const percache_new_rows_t* r, int32_t n_kv_heads, int32_t dim) 
   return r->ctx_len && r->row_start && n_kv_heads <= MAX_HEADS && rows16_ok(r->k, r->k_row_stride, n_kv_heads, dim) &&
          rows16_ok(r->v, r->v_row_stride, n_kv_heads, dim) &&
          (!r->q || (r->n_q_heads > 0 && r->n_q_heads <= MAX_HEADS && rows16_ok(r->q, r->q_row_stride, r->n_q_heads, dim) &&
-                    rows16_ok(r->q_out, r->q_out_row_stride, r->n_q_heads, dim) && (r->q_out != r->q || r->q_out_row_stride == r->q_row_stride))) &&
+                    rows16_ok(r->q_out, r->q_out_row_stride, r->n_q_heads, dim) &&
+                    ((r->q_out == r->q && r->q_out_row_stride == r->q_row_stride) ||
+                     rows_apart(r->q_out, r->q_out_row_stride, r->n_q_heads * dim, r->q, r->q_row_stride, r->n_q_heads * dim, r->n_rows)) &&
+                    rows_apart(r->q_out, r->q_out_row_stride, r->n_q_heads * dim, r->k, r->k_row_stride, n_kv_heads * dim, r->n_rows) &&
+                    rows_apart(r->q_out, r->q_out_row_stride, r->n_q_heads * dim, r->v, r->v_row_stride, n_kv_heads * dim, r->n_rows))) &&
          aligned(r->q_gain, 16) && aligned(r->k_gain, 16) && aligned(r->rope, 16) && (!r->rope || r->n_positions > 0) &&
          r->eps >= 0.f && std::isfinite(r->eps);
 }
