@@ -10,8 +10,8 @@
 // the maximum and the rounding; other blocks write the queries.  append_units_kernel (many rows of long prompts, either cache): a warp has eight
 // rows, and takes their heads one after the other through a ring of asynchronous copies.
 // Measured, 16 query and 8 KV heads of 128 elements: one row 2.6 us, 64 single rows into 8-bit pages 4.6 us (latency); 33024 rows into a 16-bit
-// context 90 us (6.0 TB/s), 11.6 thousand rows of 8 prompts into 8-bit pages 44.6 us (3.6 TB/s: instruction issue, 430 a warp for eight rows of a
-// head, of which 40 for the page's maximum).
+// context 90 us (6.2 TB/s), 11.6 thousand rows of 8 prompts into 8-bit pages 44.6 us (3.6 TB/s: 430 instructions a warp for eight rows of a
+// head, of which 40 for the page's maximum, at half the issue rate: four warps a scheduler wait for their own results, loads and shuffles).
 #include <algorithm>
 
 #include "slot_row.cuh"
@@ -649,9 +649,10 @@ int run_of(int64_t rows, int heads, int n_sms) {
 }
 
 // Whether units of rows are the faster form: from enough heads of rows on that a warp's eight or so in turn do not leave the GPU half empty, and if
-// units are full on average.  With 16 + 2 x 8 heads, rows or pages against units: into 8-bit pages 2048 rows of one prompt 15.1 / 18.4 us, 4096 20.8 / 20.9,
-// 8192 38.5 / 28.3, of 64 prompts 36.2 / 36.1, 16000 of 500 prompts 64 / 69.5, 32000 122.7 / 111.6; into 16-bit pages 2048 10.9 / 14.6, 4096
-// 21.0 / 17.5, of 64 prompts 19.7 / 19.2, 8000 of 500 35.8 / 34.8.
+// units are full on average.  With 16 + 2 x 8 heads of 128, rows or pages against units: into 8-bit pages 2048 rows of one prompt 13.0 / 14.2 us, 4096
+// 18.7 / 15.3, 6000 21.9 / 22.7, 8192 31.8 / 27.6, 64 prompts of 100 rows 24.5 / 31.3, of 128 30.9 / 26.6, 500 of 32 58.2 / 49.3, of 64 111.8 / 93.9; into
+// 16-bit pages 1024 9.2 / 8.8, 2048 8.9 / 11.0, 4096 15.4 / 11.9, 6000 25.8 / 19.3, 8192 36.0 / 26.0, 64 prompts of 64 15.3 / 12.0, 500 of 8 16.6 / 12.3, of 16
+// 34.6 / 25.9; 8192 rows of heads of 64 into 8-bit pages 15.3 / 17.9, 16-bit 14.9 / 13.7.
 bool units_pay(const NewRows& r, int kinds, bool eight) {
   return static_cast<int64_t>(r.n_rows) * kinds >= (eight ? 1 << 18 : 1 << 17) && r.n_rows / r.n_seqs >= (eight ? 64 : 16);
 }
@@ -682,9 +683,10 @@ int append(const KvView& kv, const NewRows& r, int n_sms, cudaStream_t s) {
 template <int D, bool BF16>
 int append8(const Kv8View& kv, const NewRows& r, int n_sms, cudaStream_t s) {
   if (units_pay(r, (r.q ? r.n_q_heads : 0) + 2 * kv.n_kv_heads, true)) return append_units<D, BF16, true>(KvView{}, kv, r, s);
-  // Rows of a warp: about as many as a prompt has, so that batches of single tokens spread over the warps and long prompts have a page each.
+  // Rows of a warp: about as many as a prompt has, so that batches of single tokens spread over the warps and long prompts have a page each (with
+  // eight rows half of the warps own none: 500 prompts of 32 rows 68.5 -> 58.2 us, 20000 rows of one KV head 23.7 -> 20.8).
   const int per = r.n_rows / r.n_seqs;
-  const int chunk = per >= 8 ? 8 : per >= 4 ? 4 : per >= 2 ? 2 : 1;
+  const int chunk = per >= 16 ? 16 : per >= 8 ? 8 : per >= 4 ? 4 : per >= 2 ? 2 : 1;
   const int64_t chunks = (static_cast<int64_t>(r.n_rows) + chunk - 1) / chunk;
   // Keys and values of a warp, one behind the other: four where that leaves enough warps.
   const int all = 2 * kv.n_kv_heads, kinds = chunks * ((all + 3) / 4) >= static_cast<int64_t>(n_sms) * WARPS ? 4 : 1;
