@@ -21,11 +21,6 @@ namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float y;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
-}
 
 struct RowPlace { int seq, first, n, ctx; };      // a prompt, its first row, its new rows, its slots in use
 __device__ __forceinline__ RowPlace place_from(const NewRows& r, int seq, int first, int last, int ctx) {
@@ -87,26 +82,14 @@ __device__ __forceinline__ RowPlace owner_of(const NewRows& r, int row) {
 
 // Two floats, for the packed instructions.
 struct Two { uint64_t v; };
-__device__ __forceinline__ Two two(float a, float b) {
-  Two r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
+__device__ __forceinline__ Two two(float a, float b) { return Two{pack_f32x2(a, b)}; }
 __device__ __forceinline__ float2 floats(Two x) {
   float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+  unpack_f32x2(x.v, r.x, r.y);
   return r;
 }
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
+__device__ __forceinline__ Two operator*(Two a, Two b) { return Two{mul_f32x2(a.v, b.v)}; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { return Two{fma_f32x2(a.v, b.v, c.v)}; }
 
 // A lane's part of a row of one head: eight elements from 8 l on, and the eight behind the half that they are turned with; l: lane within the
 // row's D / 16.

@@ -171,41 +171,7 @@ __device__ __forceinline__ bool next_item(Cursor& cur, const Tree8Params& a, Ite
   return true;
 }
 
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack_out(float a, float b) {
-  if constexpr (BF16) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t*>(&v);
-  } else {
-    const uint32_t lo = __half_as_ushort(isinf(a) ? __float2half_rn(a) : to_half_sat(a));
-    const uint32_t hi = __half_as_ushort(isinf(b) ? __float2half_rn(b) : to_half_sat(b));
-    return lo | (hi << 16);
-  }
-}
-
-// Per-column reduction over the warp's 32 lanes, transposing as it goes: every step exchanges half of the columns that are left
-// with the lane across and combines the other half.  Lane l returns column l % NC.
-template <int NC, typename Op>
-__device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
-  const int lane = threadIdx.x & 31;
-  float v[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) v[c] = in[c];
-#pragma unroll
-  for (int h = NC / 2; h >= 1; h >>= 1) {
-    const bool hi = (lane & h) != 0;
-#pragma unroll
-    for (int e = 0; e < h; ++e) {
-      const float other = __shfl_xor_sync(0xffffffffu, hi ? v[e] : v[e + h], h);
-      v[e] = op(hi ? v[e + h] : v[e], other);
-    }
-  }
-  float x = v[0];
-#pragma unroll
-  for (int h = NC; h < 32; h <<= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, h));
-  return x;
-}
-// The same, where the first four columns may be all that counts.
+// A sum or maximum of every column by the warp, where the first four columns may be all that counts.
 template <int NC, typename Op>
 __device__ __forceinline__ float column_reduce(const float (&in)[NC], int n_rows, Op op) {
   if (n_rows > 4) return column_reduce<NC>(in, op);
@@ -217,15 +183,6 @@ __device__ __forceinline__ float warp_max(float x) {
   float y;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
-}
-// OR of a predicate over the 128 threads of a block parity.
-__device__ __forceinline__ bool parity_any(int i, bool x) {
-  uint32_t y;
-  if (i == 0)
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
-  else
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
-  return y != 0;
 }
 // NaN if a drafted V element (slots s .. end - 1) that a row sees is NaN: it was taken out of the product.
 template <int D>

@@ -25,25 +25,6 @@ constexpr int NC = NARROW_ROWS;                  // columns of the products
 // 4 / 5 / 6: 108.3 / 110.7 / 115.5.  (What is asked for too early comes in the way of what the other SMs wait for.)
 constexpr int RING_BYTES = 128 * 1024;
 
-// Per-column reduction over the warp's 32 lanes, transposing as it goes: every step exchanges half of the columns that are left
-// with the lane across and combines the other half, so NC columns cost about NC shuffles.  Lane l returns column l % NC.
-template <typename Op>
-__device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
-  const int lane = threadIdx.x & 31;
-  float v[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) v[c] = in[c];
-#pragma unroll
-  for (int h = NC / 2; h >= 1; h >>= 1) {
-    const bool hi = (lane & h) != 0;
-#pragma unroll
-    for (int e = 0; e < h; ++e) {
-      const float other = __shfl_xor_sync(0xffffffffu, hi ? v[e] : v[e + h], h);
-      v[e] = op(hi ? v[e + h] : v[e], other);
-    }
-  }
-  return op(v[0], __shfl_xor_sync(0xffffffffu, v[0], 16));
-}
 // What the drafted V elements that are not finite (slots s .. end - 1) add to an output element of a row: they were taken out
 // of the product.
 template <bool BF16>
@@ -58,15 +39,6 @@ __device__ __noinline__ float bad_v_sum(const TreeParams& a, int seq, int ctx_le
     if (!isfinite(x)) o += x;
   }
   return o;
-}
-// OR of a predicate over the 128 threads of a block parity.
-__device__ __forceinline__ bool parity_any(int i, bool x) {
-  uint32_t y;
-  if (i == 0)
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
-  else
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
-  return y != 0;
 }
 template <int D>
 constexpr int narrow_smem() { return 1024 + RING_BYTES + 2 * NC * D * 2 + 2 * NC * BLK * 2; }

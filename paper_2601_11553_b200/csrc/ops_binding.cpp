@@ -109,8 +109,8 @@ int strides_of(PyObject* x, int64_t (&out)[N]) {
   const Ref r(PyObject_CallMethodNoArgs(x, n_stride));
   return numbers(r.p, out);
 }
-// What a tensor is.  DLPack's description (a public, stable layout: the parts of it used here are restated) comes in one call where the tensor can be
-// asked for it (not one that requires a gradient, say); its Python attributes take five: a fork of one prompt to four samples, 17 tensors, is the
+// What a tensor is.  DLPack's description (a public, stable layout: the parts of it used here are restated) comes in one call where torch gives one
+// and its type and device are among those told apart here; its Python attributes take five: a fork of one prompt to four samples, 17 tensors, is the
 // host's 13 us that way.
 constexpr int MOST = 8;                         // sizes
 struct Info {

@@ -68,22 +68,6 @@ __device__ __forceinline__ uint32_t slot_bits(const TreeRows& r, const Item& it,
   return (in_ctx > 0 ? (1u << in_ctx) - 1 : 0u) | node_bits(r, row, node, it.n_nodes, -in_ctx);
 }
 
-// Two values in the pools' type.  A finite value past fp16's range (an average of values at its limit, rounded up) becomes the
-// largest finite one; infinity stays infinity.
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack_out(float a, float b) {
-  if constexpr (BF16) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t*>(&v);
-  } else {
-    if (isinf(a) || isinf(b)) {
-      const uint32_t lo = __half_as_ushort(isinf(a) ? __float2half_rn(a) : to_half_sat(a));
-      const uint32_t hi = __half_as_ushort(isinf(b) ? __float2half_rn(b) : to_half_sat(b));
-      return lo | (hi << 16);
-    }
-    return pack_half2(a, b);
-  }
-}
 template <bool BF16>
 __device__ __forceinline__ float elem(uint32_t bits16) {
   if constexpr (BF16) return __uint_as_float(bits16 << 16);

@@ -22,34 +22,6 @@ __device__ __forceinline__ float fast_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float y;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
-}
-__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 
 // Bounded wait for kernels with many wait sites.  A wait site in line is a dozen instructions; the timed loop of mbar_wait (with its
 // error word) is one function of the kernel, entered by waits that take long.  Instruction fetches are what a small call's time
@@ -232,6 +204,54 @@ struct Cursor {
     return false;
   }
 };
+
+// Per-column reduction over the warp's 32 lanes, transposing as it goes: every step exchanges half of the columns that are left
+// with the lane across and combines the other half, so NC columns cost about NC shuffles.  Lane l returns column l % NC.
+template <int NC, typename Op>
+__device__ __forceinline__ float column_reduce(const float (&in)[NC], Op op) {
+  const int lane = threadIdx.x & 31;
+  float v[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) v[c] = in[c];
+#pragma unroll
+  for (int h = NC / 2; h >= 1; h >>= 1) {
+    const bool hi = (lane & h) != 0;
+#pragma unroll
+    for (int e = 0; e < h; ++e) {
+      const float other = __shfl_xor_sync(0xffffffffu, hi ? v[e] : v[e + h], h);
+      v[e] = op(hi ? v[e + h] : v[e], other);
+    }
+  }
+  float x = v[0];
+#pragma unroll
+  for (int h = NC; h < 32; h <<= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, h));
+  return x;
+}
+// OR of a predicate over the 128 threads of a block parity.
+__device__ __forceinline__ bool parity_any(int i, bool x) {
+  uint32_t y;
+  if (i == 0)
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
+  else
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n" : "=r"(y) : "r"(static_cast<uint32_t>(x)) : "memory");
+  return y != 0;
+}
+// Two values in the pools' type.  A finite value past fp16's range (an average of values at its limit, rounded up) becomes the
+// largest finite one; infinity stays infinity.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_out(float a, float b) {
+  if constexpr (BF16) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&v);
+  } else {
+    if (isinf(a) || isinf(b)) {
+      const uint32_t lo = __half_as_ushort(isinf(a) ? __float2half_rn(a) : to_half_sat(a));
+      const uint32_t hi = __half_as_ushort(isinf(b) ? __float2half_rn(b) : to_half_sat(b));
+      return lo | (hi << 16);
+    }
+    return pack_half2(a, b);
+  }
+}
 
 // Bits of the nodes j0 .. j0 + 31 (j0 may be negative) that a node sees.
 __device__ __forceinline__ uint32_t node_bits(const TreeRows& r, int row, int node, int n_nodes, int j0) {
