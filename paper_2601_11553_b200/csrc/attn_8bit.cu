@@ -15,7 +15,7 @@
 //
 // Bound by HBM: 2 D bytes a slot and KV head.  Measured (bf16, the chains fp16; head size 128, 8 KV heads): one token on each of 64 prompts around 2500 slots 62 us (329 MB,
 // 5.3 TB/s; the blocks run at the HBM's rate, the rest is the start, uneven ends and the merge), chains of 7 with four heads a KV head on 2 x 33024
-// slots 38.2 us (136 MB; with fp16's weights off by 2^-12 37.2), trees of 26 with two heads a KV head 122 us (339 MB; every prompt has one or two tiles of up to 32 rows, whose softmax
+// slots 37.8 us (136 MB; with fp16's weights off by 2^-12 37.0), trees of 26 with two heads a KV head 121 us, fp16 155 (339 MB; every prompt has one or two tiles of up to 32 rows, whose softmax
 // takes 0.53 - 0.78 us a block), one token on 512 slots 7.6 us (latency).  One copy per page fetches keys and values of a head: a box of [row group][K, V][8 rows][D
 // bytes], so that the row groups of K, and those of V, are one stride apart over all pages of a block.
 // Warps 0-7: softmax (even and odd blocks), 8: copies, 9: S products, 10: O products, 11: splits Q, fetches masks, cleans V.  With one warp for
@@ -89,40 +89,32 @@ template <int NC, bool BF16> struct Parts {
 };
 
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
-// To bytes of 5 exponent bits and 2 mantissa bits, to nearest even, and back: such a byte is a half's upper one.
-__device__ __forceinline__ uint32_t e5m2x2_of(__half2 x) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<const uint32_t*>(&x)));
-  return r;
-}
-__device__ __forceinline__ uint32_t e5m2x2_of(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ __half2 half2_of(uint32_t e5m2x2) { return as_half2(__byte_perm(e5m2x2, 0u, 0x1404)); }
-// The parts of two weights (at most 2^15), 16 bits each.  What a part leaves is at most 2^11 and exact in a half, also as 16 times as much: a
-// multiple of the last bit.  bf16 takes the weight as a half, whose own rounding (2^-12 of the next power of two) is less than the parts'; fp16's four keep
-// more, so its first part is the weight's itself and the half is what that leaves.
+// A number of 5 exponent bits and 2 mantissa bits is a half's upper byte.  Two halves rounded to such numbers, to nearest, ties away from zero.  (NaN becomes
+// zero here; the row sum has it, by which all of the row is divided.)  By conversions, fp16 trees of 26 on 64 x 2500 slots take 163 us, so 158.
+__device__ __forceinline__ uint32_t upper_bytes(uint32_t h) { return (h + 0x00800080u) & 0xff00ff00u; }
+__device__ __forceinline__ uint32_t bits_of(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+// The parts of two weights (at most 2^15), two halves each whose upper bytes count.  What a part leaves is at most 2^11 and exact in a half, also as 16
+// times as much: a multiple of the last bit.  bf16 takes the weight as a half, whose own rounding (2^-12 of the next power of two) is less than the parts'; fp16's
+// four keep more, so what its first part leaves is taken from the weight itself.
 template <typename X, bool BF16>
 __device__ __forceinline__ void split_weights(float w0, float w1, uint32_t (&out)[X::P]) {
   const __half2 sixteen = __float2half2_rn(16.f);
-  __half2 r;
+  __half2 r = __floats2half2_rn(w0, w1);
+  out[0] = upper_bytes(bits_of(r));
   if constexpr (BF16) {
-    r = __floats2half2_rn(w0, w1);
-    out[0] = e5m2x2_of(r);
-    r = __hmul2(__hsub2(r, half2_of(out[0])), sixteen);
+    r = __hmul2(__hsub2(r, as_half2(out[0])), sixteen);
   } else {
-    out[0] = e5m2x2_of(w0, w1);
-    const float2 f = __half22float2(half2_of(out[0]));
     float r0, r1;
-    unpack_f32x2(fma_f32x2(pack_f32x2(f.x, f.y), pack_f32x2(-16.f, -16.f), mul_f32x2(pack_f32x2(w0, w1), pack_f32x2(16.f, 16.f))), r0, r1);
+    unpack_f32x2(mul_f32x2(pack_f32x2(w0, w1), pack_f32x2(16.f, 16.f)), r0, r1);
+    // less 16 times (0xcc00 is -16) the part, fp32 from halves
+    asm("{\n .reg .b16 lo, hi, m;\n mov.b32 {lo, hi}, %2;\n mov.b16 m, 0xcc00;\n fma.rn.f32.f16 %0, lo, m, %0;\n fma.rn.f32.f16 %1, hi, m, %1;\n}\n"
+        : "+f"(r0), "+f"(r1) : "r"(out[0]));
     r = __floats2half2_rn(r0, r1);
   }
 #pragma unroll
   for (int part = 1; part < X::P; ++part) {
-    out[part] = e5m2x2_of(r);
-    if (part + 1 < X::P) r = __hmul2(__hsub2(r, half2_of(out[part])), sixteen);
+    out[part] = upper_bytes(bits_of(r));
+    if (part + 1 < X::P) r = __hmul2(__hsub2(r, as_half2(out[part])), sixteen);
   }
 }
 
@@ -715,7 +707,7 @@ attention_8bit_kernel(const __grid_constant__ CUtensorMap tm, const __grid_const
 #pragma unroll
               for (int e = 0; e < X::P; ++e) {
                 const int lo = 2 * e, hi = 2 * e + 1;
-                w[c * X::P / 4 + e] = two[lo / X::P][lo % X::P] | two[hi / X::P][hi % X::P] << 16;
+                w[c * X::P / 4 + e] = __byte_perm(two[lo / X::P][lo % X::P], two[hi / X::P][hi % X::P], 0x7531);
               }
             }
 #pragma unroll
