@@ -120,10 +120,11 @@ bool rows16_ok(const void* p, int64_t stride, int32_t heads, int32_t dim) {
 
 // Whether two sets of rows of 16-bit elements, of `a_dim` and `b_dim` elements each, share none.  Rows side by side have one stride.
 bool rows_apart(const void* a, int64_t a_stride, int64_t a_dim, const void* b, int64_t b_stride, int64_t b_dim, int64_t n) {
-  const int64_t x = reinterpret_cast<intptr_t>(a), y = reinterpret_cast<intptr_t>(b), as = a_stride * 2, bs = b_stride * 2, aw = a_dim * 2, bw = b_dim * 2;
+  using Wide = __int128;                        // strides are bounded, but not by any real memory
+  const Wide x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b), as = a_stride * 2, bs = b_stride * 2, aw = a_dim * 2, bw = b_dim * 2;
   if (x + (n - 1) * as + aw <= y || y + (n - 1) * bs + bw <= x) return true;
   if (as != bs) return false;
-  const int64_t d = ((y - x) % as + as) % as;
+  const Wide d = ((y - x) % as + as) % as;
   return d >= aw && d + bw <= as;
 }
 
