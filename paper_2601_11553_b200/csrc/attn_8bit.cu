@@ -151,7 +151,7 @@ struct Item {
 template <int NC>
 __device__ __forceinline__ bool next_item(Cursor& cur, const Tree8Params& a, Item* it) {
   Piece pc;
-  if (!cur.next(a.rows, [&](const SeqPart& p) { return shape8<NC>(a, p); }, &pc)) return false;
+  if (!cur.next<NC == 16>(a.rows, [&](const SeqPart& p) { return shape8<NC>(a, p); }, &pc)) return false;
   // the tiles of one KV head follow each other: they share K and V in L2
   const int flat = pc.part.n_nodes * a.group, tiles = (flat + NC - 1) / NC, tile = pc.unit % tiles;
   it->seq = pc.seq; it->ctx_len = pc.part.ctx_len; it->n_nodes = pc.part.n_nodes; it->row0 = pc.part.row0;
