@@ -593,12 +593,15 @@ PERCACHE_API int percache_append_rows_8bit(int32_t device, void* stream, const p
 
 /* percache_tree_attention over 8-bit pages: out = softmax(scale * q . K) V, lse, masks and rows that see nothing as there, with at
  * most 128 query heads per KV head.  Products are formed on the 8-bit values themselves, with q and the weights as sums of 8-bit
- * numbers, accumulated in fp32.  q is exact, but for elements below 2^-13 of the row's largest with bf16, 2^-14 with fp16, which are off by up to 2^-21
- * and 2^-25 of that (or, in rows below 2^-92, by up to 2^-114).  A weight times its page's V scale is off by up to 2^-11 of itself with bf16, 2^-15 with fp16; those below 2^-21 of the
- * row's largest such product by up to 2^-32 and 2^-36 of that instead.  (The largest counts whatever its slot's bytes are: beside a page
- * whose V scale is 2^30 times the others', but whose bytes are zeros, what the others add has few bits left.)  lse has the weights before
- * that.  Scales below 2^-32 (and NaN) count as 2^-32, above 2^32 as
- * 2^32; pages outside the pool hold zeros.  A q that holds infinity or NaN gives NaN. */
+ * numbers, accumulated in fp32.
+ *  - q is exact, but for elements below 2^-13 of the row's largest with bf16, 2^-14 with fp16, which are off by up to 2^-21 and
+ *    2^-25 of that (in rows below 2^-92 by up to 2^-114).
+ *  - A weight times its page's V scale is off by up to 2^-11 of itself with bf16, 2^-15 with fp16; those below 2^-21 of the row's
+ *    largest such product by up to 2^-32 and 2^-36 of that instead.  (The largest counts whatever its slot's bytes are: beside a
+ *    page whose V scale is 2^30 times the others', but whose bytes are zeros, what the others add has few bits left.)  lse has the
+ *    weights before that.
+ *  - Scales below 2^-32 (and NaN) count as 2^-32, above 2^32 as 2^32; pages outside the pool hold zeros.
+ * A q that holds infinity or NaN gives NaN. */
 PERCACHE_API int percache_tree_attention_8bit(int32_t device, void* stream, const percache_kv8_t* kv, const percache_rows_t* rows,
                                               const void* q, int64_t q_row_stride, int32_t n_q_heads, float scale, void* out,
                                               int64_t out_row_stride, float* lse, void* workspace, int64_t workspace_bytes);
